@@ -164,7 +164,7 @@ def _plain_lora(s):
     place = (lo[:, None] + at[None, :]).clamp(max=case["tokens"] - 1)
     xe, de = torch.where(live, x[place], 0.0), torch.where(live, dy[place], 0.0)       # [examples, longest, width]
     u = s["scaling"] * (de @ b)
-    h = xe @ a.T
+    h = s["scaling"] * (xe @ a.T)
     da, db = u.transpose(1, 2) @ xe, de.transpose(1, 2) @ h
     return torch.cat([da.flatten(1), db.flatten(1)], dim=1).to(_torch_type(case["dtype"]))
 
@@ -266,7 +266,7 @@ def exact(case, seed):
             x = s["codes"][lo:hi].double() * step[:, channel]
             dy = s["grad_out"][lo:hi].double()
             rows[e, :r * wi] = torch.einsum("tr,tc->rc", s["scaling"] * (dy @ b), x).reshape(-1)
-            rows[e, r * wi:] = torch.einsum("to,tr->or", dy, torch.einsum("tc,rc->tr", x, a)).reshape(-1)
+            rows[e, r * wi:] = s["scaling"] * torch.einsum("to,tr->or", dy, torch.einsum("tc,rc->tr", x, a)).reshape(-1)
         return rows
     t, h, v = case["tokens"], case["width"], case["vocab"]
     keep = torch.nonzero(s["labels"] >= 0)[:, 0]
