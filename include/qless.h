@@ -360,6 +360,52 @@ qless_status qless_select_topk_static(
     const float* scores, int64_t N, double frac, int64_t* indices, int64_t* k_out /* host */,
     void* cuda_stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Before stage 1: the gradient rows themselves. The paper takes per-example gradients of the LoRA
+ * parameters (Sec. 2.2) as given; the calls below compute them for one adapted layer from the
+ * gradient at its output and an 8-bit copy of its input, and the loss that starts the backward pass.
+ *
+ * 8-bit activation checkpoints. x [tokens, width] (ld_x elements per row) is cut into groups of
+ * `group` channels (32, 64 or 128; the last group of a row may be short). Per group:
+ *   a = max |x|;  e = the smallest integer with a <= 127 * 2^e, kept within [-120, 121];
+ *   code = round_half_even(x / 2^e) (clamped to +-127, which acts only where a > 127 * 2^121);
+ *   scale byte = e + 127; 0xFF and codes 0 where the group holds an infinity or a NaN.
+ * The value that a code stands for, code * 2^(byte - 127) (NaN for byte 0xFF), is exact in bf16 and fp32.
+ *   codes  int8 [tokens, width], ld_codes bytes per row;  scales uint8 [tokens, ceil(width / group)],
+ *   ld_scales bytes per row.
+ * qless_activation_dequantize writes those values, x [tokens, width] of `dtype`, ld_x elements per row.
+ * Any tokens >= 0 and width >= 1; rows need no alignment beyond that of their element type (16-byte
+ * aligned x rows and 8-byte aligned code rows are read and written in vectors, others element by element).
+ * No workspace. */
+qless_status qless_activation_quantize(const void* x, qless_dtype dtype, int64_t tokens, int32_t width, int64_t ld_x, int32_t group,
+                                       int8_t* codes, int64_t ld_codes, uint8_t* scales, int64_t ld_scales, void* cuda_stream);
+
+qless_status qless_activation_dequantize(const int8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales,
+                                         int64_t tokens, int32_t width, int32_t group, void* x, qless_dtype dtype, int64_t ld_x,
+                                         void* cuda_stream);
+
+/* Per-example gradients of the LoRA parameters of one layer y = W x + scaling * B (A x), A = lora_a [rank, in],
+ * B = lora_b [out, rank] (bf16, contiguous), from the checkpointed input (codes, scales: as above, width = in) and
+ * the gradient at y, grad_out [tokens, out] bf16 (ld_grad_out elements per row). The tokens of all examples are packed:
+ * example e owns rows offsets[e] .. offsets[e+1]-1 (offsets: HOST array [n+1], offsets[0] >= 0, non-decreasing,
+ * offsets[n] <= tokens; rows outside are not part of any example). With x^ the checkpointed values:
+ *   U = scaling * grad_out B,  H = scaling * x^ A^T;   dA_e = U_e^T x^_e,  dB_e = grad_out_e^T H_e
+ *   grads row e (ld_grads elements per row) = [ dA_e row-major [rank, in] | dB_e row-major [out, rank] ],
+ * rank * (in + out) elements of `dtype`. Rows of several layers are put side by side by passing grads + column offset:
+ * the result is the [n, P] matrix that qless_project_quantize reads. An empty example gives zeros; an infinity or NaN in
+ * one example's tokens reaches that example's row only. Sums are fp32; U and H are handed to the second product as sums of
+ * two (bf16 gradients) or three (fp32 gradients) bf16 terms, so that they keep 16 or 24 bits. The same inputs give the
+ * same bits (no float atomics).
+ * Requirements: tokens < 2^31; n < 2^31; in and out multiples of 16, at most 2^20; rank a multiple of 8, 8 <= rank <= 128;
+ * codes, grad_out, lora_a, lora_b, grads 16-byte aligned; ld_codes % 16 == 0; ld_grad_out % 8 == 0; ld_grads % 8 == 0. */
+size_t qless_lora_gradients_workspace(int64_t tokens, int64_t n, int32_t in, int32_t out, int32_t rank, qless_dtype dtype);
+
+qless_status qless_lora_gradients(const int8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales, int32_t group,
+                                  const void* grad_out, int64_t ld_grad_out, const void* lora_a, const void* lora_b,
+                                  const int64_t* offsets /* host */, int64_t tokens, int64_t n, int32_t in, int32_t out,
+                                  int32_t rank, float scaling, void* grads, qless_dtype dtype, int64_t ld_grads,
+                                  void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

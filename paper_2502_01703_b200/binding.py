@@ -26,6 +26,7 @@ EXPORTS = [
     "qless_profile_collect", "qless_kernel_launches", "qless_select_topk_static",
     "qless_set_projection_path", "qless_set_score_path", "qless_set_select_path", "qless_microbench",
     "qless_project_quantize_ex", "qless_project_quantize_host_ex", "qless_gaussian_entries", "qless_selftest_timeout",
+    "qless_activation_quantize", "qless_activation_dequantize", "qless_lora_gradients_workspace", "qless_lora_gradients",
 ]
 RADEMACHER, GAUSSIAN = 0, 1
 SELECT_STATIC_MAX_N = 1 << 22
@@ -125,6 +126,15 @@ def lib():
         L.qless_gaussian_entries.argtypes = [C.c_uint64, i64, i64, i64, i64, vp, vp]
         L.qless_select_topk_static.restype = C.c_int
         L.qless_select_topk_static.argtypes = [vp, i64, C.c_double, vp, C.POINTER(i64), vp]
+        L.qless_activation_quantize.restype = C.c_int
+        L.qless_activation_quantize.argtypes = [vp, C.c_int, i64, i32, i64, i32, vp, i64, vp, i64, vp]
+        L.qless_activation_dequantize.restype = C.c_int
+        L.qless_activation_dequantize.argtypes = [vp, i64, vp, i64, i64, i32, i32, vp, C.c_int, i64, vp]
+        L.qless_lora_gradients_workspace.restype = sz
+        L.qless_lora_gradients_workspace.argtypes = [i64, i64, i32, i32, i32, C.c_int]
+        L.qless_lora_gradients.restype = C.c_int
+        L.qless_lora_gradients.argtypes = [vp, i64, vp, i64, i32, vp, i64, vp, vp, vp, i64, i64, i32, i32, i32, C.c_float, vp, C.c_int,
+                                           i64, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -413,6 +423,79 @@ def qless_select_topk_static(scores, frac, indices, stream=None):
     _check(lib().qless_select_topk_static(_ptr(scores), scores.numel(), float(frac), _ptr(indices), C.byref(k),
                                           _stream(stream)))
     return indices[:k.value]
+
+
+def _row_stride(t):
+    """Elements between rows of a 2-D tensor whose rows are contiguous."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("a 2-D tensor with contiguous rows is required")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _dtype_of(dtype):
+    if dtype == torch.float32:
+        return F32
+    if dtype == torch.bfloat16:
+        return BF16
+    raise TypeError("float32 or bfloat16 is required")
+
+
+def qless_activation_quantize(x, group=32, codes=None, scales=None, stream=None):
+    """x f32/bf16 [tokens, width] (row stride allowed) -> (codes int8 [tokens, width], scales uint8
+    [tokens, ceil(width / group)]): the 8-bit checkpoint of a layer's input, one power-of-two step per group of channels."""
+    T, width = x.shape
+    if codes is None:
+        codes = torch.empty((T, width), dtype=torch.int8, device=x.device)
+    if scales is None:
+        scales = torch.empty((T, -(-width // max(int(group), 1))), dtype=torch.uint8, device=x.device)
+    _check(lib().qless_activation_quantize(_ptr(x), _dtype_code(x), T, width, _row_stride(x), group, _ptr(codes), _row_stride(codes),
+                                           _ptr(scales), _row_stride(scales), _stream(stream)))
+    return codes, scales
+
+
+def qless_activation_dequantize(codes, scales, group=32, dtype=torch.bfloat16, out=None, stream=None):
+    """The values that a checkpoint's codes stand for, [tokens, width] of `dtype` (exact in both types)."""
+    T, width = codes.shape
+    if out is None:
+        out = torch.empty((T, width), dtype=dtype, device=codes.device)
+    _check(lib().qless_activation_dequantize(_ptr(codes), _row_stride(codes), _ptr(scales), _row_stride(scales), T, width, group,
+                                             _ptr(out), _dtype_code(out), _row_stride(out), _stream(stream)))
+    return out
+
+
+def qless_lora_gradients_workspace(tokens, n, width_in, width_out, rank, dtype=torch.bfloat16):
+    return int(lib().qless_lora_gradients_workspace(tokens, n, width_in, width_out, rank, _dtype_of(dtype)))
+
+
+def qless_lora_gradients(codes, scales, grad_out, lora_a, lora_b, offsets, scaling=1.0, group=32, grads=None, dtype=torch.bfloat16,
+                         workspace=None, stream=None):
+    """Per-example LoRA gradients of one layer from its 8-bit input checkpoint: codes int8 [tokens, in], scales uint8,
+    grad_out bf16 [tokens, out], lora_a bf16 [rank, in], lora_b bf16 [out, rank]; offsets: int64 CPU tensor (or sequence)
+    [n + 1] of the examples' first tokens. Returns grads [n, rank * (in + out)], rows [dA | dB]; `grads` may be a column
+    slice of a wider [n, P] matrix."""
+    off = offsets if torch.is_tensor(offsets) else torch.tensor(list(offsets), dtype=torch.int64)
+    if off.device.type != "cpu" or off.dtype != torch.int64 or not off.is_contiguous():
+        raise TypeError("offsets must be a contiguous int64 tensor in host memory")
+    if grad_out.dtype != torch.bfloat16 or lora_a.dtype != torch.bfloat16 or lora_b.dtype != torch.bfloat16:
+        raise TypeError("grad_out, lora_a and lora_b must be bfloat16")
+    if codes.dtype != torch.int8 or scales.dtype != torch.uint8:
+        raise TypeError("codes must be int8 and scales uint8")
+    T, wi = codes.shape
+    rank, wo = lora_a.shape[0], lora_b.shape[0]
+    n = off.numel() - 1
+    if grad_out.shape != (T, wo) or lora_a.shape[1] != wi or lora_b.shape[1] != rank or scales.shape != (T, -(-wi // max(int(group), 1))):
+        raise ValueError("shapes of codes, scales, grad_out, lora_a and lora_b do not fit together")
+    if not lora_a.is_contiguous() or not lora_b.is_contiguous():
+        raise ValueError("lora_a and lora_b must be contiguous")
+    if grads is None:
+        grads = torch.empty((n, rank * (wi + wo)), dtype=dtype, device=codes.device)
+    elif grads.shape != (n, rank * (wi + wo)):
+        raise ValueError("grads must be [n, rank * (in + out)]")
+    ws = _workspace(qless_lora_gradients_workspace(T, n, wi, wo, rank, grads.dtype), codes.device, workspace)
+    _check(lib().qless_lora_gradients(_ptr(codes), _row_stride(codes), _ptr(scales), _row_stride(scales), group, _ptr(grad_out),
+                                      _row_stride(grad_out), _ptr(lora_a), _ptr(lora_b), _ptr(off), T, n, wi, wo, rank, scaling,
+                                      _ptr(grads), _dtype_code(grads), _row_stride(grads), _ptr(ws), ws.numel(), _stream(stream)))
+    return grads
 
 
 def qless_set_projection_path(path):

@@ -1,0 +1,693 @@
+// Per-example LoRA gradients from 8-bit activation checkpoints.
+//
+//   layer: y = W x + s B A x, A [r, in], B [out, r].  With dY the gradient at y and x^ = code * 2^(step - 127):
+//     U = s dY B  [T, r],   H = s x^ A^T  [T, r]                         (1) factors: one row per token
+//     dA_e = U_e^T x^_e  [r, in],   dB_e = dY_e^T H_e  [out, r]          (2) outer products: sums over the tokens of example e
+//   row e of the gradient matrix = [dA_e row-major | dB_e row-major].
+//
+// Both steps read x^ and dY once and do 2 r multiply-adds per element read: memory-bound work on the tensor cores.
+// (1) lora_factors_kernel: M = 128 tokens, K = channels. The codes go TMA -> shared memory -> registers -> tensor memory as bf16
+//     (exact: a code has 8 significant bits and the step is a power of two), from where the MMA takes its A operand; dY goes TMA ->
+//     MMA as stored. fp32 sums over a slice of the channels; lora_split_kernel adds the slices.
+// (2) lora_outer_kernel: M = 256 channels (two accumulators of 128 that share the factor operand), K = the tokens of one chunk of an
+//     example, N = r. dY feeds the MMA as stored (channel-major A operand); the codes are expanded to bf16 in shared memory in the
+//     layout such an operand has. The factors U and H are fp32 sums; a bf16 operand would cut them to 8 bits, so each is split into
+//     `parts` bf16 terms (2 terms: 16 bits, for bf16 gradients; 3 terms: 24 bits, for fp32 gradients) and the products of all terms
+//     are added in the same fp32 accumulator.
+// Tokens behind the end of a chunk share its last 64-token block: their rows are overwritten with zeros in both operands (in the
+// operand alone a NaN in the neighbour example would survive as 0 * NaN).
+// Examples longer than a chunk are summed in pieces (fp32, added in piece order by lora_join_kernel): no float atomics anywhere.
+#include "qless_kernels.h"
+#include "tc_common.cuh"
+
+namespace qless {
+
+namespace {
+
+using namespace tc;
+
+constexpr int NTHREADS = 448;               // warp 0 TMA, warp 1 MMA, warps 2-9 converters, warps 10-13 epilogue
+constexpr int MAX_STAGES = 4;
+constexpr int BIG = 32768;                  // operand bytes of one stage that come from the activations or dY
+constexpr int CH = 128;                     // (1) channels per stage
+constexpr int TOK = 64;                     // (2) tokens per stage
+constexpr int TILE = 256;                   // (2) channels per item
+
+struct FactorParams {
+    int64_t T, ld_scales;
+    const uint8_t* scales;
+    float* part;                            // [2][slices][T][N64]: 0 = H, 1 = U
+    int32_t in, out, group, nr, n64, slices, kb_x, kb_y, stages;      // kb_*: channel blocks per slice
+    int32_t token_tiles;
+    int64_t items;
+    unsigned int* timeout_word;
+};
+
+struct OuterParams {
+    const LoraChunk* chunks;
+    const uint8_t* scales;
+    int64_t ld_scales, ld_grads, items;
+    void* grads;
+    float* part;                            // [slots][rank * (in + out)]
+    int32_t in, out, rank, group, nr, n64, parts, tiles_x, tiles, stages;
+    unsigned int* timeout_word;
+};
+
+struct __align__(8) Bars {
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES], ready[2], conv_empty[2], d_full[2], d_empty[2], drain;
+    uint32_t tmem_base, abort_flag;
+};
+
+struct Ring {
+    uint32_t slot = 0, parity = 0;
+    __device__ __forceinline__ void next(uint32_t n) { if (++slot == n) { slot = 0; parity ^= 1u; } }
+};
+
+// Four codes -> four bf16 values code * 2^(step - 127). A byte under 0x43 is the bf16 number 128 + (low seven bits); taking
+// away 128, or 256 where the sign bit is set, leaves the code exactly, and so does the product with a power of two.
+__device__ __forceinline__ uint32_t codes_to_bf16x2(uint32_t pair, uint32_t step2)
+{
+    const uint32_t mag = pair & 0xFF7FFF7Fu, off = pair & 0xFF80FF80u;
+    const __nv_bfloat162 v = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&mag), *reinterpret_cast<const __nv_bfloat162*>(&off)),
+                                     *reinterpret_cast<const __nv_bfloat162*>(&step2));
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ void expand4(uint32_t w, uint32_t step2, uint32_t& lo, uint32_t& hi)
+{
+    lo = codes_to_bf16x2(__byte_perm(w, 0x43434343u, 0x4140), step2);
+    hi = codes_to_bf16x2(__byte_perm(w, 0x43434343u, 0x4342), step2);
+}
+__device__ __forceinline__ uint32_t step_bf16x2(uint32_t byte) { return (byte << 7) | (byte << 23); }      // 0xFF: infinity, and 0 * infinity = NaN
+
+__device__ __forceinline__ void init_barriers(Bars* b, int ready_count)
+{
+    for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(smem_u32(&b->full[s]), 1); mbar_init(smem_u32(&b->empty[s]), 1); }
+    for (int s = 0; s < 2; ++s) {
+        mbar_init(smem_u32(&b->ready[s]), ready_count);
+        mbar_init(smem_u32(&b->conv_empty[s]), 1);
+        mbar_init(smem_u32(&b->d_full[s]), 1);
+        mbar_init(smem_u32(&b->d_empty[s]), 4);
+    }
+    mbar_init(smem_u32(&b->drain), 1);
+    b->abort_flag = 0;
+    fence_barrier_init();
+}
+
+// The producer leaves after a failed wait: copies 0 .. it-1 have been issued; give those that may still fly a bounded wait.
+__device__ __forceinline__ void drain_copies(Bars* b, uint32_t it, uint32_t stages)
+{
+    for (uint32_t j = (it > stages ? it - stages : 0u); j < it; ++j)
+        if (!mbar_wait_quiet(smem_u32(&b->full[j % stages]), (j / stages) & 1u)) break;
+}
+
+// ---- (1) factors -------------------------------------------------------------------------------------------------------
+
+__global__ void __launch_bounds__(NTHREADS, 1)
+lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_constant__ CUtensorMap tm_dy,
+                    const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const FactorParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const int op_bytes = p.n64 * 256;                       // factor operand of one stage: 128 channels x n64 (or n64 x 128)
+    const int stage_bytes = BIG + op_bytes;
+    Bars* bars = reinterpret_cast<Bars*>(smem + (size_t)p.stages * stage_bytes);
+    volatile uint32_t* abort_flag = &bars->abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t nS = (uint32_t)p.stages;
+
+    if (threadIdx.x == 0) {
+        init_barriers(bars, 4);
+        prefetch_tmap(&tm_codes); prefetch_tmap(&tm_dy); prefetch_tmap(&tm_a); prefetch_tmap(&tm_b);
+    }
+    if (warp == 1) { tmem_alloc(smem_u32(&bars->tmem_base), 512); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem_base;                  // accumulators at columns 0 and 128, expanded codes at 256 and 320
+
+    // item -> (slice, kind, token tile); kind 1 = dY first in every slice: its tiles are the larger ones
+    const int64_t per_slice = 2LL * p.token_tiles;
+    auto item_of = [&](int64_t item, int& slice, bool& is_x, int64_t& tile, int& kb0, int& kb1) {
+        slice = (int)(item / per_slice);
+        const int64_t r = item - slice * per_slice;
+        is_x = r >= p.token_tiles;
+        tile = is_x ? r - p.token_tiles : r;
+        const int all = ((is_x ? p.in : p.out) + CH - 1) / CH, step = is_x ? p.kb_x : p.kb_y;
+        kb0 = min(all, slice * step);
+        kb1 = min(all, kb0 + step);
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            Ring ring;
+            bool ok = true;
+            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+                int slice, kb0, kb1; bool is_x; int64_t tile;
+                item_of(item, slice, is_x, tile, kb0, kb1);
+                for (int kb = kb0; kb < kb1; ++kb, ++it, ring.next(nS)) {
+                    if (!mbar_wait(smem_u32(&bars->empty[ring.slot]), ring.parity ^ 1u, abort_flag, p.timeout_word, TO_PRODUCER)) { ok = false; break; }
+                    const uint32_t full = smem_u32(&bars->full[ring.slot]);
+                    const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
+                    if (is_x) {
+                        mbar_arrive_expect_tx(full, 128 * CH + 2 * p.nr * 128);
+                        tma_load_2d(big, &tm_codes, full, kb * CH, (int32_t)(tile * 128));
+                        tma_load_2d(op, &tm_a, full, kb * CH, 0);
+                        tma_load_2d(op + p.n64 * 128, &tm_a, full, kb * CH + 64, 0);
+                    } else {
+                        mbar_arrive_expect_tx(full, 2 * 128 * 128 + p.n64 * 256);
+                        tma_load_2d(big, &tm_dy, full, kb * CH, (int32_t)(tile * 128));
+                        tma_load_2d(big + 16384, &tm_dy, full, kb * CH + 64, (int32_t)(tile * 128));
+                        for (int j = 0; j < p.n64; j += 64) tma_load_2d(op + j * 256, &tm_b, full, j, kb * CH);
+                    }
+                }
+            }
+            if (!ok) drain_copies(bars, it, nS);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t idesc_x = make_idesc(1, 1, 1, 128, p.nr), idesc_y = idesc_x | IDESC_B_MN;
+            Ring ring, conv;
+            uint32_t n = 0;
+            bool ok = true;
+            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++n) {
+                int slice, kb0, kb1; bool is_x; int64_t tile;
+                item_of(item, slice, is_x, tile, kb0, kb1);
+                const uint32_t buf = n & 1u, d = tmem + buf * 128;
+                if (!mbar_wait(smem_u32(&bars->d_empty[buf]), ((n >> 1) & 1u) ^ 1u, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                tc_fence_after();
+                for (int kb = kb0; kb < kb1; ++kb, ring.next(nS)) {
+                    if (!mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                    const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
+                    if (is_x) {
+                        if (!mbar_wait(smem_u32(&bars->ready[conv.slot]), conv.parity, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t a = tmem + 256 + conv.slot * 64;
+#pragma unroll
+                        for (int k = 0; k < CH / 16; ++k)
+                            mma_f16_ts(d, a + k * 8, make_smem_desc_sw128(op + (k >> 2) * p.n64 * 128) + (uint64_t)((k & 3) * 2), idesc_x, kb > kb0 || k > 0);
+                        mma_commit(smem_u32(&bars->conv_empty[conv.slot]));
+                        conv.next(2);
+                    } else {
+                        tc_fence_after();
+#pragma unroll
+                        for (int k = 0; k < CH / 16; ++k)
+                            mma_f16_ss(d, make_smem_desc_sw128(big + (k >> 2) * 16384) + (uint64_t)((k & 3) * 2),
+                                       make_smem_desc_mn_sw128(op + k * 2048, 16384), idesc_y, kb > kb0 || k > 0);
+                    }
+                    mma_commit(smem_u32(&bars->empty[ring.slot]));
+                }
+                if (ok) mma_commit(smem_u32(&bars->d_full[buf]));
+            }
+            mma_commit(smem_u32(&bars->drain));               // every MMA issued above completes before tensor memory is freed
+            mbar_wait_quiet(smem_u32(&bars->drain), 0u);
+        }
+    } else if (warp < 10) {
+        // Converters: thread = token = TMEM lane; warps 2-5 and 6-9 take alternate blocks of codes.
+        const int row = (warp & 3) * 32 + lane;
+        const uint32_t grp = warp >= 6 ? 1u : 0u;
+        const int groups = (p.in + p.group - 1) / p.group;
+        Ring ring, conv;
+        bool ok = true;
+        for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            int slice, kb0, kb1; bool is_x; int64_t tile;
+            item_of(item, slice, is_x, tile, kb0, kb1);
+            if (!is_x) { for (int kb = kb0; kb < kb1; ++kb) ring.next(nS); continue; }
+            const int64_t t = tile * 128 + row;
+            const uint8_t* sc = p.scales + t * p.ld_scales;
+            for (int kb = kb0; kb < kb1 && ok; ++kb, ring.next(nS), conv.next(2)) {
+                if (conv.slot != grp) continue;
+                uint32_t step[4];                              // the 128 channels lie in 4, 2 or 1 groups
+                const int g0 = kb * CH / p.group, per = CH / p.group;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) step[i] = (t < p.T && i < per && g0 + i < groups) ? sc[g0 + i] : 0u;
+                ok = mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_UNPACK);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                const uint4* src = reinterpret_cast<const uint4*>(smem + (size_t)ring.slot * stage_bytes + row * CH);
+                uint4 raw[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) raw[j] = src[j ^ (row & 7)];
+                ok = mbar_wait(smem_u32(&bars->conv_empty[conv.slot]), conv.parity ^ 1u, abort_flag, p.timeout_word, TO_UNPACK);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t dst = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 256 + conv.slot * 64;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {                  // 32 channels: 16 tensor-memory columns of two bf16 each
+                    const uint32_t s2 = step_bf16x2(p.group == 32 ? step[q] : p.group == 64 ? step[q >> 1] : step[0]);
+                    uint32_t v[16];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint4 w = raw[2 * q + h];
+                        expand4(w.x, s2, v[8 * h + 0], v[8 * h + 1]);
+                        expand4(w.y, s2, v[8 * h + 2], v[8 * h + 3]);
+                        expand4(w.z, s2, v[8 * h + 4], v[8 * h + 5]);
+                        expand4(w.w, s2, v[8 * h + 6], v[8 * h + 7]);
+                    }
+                    tmem_st_x16(dst + 16 * q, v);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                fence_proxy_async_smem();                      // the raw codes were read through the generic proxy; TMA refills them
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars->ready[conv.slot]));
+            }
+        }
+    } else {
+        const int row = (warp & 3) * 32 + lane;
+        uint32_t n = 0;
+        for (int64_t item = blockIdx.x; item < p.items; item += gridDim.x, ++n) {
+            int slice, kb0, kb1; bool is_x; int64_t tile;
+            item_of(item, slice, is_x, tile, kb0, kb1);
+            const uint32_t buf = n & 1u;
+            bool ok = mbar_wait(smem_u32(&bars->d_full[buf]), (n >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            const int64_t t = tile * 128 + row;
+            float* dst = p.part + (((int64_t)(is_x ? 0 : 1) * p.slices + slice) * p.T + t) * p.n64;
+            for (int c0 = 0; c0 < p.nr; c0 += 32) {
+                uint32_t v[32];
+                tmem_ld_x32(tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 128 + c0, v);
+                tmem_wait_ld();
+                if (t < p.T) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        float4 o = make_float4(__uint_as_float(v[j]), __uint_as_float(v[j + 1]), __uint_as_float(v[j + 2]), __uint_as_float(v[j + 3]));
+                        if (kb1 == kb0) o = make_float4(0.f, 0.f, 0.f, 0.f);       // a slice beyond the last channel block
+                        if (c0 + j < p.nr) *reinterpret_cast<float4*>(dst + c0 + j) = o;
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars->d_empty[buf]));
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, 512); }
+}
+
+// Adds the channel slices, multiplies by the adapter's scale and splits the fp32 factor into `parts` bf16 terms that add up to
+// it (8 bits each): fac [2][T][parts][n64].
+__global__ void lora_split_kernel(const float* __restrict__ part, __nv_bfloat16* __restrict__ fac, int64_t T, int32_t n64, int32_t nr,
+                                  int32_t slices, int32_t parts, float scaling)
+{
+    const int64_t rows = 2 * T, total = rows * (n64 / 4);
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t row = i / (n64 / 4);
+        const int c = (int)(i - row * (n64 / 4)) * 4;
+        if (c >= nr) continue;
+        const int64_t kind = row / T, t = row - kind * T;
+        const float* src = part + (kind * slices * T + t) * n64 + c;
+        float4 x = *reinterpret_cast<const float4*>(src);
+        for (int s = 1; s < slices; ++s) {
+            const float4 y = *reinterpret_cast<const float4*>(src + (int64_t)s * T * n64);
+            x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+        }
+        float v[4] = {x.x * scaling, x.y * scaling, x.z * scaling, x.w * scaling};
+        __nv_bfloat16* dst = fac + row * parts * n64 + c;
+        for (int q = 0; q < parts; ++q) {
+            __nv_bfloat16 b[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                b[k] = __float2bfloat16_rn(v[k]);
+                const float w = __bfloat162float(b[k]);
+                v[k] = isfinite(w) ? v[k] - w : 0.0f;          // an infinite or NaN factor stays what it is
+            }
+            *reinterpret_cast<uint2*>(dst + (int64_t)q * n64) = *reinterpret_cast<const uint2*>(b);
+        }
+    }
+}
+
+// ---- (2) outer products ------------------------------------------------------------------------------------------------
+
+template <typename OutT> __device__ __forceinline__ OutT to_out(float v);
+template <> __device__ __forceinline__ float to_out<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// One thread's 32 accumulator columns [c0, c0 + 32) of channel ch -> dA (column j of the row-major [rank, width]) or dB (row ch).
+template <typename OutT>
+__device__ __forceinline__ void store_columns(OutT* dst, bool is_x, int64_t ch, int64_t width, int c0, int rank, const uint32_t (&v)[32], bool zero)
+{
+    if (is_x) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (c0 + j < rank) dst[(int64_t)(c0 + j) * width + ch] = to_out<OutT>(zero ? 0.0f : __uint_as_float(v[j]));
+    } else {
+        OutT* row = dst + ch * rank + c0;                      // 16-byte aligned: rank is a multiple of 8
+#pragma unroll
+        for (int j = 0; j < 32; j += 8) {
+            if (c0 + j >= rank) break;
+            __align__(16) OutT o[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] = to_out<OutT>(zero ? 0.0f : __uint_as_float(v[j + k]));
+#pragma unroll
+            for (int k = 0; k < (int)(8 * sizeof(OutT) / 16); ++k) reinterpret_cast<uint4*>(row + j)[k] = reinterpret_cast<const uint4*>(o)[k];
+        }
+    }
+}
+
+template <typename OutT>
+__global__ void __launch_bounds__(NTHREADS, 1)
+lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_constant__ CUtensorMap tm_dy,
+                  const __grid_constant__ CUtensorMap tm_h, const __grid_constant__ CUtensorMap tm_u, const OuterParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const int boxes = p.parts * (p.n64 / 64);                // factor operand: boxes of 64 columns x 64 tokens
+    const int stage_bytes = BIG + boxes * 8192;
+    uint8_t* conv_buf = smem + (size_t)p.stages * stage_bytes;      // expanded codes: two buffers of 256 channels x 64 tokens
+    Bars* bars = reinterpret_cast<Bars*>(conv_buf + 2 * 32768);
+    volatile uint32_t* abort_flag = &bars->abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t nS = (uint32_t)p.stages;
+
+    if (threadIdx.x == 0) {
+        init_barriers(bars, 8);
+        prefetch_tmap(&tm_codes); prefetch_tmap(&tm_dy); prefetch_tmap(&tm_h); prefetch_tmap(&tm_u);
+    }
+    if (warp == 1) { tmem_alloc(smem_u32(&bars->tmem_base), 512); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem_base;                  // accumulator of item n, sub-tile m: column (n & 1) * 256 + m * 128
+
+    auto item_of = [&](int64_t item, LoraChunk& c, bool& is_x, int& ch0) {
+        const int64_t k = item / p.tiles;
+        const int tile = (int)(item - k * p.tiles);
+        c = p.chunks[k];
+        is_x = tile < p.tiles_x;
+        ch0 = (is_x ? tile : tile - p.tiles_x) * TILE;
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            Ring ring;
+            bool ok = true;
+            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+                LoraChunk c; bool is_x; int ch0;
+                item_of(item, c, is_x, ch0);
+                for (int t = 0; t < c.len; t += TOK, ++it, ring.next(nS)) {
+                    if (!mbar_wait(smem_u32(&bars->empty[ring.slot]), ring.parity ^ 1u, abort_flag, p.timeout_word, TO_PRODUCER)) { ok = false; break; }
+                    const uint32_t full = smem_u32(&bars->full[ring.slot]);
+                    const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
+                    const int32_t row = (int32_t)(c.t0 + t);
+                    mbar_arrive_expect_tx(full, (is_x ? 2 : 4) * 8192 + boxes * 8192);
+                    if (is_x) {
+                        for (int j = 0; j < 2; ++j) tma_load_2d(big + j * 8192, &tm_codes, full, ch0 + j * 128, row);
+                        for (int j = 0; j < boxes; ++j) tma_load_2d(op + j * 8192, &tm_u, full, j * 64, row);
+                    } else {
+                        for (int j = 0; j < 4; ++j) tma_load_2d(big + j * 8192, &tm_dy, full, ch0 + j * 64, row);
+                        for (int j = 0; j < boxes; ++j) tma_load_2d(op + j * 8192, &tm_h, full, j * 64, row);
+                    }
+                }
+            }
+            if (!ok) drain_copies(bars, it, nS);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            const uint32_t idesc = make_idesc(1, 1, 1, 128, p.nr) | IDESC_A_MN | IDESC_B_MN;
+            Ring ring, conv;
+            uint32_t n = 0;
+            bool ok = true;
+            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++n) {
+                LoraChunk c; bool is_x; int ch0;
+                item_of(item, c, is_x, ch0);
+                const int subs = (is_x ? p.in : p.out) - ch0 > 128 ? 2 : 1;
+                const uint32_t buf = n & 1u;
+                if (!mbar_wait(smem_u32(&bars->d_empty[buf]), ((n >> 1) & 1u) ^ 1u, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                tc_fence_after();
+                for (int t = 0; t < c.len; t += TOK, ring.next(nS), conv.next(2)) {
+                    if (!mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_MMA) ||
+                        !mbar_wait(smem_u32(&bars->ready[conv.slot]), conv.parity, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
+                    const uint32_t a = is_x ? smem_u32(conv_buf) + conv.slot * 32768 : big;
+                    for (int m = 0; m < subs; ++m)
+#pragma unroll
+                        for (int k = 0; k < TOK / 16; ++k)
+                            for (int q = 0; q < p.parts; ++q)
+                                mma_f16_ss(tmem + buf * 256 + m * 128, make_smem_desc_mn_sw128(a + m * 16384 + k * 2048, 8192),
+                                           make_smem_desc_mn_sw128(op + q * (p.n64 / 64) * 8192 + k * 2048, 8192), idesc, t > 0 || k > 0 || q > 0);
+                    mma_commit(smem_u32(&bars->empty[ring.slot]));
+                    mma_commit(smem_u32(&bars->conv_empty[conv.slot]));
+                }
+                if (ok) mma_commit(smem_u32(&bars->d_full[buf]));
+            }
+            mma_commit(smem_u32(&bars->drain));
+            mbar_wait_quiet(smem_u32(&bars->drain), 0u);
+        }
+    } else if (warp < 10) {
+        const int tid = threadIdx.x - 64;                    // 0 .. 255
+        const int groups = (p.in + p.group - 1) / p.group;
+        Ring ring, conv;
+        bool ok = true;
+        for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            LoraChunk c; bool is_x; int ch0;
+            item_of(item, c, is_x, ch0);
+            for (int t = 0; t < c.len; t += TOK, ring.next(nS), conv.next(2)) {
+                const int live = min(TOK, c.len - t);        // token rows of this block that belong to the chunk
+                uint32_t step[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {                // unit i * 256 + tid: box of 128 channels, token, 16 channels
+                    const int unit = i * 256 + tid, tok = (unit & 511) >> 3;
+                    const int g = (ch0 + (unit >> 9) * 128 + (unit & 7) * 16) / p.group;
+                    step[i] = (is_x && tok < live && g < groups) ? p.scales[(c.t0 + t + tok) * p.ld_scales + g] : 0u;
+                }
+                ok = mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_UNPACK) &&
+                     mbar_wait(smem_u32(&bars->conv_empty[conv.slot]), conv.parity ^ 1u, abort_flag, p.timeout_word, TO_UNPACK);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                uint8_t* big = smem + (size_t)ring.slot * stage_bytes;
+                if (is_x) {
+                    uint8_t* out = conv_buf + conv.slot * 32768;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int unit = i * 256 + tid, box = unit >> 9, tok = (unit & 511) >> 3, j = unit & 7;
+                        const uint4 w = *reinterpret_cast<const uint4*>(big + box * 8192 + tok * 128 + ((j ^ (tok & 7)) << 4));
+                        uint32_t v[8];
+                        const uint32_t s2 = step_bf16x2(step[i]);
+                        expand4(w.x, s2, v[0], v[1]);
+                        expand4(w.y, s2, v[2], v[3]);
+                        expand4(w.z, s2, v[4], v[5]);
+                        expand4(w.w, s2, v[6], v[7]);
+                        if (tok >= live) {
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) v[k] = 0u;
+                        }
+                        uint8_t* row = out + (box * 2 + (j >> 2)) * 8192 + tok * 128;
+                        const int c16 = (j & 3) * 2;
+                        *reinterpret_cast<uint4*>(row + ((c16 ^ (tok & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                        *reinterpret_cast<uint4*>(row + (((c16 + 1) ^ (tok & 7)) << 4)) = make_uint4(v[4], v[5], v[6], v[7]);
+                    }
+                }
+                if (live < TOK) {                            // rows of the next example: zero in the factors, and in dY
+                    const int first = is_x ? 4 : 0, rows = TOK - live;
+                    for (int i = tid; i < (4 - first + boxes) * rows * 8; i += 256) {
+                        const int b = first + i / (rows * 8), rest = i % (rows * 8);
+                        *reinterpret_cast<uint4*>(big + b * 8192 + (live + (rest >> 3)) * 128 + (rest & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars->ready[conv.slot]));
+            }
+        }
+    } else {
+        const int row = (warp & 3) * 32 + lane;
+        const int64_t width_all = (int64_t)p.rank * (p.in + p.out);
+        uint32_t n = 0;
+        for (int64_t item = blockIdx.x; item < p.items; item += gridDim.x, ++n) {
+            LoraChunk c; bool is_x; int ch0;
+            item_of(item, c, is_x, ch0);
+            const int width = is_x ? p.in : p.out;
+            const uint32_t buf = n & 1u;
+            bool ok = mbar_wait(smem_u32(&bars->d_full[buf]), (n >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            const int64_t base = is_x ? 0 : (int64_t)p.rank * p.in;
+            for (int m = 0; m < 2; ++m) {
+                if (ch0 + m * 128 >= width) break;
+                const int64_t ch = ch0 + m * 128 + row;
+                for (int c0 = 0; c0 < p.rank; c0 += 32) {
+                    uint32_t v[32];
+                    tmem_ld_x32(tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 256 + m * 128 + c0, v);
+                    tmem_wait_ld();
+                    if (ch < width) {
+                        if (c.slot >= 0) store_columns<float>(p.part + (int64_t)c.slot * width_all + base, is_x, ch, width, c0, p.rank, v, c.len == 0);
+                        else store_columns<OutT>(reinterpret_cast<OutT*>(p.grads) + (int64_t)c.example * p.ld_grads + base, is_x, ch, width, c0, p.rank, v, c.len == 0);
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars->d_empty[buf]));
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, 512); }
+}
+
+// Adds the pieces of the examples that were summed in more than one, in piece order.
+template <typename OutT>
+__global__ void lora_join_kernel(const LoraJoin* __restrict__ joins, const float* __restrict__ part, int64_t width, OutT* __restrict__ grads,
+                                 int64_t ld_grads)
+{
+    const LoraJoin j = joins[blockIdx.y];
+    for (int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 4; i < width; i += (int64_t)gridDim.x * blockDim.x * 4) {
+        const float* src = part + (int64_t)j.first * width + i;
+        float4 x = *reinterpret_cast<const float4*>(src);
+        for (int k = 1; k < j.count; ++k) {
+            const float4 y = *reinterpret_cast<const float4*>(src + (int64_t)k * width);
+            x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+        }
+        __align__(16) OutT o[4] = {to_out<OutT>(x.x), to_out<OutT>(x.y), to_out<OutT>(x.z), to_out<OutT>(x.w)};
+        OutT* dst = grads + (int64_t)j.example * ld_grads + i;
+        if (sizeof(OutT) == 4) *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(o);
+        else *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(o);
+    }
+}
+
+// Host tables reach the device as kernel arguments: no copy from pageable memory that could wait for the stream, and the call can be
+// captured into a graph.
+struct Words { uint64_t w[480]; };
+__global__ void upload_kernel(const __grid_constant__ Words src, uint64_t* __restrict__ dst, int n)
+{
+    if ((int)threadIdx.x < n) dst[threadIdx.x] = src.w[threadIdx.x];
+}
+cudaError_t upload(const void* host, size_t bytes, void* dev, cudaStream_t st)
+{
+    const size_t words = (bytes + 7) / 8;
+    for (size_t w0 = 0; w0 < words; w0 += 480) {
+        const size_t n = words - w0 < 480 ? words - w0 : 480;
+        Words arg;
+        const size_t len = bytes - w0 * 8 < n * 8 ? bytes - w0 * 8 : n * 8;
+        memcpy(arg.w, reinterpret_cast<const uint8_t*>(host) + w0 * 8, len);
+        upload_kernel<<<1, 512, 0, st>>>(arg, reinterpret_cast<uint64_t*>(dev) + w0, (int)n);
+        count_launches(1);
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+LoraPlan plan_lora(int64_t T, int64_t n, int32_t in, int32_t out, int32_t rank, qless_dtype dtype)
+{
+    LoraPlan pl;
+    const int64_t sms = sm_count();
+    pl.nr = (rank + 15) / 16 * 16;
+    pl.n64 = pl.nr <= 64 ? 64 : 128;
+    pl.parts = dtype == QLESS_F32 ? 3 : 2;
+    pl.tiles_x = (in + TILE - 1) / TILE;
+    pl.tiles = pl.tiles_x + (out + TILE - 1) / TILE;
+    // Pieces of at most `chunk` tokens: about four items per SM where the examples alone do not give that many, at least 512 tokens
+    // (a piece of fewer tokens writes and re-reads more partial sums than the activations it reads).
+    int64_t chunk = (T * pl.tiles + 4 * sms - 1) / (4 * sms);
+    if (chunk < 512) chunk = 512;
+    pl.chunk = (chunk + TOK - 1) / TOK * TOK;
+    const int64_t most = T / pl.chunk;
+    pl.max_slots = most + (n < most ? n : most);
+    pl.max_chunks = n + most;
+    pl.token_tiles = (T + 127) / 128;
+    // Channel slices: about three items per SM, each of at least four blocks of 128 channels.
+    const int32_t kb = ((in > out ? in : out) + CH - 1) / CH;
+    int64_t slices = pl.token_tiles > 0 ? (3 * sms + 2 * pl.token_tiles - 1) / (2 * pl.token_tiles) : 1;
+    if (slices > (kb + 3) / 4) slices = (kb + 3) / 4;
+    pl.slices = (int32_t)(slices < 1 ? 1 : slices);
+    size_t off = 0;
+    pl.fac_off = off; off += align_up((size_t)2 * T * pl.parts * pl.n64 * 2, 256);
+    pl.fpart_off = off; off += align_up((size_t)2 * pl.slices * T * pl.n64 * 4, 256);
+    pl.part_off = off; off += align_up((size_t)pl.max_slots * rank * ((size_t)in + out) * 4, 256);
+    pl.chunk_off = off; off += align_up((size_t)pl.max_chunks * sizeof(LoraChunk), 256);
+    pl.join_off = off; off += align_up((size_t)(pl.max_slots + 1) * sizeof(LoraJoin), 256);
+    pl.total = off + 256;
+    return pl;
+}
+
+qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st)
+{
+    LoraChunk* d_chunks = reinterpret_cast<LoraChunk*>(ws + pl.chunk_off);
+    LoraJoin* d_joins = reinterpret_cast<LoraJoin*>(ws + pl.join_off);
+    QLESS_CUDA_TRY(upload(a.chunks, (size_t)a.num_chunks * sizeof(LoraChunk), d_chunks, st));
+    if (a.num_joins > 0) QLESS_CUDA_TRY(upload(a.joins, (size_t)a.num_joins * sizeof(LoraJoin), d_joins, st));
+    __nv_bfloat16* fac = reinterpret_cast<__nv_bfloat16*>(ws + pl.fac_off);
+    const size_t budget = 227 * 1024 - 1024 - sizeof(Bars) - 64;
+    qless_status s;
+    if (a.T > 0) {
+        CUtensorMap tm_codes, tm_dy, tm_a, tm_b;
+        if ((s = make_tmap_2d_sw128(&tm_codes, a.codes, 1, a.in, a.T, a.ld_codes, 128, 128)) != QLESS_OK) return s;
+        if ((s = make_tmap_2d_sw128(&tm_dy, a.grad_out, 2, a.out, a.T, a.ld_grad_out * 2, 64, 128)) != QLESS_OK) return s;
+        if ((s = make_tmap_2d_sw128(&tm_a, a.lora_a, 2, a.in, a.rank, (uint64_t)a.in * 2, 64, pl.nr)) != QLESS_OK) return s;
+        if ((s = make_tmap_2d_sw128(&tm_b, a.lora_b, 2, a.rank, a.out, (uint64_t)a.rank * 2, 64, 128)) != QLESS_OK) return s;
+        FactorParams f;
+        f.T = a.T; f.ld_scales = a.ld_scales; f.scales = a.scales;
+        f.part = reinterpret_cast<float*>(ws + pl.fpart_off);
+        f.in = a.in; f.out = a.out; f.group = a.group; f.nr = pl.nr; f.n64 = pl.n64; f.slices = pl.slices;
+        f.kb_x = ((a.in + CH - 1) / CH + pl.slices - 1) / pl.slices;
+        f.kb_y = ((a.out + CH - 1) / CH + pl.slices - 1) / pl.slices;
+        f.token_tiles = (int32_t)pl.token_tiles;
+        f.items = 2 * pl.token_tiles * pl.slices;
+        f.timeout_word = timeout_word;
+        const size_t stage = BIG + (size_t)pl.n64 * 256;
+        f.stages = (int32_t)(budget / stage < MAX_STAGES ? budget / stage : MAX_STAGES);
+        const size_t smem = 1024 + f.stages * stage + sizeof(Bars);
+        const int64_t grid = f.items < sm_count() ? f.items : sm_count();
+        { ProfileScope ps("lora_factors", st);
+          QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_factors_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+          lora_factors_kernel<<<(unsigned)grid, NTHREADS, smem, st>>>(tm_codes, tm_dy, tm_a, tm_b, f); }
+        QLESS_CUDA_TRY(cudaGetLastError());
+        { ProfileScope ps("lora_split", st);
+          const int64_t blocks = (2 * a.T * (pl.n64 / 4) + 255) / 256, most = (int64_t)sm_count() * 8;
+          lora_split_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, st>>>(f.part, fac, a.T, pl.n64, pl.nr, pl.slices, pl.parts, a.scaling); }
+        QLESS_CUDA_TRY(cudaGetLastError());
+        count_launches(2);
+    }
+    CUtensorMap tm_codes, tm_dy, tm_h, tm_u;
+    const int64_t rows = a.T > 0 ? a.T : 1;                   // no tokens at all: the maps are not used, every item has length 0
+    const int64_t fw = (int64_t)pl.parts * pl.n64;
+    const void* any = ws;
+    if ((s = make_tmap_2d_sw128(&tm_codes, a.T > 0 ? (const void*)a.codes : any, 1, a.in, rows, a.T > 0 ? a.ld_codes : a.in, 128, TOK)) != QLESS_OK) return s;
+    if ((s = make_tmap_2d_sw128(&tm_dy, a.T > 0 ? a.grad_out : any, 2, a.out, rows, (a.T > 0 ? a.ld_grad_out : a.out) * 2, 64, TOK)) != QLESS_OK) return s;
+    if ((s = make_tmap_2d_sw128(&tm_h, fac, 2, fw, rows, fw * 2, 64, TOK)) != QLESS_OK) return s;
+    if ((s = make_tmap_2d_sw128(&tm_u, fac + a.T * fw, 2, fw, rows, fw * 2, 64, TOK)) != QLESS_OK) return s;
+    OuterParams o;
+    o.chunks = d_chunks; o.scales = a.scales; o.ld_scales = a.ld_scales; o.ld_grads = a.ld_grads;
+    o.grads = a.grads; o.part = reinterpret_cast<float*>(ws + pl.part_off);
+    o.in = a.in; o.out = a.out; o.rank = a.rank; o.group = a.group; o.nr = pl.nr; o.n64 = pl.n64; o.parts = pl.parts;
+    o.tiles_x = pl.tiles_x; o.tiles = pl.tiles; o.timeout_word = timeout_word;
+    o.items = (int64_t)a.num_chunks * pl.tiles;
+    const size_t stage = BIG + (size_t)pl.parts * (pl.n64 / 64) * 8192;
+    const size_t left = budget - 2 * 32768;
+    o.stages = (int32_t)(left / stage < MAX_STAGES ? left / stage : MAX_STAGES);
+    const size_t smem = 1024 + o.stages * stage + 2 * 32768 + sizeof(Bars);
+    const int64_t grid = o.items < sm_count() ? o.items : sm_count();
+    { ProfileScope ps("lora_outer", st);
+      if (a.dtype == QLESS_F32) {
+          QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_outer_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+          lora_outer_kernel<float><<<(unsigned)grid, NTHREADS, smem, st>>>(tm_codes, tm_dy, tm_h, tm_u, o);
+      } else {
+          QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_outer_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+          lora_outer_kernel<__nv_bfloat16><<<(unsigned)grid, NTHREADS, smem, st>>>(tm_codes, tm_dy, tm_h, tm_u, o);
+      } }
+    QLESS_CUDA_TRY(cudaGetLastError());
+    count_launches(1);
+    for (int64_t j0 = 0; j0 < a.num_joins; j0 += 65535) {
+        ProfileScope ps("lora_join", st);
+        const int64_t width = (int64_t)a.rank * (a.in + a.out);
+        const int64_t bx = (width / 4 + 255) / 256;
+        const dim3 g((unsigned)(bx < 1024 ? bx : 1024), (unsigned)(a.num_joins - j0 < 65535 ? a.num_joins - j0 : 65535));
+        if (a.dtype == QLESS_F32) lora_join_kernel<float><<<g, 256, 0, st>>>(d_joins + j0, o.part, width, reinterpret_cast<float*>(a.grads), a.ld_grads);
+        else lora_join_kernel<__nv_bfloat16><<<g, 256, 0, st>>>(d_joins + j0, o.part, width, reinterpret_cast<__nv_bfloat16*>(a.grads), a.ld_grads);
+        QLESS_CUDA_TRY(cudaGetLastError());
+        count_launches(1);
+    }
+    return QLESS_OK;
+}
+
+}  // namespace qless

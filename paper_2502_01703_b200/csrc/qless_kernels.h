@@ -87,4 +87,31 @@ cudaError_t launch_select_topk(const float* scores, int64_t N, int64_t k, int64_
 // 0: path by size; 1: multi-pass select at every N; 2: sampled bracket forced too high (exercises the fallback).
 void set_select_path(int mode);
 
+// 8-bit activation checkpoints (activation.cu): codes int8 [tokens][ld_codes], step bytes [tokens][ld_scales].
+cudaError_t launch_activation_quantize(const void* x, qless_dtype dtype, int64_t tokens, int32_t width, int64_t ld_x, int32_t group,
+                                       int8_t* codes, int64_t ld_codes, uint8_t* scales, int64_t ld_scales, cudaStream_t st);
+cudaError_t launch_activation_dequantize(const int8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales, int64_t tokens,
+                                         int32_t width, int32_t group, void* out, qless_dtype dtype, int64_t ld_out, cudaStream_t st);
+
+// Per-example LoRA gradients (lora_grad.cu).
+struct LoraChunk { int64_t t0; int32_t len, example, slot, unused; };      // tokens [t0, t0 + len) of an example; slot < 0: the whole example
+struct LoraJoin { int32_t example, first, count, unused; };                 // an example summed in pieces: slots first .. first + count - 1
+struct LoraPlan {
+    int64_t chunk, max_chunks, max_slots, token_tiles;
+    int32_t nr, n64, parts, tiles_x, tiles, slices;
+    size_t fac_off, fpart_off, part_off, chunk_off, join_off, total;
+};
+LoraPlan plan_lora(int64_t T, int64_t n, int32_t in, int32_t out, int32_t rank, qless_dtype dtype);
+struct LoraArgs {
+    const int8_t* codes; const uint8_t* scales; const void* grad_out; const void* lora_a; const void* lora_b;
+    int64_t T, ld_codes, ld_scales, ld_grad_out, ld_grads;
+    int32_t in, out, rank, group;
+    float scaling;
+    qless_dtype dtype;
+    void* grads;
+    const LoraChunk* chunks; const LoraJoin* joins;      // host
+    int64_t num_chunks, num_joins;
+};
+qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st);
+
 }  // namespace qless
