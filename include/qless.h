@@ -406,6 +406,27 @@ qless_status qless_lora_gradients(const int8_t* codes, int64_t ld_codes, const u
                                   int32_t rank, float scaling, void* grads, qless_dtype dtype, int64_t ld_grads,
                                   void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* Softmax cross entropy of a language model's head over a large vocabulary, with its gradient, without keeping the
+ * logits. hidden [tokens, width] bf16 (ld_hidden elements per row), weight [vocab, width] bf16 (ld_weight elements per
+ * row), labels [tokens] int64 (device), token_weight [tokens] fp32 (device; NULL = 1 for every token):
+ *   l_tv = <hidden_t, weight_v>;  p_tv = exp(l_tv) / sum_u exp(l_tu);
+ *   loss[t] = -log p_t,label                                             fp32, not multiplied by the token's weight
+ *   grad_hidden[t] = w_t (sum_v p_tv weight_v - weight_label)            bf16 [tokens, width], NULL to skip
+ *   grad_weight[v] = sum_t w_t (p_tv - [v = label_t]) hidden_t           bf16 [vocab, width], NULL to skip
+ * (the gradients of sum_t w_t loss[t]). A token whose label lies outside [0, vocab), e.g. -100, carries no loss: its loss
+ * and gradient row are 0, and whatever its hidden row and weight hold (infinities and NaN included) reaches nothing.
+ * Logits are fp32 sums of exact products; the softmax statistics and all accumulators are fp32; the probabilities enter the
+ * second product rounded to bf16 (with 1 - p of the label kept apart in fp32, so that tokens the model is sure of lose
+ * nothing), and a gradient is rounded once more to bf16. The same inputs give the same bits.
+ * Requirements: tokens < 2^31 - 256; 1 <= vocab < 2^31 - 256; width a multiple of 8, 8 <= width <= 65536; hidden, weight,
+ * grad_hidden, grad_weight 16-byte aligned, their row strides multiples of 8. */
+size_t qless_lm_loss_workspace(int64_t tokens, int32_t width, int32_t vocab, int32_t want_hidden, int32_t want_weight);
+
+qless_status qless_lm_loss(const void* hidden, int64_t ld_hidden, const void* weight, int64_t ld_weight, const int64_t* labels,
+                           const float* token_weight, int64_t tokens, int32_t width, int32_t vocab, float* loss,
+                           void* grad_hidden, int64_t ld_grad_hidden, void* grad_weight, int64_t ld_grad_weight,
+                           void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

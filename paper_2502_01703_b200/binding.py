@@ -27,6 +27,7 @@ EXPORTS = [
     "qless_set_projection_path", "qless_set_score_path", "qless_set_select_path", "qless_microbench",
     "qless_project_quantize_ex", "qless_project_quantize_host_ex", "qless_gaussian_entries", "qless_selftest_timeout",
     "qless_activation_quantize", "qless_activation_dequantize", "qless_lora_gradients_workspace", "qless_lora_gradients",
+    "qless_lm_loss_workspace", "qless_lm_loss",
 ]
 RADEMACHER, GAUSSIAN = 0, 1
 SELECT_STATIC_MAX_N = 1 << 22
@@ -135,6 +136,10 @@ def lib():
         L.qless_lora_gradients.restype = C.c_int
         L.qless_lora_gradients.argtypes = [vp, i64, vp, i64, i32, vp, i64, vp, vp, vp, i64, i64, i32, i32, i32, C.c_float, vp, C.c_int,
                                            i64, vp, sz, vp]
+        L.qless_lm_loss_workspace.restype = sz
+        L.qless_lm_loss_workspace.argtypes = [i64, i32, i32, i32, i32]
+        L.qless_lm_loss.restype = C.c_int
+        L.qless_lm_loss.argtypes = [vp, i64, vp, i64, vp, vp, i64, i32, i32, vp, vp, i64, vp, i64, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -496,6 +501,46 @@ def qless_lora_gradients(codes, scales, grad_out, lora_a, lora_b, offsets, scali
                                       _row_stride(grad_out), _ptr(lora_a), _ptr(lora_b), _ptr(off), T, n, wi, wo, rank, scaling,
                                       _ptr(grads), _dtype_code(grads), _row_stride(grads), _ptr(ws), ws.numel(), _stream(stream)))
     return grads
+
+
+def qless_lm_loss_workspace(tokens, width, vocab, want_hidden=True, want_weight=False):
+    return int(lib().qless_lm_loss_workspace(tokens, width, vocab, 1 if want_hidden else 0, 1 if want_weight else 0))
+
+
+def qless_lm_loss(hidden, weight, labels, token_weight=None, want_hidden=True, want_weight=False, out=None, workspace=None, stream=None):
+    """Softmax cross entropy over a large vocabulary with its gradient: hidden bf16 [tokens, width], weight bf16 [vocab, width],
+    labels int64 [tokens] (outside [0, vocab): no loss), token_weight f32 [tokens] or None. Returns dict(loss f32 [tokens],
+    grad_hidden bf16 [tokens, width] | None, grad_weight bf16 [vocab, width] | None), the gradients being those of
+    sum(token_weight * loss). `out` may pass preallocated tensors by those names."""
+    if hidden.dtype != torch.bfloat16 or weight.dtype != torch.bfloat16:
+        raise TypeError("hidden and weight must be bfloat16")
+    if labels.dtype != torch.int64 or not labels.is_contiguous():
+        raise TypeError("labels must be a contiguous int64 tensor")
+    T, width = hidden.shape
+    vocab = weight.shape[0]
+    if weight.shape[1] != width or labels.shape != (T,):
+        raise ValueError("shapes of hidden, weight and labels do not fit together")
+    if token_weight is not None and (token_weight.dtype != torch.float32 or token_weight.shape != (T,) or not token_weight.is_contiguous()):
+        raise ValueError("token_weight must be a contiguous float32 tensor [tokens]")
+    dev = hidden.device
+    out = out or {}
+    loss = out.get("loss")
+    if loss is None:
+        loss = torch.empty(T, dtype=torch.float32, device=dev)
+    gh = out.get("grad_hidden")
+    if gh is None and want_hidden:
+        gh = torch.empty((T, width), dtype=torch.bfloat16, device=dev)
+    gw = out.get("grad_weight")
+    if gw is None and want_weight:
+        gw = torch.empty((vocab, width), dtype=torch.bfloat16, device=dev)
+    for t, shape in ((loss, (T,)), (gh, (T, width)), (gw, (vocab, width))):
+        if t is not None and (t.shape != shape or t.dtype != (torch.float32 if t is loss else torch.bfloat16)):
+            raise ValueError("an output has the wrong shape or type")
+    ws = _workspace(qless_lm_loss_workspace(T, width, vocab, gh is not None, gw is not None), dev, workspace)
+    _check(lib().qless_lm_loss(_ptr(hidden), _row_stride(hidden), _ptr(weight), _row_stride(weight), _ptr(labels), _ptr(token_weight),
+                               T, width, vocab, _ptr(loss), _ptr(gh), _row_stride(gh) if gh is not None else 0,
+                               _ptr(gw), _row_stride(gw) if gw is not None else 0, _ptr(ws), ws.numel(), _stream(stream)))
+    return dict(loss=loss, grad_hidden=gh, grad_weight=gw)
 
 
 def qless_set_projection_path(path):

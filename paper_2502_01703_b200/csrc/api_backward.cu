@@ -136,4 +136,54 @@ qless_status qless_lora_gradients(const int8_t* codes, int64_t ld_codes, const u
     }
 }
 
+// ---- loss of the language model's head -----------------------------------------------------------
+
+static qless_status check_loss_shape(int64_t tokens, int32_t width, int32_t vocab)
+{
+    QLESS_REQUIRE(tokens >= 0 && width > 0 && vocab > 0, QLESS_ERR_INVALID_ARG, "tokens must be >= 0, width and vocab > 0 (tokens=%lld, width=%d, vocab=%d)",
+                  (long long)tokens, width, vocab);
+    QLESS_REQUIRE(tokens < ((int64_t)1 << 31) - 256 && vocab < 0x7FFFFFFF - 256, QLESS_ERR_UNSUPPORTED, "tokens and vocab must be below 2^31 - 256");
+    QLESS_REQUIRE(width % 8 == 0 && width <= 65536, QLESS_ERR_UNSUPPORTED, "width must be a multiple of 8, at most 65536 (width=%d)", width);
+    return QLESS_OK;
+}
+
+size_t qless_lm_loss_workspace(int64_t tokens, int32_t width, int32_t vocab, int32_t want_hidden, int32_t want_weight)
+{
+    if (check_loss_shape(tokens, width, vocab) != QLESS_OK || tokens == 0) return 256;
+    return plan_loss(tokens, width, vocab, want_hidden != 0, want_weight != 0).total;
+}
+
+qless_status qless_lm_loss(const void* hidden, int64_t ld_hidden, const void* weight, int64_t ld_weight, const int64_t* labels,
+                           const float* token_weight, int64_t tokens, int32_t width, int32_t vocab, float* loss, void* grad_hidden,
+                           int64_t ld_grad_hidden, void* grad_weight, int64_t ld_grad_weight, void* workspace, size_t workspace_bytes,
+                           void* cuda_stream)
+{
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+    qless_status s = check_loss_shape(tokens, width, vocab);
+    if (s != QLESS_OK) return s;
+    QLESS_REQUIRE(grad_weight == nullptr || (aligned(grad_weight, 16) && ld_grad_weight >= width && ld_grad_weight % 8 == 0), QLESS_ERR_INVALID_ARG,
+                  "grad_weight must be 16-byte aligned, ld_grad_weight >= width and a multiple of 8 (ld_grad_weight=%lld)", (long long)ld_grad_weight);
+    if (tokens == 0) {                    // the gradient of an empty sum
+        if (grad_weight != nullptr) QLESS_CUDA_TRY(cudaMemset2DAsync(grad_weight, (size_t)ld_grad_weight * 2, 0, (size_t)width * 2, (size_t)vocab, st));
+        return QLESS_OK;
+    }
+    QLESS_REQUIRE(hidden && weight && labels && loss, QLESS_ERR_INVALID_ARG, "hidden, weight, labels and loss are required");
+    QLESS_REQUIRE(aligned(hidden, 16) && aligned(weight, 16) && aligned(labels, 8), QLESS_ERR_INVALID_ARG,
+                  "hidden and weight must be 16-byte aligned, labels 8-byte aligned");
+    QLESS_REQUIRE(ld_hidden >= width && ld_hidden % 8 == 0 && ld_weight >= width && ld_weight % 8 == 0, QLESS_ERR_INVALID_ARG,
+                  "ld_hidden and ld_weight must be >= width and multiples of 8 (ld_hidden=%lld, ld_weight=%lld)", (long long)ld_hidden, (long long)ld_weight);
+    QLESS_REQUIRE(grad_hidden == nullptr || (aligned(grad_hidden, 16) && ld_grad_hidden >= width && ld_grad_hidden % 8 == 0), QLESS_ERR_INVALID_ARG,
+                  "grad_hidden must be 16-byte aligned, ld_grad_hidden >= width and a multiple of 8 (ld_grad_hidden=%lld)", (long long)ld_grad_hidden);
+    const LossPlan pl = plan_loss(tokens, width, vocab, grad_hidden != nullptr, grad_weight != nullptr);
+    QLESS_REQUIRE(workspace != nullptr && aligned(workspace, 256), QLESS_ERR_WORKSPACE, "workspace must be non-NULL and 256-byte aligned");
+    QLESS_REQUIRE(workspace_bytes >= pl.total, QLESS_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", workspace_bytes, pl.total);
+    unsigned int* flag = timeout_flag_ptr();
+    QLESS_REQUIRE(flag != nullptr, QLESS_ERR_CUDA, "cannot resolve the device timeout flag");
+    LossArgs a;
+    a.hidden = hidden; a.weight = weight; a.labels = labels; a.token_weight = token_weight;
+    a.T = tokens; a.ld_hidden = ld_hidden; a.ld_weight = ld_weight; a.ld_grad_hidden = ld_grad_hidden; a.ld_grad_weight = ld_grad_weight;
+    a.width = width; a.vocab = vocab; a.loss = loss; a.grad_hidden = grad_hidden; a.grad_weight = grad_weight;
+    return launch_loss(a, pl, reinterpret_cast<uint8_t*>(workspace), flag, st);
+}
+
 }  // extern "C"

@@ -1,0 +1,676 @@
+// Softmax cross entropy of a language model's head over a large vocabulary, with its gradient; the logits are never kept.
+//
+//   l_tv = <h_t, W_v>;  loss_t = logsumexp_v l_tv - l_t,y;  dh_t = w_t (sum_v p_tv W_v - W_y);  dW_v = sum_t w_t (p_tv - [v = y_t]) h_t
+//
+// The label's column is kept apart from the others. With s = sum_{v != y} exp(l_v - r) for some reference r:
+//   d = r + log s - l_y,  loss = log(1 + e^d),  1 - p_y = sigma(d),  dh = w sigma(d) (sum_{v != y} exp(l_v - r) W_v / s - W_y):
+// no difference of nearly equal numbers is formed for a token the model is sure of, and the operand of the second product never
+// holds p_y - 1 rounded to 8 bits. Everything is kept in powers of two (l * log2 e).
+//
+// Tokens without a label inside [0, V) take no part: the others are gathered first (their number stays on the device), so that an
+// infinity or NaN in an ignored row meets no product, and ignored tokens cost nothing.
+//
+// All products run in one kernel (head_gemm_kernel, tcgen05 on CTA pairs, 256 x 256 tiles, bf16 operands, fp32 accumulators in
+// tensor memory, two of them so that the epilogue of a tile overlaps the next tile's products):
+//   STATS   h W^T        epilogue: per row and 128 columns the maximum and the sum of exponentials          (loss alone)
+//   PROBS   h W^T        epilogue: exp(l - r) or w (p - [v = y]) as bf16 into one piece of the vocabulary    (gradients)
+//   GRAD_H  piece * W    epilogue: fp32, added to what the earlier pieces left
+//   GRAD_W  piece^T * h  epilogue: bf16 rows of dW
+// Gradient of the hidden states alone: two products instead of three. The reference r of a row is its maximum over the first 256
+// columns, known after one small launch; any reference gives the same softmax, and with fp32 and bf16 exponents one that lies up
+// to LIMIT = 64 powers of two below a row's true maximum is as good as the maximum itself. Should a row exceed that, a flag sends the
+// rest through a second pass whose reference is the true maximum: its launches are always enqueued and return at once when the
+// flag is not set (the host does not wait to find out).
+// With dW the normaliser has to be known before the piece is written: STATS first, then PROBS, GRAD_H and GRAD_W per piece.
+#include "qless_kernels.h"
+#include "tc_common.cuh"
+
+namespace qless {
+
+namespace {
+
+using namespace tc;
+
+constexpr int NTHREADS = 320;               // warp 0 TMA, warp 1 MMA, warps 2-9 epilogue (two groups of four, 128 columns each)
+constexpr int STAGES = 3;
+constexpr int KB = 128;                     // K columns per stage: 64 KiB of operands per CTA
+constexpr int HALF = 32768;                 // bytes of one operand of a stage
+constexpr int GROUP_M = 16;                 // row tiles that share a pass over the column tiles (their operand stays in L2)
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float LIMIT = 64.0f;
+
+enum { STATS = 0, PROBS = 1, GRAD_H = 2, GRAD_W = 3 };
+
+struct LossMeta { int32_t count, splits, redo, unused; };
+
+struct __align__(16) RowParam { float r2, w, wl, unused; };      // PROBS: out = w * exp2(l2 - r2), the label's column wl
+
+struct GemmParams {
+    const LossMeta* meta;
+    const int32_t* gate;                    // NULL, or a flag: 0 = nothing to do
+    int32_t cols;                           // columns of this launch (STATS, PROBS: vocabulary; GRAD_H, GRAD_W: hidden width)
+    int32_t col0;                           // first vocabulary column of the launch (STATS, PROBS, GRAD_H: rows of W; GRAD_W: rows of dW)
+    int32_t rows;                           // GRAD_W: vocabulary columns of the piece
+    int32_t k;                              // contraction length (GRAD_W: the token count instead)
+    int64_t tpad;
+    const int32_t* labels;                  // [tpad] of the gathered tokens
+    const RowParam* rowp;
+    float2* stat;                           // STATS: [2 * tiles][tpad] (maximum, sum)
+    float* psum;                            // PROBS: [2 * tiles][tpad] sums, or NULL
+    int32_t tile0;                          // tile index of the launch's first column tile in stat / psum
+    float* label_logit;                     // [tpad], in powers of two
+    __nv_bfloat16* out;                     // PROBS: piece [tpad][ld_out]; GRAD_W: rows of dW
+    int64_t ld_out;
+    float* acc;                             // GRAD_H: [splits][row tiles * 256][cols]
+    int32_t accumulate;
+    int32_t* redo;                          // PROBS: set where a row lies more than LIMIT above its reference
+    unsigned int* timeout_word;
+};
+
+struct __align__(8) Bars {
+    uint64_t full[STAGES], empty[STAGES], d_full[2], d_empty[2], drain;
+    uint32_t tmem_base, abort_flag;
+};
+
+struct Ring {
+    uint32_t slot = 0, parity = 0;
+    __device__ __forceinline__ void next(uint32_t n) { if (++slot == n) { slot = 0; parity ^= 1u; } }
+};
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    const __nv_bfloat162 z = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&z);
+}
+
+template <int MODE>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
+head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const GemmParams p)
+{
+    if (p.gate != nullptr && *p.gate == 0) return;           // the same for every thread of the grid
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    Bars* bars = reinterpret_cast<Bars*>(smem + STAGES * 2 * HALF);
+    volatile uint32_t* abort_flag = &bars->abort_flag;
+    constexpr bool A_MN = MODE == GRAD_W, B_MN = MODE == GRAD_H || MODE == GRAD_W;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_ctarank();
+    const int64_t pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
+
+    const int count = p.meta->count;
+    const int mt = ((MODE == GRAD_W ? p.rows : count) + 255) / 256, nt = (p.cols + 255) / 256;
+    const int splits = MODE == GRAD_H ? p.meta->splits : 1;
+    const int kblocks = ((MODE == GRAD_W ? count : p.k) + KB - 1) / KB;
+    const int ksplit = (kblocks + splits - 1) / splits;
+    const int64_t per_split = (int64_t)mt * nt;
+    const int64_t items = per_split * splits;
+    // item -> (split, column tile, row tile): GROUP_M row tiles at a time, row tiles fastest
+    auto item_of = [&](int64_t item, int& split, int& m, int& n, int& kb0, int& kb1) {
+        split = (int)(item / per_split);
+        const int64_t r = item - split * per_split;
+        const int64_t g = r / ((int64_t)GROUP_M * nt);
+        const int m0 = (int)g * GROUP_M, gm = min(GROUP_M, mt - m0);
+        const int rest = (int)(r - g * GROUP_M * nt);
+        n = rest / gm;
+        m = m0 + rest - n * gm;
+        kb0 = min(kblocks, split * ksplit);
+        kb1 = min(kblocks, kb0 + ksplit);
+    };
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&bars->d_full[s]), 1); mbar_init(smem_u32(&bars->d_empty[s]), 16); }
+        mbar_init(smem_u32(&bars->drain), 1);
+        bars->abort_flag = 0;
+        fence_barrier_init();
+        prefetch_tmap(&tm_a); prefetch_tmap(&tm_b);
+    }
+    if (warp == 1) { tmem_alloc_pair(smem_u32(&bars->tmem_base), 512); tmem_relinquish_pair(); }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem_base;                   // accumulators at columns 0 and 256
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            Ring ring;
+            bool ok = true;
+            for (int64_t item = pair; item < items && ok; item += num_pairs) {
+                int split, m, n, kb0, kb1;
+                item_of(item, split, m, n, kb0, kb1);
+                const int a0 = m * 256 + (int)rank * 128, b0 = n * 256 + (int)rank * 128 + (B_MN ? 0 : p.col0);
+                for (int kb = kb0; kb < kb1; ++kb, ++it, ring.next(STAGES)) {
+                    if (!mbar_wait_cluster(smem_u32(&bars->empty[ring.slot]), ring.parity ^ 1u, abort_flag, p.timeout_word, TO_PRODUCER)) { ok = false; break; }
+                    const uint32_t full = map_to_cta(smem_u32(&bars->full[ring.slot]), 0);
+                    if (rank == 0) mbar_arrive_expect_tx(smem_u32(&bars->full[ring.slot]), 4 * HALF);      // both CTAs' bytes
+                    const uint32_t a = smem_u32(smem + (size_t)ring.slot * 2 * HALF), b = a + HALF;
+                    const int k0 = kb * KB, kw = k0 + (MODE == GRAD_H ? p.col0 : 0);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        if (A_MN) tma_load_2d_pair(a + j * 16384, &tm_a, full, a0 + 64 * j, k0);
+                        else tma_load_2d_pair(a + j * 16384, &tm_a, full, k0 + 64 * j, a0);
+                        if (B_MN) tma_load_2d_pair(b + j * 16384, &tm_b, full, b0 + 64 * j, kw);
+                        else tma_load_2d_pair(b + j * 16384, &tm_b, full, k0 + 64 * j, b0);
+                    }
+                }
+            }
+            if (!ok) {       // leave no copy in flight: the leader waits (bounded) for the stages that are armed, the peer idles
+                if (rank == 0) {
+                    for (uint32_t j = (it > STAGES ? it - STAGES : 0u); j < it; ++j)
+                        if (!mbar_wait_quiet(smem_u32(&bars->full[j % STAGES]), (j / STAGES) & 1u, 1u << 14)) break;
+                } else {
+                    for (uint32_t t = 0; t < (1u << 14); ++t) __nanosleep(64);
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            const uint32_t idesc = make_idesc(1, 1, 1, 256, 256) | (A_MN ? IDESC_A_MN : 0u) | (B_MN ? IDESC_B_MN : 0u);
+            Ring ring;
+            uint32_t n_acc = 0;
+            bool ok = true;
+            for (int64_t item = pair; item < items && ok; item += num_pairs, ++n_acc) {
+                int split, m, n, kb0, kb1;
+                item_of(item, split, m, n, kb0, kb1);
+                const uint32_t buf = n_acc & 1u, d = tmem + buf * 256;
+                if (!mbar_wait_cluster(smem_u32(&bars->d_empty[buf]), ((n_acc >> 1) & 1u) ^ 1u, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                tc_fence_after();
+                for (int kb = kb0; kb < kb1; ++kb, ring.next(STAGES)) {
+                    if (!mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t a = smem_u32(smem + (size_t)ring.slot * 2 * HALF), b = a + HALF;
+#pragma unroll
+                    for (int k = 0; k < KB / 16; ++k) {
+                        const uint64_t ad = A_MN ? make_smem_desc_mn_sw128(a + k * 2048, 16384) : make_smem_desc_sw128(a + (k >> 2) * 16384) + (uint64_t)((k & 3) * 2);
+                        const uint64_t bd = B_MN ? make_smem_desc_mn_sw128(b + k * 2048, 16384) : make_smem_desc_sw128(b + (k >> 2) * 16384) + (uint64_t)((k & 3) * 2);
+                        mma_f16_ss_pair(d, ad, bd, idesc, kb > kb0 || k > 0);
+                    }
+                    mma_commit_pair(smem_u32(&bars->empty[ring.slot]));
+                }
+                if (ok) mma_commit_pair(smem_u32(&bars->d_full[buf]));
+            }
+            mma_commit_pair(smem_u32(&bars->drain));           // every MMA issued above completes before tensor memory is freed
+            mbar_wait_quiet(smem_u32(&bars->drain), 0u);
+        }
+    } else {
+        const int q = warp & 3, half = warp >= 6 ? 1 : 0;
+        const uint32_t lane_base = (uint32_t)(q * 32) << 16;
+        uint32_t n_acc = 0;
+        for (int64_t item = pair; item < items; item += num_pairs, ++n_acc) {
+            int split, m, n, kb0, kb1;
+            item_of(item, split, m, n, kb0, kb1);
+            const int64_t row = (int64_t)m * 256 + rank * 128 + q * 32 + lane;
+            const int c_lo = n * 256 + half * 128;               // first of this thread's 128 columns within the launch
+            const uint32_t buf = n_acc & 1u;
+            const uint32_t taddr = tmem + lane_base + buf * 256 + half * 128;
+            int lab = -1;                                        // the label's place among the 128 columns
+            RowParam rp = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (MODE == STATS || MODE == PROBS) {
+                if (row < count) {
+                    lab = p.labels[row] - p.col0 - c_lo;
+                    if (MODE == PROBS) rp = p.rowp[row];
+                }
+            }
+            bool ok = mbar_wait_cluster(smem_u32(&bars->d_full[buf]), (n_acc >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            float run_max = -INFINITY, run_sum = 0.0f;
+#pragma unroll 1
+            for (int c0 = 0; c0 < 128; c0 += 32) {
+                uint32_t v[32];
+                tmem_ld_x32(taddr + c0, v);
+                tmem_wait_ld();
+                if (c0 == 96) {                                  // this warp's share of the accumulator is read
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_leader_tmem(smem_u32(&bars->d_empty[buf]), rank);
+                }
+                const int have = p.cols - (c_lo + c0);           // valid columns from here on
+                if (MODE == STATS || MODE == PROBS) {
+                    const int lk = lab - c0;
+                    const bool mine = lk >= 0 && lk < 32 && lk < have;
+                    if (__any_sync(0xFFFFFFFFu, mine)) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (mine && k == lk) {
+                                p.label_logit[row] = __uint_as_float(v[k]) * LOG2E;
+                                v[k] = 0xFF800000u;              // -infinity: no part of the sum over the others
+                            }
+                    }
+                    if (have < 32) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) if (k >= have) v[k] = 0xFF800000u;
+                    }
+                    if (MODE == STATS) {
+                        float top = -INFINITY;
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) top = fmaxf(top, __uint_as_float(v[k]));
+                        top *= LOG2E;
+                        const float now = fmaxf(run_max, top);
+                        if (now > -INFINITY) {
+                            run_sum *= ex2(run_max - now);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) run_sum += ex2(fmaf(__uint_as_float(v[k]), LOG2E, -now));
+                            run_max = now;
+                        } else {                                 // nothing but -infinity so far (or NaN, which the sum has to show)
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) if (isnan(__uint_as_float(v[k]))) run_sum = NAN;
+                        }
+                    } else {
+                        float e[32];
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) {
+                            const float x = fmaf(__uint_as_float(v[k]), LOG2E, -rp.r2);
+                            run_max = fmaxf(run_max, x);
+                            e[k] = ex2(x);
+                            run_sum += e[k];
+                            e[k] *= rp.w;
+                        }
+                        if (__any_sync(0xFFFFFFFFu, mine)) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) if (mine && k == lk) e[k] = rp.wl;
+                        }
+                        if (row >= count) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) e[k] = 0.0f;
+                        }
+                        uint4* dst = reinterpret_cast<uint4*>(p.out + row * p.ld_out + c_lo + c0);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            dst[k] = make_uint4(pack_bf16(e[8 * k], e[8 * k + 1]), pack_bf16(e[8 * k + 2], e[8 * k + 3]),
+                                                pack_bf16(e[8 * k + 4], e[8 * k + 5]), pack_bf16(e[8 * k + 6], e[8 * k + 7]));
+                    }
+                } else if (MODE == GRAD_H) {
+                    if (row < count) {
+                        float* dst = p.acc + ((int64_t)split * mt * 256 + row) * p.cols + c_lo + c0;
+#pragma unroll
+                        for (int k = 0; k < 32; k += 4) {
+                            if (k >= have) break;                // the width is a multiple of 8
+                            float4 x = make_float4(__uint_as_float(v[k]), __uint_as_float(v[k + 1]), __uint_as_float(v[k + 2]), __uint_as_float(v[k + 3]));
+                            if (kb0 == kb1) x = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (p.accumulate) {
+                                const float4 y = *reinterpret_cast<const float4*>(dst + k);
+                                x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                            }
+                            *reinterpret_cast<float4*>(dst + k) = x;
+                        }
+                    }
+                } else {
+                    if (row < p.rows) {
+                        __nv_bfloat16* dst = p.out + (p.col0 + row) * p.ld_out + c_lo + c0;
+                        const bool none = kb0 == kb1;            // no token carries a loss
+#pragma unroll
+                        for (int k = 0; k < 32; k += 8) {
+                            if (k >= have) break;
+                            uint4 o = make_uint4(pack_bf16(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), pack_bf16(__uint_as_float(v[k + 2]), __uint_as_float(v[k + 3])),
+                                                 pack_bf16(__uint_as_float(v[k + 4]), __uint_as_float(v[k + 5])), pack_bf16(__uint_as_float(v[k + 6]), __uint_as_float(v[k + 7])));
+                            if (none) o = make_uint4(0u, 0u, 0u, 0u);
+                            *reinterpret_cast<uint4*>(dst + k) = o;
+                        }
+                    }
+                }
+            }
+            if (MODE == STATS && row < count) p.stat[((int64_t)(p.tile0 + n) * 2 + half) * p.tpad + row] = make_float2(run_max, run_sum);
+            if (MODE == PROBS && row < count && p.psum != nullptr) {
+                p.psum[((int64_t)(p.tile0 + n) * 2 + half) * p.tpad + row] = run_sum;
+                if (run_max > LIMIT) *p.redo = 1;
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    if (warp == 1) { tc_fence_after(); tmem_dealloc_pair(tmem, 512); }
+}
+
+// ---- tokens that carry a loss ------------------------------------------------------------------------------------------
+
+// One block: place[t] = position of token t among the tokens with a label in [0, V), or -1; order = the inverse. Also how many
+// slices the hidden-state product is cut into along the vocabulary: as many as keep the CTA pairs busy (at least 95 %, four slices
+// at most where there are tiles enough, or as many as fill one round where there are few), within the `cap_tiles` row tiles the
+// workspace has room for.
+__global__ void __launch_bounds__(1024) loss_compact_kernel(const int64_t* __restrict__ labels, int64_t T, int32_t V, const float* __restrict__ weight,
+                                                            int32_t* __restrict__ order, int32_t* __restrict__ place, int32_t* __restrict__ out_labels,
+                                                            float* __restrict__ out_weight, float* __restrict__ loss, LossMeta* meta,
+                                                            int32_t pairs, int32_t col_tiles, int32_t cap_tiles)
+{
+    __shared__ int32_t warp_sum[32];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int32_t base = 0;
+    for (int64_t t0 = 0; t0 < T; t0 += 1024) {
+        const int64_t t = t0 + threadIdx.x;
+        const int64_t y = t < T ? labels[t] : -1;
+        const bool keep = y >= 0 && y < V;
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, keep);
+        if (lane == 0) warp_sum[warp] = __popc(mask);
+        __syncthreads();
+        int32_t before = base, all = 0;
+        for (int w = 0; w < 32; ++w) { const int32_t c = warp_sum[w]; before += w < warp ? c : 0; all += c; }
+        if (t < T) {
+            const int32_t at = before + __popc(mask & ((1u << lane) - 1u));
+            place[t] = keep ? at : -1;
+            if (keep) {
+                order[at] = (int32_t)t;
+                out_labels[at] = (int32_t)y;
+                out_weight[at] = weight != nullptr ? weight[t] : 1.0f;
+            } else {
+                loss[t] = 0.0f;
+            }
+        }
+        base += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        const int mt = (base + 255) / 256, tiles = mt * col_tiles;
+        int best = 1;
+        if (mt > 0) {
+            const int most = min(cap_tiles / mt, tiles >= pairs ? 4 : max(1, pairs / tiles));
+            if (tiles < pairs) best = max(1, most);
+            else {
+                float best_use = 0.0f;
+                for (int s = 1; s <= most && best_use < 0.95f; ++s) {
+                    const int items = tiles * s, rounds = (items + pairs - 1) / pairs;
+                    const float use = (float)items / (float)(rounds * pairs);
+                    if (use > best_use) { best_use = use; best = s; }
+                }
+            }
+        }
+        meta->count = base; meta->splits = best; meta->redo = 0;
+    }
+}
+
+// Rows of the tokens that carry a loss, in order; zeros behind the last up to a multiple of 128 (GRAD_W contracts over the rows).
+__global__ void loss_gather_kernel(const __nv_bfloat16* __restrict__ hidden, int64_t ld, int32_t width, const int32_t* __restrict__ order,
+                                   const LossMeta* __restrict__ meta, __nv_bfloat16* __restrict__ out)
+{
+    const int count = meta->count, vecs = width / 8;
+    const int64_t total = (int64_t)((count + 127) / 128 * 128) * vecs;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t r = i / vecs;
+        const int c = (int)(i - r * vecs);
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (r < count) x = __ldg(reinterpret_cast<const uint4*>(hidden + (int64_t)order[r] * ld) + c);
+        reinterpret_cast<uint4*>(out + r * width)[c] = x;
+    }
+}
+
+// ---- per-row work between the products -----------------------------------------------------------------------------------
+
+enum { ROW_REFERENCE = 0, ROW_FROM_STATS = 1, ROW_FROM_SUMS = 2 };
+
+struct RowArgs {
+    const LossMeta* meta;
+    const int32_t* gate;
+    int32_t kind, entries;                  // entries: 128-column stretches with a partial result
+    int64_t tpad;
+    const float2* stat;
+    const float* psum;
+    const float* label_logit;
+    const float* weight;
+    const int32_t* order;
+    RowParam* rowp;
+    float2* coef;                           // ROW_FROM_SUMS: w sigma(d), 1 / s
+    float* loss;
+};
+
+// 32 rows per block, eight threads per row that take every eighth stretch; joined in a fixed order.
+__global__ void __launch_bounds__(256) loss_rows_kernel(const RowArgs a)
+{
+    if (a.gate != nullptr && *a.gate == 0) return;
+    __shared__ float2 part[8][32];
+    const int lane = threadIdx.x & 31, seg = threadIdx.x >> 5;
+    const int count = a.meta->count;
+    for (int64_t r0 = (int64_t)blockIdx.x * 32; r0 < count; r0 += (int64_t)gridDim.x * 32) {
+        const int64_t row = r0 + lane;
+        float m = -INFINITY, s = 0.0f;
+        if (row < count) {
+            if (a.kind == ROW_FROM_SUMS) {
+                for (int i = seg; i < a.entries; i += 8) s += a.psum[(int64_t)i * a.tpad + row];
+            } else {
+                for (int i = seg; i < a.entries; i += 8) {
+                    const float2 x = a.stat[(int64_t)i * a.tpad + row];
+                    const float now = fmaxf(m, x.x);
+                    if (now > -INFINITY) { s = s * ex2(m - now) + x.y * ex2(x.x - now); m = now; }
+                    else s += x.y;                               // 0, or NaN
+                }
+            }
+        }
+        __syncthreads();
+        part[seg][lane] = make_float2(m, s);
+        __syncthreads();
+        if (seg == 0 && row < count) {
+            for (int j = 1; j < 8; ++j) {
+                const float2 x = part[j][lane];
+                if (a.kind == ROW_FROM_SUMS) { s += x.y; continue; }
+                const float now = fmaxf(m, x.x);
+                if (now > -INFINITY) { s = s * ex2(m - now) + x.y * ex2(x.x - now); m = now; }
+                else s += x.y;
+            }
+            if (a.kind == ROW_REFERENCE) {
+                a.rowp[row] = RowParam{m > -INFINITY ? m : 0.0f, 1.0f, 0.0f, 0.0f};
+                continue;
+            }
+            const float ref = a.kind == ROW_FROM_SUMS ? a.rowp[row].r2 : m;
+            const float w = a.weight[row], ly = a.label_logit[row];
+            const float others = s == 0.0f ? -INFINITY : ref + log2f(s);      // no other column has any weight (or there is none)
+            const float d = others - ly;
+            // log(1 + e^d) and the probability of the others
+            const float e = exp2f(-fabsf(d)), tail = log1pf(e);
+            float nll = d > 0.0f ? d * LN2 + tail : tail;
+            float sigma = d > 0.0f ? 1.0f / (1.0f + e) : e / (1.0f + e);
+            if (others == -INFINITY) { nll = ly == ly ? 0.0f : ly; sigma = nll; }
+            else if (d != d) { nll = d; sigma = d; }
+            a.loss[a.order[row]] = nll;
+            if (a.kind == ROW_FROM_SUMS) a.coef[row] = make_float2(w * sigma, s == 0.0f ? 0.0f : 1.0f / s);
+            else a.rowp[row] = RowParam{fmaxf(others, ly) + tail * LOG2E, w, -w * sigma, 0.0f};      // the full normaliser
+        }
+    }
+}
+
+// Gradient rows of all tokens: joins the slices of the vocabulary; zero for tokens without a loss. `sums` = the accumulator holds
+// sum exp2(l2 - r2) W_v over the other columns; otherwise the finished gradient.
+__global__ void loss_finish_kernel(const float* __restrict__ acc, int32_t width, const LossMeta* __restrict__ meta,
+                                   const int32_t* __restrict__ place, const int32_t* __restrict__ labels, const float2* __restrict__ coef, int32_t sums,
+                                   const __nv_bfloat16* __restrict__ weight, int64_t ld_weight, int64_t T, __nv_bfloat16* __restrict__ out, int64_t ld_out)
+{
+    const int vecs = width / 8, splits = meta->splits;
+    const int64_t slice = (int64_t)(meta->count + 255) / 256 * 256;
+    const int64_t total = T * vecs;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t t = i / vecs;
+        const int c = (int)(i - t * vecs) * 8;
+        const int r = place[t];
+        uint4 o = make_uint4(0u, 0u, 0u, 0u);
+        if (r >= 0) {
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = 0.0f;
+            for (int s = 0; s < splits; ++s) {
+                const float4* src = reinterpret_cast<const float4*>(acc + (s * slice + r) * width + c);
+                const float4 a = src[0], b = src[1];
+                x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w; x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
+            }
+            if (sums) {
+                const float2 k = coef[r];
+                const uint4 y = *reinterpret_cast<const uint4*>(weight + (int64_t)labels[r] * ld_weight + c);
+                const uint32_t yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[2 * j] = k.x * (x[2 * j] * k.y - __uint_as_float(yw[j] << 16));
+                    x[2 * j + 1] = k.x * (x[2 * j + 1] * k.y - __uint_as_float(yw[j] & 0xFFFF0000u));
+                }
+            }
+            o = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+        }
+        *reinterpret_cast<uint4*>(out + t * ld_out + c) = o;
+    }
+}
+
+unsigned grid_of(int64_t work, int threads)
+{
+    const int64_t blocks = (work + threads - 1) / threads, most = (int64_t)sm_count() * 8;
+    return (unsigned)(blocks < 1 ? 1 : blocks < most ? blocks : most);
+}
+
+template <int MODE>
+qless_status launch_gemm(const char* name, const CUtensorMap& a, const CUtensorMap& b, const GemmParams& p, int64_t max_items, cudaStream_t st)
+{
+    const size_t smem = 1024 + STAGES * 2 * HALF + sizeof(Bars);
+    QLESS_CUDA_TRY(cudaFuncSetAttribute(head_gemm_kernel<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    int64_t grid = sm_count() / 2 * 2;
+    if (grid > 2 * max_items) grid = 2 * max_items;
+    { ProfileScope ps(name, st);
+      head_gemm_kernel<MODE><<<(unsigned)grid, NTHREADS, smem, st>>>(a, b, p); }
+    count_launches(1);
+    QLESS_CUDA_TRY(cudaGetLastError());
+    return QLESS_OK;
+}
+
+}  // namespace
+
+LossPlan plan_loss(int64_t T, int32_t width, int32_t vocab, bool want_h, bool want_w)
+{
+    LossPlan pl;
+    pl.tpad = (T + 255) / 256 * 256;
+    const int64_t mt = pl.tpad / 256, pairs = sm_count() / 2, nt_h = (width + 255) / 256;
+    const int64_t tiles_v = ((int64_t)vocab + 255) / 256;
+    // Piece of the vocabulary whose probabilities are held at once: at most 256 MiB of bf16.
+    int64_t piece_tiles = ((int64_t)256 << 20) / (pl.tpad * 256 * 2);
+    if (piece_tiles < 1) piece_tiles = 1;
+    if (piece_tiles > tiles_v) piece_tiles = tiles_v;
+    pl.piece = (int32_t)(piece_tiles * 256);
+    pl.entries = (int32_t)(2 * tiles_v);
+    int64_t cap = pairs / nt_h < 16 ? pairs / nt_h : 16;       // slices where there is one row tile
+    if (cap < 2 * mt) cap = 2 * mt;
+    pl.cap_tiles = (int32_t)cap;
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t at = off; off += align_up(bytes, 256); return at; };
+    pl.meta_off = take(sizeof(LossMeta));
+    pl.order_off = take((size_t)pl.tpad * 4);
+    pl.place_off = take((size_t)pl.tpad * 4);
+    pl.label_off = take((size_t)pl.tpad * 4);
+    pl.weight_off = take((size_t)pl.tpad * 4);
+    pl.logit_off = take((size_t)pl.tpad * 4);
+    pl.coef_off = take((size_t)pl.tpad * 8);
+    pl.rowp_off = take((size_t)pl.tpad * sizeof(RowParam));
+    pl.stat_off = take((size_t)pl.entries * pl.tpad * 8);
+    pl.hidden_off = take((size_t)pl.tpad * width * 2);
+    pl.piece_off = (want_h || want_w) ? take((size_t)pl.tpad * pl.piece * 2) : 0;
+    pl.acc_off = want_h ? take((size_t)cap * 256 * width * 4) : 0;
+    pl.total = off + 256;
+    return pl;
+}
+
+qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st)
+{
+    LossMeta* meta = reinterpret_cast<LossMeta*>(ws + pl.meta_off);
+    int32_t* order = reinterpret_cast<int32_t*>(ws + pl.order_off);
+    int32_t* place = reinterpret_cast<int32_t*>(ws + pl.place_off);
+    int32_t* labels = reinterpret_cast<int32_t*>(ws + pl.label_off);
+    float* weight = reinterpret_cast<float*>(ws + pl.weight_off);
+    float* logit = reinterpret_cast<float*>(ws + pl.logit_off);
+    float2* coef = reinterpret_cast<float2*>(ws + pl.coef_off);
+    RowParam* rowp = reinterpret_cast<RowParam*>(ws + pl.rowp_off);
+    float2* stat = reinterpret_cast<float2*>(ws + pl.stat_off);
+    float* psum = reinterpret_cast<float*>(ws + pl.stat_off);       // the statistics are read before the sums are written, and again the other way round
+    __nv_bfloat16* hidden = reinterpret_cast<__nv_bfloat16*>(ws + pl.hidden_off);
+    __nv_bfloat16* piece = reinterpret_cast<__nv_bfloat16*>(ws + pl.piece_off);
+    float* acc = reinterpret_cast<float*>(ws + pl.acc_off);
+    const bool want_h = a.grad_hidden != nullptr, want_w = a.grad_weight != nullptr;
+    const int64_t mt = pl.tpad / 256, nt_h = (a.width + 255) / 256;
+    const int32_t tiles_v = (a.vocab + 255) / 256;
+
+    { ProfileScope ps("loss_compact", st);
+      loss_compact_kernel<<<1, 1024, 0, st>>>(a.labels, a.T, a.vocab, a.token_weight, order, place, labels, weight, a.loss, meta,
+                                              sm_count() / 2, (int32_t)nt_h, pl.cap_tiles); }
+    QLESS_CUDA_TRY(cudaGetLastError());
+    { ProfileScope ps("loss_gather", st);
+      loss_gather_kernel<<<grid_of(a.T * (a.width / 8), 256), 256, 0, st>>>(reinterpret_cast<const __nv_bfloat16*>(a.hidden), a.ld_hidden, a.width, order, meta, hidden); }
+    QLESS_CUDA_TRY(cudaGetLastError());
+    count_launches(2);
+
+    CUtensorMap tm_x, tm_w, tm_p;
+    qless_status s;
+    if ((s = make_tmap_2d_sw128(&tm_x, hidden, 2, a.width, pl.tpad, (uint64_t)a.width * 2, 64, 128)) != QLESS_OK) return s;
+    if ((s = make_tmap_2d_sw128(&tm_w, a.weight, 2, a.width, a.vocab, (uint64_t)a.ld_weight * 2, 64, 128)) != QLESS_OK) return s;
+    if (want_h || want_w)
+        if ((s = make_tmap_2d_sw128(&tm_p, piece, 2, pl.piece, pl.tpad, (uint64_t)pl.piece * 2, 64, 128)) != QLESS_OK) return s;
+
+    GemmParams base{};
+    base.meta = meta; base.tpad = pl.tpad; base.labels = labels; base.rowp = rowp; base.label_logit = logit; base.timeout_word = timeout_word;
+    auto stats = [&](int32_t cols, const int32_t* gate) {
+        GemmParams p = base;
+        p.gate = gate; p.cols = cols; p.k = a.width; p.stat = stat;
+        return launch_gemm<STATS>("loss_stats", tm_x, tm_w, p, mt * ((cols + 255) / 256), st);
+    };
+    auto rows = [&](int kind, int32_t entries, const int32_t* gate) {
+        RowArgs r{};
+        r.meta = meta; r.gate = gate; r.kind = kind; r.entries = entries; r.tpad = pl.tpad; r.stat = stat; r.psum = psum; r.label_logit = logit;
+        r.weight = weight; r.order = order; r.rowp = rowp; r.coef = coef; r.loss = a.loss;
+        { ProfileScope ps("loss_rows", st);
+          loss_rows_kernel<<<grid_of(a.T, 32), 256, 0, st>>>(r); }
+        count_launches(1);
+        QLESS_CUDA_TRY(cudaGetLastError());
+        return QLESS_OK;
+    };
+    auto pieces = [&](bool keep_sums, const int32_t* gate) {
+        for (int32_t v0 = 0; v0 < a.vocab; v0 += pl.piece) {
+            const int32_t cols = a.vocab - v0 < pl.piece ? a.vocab - v0 : pl.piece;
+            GemmParams p = base;
+            p.gate = gate; p.cols = cols; p.col0 = v0; p.k = a.width; p.out = piece; p.ld_out = pl.piece; p.tile0 = v0 / 256;
+            p.psum = keep_sums ? psum : nullptr; p.redo = &meta->redo;
+            qless_status e = launch_gemm<PROBS>("loss_probs", tm_x, tm_w, p, mt * ((cols + 255) / 256), st);
+            if (e != QLESS_OK) return e;
+            if (want_h) {
+                GemmParams g = base;
+                g.gate = gate; g.cols = a.width; g.col0 = v0; g.k = cols; g.acc = acc; g.accumulate = v0 > 0;
+                e = launch_gemm<GRAD_H>("loss_grad_hidden", tm_p, tm_w, g, pl.cap_tiles * nt_h, st);
+                if (e != QLESS_OK) return e;
+            }
+            if (want_w) {
+                GemmParams g = base;
+                g.gate = gate; g.cols = a.width; g.rows = cols; g.col0 = v0; g.out = reinterpret_cast<__nv_bfloat16*>(a.grad_weight); g.ld_out = a.ld_grad_weight;
+                e = launch_gemm<GRAD_W>("loss_grad_weight", tm_p, tm_x, g, (int64_t)((cols + 255) / 256) * nt_h, st);
+                if (e != QLESS_OK) return e;
+            }
+        }
+        return QLESS_OK;
+    };
+
+    if (want_w || !want_h) {
+        if ((s = stats(a.vocab, nullptr)) != QLESS_OK) return s;
+        if ((s = rows(ROW_FROM_STATS, pl.entries, nullptr)) != QLESS_OK) return s;
+        if (want_w && (s = pieces(false, nullptr)) != QLESS_OK) return s;
+    } else {
+        const int32_t first = a.vocab < 256 ? a.vocab : 256;
+        if ((s = stats(first, nullptr)) != QLESS_OK) return s;
+        if ((s = rows(ROW_REFERENCE, 2, nullptr)) != QLESS_OK) return s;
+        if ((s = pieces(true, nullptr)) != QLESS_OK) return s;
+        if (tiles_v > 1) {                                      // a reference from 256 columns may be too low; one from all of them is not
+            if ((s = stats(a.vocab, &meta->redo)) != QLESS_OK) return s;
+            if ((s = rows(ROW_REFERENCE, pl.entries, &meta->redo)) != QLESS_OK) return s;
+            if ((s = pieces(true, &meta->redo)) != QLESS_OK) return s;
+        }
+        if ((s = rows(ROW_FROM_SUMS, pl.entries, nullptr)) != QLESS_OK) return s;
+    }
+    if (want_h) {
+        { ProfileScope ps("loss_finish", st);
+          loss_finish_kernel<<<grid_of(a.T * (a.width / 8), 256), 256, 0, st>>>(acc, a.width, meta, place, labels, coef, want_w ? 0 : 1,
+                                                                               reinterpret_cast<const __nv_bfloat16*>(a.weight), a.ld_weight, a.T,
+                                                                               reinterpret_cast<__nv_bfloat16*>(a.grad_hidden), a.ld_grad_hidden); }
+        count_launches(1);
+        QLESS_CUDA_TRY(cudaGetLastError());
+    }
+    return QLESS_OK;
+}
+
+}  // namespace qless

@@ -114,4 +114,19 @@ struct LoraArgs {
 };
 qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st);
 
+// Softmax cross entropy of a language model's head with its gradient (lm_loss.cu).
+struct LossPlan {
+    int64_t tpad;
+    int32_t piece, entries, cap_tiles;
+    size_t meta_off, order_off, place_off, label_off, weight_off, logit_off, coef_off, rowp_off, stat_off, hidden_off, piece_off, acc_off, total;
+};
+LossPlan plan_loss(int64_t T, int32_t width, int32_t vocab, bool want_h, bool want_w);
+struct LossArgs {
+    const void* hidden; const void* weight; const int64_t* labels; const float* token_weight;
+    int64_t T, ld_hidden, ld_weight, ld_grad_hidden, ld_grad_weight;
+    int32_t width, vocab;
+    float* loss; void* grad_hidden; void* grad_weight;
+};
+qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st);
+
 }  // namespace qless
