@@ -23,14 +23,39 @@ constexpr int LANE_CH = 8;                  // channels per lane
 constexpr int SEG = 32 * LANE_CH;           // channels per warp and token
 constexpr int UNROLL = 4;                   // tokens per warp and step
 
-template <typename T> struct Chunk;
-template <> struct Chunk<float> {
-    static __device__ __forceinline__ void load(const float* p, float (&v)[LANE_CH])
+struct ActParams {
+    int64_t tokens, ld_x, ld_codes, ld_scales;
+    int32_t width, group, segments;
+    int64_t units;                          // (token quads) x segments
+};
+
+__device__ __forceinline__ float max_nan_abs(float a, float b)      // max(a, |b|), NaN if either is
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
+}
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    const __nv_bfloat162 z = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&z);
+}
+
+// Eight channels of a lane as loaded: 8 words of fp32, or 4 words of two bf16.
+template <typename T> struct Raw;
+template <> struct Raw<float> {
+    uint32_t w[8];
+    __device__ __forceinline__ void load(const float* p)
     {
-        const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p)), b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
     }
-    static __device__ __forceinline__ float one(const float* p) { return *p; }
+    __device__ __forceinline__ void set(int i, float v) { w[i] = __float_as_uint(v); }
+    __device__ __forceinline__ float get(int i) const { return __uint_as_float(w[i]); }
+    static constexpr int WORDS = 8;
+    static __device__ __forceinline__ float read(const float* p) { return *p; }
     static __device__ __forceinline__ void store(float* p, const float (&v)[LANE_CH])
     {
         __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
@@ -38,111 +63,125 @@ template <> struct Chunk<float> {
     }
     static __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 };
-template <> struct Chunk<__nv_bfloat16> {
-    static __device__ __forceinline__ void load(const __nv_bfloat16* p, float (&v)[LANE_CH])
+template <> struct Raw<__nv_bfloat16> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const __nv_bfloat16* p)
     {
         const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p));
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
     }
-    static __device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+    __device__ __forceinline__ void set(int i, float v)      // v is a bf16 value; the words start at 0
+    {
+        w[i >> 1] |= (i & 1) ? (__float_as_uint(v) & 0xFFFF0000u) : (__float_as_uint(v) >> 16);
+    }
+    __device__ __forceinline__ float get(int i) const { return (i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]); }
+    static constexpr int WORDS = 4;
+    static __device__ __forceinline__ float read(const __nv_bfloat16* p) { return __bfloat162float(*p); }
     static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&v)[LANE_CH])
     {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 z = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&z);
-        }
-        __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
+        __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])));
     }
     static __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 };
 
-struct ActParams {
-    int64_t tokens, ld_x, ld_codes, ld_scales;
-    int32_t width, group, segments;
-    int64_t units;                          // (token quads) x segments
+// The division by a run-time number of segments is done once per warp; the loop steps (quad, segment) by constant amounts.
+struct Walk {
+    int64_t quad; int32_t seg; int64_t dq; int32_t ds;
+    __device__ __forceinline__ Walk(const ActParams& p)
+    {
+        const int64_t first = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5), step = (int64_t)gridDim.x * (THREADS / 32);
+        quad = first / p.segments; seg = (int32_t)(first - quad * p.segments);
+        dq = step / p.segments; ds = (int32_t)(step - dq * p.segments);
+    }
+    __device__ __forceinline__ void next(const ActParams& p)
+    {
+        quad += dq; seg += ds;
+        if (seg >= p.segments) { seg -= p.segments; ++quad; }
+    }
 };
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, int GROUP>
 __global__ void __launch_bounds__(THREADS) activation_quantize_kernel(const T* __restrict__ x, int8_t* __restrict__ codes,
                                                                       uint8_t* __restrict__ scales, const ActParams p)
 {
+    constexpr int LANES = GROUP / LANE_CH;                              // neighbouring lanes that share a step
     const int lane = threadIdx.x & 31;
-    const int lanes_per_group = p.group / LANE_CH;
-    const int64_t warps = (int64_t)gridDim.x * (THREADS / 32);
-    for (int64_t u = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5); u < p.units; u += warps) {
-        const int64_t quad = u / p.segments;
-        const int c = (int)(u - quad * p.segments) * SEG + lane * LANE_CH;
+    const int64_t quads = (p.tokens + UNROLL - 1) / UNROLL;
+    for (Walk u(p); u.quad < quads; u.next(p)) {
+        const int c = u.seg * SEG + lane * LANE_CH;
         const int have = min(LANE_CH, p.width - c);                     // channels of this lane (<= 0: none)
-        float v[UNROLL][LANE_CH];
+        Raw<T> r[UNROLL];
 #pragma unroll
         for (int k = 0; k < UNROLL; ++k) {
-            const int64_t t = quad * UNROLL + k;
+            const int64_t t = u.quad * UNROLL + k;
 #pragma unroll
-            for (int i = 0; i < LANE_CH; ++i) v[k][i] = 0.0f;
+            for (int i = 0; i < Raw<T>::WORDS; ++i) r[k].w[i] = 0u;
             if (t < p.tokens) {
                 const T* src = x + t * p.ld_x + c;
-                if (VEC && have == LANE_CH) Chunk<T>::load(src, v[k]);
+                if (VEC && have == LANE_CH) r[k].load(src);
                 else {
 #pragma unroll
-                    for (int i = 0; i < LANE_CH; ++i) if (i < have) v[k][i] = Chunk<T>::one(src + i);
+                    for (int i = 0; i < LANE_CH; ++i) if (i < have) r[k].set(i, Raw<T>::read(src + i));
                 }
             }
         }
 #pragma unroll
         for (int k = 0; k < UNROLL; ++k) {
-            const int64_t t = quad * UNROLL + k;
-            uint32_t top = 0;                                           // |x| as bits: ordered, NaN above infinity above the rest
+            const int64_t t = u.quad * UNROLL + k;
+            float a = 0.0f;
 #pragma unroll
-            for (int i = 0; i < LANE_CH; ++i) top = max(top, __float_as_uint(v[k][i]) & 0x7FFFFFFFu);
-            for (int s = 1; s < lanes_per_group; s <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, s));
+            for (int i = 0; i < LANE_CH; ++i) a = max_nan_abs(a, r[k].get(i));
+#pragma unroll
+            for (int s = 1; s < LANES; s <<= 1) a = max_nan_abs(a, __shfl_xor_sync(0xFFFFFFFFu, a, s));
+            const uint32_t top = __float_as_uint(a);
             // a = 1.m * 2^E: 127 * 2^(E-6) covers it unless 1.m > 127/64
             int e = (int)(top >> 23) - 127 - 6 + ((top & 0x7FFFFFu) > 0x7E0000u ? 1 : 0);
+            const bool over = e > 121;                                  // above 127 * 2^121 (or not finite)
             e = max(-120, min(121, e));
             const bool finite = top < 0x7F800000u;
-            const float inv = finite ? __uint_as_float((uint32_t)(127 - e) << 23) : 0.0f;
-            uint32_t w[2] = {0u, 0u};
+            const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+            // Adding 1.5 * 2^23 rounds to a whole number, half to even, and leaves it in two's complement in the low bits (the product
+            // is exact, so the fused multiply-add rounds once).
+            uint32_t q[LANE_CH];
 #pragma unroll
-            for (int i = 0; i < LANE_CH; ++i) {
-                // the upper clamp acts only where a lies above 127 * 2^121, the largest value that the codes can stand for
-                const int q = finite ? max(-127, min(127, __float2int_rn(v[k][i] * inv))) : 0;
-                w[i >> 2] |= ((uint32_t)q & 0xFFu) << (8 * (i & 3));
+            for (int i = 0; i < LANE_CH; ++i) q[i] = __float_as_uint(fmaf(r[k].get(i), inv, 12582912.0f));
+            if (over) {
+#pragma unroll
+                for (int i = 0; i < LANE_CH; ++i) q[i] = finite ? (uint32_t)max(-127, min(127, __float2int_rn(r[k].get(i) * inv))) : 0u;
             }
+            const uint32_t w0 = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+            const uint32_t w1 = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
             if (t < p.tokens && have > 0) {
                 int8_t* dst = codes + t * p.ld_codes + c;
-                if (VEC && have == LANE_CH) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+                if (VEC && have == LANE_CH) *reinterpret_cast<uint2*>(dst) = make_uint2(w0, w1);
                 else {
 #pragma unroll
-                    for (int i = 0; i < LANE_CH; ++i) if (i < have) dst[i] = (int8_t)(w[i >> 2] >> (8 * (i & 3)));
+                    for (int i = 0; i < LANE_CH; ++i) if (i < have) dst[i] = (int8_t)((i < 4 ? w0 : w1) >> (8 * (i & 3)));
                 }
-                if (lane % lanes_per_group == 0) scales[t * p.ld_scales + c / p.group] = finite ? (uint8_t)(e + 127) : (uint8_t)0xFF;
+                if (lane % LANES == 0) scales[t * p.ld_scales + c / GROUP] = finite ? (uint8_t)(e + 127) : (uint8_t)0xFF;
             }
         }
     }
 }
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, int GROUP>
 __global__ void __launch_bounds__(THREADS) activation_dequantize_kernel(const int8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                                         T* __restrict__ out, const ActParams p)
 {
     const int lane = threadIdx.x & 31;
-    const int64_t warps = (int64_t)gridDim.x * (THREADS / 32);
-    for (int64_t u = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5); u < p.units; u += warps) {
-        const int64_t quad = u / p.segments;
-        const int c = (int)(u - quad * p.segments) * SEG + lane * LANE_CH;
+    const int64_t quads = (p.tokens + UNROLL - 1) / UNROLL;
+    for (Walk u(p); u.quad < quads; u.next(p)) {
+        const int c = u.seg * SEG + lane * LANE_CH;
         const int have = min(LANE_CH, p.width - c);
         if (have <= 0) continue;
         uint32_t w[UNROLL][2], step[UNROLL];
 #pragma unroll
         for (int k = 0; k < UNROLL; ++k) {
-            const int64_t t = quad * UNROLL + k;
+            const int64_t t = u.quad * UNROLL + k;
             w[k][0] = w[k][1] = step[k] = 0u;
             if (t < p.tokens) {
                 const int8_t* src = codes + t * p.ld_codes + c;
-                step[k] = scales[t * p.ld_scales + c / p.group];
+                step[k] = scales[t * p.ld_scales + c / GROUP];
                 if (VEC && have == LANE_CH) {
                     const uint2 a = *reinterpret_cast<const uint2*>(src);
                     w[k][0] = a.x; w[k][1] = a.y;
@@ -154,17 +193,19 @@ __global__ void __launch_bounds__(THREADS) activation_dequantize_kernel(const in
         }
 #pragma unroll
         for (int k = 0; k < UNROLL; ++k) {
-            const int64_t t = quad * UNROLL + k;
+            const int64_t t = u.quad * UNROLL + k;
             if (t >= p.tokens) continue;
             const float s = __uint_as_float(step[k] == 0xFFu ? 0x7FC00000u : step[k] << 23);      // NaN, or 2^(byte - 127)
+            // The byte code + 128 under the bits of 2^23 is the number 2^23 + 128 + code (integer conversions run at a quarter of the rate).
             float v[LANE_CH];
 #pragma unroll
-            for (int i = 0; i < LANE_CH; ++i) v[i] = (float)(int8_t)(w[k][i >> 2] >> (8 * (i & 3))) * s;
+            for (int i = 0; i < LANE_CH; ++i)
+                v[i] = (__uint_as_float(__byte_perm(w[k][i >> 2] ^ 0x80808080u, 0x4B000000u, 0x7440 | (i & 3))) - 8388736.0f) * s;
             T* dst = out + t * p.ld_x + c;
-            if (VEC && have == LANE_CH) Chunk<T>::store(dst, v);
+            if (VEC && have == LANE_CH) Raw<T>::store(dst, v);
             else {
 #pragma unroll
-                for (int i = 0; i < LANE_CH; ++i) if (i < have) Chunk<T>::put(dst + i, v[i]);
+                for (int i = 0; i < LANE_CH; ++i) if (i < have) Raw<T>::put(dst + i, v[i]);
             }
         }
     }
@@ -191,6 +232,25 @@ bool vectors_fit(const void* x, int64_t ld_x, size_t esize, const void* codes, i
     return reinterpret_cast<uintptr_t>(x) % 16 == 0 && (ld_x * esize) % 16 == 0 && reinterpret_cast<uintptr_t>(codes) % 8 == 0 && ld_codes % 8 == 0;
 }
 
+template <typename T, bool VEC>
+void quantize_group(const void* x, int8_t* codes, uint8_t* scales, const ActParams& p, cudaStream_t st)
+{
+    const T* src = reinterpret_cast<const T*>(x);
+    const unsigned grid = grid_for(p);
+    if (p.group == 32) activation_quantize_kernel<T, VEC, 32><<<grid, THREADS, 0, st>>>(src, codes, scales, p);
+    else if (p.group == 64) activation_quantize_kernel<T, VEC, 64><<<grid, THREADS, 0, st>>>(src, codes, scales, p);
+    else activation_quantize_kernel<T, VEC, 128><<<grid, THREADS, 0, st>>>(src, codes, scales, p);
+}
+template <typename T, bool VEC>
+void dequantize_group(const int8_t* codes, const uint8_t* scales, void* out, const ActParams& p, cudaStream_t st)
+{
+    T* dst = reinterpret_cast<T*>(out);
+    const unsigned grid = grid_for(p);
+    if (p.group == 32) activation_dequantize_kernel<T, VEC, 32><<<grid, THREADS, 0, st>>>(codes, scales, dst, p);
+    else if (p.group == 64) activation_dequantize_kernel<T, VEC, 64><<<grid, THREADS, 0, st>>>(codes, scales, dst, p);
+    else activation_dequantize_kernel<T, VEC, 128><<<grid, THREADS, 0, st>>>(codes, scales, dst, p);
+}
+
 }  // namespace
 
 cudaError_t launch_activation_quantize(const void* x, qless_dtype dtype, int64_t tokens, int32_t width, int64_t ld_x, int32_t group,
@@ -198,16 +258,8 @@ cudaError_t launch_activation_quantize(const void* x, qless_dtype dtype, int64_t
 {
     const ActParams p = make_params(tokens, width, group, ld_x, ld_codes, ld_scales);
     const bool vec = vectors_fit(x, ld_x, dtype == QLESS_F32 ? 4 : 2, codes, ld_codes);
-    const unsigned grid = grid_for(p);
-    if (dtype == QLESS_F32) {
-        const float* src = reinterpret_cast<const float*>(x);
-        if (vec) activation_quantize_kernel<float, true><<<grid, THREADS, 0, st>>>(src, codes, scales, p);
-        else activation_quantize_kernel<float, false><<<grid, THREADS, 0, st>>>(src, codes, scales, p);
-    } else {
-        const __nv_bfloat16* src = reinterpret_cast<const __nv_bfloat16*>(x);
-        if (vec) activation_quantize_kernel<__nv_bfloat16, true><<<grid, THREADS, 0, st>>>(src, codes, scales, p);
-        else activation_quantize_kernel<__nv_bfloat16, false><<<grid, THREADS, 0, st>>>(src, codes, scales, p);
-    }
+    if (dtype == QLESS_F32) { if (vec) quantize_group<float, true>(x, codes, scales, p, st); else quantize_group<float, false>(x, codes, scales, p, st); }
+    else { if (vec) quantize_group<__nv_bfloat16, true>(x, codes, scales, p, st); else quantize_group<__nv_bfloat16, false>(x, codes, scales, p, st); }
     count_launches(1);
     return cudaGetLastError();
 }
@@ -217,16 +269,8 @@ cudaError_t launch_activation_dequantize(const int8_t* codes, int64_t ld_codes, 
 {
     const ActParams p = make_params(tokens, width, group, ld_out, ld_codes, ld_scales);
     const bool vec = vectors_fit(out, ld_out, dtype == QLESS_F32 ? 4 : 2, codes, ld_codes);
-    const unsigned grid = grid_for(p);
-    if (dtype == QLESS_F32) {
-        float* dst = reinterpret_cast<float*>(out);
-        if (vec) activation_dequantize_kernel<float, true><<<grid, THREADS, 0, st>>>(codes, scales, dst, p);
-        else activation_dequantize_kernel<float, false><<<grid, THREADS, 0, st>>>(codes, scales, dst, p);
-    } else {
-        __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(out);
-        if (vec) activation_dequantize_kernel<__nv_bfloat16, true><<<grid, THREADS, 0, st>>>(codes, scales, dst, p);
-        else activation_dequantize_kernel<__nv_bfloat16, false><<<grid, THREADS, 0, st>>>(codes, scales, dst, p);
-    }
+    if (dtype == QLESS_F32) { if (vec) dequantize_group<float, true>(codes, scales, out, p, st); else dequantize_group<float, false>(codes, scales, out, p, st); }
+    else { if (vec) dequantize_group<__nv_bfloat16, true>(codes, scales, out, p, st); else dequantize_group<__nv_bfloat16, false>(codes, scales, out, p, st); }
     count_launches(1);
     return cudaGetLastError();
 }

@@ -187,12 +187,13 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                     if (!mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t a = smem_u32(smem + (size_t)ring.slot * 2 * HALF), b = a + HALF;
+                    // made once per stage, advanced by constants (units of 16 bytes)
+                    const uint64_t a0 = A_MN ? make_smem_desc_mn_sw128(a, 16384) : make_smem_desc_sw128(a);
+                    const uint64_t b0 = B_MN ? make_smem_desc_mn_sw128(b, 16384) : make_smem_desc_sw128(b);
+                    mma_f16_ss_pair(d, a0, b0, idesc, kb > kb0);
 #pragma unroll
-                    for (int k = 0; k < KB / 16; ++k) {
-                        const uint64_t ad = A_MN ? make_smem_desc_mn_sw128(a + k * 2048, 16384) : make_smem_desc_sw128(a + (k >> 2) * 16384) + (uint64_t)((k & 3) * 2);
-                        const uint64_t bd = B_MN ? make_smem_desc_mn_sw128(b + k * 2048, 16384) : make_smem_desc_sw128(b + (k >> 2) * 16384) + (uint64_t)((k & 3) * 2);
-                        mma_f16_ss_pair(d, ad, bd, idesc, kb > kb0 || k > 0);
-                    }
+                    for (int k = 1; k < KB / 16; ++k)
+                        mma_f16_ss_pair(d, a0 + (uint64_t)(A_MN ? k * 128 : (k >> 2) * 1024 + (k & 3) * 2), b0 + (uint64_t)(B_MN ? k * 128 : (k >> 2) * 1024 + (k & 3) * 2), idesc, 1u);
                     mma_commit_pair(smem_u32(&bars->empty[ring.slot]));
                 }
                 if (ok) mma_commit_pair(smem_u32(&bars->d_full[buf]));

@@ -36,8 +36,10 @@ constexpr int TILE = 256;                   // (2) channels per item
 struct FactorParams {
     int64_t T, ld_scales;
     const uint8_t* scales;
-    float* part;                            // [2][slices][T][N64]: 0 = H, 1 = U
-    int32_t in, out, group, nr, n64, slices, kb_x, kb_y, stages;      // kb_*: channel blocks per slice
+    float* part;                            // [2][slices][T][N64]: 0 = H, 1 = U (more than one slice)
+    __nv_bfloat16* fac;                     // [2][T][parts][N64] (one slice)
+    float scaling;
+    int32_t in, out, group, nr, n64, parts, slices, kb_x, kb_y, stages;      // kb_*: channel blocks per slice
     int32_t token_tiles;
     int64_t items;
     unsigned int* timeout_word;
@@ -49,7 +51,7 @@ struct OuterParams {
     int64_t ld_scales, ld_grads, items;
     void* grads;
     float* part;                            // [slots][rank * (in + out)]
-    int32_t in, out, rank, group, nr, n64, parts, tiles_x, tiles, stages;
+    int32_t in, out, rank, group, nr, tiles_x, tiles, stages;
     unsigned int* timeout_word;
 };
 
@@ -79,11 +81,22 @@ __device__ __forceinline__ void expand4(uint32_t w, uint32_t step2, uint32_t& lo
 }
 __device__ __forceinline__ uint32_t step_bf16x2(uint32_t byte) { return (byte << 7) | (byte << 23); }      // 0xFF: infinity, and 0 * infinity = NaN
 
-__device__ __forceinline__ void init_barriers(Bars* b, int ready_count)
+// The leading bf16 term of two fp32 numbers, packed; what it leaves of them stays in a and b. An infinite or NaN number is its own
+// term and leaves nothing.
+__device__ __forceinline__ uint32_t split_term(float& a, float& b)
+{
+    const __nv_bfloat162 z = __floats2bfloat162_rn(a, b);
+    const float x = __low2float(z), y = __high2float(z);
+    a = fabsf(x) < INFINITY ? a - x : 0.0f;
+    b = fabsf(y) < INFINITY ? b - y : 0.0f;
+    return *reinterpret_cast<const uint32_t*>(&z);
+}
+
+__device__ __forceinline__ void init_barriers(Bars* b)
 {
     for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(smem_u32(&b->full[s]), 1); mbar_init(smem_u32(&b->empty[s]), 1); }
     for (int s = 0; s < 2; ++s) {
-        mbar_init(smem_u32(&b->ready[s]), ready_count);
+        mbar_init(smem_u32(&b->ready[s]), 4);
         mbar_init(smem_u32(&b->conv_empty[s]), 1);
         mbar_init(smem_u32(&b->d_full[s]), 1);
         mbar_init(smem_u32(&b->d_empty[s]), 4);
@@ -116,7 +129,7 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
     const uint32_t nS = (uint32_t)p.stages;
 
     if (threadIdx.x == 0) {
-        init_barriers(bars, 4);
+        init_barriers(bars);
         prefetch_tmap(&tm_codes); prefetch_tmap(&tm_dy); prefetch_tmap(&tm_a); prefetch_tmap(&tm_b);
     }
     if (warp == 1) { tmem_alloc(smem_u32(&bars->tmem_base), 512); tmem_relinquish(); }
@@ -177,25 +190,28 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
                 if (!mbar_wait(smem_u32(&bars->d_empty[buf]), ((n >> 1) & 1u) ^ 1u, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
                 tc_fence_after();
                 for (int kb = kb0; kb < kb1; ++kb, ring.next(nS)) {
-                    if (!mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                    if (!mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_MMA) ||
+                        !mbar_wait(smem_u32(&bars->ready[conv.slot]), conv.parity, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                    tc_fence_after();
                     const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
+                    // Descriptors are made once per stage and advanced by constants (addresses in units of 16 bytes): made anew for every
+                    // product they took 180 clocks of this thread where the product takes 48.
                     if (is_x) {
-                        if (!mbar_wait(smem_u32(&bars->ready[conv.slot]), conv.parity, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
-                        tc_fence_after();
                         const uint32_t a = tmem + 256 + conv.slot * 64;
+                        const uint64_t b0 = make_smem_desc_sw128(op), b1 = make_smem_desc_sw128(op + p.n64 * 128);
+                        mma_f16_ts(d, a, b0, idesc_x, kb > kb0);
 #pragma unroll
-                        for (int k = 0; k < CH / 16; ++k)
-                            mma_f16_ts(d, a + k * 8, make_smem_desc_sw128(op + (k >> 2) * p.n64 * 128) + (uint64_t)((k & 3) * 2), idesc_x, kb > kb0 || k > 0);
-                        mma_commit(smem_u32(&bars->conv_empty[conv.slot]));
-                        conv.next(2);
+                        for (int k = 1; k < CH / 16; ++k) mma_f16_ts(d, a + k * 8, (k < 4 ? b0 : b1) + (uint64_t)((k & 3) * 2), idesc_x, 1u);
                     } else {
-                        tc_fence_after();
+                        const uint64_t a0 = make_smem_desc_sw128(big), b0 = make_smem_desc_mn_sw128(op, 16384);
+                        mma_f16_ss(d, a0, b0, idesc_y, kb > kb0);
 #pragma unroll
-                        for (int k = 0; k < CH / 16; ++k)
-                            mma_f16_ss(d, make_smem_desc_sw128(big + (k >> 2) * 16384) + (uint64_t)((k & 3) * 2),
-                                       make_smem_desc_mn_sw128(op + k * 2048, 16384), idesc_y, kb > kb0 || k > 0);
+                        for (int k = 1; k < CH / 16; ++k)
+                            mma_f16_ss(d, a0 + (uint64_t)((k >> 2) * 1024 + (k & 3) * 2), b0 + (uint64_t)(k * 128), idesc_y, 1u);
                     }
                     mma_commit(smem_u32(&bars->empty[ring.slot]));
+                    mma_commit(smem_u32(&bars->conv_empty[conv.slot]));
+                    conv.next(2);
                 }
                 if (ok) mma_commit(smem_u32(&bars->d_full[buf]));
             }
@@ -203,7 +219,10 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
             mbar_wait_quiet(smem_u32(&bars->drain), 0u);
         }
     } else if (warp < 10) {
-        // Converters: thread = token = TMEM lane; warps 2-5 and 6-9 take alternate blocks of codes.
+        // Converters: thread = token = TMEM lane; warps 2-5 and 6-9 take alternate blocks, so that the barrier round trips of one
+        // overlap the work on the next. Every block passes through them, those of dY untouched: a group may look at a stage's barrier
+        // only once the stage's previous use is over (a parity would otherwise be mistaken for that of two uses before), which
+        // it knows from the products of its own previous block being done.
         const int row = (warp & 3) * 32 + lane;
         const uint32_t grp = warp >= 6 ? 1u : 0u;
         const int groups = (p.in + p.group - 1) / p.group;
@@ -212,25 +231,38 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
         for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
             int slice, kb0, kb1; bool is_x; int64_t tile;
             item_of(item, slice, is_x, tile, kb0, kb1);
-            if (!is_x) { for (int kb = kb0; kb < kb1; ++kb) ring.next(nS); continue; }
             const int64_t t = tile * 128 + row;
             const uint8_t* sc = p.scales + t * p.ld_scales;
-            for (int kb = kb0; kb < kb1 && ok; ++kb, ring.next(nS), conv.next(2)) {
-                if (conv.slot != grp) continue;
-                uint32_t step[4];                              // the 128 channels lie in 4, 2 or 1 groups
+            auto load_steps = [&](int kb, uint32_t (&v)[4]) {       // the 128 channels lie in 4, 2 or 1 groups
                 const int g0 = kb * CH / p.group, per = CH / p.group;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) step[i] = (t < p.T && i < per && g0 + i < groups) ? sc[g0 + i] : 0u;
-                ok = mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_UNPACK);
+                for (int i = 0; i < 4; ++i) v[i] = (t < p.T && i < per && g0 + i < groups) ? __ldg(sc + g0 + i) : 0u;
+            };
+            uint32_t ahead[4] = {0u, 0u, 0u, 0u};
+            bool loaded = false;
+            for (int kb = kb0; kb < kb1 && ok; ++kb, ring.next(nS), conv.next(2)) {
+                if (conv.slot != grp) continue;
+                uint32_t step[4];
+                if (is_x) {
+                    if (loaded) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) step[i] = ahead[i];
+                    } else load_steps(kb, step);
+                    loaded = kb + 2 < kb1;                     // this group's next block: its steps are requested one block early
+                    if (loaded) load_steps(kb + 2, ahead);
+                }
+                ok = mbar_wait(smem_u32(&bars->conv_empty[conv.slot]), conv.parity ^ 1u, abort_flag, p.timeout_word, TO_UNPACK) &&
+                     mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_UNPACK);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
+                if (!is_x) {
+                    if (lane == 0) mbar_arrive(smem_u32(&bars->ready[conv.slot]));
+                    continue;
+                }
                 const uint4* src = reinterpret_cast<const uint4*>(smem + (size_t)ring.slot * stage_bytes + row * CH);
                 uint4 raw[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) raw[j] = src[j ^ (row & 7)];
-                ok = mbar_wait(smem_u32(&bars->conv_empty[conv.slot]), conv.parity ^ 1u, abort_flag, p.timeout_word, TO_UNPACK);
-                ok = __all_sync(0xFFFFFFFFu, ok);
-                if (!ok) break;
                 tc_fence_after();
                 const uint32_t dst = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 256 + conv.slot * 64;
 #pragma unroll
@@ -266,18 +298,34 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
             if (!ok) break;
             tc_fence_after();
             const int64_t t = tile * 128 + row;
-            float* dst = p.part + (((int64_t)(is_x ? 0 : 1) * p.slices + slice) * p.T + t) * p.n64;
+            const int64_t kind = is_x ? 0 : 1;
             for (int c0 = 0; c0 < p.nr; c0 += 32) {
                 uint32_t v[32];
                 tmem_ld_x32(tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 128 + c0, v);
                 tmem_wait_ld();
-                if (t < p.T) {
+                if (kb1 == kb0) {                              // a slice beyond the last channel block
 #pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-                        float4 o = make_float4(__uint_as_float(v[j]), __uint_as_float(v[j + 1]), __uint_as_float(v[j + 2]), __uint_as_float(v[j + 3]));
-                        if (kb1 == kb0) o = make_float4(0.f, 0.f, 0.f, 0.f);       // a slice beyond the last channel block
-                        if (c0 + j < p.nr) *reinterpret_cast<float4*>(dst + c0 + j) = o;
-                    }
+                    for (int j = 0; j < 32; ++j) v[j] = 0u;
+                }
+                if (t >= p.T) continue;
+                if (p.slices == 1) {
+                    float x[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(v[j]) * p.scaling;
+                    __nv_bfloat16* dst = p.fac + (kind * p.T + t) * p.parts * p.n64 + c0;
+                    for (int q = 0; q < p.parts; ++q, dst += p.n64)
+#pragma unroll
+                        for (int j = 0; j < 32; j += 8) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) w[k] = split_term(x[j + 2 * k], x[j + 2 * k + 1]);
+                            if (c0 + j < p.nr) *reinterpret_cast<uint4*>(dst + j) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                } else {
+                    float* dst = p.part + ((kind * p.slices + slice) * p.T + t) * p.n64 + c0;
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4)
+                        if (c0 + j < p.nr) *reinterpret_cast<uint4*>(dst + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
                 }
             }
             tc_fence_before();
@@ -290,7 +338,7 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
     if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, 512); }
 }
 
-// Adds the channel slices, multiplies by the adapter's scale and splits the fp32 factor into `parts` bf16 terms that add up to
+// Several channel slices: adds them, multiplies by the adapter's scale and splits the fp32 factor into `parts` bf16 terms that add up to
 // it (8 bits each): fac [2][T][parts][n64].
 __global__ void lora_split_kernel(const float* __restrict__ part, __nv_bfloat16* __restrict__ fac, int64_t T, int32_t n64, int32_t nr,
                                   int32_t slices, int32_t parts, float scaling)
@@ -310,14 +358,8 @@ __global__ void lora_split_kernel(const float* __restrict__ part, __nv_bfloat16*
         float v[4] = {x.x * scaling, x.y * scaling, x.z * scaling, x.w * scaling};
         __nv_bfloat16* dst = fac + row * parts * n64 + c;
         for (int q = 0; q < parts; ++q) {
-            __nv_bfloat16 b[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                b[k] = __float2bfloat16_rn(v[k]);
-                const float w = __bfloat162float(b[k]);
-                v[k] = isfinite(w) ? v[k] - w : 0.0f;          // an infinite or NaN factor stays what it is
-            }
-            *reinterpret_cast<uint2*>(dst + (int64_t)q * n64) = *reinterpret_cast<const uint2*>(b);
+            const uint32_t lo = split_term(v[0], v[1]), hi = split_term(v[2], v[3]);
+            *reinterpret_cast<uint2*>(dst + (int64_t)q * n64) = make_uint2(lo, hi);
         }
     }
 }
@@ -350,15 +392,17 @@ __device__ __forceinline__ void store_columns(OutT* dst, bool is_x, int64_t ch, 
     }
 }
 
-template <typename OutT>
+// OutT fixes the number of terms of a factor: 2 for bf16 gradients, 3 for fp32. N64: factor columns rounded up to 64 or 128.
+template <typename OutT, int N64>
 __global__ void __launch_bounds__(NTHREADS, 1)
 lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_constant__ CUtensorMap tm_dy,
                   const __grid_constant__ CUtensorMap tm_h, const __grid_constant__ CUtensorMap tm_u, const OuterParams p)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    const int boxes = p.parts * (p.n64 / 64);                // factor operand: boxes of 64 columns x 64 tokens
-    const int stage_bytes = BIG + boxes * 8192;
+    constexpr int PARTS = sizeof(OutT) == 4 ? 3 : 2;
+    constexpr int boxes = PARTS * (N64 / 64);                // factor operand: boxes of 64 columns x 64 tokens
+    constexpr int stage_bytes = BIG + boxes * 8192;
     uint8_t* conv_buf = smem + (size_t)p.stages * stage_bytes;      // expanded codes: two buffers of 256 channels x 64 tokens
     Bars* bars = reinterpret_cast<Bars*>(conv_buf + 2 * 32768);
     volatile uint32_t* abort_flag = &bars->abort_flag;
@@ -366,7 +410,7 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
     const uint32_t nS = (uint32_t)p.stages;
 
     if (threadIdx.x == 0) {
-        init_barriers(bars, 8);
+        init_barriers(bars);
         prefetch_tmap(&tm_codes); prefetch_tmap(&tm_dy); prefetch_tmap(&tm_h); prefetch_tmap(&tm_u);
     }
     if (warp == 1) { tmem_alloc(smem_u32(&bars->tmem_base), 512); tmem_relinquish(); }
@@ -375,10 +419,10 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;                  // accumulator of item n, sub-tile m: column (n & 1) * 256 + m * 128
 
-    auto item_of = [&](int64_t item, LoraChunk& c, bool& is_x, int& ch0) {
-        const int64_t k = item / p.tiles;
-        const int tile = (int)(item - k * p.tiles);
-        c = p.chunks[k];
+    const uint32_t items = (uint32_t)p.items, step_items = gridDim.x;
+    auto chunk_of = [&](uint32_t item) { return p.chunks[min(item, items - 1) / (uint32_t)p.tiles]; };
+    auto place_of = [&](uint32_t item, bool& is_x, int& ch0) {
+        const int tile = (int)(item % (uint32_t)p.tiles);
         is_x = tile < p.tiles_x;
         ch0 = (is_x ? tile : tile - p.tiles_x) * TILE;
     };
@@ -388,9 +432,12 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
             uint32_t it = 0;
             Ring ring;
             bool ok = true;
-            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
-                LoraChunk c; bool is_x; int ch0;
-                item_of(item, c, is_x, ch0);
+            LoraChunk ahead = chunk_of(blockIdx.x);
+            for (uint32_t item = blockIdx.x; item < items && ok; item += step_items) {
+                const LoraChunk c = ahead;
+                ahead = chunk_of(item + step_items);
+                bool is_x; int ch0;
+                place_of(item, is_x, ch0);
                 for (int t = 0; t < c.len; t += TOK, ++it, ring.next(nS)) {
                     if (!mbar_wait(smem_u32(&bars->empty[ring.slot]), ring.parity ^ 1u, abort_flag, p.timeout_word, TO_PRODUCER)) { ok = false; break; }
                     const uint32_t full = smem_u32(&bars->full[ring.slot]);
@@ -414,9 +461,12 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
             Ring ring, conv;
             uint32_t n = 0;
             bool ok = true;
-            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++n) {
-                LoraChunk c; bool is_x; int ch0;
-                item_of(item, c, is_x, ch0);
+            LoraChunk ahead = chunk_of(blockIdx.x);
+            for (uint32_t item = blockIdx.x; item < items && ok; item += step_items, ++n) {
+                const LoraChunk c = ahead;
+                ahead = chunk_of(item + step_items);
+                bool is_x; int ch0;
+                place_of(item, is_x, ch0);
                 const int subs = (is_x ? p.in : p.out) - ch0 > 128 ? 2 : 1;
                 const uint32_t buf = n & 1u;
                 if (!mbar_wait(smem_u32(&bars->d_empty[buf]), ((n >> 1) & 1u) ^ 1u, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
@@ -427,12 +477,17 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
                     tc_fence_after();
                     const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
                     const uint32_t a = is_x ? smem_u32(conv_buf) + conv.slot * 32768 : big;
-                    for (int m = 0; m < subs; ++m)
+                    const uint64_t a0 = make_smem_desc_mn_sw128(a, 8192), b0 = make_smem_desc_mn_sw128(op, 8192);
+                    for (int m = 0; m < subs; ++m) {
+                        const uint64_t am = a0 + (uint64_t)(m * 1024);
+                        const uint32_t d = tmem + buf * 256 + m * 128;
+                        mma_f16_ss(d, am, b0, idesc, t > 0);
 #pragma unroll
-                        for (int k = 0; k < TOK / 16; ++k)
-                            for (int q = 0; q < p.parts; ++q)
-                                mma_f16_ss(tmem + buf * 256 + m * 128, make_smem_desc_mn_sw128(a + m * 16384 + k * 2048, 8192),
-                                           make_smem_desc_mn_sw128(op + q * (p.n64 / 64) * 8192 + k * 2048, 8192), idesc, t > 0 || k > 0 || q > 0);
+                        for (int i = 1; i < TOK / 16 * PARTS; ++i) {
+                            const int k = i / PARTS, q = i % PARTS;
+                            mma_f16_ss(d, am + (uint64_t)(k * 128), b0 + (uint64_t)(k * 128 + q * (N64 * 8)), idesc, 1u);
+                        }
+                    }
                     mma_commit(smem_u32(&bars->empty[ring.slot]));
                     mma_commit(smem_u32(&bars->conv_empty[conv.slot]));
                 }
@@ -442,68 +497,102 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
             mbar_wait_quiet(smem_u32(&bars->drain), 0u);
         }
     } else if (warp < 10) {
-        const int tid = threadIdx.x - 64;                    // 0 .. 255
-        const int groups = (p.in + p.group - 1) / p.group;
-        Ring ring, conv;
-        bool ok = true;
-        for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
-            LoraChunk c; bool is_x; int ch0;
-            item_of(item, c, is_x, ch0);
-            for (int t = 0; t < c.len; t += TOK, ring.next(nS), conv.next(2)) {
-                const int live = min(TOK, c.len - t);        // token rows of this block that belong to the chunk
-                uint32_t step[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {                // unit i * 256 + tid: box of 128 channels, token, 16 channels
-                    const int unit = i * 256 + tid, tok = (unit & 511) >> 3;
-                    const int g = (ch0 + (unit >> 9) * 128 + (unit & 7) * 16) / p.group;
-                    step[i] = (is_x && tok < live && g < groups) ? p.scales[(c.t0 + t + tok) * p.ld_scales + g] : 0u;
+        // Converters: two groups of four warps take alternate blocks (as above: every block, dY untouched but for the last, partly
+        // filled block of a chunk). A thread owns one token and 128 channels; the step bytes of its next block are requested before it
+        // works on the present one.
+        const int tid = (threadIdx.x - 64) & 127, tok = tid & 63, box = tid >> 6;
+        const uint32_t grp = warp >= 6 ? 1u : 0u;
+        const int groups = (p.in + p.group - 1) / p.group, per = 128 / p.group;
+        struct Cursor { uint32_t item; LoraChunk c; bool is_x; int ch0, t; Ring ring, conv; } cur;
+        // The next block of this group, at or behind the cursor's place.
+        auto seek = [&](Cursor& q) {
+            while (q.item < items) {
+                if (q.t >= q.c.len) {
+                    q.item += step_items;
+                    if (q.item >= items) return;
+                    q.c = chunk_of(q.item);
+                    place_of(q.item, q.is_x, q.ch0);
+                    q.t = 0;
+                    continue;
                 }
-                ok = mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_UNPACK) &&
-                     mbar_wait(smem_u32(&bars->conv_empty[conv.slot]), conv.parity ^ 1u, abort_flag, p.timeout_word, TO_UNPACK);
-                ok = __all_sync(0xFFFFFFFFu, ok);
-                if (!ok) break;
-                uint8_t* big = smem + (size_t)ring.slot * stage_bytes;
-                if (is_x) {
-                    uint8_t* out = conv_buf + conv.slot * 32768;
+                if (q.conv.slot == grp) return;
+                q.conv.next(2); q.t += TOK; q.ring.next(nS);
+            }
+        };
+        auto step_over = [&](Cursor& q) { q.conv.next(2); q.t += TOK; q.ring.next(nS); };
+        auto load_steps = [&](const Cursor& q, uint32_t (&v)[4]) {
+            const int g0 = (q.ch0 + box * 128) / p.group;
+            const uint8_t* sc = p.scales + (q.c.t0 + q.t + tok) * p.ld_scales + g0;
+            const bool in_range = q.item < items && q.is_x && q.t + tok < q.c.len;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int unit = i * 256 + tid, box = unit >> 9, tok = (unit & 511) >> 3, j = unit & 7;
-                        const uint4 w = *reinterpret_cast<const uint4*>(big + box * 8192 + tok * 128 + ((j ^ (tok & 7)) << 4));
-                        uint32_t v[8];
-                        const uint32_t s2 = step_bf16x2(step[i]);
-                        expand4(w.x, s2, v[0], v[1]);
-                        expand4(w.y, s2, v[2], v[3]);
-                        expand4(w.z, s2, v[4], v[5]);
-                        expand4(w.w, s2, v[6], v[7]);
-                        if (tok >= live) {
+            for (int i = 0; i < 4; ++i) v[i] = (in_range && i < per && g0 + i < groups) ? __ldg(sc + i) : 0u;
+        };
+        cur.item = blockIdx.x; cur.t = 0;
+        cur.c = chunk_of(cur.item);
+        place_of(cur.item, cur.is_x, cur.ch0);
+        seek(cur);
+        uint32_t step[4];
+        load_steps(cur, step);
+        while (cur.item < items) {
+            Cursor nxt = cur;
+            step_over(nxt);
+            seek(nxt);
+            uint32_t step_next[4];
+            load_steps(nxt, step_next);
+            const int live = min(TOK, cur.c.len - cur.t);        // token rows of this block that belong to the chunk
+            bool ok = mbar_wait(smem_u32(&bars->conv_empty[grp]), cur.conv.parity ^ 1u, abort_flag, p.timeout_word, TO_UNPACK) &&
+                      mbar_wait(smem_u32(&bars->full[cur.ring.slot]), cur.ring.parity, abort_flag, p.timeout_word, TO_UNPACK);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+            if (!ok) break;
+            uint8_t* big = smem + (size_t)cur.ring.slot * stage_bytes;
+            if (cur.is_x) {
+                const uint4* src = reinterpret_cast<const uint4*>(big + box * 8192 + tok * 128);
+                uint4 raw[8];
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) v[k] = 0u;
-                        }
-                        uint8_t* row = out + (box * 2 + (j >> 2)) * 8192 + tok * 128;
-                        const int c16 = (j & 3) * 2;
-                        *reinterpret_cast<uint4*>(row + ((c16 ^ (tok & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
-                        *reinterpret_cast<uint4*>(row + (((c16 + 1) ^ (tok & 7)) << 4)) = make_uint4(v[4], v[5], v[6], v[7]);
-                    }
+                for (int j = 0; j < 8; ++j) raw[j] = src[j ^ (tok & 7)];
+                uint8_t* out = conv_buf + grp * 32768 + box * 16384 + tok * 128;
+                const bool dead = tok >= live;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {                    // 16 channels -> two 16-byte pieces of block j / 4 of 64 channels
+                    const uint32_t s2 = step_bf16x2(p.group == 32 ? step[j >> 1] : p.group == 64 ? step[j >> 2] : step[0]);
+                    uint32_t v[8];
+                    const uint4 w = dead ? make_uint4(0u, 0u, 0u, 0u) : raw[j];      // (and step 0: the expanded value is +0)
+                    expand4(w.x, s2, v[0], v[1]);
+                    expand4(w.y, s2, v[2], v[3]);
+                    expand4(w.z, s2, v[4], v[5]);
+                    expand4(w.w, s2, v[6], v[7]);
+                    uint8_t* row = out + (j >> 2) * 8192;
+                    const int c16 = (j & 3) * 2;
+                    *reinterpret_cast<uint4*>(row + ((c16 ^ (tok & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+                    *reinterpret_cast<uint4*>(row + (((c16 + 1) ^ (tok & 7)) << 4)) = make_uint4(v[4], v[5], v[6], v[7]);
                 }
-                if (live < TOK) {                            // rows of the next example: zero in the factors, and in dY
-                    const int first = is_x ? 4 : 0, rows = TOK - live;
-                    for (int i = tid; i < (4 - first + boxes) * rows * 8; i += 256) {
-                        const int b = first + i / (rows * 8), rest = i % (rows * 8);
-                        *reinterpret_cast<uint4*>(big + b * 8192 + (live + (rest >> 3)) * 128 + (rest & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-                    }
+            }
+            if (live < TOK) {                                    // rows of the next example: zero in the factors, and in dY
+                const int first = cur.is_x ? 4 : 0, rows = TOK - live;
+                for (int i = tid; i < (4 - first + boxes) * rows * 8; i += 128) {
+                    const int b = first + i / (rows * 8), rest = i % (rows * 8);
+                    *reinterpret_cast<uint4*>(big + b * 8192 + (live + (rest >> 3)) * 128 + (rest & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                 }
+            }
+            if (cur.is_x || live < TOK) {
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bars->ready[conv.slot]));
             }
+            if (lane == 0) mbar_arrive(smem_u32(&bars->ready[grp]));
+            cur = nxt;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) step[i] = step_next[i];
         }
     } else {
         const int row = (warp & 3) * 32 + lane;
         const int64_t width_all = (int64_t)p.rank * (p.in + p.out);
         uint32_t n = 0;
-        for (int64_t item = blockIdx.x; item < p.items; item += gridDim.x, ++n) {
-            LoraChunk c; bool is_x; int ch0;
-            item_of(item, c, is_x, ch0);
+        LoraChunk ahead = chunk_of(blockIdx.x);
+        for (uint32_t item = blockIdx.x; item < items; item += step_items, ++n) {
+            const LoraChunk c = ahead;
+            ahead = chunk_of(item + step_items);
+            bool is_x; int ch0;
+            place_of(item, is_x, ch0);
             const int width = is_x ? p.in : p.out;
             const uint32_t buf = n & 1u;
             bool ok = mbar_wait(smem_u32(&bars->d_full[buf]), (n >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE);
@@ -628,7 +717,8 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
         FactorParams f;
         f.T = a.T; f.ld_scales = a.ld_scales; f.scales = a.scales;
         f.part = reinterpret_cast<float*>(ws + pl.fpart_off);
-        f.in = a.in; f.out = a.out; f.group = a.group; f.nr = pl.nr; f.n64 = pl.n64; f.slices = pl.slices;
+        f.in = a.in; f.out = a.out; f.group = a.group; f.nr = pl.nr; f.n64 = pl.n64; f.parts = pl.parts; f.slices = pl.slices;
+        f.fac = fac; f.scaling = a.scaling;
         f.kb_x = ((a.in + CH - 1) / CH + pl.slices - 1) / pl.slices;
         f.kb_y = ((a.out + CH - 1) / CH + pl.slices - 1) / pl.slices;
         f.token_tiles = (int32_t)pl.token_tiles;
@@ -642,11 +732,14 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
           QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_factors_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
           lora_factors_kernel<<<(unsigned)grid, NTHREADS, smem, st>>>(tm_codes, tm_dy, tm_a, tm_b, f); }
         QLESS_CUDA_TRY(cudaGetLastError());
-        { ProfileScope ps("lora_split", st);
+        if (pl.slices > 1) {
+          ProfileScope ps("lora_split", st);
           const int64_t blocks = (2 * a.T * (pl.n64 / 4) + 255) / 256, most = (int64_t)sm_count() * 8;
-          lora_split_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, st>>>(f.part, fac, a.T, pl.n64, pl.nr, pl.slices, pl.parts, a.scaling); }
+          lora_split_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, st>>>(f.part, fac, a.T, pl.n64, pl.nr, pl.slices, pl.parts, a.scaling);
+          count_launches(1);
+        }
         QLESS_CUDA_TRY(cudaGetLastError());
-        count_launches(2);
+        count_launches(1);
     }
     CUtensorMap tm_codes, tm_dy, tm_h, tm_u;
     const int64_t rows = a.T > 0 ? a.T : 1;                   // no tokens at all: the maps are not used, every item has length 0
@@ -659,22 +752,26 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
     OuterParams o;
     o.chunks = d_chunks; o.scales = a.scales; o.ld_scales = a.ld_scales; o.ld_grads = a.ld_grads;
     o.grads = a.grads; o.part = reinterpret_cast<float*>(ws + pl.part_off);
-    o.in = a.in; o.out = a.out; o.rank = a.rank; o.group = a.group; o.nr = pl.nr; o.n64 = pl.n64; o.parts = pl.parts;
+    o.in = a.in; o.out = a.out; o.rank = a.rank; o.group = a.group; o.nr = pl.nr;
     o.tiles_x = pl.tiles_x; o.tiles = pl.tiles; o.timeout_word = timeout_word;
     o.items = (int64_t)a.num_chunks * pl.tiles;
+    QLESS_REQUIRE(o.items < ((int64_t)1 << 31) - 65536, QLESS_ERR_UNSUPPORTED, "too many examples: %lld pieces of %d tiles", (long long)a.num_chunks, pl.tiles);
     const size_t stage = BIG + (size_t)pl.parts * (pl.n64 / 64) * 8192;
     const size_t left = budget - 2 * 32768;
     o.stages = (int32_t)(left / stage < MAX_STAGES ? left / stage : MAX_STAGES);
     const size_t smem = 1024 + o.stages * stage + 2 * 32768 + sizeof(Bars);
     const int64_t grid = o.items < sm_count() ? o.items : sm_count();
     { ProfileScope ps("lora_outer", st);
+#define QLESS_LAUNCH_LORA_OUTER(OUT, N)                                                                                              \
+      QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_outer_kernel<OUT, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));          \
+      lora_outer_kernel<OUT, N><<<(unsigned)grid, NTHREADS, smem, st>>>(tm_codes, tm_dy, tm_h, tm_u, o);
       if (a.dtype == QLESS_F32) {
-          QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_outer_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-          lora_outer_kernel<float><<<(unsigned)grid, NTHREADS, smem, st>>>(tm_codes, tm_dy, tm_h, tm_u, o);
+          if (pl.n64 == 64) { QLESS_LAUNCH_LORA_OUTER(float, 64) } else { QLESS_LAUNCH_LORA_OUTER(float, 128) }
       } else {
-          QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_outer_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-          lora_outer_kernel<__nv_bfloat16><<<(unsigned)grid, NTHREADS, smem, st>>>(tm_codes, tm_dy, tm_h, tm_u, o);
-      } }
+          if (pl.n64 == 64) { QLESS_LAUNCH_LORA_OUTER(__nv_bfloat16, 64) } else { QLESS_LAUNCH_LORA_OUTER(__nv_bfloat16, 128) }
+      }
+#undef QLESS_LAUNCH_LORA_OUTER
+    }
     QLESS_CUDA_TRY(cudaGetLastError());
     count_launches(1);
     for (int64_t j0 = 0; j0 < a.num_joins; j0 += 65535) {

@@ -172,6 +172,18 @@ def test_lora_gradients_of_many_examples():
     _check_lora(got, want, mag, 64, 96, 9, torch.float32)
 
 
+def test_lora_gradients_of_more_tiles_than_multiprocessors():
+    # every block of the grid works through several tiles of both kinds, with pieces of one to several 64-token blocks
+    g = np.random.default_rng(5)
+    offsets = np.concatenate([[0], np.cumsum(g.integers(1, 1200, 40))]).tolist()
+    T, wi, wo, rank = offsets[-1], 528, 1296, 16
+    case = _lora_case(T, wi, wo, rank, 32, 81)
+    got = B.qless_lora_gradients(*case, offsets, group=32, dtype=torch.float32)
+    want, mag = reference_lora(*case, offsets, 1.0, 32)
+    B.qless_check()
+    _check_lora(got, want, mag, wi, wo, 1200, torch.float32)
+
+
 def test_lora_gradients_into_a_slice_of_the_gradient_matrix():
     offsets, wi, wo, rank = [0, 70, 71, 200], 128, 256, 16
     P = rank * (wi + wo)
