@@ -434,9 +434,10 @@ def qless_select_topk_static(scores, frac, indices, stream=None):
 
 def _row_stride(t):
     """Elements between rows of a 2-D tensor whose rows are contiguous."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError("a 2-D tensor with contiguous rows is required")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return stride[0] if shape[0] > 1 else max(stride[0], shape[1])
 
 
 def _dtype_of(dtype):

@@ -401,6 +401,9 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     constexpr int PARTS = sizeof(OutT) == 4 ? 3 : 2;
+    // Two terms of at most 64 columns are one operand of 128 columns (their sums meet in the epilogue): the channel operand is read from
+    // shared memory once for both, whose bandwidth bounds this loop. Otherwise one product per term into the same accumulator.
+    constexpr bool WIDE = PARTS * N64 == 128;
     constexpr int boxes = PARTS * (N64 / 64);                // factor operand: boxes of 64 columns x 64 tokens
     constexpr int stage_bytes = BIG + boxes * 8192;
     uint8_t* conv_buf = smem + (size_t)p.stages * stage_bytes;      // expanded codes: two buffers of 256 channels x 64 tokens
@@ -457,7 +460,8 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
         }
     } else if (warp == 1) {
         if (lane == 0) {
-            const uint32_t idesc = make_idesc(1, 1, 1, 128, p.nr) | IDESC_A_MN | IDESC_B_MN;
+            const uint32_t idesc = make_idesc(1, 1, 1, 128, WIDE ? 128 : p.nr) | IDESC_A_MN | IDESC_B_MN;
+            constexpr int TERMS = WIDE ? 1 : PARTS;
             Ring ring, conv;
             uint32_t n = 0;
             bool ok = true;
@@ -483,8 +487,8 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
                         const uint32_t d = tmem + buf * 256 + m * 128;
                         mma_f16_ss(d, am, b0, idesc, t > 0);
 #pragma unroll
-                        for (int i = 1; i < TOK / 16 * PARTS; ++i) {
-                            const int k = i / PARTS, q = i % PARTS;
+                        for (int i = 1; i < TOK / 16 * TERMS; ++i) {
+                            const int k = i / TERMS, q = i % TERMS;
                             mma_f16_ss(d, am + (uint64_t)(k * 128), b0 + (uint64_t)(k * 128 + q * (N64 * 8)), idesc, 1u);
                         }
                     }
@@ -605,7 +609,15 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
                 const int64_t ch = ch0 + m * 128 + row;
                 for (int c0 = 0; c0 < p.rank; c0 += 32) {
                     uint32_t v[32];
-                    tmem_ld_x32(tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 256 + m * 128 + c0, v);
+                    const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 256 + m * 128 + c0;
+                    tmem_ld_x32(taddr, v);
+                    if (WIDE) {
+                        uint32_t low[32];
+                        tmem_ld_x32(taddr + 64, low);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(low[j]));
+                    }
                     tmem_wait_ld();
                     if (ch < width) {
                         if (c.slot >= 0) store_columns<float>(p.part + (int64_t)c.slot * width_all + base, is_x, ch, width, c0, p.rank, v, c.len == 0);
