@@ -37,9 +37,10 @@ struct FactorParams {
     int64_t T, ld_scales;
     const uint8_t* scales;
     float* part;                            // [2][slices][T][N64]: 0 = H, 1 = U (more than one slice)
-    __nv_bfloat16* fac;                     // [2][T][parts][N64] (one slice)
+    __nv_bfloat16* fac;                     // [2][parts][N64 / 64][T][64] (one slice)
     float scaling;
     int32_t in, out, group, nr, n64, parts, slices, kb_x, kb_y, stages;      // kb_*: channel blocks per slice
+    int32_t y_whole, steps_whole;
     int32_t token_tiles;
     int64_t items;
     unsigned int* timeout_word;
@@ -52,11 +53,16 @@ struct OuterParams {
     void* grads;
     float* part;                            // [slots][rank * (in + out)]
     int32_t in, out, rank, group, nr, tiles_x, tiles, stages;
+    int32_t x_whole, y_whole;               // rows of the codes / of dY are whole 128-byte blocks: one copy brings several side by side
+    int32_t steps_whole;                    // step bytes of 128 channels are one aligned word
     unsigned int* timeout_word;
 };
 
+// codes1, dy1, a, b: step (1), boxes of 128 tokens (channels of the weights) by 128 bytes; codes2, dy2, fac: step (2), 64 tokens.
+struct LoraMaps { CUtensorMap codes1, codes2, dy1, dy2, a, b, fac; };
+
 struct __align__(8) Bars {
-    uint64_t full[MAX_STAGES], empty[MAX_STAGES], ready[2], conv_empty[2], d_full[2], d_empty[2], drain;
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES], ready[2], d_full[2], d_empty[2], drain;
     uint32_t tmem_base, abort_flag;
 };
 
@@ -81,6 +87,25 @@ __device__ __forceinline__ void expand4(uint32_t w, uint32_t step2, uint32_t& lo
 }
 __device__ __forceinline__ uint32_t step_bf16x2(uint32_t byte) { return (byte << 7) | (byte << 23); }      // 0xFF: infinity, and 0 * infinity = NaN
 
+// Up to four consecutive step bytes, the first in the low byte. Volatile: requested here, a block before they are used, and not
+// where the compiler sees the use. `whole`: the groups of 128 channels start at a multiple of their number of bytes in memory.
+__device__ __forceinline__ uint32_t load_step_bytes(const uint8_t* p, int n, bool whole)
+{
+    uint32_t v = 0u;
+    if (whole && n == 4) {
+        asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v) : "l"(p));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) {
+                uint32_t b;
+                asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(b) : "l"(p + i));
+                v |= b << (8 * i);
+            }
+    }
+    return v;
+}
+
 // The leading bf16 term of two fp32 numbers, packed; what it leaves of them stays in a and b. An infinite or NaN number is its own
 // term and leaves nothing.
 __device__ __forceinline__ uint32_t split_term(float& a, float& b)
@@ -97,7 +122,6 @@ __device__ __forceinline__ void init_barriers(Bars* b)
     for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(smem_u32(&b->full[s]), 1); mbar_init(smem_u32(&b->empty[s]), 1); }
     for (int s = 0; s < 2; ++s) {
         mbar_init(smem_u32(&b->ready[s]), 4);
-        mbar_init(smem_u32(&b->conv_empty[s]), 1);
         mbar_init(smem_u32(&b->d_full[s]), 1);
         mbar_init(smem_u32(&b->d_empty[s]), 4);
     }
@@ -116,8 +140,7 @@ __device__ __forceinline__ void drain_copies(Bars* b, uint32_t it, uint32_t stag
 // ---- (1) factors -------------------------------------------------------------------------------------------------------
 
 __global__ void __launch_bounds__(NTHREADS, 1)
-lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_constant__ CUtensorMap tm_dy,
-                    const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const FactorParams p)
+lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -130,7 +153,7 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
 
     if (threadIdx.x == 0) {
         init_barriers(bars);
-        prefetch_tmap(&tm_codes); prefetch_tmap(&tm_dy); prefetch_tmap(&tm_a); prefetch_tmap(&tm_b);
+        prefetch_tmap(&maps.codes1); prefetch_tmap(&maps.dy1); prefetch_tmap(&maps.a); prefetch_tmap(&maps.b);
     }
     if (warp == 1) { tmem_alloc(smem_u32(&bars->tmem_base), 512); tmem_relinquish(); }
     tc_fence_before();
@@ -138,20 +161,27 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;                  // accumulators at columns 0 and 128, expanded codes at 256 and 320
 
-    // item -> (slice, kind, token tile); kind 1 = dY first in every slice: its tiles are the larger ones
+    // item -> (slice, token tile, kind): of two neighbouring items one reads codes and one dY, and a block takes them in turn, so that at
+    // any time half of the blocks read the one (bound by the work per block of codes) and half the other (bound by its bytes).
     const int64_t per_slice = 2LL * p.token_tiles;
     auto item_of = [&](int64_t item, int& slice, bool& is_x, int64_t& tile, int& kb0, int& kb1) {
         slice = (int)(item / per_slice);
         const int64_t r = item - slice * per_slice;
-        is_x = r >= p.token_tiles;
-        tile = is_x ? r - p.token_tiles : r;
+        is_x = ((r + item / gridDim.x) & 1) != 0;
+        tile = r >> 1;
         const int all = ((is_x ? p.in : p.out) + CH - 1) / CH, step = is_x ? p.kb_x : p.kb_y;
         kb0 = min(all, slice * step);
         kb1 = min(all, kb0 + step);
     };
 
+    // A wait of a whole warp: the same answer in every lane.
+    auto warp_wait = [&](uint64_t* bar, uint32_t parity, uint32_t code) -> bool {
+        const bool w = mbar_wait(smem_u32(bar), parity, abort_flag, p.timeout_word, code);
+        return __all_sync(0xFFFFFFFFu, w);
+    };
+
     if (warp == 0) {
-        if (lane == 0) {
+        {
             uint32_t it = 0;
             Ring ring;
             bool ok = true;
@@ -159,26 +189,28 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
                 int slice, kb0, kb1; bool is_x; int64_t tile;
                 item_of(item, slice, is_x, tile, kb0, kb1);
                 for (int kb = kb0; kb < kb1; ++kb, ++it, ring.next(nS)) {
-                    if (!mbar_wait(smem_u32(&bars->empty[ring.slot]), ring.parity ^ 1u, abort_flag, p.timeout_word, TO_PRODUCER)) { ok = false; break; }
+                    if (!warp_wait(&bars->empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
                     const uint32_t full = smem_u32(&bars->full[ring.slot]);
                     const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
-                    if (is_x) {
-                        mbar_arrive_expect_tx(full, 128 * CH + 2 * p.nr * 128);
-                        tma_load_2d(big, &tm_codes, full, kb * CH, (int32_t)(tile * 128));
-                        tma_load_2d(op, &tm_a, full, kb * CH, 0);
-                        tma_load_2d(op + p.n64 * 128, &tm_a, full, kb * CH + 64, 0);
-                    } else {
-                        mbar_arrive_expect_tx(full, 2 * 128 * 128 + p.n64 * 256);
-                        tma_load_2d(big, &tm_dy, full, kb * CH, (int32_t)(tile * 128));
-                        tma_load_2d(big + 16384, &tm_dy, full, kb * CH + 64, (int32_t)(tile * 128));
-                        for (int j = 0; j < p.n64; j += 64) tma_load_2d(op + j * 256, &tm_b, full, j, kb * CH);
+                    if (elect_one()) {
+                        if (is_x) {
+                            mbar_arrive_expect_tx(full, 128 * CH + 2 * p.nr * 128);
+                            tma_load_2d(big, &maps.codes1, full, kb * CH, (int32_t)(tile * 128));
+                            for (int j = 0; j < 2; ++j) tma_load_2d(op + j * p.n64 * 128, &maps.a, full, kb * CH + j * 64, 0);
+                        } else {
+                            mbar_arrive_expect_tx(full, 2 * 128 * 128 + p.n64 * 256);
+                            if (p.y_whole) tma_load_3d(big, &maps.dy1, full, 0, (int32_t)(tile * 128), kb * 2);
+                            else for (int j = 0; j < 2; ++j) tma_load_2d(big + j * 16384, &maps.dy1, full, kb * CH + j * 64, (int32_t)(tile * 128));
+                            for (int j = 0; j < p.n64; j += 64) tma_load_2d(op + j * 256, &maps.b, full, j, kb * CH);
+                        }
                     }
+                    __syncwarp();
                 }
             }
             if (!ok) drain_copies(bars, it, nS);
         }
     } else if (warp == 1) {
-        if (lane == 0) {
+        {
             const uint32_t idesc_x = make_idesc(1, 1, 1, 128, p.nr), idesc_y = idesc_x | IDESC_B_MN;
             Ring ring, conv;
             uint32_t n = 0;
@@ -187,13 +219,14 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
                 int slice, kb0, kb1; bool is_x; int64_t tile;
                 item_of(item, slice, is_x, tile, kb0, kb1);
                 const uint32_t buf = n & 1u, d = tmem + buf * 128;
-                if (!mbar_wait(smem_u32(&bars->d_empty[buf]), ((n >> 1) & 1u) ^ 1u, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                if (!warp_wait(&bars->d_empty[buf], ((n >> 1) & 1u) ^ 1u, TO_MMA)) { ok = false; break; }
                 tc_fence_after();
                 for (int kb = kb0; kb < kb1; ++kb, ring.next(nS)) {
-                    if (!mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_MMA) ||
-                        !mbar_wait(smem_u32(&bars->ready[conv.slot]), conv.parity, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                    // the converters have seen the stage's copies land before they arrive here
+                    if (!warp_wait(&bars->ready[conv.slot], conv.parity, TO_MMA)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
+                    if (elect_one()) {
                     // Descriptors are made once per stage and advanced by constants (addresses in units of 16 bytes): made anew for every
                     // product they took 180 clocks of this thread where the product takes 48.
                     if (is_x) {
@@ -210,12 +243,14 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
                             mma_f16_ss(d, a0 + (uint64_t)((k >> 2) * 1024 + (k & 3) * 2), b0 + (uint64_t)(k * 128), idesc_y, 1u);
                     }
                     mma_commit(smem_u32(&bars->empty[ring.slot]));
-                    mma_commit(smem_u32(&bars->conv_empty[conv.slot]));
+                    }
+                    __syncwarp();
                     conv.next(2);
                 }
-                if (ok) mma_commit(smem_u32(&bars->d_full[buf]));
+                if (ok && elect_one()) mma_commit(smem_u32(&bars->d_full[buf]));
+                __syncwarp();
             }
-            mma_commit(smem_u32(&bars->drain));               // every MMA issued above completes before tensor memory is freed
+            if (elect_one()) mma_commit(smem_u32(&bars->drain));               // every MMA issued above completes before tensor memory is freed
             mbar_wait_quiet(smem_u32(&bars->drain), 0u);
         }
     } else if (warp < 10) {
@@ -225,34 +260,28 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
         // it knows from the products of its own previous block being done.
         const int row = (warp & 3) * 32 + lane;
         const uint32_t grp = warp >= 6 ? 1u : 0u;
-        const int groups = (p.in + p.group - 1) / p.group;
-        Ring ring, conv;
-        bool ok = true;
+        const int groups = (p.in + p.group - 1) / p.group, per = CH / p.group;
+        Ring ring, conv, mine;                                 // mine: the stage of this group's previous block
+        bool ok = true, first = true;
         for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
             int slice, kb0, kb1; bool is_x; int64_t tile;
             item_of(item, slice, is_x, tile, kb0, kb1);
             const int64_t t = tile * 128 + row;
             const uint8_t* sc = p.scales + t * p.ld_scales;
-            auto load_steps = [&](int kb, uint32_t (&v)[4]) {       // the 128 channels lie in 4, 2 or 1 groups
-                const int g0 = kb * CH / p.group, per = CH / p.group;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = (t < p.T && i < per && g0 + i < groups) ? __ldg(sc + g0 + i) : 0u;
+            auto load_steps = [&](int kb) -> uint32_t {        // the step bytes of the 4, 2 or 1 groups that the 128 channels lie in
+                return (is_x && t < p.T) ? load_step_bytes(sc + kb * CH / p.group, min(per, groups - kb * CH / p.group), p.steps_whole != 0) : 0u;
             };
-            uint32_t ahead[4] = {0u, 0u, 0u, 0u};
+            uint32_t ahead = 0u;
             bool loaded = false;
             for (int kb = kb0; kb < kb1 && ok; ++kb, ring.next(nS), conv.next(2)) {
                 if (conv.slot != grp) continue;
-                uint32_t step[4];
-                if (is_x) {
-                    if (loaded) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) step[i] = ahead[i];
-                    } else load_steps(kb, step);
-                    loaded = kb + 2 < kb1;                     // this group's next block: its steps are requested one block early
-                    if (loaded) load_steps(kb + 2, ahead);
-                }
-                ok = mbar_wait(smem_u32(&bars->conv_empty[conv.slot]), conv.parity ^ 1u, abort_flag, p.timeout_word, TO_UNPACK) &&
+                const uint32_t step = loaded ? ahead : load_steps(kb);
+                loaded = kb + 2 < kb1;                         // this group's next block: its steps are requested one block early
+                if (loaded) ahead = load_steps(kb + 2);
+                ok = (first || mbar_wait(smem_u32(&bars->empty[mine.slot]), mine.parity, abort_flag, p.timeout_word, TO_UNPACK)) &&
                      mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_UNPACK);
+                first = false;
+                mine = ring;
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 if (!is_x) {
@@ -267,7 +296,7 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
                 const uint32_t dst = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 256 + conv.slot * 64;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {                  // 32 channels: 16 tensor-memory columns of two bf16 each
-                    const uint32_t s2 = step_bf16x2(p.group == 32 ? step[q] : p.group == 64 ? step[q >> 1] : step[0]);
+                    const uint32_t s2 = step_bf16x2((step >> ((q * 32 / p.group) * 8)) & 0xFFu);
                     uint32_t v[16];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
@@ -312,8 +341,9 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
                     float x[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(v[j]) * p.scaling;
-                    __nv_bfloat16* dst = p.fac + (kind * p.T + t) * p.parts * p.n64 + c0;
-                    for (int q = 0; q < p.parts; ++q, dst += p.n64)
+                    const int blocks = p.n64 / 64;
+                    __nv_bfloat16* dst = p.fac + ((kind * p.parts * blocks + c0 / 64) * p.T + t) * 64 + c0 % 64;
+                    for (int q = 0; q < p.parts; ++q, dst += blocks * p.T * 64)
 #pragma unroll
                         for (int j = 0; j < 32; j += 8) {
                             uint32_t w[4];
@@ -339,7 +369,7 @@ lora_factors_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_c
 }
 
 // Several channel slices: adds them, multiplies by the adapter's scale and splits the fp32 factor into `parts` bf16 terms that add up to
-// it (8 bits each): fac [2][T][parts][n64].
+// it (8 bits each): fac [2][parts][n64 / 64][T][64].
 __global__ void lora_split_kernel(const float* __restrict__ part, __nv_bfloat16* __restrict__ fac, int64_t T, int32_t n64, int32_t nr,
                                   int32_t slices, int32_t parts, float scaling)
 {
@@ -356,10 +386,11 @@ __global__ void lora_split_kernel(const float* __restrict__ part, __nv_bfloat16*
             x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
         }
         float v[4] = {x.x * scaling, x.y * scaling, x.z * scaling, x.w * scaling};
-        __nv_bfloat16* dst = fac + row * parts * n64 + c;
+        const int blocks = n64 / 64;
+        __nv_bfloat16* dst = fac + ((kind * parts * blocks + c / 64) * T + t) * 64 + c % 64;
         for (int q = 0; q < parts; ++q) {
             const uint32_t lo = split_term(v[0], v[1]), hi = split_term(v[2], v[3]);
-            *reinterpret_cast<uint2*>(dst + (int64_t)q * n64) = make_uint2(lo, hi);
+            *reinterpret_cast<uint2*>(dst + (int64_t)q * blocks * T * 64) = make_uint2(lo, hi);
         }
     }
 }
@@ -395,8 +426,7 @@ __device__ __forceinline__ void store_columns(OutT* dst, bool is_x, int64_t ch, 
 // OutT fixes the number of terms of a factor: 2 for bf16 gradients, 3 for fp32. N64: factor columns rounded up to 64 or 128.
 template <typename OutT, int N64>
 __global__ void __launch_bounds__(NTHREADS, 1)
-lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_constant__ CUtensorMap tm_dy,
-                  const __grid_constant__ CUtensorMap tm_h, const __grid_constant__ CUtensorMap tm_u, const OuterParams p)
+lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -414,7 +444,7 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
 
     if (threadIdx.x == 0) {
         init_barriers(bars);
-        prefetch_tmap(&tm_codes); prefetch_tmap(&tm_dy); prefetch_tmap(&tm_h); prefetch_tmap(&tm_u);
+        prefetch_tmap(&maps.codes2); prefetch_tmap(&maps.dy2); prefetch_tmap(&maps.fac);
     }
     if (warp == 1) { tmem_alloc(smem_u32(&bars->tmem_base), 512); tmem_relinquish(); }
     tc_fence_before();
@@ -430,8 +460,14 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
         ch0 = (is_x ? tile : tile - p.tiles_x) * TILE;
     };
 
+    // A wait of a whole warp: the same answer in every lane.
+    auto warp_wait = [&](uint64_t* bar, uint32_t parity, uint32_t code) -> bool {
+        const bool w = mbar_wait(smem_u32(bar), parity, abort_flag, p.timeout_word, code);
+        return __all_sync(0xFFFFFFFFu, w);
+    };
+
     if (warp == 0) {
-        if (lane == 0) {
+        {
             uint32_t it = 0;
             Ring ring;
             bool ok = true;
@@ -442,24 +478,28 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
                 bool is_x; int ch0;
                 place_of(item, is_x, ch0);
                 for (int t = 0; t < c.len; t += TOK, ++it, ring.next(nS)) {
-                    if (!mbar_wait(smem_u32(&bars->empty[ring.slot]), ring.parity ^ 1u, abort_flag, p.timeout_word, TO_PRODUCER)) { ok = false; break; }
+                    if (!warp_wait(&bars->empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
                     const uint32_t full = smem_u32(&bars->full[ring.slot]);
                     const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
                     const int32_t row = (int32_t)(c.t0 + t);
-                    mbar_arrive_expect_tx(full, (is_x ? 2 : 4) * 8192 + boxes * 8192);
-                    if (is_x) {
-                        for (int j = 0; j < 2; ++j) tma_load_2d(big + j * 8192, &tm_codes, full, ch0 + j * 128, row);
-                        for (int j = 0; j < boxes; ++j) tma_load_2d(op + j * 8192, &tm_u, full, j * 64, row);
-                    } else {
-                        for (int j = 0; j < 4; ++j) tma_load_2d(big + j * 8192, &tm_dy, full, ch0 + j * 64, row);
-                        for (int j = 0; j < boxes; ++j) tma_load_2d(op + j * 8192, &tm_h, full, j * 64, row);
+                    if (elect_one()) {
+                        mbar_arrive_expect_tx(full, (is_x ? 2 : 4) * 8192 + boxes * 8192);
+                        if (is_x) {
+                            if (p.x_whole) tma_load_3d(big, &maps.codes2, full, 0, row, ch0 / 128);
+                            else for (int j = 0; j < 2; ++j) tma_load_2d(big + j * 8192, &maps.codes2, full, ch0 + j * 128, row);
+                        } else {
+                            if (p.y_whole) tma_load_3d(big, &maps.dy2, full, 0, row, ch0 / 64);
+                            else for (int j = 0; j < 4; ++j) tma_load_2d(big + j * 8192, &maps.dy2, full, ch0 + j * 64, row);
+                        }
+                        tma_load_3d(op, &maps.fac, full, 0, row, (is_x ? 1 : 0) * boxes);      // U for the codes, H for dY
                     }
+                    __syncwarp();
                 }
             }
             if (!ok) drain_copies(bars, it, nS);
         }
     } else if (warp == 1) {
-        if (lane == 0) {
+        {
             const uint32_t idesc = make_idesc(1, 1, 1, 128, WIDE ? 128 : p.nr) | IDESC_A_MN | IDESC_B_MN;
             constexpr int TERMS = WIDE ? 1 : PARTS;
             Ring ring, conv;
@@ -473,14 +513,14 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
                 place_of(item, is_x, ch0);
                 const int subs = (is_x ? p.in : p.out) - ch0 > 128 ? 2 : 1;
                 const uint32_t buf = n & 1u;
-                if (!mbar_wait(smem_u32(&bars->d_empty[buf]), ((n >> 1) & 1u) ^ 1u, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                if (!warp_wait(&bars->d_empty[buf], ((n >> 1) & 1u) ^ 1u, TO_MMA)) { ok = false; break; }
                 tc_fence_after();
                 for (int t = 0; t < c.len; t += TOK, ring.next(nS), conv.next(2)) {
-                    if (!mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_MMA) ||
-                        !mbar_wait(smem_u32(&bars->ready[conv.slot]), conv.parity, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                    if (!warp_wait(&bars->ready[conv.slot], conv.parity, TO_MMA)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
                     const uint32_t a = is_x ? smem_u32(conv_buf) + conv.slot * 32768 : big;
+                    if (elect_one()) {
                     const uint64_t a0 = make_smem_desc_mn_sw128(a, 8192), b0 = make_smem_desc_mn_sw128(op, 8192);
                     for (int m = 0; m < subs; ++m) {
                         const uint64_t am = a0 + (uint64_t)(m * 1024);
@@ -493,11 +533,13 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
                         }
                     }
                     mma_commit(smem_u32(&bars->empty[ring.slot]));
-                    mma_commit(smem_u32(&bars->conv_empty[conv.slot]));
+                    }
+                    __syncwarp();
                 }
-                if (ok) mma_commit(smem_u32(&bars->d_full[buf]));
+                if (ok && elect_one()) mma_commit(smem_u32(&bars->d_full[buf]));
+                __syncwarp();
             }
-            mma_commit(smem_u32(&bars->drain));
+            if (elect_one()) mma_commit(smem_u32(&bars->drain));
             mbar_wait_quiet(smem_u32(&bars->drain), 0u);
         }
     } else if (warp < 10) {
@@ -524,30 +566,30 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
             }
         };
         auto step_over = [&](Cursor& q) { q.conv.next(2); q.t += TOK; q.ring.next(nS); };
-        auto load_steps = [&](const Cursor& q, uint32_t (&v)[4]) {
+        auto load_steps = [&](const Cursor& q) -> uint32_t {
             const int g0 = (q.ch0 + box * 128) / p.group;
-            const uint8_t* sc = p.scales + (q.c.t0 + q.t + tok) * p.ld_scales + g0;
-            const bool in_range = q.item < items && q.is_x && q.t + tok < q.c.len;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = (in_range && i < per && g0 + i < groups) ? __ldg(sc + i) : 0u;
+            return (q.item < items && q.is_x && q.t + tok < q.c.len)
+                       ? load_step_bytes(p.scales + (q.c.t0 + q.t + tok) * p.ld_scales + g0, min(per, groups - g0), p.steps_whole != 0) : 0u;
         };
         cur.item = blockIdx.x; cur.t = 0;
         cur.c = chunk_of(cur.item);
         place_of(cur.item, cur.is_x, cur.ch0);
         seek(cur);
-        uint32_t step[4];
-        load_steps(cur, step);
+        uint32_t step = load_steps(cur);
+        Ring mine;                                               // the stage of this group's previous block
+        bool first = true;
         while (cur.item < items) {
             Cursor nxt = cur;
             step_over(nxt);
             seek(nxt);
-            uint32_t step_next[4];
-            load_steps(nxt, step_next);
+            const uint32_t step_next = load_steps(nxt);
             const int live = min(TOK, cur.c.len - cur.t);        // token rows of this block that belong to the chunk
-            bool ok = mbar_wait(smem_u32(&bars->conv_empty[grp]), cur.conv.parity ^ 1u, abort_flag, p.timeout_word, TO_UNPACK) &&
+            bool ok = (first || mbar_wait(smem_u32(&bars->empty[mine.slot]), mine.parity, abort_flag, p.timeout_word, TO_UNPACK)) &&
                       mbar_wait(smem_u32(&bars->full[cur.ring.slot]), cur.ring.parity, abort_flag, p.timeout_word, TO_UNPACK);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
+            first = false;
+            mine = cur.ring;
             uint8_t* big = smem + (size_t)cur.ring.slot * stage_bytes;
             if (cur.is_x) {
                 const uint4* src = reinterpret_cast<const uint4*>(big + box * 8192 + tok * 128);
@@ -558,7 +600,7 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
                 const bool dead = tok >= live;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {                    // 16 channels -> two 16-byte pieces of block j / 4 of 64 channels
-                    const uint32_t s2 = step_bf16x2(p.group == 32 ? step[j >> 1] : p.group == 64 ? step[j >> 2] : step[0]);
+                    const uint32_t s2 = step_bf16x2((step >> ((j * 16 / p.group) * 8)) & 0xFFu);
                     uint32_t v[8];
                     const uint4 w = dead ? make_uint4(0u, 0u, 0u, 0u) : raw[j];      // (and step 0: the expanded value is +0)
                     expand4(w.x, s2, v[0], v[1]);
@@ -572,9 +614,9 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
                 }
             }
             if (live < TOK) {                                    // rows of the next example: zero in the factors, and in dY
-                const int first = cur.is_x ? 4 : 0, rows = TOK - live;
-                for (int i = tid; i < (4 - first + boxes) * rows * 8; i += 128) {
-                    const int b = first + i / (rows * 8), rest = i % (rows * 8);
+                const int from = cur.is_x ? 4 : 0, rows = TOK - live;
+                for (int i = tid; i < (4 - from + boxes) * rows * 8; i += 128) {
+                    const int b = from + i / (rows * 8), rest = i % (rows * 8);
                     *reinterpret_cast<uint4*>(big + b * 8192 + (live + (rest >> 3)) * 128 + (rest & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                 }
             }
@@ -584,8 +626,7 @@ lora_outer_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_con
             }
             if (lane == 0) mbar_arrive(smem_u32(&bars->ready[grp]));
             cur = nxt;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) step[i] = step_next[i];
+            step = step_next;
         }
     } else {
         const int row = (warp & 3) * 32 + lane;
@@ -702,7 +743,7 @@ LoraPlan plan_lora(int64_t T, int64_t n, int32_t in, int32_t out, int32_t rank, 
     if (slices > (kb + 3) / 4) slices = (kb + 3) / 4;
     pl.slices = (int32_t)(slices < 1 ? 1 : slices);
     size_t off = 0;
-    pl.fac_off = off; off += align_up((size_t)2 * T * pl.parts * pl.n64 * 2, 256);
+    pl.fac_off = off; off += align_up((size_t)2 * (T > 0 ? T : 1) * pl.parts * pl.n64 * 2, 256);
     pl.fpart_off = off; off += align_up((size_t)2 * pl.slices * T * pl.n64 * 4, 256);
     pl.part_off = off; off += align_up((size_t)pl.max_slots * rank * ((size_t)in + out) * 4, 256);
     pl.chunk_off = off; off += align_up((size_t)pl.max_chunks * sizeof(LoraChunk), 256);
@@ -719,13 +760,26 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
     if (a.num_joins > 0) QLESS_CUDA_TRY(upload(a.joins, (size_t)a.num_joins * sizeof(LoraJoin), d_joins, st));
     __nv_bfloat16* fac = reinterpret_cast<__nv_bfloat16*>(ws + pl.fac_off);
     const size_t budget = 227 * 1024 - 1024 - sizeof(Bars) - 64;
+    const int64_t rows = a.T > 0 ? a.T : 1;                   // no tokens at all: the maps are not used, every item has length 0
+    const void* codes = a.T > 0 ? (const void*)a.codes : ws;
+    const void* dy = a.T > 0 ? a.grad_out : ws;
+    const int64_t ldc = a.T > 0 ? a.ld_codes : a.in, ldy = (a.T > 0 ? a.ld_grad_out : a.out) * 2;
+    const bool x_whole = a.in % 128 == 0, y_whole = a.out % 64 == 0;
+    const int boxes = pl.parts * (pl.n64 / 64);
+    LoraMaps m;
     qless_status s;
+    if ((s = make_tmap_2d_sw128(&m.codes1, codes, 1, a.in, rows, ldc, 128, 128)) != QLESS_OK) return s;
+    if ((s = x_whole ? make_tmap_blocks_sw128(&m.codes2, codes, 1, a.in / 128, rows, ldc, 128, TOK, 2)
+                     : make_tmap_2d_sw128(&m.codes2, codes, 1, a.in, rows, ldc, 128, TOK)) != QLESS_OK) return s;
+    if ((s = y_whole ? make_tmap_blocks_sw128(&m.dy1, dy, 2, a.out / 64, rows, ldy, 128, 128, 2)
+                     : make_tmap_2d_sw128(&m.dy1, dy, 2, a.out, rows, ldy, 64, 128)) != QLESS_OK) return s;
+    if ((s = y_whole ? make_tmap_blocks_sw128(&m.dy2, dy, 2, a.out / 64, rows, ldy, 128, TOK, 4)
+                     : make_tmap_2d_sw128(&m.dy2, dy, 2, a.out, rows, ldy, 64, TOK)) != QLESS_OK) return s;
+    if ((s = make_tmap_2d_sw128(&m.a, a.T > 0 ? a.lora_a : ws, 2, a.in, a.rank, (uint64_t)a.in * 2, 64, pl.nr)) != QLESS_OK) return s;
+    if ((s = make_tmap_2d_sw128(&m.b, a.T > 0 ? a.lora_b : ws, 2, a.rank, a.out, (uint64_t)a.rank * 2, 64, 128)) != QLESS_OK) return s;
+    if ((s = make_tmap_blocks_sw128(&m.fac, fac, 2, 2 * boxes, rows, 128, rows * 128, TOK, boxes)) != QLESS_OK) return s;
+    const bool steps_whole = a.group == 32 && reinterpret_cast<uintptr_t>(a.scales) % 4 == 0 && a.ld_scales % 4 == 0;
     if (a.T > 0) {
-        CUtensorMap tm_codes, tm_dy, tm_a, tm_b;
-        if ((s = make_tmap_2d_sw128(&tm_codes, a.codes, 1, a.in, a.T, a.ld_codes, 128, 128)) != QLESS_OK) return s;
-        if ((s = make_tmap_2d_sw128(&tm_dy, a.grad_out, 2, a.out, a.T, a.ld_grad_out * 2, 64, 128)) != QLESS_OK) return s;
-        if ((s = make_tmap_2d_sw128(&tm_a, a.lora_a, 2, a.in, a.rank, (uint64_t)a.in * 2, 64, pl.nr)) != QLESS_OK) return s;
-        if ((s = make_tmap_2d_sw128(&tm_b, a.lora_b, 2, a.rank, a.out, (uint64_t)a.rank * 2, 64, 128)) != QLESS_OK) return s;
         FactorParams f;
         f.T = a.T; f.ld_scales = a.ld_scales; f.scales = a.scales;
         f.part = reinterpret_cast<float*>(ws + pl.fpart_off);
@@ -735,6 +789,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
         f.kb_y = ((a.out + CH - 1) / CH + pl.slices - 1) / pl.slices;
         f.token_tiles = (int32_t)pl.token_tiles;
         f.items = 2 * pl.token_tiles * pl.slices;
+        f.y_whole = y_whole; f.steps_whole = steps_whole;
         f.timeout_word = timeout_word;
         const size_t stage = BIG + (size_t)pl.n64 * 256;
         f.stages = (int32_t)(budget / stage < MAX_STAGES ? budget / stage : MAX_STAGES);
@@ -742,7 +797,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
         const int64_t grid = f.items < sm_count() ? f.items : sm_count();
         { ProfileScope ps("lora_factors", st);
           QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_factors_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-          lora_factors_kernel<<<(unsigned)grid, NTHREADS, smem, st>>>(tm_codes, tm_dy, tm_a, tm_b, f); }
+          lora_factors_kernel<<<(unsigned)grid, NTHREADS, smem, st>>>(m, f); }
         QLESS_CUDA_TRY(cudaGetLastError());
         if (pl.slices > 1) {
           ProfileScope ps("lora_split", st);
@@ -753,19 +808,12 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
         QLESS_CUDA_TRY(cudaGetLastError());
         count_launches(1);
     }
-    CUtensorMap tm_codes, tm_dy, tm_h, tm_u;
-    const int64_t rows = a.T > 0 ? a.T : 1;                   // no tokens at all: the maps are not used, every item has length 0
-    const int64_t fw = (int64_t)pl.parts * pl.n64;
-    const void* any = ws;
-    if ((s = make_tmap_2d_sw128(&tm_codes, a.T > 0 ? (const void*)a.codes : any, 1, a.in, rows, a.T > 0 ? a.ld_codes : a.in, 128, TOK)) != QLESS_OK) return s;
-    if ((s = make_tmap_2d_sw128(&tm_dy, a.T > 0 ? a.grad_out : any, 2, a.out, rows, (a.T > 0 ? a.ld_grad_out : a.out) * 2, 64, TOK)) != QLESS_OK) return s;
-    if ((s = make_tmap_2d_sw128(&tm_h, fac, 2, fw, rows, fw * 2, 64, TOK)) != QLESS_OK) return s;
-    if ((s = make_tmap_2d_sw128(&tm_u, fac + a.T * fw, 2, fw, rows, fw * 2, 64, TOK)) != QLESS_OK) return s;
     OuterParams o;
     o.chunks = d_chunks; o.scales = a.scales; o.ld_scales = a.ld_scales; o.ld_grads = a.ld_grads;
     o.grads = a.grads; o.part = reinterpret_cast<float*>(ws + pl.part_off);
     o.in = a.in; o.out = a.out; o.rank = a.rank; o.group = a.group; o.nr = pl.nr;
     o.tiles_x = pl.tiles_x; o.tiles = pl.tiles; o.timeout_word = timeout_word;
+    o.x_whole = x_whole; o.y_whole = y_whole; o.steps_whole = steps_whole;
     o.items = (int64_t)a.num_chunks * pl.tiles;
     QLESS_REQUIRE(o.items < ((int64_t)1 << 31) - 65536, QLESS_ERR_UNSUPPORTED, "too many examples: %lld pieces of %d tiles", (long long)a.num_chunks, pl.tiles);
     const size_t stage = BIG + (size_t)pl.parts * (pl.n64 / 64) * 8192;
@@ -776,7 +824,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
     { ProfileScope ps("lora_outer", st);
 #define QLESS_LAUNCH_LORA_OUTER(OUT, N)                                                                                              \
       QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_outer_kernel<OUT, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));          \
-      lora_outer_kernel<OUT, N><<<(unsigned)grid, NTHREADS, smem, st>>>(tm_codes, tm_dy, tm_h, tm_u, o);
+      lora_outer_kernel<OUT, N><<<(unsigned)grid, NTHREADS, smem, st>>>(m, o);
       if (a.dtype == QLESS_F32) {
           if (pl.n64 == 64) { QLESS_LAUNCH_LORA_OUTER(float, 64) } else { QLESS_LAUNCH_LORA_OUTER(float, 128) }
       } else {

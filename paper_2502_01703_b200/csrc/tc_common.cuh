@@ -110,6 +110,16 @@ __device__ __forceinline__ bool mbar_wait_quiet(uint32_t bar, uint32_t parity, u
     return false;
 }
 
+// True in one lane of a fully active warp. A role that issues copies or tensor-core instructions runs with its whole warp and issues
+// under this: the operands then live in uniform registers (eight products with a wait and a commit take 770 clocks of the issuing
+// warp this way and 1310 when a single thread runs the role).
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
+
 // ---- CTA pairs (cta_group::2) --------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_ctarank()
 {
@@ -419,6 +429,11 @@ __device__ __forceinline__ void mma_commit(uint32_t bar)
 // elem_bytes in {1, 2}; box_inner * elem_bytes must be 128.
 qless_status make_tmap_2d_sw128(CUtensorMap* out, const void* base, int elem_bytes, uint64_t inner, uint64_t outer,
                                 uint64_t row_stride_bytes, uint32_t box_inner, uint32_t box_outer);
+
+// Host: a matrix of `blocks` side-by-side column blocks of 128 bytes, seen as [block][row][128 bytes] (block_stride bytes apart,
+// rows row_stride bytes apart), so that one copy brings box_blocks blocks of box_rows rows each, 128-byte-swizzled.
+qless_status make_tmap_blocks_sw128(CUtensorMap* out, const void* base, int elem_bytes, uint64_t blocks, uint64_t rows, uint64_t row_stride,
+                                    uint64_t block_stride, uint32_t box_rows, uint32_t box_blocks);
 
 // Host: 3-D byte tensor map [outer2][outer1][inner bytes] (uint8 elements). swizzle128 = true needs a 128-byte
 // wide box; otherwise the box lands in shared memory as plain rows of box_inner bytes (a multiple of 16).
