@@ -62,7 +62,7 @@ struct OuterParams {
 struct LoraMaps { CUtensorMap codes1, codes2, dy1, dy2, a, b, fac; };
 
 struct __align__(8) Bars {
-    uint64_t full[MAX_STAGES], empty[MAX_STAGES], ready[2], d_full[2], d_empty[2], drain;
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES], ready[MAX_STAGES], d_full[2], d_empty[2], read[2], drain;
     uint32_t tmem_base, abort_flag;
 };
 
@@ -119,11 +119,11 @@ __device__ __forceinline__ uint32_t split_term(float& a, float& b)
 
 __device__ __forceinline__ void init_barriers(Bars* b)
 {
-    for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(smem_u32(&b->full[s]), 1); mbar_init(smem_u32(&b->empty[s]), 1); }
+    for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(smem_u32(&b->full[s]), 1); mbar_init(smem_u32(&b->empty[s]), 1); mbar_init(smem_u32(&b->ready[s]), 4); }
     for (int s = 0; s < 2; ++s) {
-        mbar_init(smem_u32(&b->ready[s]), 4);
         mbar_init(smem_u32(&b->d_full[s]), 1);
         mbar_init(smem_u32(&b->d_empty[s]), 4);
+        mbar_init(smem_u32(&b->read[s]), 4);
     }
     mbar_init(smem_u32(&b->drain), 1);
     b->abort_flag = 0;
@@ -436,8 +436,7 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
     constexpr bool WIDE = PARTS * N64 == 128;
     constexpr int boxes = PARTS * (N64 / 64);                // factor operand: boxes of 64 columns x 64 tokens
     constexpr int stage_bytes = BIG + boxes * 8192;
-    uint8_t* conv_buf = smem + (size_t)p.stages * stage_bytes;      // expanded codes: two buffers of 256 channels x 64 tokens
-    Bars* bars = reinterpret_cast<Bars*>(conv_buf + 2 * 32768);
+    Bars* bars = reinterpret_cast<Bars*>(smem + (size_t)p.stages * stage_bytes);
     volatile uint32_t* abort_flag = &bars->abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t nS = (uint32_t)p.stages;
@@ -502,7 +501,7 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
         {
             const uint32_t idesc = make_idesc(1, 1, 1, 128, WIDE ? 128 : p.nr) | IDESC_A_MN | IDESC_B_MN;
             constexpr int TERMS = WIDE ? 1 : PARTS;
-            Ring ring, conv;
+            Ring ring;
             uint32_t n = 0;
             bool ok = true;
             LoraChunk ahead = chunk_of(blockIdx.x);
@@ -515,13 +514,12 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
                 const uint32_t buf = n & 1u;
                 if (!warp_wait(&bars->d_empty[buf], ((n >> 1) & 1u) ^ 1u, TO_MMA)) { ok = false; break; }
                 tc_fence_after();
-                for (int t = 0; t < c.len; t += TOK, ring.next(nS), conv.next(2)) {
-                    if (!warp_wait(&bars->ready[conv.slot], conv.parity, TO_MMA)) { ok = false; break; }
+                for (int t = 0; t < c.len; t += TOK, ring.next(nS)) {
+                    if (!warp_wait(&bars->ready[ring.slot], ring.parity, TO_MMA)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
-                    const uint32_t a = is_x ? smem_u32(conv_buf) + conv.slot * 32768 : big;
                     if (elect_one()) {
-                    const uint64_t a0 = make_smem_desc_mn_sw128(a, 8192), b0 = make_smem_desc_mn_sw128(op, 8192);
+                    const uint64_t a0 = make_smem_desc_mn_sw128(big, 8192), b0 = make_smem_desc_mn_sw128(op, 8192);
                     for (int m = 0; m < subs; ++m) {
                         const uint64_t am = a0 + (uint64_t)(m * 1024);
                         const uint32_t d = tmem + buf * 256 + m * 128;
@@ -543,13 +541,15 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
             mbar_wait_quiet(smem_u32(&bars->drain), 0u);
         }
     } else if (warp < 10) {
-        // Converters: two groups of four warps take alternate blocks (as above: every block, dY untouched but for the last, partly
-        // filled block of a chunk). A thread owns one token and 128 channels; the step bytes of its next block are requested before it
-        // works on the present one.
+        // Converters: two groups of four warps take alternate blocks (every block passes through them, dY untouched but for the last,
+        // partly filled block of a piece). A thread owns one token and 128 channels; the step bytes of its next block are requested
+        // before it works on the present one. The number of stages is even, so that a stage always belongs to the same group: the
+        // phase of its barrier that the group waits for is the one behind the phase it saw last. A group may run ahead of the products by
+        // as many stages as there are, so each stage has its own barrier for what the group is done with.
         const int tid = (threadIdx.x - 64) & 127, tok = tid & 63, box = tid >> 6;
         const uint32_t grp = warp >= 6 ? 1u : 0u;
         const int groups = (p.in + p.group - 1) / p.group, per = 128 / p.group;
-        struct Cursor { uint32_t item; LoraChunk c; bool is_x; int ch0, t; Ring ring, conv; } cur;
+        struct Cursor { uint32_t item; LoraChunk c; bool is_x; int ch0, t; Ring ring; } cur;
         // The next block of this group, at or behind the cursor's place.
         auto seek = [&](Cursor& q) {
             while (q.item < items) {
@@ -561,11 +561,11 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
                     q.t = 0;
                     continue;
                 }
-                if (q.conv.slot == grp) return;
-                q.conv.next(2); q.t += TOK; q.ring.next(nS);
+                if ((q.ring.slot & 1u) == grp) return;
+                q.t += TOK; q.ring.next(nS);
             }
         };
-        auto step_over = [&](Cursor& q) { q.conv.next(2); q.t += TOK; q.ring.next(nS); };
+        auto step_over = [&](Cursor& q) { q.t += TOK; q.ring.next(nS); };
         auto load_steps = [&](const Cursor& q) -> uint32_t {
             const int g0 = (q.ch0 + box * 128) / p.group;
             return (q.item < items && q.is_x && q.t + tok < q.c.len)
@@ -575,28 +575,30 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
         cur.c = chunk_of(cur.item);
         place_of(cur.item, cur.is_x, cur.ch0);
         seek(cur);
-        uint32_t step = load_steps(cur);
-        Ring mine;                                               // the stage of this group's previous block
-        bool first = true;
+        uint32_t step = load_steps(cur), read_parity = 0u;
         while (cur.item < items) {
             Cursor nxt = cur;
             step_over(nxt);
             seek(nxt);
             const uint32_t step_next = load_steps(nxt);
             const int live = min(TOK, cur.c.len - cur.t);        // token rows of this block that belong to the chunk
-            bool ok = (first || mbar_wait(smem_u32(&bars->empty[mine.slot]), mine.parity, abort_flag, p.timeout_word, TO_UNPACK)) &&
-                      mbar_wait(smem_u32(&bars->full[cur.ring.slot]), cur.ring.parity, abort_flag, p.timeout_word, TO_UNPACK);
+            bool ok = mbar_wait(smem_u32(&bars->full[cur.ring.slot]), cur.ring.parity, abort_flag, p.timeout_word, TO_UNPACK);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
-            first = false;
-            mine = cur.ring;
             uint8_t* big = smem + (size_t)cur.ring.slot * stage_bytes;
             if (cur.is_x) {
                 const uint4* src = reinterpret_cast<const uint4*>(big + box * 8192 + tok * 128);
                 uint4 raw[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) raw[j] = src[j ^ (tok & 7)];
-                uint8_t* out = conv_buf + grp * 32768 + box * 16384 + tok * 128;
+                // The codes take half of the stage; expanded they take all of it, once every thread of the group has read its share.
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars->read[grp]));
+                ok = mbar_wait(smem_u32(&bars->read[grp]), read_parity, abort_flag, p.timeout_word, TO_UNPACK);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                read_parity ^= 1u;
+                uint8_t* out = big + box * 16384 + tok * 128;
                 const bool dead = tok >= live;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {                    // 16 channels -> two 16-byte pieces of block j / 4 of 64 channels
@@ -624,7 +626,7 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
                 fence_proxy_async_smem();
                 __syncwarp();
             }
-            if (lane == 0) mbar_arrive(smem_u32(&bars->ready[grp]));
+            if (lane == 0) mbar_arrive(smem_u32(&bars->ready[cur.ring.slot]));
             cur = nxt;
             step = step_next;
         }
@@ -817,9 +819,8 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
     o.items = (int64_t)a.num_chunks * pl.tiles;
     QLESS_REQUIRE(o.items < ((int64_t)1 << 31) - 65536, QLESS_ERR_UNSUPPORTED, "too many examples: %lld pieces of %d tiles", (long long)a.num_chunks, pl.tiles);
     const size_t stage = BIG + (size_t)pl.parts * (pl.n64 / 64) * 8192;
-    const size_t left = budget - 2 * 32768;
-    o.stages = (int32_t)(left / stage < MAX_STAGES ? left / stage : MAX_STAGES);
-    const size_t smem = 1024 + o.stages * stage + 2 * 32768 + sizeof(Bars);
+    o.stages = (int32_t)(budget / stage < MAX_STAGES ? budget / stage : MAX_STAGES) & ~1;
+    const size_t smem = 1024 + o.stages * stage + sizeof(Bars);
     const int64_t grid = o.items < sm_count() ? o.items : sm_count();
     { ProfileScope ps("lora_outer", st);
 #define QLESS_LAUNCH_LORA_OUTER(OUT, N)                                                                                              \
