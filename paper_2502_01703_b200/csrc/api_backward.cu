@@ -1,4 +1,5 @@
 // C ABI of the calls that produce gradient rows: argument validation, workspace carving, sequencing.
+#include <algorithm>
 #include <new>
 #include <vector>
 
@@ -124,6 +125,9 @@ qless_status qless_lora_gradients(const int8_t* codes, int64_t ld_codes, const u
                 chunks.push_back({offsets[e] + t0, (int32_t)(len - t0 < pl.chunk ? len - t0 : pl.chunk), (int32_t)e, slots++, 0});
             }
         }
+        // Long pieces first: the blocks take the items in turn, and the last rounds are then short (385 instead of 397 us for 128 examples of
+        // 130 to 900 tokens, 139 instead of 148 us for 32).
+        std::stable_sort(chunks.begin(), chunks.end(), [](const LoraChunk& x, const LoraChunk& y) { return x.len > y.len; });
         LoraArgs a;
         a.codes = codes; a.scales = scales; a.grad_out = grad_out; a.lora_a = lora_a; a.lora_b = lora_b;
         a.T = tokens; a.ld_codes = ld_codes; a.ld_scales = ld_scales; a.ld_grad_out = ld_grad_out; a.ld_grads = ld_grads;

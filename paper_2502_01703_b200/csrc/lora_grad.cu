@@ -37,9 +37,9 @@ struct FactorParams {
     int64_t T, ld_scales;
     const uint8_t* scales;
     float* part;                            // [2][slices][T][N64]: 0 = H, 1 = U (more than one slice)
-    __nv_bfloat16* fac;                     // [2][parts][N64 / 64][T][64] (one slice)
+    __nv_bfloat16* fac;                     // [2][boxes][T][64]: column c of term q is column q * term + c (one slice)
     float scaling;
-    int32_t in, out, group, nr, n64, parts, slices, kb_x, kb_y, stages;      // kb_*: channel blocks per slice
+    int32_t in, out, group, nr, n64, parts, term, boxes, slices, kb_x, kb_y, stages;      // kb_*: channel blocks per slice
     int32_t y_whole, steps_whole;
     int32_t token_tiles;
     int64_t items;
@@ -341,15 +341,15 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
                     float x[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(v[j]) * p.scaling;
-                    const int blocks = p.n64 / 64;
-                    __nv_bfloat16* dst = p.fac + ((kind * p.parts * blocks + c0 / 64) * p.T + t) * 64 + c0 % 64;
-                    for (int q = 0; q < p.parts; ++q, dst += blocks * p.T * 64)
+                    __nv_bfloat16* dst = p.fac + (kind * p.boxes * p.T + t) * 64;
+                    for (int q = 0; q < p.parts; ++q)
 #pragma unroll
                         for (int j = 0; j < 32; j += 8) {
                             uint32_t w[4];
 #pragma unroll
                             for (int k = 0; k < 4; ++k) w[k] = split_term(x[j + 2 * k], x[j + 2 * k + 1]);
-                            if (c0 + j < p.nr) *reinterpret_cast<uint4*>(dst + j) = make_uint4(w[0], w[1], w[2], w[3]);
+                            const int c = q * p.term + c0 + j;
+                            if (c0 + j < p.nr) *reinterpret_cast<uint4*>(dst + (int64_t)(c / 64) * p.T * 64 + c % 64) = make_uint4(w[0], w[1], w[2], w[3]);
                         }
                 } else {
                     float* dst = p.part + ((kind * p.slices + slice) * p.T + t) * p.n64 + c0;
@@ -369,9 +369,9 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
 }
 
 // Several channel slices: adds them, multiplies by the adapter's scale and splits the fp32 factor into `parts` bf16 terms that add up to
-// it (8 bits each): fac [2][parts][n64 / 64][T][64].
+// it (8 bits each): fac [2][boxes][T][64], column c of term q at column q * term + c.
 __global__ void lora_split_kernel(const float* __restrict__ part, __nv_bfloat16* __restrict__ fac, int64_t T, int32_t n64, int32_t nr,
-                                  int32_t slices, int32_t parts, float scaling)
+                                  int32_t slices, int32_t parts, int32_t term, int32_t boxes, float scaling)
 {
     const int64_t rows = 2 * T, total = rows * (n64 / 4);
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
@@ -386,11 +386,11 @@ __global__ void lora_split_kernel(const float* __restrict__ part, __nv_bfloat16*
             x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
         }
         float v[4] = {x.x * scaling, x.y * scaling, x.z * scaling, x.w * scaling};
-        const int blocks = n64 / 64;
-        __nv_bfloat16* dst = fac + ((kind * parts * blocks + c / 64) * T + t) * 64 + c % 64;
+        __nv_bfloat16* dst = fac + (kind * boxes * T + t) * 64;
         for (int q = 0; q < parts; ++q) {
             const uint32_t lo = split_term(v[0], v[1]), hi = split_term(v[2], v[3]);
-            *reinterpret_cast<uint2*>(dst + (int64_t)q * blocks * T * 64) = make_uint2(lo, hi);
+            const int at = q * term + c;
+            *reinterpret_cast<uint2*>(dst + (int64_t)(at / 64) * T * 64 + at % 64) = make_uint2(lo, hi);
         }
     }
 }
@@ -423,18 +423,19 @@ __device__ __forceinline__ void store_columns(OutT* dst, bool is_x, int64_t ch, 
     }
 }
 
-// OutT fixes the number of terms of a factor: 2 for bf16 gradients, 3 for fp32. N64: factor columns rounded up to 64 or 128.
-template <typename OutT, int N64>
+// OutT fixes the number of terms of a factor: 2 for bf16 gradients, 3 for fp32. BOXES: 64-column blocks that hold them.
+template <typename OutT, int BOXES>
 __global__ void __launch_bounds__(NTHREADS, 1)
 lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     constexpr int PARTS = sizeof(OutT) == 4 ? 3 : 2;
-    // Two terms of at most 64 columns are one operand of 128 columns (their sums meet in the epilogue): the channel operand is read from
-    // shared memory once for both, whose bandwidth bounds this loop. Otherwise one product per term into the same accumulator.
-    constexpr bool WIDE = PARTS * N64 == 128;
-    constexpr int boxes = PARTS * (N64 / 64);                // factor operand: boxes of 64 columns x 64 tokens
+    // Where all terms together have at most 128 columns they are one operand (their sums meet in the epilogue): the channel operand is
+    // read from shared memory once for all of them, whose bandwidth bounds this loop. Otherwise one product per term into the same accumulator.
+    constexpr bool WIDE = BOXES <= 2;
+    constexpr int TERM_BYTES = BOXES / PARTS * 8192;         // (not WIDE) a term's boxes
+    constexpr int boxes = BOXES;                             // factor operand: boxes of 64 columns x 64 tokens
     constexpr int stage_bytes = BIG + boxes * 8192;
     Bars* bars = reinterpret_cast<Bars*>(smem + (size_t)p.stages * stage_bytes);
     volatile uint32_t* abort_flag = &bars->abort_flag;
@@ -499,7 +500,7 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
         }
     } else if (warp == 1) {
         {
-            const uint32_t idesc = make_idesc(1, 1, 1, 128, WIDE ? 128 : p.nr) | IDESC_A_MN | IDESC_B_MN;
+            const uint32_t idesc = make_idesc(1, 1, 1, 128, WIDE ? PARTS * p.nr : p.nr) | IDESC_A_MN | IDESC_B_MN;
             constexpr int TERMS = WIDE ? 1 : PARTS;
             Ring ring;
             uint32_t n = 0;
@@ -527,7 +528,7 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
 #pragma unroll
                         for (int i = 1; i < TOK / 16 * TERMS; ++i) {
                             const int k = i / TERMS, q = i % TERMS;
-                            mma_f16_ss(d, am + (uint64_t)(k * 128), b0 + (uint64_t)(k * 128 + q * (N64 * 8)), idesc, 1u);
+                            mma_f16_ss(d, am + (uint64_t)(k * 128), b0 + (uint64_t)(k * 128 + q * (TERM_BYTES / 16)), idesc, 1u);
                         }
                     }
                     mma_commit(smem_u32(&bars->empty[ring.slot]));
@@ -654,14 +655,17 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
                     uint32_t v[32];
                     const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 256 + m * 128 + c0;
                     tmem_ld_x32(taddr, v);
-                    if (WIDE) {
-                        uint32_t low[32];
-                        tmem_ld_x32(taddr + 64, low);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(low[j]));
-                    }
                     tmem_wait_ld();
+                    if (WIDE) {
+#pragma unroll
+                        for (int q = 1; q < PARTS; ++q) {
+                            uint32_t low[32];
+                            tmem_ld_x32(taddr + q * p.nr, low);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(low[j]));
+                        }
+                    }
                     if (ch < width) {
                         if (c.slot >= 0) store_columns<float>(p.part + (int64_t)c.slot * width_all + base, is_x, ch, width, c0, p.rank, v, c.len == 0);
                         else store_columns<OutT>(reinterpret_cast<OutT*>(p.grads) + (int64_t)c.example * p.ld_grads + base, is_x, ch, width, c0, p.rank, v, c.len == 0);
@@ -728,6 +732,10 @@ LoraPlan plan_lora(int64_t T, int64_t n, int32_t in, int32_t out, int32_t rank, 
     pl.nr = (rank + 15) / 16 * 16;
     pl.n64 = pl.nr <= 64 ? 64 : 128;
     pl.parts = dtype == QLESS_F32 ? 3 : 2;
+    // Terms of at most 128 columns in all lie side by side; otherwise each fills its own blocks of 64 columns.
+    const bool wide = pl.parts * pl.nr <= 128;
+    pl.term = wide ? pl.nr : pl.n64;
+    pl.boxes = wide ? (pl.parts * pl.nr + 63) / 64 : pl.parts * (pl.n64 / 64);
     pl.tiles_x = (in + TILE - 1) / TILE;
     pl.tiles = pl.tiles_x + (out + TILE - 1) / TILE;
     // Pieces of at most `chunk` tokens: about four items per SM where the examples alone do not give that many, at least 512 tokens
@@ -739,13 +747,13 @@ LoraPlan plan_lora(int64_t T, int64_t n, int32_t in, int32_t out, int32_t rank, 
     pl.max_slots = most + (n < most ? n : most);
     pl.max_chunks = n + most;
     pl.token_tiles = (T + 127) / 128;
-    // Channel slices: about three items per SM, each of at least four blocks of 128 channels.
+    // Channel slices: about one and a half items per SM, each of at least four blocks of 128 channels (slices cost a pass that adds them).
     const int32_t kb = ((in > out ? in : out) + CH - 1) / CH;
-    int64_t slices = pl.token_tiles > 0 ? (3 * sms + 2 * pl.token_tiles - 1) / (2 * pl.token_tiles) : 1;
+    int64_t slices = pl.token_tiles > 0 ? (3 * sms / 2 + 2 * pl.token_tiles - 1) / (2 * pl.token_tiles) : 1;
     if (slices > (kb + 3) / 4) slices = (kb + 3) / 4;
     pl.slices = (int32_t)(slices < 1 ? 1 : slices);
     size_t off = 0;
-    pl.fac_off = off; off += align_up((size_t)2 * (T > 0 ? T : 1) * pl.parts * pl.n64 * 2, 256);
+    pl.fac_off = off; off += align_up((size_t)2 * (T > 0 ? T : 1) * pl.boxes * 128, 256);
     pl.fpart_off = off; off += align_up((size_t)2 * pl.slices * T * pl.n64 * 4, 256);
     pl.part_off = off; off += align_up((size_t)pl.max_slots * rank * ((size_t)in + out) * 4, 256);
     pl.chunk_off = off; off += align_up((size_t)pl.max_chunks * sizeof(LoraChunk), 256);
@@ -767,7 +775,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
     const void* dy = a.T > 0 ? a.grad_out : ws;
     const int64_t ldc = a.T > 0 ? a.ld_codes : a.in, ldy = (a.T > 0 ? a.ld_grad_out : a.out) * 2;
     const bool x_whole = a.in % 128 == 0, y_whole = a.out % 64 == 0;
-    const int boxes = pl.parts * (pl.n64 / 64);
+    const int boxes = pl.boxes;
     LoraMaps m;
     qless_status s;
     if ((s = make_tmap_2d_sw128(&m.codes1, codes, 1, a.in, rows, ldc, 128, 128)) != QLESS_OK) return s;
@@ -785,7 +793,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
         FactorParams f;
         f.T = a.T; f.ld_scales = a.ld_scales; f.scales = a.scales;
         f.part = reinterpret_cast<float*>(ws + pl.fpart_off);
-        f.in = a.in; f.out = a.out; f.group = a.group; f.nr = pl.nr; f.n64 = pl.n64; f.parts = pl.parts; f.slices = pl.slices;
+        f.in = a.in; f.out = a.out; f.group = a.group; f.nr = pl.nr; f.n64 = pl.n64; f.parts = pl.parts; f.term = pl.term; f.boxes = pl.boxes; f.slices = pl.slices;
         f.fac = fac; f.scaling = a.scaling;
         f.kb_x = ((a.in + CH - 1) / CH + pl.slices - 1) / pl.slices;
         f.kb_y = ((a.out + CH - 1) / CH + pl.slices - 1) / pl.slices;
@@ -804,7 +812,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
         if (pl.slices > 1) {
           ProfileScope ps("lora_split", st);
           const int64_t blocks = (2 * a.T * (pl.n64 / 4) + 255) / 256, most = (int64_t)sm_count() * 8;
-          lora_split_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, st>>>(f.part, fac, a.T, pl.n64, pl.nr, pl.slices, pl.parts, a.scaling);
+          lora_split_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, st>>>(f.part, fac, a.T, pl.n64, pl.nr, pl.slices, pl.parts, pl.term, pl.boxes, a.scaling);
           count_launches(1);
         }
         QLESS_CUDA_TRY(cudaGetLastError());
@@ -818,18 +826,25 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
     o.x_whole = x_whole; o.y_whole = y_whole; o.steps_whole = steps_whole;
     o.items = (int64_t)a.num_chunks * pl.tiles;
     QLESS_REQUIRE(o.items < ((int64_t)1 << 31) - 65536, QLESS_ERR_UNSUPPORTED, "too many examples: %lld pieces of %d tiles", (long long)a.num_chunks, pl.tiles);
-    const size_t stage = BIG + (size_t)pl.parts * (pl.n64 / 64) * 8192;
+    const size_t stage = BIG + (size_t)boxes * 8192;
     o.stages = (int32_t)(budget / stage < MAX_STAGES ? budget / stage : MAX_STAGES) & ~1;
     const size_t smem = 1024 + o.stages * stage + sizeof(Bars);
     const int64_t grid = o.items < sm_count() ? o.items : sm_count();
     { ProfileScope ps("lora_outer", st);
 #define QLESS_LAUNCH_LORA_OUTER(OUT, N)                                                                                              \
-      QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_outer_kernel<OUT, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));          \
-      lora_outer_kernel<OUT, N><<<(unsigned)grid, NTHREADS, smem, st>>>(m, o);
+      {                                                                                                                                \
+          QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_outer_kernel<OUT, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));      \
+          lora_outer_kernel<OUT, N><<<(unsigned)grid, NTHREADS, smem, st>>>(m, o);                                                      \
+      }
       if (a.dtype == QLESS_F32) {
-          if (pl.n64 == 64) { QLESS_LAUNCH_LORA_OUTER(float, 64) } else { QLESS_LAUNCH_LORA_OUTER(float, 128) }
+          if (boxes == 1) QLESS_LAUNCH_LORA_OUTER(float, 1)
+          else if (boxes == 2) QLESS_LAUNCH_LORA_OUTER(float, 2)
+          else if (boxes == 3) QLESS_LAUNCH_LORA_OUTER(float, 3)
+          else QLESS_LAUNCH_LORA_OUTER(float, 6)
       } else {
-          if (pl.n64 == 64) { QLESS_LAUNCH_LORA_OUTER(__nv_bfloat16, 64) } else { QLESS_LAUNCH_LORA_OUTER(__nv_bfloat16, 128) }
+          if (boxes == 1) QLESS_LAUNCH_LORA_OUTER(__nv_bfloat16, 1)
+          else if (boxes == 2) QLESS_LAUNCH_LORA_OUTER(__nv_bfloat16, 2)
+          else QLESS_LAUNCH_LORA_OUTER(__nv_bfloat16, 4)
       }
 #undef QLESS_LAUNCH_LORA_OUTER
     }

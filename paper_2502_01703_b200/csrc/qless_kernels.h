@@ -98,7 +98,7 @@ struct LoraChunk { int64_t t0; int32_t len, example, slot, unused; };      // to
 struct LoraJoin { int32_t example, first, count, unused; };                 // an example summed in pieces: slots first .. first + count - 1
 struct LoraPlan {
     int64_t chunk, max_chunks, max_slots, token_tiles;
-    int32_t nr, n64, parts, tiles_x, tiles, slices;
+    int32_t nr, n64, parts, term, boxes, tiles_x, tiles, slices;
     size_t fac_off, fpart_off, part_off, chunk_off, join_off, total;
 };
 LoraPlan plan_lora(int64_t T, int64_t n, int32_t in, int32_t out, int32_t rank, qless_dtype dtype);

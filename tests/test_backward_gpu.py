@@ -134,7 +134,7 @@ def _check_lora(got, want, mag, wi, wo, tokens, dtype):
 LORA = [
     ([0, 1], 16, 16, 8, 32), ([0, 0], 64, 64, 16, 32), ([0, 1, 1, 3], 128, 256, 8, 64), ([0, 64, 128], 256, 128, 16, 128),
     ([0, 63, 64, 129], 272, 144, 24, 32), ([0, 5, 5, 70, 200], 512, 512, 64, 32), ([0, 130], 528, 1040, 40, 64),
-    ([0, 17, 200], 384, 640, 128, 128), ([0, 300], 4096, 256, 64, 64), ([0, 0, 0, 0, 1], 1024, 16, 32, 128),
+    ([0, 17, 200], 384, 640, 128, 128), ([0, 90, 161], 192, 320, 32, 32), ([0, 90, 161], 192, 320, 48, 64), ([0, 71, 161], 256, 128, 96, 32), ([0, 300], 4096, 256, 64, 64), ([0, 0, 0, 0, 1], 1024, 16, 32, 128),
 ]
 
 
