@@ -26,7 +26,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int NTHREADS = 448;               // warp 0 TMA, warp 1 MMA, warps 2-9 converters, warps 10-13 epilogue
+constexpr int NTHREADS = 704;               // warp 0 TMA, warp 1 MMA, warps 2-17 converters, warps 18-21 epilogue
 constexpr int MAX_STAGES = 4;
 constexpr int BIG = 32768;                  // operand bytes of one stage that come from the activations or dY
 constexpr int CH = 128;                     // (1) channels per stage
@@ -62,7 +62,7 @@ struct OuterParams {
 struct LoraMaps { CUtensorMap codes1, codes2, dy1, dy2, a, b, fac; };
 
 struct __align__(8) Bars {
-    uint64_t full[MAX_STAGES], empty[MAX_STAGES], ready[MAX_STAGES], d_full[2], d_empty[2], read[2], drain;
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES], ready[MAX_STAGES], read[MAX_STAGES], d_full[2], d_empty[2], drain;
     uint32_t tmem_base, abort_flag;
 };
 
@@ -119,11 +119,10 @@ __device__ __forceinline__ uint32_t split_term(float& a, float& b)
 
 __device__ __forceinline__ void init_barriers(Bars* b)
 {
-    for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(smem_u32(&b->full[s]), 1); mbar_init(smem_u32(&b->empty[s]), 1); mbar_init(smem_u32(&b->ready[s]), 4); }
+    for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(smem_u32(&b->full[s]), 1); mbar_init(smem_u32(&b->empty[s]), 1); mbar_init(smem_u32(&b->ready[s]), 4); mbar_init(smem_u32(&b->read[s]), 4); }
     for (int s = 0; s < 2; ++s) {
         mbar_init(smem_u32(&b->d_full[s]), 1);
         mbar_init(smem_u32(&b->d_empty[s]), 4);
-        mbar_init(smem_u32(&b->read[s]), 4);
     }
     mbar_init(smem_u32(&b->drain), 1);
     b->abort_flag = 0;
@@ -159,7 +158,7 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = bars->tmem_base;                  // accumulators at columns 0 and 128, expanded codes at 256 and 320
+    const uint32_t tmem = bars->tmem_base;                  // accumulators at columns 0 and 128, expanded codes of stage s at 256 + 64 s
 
     // item -> (slice, token tile, kind): of two neighbouring items one reads codes and one dY, and a block takes them in turn, so that at
     // any time half of the blocks read the one (bound by the work per block of codes) and half the other (bound by its bytes).
@@ -212,7 +211,7 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
     } else if (warp == 1) {
         {
             const uint32_t idesc_x = make_idesc(1, 1, 1, 128, p.nr), idesc_y = idesc_x | IDESC_B_MN;
-            Ring ring, conv;
+            Ring ring;
             uint32_t n = 0;
             bool ok = true;
             for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++n) {
@@ -223,14 +222,14 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
                 tc_fence_after();
                 for (int kb = kb0; kb < kb1; ++kb, ring.next(nS)) {
                     // the converters have seen the stage's copies land before they arrive here
-                    if (!warp_wait(&bars->ready[conv.slot], conv.parity, TO_MMA)) { ok = false; break; }
+                    if (!warp_wait(&bars->ready[ring.slot], ring.parity, TO_MMA)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
                     if (elect_one()) {
                     // Descriptors are made once per stage and advanced by constants (addresses in units of 16 bytes): made anew for every
                     // product they took 180 clocks of this thread where the product takes 48.
                     if (is_x) {
-                        const uint32_t a = tmem + 256 + conv.slot * 64;
+                        const uint32_t a = tmem + 256 + ring.slot * 64;
                         const uint64_t b0 = make_smem_desc_sw128(op), b1 = make_smem_desc_sw128(op + p.n64 * 128);
                         mma_f16_ts(d, a, b0, idesc_x, kb > kb0);
 #pragma unroll
@@ -245,7 +244,6 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
                     mma_commit(smem_u32(&bars->empty[ring.slot]));
                     }
                     __syncwarp();
-                    conv.next(2);
                 }
                 if (ok && elect_one()) mma_commit(smem_u32(&bars->d_full[buf]));
                 __syncwarp();
@@ -253,16 +251,15 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
             if (elect_one()) mma_commit(smem_u32(&bars->drain));               // every MMA issued above completes before tensor memory is freed
             mbar_wait_quiet(smem_u32(&bars->drain), 0u);
         }
-    } else if (warp < 10) {
-        // Converters: thread = token = TMEM lane; warps 2-5 and 6-9 take alternate blocks, so that the barrier round trips of one
-        // overlap the work on the next. Every block passes through them, those of dY untouched: a group may look at a stage's barrier
-        // only once the stage's previous use is over (a parity would otherwise be mistaken for that of two uses before), which
-        // it knows from the products of its own previous block being done.
+    } else if (warp < 18) {
+        // Converters: thread = token = TMEM lane; a group of four warps to each stage (there are two or four), so that the barrier round
+        // trips and latencies of one block overlap the work on the others. Every block passes through them, those of dY untouched: the
+        // phase of a stage's barrier that its group waits for is always the one behind the phase it saw last.
         const int row = (warp & 3) * 32 + lane;
-        const uint32_t grp = warp >= 6 ? 1u : 0u;
+        const uint32_t grp = (uint32_t)(warp - 2) >> 2;
         const int groups = (p.in + p.group - 1) / p.group, per = CH / p.group;
-        Ring ring, conv, mine;                                 // mine: the stage of this group's previous block
-        bool ok = true, first = true;
+        Ring ring;
+        bool ok = grp < nS;
         for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
             int slice, kb0, kb1; bool is_x; int64_t tile;
             item_of(item, slice, is_x, tile, kb0, kb1);
@@ -273,19 +270,15 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
             };
             uint32_t ahead = 0u;
             bool loaded = false;
-            for (int kb = kb0; kb < kb1 && ok; ++kb, ring.next(nS), conv.next(2)) {
-                if (conv.slot != grp) continue;
+            for (int kb = kb0; kb < kb1 && ok; ++kb, ring.next(nS)) {
+                if (ring.slot != grp) continue;
                 const uint32_t step = loaded ? ahead : load_steps(kb);
-                loaded = kb + 2 < kb1;                         // this group's next block: its steps are requested one block early
-                if (loaded) ahead = load_steps(kb + 2);
-                ok = (first || mbar_wait(smem_u32(&bars->empty[mine.slot]), mine.parity, abort_flag, p.timeout_word, TO_UNPACK)) &&
-                     mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_UNPACK);
-                first = false;
-                mine = ring;
-                ok = __all_sync(0xFFFFFFFFu, ok);
+                loaded = kb + (int)nS < kb1;                   // this group's next block: its steps are requested one block early
+                if (loaded) ahead = load_steps(kb + (int)nS);
+                ok = warp_wait(&bars->full[ring.slot], ring.parity, TO_UNPACK);
                 if (!ok) break;
                 if (!is_x) {
-                    if (lane == 0) mbar_arrive(smem_u32(&bars->ready[conv.slot]));
+                    if (lane == 0) mbar_arrive(smem_u32(&bars->ready[ring.slot]));
                     continue;
                 }
                 const uint4* src = reinterpret_cast<const uint4*>(smem + (size_t)ring.slot * stage_bytes + row * CH);
@@ -293,7 +286,7 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) raw[j] = src[j ^ (row & 7)];
                 tc_fence_after();
-                const uint32_t dst = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 256 + conv.slot * 64;
+                const uint32_t dst = tmem + ((uint32_t)((warp & 3) * 32) << 16) + 256 + ring.slot * 64;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {                  // 32 channels: 16 tensor-memory columns of two bf16 each
                     const uint32_t s2 = step_bf16x2((step >> ((q * 32 / p.group) * 8)) & 0xFFu);
@@ -312,7 +305,7 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
                 tc_fence_before();
                 fence_proxy_async_smem();                      // the raw codes were read through the generic proxy; TMA refills them
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bars->ready[conv.slot]));
+                if (lane == 0) mbar_arrive(smem_u32(&bars->ready[ring.slot]));
             }
         }
     } else {
@@ -328,34 +321,34 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
             tc_fence_after();
             const int64_t t = tile * 128 + row;
             const int64_t kind = is_x ? 0 : 1;
-            for (int c0 = 0; c0 < p.nr; c0 += 32) {
-                uint32_t v[32];
-                tmem_ld_x32(tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 128 + c0, v);
+            for (int c0 = 0; c0 < p.nr; c0 += 16) {
+                uint32_t v[16];
+                tmem_ld_x16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 128 + c0, v);
                 tmem_wait_ld();
                 if (kb1 == kb0) {                              // a slice beyond the last channel block
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = 0u;
+                    for (int j = 0; j < 16; ++j) v[j] = 0u;
                 }
                 if (t >= p.T) continue;
                 if (p.slices == 1) {
-                    float x[32];
+                    float x[16];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(v[j]) * p.scaling;
+                    for (int j = 0; j < 16; ++j) x[j] = __uint_as_float(v[j]) * p.scaling;
                     __nv_bfloat16* dst = p.fac + (kind * p.boxes * p.T + t) * 64;
                     for (int q = 0; q < p.parts; ++q)
 #pragma unroll
-                        for (int j = 0; j < 32; j += 8) {
+                        for (int j = 0; j < 16; j += 8) {
                             uint32_t w[4];
 #pragma unroll
                             for (int k = 0; k < 4; ++k) w[k] = split_term(x[j + 2 * k], x[j + 2 * k + 1]);
                             const int c = q * p.term + c0 + j;
-                            if (c0 + j < p.nr) *reinterpret_cast<uint4*>(dst + (int64_t)(c / 64) * p.T * 64 + c % 64) = make_uint4(w[0], w[1], w[2], w[3]);
+                            *reinterpret_cast<uint4*>(dst + (int64_t)(c / 64) * p.T * 64 + c % 64) = make_uint4(w[0], w[1], w[2], w[3]);
                         }
                 } else {
                     float* dst = p.part + ((kind * p.slices + slice) * p.T + t) * p.n64 + c0;
 #pragma unroll
-                    for (int j = 0; j < 32; j += 4)
-                        if (c0 + j < p.nr) *reinterpret_cast<uint4*>(dst + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                    for (int j = 0; j < 16; j += 4)
+                        *reinterpret_cast<uint4*>(dst + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
                 }
             }
             tc_fence_before();
@@ -401,18 +394,18 @@ template <typename OutT> __device__ __forceinline__ OutT to_out(float v);
 template <> __device__ __forceinline__ float to_out<float>(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// One thread's 32 accumulator columns [c0, c0 + 32) of channel ch -> dA (column j of the row-major [rank, width]) or dB (row ch).
+// One thread's 16 accumulator columns [c0, c0 + 16) of channel ch -> dA (column j of the row-major [rank, width]) or dB (row ch).
 template <typename OutT>
-__device__ __forceinline__ void store_columns(OutT* dst, bool is_x, int64_t ch, int64_t width, int c0, int rank, const uint32_t (&v)[32], bool zero)
+__device__ __forceinline__ void store_columns(OutT* dst, bool is_x, int64_t ch, int64_t width, int c0, int rank, const uint32_t (&v)[16], bool zero)
 {
     if (is_x) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
+        for (int j = 0; j < 16; ++j)
             if (c0 + j < rank) dst[(int64_t)(c0 + j) * width + ch] = to_out<OutT>(zero ? 0.0f : __uint_as_float(v[j]));
     } else {
         OutT* row = dst + ch * rank + c0;                      // 16-byte aligned: rank is a multiple of 8
 #pragma unroll
-        for (int j = 0; j < 32; j += 8) {
+        for (int j = 0; j < 16; j += 8) {
             if (c0 + j >= rank) break;
             __align__(16) OutT o[8];
 #pragma unroll
@@ -541,14 +534,12 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
             if (elect_one()) mma_commit(smem_u32(&bars->drain));
             mbar_wait_quiet(smem_u32(&bars->drain), 0u);
         }
-    } else if (warp < 10) {
-        // Converters: two groups of four warps take alternate blocks (every block passes through them, dY untouched but for the last,
+    } else if (warp < 18) {
+        // Converters: a group of four warps to each stage (as above: every block passes through them, dY untouched but for the last,
         // partly filled block of a piece). A thread owns one token and 128 channels; the step bytes of its next block are requested
-        // before it works on the present one. The number of stages is even, so that a stage always belongs to the same group: the
-        // phase of its barrier that the group waits for is the one behind the phase it saw last. A group may run ahead of the products by
-        // as many stages as there are, so each stage has its own barrier for what the group is done with.
+        // before it works on the present one.
         const int tid = (threadIdx.x - 64) & 127, tok = tid & 63, box = tid >> 6;
-        const uint32_t grp = warp >= 6 ? 1u : 0u;
+        const uint32_t grp = (uint32_t)(warp - 2) >> 2;
         const int groups = (p.in + p.group - 1) / p.group, per = 128 / p.group;
         struct Cursor { uint32_t item; LoraChunk c; bool is_x; int ch0, t; Ring ring; } cur;
         // The next block of this group, at or behind the cursor's place.
@@ -562,7 +553,7 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
                     q.t = 0;
                     continue;
                 }
-                if ((q.ring.slot & 1u) == grp) return;
+                if (q.ring.slot == grp) return;
                 q.t += TOK; q.ring.next(nS);
             }
         };
@@ -572,7 +563,7 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
             return (q.item < items && q.is_x && q.t + tok < q.c.len)
                        ? load_step_bytes(p.scales + (q.c.t0 + q.t + tok) * p.ld_scales + g0, min(per, groups - g0), p.steps_whole != 0) : 0u;
         };
-        cur.item = blockIdx.x; cur.t = 0;
+        cur.item = grp < nS ? blockIdx.x : items; cur.t = 0;
         cur.c = chunk_of(cur.item);
         place_of(cur.item, cur.is_x, cur.ch0);
         seek(cur);
@@ -651,19 +642,19 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
             for (int m = 0; m < 2; ++m) {
                 if (ch0 + m * 128 >= width) break;
                 const int64_t ch = ch0 + m * 128 + row;
-                for (int c0 = 0; c0 < p.rank; c0 += 32) {
-                    uint32_t v[32];
+                for (int c0 = 0; c0 < p.rank; c0 += 16) {
+                    uint32_t v[16];
                     const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 256 + m * 128 + c0;
-                    tmem_ld_x32(taddr, v);
+                    tmem_ld_x16(taddr, v);
                     tmem_wait_ld();
                     if (WIDE) {
 #pragma unroll
                         for (int q = 1; q < PARTS; ++q) {
-                            uint32_t low[32];
-                            tmem_ld_x32(taddr + q * p.nr, low);
+                            uint32_t low[16];
+                            tmem_ld_x16(taddr + q * p.nr, low);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(low[j]));
+                            for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(low[j]));
                         }
                     }
                     if (ch < width) {
@@ -802,7 +793,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
         f.y_whole = y_whole; f.steps_whole = steps_whole;
         f.timeout_word = timeout_word;
         const size_t stage = BIG + (size_t)pl.n64 * 256;
-        f.stages = (int32_t)(budget / stage < MAX_STAGES ? budget / stage : MAX_STAGES);
+        f.stages = (int32_t)(budget / stage < MAX_STAGES ? budget / stage : MAX_STAGES) & ~1;
         const size_t smem = 1024 + f.stages * stage + sizeof(Bars);
         const int64_t grid = f.items < sm_count() ? f.items : sm_count();
         { ProfileScope ps("lora_factors", st);

@@ -359,6 +359,17 @@ __device__ __forceinline__ void tmem_ld_x32(uint32_t taddr, uint32_t (&v)[32])
         : "memory");
 }
 
+// 32 lanes x 16 consecutive 32-bit columns (whole warp).
+__device__ __forceinline__ void tmem_ld_x16(uint32_t taddr, uint32_t (&v)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr)
+        : "memory");
+}
+
 // ---- MMA ---------------------------------------------------------------------------------------
 // Instruction descriptor of tcgen05.mma kind::f16 / kind::i8: D format bits [4,6) (1 = F32, 2 = S32),
 // A format bits [7,10), B format bits [10,13) (f16 kinds: 0 = F16, 1 = BF16; i8: 0 = U8, 1 = S8),
