@@ -16,11 +16,11 @@
 //   PROBS   h W^T        epilogue: exp(l - r) or w (p - [v = y]) as bf16 into one piece of the vocabulary    (gradients)
 //   GRAD_H  piece * W    epilogue: fp32, added to what the earlier pieces left
 //   GRAD_W  piece^T * h  epilogue: bf16 rows of dW
-// Gradient of the hidden states alone: two products instead of three. The reference r of a row is its maximum over the first 256
-// columns, known after one small launch; any reference gives the same softmax, and with fp32 and bf16 exponents one that lies up
-// to LIMIT = 64 powers of two below a row's true maximum is as good as the maximum itself. Should a row exceed that, a flag sends the
-// rest through a second pass whose reference is the true maximum: its launches are always enqueued and return at once when the
-// flag is not set (the host does not wait to find out).
+// Gradient of the hidden states alone: two products instead of three. The reference r of a row is its label's logit, a dot product
+// taken when the row is gathered. Any reference gives the same softmax, and with the exponents of fp32 and bf16 one that lies up to
+// LIMIT = 64 powers of two (a loss of 44) below the row's maximum is as good as the maximum itself. Should a row exceed that, a flag
+// sends the rest through a second pass whose reference is the true maximum: its launches are always enqueued and return at once
+// when the flag is not set (the host does not wait to find out).
 // With dW the normaliser has to be known before the piece is written: STATS first, then PROBS, GRAD_H and GRAD_W per piece.
 #include "qless_kernels.h"
 #include "tc_common.cuh"
@@ -58,12 +58,12 @@ struct GemmParams {
     float2* stat;                           // STATS: [2 * tiles][tpad] (maximum, sum)
     float* psum;                            // PROBS: [2 * tiles][tpad] sums, or NULL
     int32_t tile0;                          // tile index of the launch's first column tile in stat / psum
-    float* label_logit;                     // [tpad], in powers of two
     __nv_bfloat16* out;                     // PROBS: piece [tpad][ld_out]; GRAD_W: rows of dW
     int64_t ld_out;
     float* acc;                             // GRAD_H: [splits][row tiles * 256][cols]
     int32_t accumulate;
     int32_t* redo;                          // PROBS: set where a row lies more than LIMIT above its reference
+    int32_t a_whole, b_whole;               // operand rows are whole 128-byte blocks: one copy brings two side by side
     unsigned int* timeout_word;
 };
 
@@ -138,8 +138,14 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;                   // accumulators at columns 0 and 256
 
+    // A wait of a whole warp: the same answer in every lane.
+    auto warp_wait = [&](uint64_t* bar, uint32_t parity, uint32_t code) -> bool {
+        const bool w = mbar_wait_cluster(smem_u32(bar), parity, abort_flag, p.timeout_word, code);
+        return __all_sync(0xFFFFFFFFu, w);
+    };
+
     if (warp == 0) {
-        if (lane == 0) {
+        {
             uint32_t it = 0;
             Ring ring;
             bool ok = true;
@@ -148,18 +154,19 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                 item_of(item, split, m, n, kb0, kb1);
                 const int a0 = m * 256 + (int)rank * 128, b0 = n * 256 + (int)rank * 128 + (B_MN ? 0 : p.col0);
                 for (int kb = kb0; kb < kb1; ++kb, ++it, ring.next(STAGES)) {
-                    if (!mbar_wait_cluster(smem_u32(&bars->empty[ring.slot]), ring.parity ^ 1u, abort_flag, p.timeout_word, TO_PRODUCER)) { ok = false; break; }
+                    if (!warp_wait(&bars->empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
                     const uint32_t full = map_to_cta(smem_u32(&bars->full[ring.slot]), 0);
-                    if (rank == 0) mbar_arrive_expect_tx(smem_u32(&bars->full[ring.slot]), 4 * HALF);      // both CTAs' bytes
                     const uint32_t a = smem_u32(smem + (size_t)ring.slot * 2 * HALF), b = a + HALF;
                     const int k0 = kb * KB, kw = k0 + (MODE == GRAD_H ? p.col0 : 0);
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        if (A_MN) tma_load_2d_pair(a + j * 16384, &tm_a, full, a0 + 64 * j, k0);
-                        else tma_load_2d_pair(a + j * 16384, &tm_a, full, k0 + 64 * j, a0);
-                        if (B_MN) tma_load_2d_pair(b + j * 16384, &tm_b, full, b0 + 64 * j, kw);
-                        else tma_load_2d_pair(b + j * 16384, &tm_b, full, k0 + 64 * j, b0);
+                    const int ac = A_MN ? a0 : k0, ar = A_MN ? k0 : a0, bc = B_MN ? b0 : k0, br = B_MN ? kw : b0;      // first column and row
+                    if (elect_one()) {
+                        if (rank == 0) mbar_arrive_expect_tx(smem_u32(&bars->full[ring.slot]), 4 * HALF);      // both CTAs' bytes
+                        if (p.a_whole) tma_load_3d_pair(a, &tm_a, full, 0, ar, ac / 64);
+                        else for (int j = 0; j < 2; ++j) tma_load_2d_pair(a + j * 16384, &tm_a, full, ac + 64 * j, ar);
+                        if (p.b_whole) tma_load_3d_pair(b, &tm_b, full, 0, br, bc / 64);
+                        else for (int j = 0; j < 2; ++j) tma_load_2d_pair(b + j * 16384, &tm_b, full, bc + 64 * j, br);
                     }
+                    __syncwarp();
                 }
             }
             if (!ok) {       // leave no copy in flight: the leader waits (bounded) for the stages that are armed, the peer idles
@@ -172,7 +179,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
             }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             const uint32_t idesc = make_idesc(1, 1, 1, 256, 256) | (A_MN ? IDESC_A_MN : 0u) | (B_MN ? IDESC_B_MN : 0u);
             Ring ring;
             uint32_t n_acc = 0;
@@ -181,11 +188,12 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                 int split, m, n, kb0, kb1;
                 item_of(item, split, m, n, kb0, kb1);
                 const uint32_t buf = n_acc & 1u, d = tmem + buf * 256;
-                if (!mbar_wait_cluster(smem_u32(&bars->d_empty[buf]), ((n_acc >> 1) & 1u) ^ 1u, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                if (!warp_wait(&bars->d_empty[buf], ((n_acc >> 1) & 1u) ^ 1u, TO_MMA)) { ok = false; break; }
                 tc_fence_after();
                 for (int kb = kb0; kb < kb1; ++kb, ring.next(STAGES)) {
-                    if (!mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_MMA)) { ok = false; break; }
+                    if (!warp_wait(&bars->full[ring.slot], ring.parity, TO_MMA)) { ok = false; break; }
                     tc_fence_after();
+                    if (elect_one()) {
                     const uint32_t a = smem_u32(smem + (size_t)ring.slot * 2 * HALF), b = a + HALF;
                     // made once per stage, advanced by constants (units of 16 bytes)
                     const uint64_t a0 = A_MN ? make_smem_desc_mn_sw128(a, 16384) : make_smem_desc_sw128(a);
@@ -195,10 +203,13 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                     for (int k = 1; k < KB / 16; ++k)
                         mma_f16_ss_pair(d, a0 + (uint64_t)(A_MN ? k * 128 : (k >> 2) * 1024 + (k & 3) * 2), b0 + (uint64_t)(B_MN ? k * 128 : (k >> 2) * 1024 + (k & 3) * 2), idesc, 1u);
                     mma_commit_pair(smem_u32(&bars->empty[ring.slot]));
+                    }
+                    __syncwarp();
                 }
-                if (ok) mma_commit_pair(smem_u32(&bars->d_full[buf]));
+                if (ok && elect_one()) mma_commit_pair(smem_u32(&bars->d_full[buf]));
+                __syncwarp();
             }
-            mma_commit_pair(smem_u32(&bars->drain));           // every MMA issued above completes before tensor memory is freed
+            if (elect_one()) mma_commit_pair(smem_u32(&bars->drain));           // every MMA issued above completes before tensor memory is freed
             mbar_wait_quiet(smem_u32(&bars->drain), 0u);
         }
     } else {
@@ -242,10 +253,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                     if (__any_sync(0xFFFFFFFFu, mine)) {
 #pragma unroll
                         for (int k = 0; k < 32; ++k)
-                            if (mine && k == lk) {
-                                p.label_logit[row] = __uint_as_float(v[k]) * LOG2E;
-                                v[k] = 0xFF800000u;              // -infinity: no part of the sum over the others
-                            }
+                            if (mine && k == lk) v[k] = 0xFF800000u;      // -infinity: no part of the sum over the others
                     }
                     if (have < 32) {
 #pragma unroll
@@ -335,46 +343,111 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
 
 // ---- tokens that carry a loss ------------------------------------------------------------------------------------------
 
-// One block: place[t] = position of token t among the tokens with a label in [0, V), or -1; order = the inverse. Also how many
-// slices the hidden-state product is cut into along the vocabulary: as many as keep the CTA pairs busy (at least 95 %, four slices
-// at most where there are tiles enough, or as many as fill one round where there are few), within the `cap_tiles` row tiles the
-// workspace has room for.
-__global__ void __launch_bounds__(1024) loss_compact_kernel(const int64_t* __restrict__ labels, int64_t T, int32_t V, const float* __restrict__ weight,
-                                                            int32_t* __restrict__ order, int32_t* __restrict__ place, int32_t* __restrict__ out_labels,
-                                                            float* __restrict__ out_weight, float* __restrict__ loss, LossMeta* meta,
-                                                            int32_t pairs, int32_t col_tiles, int32_t cap_tiles)
+// place[t] = position of token t among the tokens with a label in [0, V), or -1; order = the inverse. Every block scans all labels (they
+// are few against the rows) and lists the tokens whose rows fall to it; then its warps copy a row each and take the dot product with the
+// label's row of W on the way. Rows land in `out` in order, zeros behind the last up to a multiple of 128 (GRAD_W contracts over the rows).
+// Also how many slices the hidden-state product is cut into along the vocabulary: as many as keep the CTA pairs busy (at least 95 %,
+// four slices at most where there are tiles enough, or as many as fill one round where there are few), within the `cap_tiles` row
+// tiles the workspace has room for.
+struct GatherArgs {
+    const int64_t* labels;
+    const float* token_weight;
+    const __nv_bfloat16* hidden;
+    const __nv_bfloat16* weight;
+    int64_t T, ld_hidden, ld_weight;
+    int32_t V, width, pairs, col_tiles, cap_tiles;
+    int32_t* order; int32_t* place; int32_t* out_labels;
+    float* out_weight; float* label_logit; float* loss;
+    RowParam* rowp;
+    __nv_bfloat16* out;
+    LossMeta* meta;
+};
+
+constexpr int LIST = 512;
+
+__global__ void __launch_bounds__(1024) loss_gather_kernel(const GatherArgs a)
 {
-    __shared__ int32_t warp_sum[32];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int32_t base = 0;
-    for (int64_t t0 = 0; t0 < T; t0 += 1024) {
-        const int64_t t = t0 + threadIdx.x;
-        const int64_t y = t < T ? labels[t] : -1;
-        const bool keep = y >= 0 && y < V;
-        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, keep);
-        if (lane == 0) warp_sum[warp] = __popc(mask);
+    __shared__ int32_t warp_sum[2][32];
+    __shared__ int2 list[LIST];                                  // token, place
+    __shared__ int32_t list_label[LIST];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, vecs = a.width / 8;
+    const int32_t grid = (int32_t)gridDim.x, me = (int32_t)blockIdx.x;
+    int32_t base = 0, listed = 0;                                // tokens kept so far, and how many of them fell to this block since the last flush
+    auto flush = [&]() {                                         // whole block
         __syncthreads();
-        int32_t before = base, all = 0;
-        for (int w = 0; w < 32; ++w) { const int32_t c = warp_sum[w]; before += w < warp ? c : 0; all += c; }
-        if (t < T) {
-            const int32_t at = before + __popc(mask & ((1u << lane) - 1u));
-            place[t] = keep ? at : -1;
-            if (keep) {
-                order[at] = (int32_t)t;
-                out_labels[at] = (int32_t)y;
-                out_weight[at] = weight != nullptr ? weight[t] : 1.0f;
-            } else {
-                loss[t] = 0.0f;
+        for (int i = warp; i < listed; i += 32) {
+            const int2 e = list[i];
+            const uint4* src = reinterpret_cast<const uint4*>(a.hidden + (int64_t)e.x * a.ld_hidden);
+            const uint4* wrow = reinterpret_cast<const uint4*>(a.weight + (int64_t)list_label[i] * a.ld_weight);
+            uint4* dst = reinterpret_cast<uint4*>(a.out + (int64_t)e.y * a.width);
+            float dot = 0.0f;
+#pragma unroll 4
+            for (int c = lane; c < vecs; c += 32) {
+                const uint4 x = __ldg(src + c), w = __ldg(wrow + c);
+                dst[c] = x;
+                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    dot = fmaf(__uint_as_float(xs[k] << 16), __uint_as_float(ws[k] << 16), dot);
+                    dot = fmaf(__uint_as_float(xs[k] & 0xFFFF0000u), __uint_as_float(ws[k] & 0xFFFF0000u), dot);
+                }
+            }
+#pragma unroll
+            for (int s = 16; s > 0; s >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, s);
+            if (lane == 0) {
+                const float l2 = dot * LOG2E;
+                a.label_logit[e.y] = l2;
+                a.rowp[e.y] = RowParam{l2, 1.0f, 0.0f, 0.0f};
             }
         }
-        base += all;
         __syncthreads();
+        listed = 0;
+    };
+    int64_t y_next = (int64_t)threadIdx.x < a.T ? a.labels[threadIdx.x] : -1;
+    for (int64_t t0 = 0; t0 < a.T; t0 += 1024) {
+        const int64_t t = t0 + threadIdx.x, y = y_next;
+        y_next = t + 1024 < a.T ? a.labels[t + 1024] : -1;
+        const bool keep = y >= 0 && y < a.V;
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, keep);
+        int32_t* sums = warp_sum[(t0 >> 10) & 1];                // two in turn: one barrier per step
+        if (lane == 0) sums[warp] = __popc(mask);
+        __syncthreads();
+        const int32_t mine = sums[lane];
+        int32_t upto = mine;                                     // sums over the warps up to and with warp `lane`
+#pragma unroll
+        for (int s = 1; s < 32; s <<= 1) { const int32_t v = __shfl_up_sync(0xFFFFFFFFu, upto, s); if (lane >= s) upto += v; }
+        const int32_t all = __shfl_sync(0xFFFFFFFFu, upto, 31);
+        const int32_t at = base + __shfl_sync(0xFFFFFFFFu, upto - mine, warp) + __popc(mask & ((1u << lane) - 1u));
+        if (me == 0 && t < a.T) {
+            a.place[t] = keep ? at : -1;
+            if (keep) {
+                a.order[at] = (int32_t)t;
+                a.out_labels[at] = (int32_t)y;
+                a.out_weight[at] = a.token_weight != nullptr ? a.token_weight[t] : 1.0f;
+            } else {
+                a.loss[t] = 0.0f;
+            }
+        }
+        // places base .. base + all - 1: those that are `me` modulo the grid
+        const int32_t first = base + ((me - base % grid) + grid) % grid;
+        if (keep && at % grid == me) {
+            const int i = listed + (at - first) / grid;
+            list[i] = make_int2((int32_t)t, at);
+            list_label[i] = (int32_t)y;
+        }
+        base += all;
+        listed += first < base ? (base - 1 - first) / grid + 1 : 0;
+        if (listed + 1024 / grid + 1 > LIST) flush();          // room for another step
     }
-    if (threadIdx.x == 0) {
-        const int mt = (base + 255) / 256, tiles = mt * col_tiles;
+    flush();
+    const int64_t z0 = (int64_t)base * vecs, z1 = (int64_t)(base + 127) / 128 * 128 * vecs;
+    for (int64_t i = z0 + (int64_t)blockIdx.x * 1024 + threadIdx.x; i < z1; i += (int64_t)gridDim.x * 1024)
+        reinterpret_cast<uint4*>(a.out)[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        const int mt = (base + 255) / 256, tiles = mt * a.col_tiles;
         int best = 1;
         if (mt > 0) {
-            const int most = min(cap_tiles / mt, tiles >= pairs ? 4 : max(1, pairs / tiles));
+            const int pairs = a.pairs, most = min(a.cap_tiles / mt, tiles >= pairs ? 4 : max(1, pairs / tiles));
             if (tiles < pairs) best = max(1, most);
             else {
                 float best_use = 0.0f;
@@ -385,22 +458,7 @@ __global__ void __launch_bounds__(1024) loss_compact_kernel(const int64_t* __res
                 }
             }
         }
-        meta->count = base; meta->splits = best; meta->redo = 0;
-    }
-}
-
-// Rows of the tokens that carry a loss, in order; zeros behind the last up to a multiple of 128 (GRAD_W contracts over the rows).
-__global__ void loss_gather_kernel(const __nv_bfloat16* __restrict__ hidden, int64_t ld, int32_t width, const int32_t* __restrict__ order,
-                                   const LossMeta* __restrict__ meta, __nv_bfloat16* __restrict__ out)
-{
-    const int count = meta->count, vecs = width / 8;
-    const int64_t total = (int64_t)((count + 127) / 128 * 128) * vecs;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
-        const int64_t r = i / vecs;
-        const int c = (int)(i - r * vecs);
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (r < count) x = __ldg(reinterpret_cast<const uint4*>(hidden + (int64_t)order[r] * ld) + c);
-        reinterpret_cast<uint4*>(out + r * width)[c] = x;
+        a.meta->count = base; a.meta->splits = best; a.meta->redo = 0;
     }
 }
 
@@ -544,14 +602,18 @@ LossPlan plan_loss(int64_t T, int32_t width, int32_t vocab, bool want_h, bool wa
     pl.tpad = (T + 255) / 256 * 256;
     const int64_t mt = pl.tpad / 256, pairs = sm_count() / 2, nt_h = (width + 255) / 256;
     const int64_t tiles_v = ((int64_t)vocab + 255) / 256;
-    // Piece of the vocabulary whose probabilities are held at once: at most 256 MiB of bf16.
-    int64_t piece_tiles = ((int64_t)256 << 20) / (pl.tpad * 256 * 2);
+    // The normaliser first (one more product), or a reference that may have to be redone (a few more launches): with the gradient of the
+    // weights always the former; otherwise where that product takes less than the launches (about 12 us: 5.5 TB/s, 1.2 PFLOP/s).
+    const double product_us = 2.0 * vocab * width / 5.5e6, flop_us = 2.0 * pl.tpad * (double)vocab * width / 1.2e9;
+    pl.exact = !want_h || want_w || (product_us > flop_us ? product_us : flop_us) < 12.0;
+    // Piece of the vocabulary whose probabilities are held at once: at most 512 MiB of bf16.
+    int64_t piece_tiles = ((int64_t)512 << 20) / (pl.tpad * 256 * 2);
     if (piece_tiles < 1) piece_tiles = 1;
     if (piece_tiles > tiles_v) piece_tiles = tiles_v;
     pl.piece = (int32_t)(piece_tiles * 256);
     pl.entries = (int32_t)(2 * tiles_v);
     int64_t cap = pairs / nt_h < 16 ? pairs / nt_h : 16;       // slices where there is one row tile
-    if (cap < 2 * mt) cap = 2 * mt;
+    if (cap < 3 * mt) cap = 3 * mt;
     pl.cap_tiles = (int32_t)cap;
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t at = off; off += align_up(bytes, 256); return at; };
@@ -590,27 +652,34 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
     const int64_t mt = pl.tpad / 256, nt_h = (a.width + 255) / 256;
     const int32_t tiles_v = (a.vocab + 255) / 256;
 
-    { ProfileScope ps("loss_compact", st);
-      loss_compact_kernel<<<1, 1024, 0, st>>>(a.labels, a.T, a.vocab, a.token_weight, order, place, labels, weight, a.loss, meta,
-                                              sm_count() / 2, (int32_t)nt_h, pl.cap_tiles); }
-    QLESS_CUDA_TRY(cudaGetLastError());
     { ProfileScope ps("loss_gather", st);
-      loss_gather_kernel<<<grid_of(a.T * (a.width / 8), 256), 256, 0, st>>>(reinterpret_cast<const __nv_bfloat16*>(a.hidden), a.ld_hidden, a.width, order, meta, hidden); }
+      // a block lists at most LIST of the 1024 tokens of a step: at least four blocks
+      int64_t blocks = (a.T + 7) / 8 < sm_count() ? (a.T + 7) / 8 : sm_count();
+      if (blocks < 4) blocks = 4;
+      GatherArgs g{};
+      g.labels = a.labels; g.token_weight = a.token_weight; g.hidden = reinterpret_cast<const __nv_bfloat16*>(a.hidden);
+      g.weight = reinterpret_cast<const __nv_bfloat16*>(a.weight); g.T = a.T; g.ld_hidden = a.ld_hidden; g.ld_weight = a.ld_weight; g.V = a.vocab;
+      g.width = a.width; g.pairs = sm_count() / 2; g.col_tiles = (int32_t)nt_h; g.cap_tiles = pl.cap_tiles; g.order = order; g.place = place;
+      g.out_labels = labels; g.out_weight = weight; g.label_logit = logit; g.loss = a.loss; g.rowp = rowp; g.out = hidden; g.meta = meta;
+      loss_gather_kernel<<<(unsigned)blocks, 1024, 0, st>>>(g); }
     QLESS_CUDA_TRY(cudaGetLastError());
-    count_launches(2);
+    count_launches(1);
 
     CUtensorMap tm_x, tm_w, tm_p;
     qless_status s;
-    if ((s = make_tmap_2d_sw128(&tm_x, hidden, 2, a.width, pl.tpad, (uint64_t)a.width * 2, 64, 128)) != QLESS_OK) return s;
-    if ((s = make_tmap_2d_sw128(&tm_w, a.weight, 2, a.width, a.vocab, (uint64_t)a.ld_weight * 2, 64, 128)) != QLESS_OK) return s;
+    const bool whole = a.width % 64 == 0;
+    if ((s = whole ? make_tmap_blocks_sw128(&tm_x, hidden, 2, a.width / 64, pl.tpad, (uint64_t)a.width * 2, 128, 128, 2)
+                   : make_tmap_2d_sw128(&tm_x, hidden, 2, a.width, pl.tpad, (uint64_t)a.width * 2, 64, 128)) != QLESS_OK) return s;
+    if ((s = whole ? make_tmap_blocks_sw128(&tm_w, a.weight, 2, a.width / 64, a.vocab, (uint64_t)a.ld_weight * 2, 128, 128, 2)
+                   : make_tmap_2d_sw128(&tm_w, a.weight, 2, a.width, a.vocab, (uint64_t)a.ld_weight * 2, 64, 128)) != QLESS_OK) return s;
     if (want_h || want_w)
-        if ((s = make_tmap_2d_sw128(&tm_p, piece, 2, pl.piece, pl.tpad, (uint64_t)pl.piece * 2, 64, 128)) != QLESS_OK) return s;
+        if ((s = make_tmap_blocks_sw128(&tm_p, piece, 2, pl.piece / 64, pl.tpad, (uint64_t)pl.piece * 2, 128, 128, 2)) != QLESS_OK) return s;
 
     GemmParams base{};
-    base.meta = meta; base.tpad = pl.tpad; base.labels = labels; base.rowp = rowp; base.label_logit = logit; base.timeout_word = timeout_word;
+    base.meta = meta; base.tpad = pl.tpad; base.labels = labels; base.rowp = rowp; base.timeout_word = timeout_word;
     auto stats = [&](int32_t cols, const int32_t* gate) {
         GemmParams p = base;
-        p.gate = gate; p.cols = cols; p.k = a.width; p.stat = stat;
+        p.gate = gate; p.cols = cols; p.k = a.width; p.stat = stat; p.a_whole = p.b_whole = whole;
         return launch_gemm<STATS>("loss_stats", tm_x, tm_w, p, mt * ((cols + 255) / 256), st);
     };
     auto rows = [&](int kind, int32_t entries, const int32_t* gate) {
@@ -628,18 +697,18 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
             const int32_t cols = a.vocab - v0 < pl.piece ? a.vocab - v0 : pl.piece;
             GemmParams p = base;
             p.gate = gate; p.cols = cols; p.col0 = v0; p.k = a.width; p.out = piece; p.ld_out = pl.piece; p.tile0 = v0 / 256;
-            p.psum = keep_sums ? psum : nullptr; p.redo = &meta->redo;
+            p.psum = keep_sums ? psum : nullptr; p.redo = &meta->redo; p.a_whole = p.b_whole = whole;
             qless_status e = launch_gemm<PROBS>("loss_probs", tm_x, tm_w, p, mt * ((cols + 255) / 256), st);
             if (e != QLESS_OK) return e;
             if (want_h) {
                 GemmParams g = base;
-                g.gate = gate; g.cols = a.width; g.col0 = v0; g.k = cols; g.acc = acc; g.accumulate = v0 > 0;
+                g.gate = gate; g.cols = a.width; g.col0 = v0; g.k = cols; g.acc = acc; g.accumulate = v0 > 0; g.a_whole = 1; g.b_whole = whole;
                 e = launch_gemm<GRAD_H>("loss_grad_hidden", tm_p, tm_w, g, pl.cap_tiles * nt_h, st);
                 if (e != QLESS_OK) return e;
             }
             if (want_w) {
                 GemmParams g = base;
-                g.gate = gate; g.cols = a.width; g.rows = cols; g.col0 = v0; g.out = reinterpret_cast<__nv_bfloat16*>(a.grad_weight); g.ld_out = a.ld_grad_weight;
+                g.gate = gate; g.cols = a.width; g.rows = cols; g.col0 = v0; g.out = reinterpret_cast<__nv_bfloat16*>(a.grad_weight); g.ld_out = a.ld_grad_weight; g.a_whole = 1; g.b_whole = whole;
                 e = launch_gemm<GRAD_W>("loss_grad_weight", tm_p, tm_x, g, (int64_t)((cols + 255) / 256) * nt_h, st);
                 if (e != QLESS_OK) return e;
             }
@@ -647,25 +716,20 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
         return QLESS_OK;
     };
 
-    if (want_w || !want_h) {
+    if (pl.exact) {
         if ((s = stats(a.vocab, nullptr)) != QLESS_OK) return s;
         if ((s = rows(ROW_FROM_STATS, pl.entries, nullptr)) != QLESS_OK) return s;
-        if (want_w && (s = pieces(false, nullptr)) != QLESS_OK) return s;
+        if ((want_h || want_w) && (s = pieces(false, nullptr)) != QLESS_OK) return s;
     } else {
-        const int32_t first = a.vocab < 256 ? a.vocab : 256;
-        if ((s = stats(first, nullptr)) != QLESS_OK) return s;
-        if ((s = rows(ROW_REFERENCE, 2, nullptr)) != QLESS_OK) return s;
         if ((s = pieces(true, nullptr)) != QLESS_OK) return s;
-        if (tiles_v > 1) {                                      // a reference from 256 columns may be too low; one from all of them is not
-            if ((s = stats(a.vocab, &meta->redo)) != QLESS_OK) return s;
-            if ((s = rows(ROW_REFERENCE, pl.entries, &meta->redo)) != QLESS_OK) return s;
-            if ((s = pieces(true, &meta->redo)) != QLESS_OK) return s;
-        }
+        if ((s = stats(a.vocab, &meta->redo)) != QLESS_OK) return s;
+        if ((s = rows(ROW_REFERENCE, pl.entries, &meta->redo)) != QLESS_OK) return s;
+        if ((s = pieces(true, &meta->redo)) != QLESS_OK) return s;
         if ((s = rows(ROW_FROM_SUMS, pl.entries, nullptr)) != QLESS_OK) return s;
     }
     if (want_h) {
         { ProfileScope ps("loss_finish", st);
-          loss_finish_kernel<<<grid_of(a.T * (a.width / 8), 256), 256, 0, st>>>(acc, a.width, meta, place, labels, coef, want_w ? 0 : 1,
+          loss_finish_kernel<<<grid_of(a.T * (a.width / 8), 256), 256, 0, st>>>(acc, a.width, meta, place, labels, coef, pl.exact ? 0 : 1,
                                                                                reinterpret_cast<const __nv_bfloat16*>(a.weight), a.ld_weight, a.T,
                                                                                reinterpret_cast<__nv_bfloat16*>(a.grad_hidden), a.ld_grad_hidden); }
         count_launches(1);

@@ -82,10 +82,42 @@ def test_loss_and_gradients(T, width, vocab, keep, wants):
         assert got[k] is None or torch.equal(got[k], again[k])
 
 
+@pytest.mark.parametrize("T,width,vocab,keep", [(5, 2048, 40_000, 1.0), (300, 1024, 40_001, 0.8), (1300, 1024, 9000, 0.9)])
+def test_gradient_of_the_hidden_states_in_two_products(T, width, vocab, keep):
+    # large enough that the normaliser is not computed first
+    case = _case(T, width, vocab, 31, keep, spread=0.02)
+    got = B.qless_lm_loss(*case)
+    B.qless_check()
+    check(got, reference(*case), T, vocab)
+    again = B.qless_lm_loss(*case)
+    assert torch.equal(got["loss"], again["loss"]) and torch.equal(got["grad_hidden"], again["grad_hidden"])
+
+
+def test_two_products_with_a_row_far_above_its_reference():
+    # row 7's largest logit lies more than 64 powers of two above its label's: the pass has to be redone from the true maximum; row 9's
+    # label lies as far above everything else, and row 11 holds an infinity
+    T, width, vocab = 40, 1024, 40_000
+    hidden, weight, labels, tw = _case(T, width, vocab, 37, spread=0.02)
+    weight = weight.clone()
+    weight[39_000] = hidden[7] * 0.0625
+    weight[25_000] = hidden[9] * 0.0625
+    labels[7], labels[9] = 3, 25_000
+    assert float((hidden[7].double() @ weight[39_000].double()) - (hidden[7].double() @ weight[3].double())) > 64 * 0.6932
+    got = B.qless_lm_loss(hidden, weight, labels, tw)
+    B.qless_check()
+    check(got, reference(hidden, weight, labels, tw), T, vocab)
+    bad = hidden.clone()
+    bad[11, 0] = float("inf")
+    dirty = B.qless_lm_loss(bad, weight, labels, tw)
+    keep = torch.arange(T, device=DEV) != 11
+    assert torch.equal(dirty["loss"][keep], got["loss"][keep]) and torch.equal(dirty["grad_hidden"][keep], got["grad_hidden"][keep])
+    assert not torch.isfinite(dirty["loss"][11])
+
+
 def test_several_pieces_of_the_vocabulary():
-    # 70 000 tokens' capacity (almost all without a loss): a piece holds 7 column tiles, so 5000 columns take three
-    T, width, vocab = 70_000, 64, 5000
-    hidden, weight, labels, tw = _case(T, width, vocab, 7, 0.01)
+    # 140 000 tokens' capacity (almost all without a loss): a piece holds 7 column tiles, so 5000 columns take three
+    T, width, vocab = 140_000, 64, 5000
+    hidden, weight, labels, tw = _case(T, width, vocab, 7, 0.005)
     for wants in ((True, False), (True, True)):
         got = B.qless_lm_loss(hidden, weight, labels, tw, want_hidden=wants[0], want_weight=wants[1])
         B.qless_check()
