@@ -107,6 +107,8 @@ __global__ void __launch_bounds__(THREADS) activation_quantize_kernel(const T* _
     constexpr int LANES = GROUP / LANE_CH;                              // neighbouring lanes that share a step
     const int lane = threadIdx.x & 31;
     const int64_t quads = (p.tokens + UNROLL - 1) / UNROLL;
+    ahead_release();
+    ahead_wait();
     for (Walk u(p); u.quad < quads; u.next(p)) {
         const int c = u.seg * SEG + lane * LANE_CH;
         const int have = min(LANE_CH, p.width - c);                     // channels of this lane (<= 0: none)
@@ -170,6 +172,8 @@ __global__ void __launch_bounds__(THREADS) activation_dequantize_kernel(const in
 {
     const int lane = threadIdx.x & 31;
     const int64_t quads = (p.tokens + UNROLL - 1) / UNROLL;
+    ahead_release();
+    ahead_wait();
     for (Walk u(p); u.quad < quads; u.next(p)) {
         const int c = u.seg * SEG + lane * LANE_CH;
         const int have = min(LANE_CH, p.width - c);
@@ -233,22 +237,26 @@ bool vectors_fit(const void* x, int64_t ld_x, size_t esize, const void* codes, i
 }
 
 template <typename T, bool VEC>
-void quantize_group(const void* x, int8_t* codes, uint8_t* scales, const ActParams& p, cudaStream_t st)
+cudaError_t quantize_group(const void* x, int8_t* codes, uint8_t* scales, const ActParams& p, cudaStream_t st)
 {
     const T* src = reinterpret_cast<const T*>(x);
     const unsigned grid = grid_for(p);
-    if (p.group == 32) activation_quantize_kernel<T, VEC, 32><<<grid, THREADS, 0, st>>>(src, codes, scales, p);
-    else if (p.group == 64) activation_quantize_kernel<T, VEC, 64><<<grid, THREADS, 0, st>>>(src, codes, scales, p);
-    else activation_quantize_kernel<T, VEC, 128><<<grid, THREADS, 0, st>>>(src, codes, scales, p);
+    cudaError_t e;
+    if (p.group == 32) e = launch_ahead(activation_quantize_kernel<T, VEC, 32>, dim3(grid), dim3(THREADS), 0, st, src, codes, scales, p);
+    else if (p.group == 64) e = launch_ahead(activation_quantize_kernel<T, VEC, 64>, dim3(grid), dim3(THREADS), 0, st, src, codes, scales, p);
+    else e = launch_ahead(activation_quantize_kernel<T, VEC, 128>, dim3(grid), dim3(THREADS), 0, st, src, codes, scales, p);
+    return e;
 }
 template <typename T, bool VEC>
-void dequantize_group(const int8_t* codes, const uint8_t* scales, void* out, const ActParams& p, cudaStream_t st)
+cudaError_t dequantize_group(const int8_t* codes, const uint8_t* scales, void* out, const ActParams& p, cudaStream_t st)
 {
     T* dst = reinterpret_cast<T*>(out);
     const unsigned grid = grid_for(p);
-    if (p.group == 32) activation_dequantize_kernel<T, VEC, 32><<<grid, THREADS, 0, st>>>(codes, scales, dst, p);
-    else if (p.group == 64) activation_dequantize_kernel<T, VEC, 64><<<grid, THREADS, 0, st>>>(codes, scales, dst, p);
-    else activation_dequantize_kernel<T, VEC, 128><<<grid, THREADS, 0, st>>>(codes, scales, dst, p);
+    cudaError_t e;
+    if (p.group == 32) e = launch_ahead(activation_dequantize_kernel<T, VEC, 32>, dim3(grid), dim3(THREADS), 0, st, codes, scales, dst, p);
+    else if (p.group == 64) e = launch_ahead(activation_dequantize_kernel<T, VEC, 64>, dim3(grid), dim3(THREADS), 0, st, codes, scales, dst, p);
+    else e = launch_ahead(activation_dequantize_kernel<T, VEC, 128>, dim3(grid), dim3(THREADS), 0, st, codes, scales, dst, p);
+    return e;
 }
 
 }  // namespace
@@ -258,10 +266,9 @@ cudaError_t launch_activation_quantize(const void* x, qless_dtype dtype, int64_t
 {
     const ActParams p = make_params(tokens, width, group, ld_x, ld_codes, ld_scales);
     const bool vec = vectors_fit(x, ld_x, dtype == QLESS_F32 ? 4 : 2, codes, ld_codes);
-    if (dtype == QLESS_F32) { if (vec) quantize_group<float, true>(x, codes, scales, p, st); else quantize_group<float, false>(x, codes, scales, p, st); }
-    else { if (vec) quantize_group<__nv_bfloat16, true>(x, codes, scales, p, st); else quantize_group<__nv_bfloat16, false>(x, codes, scales, p, st); }
     count_launches(1);
-    return cudaGetLastError();
+    if (dtype == QLESS_F32) return vec ? quantize_group<float, true>(x, codes, scales, p, st) : quantize_group<float, false>(x, codes, scales, p, st);
+    return vec ? quantize_group<__nv_bfloat16, true>(x, codes, scales, p, st) : quantize_group<__nv_bfloat16, false>(x, codes, scales, p, st);
 }
 
 cudaError_t launch_activation_dequantize(const int8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales, int64_t tokens,
@@ -269,10 +276,9 @@ cudaError_t launch_activation_dequantize(const int8_t* codes, int64_t ld_codes, 
 {
     const ActParams p = make_params(tokens, width, group, ld_out, ld_codes, ld_scales);
     const bool vec = vectors_fit(out, ld_out, dtype == QLESS_F32 ? 4 : 2, codes, ld_codes);
-    if (dtype == QLESS_F32) { if (vec) dequantize_group<float, true>(codes, scales, out, p, st); else dequantize_group<float, false>(codes, scales, out, p, st); }
-    else { if (vec) dequantize_group<__nv_bfloat16, true>(codes, scales, out, p, st); else dequantize_group<__nv_bfloat16, false>(codes, scales, out, p, st); }
     count_launches(1);
-    return cudaGetLastError();
+    if (dtype == QLESS_F32) return vec ? dequantize_group<float, true>(codes, scales, out, p, st) : dequantize_group<float, false>(codes, scales, out, p, st);
+    return vec ? dequantize_group<__nv_bfloat16, true>(codes, scales, out, p, st) : dequantize_group<__nv_bfloat16, false>(codes, scales, out, p, st);
 }
 
 }  // namespace qless

@@ -93,7 +93,6 @@ template <int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
 head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const GemmParams p)
 {
-    if (p.gate != nullptr && *p.gate == 0) return;           // the same for every thread of the grid
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     Bars* bars = reinterpret_cast<Bars*>(smem + STAGES * 2 * HALF);
@@ -103,26 +102,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     const uint32_t rank = cluster_ctarank();
     const int64_t pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
 
-    const int count = p.meta->count;
-    const int mt = ((MODE == GRAD_W ? p.rows : count) + 255) / 256, nt = (p.cols + 255) / 256;
-    const int splits = MODE == GRAD_H ? p.meta->splits : 1;
-    const int kblocks = ((MODE == GRAD_W ? count : p.k) + KB - 1) / KB;
-    const int ksplit = (kblocks + splits - 1) / splits;
-    const int64_t per_split = (int64_t)mt * nt;
-    const int64_t items = per_split * splits;
-    // item -> (split, column tile, row tile): GROUP_M row tiles at a time, row tiles fastest
-    auto item_of = [&](int64_t item, int& split, int& m, int& n, int& kb0, int& kb1) {
-        split = (int)(item / per_split);
-        const int64_t r = item - split * per_split;
-        const int64_t g = r / ((int64_t)GROUP_M * nt);
-        const int m0 = (int)g * GROUP_M, gm = min(GROUP_M, mt - m0);
-        const int rest = (int)(r - g * GROUP_M * nt);
-        n = rest / gm;
-        m = m0 + rest - n * gm;
-        kb0 = min(kblocks, split * ksplit);
-        kb1 = min(kblocks, kb0 + ksplit);
-    };
-
+    ahead_release();
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&bars->d_full[s]), 1); mbar_init(smem_u32(&bars->d_empty[s]), 16); }
@@ -137,6 +117,28 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;                   // accumulators at columns 0 and 256
+    ahead_wait();
+    const bool idle = p.gate != nullptr && *p.gate == 0;     // the same for every thread of the grid
+
+    const int count = p.meta->count;
+    const int mt = ((MODE == GRAD_W ? p.rows : count) + 255) / 256, nt = (p.cols + 255) / 256;
+    const int splits = MODE == GRAD_H ? p.meta->splits : 1;
+    const int kblocks = ((MODE == GRAD_W ? count : p.k) + KB - 1) / KB;
+    const int ksplit = (kblocks + splits - 1) / splits;
+    const int64_t per_split = (int64_t)mt * nt;
+    const int64_t items = idle ? 0 : per_split * splits;
+    // item -> (split, column tile, row tile): GROUP_M row tiles at a time, row tiles fastest
+    auto item_of = [&](int64_t item, int& split, int& m, int& n, int& kb0, int& kb1) {
+        split = (int)(item / per_split);
+        const int64_t r = item - split * per_split;
+        const int64_t g = r / ((int64_t)GROUP_M * nt);
+        const int m0 = (int)g * GROUP_M, gm = min(GROUP_M, mt - m0);
+        const int rest = (int)(r - g * GROUP_M * nt);
+        n = rest / gm;
+        m = m0 + rest - n * gm;
+        kb0 = min(kblocks, split * ksplit);
+        kb1 = min(kblocks, kb0 + ksplit);
+    };
 
     // A wait of a whole warp: the same answer in every lane.
     auto warp_wait = [&](uint64_t* bar, uint32_t parity, uint32_t code) -> bool {
@@ -372,6 +374,8 @@ __global__ void __launch_bounds__(1024) loss_gather_kernel(const GatherArgs a)
     __shared__ int32_t list_label[LIST];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, vecs = a.width / 8;
     const int32_t grid = (int32_t)gridDim.x, me = (int32_t)blockIdx.x;
+    ahead_release();
+    ahead_wait();
     int32_t base = 0, listed = 0;                                // tokens kept so far, and how many of them fell to this block since the last flush
     auto flush = [&]() {                                         // whole block
         __syncthreads();
@@ -484,6 +488,8 @@ struct RowArgs {
 // 32 rows per block, eight threads per row that take every eighth stretch; joined in a fixed order.
 __global__ void __launch_bounds__(256) loss_rows_kernel(const RowArgs a)
 {
+    ahead_release();
+    ahead_wait();
     if (a.gate != nullptr && *a.gate == 0) return;
     __shared__ float2 part[8][32];
     const int lane = threadIdx.x & 31, seg = threadIdx.x >> 5;
@@ -541,6 +547,8 @@ __global__ void loss_finish_kernel(const float* __restrict__ acc, int32_t width,
                                    const int32_t* __restrict__ place, const int32_t* __restrict__ labels, const float2* __restrict__ coef, int32_t sums,
                                    const __nv_bfloat16* __restrict__ weight, int64_t ld_weight, int64_t T, __nv_bfloat16* __restrict__ out, int64_t ld_out)
 {
+    ahead_release();
+    ahead_wait();
     const int vecs = width / 8, splits = meta->splits;
     const int64_t slice = (int64_t)(meta->count + 255) / 256 * 256;
     const int64_t total = T * vecs;
@@ -588,9 +596,8 @@ qless_status launch_gemm(const char* name, const CUtensorMap& a, const CUtensorM
     int64_t grid = sm_count() / 2 * 2;
     if (grid > 2 * max_items) grid = 2 * max_items;
     { ProfileScope ps(name, st);
-      head_gemm_kernel<MODE><<<(unsigned)grid, NTHREADS, smem, st>>>(a, b, p); }
+      QLESS_CUDA_TRY(launch_ahead(head_gemm_kernel<MODE>, dim3((unsigned)grid), dim3(NTHREADS), smem, st, a, b, p)); }
     count_launches(1);
-    QLESS_CUDA_TRY(cudaGetLastError());
     return QLESS_OK;
 }
 
@@ -661,8 +668,7 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
       g.weight = reinterpret_cast<const __nv_bfloat16*>(a.weight); g.T = a.T; g.ld_hidden = a.ld_hidden; g.ld_weight = a.ld_weight; g.V = a.vocab;
       g.width = a.width; g.pairs = sm_count() / 2; g.col_tiles = (int32_t)nt_h; g.cap_tiles = pl.cap_tiles; g.order = order; g.place = place;
       g.out_labels = labels; g.out_weight = weight; g.label_logit = logit; g.loss = a.loss; g.rowp = rowp; g.out = hidden; g.meta = meta;
-      loss_gather_kernel<<<(unsigned)blocks, 1024, 0, st>>>(g); }
-    QLESS_CUDA_TRY(cudaGetLastError());
+      QLESS_CUDA_TRY(launch_ahead(loss_gather_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, g)); }
     count_launches(1);
 
     CUtensorMap tm_x, tm_w, tm_p;
@@ -682,14 +688,13 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
         p.gate = gate; p.cols = cols; p.k = a.width; p.stat = stat; p.a_whole = p.b_whole = whole;
         return launch_gemm<STATS>("loss_stats", tm_x, tm_w, p, mt * ((cols + 255) / 256), st);
     };
-    auto rows = [&](int kind, int32_t entries, const int32_t* gate) {
+    auto rows = [&](int kind, int32_t entries, const int32_t* gate) -> qless_status {
         RowArgs r{};
         r.meta = meta; r.gate = gate; r.kind = kind; r.entries = entries; r.tpad = pl.tpad; r.stat = stat; r.psum = psum; r.label_logit = logit;
         r.weight = weight; r.order = order; r.rowp = rowp; r.coef = coef; r.loss = a.loss;
         { ProfileScope ps("loss_rows", st);
-          loss_rows_kernel<<<grid_of(a.T, 32), 256, 0, st>>>(r); }
+          QLESS_CUDA_TRY(launch_ahead(loss_rows_kernel, dim3(grid_of(a.T, 32)), dim3(256), 0, st, r)); }
         count_launches(1);
-        QLESS_CUDA_TRY(cudaGetLastError());
         return QLESS_OK;
     };
     auto pieces = [&](bool keep_sums, const int32_t* gate) {
@@ -729,11 +734,11 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
     }
     if (want_h) {
         { ProfileScope ps("loss_finish", st);
-          loss_finish_kernel<<<grid_of(a.T * (a.width / 8), 256), 256, 0, st>>>(acc, a.width, meta, place, labels, coef, pl.exact ? 0 : 1,
-                                                                               reinterpret_cast<const __nv_bfloat16*>(a.weight), a.ld_weight, a.T,
-                                                                               reinterpret_cast<__nv_bfloat16*>(a.grad_hidden), a.ld_grad_hidden); }
+          QLESS_CUDA_TRY(launch_ahead(loss_finish_kernel, dim3(grid_of(a.T * (a.width / 8), 256)), dim3(256), 0, st, (const float*)acc, a.width, (const LossMeta*)meta,
+                                      (const int32_t*)place, (const int32_t*)labels, (const float2*)coef, (int32_t)(pl.exact ? 0 : 1),
+                                      reinterpret_cast<const __nv_bfloat16*>(a.weight), a.ld_weight, a.T, reinterpret_cast<__nv_bfloat16*>(a.grad_hidden),
+                                      a.ld_grad_hidden)); }
         count_launches(1);
-        QLESS_CUDA_TRY(cudaGetLastError());
     }
     return QLESS_OK;
 }

@@ -150,6 +150,7 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t nS = (uint32_t)p.stages;
 
+    ahead_release();
     if (threadIdx.x == 0) {
         init_barriers(bars);
         prefetch_tmap(&maps.codes1); prefetch_tmap(&maps.dy1); prefetch_tmap(&maps.a); prefetch_tmap(&maps.b);
@@ -158,6 +159,7 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    ahead_wait();
     const uint32_t tmem = bars->tmem_base;                  // accumulators at columns 0 and 128, expanded codes of stage s at 256 + 64 s
 
     // item -> (slice, token tile, kind): of two neighbouring items one reads codes and one dY, and a block takes them in turn, so that at
@@ -367,6 +369,8 @@ __global__ void lora_split_kernel(const float* __restrict__ part, __nv_bfloat16*
                                   int32_t slices, int32_t parts, int32_t term, int32_t boxes, float scaling)
 {
     const int64_t rows = 2 * T, total = rows * (n64 / 4);
+    ahead_release();
+    ahead_wait();
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
         const int64_t row = i / (n64 / 4);
         const int c = (int)(i - row * (n64 / 4)) * 4;
@@ -435,6 +439,7 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t nS = (uint32_t)p.stages;
 
+    ahead_release();
     if (threadIdx.x == 0) {
         init_barriers(bars);
         prefetch_tmap(&maps.codes2); prefetch_tmap(&maps.dy2); prefetch_tmap(&maps.fac);
@@ -443,6 +448,7 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    ahead_wait();
     const uint32_t tmem = bars->tmem_base;                  // accumulator of item n, sub-tile m: column (n & 1) * 256 + m * 128
 
     const uint32_t items = (uint32_t)p.items, step_items = gridDim.x;
@@ -678,6 +684,8 @@ template <typename OutT>
 __global__ void lora_join_kernel(const LoraJoin* __restrict__ joins, const float* __restrict__ part, int64_t width, OutT* __restrict__ grads,
                                  int64_t ld_grads)
 {
+    ahead_release();
+    ahead_wait();
     const LoraJoin j = joins[blockIdx.y];
     for (int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * 4; i < width; i += (int64_t)gridDim.x * blockDim.x * 4) {
         const float* src = part + (int64_t)j.first * width + i;
@@ -698,6 +706,8 @@ __global__ void lora_join_kernel(const LoraJoin* __restrict__ joins, const float
 struct Words { uint64_t w[480]; };
 __global__ void upload_kernel(const __grid_constant__ Words src, uint64_t* __restrict__ dst, int n)
 {
+    ahead_release();
+    ahead_wait();
     if ((int)threadIdx.x < n) dst[threadIdx.x] = src.w[threadIdx.x];
 }
 cudaError_t upload(const void* host, size_t bytes, void* dev, cudaStream_t st)
@@ -708,10 +718,11 @@ cudaError_t upload(const void* host, size_t bytes, void* dev, cudaStream_t st)
         Words arg;
         const size_t len = bytes - w0 * 8 < n * 8 ? bytes - w0 * 8 : n * 8;
         memcpy(arg.w, reinterpret_cast<const uint8_t*>(host) + w0 * 8, len);
-        upload_kernel<<<1, 512, 0, st>>>(arg, reinterpret_cast<uint64_t*>(dev) + w0, (int)n);
+        const cudaError_t e = launch_ahead(upload_kernel, dim3(1), dim3(512), 0, st, arg, reinterpret_cast<uint64_t*>(dev) + w0, (int)n);
+        if (e != cudaSuccess) return e;
         count_launches(1);
     }
-    return cudaGetLastError();
+    return cudaSuccess;
 }
 
 }  // namespace
@@ -798,12 +809,12 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
         const int64_t grid = f.items < sm_count() ? f.items : sm_count();
         { ProfileScope ps("lora_factors", st);
           QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_factors_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-          lora_factors_kernel<<<(unsigned)grid, NTHREADS, smem, st>>>(m, f); }
-        QLESS_CUDA_TRY(cudaGetLastError());
+          QLESS_CUDA_TRY(launch_ahead(lora_factors_kernel, dim3((unsigned)grid), dim3(NTHREADS), smem, st, m, f)); }
         if (pl.slices > 1) {
           ProfileScope ps("lora_split", st);
           const int64_t blocks = (2 * a.T * (pl.n64 / 4) + 255) / 256, most = (int64_t)sm_count() * 8;
-          lora_split_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, st>>>(f.part, fac, a.T, pl.n64, pl.nr, pl.slices, pl.parts, pl.term, pl.boxes, a.scaling);
+          QLESS_CUDA_TRY(launch_ahead(lora_split_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, (const float*)f.part, fac, a.T, pl.n64,
+                                      pl.nr, pl.slices, pl.parts, pl.term, pl.boxes, a.scaling));
           count_launches(1);
         }
         QLESS_CUDA_TRY(cudaGetLastError());
@@ -825,7 +836,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
 #define QLESS_LAUNCH_LORA_OUTER(OUT, N)                                                                                              \
       {                                                                                                                                \
           QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_outer_kernel<OUT, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));      \
-          lora_outer_kernel<OUT, N><<<(unsigned)grid, NTHREADS, smem, st>>>(m, o);                                                      \
+          QLESS_CUDA_TRY(launch_ahead(lora_outer_kernel<OUT, N>, dim3((unsigned)grid), dim3(NTHREADS), smem, st, m, o));                \
       }
       if (a.dtype == QLESS_F32) {
           if (boxes == 1) QLESS_LAUNCH_LORA_OUTER(float, 1)
@@ -846,9 +857,10 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
         const int64_t width = (int64_t)a.rank * (a.in + a.out);
         const int64_t bx = (width / 4 + 255) / 256;
         const dim3 g((unsigned)(bx < 1024 ? bx : 1024), (unsigned)(a.num_joins - j0 < 65535 ? a.num_joins - j0 : 65535));
-        if (a.dtype == QLESS_F32) lora_join_kernel<float><<<g, 256, 0, st>>>(d_joins + j0, o.part, width, reinterpret_cast<float*>(a.grads), a.ld_grads);
-        else lora_join_kernel<__nv_bfloat16><<<g, 256, 0, st>>>(d_joins + j0, o.part, width, reinterpret_cast<__nv_bfloat16*>(a.grads), a.ld_grads);
-        QLESS_CUDA_TRY(cudaGetLastError());
+        const LoraJoin* list = d_joins + j0;
+        const float* part = o.part;
+        if (a.dtype == QLESS_F32) QLESS_CUDA_TRY(launch_ahead(lora_join_kernel<float>, g, dim3(256), 0, st, list, part, width, reinterpret_cast<float*>(a.grads), a.ld_grads));
+        else QLESS_CUDA_TRY(launch_ahead(lora_join_kernel<__nv_bfloat16>, g, dim3(256), 0, st, list, part, width, reinterpret_cast<__nv_bfloat16*>(a.grads), a.ld_grads));
         count_launches(1);
     }
     return QLESS_OK;

@@ -5,6 +5,7 @@
 #include <cuda_bf16.h>
 #include <stdint.h>
 #include <stddef.h>
+#include <utility>
 
 #include "qless.h"
 
@@ -37,6 +38,26 @@ struct ProfileScope {
 void count_launches(int n);   // bookkeeping behind qless_kernel_launches()
 
 int sm_count();   // SM count of the current device (cached)
+
+#ifdef __CUDACC__
+// Launches that may begin while the kernel before them in the stream still runs (programmatic dependent launch): a kernel launched
+// by launch_ahead calls ahead_wait() before it touches global memory, which returns when the kernels before it have ended and
+// their writes can be seen, and ahead_release() once it no longer minds the next one's blocks moving in. What it saves is the
+// launch latency and the set-up (barriers, tensor memory, tensor maps) between dependent kernels: 2 to 3 us each.
+__device__ __forceinline__ void ahead_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void ahead_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <typename... Params, typename... Args>
+inline cudaError_t launch_ahead(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args)
+{
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = st; cfg.attrs = &attr; cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+#endif
 
 // Address of the device-side timeout word that kernels with bounded waits set when they give up.
 unsigned int* timeout_flag_ptr();
