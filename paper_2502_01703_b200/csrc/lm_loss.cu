@@ -16,6 +16,8 @@
 //   PROBS   h W^T        epilogue: exp(l - r) or w (p - [v = y]) as bf16 into one piece of the vocabulary    (gradients)
 //   GRAD_H  piece * W    epilogue: fp32, added to what the earlier pieces left
 //   GRAD_W  piece^T * h  epilogue: bf16 rows of dW
+// Up to FEW = 256 tokens the roles of rows and columns are swapped (256 rows of W, or hidden channels, by all tokens): with the tokens
+// as the 256 rows of a tile most of the tensor pipe's work would go to rows that do not exist, and took longer than W's bytes.
 // Gradient of the hidden states alone: two products instead of three. The reference r of a row is its label's logit, a dot product
 // taken when the row is gathered. Any reference gives the same softmax, and with the exponents of fp32 and bf16 one that lies up to
 // LIMIT = 64 powers of two (a loss of 44) below the row's maximum is as good as the maximum itself. Should a row exceed that, a flag
@@ -32,9 +34,10 @@ namespace {
 using namespace tc;
 
 constexpr int NTHREADS = 320;               // warp 0 TMA, warp 1 MMA, warps 2-9 epilogue (two groups of four, 128 columns each)
-constexpr int STAGES = 3;
+constexpr int MAX_STAGES = 5;
 constexpr int KB = 128;                     // K columns per stage: 64 KiB of operands per CTA
-constexpr int HALF = 32768;                 // bytes of one operand of a stage
+constexpr int HALF = 32768;                 // bytes of the A operand of a stage (and of B, where it has 256 columns)
+constexpr int FEW = 256;                    // tokens up to which the roles are swapped
 constexpr int GROUP_M = 16;                 // row tiles that share a pass over the column tiles (their operand stays in L2)
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LIMIT = 64.0f;
@@ -53,10 +56,11 @@ struct GemmParams {
     int32_t rows;                           // GRAD_W: vocabulary columns of the piece
     int32_t k;                              // contraction length (GRAD_W: the token count instead)
     int64_t tpad;
+    int32_t stages, b_rows;                 // b_rows: rows of B that one CTA of the pair brings
     const int32_t* labels;                  // [tpad] of the gathered tokens
     const RowParam* rowp;
-    float2* stat;                           // STATS: [2 * tiles][tpad] (maximum, sum)
-    float* psum;                            // PROBS: [2 * tiles][tpad] sums, or NULL
+    float2* stat;                           // STATS: [entries per tile * tiles][tpad] (maximum, sum)
+    float* psum;                            // PROBS: [entries per tile * tiles][tpad] sums, or NULL
     int32_t tile0;                          // tile index of the launch's first column tile in stat / psum
     __nv_bfloat16* out;                     // PROBS: piece [tpad][ld_out]; GRAD_W: rows of dW
     int64_t ld_out;
@@ -68,8 +72,10 @@ struct GemmParams {
 };
 
 struct __align__(8) Bars {
-    uint64_t full[STAGES], empty[STAGES], d_full[2], d_empty[2], drain;
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES], d_full[2], d_empty[2], drain;
     uint32_t tmem_base, abort_flag;
+    __align__(16) RowParam rowp[FEW];       // swapped roles: of every token
+    int32_t label[FEW];
 };
 
 struct Ring {
@@ -89,22 +95,43 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
     return *reinterpret_cast<const uint32_t*>(&z);
 }
 
-template <int MODE>
+// Sum (or maximum) over the 32 lanes of each of 32 values: lane L ends with that of value L, after 31 shuffles.
+template <bool MAX>
+__device__ __forceinline__ float across_lanes(float (&v)[32], int lane)
+{
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) {
+        const bool up = (lane & s) != 0;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            if (k >= s) break;
+            const float give = up ? v[k] : v[k + s], keep = up ? v[k + s] : v[k];
+            const float got = __shfl_xor_sync(0xFFFFFFFFu, give, s);
+            v[k] = MAX ? fmaxf(keep, got) : keep + got;
+        }
+    }
+    return v[0];
+}
+
+template <int MODE, bool SWAP>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
 head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const GemmParams p)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    Bars* bars = reinterpret_cast<Bars*>(smem + STAGES * 2 * HALF);
+    const int half_b = SWAP ? p.b_rows * 2 * KB : HALF;        // bytes of a stage's B operand in this CTA
+    const int stage_bytes = HALF + half_b;
+    Bars* bars = reinterpret_cast<Bars*>(smem + (size_t)p.stages * stage_bytes);
+    const uint32_t nS = (uint32_t)p.stages;
     volatile uint32_t* abort_flag = &bars->abort_flag;
-    constexpr bool A_MN = MODE == GRAD_W, B_MN = MODE == GRAD_H || MODE == GRAD_W;
+    constexpr bool A_MN = MODE == GRAD_W || (SWAP && MODE == GRAD_H), B_MN = !SWAP && (MODE == GRAD_H || MODE == GRAD_W);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = cluster_ctarank();
     const int64_t pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
 
     ahead_release();
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }
+        for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&bars->d_full[s]), 1); mbar_init(smem_u32(&bars->d_empty[s]), 16); }
         mbar_init(smem_u32(&bars->drain), 1);
         bars->abort_flag = 0;
@@ -121,7 +148,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     const bool idle = p.gate != nullptr && *p.gate == 0;     // the same for every thread of the grid
 
     const int count = p.meta->count;
-    const int mt = ((MODE == GRAD_W ? p.rows : count) + 255) / 256, nt = (p.cols + 255) / 256;
+    const int mt = ((MODE == GRAD_W ? p.rows : SWAP ? (count > 0 ? p.cols : 0) : count) + 255) / 256, nt = SWAP ? 1 : (p.cols + 255) / 256;
     const int splits = MODE == GRAD_H ? p.meta->splits : 1;
     const int kblocks = ((MODE == GRAD_W ? count : p.k) + KB - 1) / KB;
     const int ksplit = (kblocks + splits - 1) / splits;
@@ -154,27 +181,29 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
             for (int64_t item = pair; item < items && ok; item += num_pairs) {
                 int split, m, n, kb0, kb1;
                 item_of(item, split, m, n, kb0, kb1);
-                const int a0 = m * 256 + (int)rank * 128, b0 = n * 256 + (int)rank * 128 + (B_MN ? 0 : p.col0);
-                for (int kb = kb0; kb < kb1; ++kb, ++it, ring.next(STAGES)) {
+                // (S) rows of W start at col0, (GRAD_H) its contraction does
+                const int a0 = m * 256 + (int)rank * 128 + (SWAP && !A_MN ? p.col0 : 0);
+                const int b0 = SWAP ? (int)rank * p.b_rows : n * 256 + (int)rank * 128 + (B_MN ? 0 : p.col0);
+                for (int kb = kb0; kb < kb1; ++kb, ++it, ring.next(nS)) {
                     if (!warp_wait(&bars->empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
                     const uint32_t full = map_to_cta(smem_u32(&bars->full[ring.slot]), 0);
-                    const uint32_t a = smem_u32(smem + (size_t)ring.slot * 2 * HALF), b = a + HALF;
+                    const uint32_t a = smem_u32(smem + (size_t)ring.slot * stage_bytes), b = a + HALF;
                     const int k0 = kb * KB, kw = k0 + (MODE == GRAD_H ? p.col0 : 0);
-                    const int ac = A_MN ? a0 : k0, ar = A_MN ? k0 : a0, bc = B_MN ? b0 : k0, br = B_MN ? kw : b0;      // first column and row
+                    const int ac = A_MN ? a0 : k0, ar = A_MN ? (SWAP ? kw : k0) : a0, bc = B_MN ? b0 : k0, br = B_MN ? kw : b0;      // first column and row
                     if (elect_one()) {
-                        if (rank == 0) mbar_arrive_expect_tx(smem_u32(&bars->full[ring.slot]), 4 * HALF);      // both CTAs' bytes
+                        if (rank == 0) mbar_arrive_expect_tx(smem_u32(&bars->full[ring.slot]), 2 * stage_bytes);      // both CTAs' bytes
                         if (p.a_whole) tma_load_3d_pair(a, &tm_a, full, 0, ar, ac / 64);
                         else for (int j = 0; j < 2; ++j) tma_load_2d_pair(a + j * 16384, &tm_a, full, ac + 64 * j, ar);
                         if (p.b_whole) tma_load_3d_pair(b, &tm_b, full, 0, br, bc / 64);
-                        else for (int j = 0; j < 2; ++j) tma_load_2d_pair(b + j * 16384, &tm_b, full, bc + 64 * j, br);
+                        else for (int j = 0; j < 2; ++j) tma_load_2d_pair(b + j * (half_b / 2), &tm_b, full, bc + 64 * j, br);
                     }
                     __syncwarp();
                 }
             }
             if (!ok) {       // leave no copy in flight: the leader waits (bounded) for the stages that are armed, the peer idles
                 if (rank == 0) {
-                    for (uint32_t j = (it > STAGES ? it - STAGES : 0u); j < it; ++j)
-                        if (!mbar_wait_quiet(smem_u32(&bars->full[j % STAGES]), (j / STAGES) & 1u, 1u << 14)) break;
+                    for (uint32_t j = (it > nS ? it - nS : 0u); j < it; ++j)
+                        if (!mbar_wait_quiet(smem_u32(&bars->full[j % nS]), (j / nS) & 1u, 1u << 14)) break;
                 } else {
                     for (uint32_t t = 0; t < (1u << 14); ++t) __nanosleep(64);
                 }
@@ -182,7 +211,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
         }
     } else if (warp == 1) {
         if (rank == 0) {
-            const uint32_t idesc = make_idesc(1, 1, 1, 256, 256) | (A_MN ? IDESC_A_MN : 0u) | (B_MN ? IDESC_B_MN : 0u);
+            const uint32_t idesc = make_idesc(1, 1, 1, 256, SWAP ? 2 * p.b_rows : 256) | (A_MN ? IDESC_A_MN : 0u) | (B_MN ? IDESC_B_MN : 0u);
             Ring ring;
             uint32_t n_acc = 0;
             bool ok = true;
@@ -192,18 +221,19 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                 const uint32_t buf = n_acc & 1u, d = tmem + buf * 256;
                 if (!warp_wait(&bars->d_empty[buf], ((n_acc >> 1) & 1u) ^ 1u, TO_MMA)) { ok = false; break; }
                 tc_fence_after();
-                for (int kb = kb0; kb < kb1; ++kb, ring.next(STAGES)) {
+                for (int kb = kb0; kb < kb1; ++kb, ring.next(nS)) {
                     if (!warp_wait(&bars->full[ring.slot], ring.parity, TO_MMA)) { ok = false; break; }
                     tc_fence_after();
                     if (elect_one()) {
-                    const uint32_t a = smem_u32(smem + (size_t)ring.slot * 2 * HALF), b = a + HALF;
+                    const uint32_t a = smem_u32(smem + (size_t)ring.slot * stage_bytes), b = a + HALF;
+                    const uint64_t b_next = (uint64_t)(half_b / 32);      // (K-major) the second 64 columns of K
                     // made once per stage, advanced by constants (units of 16 bytes)
                     const uint64_t a0 = A_MN ? make_smem_desc_mn_sw128(a, 16384) : make_smem_desc_sw128(a);
                     const uint64_t b0 = B_MN ? make_smem_desc_mn_sw128(b, 16384) : make_smem_desc_sw128(b);
                     mma_f16_ss_pair(d, a0, b0, idesc, kb > kb0);
 #pragma unroll
                     for (int k = 1; k < KB / 16; ++k)
-                        mma_f16_ss_pair(d, a0 + (uint64_t)(A_MN ? k * 128 : (k >> 2) * 1024 + (k & 3) * 2), b0 + (uint64_t)(B_MN ? k * 128 : (k >> 2) * 1024 + (k & 3) * 2), idesc, 1u);
+                        mma_f16_ss_pair(d, a0 + (uint64_t)(A_MN ? k * 128 : (k >> 2) * 1024 + (k & 3) * 2), b0 + (B_MN ? (uint64_t)(k * 128) : (k >> 2) * b_next + (uint64_t)((k & 3) * 2)), idesc, 1u);
                     mma_commit_pair(smem_u32(&bars->empty[ring.slot]));
                     }
                     __syncwarp();
@@ -218,7 +248,84 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
         const int q = warp & 3, half = warp >= 6 ? 1 : 0;
         const uint32_t lane_base = (uint32_t)(q * 32) << 16;
         uint32_t n_acc = 0;
-        for (int64_t item = pair; item < items; item += num_pairs, ++n_acc) {
+        if (SWAP && MODE != GRAD_H) {
+            for (int t = threadIdx.x - 64; t < count; t += 256) {
+                bars->label[t] = p.labels[t];
+                if (MODE == PROBS) bars->rowp[t] = p.rowp[t];
+            }
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+        }
+        for (int64_t item = pair; SWAP && item < items; item += num_pairs, ++n_acc) {
+            // lane = row of W (or hidden channel), column = token; the second group of warps takes the second half of the tokens
+            int split, m, n, kb0, kb1;
+            item_of(item, split, m, n, kb0, kb1);
+            const int v = m * 256 + (int)rank * 128 + q * 32 + lane;
+            const uint32_t buf = n_acc & 1u;
+            const int lim = min(count - half * p.b_rows, p.b_rows);      // tokens of this half
+            bool ok = mbar_wait_cluster(smem_u32(&bars->d_full[buf]), (n_acc >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            float run_max = -INFINITY;
+#pragma unroll 1
+            for (int c0 = 0; c0 < lim; c0 += 32) {
+                uint32_t raw[32];
+                tmem_ld_x32(tmem + lane_base + buf * 256 + half * p.b_rows + c0, raw);
+                tmem_wait_ld();
+                const int t0 = half * p.b_rows + c0, have = lim - c0;
+                if (MODE == GRAD_H) {
+                    if (v < p.cols) {
+                        float* dst = p.acc + ((int64_t)split * FEW + t0) * p.cols + v;
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) {
+                            if (k >= have) break;
+                            float x = kb0 == kb1 ? 0.0f : __uint_as_float(raw[k]);
+                            if (p.accumulate) x += dst[(int64_t)k * p.cols];
+                            dst[(int64_t)k * p.cols] = x;
+                        }
+                    }
+                    continue;
+                }
+                float e[32];
+                const int64_t entry = ((int64_t)(p.tile0 + m) * 2 + rank) * 4 + q;
+                if (MODE == STATS) {
+                    float top[32];
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        const bool out = k >= have || v >= p.cols || (k < have && bars->label[t0 + k] == p.col0 + v);
+                        e[k] = out ? -INFINITY : __uint_as_float(raw[k]) * LOG2E;
+                        top[k] = e[k];
+                    }
+                    const float most = across_lanes<true>(top, lane), ref = most > -INFINITY ? most : 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) e[k] = ex2(e[k] - __shfl_sync(0xFFFFFFFFu, ref, k));
+                    const float sum = across_lanes<false>(e, lane);
+                    if (lane < have) p.stat[entry * p.tpad + t0 + lane] = make_float2(most, sum);
+                } else {
+                    __nv_bfloat16* dst = p.out + (int64_t)t0 * p.ld_out + v;
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) {
+                        if (k < have) {
+                            const RowParam rp = bars->rowp[t0 + k];
+                            const bool own = bars->label[t0 + k] == p.col0 + v, out = own || v >= p.cols;
+                            const float x = out ? -INFINITY : fmaf(__uint_as_float(raw[k]), LOG2E, -rp.r2);
+                            run_max = fmaxf(run_max, x);
+                            e[k] = ex2(x);
+                            dst[(int64_t)k * p.ld_out] = __float2bfloat16_rn(own ? rp.wl : e[k] * rp.w);
+                        } else e[k] = 0.0f;
+                    }
+                    if (p.psum != nullptr) {
+                        const float sum = across_lanes<false>(e, lane);
+                        if (lane < have) p.psum[entry * p.tpad + t0 + lane] = sum;
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_leader_tmem(smem_u32(&bars->d_empty[buf]), rank);
+            if (MODE == PROBS && p.psum != nullptr && run_max > LIMIT) *p.redo = 1;
+        }
+        for (int64_t item = pair; !SWAP && item < items; item += num_pairs, ++n_acc) {
             int split, m, n, kb0, kb1;
             item_of(item, split, m, n, kb0, kb1);
             const int64_t row = (int64_t)m * 256 + rank * 128 + q * 32 + lane;
@@ -348,9 +455,8 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
 // place[t] = position of token t among the tokens with a label in [0, V), or -1; order = the inverse. Every block scans all labels (they
 // are few against the rows) and lists the tokens whose rows fall to it; then its warps copy a row each and take the dot product with the
 // label's row of W on the way. Rows land in `out` in order, zeros behind the last up to a multiple of 128 (GRAD_W contracts over the rows).
-// Also how many slices the hidden-state product is cut into along the vocabulary: as many as keep the CTA pairs busy (at least 95 %,
-// four slices at most where there are tiles enough, or as many as fill one round where there are few), within the `cap_tiles` row
-// tiles the workspace has room for.
+// Also how many slices the hidden-state product is cut into along the vocabulary: the fewest that keep 95 % of the CTA pairs busy, or
+// the best of up to four (16 where the tiles do not fill one round), within the `cap_tiles` row tiles the workspace has room for.
 struct GatherArgs {
     const int64_t* labels;
     const float* token_weight;
@@ -451,15 +557,12 @@ __global__ void __launch_bounds__(1024) loss_gather_kernel(const GatherArgs a)
         const int mt = (base + 255) / 256, tiles = mt * a.col_tiles;
         int best = 1;
         if (mt > 0) {
-            const int pairs = a.pairs, most = min(a.cap_tiles / mt, tiles >= pairs ? 4 : max(1, pairs / tiles));
-            if (tiles < pairs) best = max(1, most);
-            else {
-                float best_use = 0.0f;
-                for (int s = 1; s <= most && best_use < 0.95f; ++s) {
-                    const int items = tiles * s, rounds = (items + pairs - 1) / pairs;
-                    const float use = (float)items / (float)(rounds * pairs);
-                    if (use > best_use) { best_use = use; best = s; }
-                }
+            const int pairs = a.pairs, most = min(a.cap_tiles / mt, tiles >= pairs ? 4 : 16);
+            float best_use = 0.0f;
+            for (int s = 1; s <= most && best_use < 0.95f; ++s) {
+                const int items = tiles * s, rounds = (items + pairs - 1) / pairs;
+                const float use = (float)items / (float)(rounds * pairs);
+                if (use > best_use) { best_use = use; best = s; }
             }
         }
         a.meta->count = base; a.meta->splits = best; a.meta->redo = 0;
@@ -473,7 +576,8 @@ enum { ROW_REFERENCE = 0, ROW_FROM_STATS = 1, ROW_FROM_SUMS = 2 };
 struct RowArgs {
     const LossMeta* meta;
     const int32_t* gate;
-    int32_t kind, entries;                  // entries: 128-column stretches with a partial result
+    int32_t kind, entries;                  // entries: stretches of columns with a partial result
+    int32_t apart;                          // ROW_FROM_STATS: the hidden states' gradient alone is wanted
     int64_t tpad;
     const float2* stat;
     const float* psum;
@@ -481,17 +585,17 @@ struct RowArgs {
     const float* weight;
     const int32_t* order;
     RowParam* rowp;
-    float2* coef;                           // ROW_FROM_SUMS: w sigma(d), 1 / s
+    float2* coef;                           // w sigma(d), and what the sum over the other columns is multiplied by
     float* loss;
 };
 
-// 32 rows per block, eight threads per row that take every eighth stretch; joined in a fixed order.
-__global__ void __launch_bounds__(256) loss_rows_kernel(const RowArgs a)
+// 32 rows per block, 32 threads per row that take every 32nd stretch; joined in a fixed order.
+__global__ void __launch_bounds__(1024) loss_rows_kernel(const RowArgs a)
 {
     ahead_release();
     ahead_wait();
     if (a.gate != nullptr && *a.gate == 0) return;
-    __shared__ float2 part[8][32];
+    __shared__ float2 part[32][32];
     const int lane = threadIdx.x & 31, seg = threadIdx.x >> 5;
     const int count = a.meta->count;
     for (int64_t r0 = (int64_t)blockIdx.x * 32; r0 < count; r0 += (int64_t)gridDim.x * 32) {
@@ -499,9 +603,11 @@ __global__ void __launch_bounds__(256) loss_rows_kernel(const RowArgs a)
         float m = -INFINITY, s = 0.0f;
         if (row < count) {
             if (a.kind == ROW_FROM_SUMS) {
-                for (int i = seg; i < a.entries; i += 8) s += a.psum[(int64_t)i * a.tpad + row];
+#pragma unroll 4
+                for (int i = seg; i < a.entries; i += 32) s += a.psum[(int64_t)i * a.tpad + row];
             } else {
-                for (int i = seg; i < a.entries; i += 8) {
+#pragma unroll 4
+                for (int i = seg; i < a.entries; i += 32) {
                     const float2 x = a.stat[(int64_t)i * a.tpad + row];
                     const float now = fmaxf(m, x.x);
                     if (now > -INFINITY) { s = s * ex2(m - now) + x.y * ex2(x.x - now); m = now; }
@@ -513,7 +619,7 @@ __global__ void __launch_bounds__(256) loss_rows_kernel(const RowArgs a)
         part[seg][lane] = make_float2(m, s);
         __syncthreads();
         if (seg == 0 && row < count) {
-            for (int j = 1; j < 8; ++j) {
+            for (int j = 1; j < 32; ++j) {
                 const float2 x = part[j][lane];
                 if (a.kind == ROW_FROM_SUMS) { s += x.y; continue; }
                 const float now = fmaxf(m, x.x);
@@ -536,7 +642,10 @@ __global__ void __launch_bounds__(256) loss_rows_kernel(const RowArgs a)
             else if (d != d) { nll = d; sigma = d; }
             a.loss[a.order[row]] = nll;
             if (a.kind == ROW_FROM_SUMS) a.coef[row] = make_float2(w * sigma, s == 0.0f ? 0.0f : 1.0f / s);
-            else a.rowp[row] = RowParam{fmaxf(others, ly) + tail * LOG2E, w, -w * sigma, 0.0f};      // the full normaliser
+            else if (a.apart) {                                  // probabilities among the other columns; the label's row joins at the end
+                a.rowp[row] = RowParam{s == 0.0f ? 0.0f : others, 1.0f, 0.0f, 0.0f};
+                a.coef[row] = make_float2(w * sigma, 1.0f);
+            } else a.rowp[row] = RowParam{fmaxf(others, ly) + tail * LOG2E, w, -w * sigma, 0.0f};      // the full normaliser
         }
     }
 }
@@ -588,15 +697,17 @@ unsigned grid_of(int64_t work, int threads)
     return (unsigned)(blocks < 1 ? 1 : blocks < most ? blocks : most);
 }
 
-template <int MODE>
-qless_status launch_gemm(const char* name, const CUtensorMap& a, const CUtensorMap& b, const GemmParams& p, int64_t max_items, cudaStream_t st)
+template <int MODE, bool SWAP>
+qless_status launch_gemm(const char* name, const CUtensorMap& a, const CUtensorMap& b, GemmParams p, int64_t max_items, cudaStream_t st)
 {
-    const size_t smem = 1024 + STAGES * 2 * HALF + sizeof(Bars);
-    QLESS_CUDA_TRY(cudaFuncSetAttribute(head_gemm_kernel<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    const size_t stage = HALF + (SWAP ? (size_t)p.b_rows * 2 * KB : HALF), budget = 227 * 1024 - 1024 - sizeof(Bars);
+    p.stages = (int32_t)(budget / stage < MAX_STAGES ? budget / stage : MAX_STAGES);
+    const size_t smem = 1024 + p.stages * stage + sizeof(Bars);
+    QLESS_CUDA_TRY((allow_full_smem<head_gemm_kernel<MODE, SWAP>>()));
     int64_t grid = sm_count() / 2 * 2;
     if (grid > 2 * max_items) grid = 2 * max_items;
     { ProfileScope ps(name, st);
-      QLESS_CUDA_TRY(launch_ahead(head_gemm_kernel<MODE>, dim3((unsigned)grid), dim3(NTHREADS), smem, st, a, b, p)); }
+      QLESS_CUDA_TRY(launch_ahead(head_gemm_kernel<MODE, SWAP>, dim3((unsigned)grid), dim3(NTHREADS), smem, st, a, b, p)); }
     count_launches(1);
     return QLESS_OK;
 }
@@ -618,8 +729,9 @@ LossPlan plan_loss(int64_t T, int32_t width, int32_t vocab, bool want_h, bool wa
     if (piece_tiles < 1) piece_tiles = 1;
     if (piece_tiles > tiles_v) piece_tiles = tiles_v;
     pl.piece = (int32_t)(piece_tiles * 256);
-    pl.entries = (int32_t)(2 * tiles_v);
-    int64_t cap = pairs / nt_h < 16 ? pairs / nt_h : 16;       // slices where there is one row tile
+    pl.few = T <= FEW && !want_w;
+    pl.entries = (int32_t)((pl.few ? 8 : 2) * tiles_v);         // partial statistics: one per warp of 32 rows of W, or per 128 columns
+    int64_t cap = 16;                                           // slices where there is one row tile
     if (cap < 3 * mt) cap = 3 * mt;
     pl.cap_tiles = (int32_t)cap;
     size_t off = 0;
@@ -672,28 +784,31 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
     count_launches(1);
 
     CUtensorMap tm_x, tm_w, tm_p;
+    const bool few = pl.few;
+    const int32_t b_rows = few ? (int32_t)((a.T + 31) / 32 * 16) : 128;      // rows of hidden states or of the piece that one CTA brings
     qless_status s;
     const bool whole = a.width % 64 == 0;
-    if ((s = whole ? make_tmap_blocks_sw128(&tm_x, hidden, 2, a.width / 64, pl.tpad, (uint64_t)a.width * 2, 128, 128, 2)
-                   : make_tmap_2d_sw128(&tm_x, hidden, 2, a.width, pl.tpad, (uint64_t)a.width * 2, 64, 128)) != QLESS_OK) return s;
+    if ((s = whole ? make_tmap_blocks_sw128(&tm_x, hidden, 2, a.width / 64, pl.tpad, (uint64_t)a.width * 2, 128, b_rows, 2)
+                   : make_tmap_2d_sw128(&tm_x, hidden, 2, a.width, pl.tpad, (uint64_t)a.width * 2, 64, b_rows)) != QLESS_OK) return s;
     if ((s = whole ? make_tmap_blocks_sw128(&tm_w, a.weight, 2, a.width / 64, a.vocab, (uint64_t)a.ld_weight * 2, 128, 128, 2)
                    : make_tmap_2d_sw128(&tm_w, a.weight, 2, a.width, a.vocab, (uint64_t)a.ld_weight * 2, 64, 128)) != QLESS_OK) return s;
     if (want_h || want_w)
-        if ((s = make_tmap_blocks_sw128(&tm_p, piece, 2, pl.piece / 64, pl.tpad, (uint64_t)pl.piece * 2, 128, 128, 2)) != QLESS_OK) return s;
+        if ((s = make_tmap_blocks_sw128(&tm_p, piece, 2, pl.piece / 64, pl.tpad, (uint64_t)pl.piece * 2, 128, b_rows, 2)) != QLESS_OK) return s;
 
     GemmParams base{};
-    base.meta = meta; base.tpad = pl.tpad; base.labels = labels; base.rowp = rowp; base.timeout_word = timeout_word;
+    base.meta = meta; base.tpad = pl.tpad; base.labels = labels; base.rowp = rowp; base.b_rows = b_rows; base.timeout_word = timeout_word;
     auto stats = [&](int32_t cols, const int32_t* gate) {
         GemmParams p = base;
         p.gate = gate; p.cols = cols; p.k = a.width; p.stat = stat; p.a_whole = p.b_whole = whole;
-        return launch_gemm<STATS>("loss_stats", tm_x, tm_w, p, mt * ((cols + 255) / 256), st);
+        const int64_t tiles = (cols + 255) / 256;
+        return few ? launch_gemm<STATS, true>("loss_stats", tm_w, tm_x, p, tiles, st) : launch_gemm<STATS, false>("loss_stats", tm_x, tm_w, p, mt * tiles, st);
     };
     auto rows = [&](int kind, int32_t entries, const int32_t* gate) -> qless_status {
         RowArgs r{};
         r.meta = meta; r.gate = gate; r.kind = kind; r.entries = entries; r.tpad = pl.tpad; r.stat = stat; r.psum = psum; r.label_logit = logit;
-        r.weight = weight; r.order = order; r.rowp = rowp; r.coef = coef; r.loss = a.loss;
+        r.weight = weight; r.order = order; r.rowp = rowp; r.coef = coef; r.loss = a.loss; r.apart = want_h && !want_w;
         { ProfileScope ps("loss_rows", st);
-          QLESS_CUDA_TRY(launch_ahead(loss_rows_kernel, dim3(grid_of(a.T, 32)), dim3(256), 0, st, r)); }
+          QLESS_CUDA_TRY(launch_ahead(loss_rows_kernel, dim3(grid_of(a.T, 32)), dim3(1024), 0, st, r)); }
         count_launches(1);
         return QLESS_OK;
     };
@@ -703,18 +818,21 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
             GemmParams p = base;
             p.gate = gate; p.cols = cols; p.col0 = v0; p.k = a.width; p.out = piece; p.ld_out = pl.piece; p.tile0 = v0 / 256;
             p.psum = keep_sums ? psum : nullptr; p.redo = &meta->redo; p.a_whole = p.b_whole = whole;
-            qless_status e = launch_gemm<PROBS>("loss_probs", tm_x, tm_w, p, mt * ((cols + 255) / 256), st);
+            const int64_t tiles = (cols + 255) / 256;
+            qless_status e = few ? launch_gemm<PROBS, true>("loss_probs", tm_w, tm_x, p, tiles, st) : launch_gemm<PROBS, false>("loss_probs", tm_x, tm_w, p, mt * tiles, st);
             if (e != QLESS_OK) return e;
             if (want_h) {
                 GemmParams g = base;
-                g.gate = gate; g.cols = a.width; g.col0 = v0; g.k = cols; g.acc = acc; g.accumulate = v0 > 0; g.a_whole = 1; g.b_whole = whole;
-                e = launch_gemm<GRAD_H>("loss_grad_hidden", tm_p, tm_w, g, pl.cap_tiles * nt_h, st);
+                g.gate = gate; g.cols = a.width; g.col0 = v0; g.k = cols; g.acc = acc; g.accumulate = v0 > 0;
+                g.a_whole = few ? whole : 1; g.b_whole = few ? 1 : whole;
+                e = few ? launch_gemm<GRAD_H, true>("loss_grad_hidden", tm_w, tm_p, g, pl.cap_tiles * nt_h, st)
+                        : launch_gemm<GRAD_H, false>("loss_grad_hidden", tm_p, tm_w, g, pl.cap_tiles * nt_h, st);
                 if (e != QLESS_OK) return e;
             }
             if (want_w) {
                 GemmParams g = base;
                 g.gate = gate; g.cols = a.width; g.rows = cols; g.col0 = v0; g.out = reinterpret_cast<__nv_bfloat16*>(a.grad_weight); g.ld_out = a.ld_grad_weight; g.a_whole = 1; g.b_whole = whole;
-                e = launch_gemm<GRAD_W>("loss_grad_weight", tm_p, tm_x, g, (int64_t)((cols + 255) / 256) * nt_h, st);
+                e = launch_gemm<GRAD_W, false>("loss_grad_weight", tm_p, tm_x, g, (int64_t)((cols + 255) / 256) * nt_h, st);
                 if (e != QLESS_OK) return e;
             }
         }
@@ -735,7 +853,7 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
     if (want_h) {
         { ProfileScope ps("loss_finish", st);
           QLESS_CUDA_TRY(launch_ahead(loss_finish_kernel, dim3(grid_of(a.T * (a.width / 8), 256)), dim3(256), 0, st, (const float*)acc, a.width, (const LossMeta*)meta,
-                                      (const int32_t*)place, (const int32_t*)labels, (const float2*)coef, (int32_t)(pl.exact ? 0 : 1),
+                                      (const int32_t*)place, (const int32_t*)labels, (const float2*)coef, (int32_t)(want_w ? 0 : 1),
                                       reinterpret_cast<const __nv_bfloat16*>(a.weight), a.ld_weight, a.T, reinterpret_cast<__nv_bfloat16*>(a.grad_hidden),
                                       a.ld_grad_hidden)); }
         count_launches(1);

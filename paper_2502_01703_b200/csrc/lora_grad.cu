@@ -808,7 +808,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
         const size_t smem = 1024 + f.stages * stage + sizeof(Bars);
         const int64_t grid = f.items < sm_count() ? f.items : sm_count();
         { ProfileScope ps("lora_factors", st);
-          QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_factors_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+          QLESS_CUDA_TRY(allow_full_smem<lora_factors_kernel>());
           QLESS_CUDA_TRY(launch_ahead(lora_factors_kernel, dim3((unsigned)grid), dim3(NTHREADS), smem, st, m, f)); }
         if (pl.slices > 1) {
           ProfileScope ps("lora_split", st);
@@ -835,7 +835,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
     { ProfileScope ps("lora_outer", st);
 #define QLESS_LAUNCH_LORA_OUTER(OUT, N)                                                                                              \
       {                                                                                                                                \
-          QLESS_CUDA_TRY(cudaFuncSetAttribute(lora_outer_kernel<OUT, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));      \
+          QLESS_CUDA_TRY((allow_full_smem<lora_outer_kernel<OUT, N>>()));                                                              \
           QLESS_CUDA_TRY(launch_ahead(lora_outer_kernel<OUT, N>, dim3((unsigned)grid), dim3(NTHREADS), smem, st, m, o));                \
       }
       if (a.dtype == QLESS_F32) {

@@ -118,6 +118,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
 struct LossPlan {
     int64_t tpad;
     bool exact;                             // the softmax normaliser is known before the probabilities are formed
+    bool few;                               // roles of tokens and vocabulary swapped
     int32_t piece, entries, cap_tiles;
     size_t meta_off, order_off, place_off, label_off, weight_off, logit_off, coef_off, rowp_off, stat_off, hidden_off, piece_off, acc_off, total;
 };
