@@ -491,7 +491,7 @@ __global__ void __launch_bounds__(1024) loss_gather_kernel(const GatherArgs a)
             const uint4* wrow = reinterpret_cast<const uint4*>(a.weight + (int64_t)list_label[i] * a.ld_weight);
             uint4* dst = reinterpret_cast<uint4*>(a.out + (int64_t)e.y * a.width);
             float dot = 0.0f;
-#pragma unroll 4
+#pragma unroll 8
             for (int c = lane; c < vecs; c += 32) {
                 const uint4 x = __ldg(src + c), w = __ldg(wrow + c);
                 dst[c] = x;

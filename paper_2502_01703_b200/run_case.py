@@ -4,8 +4,9 @@
     python -m paper_2502_01703_b200.run_case quantize --n 32768 --d 8192 --bits 4
     python -m paper_2502_01703_b200.run_case score    --N 20000 --V 448 --C 4 --d 8192 --bits 8     (16: the bf16 baseline)
     python -m paper_2502_01703_b200.run_case select   --N 67108864 --frac 0.05
+    python -m paper_2502_01703_b200.run_case extract  --n 32 --tokens 16384 --width 2048 --vocab 32000 --rank 16 --d 1024 --bits 4
 
-Prints the CUDA-event time per iteration of the library call.
+Prints the CUDA-event time per iteration of the library call (extract: of each call).
 """
 import argparse
 
@@ -15,9 +16,54 @@ from . import binding as B
 from . import workloads as W
 
 
+def extract(n, tokens, width, vocab, rank, d, bits, seed=1, group=32, scaling=2.0, device="cuda"):
+    """From packed tokens to datastore rows: the last adapted layer y = W x + scaling * B (A x) of a language model (random weights)
+    feeds its head. The layer's input is kept as an 8-bit checkpoint, the loss of the second half of every example's tokens (the
+    answer; mean per example) gives the gradient at y, that and the checkpoint the example's LoRA gradient, and the gradient its
+    projected code. Returns the inputs, every intermediate result and the milliseconds of each library call."""
+    g = torch.Generator(device=device)
+    g.manual_seed(seed)
+    def rand(*shape, scale=1.0):
+        return (torch.randn(shape, generator=g, device=device) * scale).to(torch.bfloat16)
+    cuts = torch.randint(1, max(tokens, 2), (n - 1,), generator=g, device=device).sort().values.cpu()
+    offsets = torch.cat([torch.zeros(1, dtype=torch.int64), cuts, torch.tensor([tokens])])
+    x, w = rand(tokens, width), rand(width, width, scale=width ** -0.5)
+    a, b = rand(rank, width, scale=width ** -0.5), rand(width, rank, scale=0.05)
+    head = rand(vocab, width, scale=2.0 * width ** -0.5)
+    labels = torch.randint(0, vocab, (tokens,), generator=g, device=device)
+    weight = torch.zeros(tokens, device=device)
+    for e in range(n):
+        lo, hi = int(offsets[e]), int(offsets[e + 1])
+        answer = lo + (hi - lo) // 2
+        labels[lo:answer] = -100
+        weight[answer:hi] = 1.0 / max(hi - answer, 1)
+    hidden = x @ w.T + (scaling * (x @ a.T) @ b.T).to(torch.bfloat16)
+
+    ms = {}
+    def timed(name, fn):
+        start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record()
+        out = fn()
+        end.record()
+        end.synchronize()
+        ms[name] = start.elapsed_time(end)
+        return out
+    codes, scales = timed("qless_activation_quantize", lambda: B.qless_activation_quantize(x, group=group))
+    loss = timed("qless_lm_loss", lambda: B.qless_lm_loss(hidden, head, labels, token_weight=weight))
+    grads = timed("qless_lora_gradients", lambda: B.qless_lora_gradients(codes, scales, loss["grad_hidden"], a, b, offsets, scaling=scaling, group=group))
+    store = timed("qless_project_quantize", lambda: B.qless_project_quantize(grads, d, 7, bits))
+    B.qless_check()
+    return dict(offsets=offsets, x=x, a=a, b=b, head=head, labels=labels, weight=weight, hidden=hidden, scaling=scaling, group=group,
+                checkpoint=(codes, scales), loss=loss, grads=grads, store=store, ms=ms)
+
+
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("stage", choices=["project", "quantize", "score", "select"])
+    ap.add_argument("stage", choices=["project", "quantize", "score", "select", "extract"])
+    ap.add_argument("--tokens", type=int, default=16384)
+    ap.add_argument("--width", type=int, default=2048)
+    ap.add_argument("--vocab", type=int, default=32000)
+    ap.add_argument("--rank", type=int, default=16)
     ap.add_argument("--n", type=int, default=256)
     ap.add_argument("--N", type=int, default=20000)
     ap.add_argument("--V", type=int, default=448)
@@ -31,6 +77,13 @@ def main():
     ap.add_argument("--matrix", choices=["rademacher", "gaussian"], default="rademacher", help="random matrix of the projection")
     a = ap.parse_args()
     dev = "cuda"
+    if a.stage == "extract":
+        for _ in range(a.iters):
+            got = extract(a.n, a.tokens, a.width, a.vocab, a.rank, a.d, a.bits)
+        kept = int((got["labels"] >= 0).sum())
+        print(f"extract: {a.n} examples, {a.tokens} tokens ({kept} with a loss), mean loss {got['loss']['loss'].sum().item() / max(kept, 1):.4f}, "
+              f"{got['grads'].shape[1]} gradient entries each; " + ", ".join(f"{k} {v:.3f} ms" for k, v in got["ms"].items()))
+        return
     if a.stage == "project":
         matrix = B.GAUSSIAN if a.matrix == "gaussian" else B.RADEMACHER
         g = W.student_t_gradients(a.n, a.P, seed=1, device=dev, dtype=torch.bfloat16)
