@@ -17,6 +17,8 @@
 // Tokens behind the end of a chunk share its last 64-token block: their rows are overwritten with zeros in both operands (in the
 // operand alone a NaN in the neighbour example would survive as 0 * NaN).
 // Examples longer than a chunk are summed in pieces (fp32, added in piece order by lora_join_kernel): no float atomics anywhere.
+#include <cstring>
+
 #include "qless_kernels.h"
 #include "tc_common.cuh"
 
@@ -46,8 +48,10 @@ struct FactorParams {
     unsigned int* timeout_word;
 };
 
+constexpr int INLINE = 64;                  // pieces that travel in the launch itself
+
 struct OuterParams {
-    const LoraChunk* chunks;
+    const LoraChunk* chunks;                // NULL: they are in `few`
     const uint8_t* scales;
     int64_t ld_scales, ld_grads, items;
     void* grads;
@@ -56,6 +60,7 @@ struct OuterParams {
     int32_t x_whole, y_whole;               // rows of the codes / of dY are whole 128-byte blocks: one copy brings several side by side
     int32_t steps_whole;                    // step bytes of 128 channels are one aligned word
     unsigned int* timeout_word;
+    LoraChunk few[INLINE];
 };
 
 // codes1, dy1, a, b: step (1), boxes of 128 tokens (channels of the weights) by 128 bytes; codes2, dy2, fac: step (2), 64 tokens.
@@ -423,7 +428,7 @@ __device__ __forceinline__ void store_columns(OutT* dst, bool is_x, int64_t ch, 
 // OutT fixes the number of terms of a factor: 2 for bf16 gradients, 3 for fp32. BOXES: 64-column blocks that hold them.
 template <typename OutT, int BOXES>
 __global__ void __launch_bounds__(NTHREADS, 1)
-lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
+lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__ OuterParams p)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -452,7 +457,10 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const OuterParams p)
     const uint32_t tmem = bars->tmem_base;                  // accumulator of item n, sub-tile m: column (n & 1) * 256 + m * 128
 
     const uint32_t items = (uint32_t)p.items, step_items = gridDim.x;
-    auto chunk_of = [&](uint32_t item) { return p.chunks[min(item, items - 1) / (uint32_t)p.tiles]; };
+    auto chunk_of = [&](uint32_t item) {
+        const uint32_t k = min(item, items - 1) / (uint32_t)p.tiles;
+        return p.chunks != nullptr ? p.chunks[k] : p.few[k];
+    };
     auto place_of = [&](uint32_t item, bool& is_x, int& ch0) {
         const int tile = (int)(item % (uint32_t)p.tiles);
         is_x = tile < p.tiles_x;
@@ -768,7 +776,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
 {
     LoraChunk* d_chunks = reinterpret_cast<LoraChunk*>(ws + pl.chunk_off);
     LoraJoin* d_joins = reinterpret_cast<LoraJoin*>(ws + pl.join_off);
-    QLESS_CUDA_TRY(upload(a.chunks, (size_t)a.num_chunks * sizeof(LoraChunk), d_chunks, st));
+    if (a.num_chunks > INLINE) QLESS_CUDA_TRY(upload(a.chunks, (size_t)a.num_chunks * sizeof(LoraChunk), d_chunks, st));
     if (a.num_joins > 0) QLESS_CUDA_TRY(upload(a.joins, (size_t)a.num_joins * sizeof(LoraJoin), d_joins, st));
     __nv_bfloat16* fac = reinterpret_cast<__nv_bfloat16*>(ws + pl.fac_off);
     const size_t budget = 227 * 1024 - 1024 - sizeof(Bars) - 64;
@@ -821,7 +829,8 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
         count_launches(1);
     }
     OuterParams o;
-    o.chunks = d_chunks; o.scales = a.scales; o.ld_scales = a.ld_scales; o.ld_grads = a.ld_grads;
+    o.chunks = a.num_chunks > INLINE ? d_chunks : nullptr;
+    if (o.chunks == nullptr) memcpy(o.few, a.chunks, (size_t)a.num_chunks * sizeof(LoraChunk)); o.scales = a.scales; o.ld_scales = a.ld_scales; o.ld_grads = a.ld_grads;
     o.grads = a.grads; o.part = reinterpret_cast<float*>(ws + pl.part_off);
     o.in = a.in; o.out = a.out; o.rank = a.rank; o.group = a.group; o.nr = pl.nr;
     o.tiles_x = pl.tiles_x; o.tiles = pl.tiles; o.timeout_word = timeout_word;
