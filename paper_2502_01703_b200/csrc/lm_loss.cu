@@ -589,42 +589,52 @@ struct RowArgs {
     float* loss;
 };
 
-// 32 rows per block, 32 threads per row that take every 32nd stretch; joined in a fixed order.
+// Eight rows per block, 128 threads per row that take every 128th stretch: the partial results of a row lie tpad apart, so it is
+// the number of loads in flight that counts. Joined in a fixed order.
+constexpr int ROWS = 8;
 __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowArgs a)
 {
     ahead_release();
     ahead_wait();
     if (a.gate != nullptr && *a.gate == 0) return;
-    __shared__ float2 part[32][32];
-    const int lane = threadIdx.x & 31, seg = threadIdx.x >> 5;
+    __shared__ float2 part[32][ROWS];
+    const int r = threadIdx.x & (ROWS - 1), seg = threadIdx.x / ROWS, warp = threadIdx.x >> 5;
     const int count = a.meta->count;
-    for (int64_t r0 = (int64_t)blockIdx.x * 32; r0 < count; r0 += (int64_t)gridDim.x * 32) {
-        const int64_t row = r0 + lane;
+    // (m, s) stands for s * 2^m; plain sums have m = 0
+    auto join = [](float& m, float& s, float m2, float s2) {
+        const float now = fmaxf(m, m2);
+        if (now > -INFINITY) { s = s * ex2(m - now) + s2 * ex2(m2 - now); m = now; }
+        else s += s2;                                        // 0, or NaN
+    };
+    for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < count; r0 += (int64_t)gridDim.x * ROWS) {
+        const int64_t row = r0 + r;
         float m = -INFINITY, s = 0.0f;
         if (row < count) {
             if (a.kind == ROW_FROM_SUMS) {
 #pragma unroll 4
-                for (int i = seg; i < a.entries; i += 32) s += a.psum[(int64_t)i * a.tpad + row];
+                for (int i = seg; i < a.entries; i += 1024 / ROWS) s += a.psum[(int64_t)i * a.tpad + row];
             } else {
 #pragma unroll 4
-                for (int i = seg; i < a.entries; i += 32) {
+                for (int i = seg; i < a.entries; i += 1024 / ROWS) {
                     const float2 x = a.stat[(int64_t)i * a.tpad + row];
-                    const float now = fmaxf(m, x.x);
-                    if (now > -INFINITY) { s = s * ex2(m - now) + x.y * ex2(x.x - now); m = now; }
-                    else s += x.y;                               // 0, or NaN
+                    join(m, s, x.x, x.y);
                 }
             }
         }
+#pragma unroll
+        for (int o = ROWS; o < 32; o <<= 1) {
+            const float m2 = __shfl_xor_sync(0xFFFFFFFFu, m, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, s, o);
+            if (a.kind == ROW_FROM_SUMS) s += s2;
+            else join(m, s, m2, s2);
+        }
         __syncthreads();
-        part[seg][lane] = make_float2(m, s);
+        if ((threadIdx.x & 31) < ROWS) part[warp][r] = make_float2(m, s);
         __syncthreads();
         if (seg == 0 && row < count) {
             for (int j = 1; j < 32; ++j) {
-                const float2 x = part[j][lane];
-                if (a.kind == ROW_FROM_SUMS) { s += x.y; continue; }
-                const float now = fmaxf(m, x.x);
-                if (now > -INFINITY) { s = s * ex2(m - now) + x.y * ex2(x.x - now); m = now; }
-                else s += x.y;
+                const float2 x = part[j][r];
+                if (a.kind == ROW_FROM_SUMS) s += x.y;
+                else join(m, s, x.x, x.y);
             }
             if (a.kind == ROW_REFERENCE) {
                 a.rowp[row] = RowParam{m > -INFINITY ? m : 0.0f, 1.0f, 0.0f, 0.0f};
@@ -808,7 +818,7 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
         r.meta = meta; r.gate = gate; r.kind = kind; r.entries = entries; r.tpad = pl.tpad; r.stat = stat; r.psum = psum; r.label_logit = logit;
         r.weight = weight; r.order = order; r.rowp = rowp; r.coef = coef; r.loss = a.loss; r.apart = want_h && !want_w;
         { ProfileScope ps("loss_rows", st);
-          QLESS_CUDA_TRY(launch_ahead(loss_rows_kernel, dim3(grid_of(a.T, 32)), dim3(1024), 0, st, r)); }
+          QLESS_CUDA_TRY(launch_ahead(loss_rows_kernel, dim3(grid_of(a.T, ROWS)), dim3(1024), 0, st, r)); }
         count_launches(1);
         return QLESS_OK;
     };
