@@ -222,7 +222,10 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                 if (!warp_wait(&bars->d_empty[buf], ((n_acc >> 1) & 1u) ^ 1u, TO_MMA)) { ok = false; break; }
                 tc_fence_after();
                 for (int kb = kb0; kb < kb1; ++kb, ring.next(nS)) {
-                    if (!warp_wait(&bars->full[ring.slot], ring.parity, TO_MMA)) { ok = false; break; }
+                    // (an own barrier that only copies arrive on: no cluster-scope acquire)
+                    bool landed = mbar_wait(smem_u32(&bars->full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_MMA);
+                    landed = __all_sync(0xFFFFFFFFu, landed);
+                    if (!landed) { ok = false; break; }
                     tc_fence_after();
                     if (elect_one()) {
                     const uint32_t a = smem_u32(smem + (size_t)ring.slot * stage_bytes), b = a + HALF;

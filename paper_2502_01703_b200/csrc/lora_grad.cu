@@ -259,7 +259,7 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
             mbar_wait_quiet(smem_u32(&bars->drain), 0u);
         }
     } else if (warp < 18) {
-        // Converters: thread = token = TMEM lane; a group of four warps to each stage (there are two or four), so that the barrier round
+        // Converters: thread = token = TMEM lane; a group of four warps to each stage (there are two to four), so that the barrier round
         // trips and latencies of one block overlap the work on the others. Every block passes through them, those of dY untouched: the
         // phase of a stage's barrier that its group waits for is always the one behind the phase it saw last.
         const int row = (warp & 3) * 32 + lane;
@@ -435,8 +435,9 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
     constexpr int PARTS = sizeof(OutT) == 4 ? 3 : 2;
     // Where all terms together have at most 128 columns they are one operand (their sums meet in the epilogue): the channel operand is
     // read from shared memory once for all of them, whose bandwidth bounds this loop. Otherwise one product per term into the same accumulator.
-    constexpr bool WIDE = BOXES <= 2;
-    constexpr int TERM_BYTES = BOXES / PARTS * 8192;         // (not WIDE) a term's boxes
+    // Three terms of 64 columns: the first two side by side, the third into the first's columns.
+    constexpr bool WIDE = BOXES <= 3;
+    constexpr int TERM_BYTES = BOXES / PARTS * 8192;         // a term's boxes, where it has boxes of its own
     constexpr int boxes = BOXES;                             // factor operand: boxes of 64 columns x 64 tokens
     constexpr int stage_bytes = BIG + boxes * 8192;
     Bars* bars = reinterpret_cast<Bars*>(smem + (size_t)p.stages * stage_bytes);
@@ -507,8 +508,9 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
         }
     } else if (warp == 1) {
         {
-            const uint32_t idesc = make_idesc(1, 1, 1, 128, WIDE ? PARTS * p.nr : p.nr) | IDESC_A_MN | IDESC_B_MN;
-            constexpr int TERMS = WIDE ? 1 : PARTS;
+            const uint32_t idesc = make_idesc(1, 1, 1, 128, BOXES == 3 ? 64 + p.nr : WIDE ? PARTS * p.nr : p.nr) | IDESC_A_MN | IDESC_B_MN;
+            const uint32_t idesc_third = make_idesc(1, 1, 1, 128, p.nr) | IDESC_A_MN | IDESC_B_MN;
+            constexpr int TERMS = BOXES == 3 ? 2 : WIDE ? 1 : PARTS;
             Ring ring;
             uint32_t n = 0;
             bool ok = true;
@@ -535,7 +537,8 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
 #pragma unroll
                         for (int i = 1; i < TOK / 16 * TERMS; ++i) {
                             const int k = i / TERMS, q = i % TERMS;
-                            mma_f16_ss(d, am + (uint64_t)(k * 128), b0 + (uint64_t)(k * 128 + q * (TERM_BYTES / 16)), idesc, 1u);
+                            if (BOXES == 3 && q == 1) mma_f16_ss(d, am + (uint64_t)(k * 128), b0 + (uint64_t)(k * 128 + 2 * (TERM_BYTES / 16)), idesc_third, 1u);
+                            else mma_f16_ss(d, am + (uint64_t)(k * 128), b0 + (uint64_t)(k * 128 + q * (TERM_BYTES / 16)), idesc, 1u);
                         }
                     }
                     mma_commit(smem_u32(&bars->empty[ring.slot]));
@@ -663,9 +666,9 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
                     tmem_wait_ld();
                     if (WIDE) {
 #pragma unroll
-                        for (int q = 1; q < PARTS; ++q) {
+                        for (int q = 1; q < (BOXES == 3 ? 2 : PARTS); ++q) {
                             uint32_t low[16];
-                            tmem_ld_x16(taddr + q * p.nr, low);
+                            tmem_ld_x16(taddr + (BOXES == 3 ? 64 : q * p.nr), low);
                             tmem_wait_ld();
 #pragma unroll
                             for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(low[j]));
@@ -812,7 +815,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
         f.y_whole = y_whole; f.steps_whole = steps_whole;
         f.timeout_word = timeout_word;
         const size_t stage = BIG + (size_t)pl.n64 * 256;
-        f.stages = (int32_t)(budget / stage < MAX_STAGES ? budget / stage : MAX_STAGES) & ~1;
+        f.stages = (int32_t)(budget / stage < MAX_STAGES ? budget / stage : MAX_STAGES);
         const size_t smem = 1024 + f.stages * stage + sizeof(Bars);
         const int64_t grid = f.items < sm_count() ? f.items : sm_count();
         { ProfileScope ps("lora_factors", st);
@@ -838,7 +841,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
     o.items = (int64_t)a.num_chunks * pl.tiles;
     QLESS_REQUIRE(o.items < ((int64_t)1 << 31) - 65536, QLESS_ERR_UNSUPPORTED, "too many examples: %lld pieces of %d tiles", (long long)a.num_chunks, pl.tiles);
     const size_t stage = BIG + (size_t)boxes * 8192;
-    o.stages = (int32_t)(budget / stage < MAX_STAGES ? budget / stage : MAX_STAGES) & ~1;
+    o.stages = (int32_t)(budget / stage < MAX_STAGES ? budget / stage : MAX_STAGES);
     const size_t smem = 1024 + o.stages * stage + sizeof(Bars);
     const int64_t grid = o.items < sm_count() ? o.items : sm_count();
     { ProfileScope ps("lora_outer", st);
