@@ -95,6 +95,29 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
     return *reinterpret_cast<const uint32_t*>(&z);
 }
 
+// Four neighbouring lanes hold four 16-byte pieces each of a row of their own; afterwards lane i of the four holds piece i of each of the
+// four rows: a store instruction then covers 64 consecutive bytes of eight rows instead of 16 of thirty-two (GRAD_W of 23 tokens x
+// 3424 x 65225, whose time is its stores).
+__device__ __forceinline__ void transpose4(uint4 (&v)[4], int lane)
+{
+    auto swap = [](uint4 a, int m) {
+        a.x = __shfl_xor_sync(0xFFFFFFFFu, a.x, m); a.y = __shfl_xor_sync(0xFFFFFFFFu, a.y, m);
+        a.z = __shfl_xor_sync(0xFFFFFFFFu, a.z, m); a.w = __shfl_xor_sync(0xFFFFFFFFu, a.w, m);
+        return a;
+    };
+#pragma unroll
+    for (int m = 1; m <= 2; m <<= 1) {
+        const bool up = (lane & m) != 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (k & m) continue;
+            const uint4 got = swap(up ? v[k] : v[k + m], m);
+            if (up) v[k] = got;
+            else v[k + m] = got;
+        }
+    }
+}
+
 // Sum (or maximum) over the 32 lanes of each of 32 values: lane L ends with that of value L, after 31 shuffles.
 template <bool MAX>
 __device__ __forceinline__ float across_lanes(float (&v)[32], int lane)
@@ -234,9 +257,10 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                     const uint64_t a0 = A_MN ? make_smem_desc_mn_sw128(a, 16384) : make_smem_desc_sw128(a);
                     const uint64_t b0 = B_MN ? make_smem_desc_mn_sw128(b, 16384) : make_smem_desc_sw128(b);
                     mma_f16_ss_pair(d, a0, b0, idesc, kb > kb0);
+                    const int steps = MODE == GRAD_W ? min(KB / 16, (count - kb * KB + 15) / 16) : KB / 16;      // rows behind are not cleared
 #pragma unroll
                     for (int k = 1; k < KB / 16; ++k)
-                        mma_f16_ss_pair(d, a0 + (uint64_t)(A_MN ? k * 128 : (k >> 2) * 1024 + (k & 3) * 2), b0 + (B_MN ? (uint64_t)(k * 128) : (k >> 2) * b_next + (uint64_t)((k & 3) * 2)), idesc, 1u);
+                        if (MODE != GRAD_W || k < steps) mma_f16_ss_pair(d, a0 + (uint64_t)(A_MN ? k * 128 : (k >> 2) * 1024 + (k & 3) * 2), b0 + (B_MN ? (uint64_t)(k * 128) : (k >> 2) * b_next + (uint64_t)((k & 3) * 2)), idesc, 1u);
                     mma_commit_pair(smem_u32(&bars->empty[ring.slot]));
                     }
                     __syncwarp();
@@ -265,13 +289,14 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
             const int v = m * 256 + (int)rank * 128 + q * 32 + lane;
             const uint32_t buf = n_acc & 1u;
             const int lim = min(count - half * p.b_rows, p.b_rows);      // tokens of this half
+            const int upto = MODE == PROBS ? min(((count + 15) & ~15) - half * p.b_rows, p.b_rows) : lim;      // (b_rows is a multiple of 16)
             bool ok = mbar_wait_cluster(smem_u32(&bars->d_full[buf]), (n_acc >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
             tc_fence_after();
             float run_max = -INFINITY;
 #pragma unroll 1
-            for (int c0 = 0; c0 < lim; c0 += 32) {
+            for (int c0 = 0; c0 < upto; c0 += 32) {
                 uint32_t raw[32];
                 tmem_ld_x32(tmem + lane_base + buf * 256 + half * p.b_rows + c0, raw);
                 tmem_wait_ld();
@@ -315,7 +340,11 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                             run_max = fmaxf(run_max, x);
                             e[k] = ex2(x);
                             dst[(int64_t)k * p.ld_out] = __float2bfloat16_rn(own ? rp.wl : e[k] * rp.w);
-                        } else e[k] = 0.0f;
+                        } else {
+                            e[k] = 0.0f;
+                            // GRAD_W contracts over steps of 16 tokens
+                            if (c0 + k < upto) dst[(int64_t)k * p.ld_out] = __float2bfloat16_rn(0.0f);
+                        }
                     }
                     if (p.psum != nullptr) {
                         const float sum = across_lanes<false>(e, lane);
@@ -404,40 +433,54 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
 #pragma unroll
                             for (int k = 0; k < 32; ++k) e[k] = 0.0f;
                         }
-                        uint4* dst = reinterpret_cast<uint4*>(p.out + row * p.ld_out + c_lo + c0);
+                        uint4 w[4];
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            dst[k] = make_uint4(pack_bf16(e[8 * k], e[8 * k + 1]), pack_bf16(e[8 * k + 2], e[8 * k + 3]),
-                                                pack_bf16(e[8 * k + 4], e[8 * k + 5]), pack_bf16(e[8 * k + 6], e[8 * k + 7]));
+                            w[k] = make_uint4(pack_bf16(e[8 * k], e[8 * k + 1]), pack_bf16(e[8 * k + 2], e[8 * k + 3]),
+                                              pack_bf16(e[8 * k + 4], e[8 * k + 5]), pack_bf16(e[8 * k + 6], e[8 * k + 7]));
+                        transpose4(w, lane);
+                        __nv_bfloat16* dst = p.out + (row - (lane & 3)) * p.ld_out + c_lo + c0 + (lane & 3) * 8;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(dst + k * p.ld_out) = w[k];
                     }
                 } else if (MODE == GRAD_H) {
-                    if (row < count) {
-                        float* dst = p.acc + ((int64_t)split * mt * 256 + row) * p.cols + c_lo + c0;
+                    float* base = p.acc + ((int64_t)split * mt * 256 + row - (lane & 3)) * p.cols + c_lo + c0 + (lane & 3) * 4;
 #pragma unroll
-                        for (int k = 0; k < 32; k += 4) {
-                            if (k >= have) break;                // the width is a multiple of 8
-                            float4 x = make_float4(__uint_as_float(v[k]), __uint_as_float(v[k + 1]), __uint_as_float(v[k + 2]), __uint_as_float(v[k + 3]));
-                            if (kb0 == kb1) x = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int h = 0; h < 2; ++h) {                // 16 columns at a time
+                        uint4 w[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            w[k] = kb0 == kb1 ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(v[16 * h + 4 * k], v[16 * h + 4 * k + 1], v[16 * h + 4 * k + 2], v[16 * h + 4 * k + 3]);
+                        transpose4(w, lane);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            // the width is a multiple of 8; rows up to the tile's 256 have room
+                            if (16 * h + (lane & 3) * 4 >= have || row - (lane & 3) + k >= count) continue;
+                            float4* dst = reinterpret_cast<float4*>(base + (int64_t)k * p.cols + 16 * h);
+                            float4 x = make_float4(__uint_as_float(w[k].x), __uint_as_float(w[k].y), __uint_as_float(w[k].z), __uint_as_float(w[k].w));
                             if (p.accumulate) {
-                                const float4 y = *reinterpret_cast<const float4*>(dst + k);
+                                const float4 y = *dst;
                                 x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
                             }
-                            *reinterpret_cast<float4*>(dst + k) = x;
+                            *dst = x;
                         }
                     }
                 } else {
-                    if (row < p.rows) {
-                        __nv_bfloat16* dst = p.out + (p.col0 + row) * p.ld_out + c_lo + c0;
-                        const bool none = kb0 == kb1;            // no token carries a loss
+                    const bool none = kb0 == kb1;                // no token carries a loss
+                    uint4 w[4];
 #pragma unroll
-                        for (int k = 0; k < 32; k += 8) {
-                            if (k >= have) break;
-                            uint4 o = make_uint4(pack_bf16(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), pack_bf16(__uint_as_float(v[k + 2]), __uint_as_float(v[k + 3])),
-                                                 pack_bf16(__uint_as_float(v[k + 4]), __uint_as_float(v[k + 5])), pack_bf16(__uint_as_float(v[k + 6]), __uint_as_float(v[k + 7])));
-                            if (none) o = make_uint4(0u, 0u, 0u, 0u);
-                            *reinterpret_cast<uint4*>(dst + k) = o;
-                        }
+                    for (int k = 0; k < 4; ++k) {
+                        const int c = 8 * k;
+                        w[k] = make_uint4(pack_bf16(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), pack_bf16(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])),
+                                          pack_bf16(__uint_as_float(v[c + 4]), __uint_as_float(v[c + 5])), pack_bf16(__uint_as_float(v[c + 6]), __uint_as_float(v[c + 7])));
+                        if (none) w[k] = make_uint4(0u, 0u, 0u, 0u);
                     }
+                    transpose4(w, lane);
+                    const int64_t first = row - (lane & 3);
+                    __nv_bfloat16* dst = p.out + (p.col0 + first) * p.ld_out + c_lo + c0 + (lane & 3) * 8;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if ((lane & 3) * 8 < have && first + k < p.rows) *reinterpret_cast<uint4*>(dst + k * p.ld_out) = w[k];
                 }
             }
             if (MODE == STATS && row < count) p.stat[((int64_t)(p.tile0 + n) * 2 + half) * p.tpad + row] = make_float2(run_max, run_sum);
@@ -456,17 +499,17 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
 // ---- tokens that carry a loss ------------------------------------------------------------------------------------------
 
 // place[t] = position of token t among the tokens with a label in [0, V), or -1; order = the inverse. Every block scans all labels (they
-// are few against the rows) and lists the tokens whose rows fall to it; then its warps copy a row each and take the dot product with the
-// label's row of W on the way. Rows land in `out` in order, zeros behind the last up to a multiple of 128 (GRAD_W contracts over the rows).
+// are few against the rows) and lists the tokens whose rows fall to it; then its warps copy a row each (or share the rows where there are few) and take the dot
+// product with the label's row of W on the way. Rows land in `out` in order, zeros behind the last up to a multiple of 128 (GRAD_W contracts over the rows).
 // Also how many slices the hidden-state product is cut into along the vocabulary: the fewest that keep 95 % of the CTA pairs busy, or
-// the best of up to four (16 where the tiles do not fill one round), within the `cap_tiles` row tiles the workspace has room for.
+// the best of up to four (any number where the tiles do not fill one round), within the `cap_tiles` row tiles the workspace has room for.
 struct GatherArgs {
     const int64_t* labels;
     const float* token_weight;
     const __nv_bfloat16* hidden;
     const __nv_bfloat16* weight;
     int64_t T, ld_hidden, ld_weight;
-    int32_t V, width, pairs, col_tiles, cap_tiles;
+    int32_t V, width, pairs, col_tiles, cap_tiles, most_slices;
     int32_t* order; int32_t* place; int32_t* out_labels;
     float* out_weight; float* label_logit; float* loss;
     RowParam* rowp;
@@ -481,21 +524,29 @@ __global__ void __launch_bounds__(1024) loss_gather_kernel(const GatherArgs a)
     __shared__ int32_t warp_sum[2][32];
     __shared__ int2 list[LIST];                                  // token, place
     __shared__ int32_t list_label[LIST];
+    __shared__ float dots[32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, vecs = a.width / 8;
     const int32_t grid = (int32_t)gridDim.x, me = (int32_t)blockIdx.x;
+    auto put_logit = [&](int32_t at, float dot) {
+        const float l2 = dot * LOG2E;
+        a.label_logit[at] = l2;
+        a.rowp[at] = RowParam{l2, 1.0f, 0.0f, 0.0f};
+    };
     ahead_release();
     ahead_wait();
     int32_t base = 0, listed = 0;                                // tokens kept so far, and how many of them fell to this block since the last flush
     auto flush = [&]() {                                         // whole block
         __syncthreads();
-        for (int i = warp; i < listed; i += 32) {
+        int share = 1;                                           // warps to a row: all of them where there are few rows
+        while (share * 2 * listed <= 32 && share < 32) share *= 2;
+        for (int i = warp / share; i < listed; i += 32 / share) {
             const int2 e = list[i];
             const uint4* src = reinterpret_cast<const uint4*>(a.hidden + (int64_t)e.x * a.ld_hidden);
             const uint4* wrow = reinterpret_cast<const uint4*>(a.weight + (int64_t)list_label[i] * a.ld_weight);
             uint4* dst = reinterpret_cast<uint4*>(a.out + (int64_t)e.y * a.width);
             float dot = 0.0f;
-#pragma unroll 8
-            for (int c = lane; c < vecs; c += 32) {
+#pragma unroll 4
+            for (int c = lane + 32 * (warp % share); c < vecs; c += 32 * share) {
                 const uint4 x = __ldg(src + c), w = __ldg(wrow + c);
                 dst[c] = x;
                 const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ws[4] = {w.x, w.y, w.z, w.w};
@@ -507,11 +558,14 @@ __global__ void __launch_bounds__(1024) loss_gather_kernel(const GatherArgs a)
             }
 #pragma unroll
             for (int s = 16; s > 0; s >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, s);
-            if (lane == 0) {
-                const float l2 = dot * LOG2E;
-                a.label_logit[e.y] = l2;
-                a.rowp[e.y] = RowParam{l2, 1.0f, 0.0f, 0.0f};
-            }
+            if (share == 1 && lane == 0) put_logit(e.y, dot);
+            if (share > 1 && lane == 0) dots[warp] = dot;
+        }
+        __syncthreads();
+        if (share > 1 && (int)threadIdx.x < listed) {            // at most 16 rows, one pass: the warps' shares in order
+            float dot = 0.0f;
+            for (int w = 0; w < share; ++w) dot += dots[threadIdx.x * share + w];
+            put_logit(list[threadIdx.x].y, dot);
         }
         __syncthreads();
         listed = 0;
@@ -560,7 +614,7 @@ __global__ void __launch_bounds__(1024) loss_gather_kernel(const GatherArgs a)
         const int mt = (base + 255) / 256, tiles = mt * a.col_tiles;
         int best = 1;
         if (mt > 0) {
-            const int pairs = a.pairs, most = min(a.cap_tiles / mt, tiles >= pairs ? 4 : 16);
+            const int pairs = a.pairs, most = min(min(a.cap_tiles / mt, a.most_slices), tiles >= pairs ? 4 : pairs);
             float best_use = 0.0f;
             for (int s = 1; s <= most && best_use < 0.95f; ++s) {
                 const int items = tiles * s, rounds = (items + pairs - 1) / pairs;
@@ -580,7 +634,6 @@ struct RowArgs {
     const LossMeta* meta;
     const int32_t* gate;
     int32_t kind, entries;                  // entries: stretches of columns with a partial result
-    int32_t apart;                          // ROW_FROM_STATS: the hidden states' gradient alone is wanted
     int64_t tpad;
     const float2* stat;
     const float* psum;
@@ -588,7 +641,7 @@ struct RowArgs {
     const float* weight;
     const int32_t* order;
     RowParam* rowp;
-    float2* coef;                           // w sigma(d), and what the sum over the other columns is multiplied by
+    float2* coef;                           // ROW_FROM_SUMS: w sigma(d), 1 / s
     float* loss;
 };
 
@@ -655,10 +708,7 @@ __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowArgs a)
             else if (d != d) { nll = d; sigma = d; }
             a.loss[a.order[row]] = nll;
             if (a.kind == ROW_FROM_SUMS) a.coef[row] = make_float2(w * sigma, s == 0.0f ? 0.0f : 1.0f / s);
-            else if (a.apart) {                                  // probabilities among the other columns; the label's row joins at the end
-                a.rowp[row] = RowParam{s == 0.0f ? 0.0f : others, 1.0f, 0.0f, 0.0f};
-                a.coef[row] = make_float2(w * sigma, 1.0f);
-            } else a.rowp[row] = RowParam{fmaxf(others, ly) + tail * LOG2E, w, -w * sigma, 0.0f};      // the full normaliser
+            else a.rowp[row] = RowParam{fmaxf(others, ly) + tail * LOG2E, w, -w * sigma, 0.0f};      // the full normaliser
         }
     }
 }
@@ -733,18 +783,20 @@ LossPlan plan_loss(int64_t T, int32_t width, int32_t vocab, bool want_h, bool wa
     pl.tpad = (T + 255) / 256 * 256;
     const int64_t mt = pl.tpad / 256, pairs = sm_count() / 2, nt_h = (width + 255) / 256;
     const int64_t tiles_v = ((int64_t)vocab + 255) / 256;
-    // The normaliser first (one more product), or a reference that may have to be redone (a few more launches): with the gradient of the
-    // weights always the former; otherwise where that product takes less than the launches (about 12 us: 5.5 TB/s, 1.2 PFLOP/s).
-    const double product_us = 2.0 * vocab * width / 5.5e6, flop_us = 2.0 * pl.tpad * (double)vocab * width / 1.2e9;
-    pl.exact = !want_h || want_w || (product_us > flop_us ? product_us : flop_us) < 12.0;
+    // The normaliser first (one more product): for the loss alone, and with the gradient of the weights. For the gradient of the hidden
+    // states a reference that may have to be redone is never slower, the smallest problems included (28 tokens x 1720 x 1079: 38 us
+    // against 43 us with the product first, 33 x 512 x 4099: 36.7 against 36.0 us, 88 x 4040 x 2783: 57 against 73 us).
+    pl.exact = !want_h || want_w;
     // Piece of the vocabulary whose probabilities are held at once: at most 512 MiB of bf16.
     int64_t piece_tiles = ((int64_t)512 << 20) / (pl.tpad * 256 * 2);
     if (piece_tiles < 1) piece_tiles = 1;
     if (piece_tiles > tiles_v) piece_tiles = tiles_v;
     pl.piece = (int32_t)(piece_tiles * 256);
-    pl.few = T <= FEW && !want_w;
+    pl.few = T <= FEW;
     pl.entries = (int32_t)((pl.few ? 8 : 2) * tiles_v);         // partial statistics: one per warp of 32 rows of W, or per 128 columns
-    int64_t cap = 16;                                           // slices where there is one row tile
+    // Slices where there is one row tile: as many as fill the pairs, in at most 64 MiB of sums.
+    int64_t cap = ((int64_t)64 << 20) / (256 * 4 * (int64_t)width);
+    cap = cap < 1 ? 1 : cap > pairs ? pairs : cap;
     if (cap < 3 * mt) cap = 3 * mt;
     pl.cap_tiles = (int32_t)cap;
     size_t off = 0;
@@ -786,12 +838,15 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
 
     { ProfileScope ps("loss_gather", st);
       // a block lists at most LIST of the 1024 tokens of a step: at least four blocks
-      int64_t blocks = (a.T + 7) / 8 < sm_count() ? (a.T + 7) / 8 : sm_count();
+      int64_t blocks = a.T < sm_count() ? a.T : sm_count();
       if (blocks < 4) blocks = 4;
       GatherArgs g{};
       g.labels = a.labels; g.token_weight = a.token_weight; g.hidden = reinterpret_cast<const __nv_bfloat16*>(a.hidden);
       g.weight = reinterpret_cast<const __nv_bfloat16*>(a.weight); g.T = a.T; g.ld_hidden = a.ld_hidden; g.ld_weight = a.ld_weight; g.V = a.vocab;
-      g.width = a.width; g.pairs = sm_count() / 2; g.col_tiles = (int32_t)nt_h; g.cap_tiles = pl.cap_tiles; g.order = order; g.place = place;
+      g.width = a.width; g.pairs = sm_count() / 2; g.col_tiles = (int32_t)nt_h; g.cap_tiles = pl.cap_tiles;
+      // a slice has at least three blocks of K
+      const int32_t kb = ((a.vocab < pl.piece ? a.vocab : pl.piece) + KB - 1) / KB;
+      g.most_slices = kb / 3 > 1 ? kb / 3 : 1; g.order = order; g.place = place;
       g.out_labels = labels; g.out_weight = weight; g.label_logit = logit; g.loss = a.loss; g.rowp = rowp; g.out = hidden; g.meta = meta;
       QLESS_CUDA_TRY(launch_ahead(loss_gather_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, g)); }
     count_launches(1);
@@ -805,6 +860,12 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
                    : make_tmap_2d_sw128(&tm_x, hidden, 2, a.width, pl.tpad, (uint64_t)a.width * 2, 64, b_rows)) != QLESS_OK) return s;
     if ((s = whole ? make_tmap_blocks_sw128(&tm_w, a.weight, 2, a.width / 64, a.vocab, (uint64_t)a.ld_weight * 2, 128, 128, 2)
                    : make_tmap_2d_sw128(&tm_w, a.weight, 2, a.width, a.vocab, (uint64_t)a.ld_weight * 2, 64, 128)) != QLESS_OK) return s;
+    CUtensorMap tm_xg, tm_pg;                                    // GRAD_W: boxes of 128 tokens whatever their number
+    if (want_w) {
+        if ((s = whole ? make_tmap_blocks_sw128(&tm_xg, hidden, 2, a.width / 64, pl.tpad, (uint64_t)a.width * 2, 128, 128, 2)
+                       : make_tmap_2d_sw128(&tm_xg, hidden, 2, a.width, pl.tpad, (uint64_t)a.width * 2, 64, 128)) != QLESS_OK) return s;
+        if ((s = make_tmap_blocks_sw128(&tm_pg, piece, 2, pl.piece / 64, pl.tpad, (uint64_t)pl.piece * 2, 128, 128, 2)) != QLESS_OK) return s;
+    }
     if (want_h || want_w)
         if ((s = make_tmap_blocks_sw128(&tm_p, piece, 2, pl.piece / 64, pl.tpad, (uint64_t)pl.piece * 2, 128, b_rows, 2)) != QLESS_OK) return s;
 
@@ -819,7 +880,7 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
     auto rows = [&](int kind, int32_t entries, const int32_t* gate) -> qless_status {
         RowArgs r{};
         r.meta = meta; r.gate = gate; r.kind = kind; r.entries = entries; r.tpad = pl.tpad; r.stat = stat; r.psum = psum; r.label_logit = logit;
-        r.weight = weight; r.order = order; r.rowp = rowp; r.coef = coef; r.loss = a.loss; r.apart = want_h && !want_w;
+        r.weight = weight; r.order = order; r.rowp = rowp; r.coef = coef; r.loss = a.loss;
         { ProfileScope ps("loss_rows", st);
           QLESS_CUDA_TRY(launch_ahead(loss_rows_kernel, dim3(grid_of(a.T, ROWS)), dim3(1024), 0, st, r)); }
         count_launches(1);
@@ -845,7 +906,7 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
             if (want_w) {
                 GemmParams g = base;
                 g.gate = gate; g.cols = a.width; g.rows = cols; g.col0 = v0; g.out = reinterpret_cast<__nv_bfloat16*>(a.grad_weight); g.ld_out = a.ld_grad_weight; g.a_whole = 1; g.b_whole = whole;
-                e = launch_gemm<GRAD_W, false>("loss_grad_weight", tm_p, tm_x, g, (int64_t)((cols + 255) / 256) * nt_h, st);
+                e = launch_gemm<GRAD_W, false>("loss_grad_weight", tm_pg, tm_xg, g, (int64_t)((cols + 255) / 256) * nt_h, st);
                 if (e != QLESS_OK) return e;
             }
         }
@@ -855,7 +916,7 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
     if (pl.exact) {
         if ((s = stats(a.vocab, nullptr)) != QLESS_OK) return s;
         if ((s = rows(ROW_FROM_STATS, pl.entries, nullptr)) != QLESS_OK) return s;
-        if ((want_h || want_w) && (s = pieces(false, nullptr)) != QLESS_OK) return s;
+        if (want_w && (s = pieces(false, nullptr)) != QLESS_OK) return s;
     } else {
         if ((s = pieces(true, nullptr)) != QLESS_OK) return s;
         if ((s = stats(a.vocab, &meta->redo)) != QLESS_OK) return s;

@@ -84,7 +84,7 @@ def test_loss_and_gradients(T, width, vocab, keep, wants):
 
 @pytest.mark.parametrize("T,width,vocab,keep", [(5, 2048, 40_000, 1.0), (300, 1024, 40_001, 0.8), (1300, 1024, 9000, 0.9)])
 def test_gradient_of_the_hidden_states_in_two_products(T, width, vocab, keep):
-    # large enough that the normaliser is not computed first
+    # more columns than one round of tiles, in both orientations of the products (up to 256 tokens the vocabulary's rows are the tile's)
     case = _case(T, width, vocab, 31, keep, spread=0.02)
     got = B.qless_lm_loss(*case)
     B.qless_check()
