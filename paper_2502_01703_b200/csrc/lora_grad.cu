@@ -5,7 +5,9 @@
 //     dA_e = U_e^T x^_e  [r, in],   dB_e = dY_e^T H_e  [out, r]          (2) outer products: sums over the tokens of example e
 //   row e of the gradient matrix = [dA_e row-major | dB_e row-major].
 //
-// Both steps read x^ and dY once and do 2 r multiply-adds per element read: memory-bound work on the tensor cores.
+// Both steps read x^ and dY once and do 2 r multiply-adds per element read: memory-bound work on the tensor cores. Measured, 128 examples of 65 536
+// tokens in all, 4096 -> 4096, rank 64, bf16 gradients: (1) 157 us, 5.1 TB/s of codes and dY; (2) 213 us, 3.8 TB/s and 134 MB of rows. In (2) stores,
+// expansion and products each cost a seventh (without one of them 186 to 190 us, without all three 138).
 // (1) lora_factors_kernel: M = 128 tokens, K = channels. The codes go TMA -> shared memory -> registers -> tensor memory as bf16
 //     (exact: a code has 8 significant bits and the step is a power of two), from where the MMA takes its A operand; dY goes TMA ->
 //     MMA as stored. fp32 sums over a slice of the channels; lora_split_kernel adds the slices.
@@ -16,7 +18,8 @@
 //     are added in the same fp32 accumulator.
 // Tokens behind the end of a chunk share its last 64-token block: their rows are overwritten with zeros in both operands (in the
 // operand alone a NaN in the neighbour example would survive as 0 * NaN).
-// Examples longer than a chunk are summed in pieces (fp32, added in piece order by lora_join_kernel): no float atomics anywhere.
+// Examples longer than a chunk are summed in pieces (fp32, added in piece order by lora_join_kernel). No float atomics between threads: the same
+// inputs give the same bits.
 #include <cstring>
 
 #include "qless_kernels.h"
@@ -34,15 +37,22 @@ constexpr int BIG = 32768;                  // operand bytes of one stage that c
 constexpr int CH = 128;                     // (1) channels per stage
 constexpr int TOK = 64;                     // (2) tokens per stage
 constexpr int TILE = 256;                   // (2) channels per item
+// fp32 gradients: an accumulator in tensor memory takes at most SPAN channels or tokens (half as many tokens where three terms share it), then the
+// epilogue adds it to the sum so far in global memory (always the same thread; in L2). The tensor core cuts the sum's last bits at each of its steps
+// of 16 instead of rounding them, so a sum's error grows with its length, one way: 8 examples of 512 tokens, 4096 -> 4096, rank 64: 1.6e-6 of the norm
+// with sums taken whole, 5.4e-7 so (fp32 products elsewhere: 4.4e-7), for 125 -> 145 us with 32 examples of 16 381 tokens (spans of 256: 2.7e-7, and
+// twice the additions). bf16 gradients are rounded to 8 bits and take their sums whole.
+constexpr int SPAN = 512;
 
 struct FactorParams {
     int64_t T, ld_scales;
     const uint8_t* scales;
-    float* part;                            // [2][slices][T][N64]: 0 = H, 1 = U (more than one slice)
+    float* part;                            // [2][slices][T][N64]: 0 = H, 1 = U (more than one slice or span)
     __nv_bfloat16* fac;                     // [2][boxes][T][64]: column c of term q is column q * term + c (one slice)
     float scaling;
     int32_t in, out, group, nr, n64, parts, term, boxes, slices, kb_x, kb_y, stages;      // kb_*: channel blocks per slice
     int32_t y_whole, steps_whole;
+    int32_t span;                           // channel blocks that one accumulator takes
     int32_t token_tiles;
     int64_t items;
     unsigned int* timeout_word;
@@ -120,6 +130,17 @@ __device__ __forceinline__ uint32_t split_term(float& a, float& b)
     a = fabsf(x) < INFINITY ? a - x : 0.0f;
     b = fabsf(y) < INFINITY ? b - y : 0.0f;
     return *reinterpret_cast<const uint32_t*>(&z);
+}
+
+// Adds in L2, without waiting for the sum that is there. Only one thread ever adds to an address, so the order is that of its program.
+__device__ __forceinline__ void add_to(float* p, uint32_t v)
+{
+    asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(p), "f"(__uint_as_float(v)) : "memory");
+}
+__device__ __forceinline__ void add4_to(float* p, uint32_t a, uint32_t b, uint32_t c, uint32_t d)      // p: 16-byte aligned
+{
+    asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(__uint_as_float(a)), "f"(__uint_as_float(b)),
+                 "f"(__uint_as_float(c)), "f"(__uint_as_float(d)) : "memory");
 }
 
 __device__ __forceinline__ void init_barriers(Bars* b)
@@ -221,39 +242,42 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
             Ring ring;
             uint32_t n = 0;
             bool ok = true;
-            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++n) {
-                int slice, kb0, kb1; bool is_x; int64_t tile;
-                item_of(item, slice, is_x, tile, kb0, kb1);
-                const uint32_t buf = n & 1u, d = tmem + buf * 128;
-                if (!warp_wait(&bars->d_empty[buf], ((n >> 1) & 1u) ^ 1u, TO_MMA)) { ok = false; break; }
-                tc_fence_after();
-                for (int kb = kb0; kb < kb1; ++kb, ring.next(nS)) {
-                    // the converters have seen the stage's copies land before they arrive here
-                    if (!warp_wait(&bars->ready[ring.slot], ring.parity, TO_MMA)) { ok = false; break; }
+            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+                int slice, from, end; bool is_x; int64_t tile;
+                item_of(item, slice, is_x, tile, from, end);
+                for (int kb0 = from; (kb0 < end || kb0 == from) && ok; kb0 += p.span, ++n) {
+                    const int kb1 = min(end, kb0 + p.span);
+                    const uint32_t buf = n & 1u, d = tmem + buf * 128;
+                    if (!warp_wait(&bars->d_empty[buf], ((n >> 1) & 1u) ^ 1u, TO_MMA)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
-                    if (elect_one()) {
-                    // Descriptors are made once per stage and advanced by constants (addresses in units of 16 bytes): made anew for every
-                    // product they took 180 clocks of this thread where the product takes 48.
-                    if (is_x) {
-                        const uint32_t a = tmem + 256 + ring.slot * 64;
-                        const uint64_t b0 = make_smem_desc_sw128(op), b1 = make_smem_desc_sw128(op + p.n64 * 128);
-                        mma_f16_ts(d, a, b0, idesc_x, kb > kb0);
+                    for (int kb = kb0; kb < kb1; ++kb, ring.next(nS)) {
+                        // the converters have seen the stage's copies land before they arrive here
+                        if (!warp_wait(&bars->ready[ring.slot], ring.parity, TO_MMA)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
+                        if (elect_one()) {
+                        // Descriptors are made once per stage and advanced by constants (addresses in units of 16 bytes): made anew for every
+                        // product they took 180 clocks of this thread where the product takes 48.
+                        if (is_x) {
+                            const uint32_t a = tmem + 256 + ring.slot * 64;
+                            const uint64_t b0 = make_smem_desc_sw128(op), b1 = make_smem_desc_sw128(op + p.n64 * 128);
+                            mma_f16_ts(d, a, b0, idesc_x, kb > kb0);
 #pragma unroll
-                        for (int k = 1; k < CH / 16; ++k) mma_f16_ts(d, a + k * 8, (k < 4 ? b0 : b1) + (uint64_t)((k & 3) * 2), idesc_x, 1u);
-                    } else {
-                        const uint64_t a0 = make_smem_desc_sw128(big), b0 = make_smem_desc_mn_sw128(op, 16384);
-                        mma_f16_ss(d, a0, b0, idesc_y, kb > kb0);
+                            for (int k = 1; k < CH / 16; ++k) mma_f16_ts(d, a + k * 8, (k < 4 ? b0 : b1) + (uint64_t)((k & 3) * 2), idesc_x, 1u);
+                        } else {
+                            const uint64_t a0 = make_smem_desc_sw128(big), b0 = make_smem_desc_mn_sw128(op, 16384);
+                            mma_f16_ss(d, a0, b0, idesc_y, kb > kb0);
 #pragma unroll
-                        for (int k = 1; k < CH / 16; ++k)
-                            mma_f16_ss(d, a0 + (uint64_t)((k >> 2) * 1024 + (k & 3) * 2), b0 + (uint64_t)(k * 128), idesc_y, 1u);
+                            for (int k = 1; k < CH / 16; ++k)
+                                mma_f16_ss(d, a0 + (uint64_t)((k >> 2) * 1024 + (k & 3) * 2), b0 + (uint64_t)(k * 128), idesc_y, 1u);
+                        }
+                        mma_commit(smem_u32(&bars->empty[ring.slot]));
+                        }
+                        __syncwarp();
                     }
-                    mma_commit(smem_u32(&bars->empty[ring.slot]));
-                    }
+                    if (ok && elect_one()) mma_commit(smem_u32(&bars->d_full[buf]));
                     __syncwarp();
                 }
-                if (ok && elect_one()) mma_commit(smem_u32(&bars->d_full[buf]));
-                __syncwarp();
             }
             if (elect_one()) mma_commit(smem_u32(&bars->drain));               // every MMA issued above completes before tensor memory is freed
             mbar_wait_quiet(smem_u32(&bars->drain), 0u);
@@ -318,49 +342,68 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
     } else {
         const int row = (warp & 3) * 32 + lane;
         uint32_t n = 0;
-        for (int64_t item = blockIdx.x; item < p.items; item += gridDim.x, ++n) {
-            int slice, kb0, kb1; bool is_x; int64_t tile;
-            item_of(item, slice, is_x, tile, kb0, kb1);
-            const uint32_t buf = n & 1u;
-            bool ok = mbar_wait(smem_u32(&bars->d_full[buf]), (n >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE);
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            if (!ok) break;
-            tc_fence_after();
-            const int64_t t = tile * 128 + row;
-            const int64_t kind = is_x ? 0 : 1;
-            for (int c0 = 0; c0 < p.nr; c0 += 16) {
-                uint32_t v[16];
-                tmem_ld_x16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 128 + c0, v);
-                tmem_wait_ld();
-                if (kb1 == kb0) {                              // a slice beyond the last channel block
+        bool ok = true;
+        for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            int slice, kb0, end; bool is_x; int64_t tile;
+            item_of(item, slice, is_x, tile, kb0, end);
+            for (int kb = kb0; kb < end || kb == kb0; kb += p.span, ++n) {
+                const uint32_t buf = n & 1u;
+                ok = mbar_wait(smem_u32(&bars->d_full[buf]), (n >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                const int64_t t = tile * 128 + row;
+                const int64_t kind = is_x ? 0 : 1;
+                for (int c0 = 0; c0 < p.nr; c0 += 16) {
+                    uint32_t v[16];
+                    tmem_ld_x16(tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 128 + c0, v);
+                    tmem_wait_ld();
+                    if (end == kb0) {                              // a slice beyond the last channel block
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) v[j] = 0u;
-                }
-                if (t >= p.T) continue;
-                if (p.slices == 1) {
-                    float x[16];
+                        for (int j = 0; j < 16; ++j) v[j] = 0u;
+                    }
+                    if (t >= p.T) continue;
+                    float* sum = p.part + ((kind * p.slices + slice) * p.T + t) * p.n64 + c0;
+                    const bool last = p.slices == 1 && kb + p.span >= end;
+                    if (kb > kb0 && !last) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) x[j] = __uint_as_float(v[j]) * p.scaling;
-                    __nv_bfloat16* dst = p.fac + (kind * p.boxes * p.T + t) * 64;
-                    for (int q = 0; q < p.parts; ++q)
+                        for (int j = 0; j < 16; j += 4) add4_to(sum + j, v[j], v[j + 1], v[j + 2], v[j + 3]);
+                        continue;
+                    }
+                    if (kb > kb0) {
 #pragma unroll
-                        for (int j = 0; j < 16; j += 8) {
-                            uint32_t w[4];
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) w[k] = split_term(x[j + 2 * k], x[j + 2 * k + 1]);
-                            const int c = q * p.term + c0 + j;
-                            *reinterpret_cast<uint4*>(dst + (int64_t)(c / 64) * p.T * 64 + c % 64) = make_uint4(w[0], w[1], w[2], w[3]);
+                        for (int j = 0; j < 16; j += 4) {
+                            const float4 y = __ldcg(reinterpret_cast<const float4*>(sum + j));
+                            v[j] = __float_as_uint(y.x + __uint_as_float(v[j]));
+                            v[j + 1] = __float_as_uint(y.y + __uint_as_float(v[j + 1]));
+                            v[j + 2] = __float_as_uint(y.z + __uint_as_float(v[j + 2]));
+                            v[j + 3] = __float_as_uint(y.w + __uint_as_float(v[j + 3]));
                         }
-                } else {
-                    float* dst = p.part + ((kind * p.slices + slice) * p.T + t) * p.n64 + c0;
+                    }
+                    if (last) {
+                        float x[16];
 #pragma unroll
-                    for (int j = 0; j < 16; j += 4)
-                        *reinterpret_cast<uint4*>(dst + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                        for (int j = 0; j < 16; ++j) x[j] = __uint_as_float(v[j]) * p.scaling;
+                        __nv_bfloat16* dst = p.fac + (kind * p.boxes * p.T + t) * 64;
+                        for (int q = 0; q < p.parts; ++q)
+#pragma unroll
+                            for (int j = 0; j < 16; j += 8) {
+                                uint32_t w[4];
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) w[k] = split_term(x[j + 2 * k], x[j + 2 * k + 1]);
+                                const int c = q * p.term + c0 + j;
+                                *reinterpret_cast<uint4*>(dst + (int64_t)(c / 64) * p.T * 64 + c % 64) = make_uint4(w[0], w[1], w[2], w[3]);
+                            }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; j += 4)
+                            *reinterpret_cast<uint4*>(sum + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                    }
                 }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars->d_empty[buf]));
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bars->d_empty[buf]));
         }
     }
     tc_fence_before();
@@ -405,8 +448,22 @@ template <> __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float
 
 // One thread's 16 accumulator columns [c0, c0 + 16) of channel ch -> dA (column j of the row-major [rank, width]) or dB (row ch).
 template <typename OutT>
-__device__ __forceinline__ void store_columns(OutT* dst, bool is_x, int64_t ch, int64_t width, int c0, int rank, const uint32_t (&v)[16], bool zero)
+__device__ __forceinline__ void store_columns(OutT* dst, bool is_x, int64_t ch, int64_t width, int c0, int rank, const uint32_t (&v)[16], bool zero,
+                                              bool add)
 {
+    if (sizeof(OutT) == 4 && add) {                            // onto what the spans before have left there
+        float* sum = reinterpret_cast<float*>(dst);
+        if (is_x) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (c0 + j < rank) add_to(sum + (int64_t)(c0 + j) * width + ch, v[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; j += 4)
+                if (c0 + j < rank) add4_to(sum + ch * rank + c0 + j, v[j], v[j + 1], v[j + 2], v[j + 3]);
+        }
+        return;
+    }
     if (is_x) {
 #pragma unroll
         for (int j = 0; j < 16; ++j)
@@ -435,7 +492,7 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
     constexpr int PARTS = sizeof(OutT) == 4 ? 3 : 2;
     // Where all terms together have at most 128 columns they are one operand (their sums meet in the epilogue): the channel operand is
     // read from shared memory once for all of them, whose bandwidth bounds this loop. Otherwise one product per term into the same accumulator.
-    // Three terms of 64 columns: the first two side by side, the third into the first's columns.
+    // Three terms of 64 columns: the first two side by side, the third into the second's columns (it is the smaller sum and loses less to them).
     constexpr bool WIDE = BOXES <= 3;
     constexpr int TERM_BYTES = BOXES / PARTS * 8192;         // a term's boxes, where it has boxes of its own
     constexpr int boxes = BOXES;                             // factor operand: boxes of 64 columns x 64 tokens
@@ -458,6 +515,7 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
     const uint32_t tmem = bars->tmem_base;                  // accumulator of item n, sub-tile m: column (n & 1) * 256 + m * 128
 
     const uint32_t items = (uint32_t)p.items, step_items = gridDim.x;
+    constexpr int span = sizeof(OutT) == 4 ? (BOXES == 6 ? SPAN / 2 : SPAN) : 1 << 30;
     auto chunk_of = [&](uint32_t item) {
         const uint32_t k = min(item, items - 1) / (uint32_t)p.tiles;
         return p.chunks != nullptr ? p.chunks[k] : p.few[k];
@@ -515,38 +573,41 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
             uint32_t n = 0;
             bool ok = true;
             LoraChunk ahead = chunk_of(blockIdx.x);
-            for (uint32_t item = blockIdx.x; item < items && ok; item += step_items, ++n) {
+            for (uint32_t item = blockIdx.x; item < items && ok; item += step_items) {
                 const LoraChunk c = ahead;
                 ahead = chunk_of(item + step_items);
                 bool is_x; int ch0;
                 place_of(item, is_x, ch0);
                 const int subs = (is_x ? p.in : p.out) - ch0 > 128 ? 2 : 1;
-                const uint32_t buf = n & 1u;
-                if (!warp_wait(&bars->d_empty[buf], ((n >> 1) & 1u) ^ 1u, TO_MMA)) { ok = false; break; }
-                tc_fence_after();
-                for (int t = 0; t < c.len; t += TOK, ring.next(nS)) {
-                    if (!warp_wait(&bars->ready[ring.slot], ring.parity, TO_MMA)) { ok = false; break; }
+                for (int t0 = 0; (t0 < c.len || t0 == 0) && ok; t0 += span, ++n) {
+                    const uint32_t buf = n & 1u;
+                    if (!warp_wait(&bars->d_empty[buf], ((n >> 1) & 1u) ^ 1u, TO_MMA)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
-                    if (elect_one()) {
-                    const uint64_t a0 = make_smem_desc_mn_sw128(big, 8192), b0 = make_smem_desc_mn_sw128(op, 8192);
-                    for (int m = 0; m < subs; ++m) {
-                        const uint64_t am = a0 + (uint64_t)(m * 1024);
-                        const uint32_t d = tmem + buf * 256 + m * 128;
-                        mma_f16_ss(d, am, b0, idesc, t > 0);
+                    const int end = min(c.len, t0 + span);
+                    for (int t = t0; t < end; t += TOK, ring.next(nS)) {
+                        if (!warp_wait(&bars->ready[ring.slot], ring.parity, TO_MMA)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t big = smem_u32(smem + (size_t)ring.slot * stage_bytes), op = big + BIG;
+                        if (elect_one()) {
+                        const uint64_t a0 = make_smem_desc_mn_sw128(big, 8192), b0 = make_smem_desc_mn_sw128(op, 8192);
+                        for (int m = 0; m < subs; ++m) {
+                            const uint64_t am = a0 + (uint64_t)(m * 1024);
+                            const uint32_t d = tmem + buf * 256 + m * 128;
+                            mma_f16_ss(d, am, b0, idesc, t > t0);
 #pragma unroll
-                        for (int i = 1; i < TOK / 16 * TERMS; ++i) {
-                            const int k = i / TERMS, q = i % TERMS;
-                            if (BOXES == 3 && q == 1) mma_f16_ss(d, am + (uint64_t)(k * 128), b0 + (uint64_t)(k * 128 + 2 * (TERM_BYTES / 16)), idesc_third, 1u);
-                            else mma_f16_ss(d, am + (uint64_t)(k * 128), b0 + (uint64_t)(k * 128 + q * (TERM_BYTES / 16)), idesc, 1u);
+                            for (int i = 1; i < TOK / 16 * TERMS; ++i) {
+                                const int k = i / TERMS, q = i % TERMS;
+                                if (BOXES == 3 && q == 1) mma_f16_ss(d + 64, am + (uint64_t)(k * 128), b0 + (uint64_t)(k * 128 + 2 * (TERM_BYTES / 16)), idesc_third, 1u);
+                                else mma_f16_ss(d, am + (uint64_t)(k * 128), b0 + (uint64_t)(k * 128 + q * (TERM_BYTES / 16)), idesc, 1u);
+                            }
                         }
+                        mma_commit(smem_u32(&bars->empty[ring.slot]));
+                        }
+                        __syncwarp();
                     }
-                    mma_commit(smem_u32(&bars->empty[ring.slot]));
-                    }
+                    if (ok && elect_one()) mma_commit(smem_u32(&bars->d_full[buf]));
                     __syncwarp();
                 }
-                if (ok && elect_one()) mma_commit(smem_u32(&bars->d_full[buf]));
-                __syncwarp();
             }
             if (elect_one()) mma_commit(smem_u32(&bars->drain));
             mbar_wait_quiet(smem_u32(&bars->drain), 0u);
@@ -644,45 +705,48 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
         const int64_t width_all = (int64_t)p.rank * (p.in + p.out);
         uint32_t n = 0;
         LoraChunk ahead = chunk_of(blockIdx.x);
-        for (uint32_t item = blockIdx.x; item < items; item += step_items, ++n) {
+        bool ok = true;
+        for (uint32_t item = blockIdx.x; item < items && ok; item += step_items) {
             const LoraChunk c = ahead;
             ahead = chunk_of(item + step_items);
             bool is_x; int ch0;
             place_of(item, is_x, ch0);
             const int width = is_x ? p.in : p.out;
-            const uint32_t buf = n & 1u;
-            bool ok = mbar_wait(smem_u32(&bars->d_full[buf]), (n >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE);
-            ok = __all_sync(0xFFFFFFFFu, ok);
-            if (!ok) break;
-            tc_fence_after();
-            const int64_t base = is_x ? 0 : (int64_t)p.rank * p.in;
-            for (int m = 0; m < 2; ++m) {
-                if (ch0 + m * 128 >= width) break;
-                const int64_t ch = ch0 + m * 128 + row;
-                for (int c0 = 0; c0 < p.rank; c0 += 16) {
-                    uint32_t v[16];
-                    const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 256 + m * 128 + c0;
-                    tmem_ld_x16(taddr, v);
-                    tmem_wait_ld();
-                    if (WIDE) {
+            for (int t0 = 0; t0 < c.len || t0 == 0; t0 += span, ++n) {
+                const uint32_t buf = n & 1u;
+                ok = mbar_wait(smem_u32(&bars->d_full[buf]), (n >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                const int64_t base = is_x ? 0 : (int64_t)p.rank * p.in;
+                for (int m = 0; m < 2; ++m) {
+                    if (ch0 + m * 128 >= width) break;
+                    const int64_t ch = ch0 + m * 128 + row;
+                    for (int c0 = 0; c0 < p.rank; c0 += 16) {
+                        uint32_t v[16];
+                        const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 256 + m * 128 + c0;
+                        tmem_ld_x16(taddr, v);
+                        tmem_wait_ld();
+                        if (WIDE) {
 #pragma unroll
-                        for (int q = 1; q < (BOXES == 3 ? 2 : PARTS); ++q) {
-                            uint32_t low[16];
-                            tmem_ld_x16(taddr + (BOXES == 3 ? 64 : q * p.nr), low);
-                            tmem_wait_ld();
+                            for (int q = 1; q < (BOXES == 3 ? 2 : PARTS); ++q) {
+                                uint32_t low[16];
+                                tmem_ld_x16(taddr + (BOXES == 3 ? 64 : q * p.nr), low);
+                                tmem_wait_ld();
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(low[j]));
+                                for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(low[j]));
+                            }
+                        }
+                        if (ch < width) {
+                            if (c.slot >= 0) store_columns<float>(p.part + (int64_t)c.slot * width_all + base, is_x, ch, width, c0, p.rank, v, c.len == 0, t0 > 0);
+                            else store_columns<OutT>(reinterpret_cast<OutT*>(p.grads) + (int64_t)c.example * p.ld_grads + base, is_x, ch, width, c0, p.rank, v, c.len == 0, t0 > 0);
                         }
                     }
-                    if (ch < width) {
-                        if (c.slot >= 0) store_columns<float>(p.part + (int64_t)c.slot * width_all + base, is_x, ch, width, c0, p.rank, v, c.len == 0);
-                        else store_columns<OutT>(reinterpret_cast<OutT*>(p.grads) + (int64_t)c.example * p.ld_grads + base, is_x, ch, width, c0, p.rank, v, c.len == 0);
-                    }
                 }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars->d_empty[buf]));
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bars->d_empty[buf]));
         }
     }
     tc_fence_before();
@@ -814,6 +878,7 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
         f.token_tiles = (int32_t)pl.token_tiles;
         f.items = 2 * pl.token_tiles * pl.slices;
         f.y_whole = y_whole; f.steps_whole = steps_whole;
+        f.span = a.dtype == QLESS_F32 ? SPAN / CH : 1 << 24;
         f.timeout_word = timeout_word;
         const size_t stage = BIG + (size_t)pl.n64 * 256;
         f.stages = (int32_t)(budget / stage < MAX_STAGES ? budget / stage : MAX_STAGES);

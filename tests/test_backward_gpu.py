@@ -242,3 +242,26 @@ def test_lora_gradients_on_another_stream():
     B.qless_lora_gradients(*case, offsets, group=64, grads=got, workspace=ws, stream=st)
     st.synchronize()
     assert torch.equal(got, want)
+
+
+# An fp32 sum is taken in accumulators of at most 512 channels or tokens: 32 steps of 16, each of which cuts the running sum's last bits by
+# half a unit (2^-24 of it) on average, one way; a sum of random signs is on average at 2/3 of its end: 32 * 2^-24 * 2/3 = 1.3e-6 a product,
+# two products in a row. Above 64 columns the three terms share accumulators of 256 tokens: 48 steps, 1.9e-6. Sums taken whole would
+# have three to eight times as many steps here.
+@pytest.mark.parametrize("offsets,wi,wo,rank,bound", [
+    ([0, 7000, 7001, 14300], 4096, 2064, 16, 2.6e-6),            # one slice, eight accumulators a factor, pieces of 1216 tokens
+    ([0, 2000, 6000], 4096, 4112, 48, 2.6e-6),                   # slices of the channels, terms of 64 columns
+    ([0, 1100, 4100], 1040, 528, 128, 3.2e-6),
+    ([3, 515, 516, 1029], 640, 512, 64, 2.6e-6),                 # one token behind an accumulator's last
+])
+def test_fp32_lora_gradients_do_not_lose_digits_with_length(offsets, wi, wo, rank, bound):
+    case = _lora_case(offsets[-1] + 5, wi, wo, rank, 32, 91)
+    got = B.qless_lora_gradients(*case, offsets, scaling=0.5, group=32, dtype=torch.float32)
+    want, mag = reference_lora(*case, offsets, 0.5, 32)
+    B.qless_check()
+    _check_lora(got, want, mag, wi, wo, max(b - a for a, b in zip(offsets, offsets[1:])), torch.float32)
+    for part in (slice(0, rank * wi), slice(rank * wi, None)):
+        for e in range(len(offsets) - 1):
+            w = want[e, part].double()
+            assert (got[e, part].double() - w.to(got.device)).norm() <= bound * w.norm().to(got.device)
+    assert torch.equal(got, B.qless_lora_gradients(*case, offsets, scaling=0.5, group=32, dtype=torch.float32))
