@@ -59,9 +59,8 @@ struct GemmParams {
     int32_t stages, b_rows;                 // b_rows: rows of B that one CTA of the pair brings
     const int32_t* labels;                  // [tpad] of the gathered tokens
     const RowParam* rowp;
-    float2* stat;                           // STATS: [entries per tile * tiles][tpad] (maximum, sum)
-    float* psum;                            // PROBS: [entries per tile * tiles][tpad] sums, or NULL
-    int32_t tile0;                          // tile index of the launch's first column tile in stat / psum
+    float2* stat;                           // [entries per tile * tiles][tpad]: (maximum, sum relative to it; PROBS: to the row's reference), PROBS: or NULL
+    int32_t tile0;                          // tile index of the launch's first column tile in stat
     __nv_bfloat16* out;                     // PROBS: piece [tpad][ld_out]; GRAD_W: rows of dW
     int64_t ld_out;
     float* acc;                             // GRAD_H: [splits][row tiles * 256][cols]
@@ -331,11 +330,14 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                     if (lane < have) p.stat[entry * p.tpad + t0 + lane] = make_float2(most, sum);
                 } else {
                     __nv_bfloat16* dst = p.out + (int64_t)t0 * p.ld_out + v;
+                    float top[32];
 #pragma unroll
                     for (int k = 0; k < 32; ++k) {
+                        top[k] = -INFINITY;
                         if (k < have) {
                             const RowParam rp = bars->rowp[t0 + k];
                             const bool own = bars->label[t0 + k] == p.col0 + v, out = own || v >= p.cols;
+                            if (!out) top[k] = __uint_as_float(raw[k]);
                             const float x = out ? -INFINITY : fmaf(__uint_as_float(raw[k]), LOG2E, -rp.r2);
                             run_max = fmaxf(run_max, x);
                             e[k] = ex2(x);
@@ -346,16 +348,16 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                             if (c0 + k < upto) dst[(int64_t)k * p.ld_out] = __float2bfloat16_rn(0.0f);
                         }
                     }
-                    if (p.psum != nullptr) {
-                        const float sum = across_lanes<false>(e, lane);
-                        if (lane < have) p.psum[entry * p.tpad + t0 + lane] = sum;
+                    if (p.stat != nullptr) {
+                        const float sum = across_lanes<false>(e, lane), most = across_lanes<true>(top, lane) * LOG2E;
+                        if (lane < have) p.stat[entry * p.tpad + t0 + lane] = make_float2(most, sum);
                     }
                 }
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_leader_tmem(smem_u32(&bars->d_empty[buf]), rank);
-            if (MODE == PROBS && p.psum != nullptr && run_max > LIMIT) *p.redo = 1;
+            if (MODE == PROBS && p.stat != nullptr && run_max > LIMIT) *p.redo = 1;
         }
         for (int64_t item = pair; !SWAP && item < items; item += num_pairs, ++n_acc) {
             int split, m, n, kb0, kb1;
@@ -419,9 +421,8 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                         float e[32];
 #pragma unroll
                         for (int k = 0; k < 32; ++k) {
-                            const float x = fmaf(__uint_as_float(v[k]), LOG2E, -rp.r2);
-                            run_max = fmaxf(run_max, x);
-                            e[k] = ex2(x);
+                            run_max = fmaxf(run_max, __uint_as_float(v[k]));
+                            e[k] = ex2(fmaf(__uint_as_float(v[k]), LOG2E, -rp.r2));
                             run_sum += e[k];
                             e[k] *= rp.w;
                         }
@@ -484,9 +485,9 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                 }
             }
             if (MODE == STATS && row < count) p.stat[((int64_t)(p.tile0 + n) * 2 + half) * p.tpad + row] = make_float2(run_max, run_sum);
-            if (MODE == PROBS && row < count && p.psum != nullptr) {
-                p.psum[((int64_t)(p.tile0 + n) * 2 + half) * p.tpad + row] = run_sum;
-                if (run_max > LIMIT) *p.redo = 1;
+            if (MODE == PROBS && row < count && p.stat != nullptr) {
+                p.stat[((int64_t)(p.tile0 + n) * 2 + half) * p.tpad + row] = make_float2(run_max * LOG2E, run_sum);
+                if (fmaf(run_max, LOG2E, -rp.r2) > LIMIT) *p.redo = 1;
             }
         }
     }
@@ -636,7 +637,6 @@ struct RowArgs {
     int32_t kind, entries;                  // entries: stretches of columns with a partial result
     int64_t tpad;
     const float2* stat;
-    const float* psum;
     const float* label_logit;
     const float* weight;
     const int32_t* order;
@@ -644,6 +644,22 @@ struct RowArgs {
     float2* coef;                           // ROW_FROM_SUMS: w sigma(d), 1 / s
     float* loss;
 };
+
+// What the others' sum s 2^ref and the label's logit (both in powers of two) say of a row: its loss, the probability of the others, the
+// normaliser of all columns.
+struct RowEnd { float nll, sigma, all; };
+__device__ __forceinline__ RowEnd row_end(float ref, float s, float ly)
+{
+    const float others = s == 0.0f ? -INFINITY : ref + log2f(s);      // no other column has any weight (or there is none)
+    const float d = others - ly, e = exp2f(-fabsf(d)), tail = log1pf(e);
+    RowEnd o;
+    o.nll = d > 0.0f ? d * LN2 + tail : tail;
+    o.sigma = d > 0.0f ? 1.0f / (1.0f + e) : e / (1.0f + e);
+    if (others == -INFINITY) { o.nll = ly == ly ? 0.0f : ly; o.sigma = o.nll; }
+    else if (d != d) { o.nll = d; o.sigma = d; }
+    o.all = fmaxf(others, ly) + tail * LOG2E;
+    return o;
+}
 
 // Eight rows per block, 128 threads per row that take every 128th stretch: the partial results of a row lie tpad apart, so it is
 // the number of loads in flight that counts. Joined in a fixed order.
@@ -668,7 +684,7 @@ __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowArgs a)
         if (row < count) {
             if (a.kind == ROW_FROM_SUMS) {
 #pragma unroll 4
-                for (int i = seg; i < a.entries; i += 1024 / ROWS) s += a.psum[(int64_t)i * a.tpad + row];
+                for (int i = seg; i < a.entries; i += 1024 / ROWS) s += a.stat[(int64_t)i * a.tpad + row].y;
             } else {
 #pragma unroll 4
                 for (int i = seg; i < a.entries; i += 1024 / ROWS) {
@@ -696,61 +712,111 @@ __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowArgs a)
                 a.rowp[row] = RowParam{m > -INFINITY ? m : 0.0f, 1.0f, 0.0f, 0.0f};
                 continue;
             }
-            const float ref = a.kind == ROW_FROM_SUMS ? a.rowp[row].r2 : m;
-            const float w = a.weight[row], ly = a.label_logit[row];
-            const float others = s == 0.0f ? -INFINITY : ref + log2f(s);      // no other column has any weight (or there is none)
-            const float d = others - ly;
-            // log(1 + e^d) and the probability of the others
-            const float e = exp2f(-fabsf(d)), tail = log1pf(e);
-            float nll = d > 0.0f ? d * LN2 + tail : tail;
-            float sigma = d > 0.0f ? 1.0f / (1.0f + e) : e / (1.0f + e);
-            if (others == -INFINITY) { nll = ly == ly ? 0.0f : ly; sigma = nll; }
-            else if (d != d) { nll = d; sigma = d; }
-            a.loss[a.order[row]] = nll;
-            if (a.kind == ROW_FROM_SUMS) a.coef[row] = make_float2(w * sigma, s == 0.0f ? 0.0f : 1.0f / s);
-            else a.rowp[row] = RowParam{fmaxf(others, ly) + tail * LOG2E, w, -w * sigma, 0.0f};      // the full normaliser
+            const float w = a.weight[row];
+            const RowEnd end = row_end(a.kind == ROW_FROM_SUMS ? a.rowp[row].r2 : m, s, a.label_logit[row]);
+            a.loss[a.order[row]] = end.nll;
+            if (a.kind == ROW_FROM_SUMS) a.coef[row] = make_float2(w * end.sigma, s == 0.0f ? 0.0f : 1.0f / s);
+            else a.rowp[row] = RowParam{end.all, w, -w * end.sigma, 0.0f};
         }
     }
 }
 
-// Gradient rows of all tokens: joins the slices of the vocabulary; zero for tokens without a loss. `sums` = the accumulator holds
-// sum exp2(l2 - r2) W_v over the other columns; otherwise the finished gradient.
-__global__ void loss_finish_kernel(const float* __restrict__ acc, int32_t width, const LossMeta* __restrict__ meta,
-                                   const int32_t* __restrict__ place, const int32_t* __restrict__ labels, const float2* __restrict__ coef, int32_t sums,
-                                   const __nv_bfloat16* __restrict__ weight, int64_t ld_weight, int64_t T, __nv_bfloat16* __restrict__ out, int64_t ld_out)
+// Eight columns of a gradient row: joins the slices of the vocabulary. `sums`: the accumulator holds sum exp2(l2 - r2) W_v over the
+// other columns, `k` is the row's coef and `y` the label's row of W; otherwise it holds the finished gradient.
+__device__ __forceinline__ uint4 finish8(const float* __restrict__ acc, int64_t slice, int splits, bool sums, float2 k, const __nv_bfloat16* __restrict__ y)
+{
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = 0.0f;
+    for (int s = 0; s < splits; ++s) {
+        const float4* src = reinterpret_cast<const float4*>(acc + s * slice);
+        const float4 a = src[0], b = src[1];
+        x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w; x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
+    }
+    if (sums) {
+        const uint4 w = *reinterpret_cast<const uint4*>(y);
+        const uint32_t yw[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[2 * j] = k.x * (x[2 * j] * k.y - __uint_as_float(yw[j] << 16));
+            x[2 * j + 1] = k.x * (x[2 * j + 1] * k.y - __uint_as_float(yw[j] & 0xFFFF0000u));
+        }
+    }
+    return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+}
+
+struct FinishArgs {
+    const float* acc;
+    int32_t width, sums, entries;           // entries: stretches of columns with a partial sum (loss_close_kernel)
+    const LossMeta* meta;
+    const int32_t* place;
+    const int32_t* labels;
+    const float2* coef;
+    const __nv_bfloat16* weight;
+    int64_t ld_weight, T, ld_out, tpad;
+    __nv_bfloat16* out;
+    const float2* stat;                     // from here on: loss_close_kernel
+    const float* label_logit;
+    const float* token_weight;              // of the gathered tokens
+    const RowParam* rowp;
+    float* loss;
+};
+
+// Gradient rows of all tokens; zero for tokens without a loss.
+__global__ void loss_finish_kernel(const FinishArgs a)
 {
     ahead_release();
     ahead_wait();
-    const int vecs = width / 8, splits = meta->splits;
-    const int64_t slice = (int64_t)(meta->count + 255) / 256 * 256;
-    const int64_t total = T * vecs;
+    const int vecs = a.width / 8, splits = a.meta->splits;
+    const int64_t slice = (int64_t)(a.meta->count + 255) / 256 * 256 * a.width;
+    const int64_t total = a.T * vecs;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
         const int64_t t = i / vecs;
         const int c = (int)(i - t * vecs) * 8;
-        const int r = place[t];
+        const int r = a.place[t];
         uint4 o = make_uint4(0u, 0u, 0u, 0u);
+        if (r >= 0)
+            o = a.sums ? finish8(a.acc + (int64_t)r * a.width + c, slice, splits, true, a.coef[r], a.weight + (int64_t)a.labels[r] * a.ld_weight + c)
+                       : finish8(a.acc + (int64_t)r * a.width + c, slice, splits, false, make_float2(0.0f, 0.0f), nullptr);
+        *reinterpret_cast<uint4*>(a.out + t * a.ld_out + c) = o;
+    }
+}
+
+// Few tokens, gradient of the hidden states alone: a block per token takes the row's sums together and finishes its gradient, one launch
+// in place of loss_rows_kernel and loss_finish_kernel. (With many tokens the former reads a sector of eight rows' sums once, this eight times.)
+__global__ void __launch_bounds__(512) loss_close_kernel(const FinishArgs a)
+{
+    __shared__ float part[16];
+    __shared__ float2 coef;
+    ahead_release();
+    ahead_wait();
+    const int vecs = a.width / 8, splits = a.meta->splits, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t slice = (int64_t)(a.meta->count + 255) / 256 * 256 * a.width;
+    for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+        const int r = a.place[t];
         if (r >= 0) {
-            float x[8];
+            float s = 0.0f;
+#pragma unroll 4
+            for (int i = threadIdx.x; i < a.entries; i += 512) s += a.stat[(int64_t)i * a.tpad + r].y;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = 0.0f;
-            for (int s = 0; s < splits; ++s) {
-                const float4* src = reinterpret_cast<const float4*>(acc + (s * slice + r) * width + c);
-                const float4 a = src[0], b = src[1];
-                x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w; x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
+            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+            __syncthreads();                                 // the last row's coef has been read
+            if (lane == 0) part[warp] = s;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                s = 0.0f;
+                for (int j = 0; j < 16; ++j) s += part[j];
+                const RowEnd end = row_end(a.rowp[r].r2, s, a.label_logit[r]);
+                a.loss[t] = end.nll;
+                coef = make_float2(a.token_weight[r] * end.sigma, s == 0.0f ? 0.0f : 1.0f / s);
             }
-            if (sums) {
-                const float2 k = coef[r];
-                const uint4 y = *reinterpret_cast<const uint4*>(weight + (int64_t)labels[r] * ld_weight + c);
-                const uint32_t yw[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    x[2 * j] = k.x * (x[2 * j] * k.y - __uint_as_float(yw[j] << 16));
-                    x[2 * j + 1] = k.x * (x[2 * j + 1] * k.y - __uint_as_float(yw[j] & 0xFFFF0000u));
-                }
-            }
-            o = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+            __syncthreads();
         }
-        *reinterpret_cast<uint4*>(out + t * ld_out + c) = o;
+        for (int v = threadIdx.x; v < vecs; v += 512) {
+            uint4 o = make_uint4(0u, 0u, 0u, 0u);
+            if (r >= 0) o = finish8(a.acc + (int64_t)r * a.width + v * 8, slice, splits, true, coef, a.weight + (int64_t)a.labels[r] * a.ld_weight + v * 8);
+            *reinterpret_cast<uint4*>(a.out + t * a.ld_out + v * 8) = o;
+        }
     }
 }
 
@@ -828,7 +894,6 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
     float2* coef = reinterpret_cast<float2*>(ws + pl.coef_off);
     RowParam* rowp = reinterpret_cast<RowParam*>(ws + pl.rowp_off);
     float2* stat = reinterpret_cast<float2*>(ws + pl.stat_off);
-    float* psum = reinterpret_cast<float*>(ws + pl.stat_off);       // the statistics are read before the sums are written, and again the other way round
     __nv_bfloat16* hidden = reinterpret_cast<__nv_bfloat16*>(ws + pl.hidden_off);
     __nv_bfloat16* piece = reinterpret_cast<__nv_bfloat16*>(ws + pl.piece_off);
     float* acc = reinterpret_cast<float*>(ws + pl.acc_off);
@@ -871,65 +936,74 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
 
     GemmParams base{};
     base.meta = meta; base.tpad = pl.tpad; base.labels = labels; base.rowp = rowp; base.b_rows = b_rows; base.timeout_word = timeout_word;
-    auto stats = [&](int32_t cols, const int32_t* gate) {
+    auto stats = [&](int32_t cols) {
         GemmParams p = base;
-        p.gate = gate; p.cols = cols; p.k = a.width; p.stat = stat; p.a_whole = p.b_whole = whole;
+        p.cols = cols; p.k = a.width; p.stat = stat; p.a_whole = p.b_whole = whole;
         const int64_t tiles = (cols + 255) / 256;
         return few ? launch_gemm<STATS, true>("loss_stats", tm_w, tm_x, p, tiles, st) : launch_gemm<STATS, false>("loss_stats", tm_x, tm_w, p, mt * tiles, st);
     };
     auto rows = [&](int kind, int32_t entries, const int32_t* gate) -> qless_status {
         RowArgs r{};
-        r.meta = meta; r.gate = gate; r.kind = kind; r.entries = entries; r.tpad = pl.tpad; r.stat = stat; r.psum = psum; r.label_logit = logit;
+        r.meta = meta; r.gate = gate; r.kind = kind; r.entries = entries; r.tpad = pl.tpad; r.stat = stat; r.label_logit = logit;
         r.weight = weight; r.order = order; r.rowp = rowp; r.coef = coef; r.loss = a.loss;
         { ProfileScope ps("loss_rows", st);
           QLESS_CUDA_TRY(launch_ahead(loss_rows_kernel, dim3(grid_of(a.T, ROWS)), dim3(1024), 0, st, r)); }
         count_launches(1);
         return QLESS_OK;
     };
-    auto pieces = [&](bool keep_sums, const int32_t* gate) {
-        for (int32_t v0 = 0; v0 < a.vocab; v0 += pl.piece) {
-            const int32_t cols = a.vocab - v0 < pl.piece ? a.vocab - v0 : pl.piece;
-            GemmParams p = base;
-            p.gate = gate; p.cols = cols; p.col0 = v0; p.k = a.width; p.out = piece; p.ld_out = pl.piece; p.tile0 = v0 / 256;
-            p.psum = keep_sums ? psum : nullptr; p.redo = &meta->redo; p.a_whole = p.b_whole = whole;
-            const int64_t tiles = (cols + 255) / 256;
-            qless_status e = few ? launch_gemm<PROBS, true>("loss_probs", tm_w, tm_x, p, tiles, st) : launch_gemm<PROBS, false>("loss_probs", tm_x, tm_w, p, mt * tiles, st);
-            if (e != QLESS_OK) return e;
-            if (want_h) {
-                GemmParams g = base;
-                g.gate = gate; g.cols = a.width; g.col0 = v0; g.k = cols; g.acc = acc; g.accumulate = v0 > 0;
-                g.a_whole = few ? whole : 1; g.b_whole = few ? 1 : whole;
-                e = few ? launch_gemm<GRAD_H, true>("loss_grad_hidden", tm_w, tm_p, g, pl.cap_tiles * nt_h, st)
-                        : launch_gemm<GRAD_H, false>("loss_grad_hidden", tm_p, tm_w, g, pl.cap_tiles * nt_h, st);
-                if (e != QLESS_OK) return e;
-            }
-            if (want_w) {
-                GemmParams g = base;
-                g.gate = gate; g.cols = a.width; g.rows = cols; g.col0 = v0; g.out = reinterpret_cast<__nv_bfloat16*>(a.grad_weight); g.ld_out = a.ld_grad_weight; g.a_whole = 1; g.b_whole = whole;
-                e = launch_gemm<GRAD_W, false>("loss_grad_weight", tm_pg, tm_xg, g, (int64_t)((cols + 255) / 256) * nt_h, st);
-                if (e != QLESS_OK) return e;
-            }
+    auto probs = [&](int32_t v0, int32_t cols, bool keep_sums, const int32_t* gate) {
+        GemmParams p = base;
+        p.gate = gate; p.cols = cols; p.col0 = v0; p.k = a.width; p.out = piece; p.ld_out = pl.piece; p.tile0 = v0 / 256;
+        p.stat = keep_sums ? stat : nullptr; p.redo = &meta->redo; p.a_whole = p.b_whole = whole;
+        const int64_t tiles = (cols + 255) / 256;
+        return few ? launch_gemm<PROBS, true>("loss_probs", tm_w, tm_x, p, tiles, st) : launch_gemm<PROBS, false>("loss_probs", tm_x, tm_w, p, mt * tiles, st);
+    };
+    auto grads = [&](int32_t v0, int32_t cols, const int32_t* gate) {
+        qless_status e = QLESS_OK;
+        if (want_h) {
+            GemmParams g = base;
+            g.gate = gate; g.cols = a.width; g.col0 = v0; g.k = cols; g.acc = acc; g.accumulate = v0 > 0;
+            g.a_whole = few ? whole : 1; g.b_whole = few ? 1 : whole;
+            e = few ? launch_gemm<GRAD_H, true>("loss_grad_hidden", tm_w, tm_p, g, pl.cap_tiles * nt_h, st)
+                    : launch_gemm<GRAD_H, false>("loss_grad_hidden", tm_p, tm_w, g, pl.cap_tiles * nt_h, st);
         }
-        return QLESS_OK;
+        if (want_w && e == QLESS_OK) {
+            GemmParams g = base;
+            g.gate = gate; g.cols = a.width; g.rows = cols; g.col0 = v0; g.out = reinterpret_cast<__nv_bfloat16*>(a.grad_weight); g.ld_out = a.ld_grad_weight; g.a_whole = 1; g.b_whole = whole;
+            e = launch_gemm<GRAD_W, false>("loss_grad_weight", tm_pg, tm_xg, g, (int64_t)((cols + 255) / 256) * nt_h, st);
+        }
+        return e;
+    };
+    auto pieces = [&](bool keep_sums, const int32_t* gate) {
+        qless_status e = QLESS_OK;
+        for (int32_t v0 = 0; v0 < a.vocab && e == QLESS_OK; v0 += pl.piece) {
+            const int32_t cols = a.vocab - v0 < pl.piece ? a.vocab - v0 : pl.piece;
+            if ((e = probs(v0, cols, keep_sums, gate)) == QLESS_OK) e = grads(v0, cols, gate);
+        }
+        return e;
     };
 
+    const bool close = few && !pl.exact;
     if (pl.exact) {
-        if ((s = stats(a.vocab, nullptr)) != QLESS_OK) return s;
+        if ((s = stats(a.vocab)) != QLESS_OK) return s;
         if ((s = rows(ROW_FROM_STATS, pl.entries, nullptr)) != QLESS_OK) return s;
         if (want_w && (s = pieces(false, nullptr)) != QLESS_OK) return s;
     } else {
-        if ((s = pieces(true, nullptr)) != QLESS_OK) return s;
-        if ((s = stats(a.vocab, &meta->redo)) != QLESS_OK) return s;
+        const bool one = a.vocab <= pl.piece;                    // one piece: whether it has to be redone is known before its gradient
+        if ((s = one ? probs(0, a.vocab, true, nullptr) : pieces(true, nullptr)) != QLESS_OK) return s;
         if ((s = rows(ROW_REFERENCE, pl.entries, &meta->redo)) != QLESS_OK) return s;
-        if ((s = pieces(true, &meta->redo)) != QLESS_OK) return s;
-        if ((s = rows(ROW_FROM_SUMS, pl.entries, nullptr)) != QLESS_OK) return s;
+        if ((s = one ? probs(0, a.vocab, true, &meta->redo) : pieces(true, &meta->redo)) != QLESS_OK) return s;
+        if (one && (s = grads(0, a.vocab, nullptr)) != QLESS_OK) return s;
+        if (!close && (s = rows(ROW_FROM_SUMS, pl.entries, nullptr)) != QLESS_OK) return s;
     }
     if (want_h) {
+        FinishArgs f{};
+        f.acc = acc; f.width = a.width; f.sums = want_w ? 0 : 1; f.entries = pl.entries; f.meta = meta; f.place = place; f.labels = labels; f.coef = coef;
+        f.weight = reinterpret_cast<const __nv_bfloat16*>(a.weight); f.ld_weight = a.ld_weight; f.T = a.T; f.ld_out = a.ld_grad_hidden; f.tpad = pl.tpad;
+        f.out = reinterpret_cast<__nv_bfloat16*>(a.grad_hidden); f.stat = stat; f.label_logit = logit; f.token_weight = weight; f.rowp = rowp; f.loss = a.loss;
         { ProfileScope ps("loss_finish", st);
-          QLESS_CUDA_TRY(launch_ahead(loss_finish_kernel, dim3(grid_of(a.T * (a.width / 8), 256)), dim3(256), 0, st, (const float*)acc, a.width, (const LossMeta*)meta,
-                                      (const int32_t*)place, (const int32_t*)labels, (const float2*)coef, (int32_t)(want_w ? 0 : 1),
-                                      reinterpret_cast<const __nv_bfloat16*>(a.weight), a.ld_weight, a.T, reinterpret_cast<__nv_bfloat16*>(a.grad_hidden),
-                                      a.ld_grad_hidden)); }
+          if (close) QLESS_CUDA_TRY(launch_ahead(loss_close_kernel, dim3((unsigned)a.T), dim3(512), 0, st, f));
+          else QLESS_CUDA_TRY(launch_ahead(loss_finish_kernel, dim3(grid_of(a.T * (a.width / 8), 256)), dim3(256), 0, st, f)); }
         count_launches(1);
     }
     return QLESS_OK;
