@@ -58,7 +58,9 @@ struct GemmParams {
     int64_t tpad;
     int32_t stages, b_rows;                 // b_rows: rows of B that one CTA of the pair brings
     const int32_t* labels;                  // [tpad] of the gathered tokens
-    const RowParam* rowp;
+    RowParam* rowp;
+    const float2* first;                    // swapped PROBS, second pass: what the first left in stat; its maxima become the references
+    int32_t entries;
     float2* stat;                           // [entries per tile * tiles][tpad]: (maximum, sum relative to it; PROBS: to the row's reference), PROBS: or NULL
     int32_t tile0;                          // tile index of the launch's first column tile in stat
     __nv_bfloat16* out;                     // PROBS: piece [tpad][ld_out]; GRAD_W: rows of dW
@@ -274,10 +276,17 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
         const int q = warp & 3, half = warp >= 6 ? 1 : 0;
         const uint32_t lane_base = (uint32_t)(q * 32) << 16;
         uint32_t n_acc = 0;
-        if (SWAP && MODE != GRAD_H) {
+        if (SWAP && MODE != GRAD_H && !idle) {
             for (int t = threadIdx.x - 64; t < count; t += 256) {
                 bars->label[t] = p.labels[t];
-                if (MODE == PROBS) bars->rowp[t] = p.rowp[t];
+                if (MODE == PROBS && p.first == nullptr) bars->rowp[t] = p.rowp[t];
+                if (MODE == PROBS && p.first != nullptr) {           // every block for itself; block 0 also for loss_close_kernel
+                    float m = -INFINITY;
+#pragma unroll 4
+                    for (int i = 0; i < p.entries; ++i) m = fmaxf(m, p.first[(int64_t)i * p.tpad + t].x);
+                    bars->rowp[t] = RowParam{m > -INFINITY ? m : 0.0f, 1.0f, 0.0f, 0.0f};
+                    if (blockIdx.x == 0) p.rowp[t] = bars->rowp[t];
+                }
             }
             asm volatile("bar.sync 1, 256;" ::: "memory");
         }
@@ -755,7 +764,7 @@ struct FinishArgs {
     const __nv_bfloat16* weight;
     int64_t ld_weight, T, ld_out, tpad;
     __nv_bfloat16* out;
-    const float2* stat;                     // from here on: loss_close_kernel
+    const float2* stat;                     // from here on: loss_close_kernel; a second pass leaves its sums behind the first's
     const float* label_logit;
     const float* token_weight;              // of the gathered tokens
     const RowParam* rowp;
@@ -795,9 +804,10 @@ __global__ void __launch_bounds__(512) loss_close_kernel(const FinishArgs a)
     for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
         const int r = a.place[t];
         if (r >= 0) {
+            const float2* stat = a.stat + (a.meta->redo != 0 ? (int64_t)a.entries * a.tpad : 0);
             float s = 0.0f;
 #pragma unroll 4
-            for (int i = threadIdx.x; i < a.entries; i += 512) s += a.stat[(int64_t)i * a.tpad + r].y;
+            for (int i = threadIdx.x; i < a.entries; i += 512) s += stat[(int64_t)i * a.tpad + r].y;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
             __syncthreads();                                 // the last row's coef has been read
@@ -875,7 +885,7 @@ LossPlan plan_loss(int64_t T, int32_t width, int32_t vocab, bool want_h, bool wa
     pl.logit_off = take((size_t)pl.tpad * 4);
     pl.coef_off = take((size_t)pl.tpad * 8);
     pl.rowp_off = take((size_t)pl.tpad * sizeof(RowParam));
-    pl.stat_off = take((size_t)pl.entries * pl.tpad * 8);
+    pl.stat_off = take((size_t)pl.entries * pl.tpad * (pl.few && !pl.exact ? 16 : 8));      // (few: a second pass has its own)
     pl.hidden_off = take((size_t)pl.tpad * width * 2);
     pl.piece_off = (want_h || want_w) ? take((size_t)pl.tpad * pl.piece * 2) : 0;
     pl.acc_off = want_h ? take((size_t)cap * 256 * width * 4) : 0;
@@ -951,10 +961,12 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
         count_launches(1);
         return QLESS_OK;
     };
+    const bool close = few && !pl.exact;
     auto probs = [&](int32_t v0, int32_t cols, bool keep_sums, const int32_t* gate) {
         GemmParams p = base;
         p.gate = gate; p.cols = cols; p.col0 = v0; p.k = a.width; p.out = piece; p.ld_out = pl.piece; p.tile0 = v0 / 256;
         p.stat = keep_sums ? stat : nullptr; p.redo = &meta->redo; p.a_whole = p.b_whole = whole;
+        if (close && gate != nullptr) { p.first = stat; p.entries = pl.entries; p.stat = stat + (int64_t)pl.entries * pl.tpad; }
         const int64_t tiles = (cols + 255) / 256;
         return few ? launch_gemm<PROBS, true>("loss_probs", tm_w, tm_x, p, tiles, st) : launch_gemm<PROBS, false>("loss_probs", tm_x, tm_w, p, mt * tiles, st);
     };
@@ -983,7 +995,6 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
         return e;
     };
 
-    const bool close = few && !pl.exact;
     if (pl.exact) {
         if ((s = stats(a.vocab)) != QLESS_OK) return s;
         if ((s = rows(ROW_FROM_STATS, pl.entries, nullptr)) != QLESS_OK) return s;
@@ -991,7 +1002,7 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
     } else {
         const bool one = a.vocab <= pl.piece;                    // one piece: whether it has to be redone is known before its gradient
         if ((s = one ? probs(0, a.vocab, true, nullptr) : pieces(true, nullptr)) != QLESS_OK) return s;
-        if ((s = rows(ROW_REFERENCE, pl.entries, &meta->redo)) != QLESS_OK) return s;
+        if (!close && (s = rows(ROW_REFERENCE, pl.entries, &meta->redo)) != QLESS_OK) return s;
         if ((s = one ? probs(0, a.vocab, true, &meta->redo) : pieces(true, &meta->redo)) != QLESS_OK) return s;
         if (one && (s = grads(0, a.vocab, nullptr)) != QLESS_OK) return s;
         if (!close && (s = rows(ROW_FROM_SUMS, pl.entries, nullptr)) != QLESS_OK) return s;

@@ -244,3 +244,29 @@ def test_on_another_stream():
     B.qless_lm_loss(*case, out=out, workspace=ws, stream=st)
     st.synchronize()
     assert torch.equal(out["loss"], want["loss"]) and torch.equal(out["grad_hidden"], want["grad_hidden"])
+
+
+@pytest.mark.parametrize("T,keep", [(256, 1.0), (300, 1.0), (1100, 0.5), (140_000, 0.003)])
+def test_a_second_pass_at_every_layout(T, keep):
+    # a row far above its label, in either orientation of the products and with one or several pieces of the vocabulary (the last: three)
+    width, vocab = 128, 5000
+    hidden, weight, labels, tw = _case(T, width, vocab, 41, keep)
+    live = (labels >= 0).nonzero()[:, 0]
+    a, b, c = (int(live[i]) for i in (0, len(live) // 2, -1))
+    weight = weight.clone()
+    weight[4990] = hidden[a]
+    weight[10] = hidden[c]
+    labels[a], labels[b], labels[c] = 7, 4990, 4991
+    assert float(hidden[a].double() @ (weight[4990] - weight[7]).double()) > 64 * 0.6932
+    got = B.qless_lm_loss(hidden, weight, labels, tw)
+    B.qless_check()
+    ref = reference(hidden[live], weight, labels[live], tw[live])
+    check(dict(loss=got["loss"][live], grad_hidden=got["grad_hidden"][live], grad_weight=None), ref, len(live), vocab)
+    again = B.qless_lm_loss(hidden, weight, labels, tw)
+    assert torch.equal(got["loss"], again["loss"]) and torch.equal(got["grad_hidden"], again["grad_hidden"])
+    # and a call that needs none, after one that did
+    plain = _case(T, width, vocab, 43, keep)
+    live = (plain[2] >= 0).nonzero()[:, 0]
+    got = B.qless_lm_loss(*plain)
+    check(dict(loss=got["loss"][live], grad_hidden=got["grad_hidden"][live], grad_weight=None),
+          reference(plain[0][live], plain[1], plain[2][live], plain[3][live]), len(live), vocab)
