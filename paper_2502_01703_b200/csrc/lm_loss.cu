@@ -1,4 +1,4 @@
-// Softmax cross entropy of a language model's head over a large vocabulary, with its gradient; the logits are never kept.
+// Softmax cross entropy of a language model's head over a large vocabulary, with its gradient; the logits are not kept (but for few tokens).
 //
 //   l_tv = <h_t, W_v>;  loss_t = logsumexp_v l_tv - l_t,y;  dh_t = w_t (sum_v p_tv W_v - W_y);  dW_v = sum_t w_t (p_tv - [v = y_t]) h_t
 //
@@ -23,7 +23,10 @@
 // LIMIT = 64 powers of two (a loss of 44) below the row's maximum is as good as the maximum itself. Should a row exceed that, a flag
 // sends the rest through a second pass whose reference is the true maximum: its launches are always enqueued and return at once
 // when the flag is not set (the host does not wait to find out).
-// With dW the normaliser has to be known before the piece is written: STATS first, then PROBS, GRAD_H and GRAD_W per piece.
+// With dW the normaliser has to be known before the piece is written: STATS first, then PROBS, GRAD_H and GRAD_W per piece. (Left for the
+// hidden rows of GRAD_W to carry, the normaliser would round them to bf16 once more.) Up to FEW tokens STATS leaves its logits and
+// loss_softmax_kernel makes the piece of them instead of a second product: 64 tokens x 4096 x 32001 246 -> 212 us, 16 x 4096 x 131072
+// 782 -> 620 us. With many tokens writing and reading fp32 logits would take as long as the product (4096 x 2048 x 50021: 2.0 GB, 330 us).
 #include "qless_kernels.h"
 #include "tc_common.cuh"
 
@@ -63,6 +66,7 @@ struct GemmParams {
     int32_t entries;
     float2* stat;                           // [entries per tile * tiles][tpad]: (maximum, sum relative to it; PROBS: to the row's reference), PROBS: or NULL
     int32_t tile0;                          // tile index of the launch's first column tile in stat
+    float* logits;                          // swapped STATS: NULL, or [tpad][ld_out] logits
     __nv_bfloat16* out;                     // PROBS: piece [tpad][ld_out]; GRAD_W: rows of dW
     int64_t ld_out;
     float* acc;                             // GRAD_H: [splits][row tiles * 256][cols]
@@ -75,7 +79,7 @@ struct GemmParams {
 struct __align__(8) Bars {
     uint64_t full[MAX_STAGES], empty[MAX_STAGES], d_full[2], d_empty[2], drain;
     uint32_t tmem_base, abort_flag;
-    __align__(16) RowParam rowp[FEW];       // swapped roles: of every token
+    float ref[FEW];                         // swapped roles: of every token
     int32_t label[FEW];
 };
 
@@ -279,13 +283,13 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
         if (SWAP && MODE != GRAD_H && !idle) {
             for (int t = threadIdx.x - 64; t < count; t += 256) {
                 bars->label[t] = p.labels[t];
-                if (MODE == PROBS && p.first == nullptr) bars->rowp[t] = p.rowp[t];
+                if (MODE == PROBS && p.first == nullptr) bars->ref[t] = p.rowp[t].r2;
                 if (MODE == PROBS && p.first != nullptr) {           // every block for itself; block 0 also for loss_close_kernel
                     float m = -INFINITY;
 #pragma unroll 4
                     for (int i = 0; i < p.entries; ++i) m = fmaxf(m, p.first[(int64_t)i * p.tpad + t].x);
-                    bars->rowp[t] = RowParam{m > -INFINITY ? m : 0.0f, 1.0f, 0.0f, 0.0f};
-                    if (blockIdx.x == 0) p.rowp[t] = bars->rowp[t];
+                    bars->ref[t] = m > -INFINITY ? m : 0.0f;
+                    if (blockIdx.x == 0) p.rowp[t].r2 = bars->ref[t];
                 }
             }
             asm volatile("bar.sync 1, 256;" ::: "memory");
@@ -297,14 +301,13 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
             const int v = m * 256 + (int)rank * 128 + q * 32 + lane;
             const uint32_t buf = n_acc & 1u;
             const int lim = min(count - half * p.b_rows, p.b_rows);      // tokens of this half
-            const int upto = MODE == PROBS ? min(((count + 15) & ~15) - half * p.b_rows, p.b_rows) : lim;      // (b_rows is a multiple of 16)
             bool ok = mbar_wait_cluster(smem_u32(&bars->d_full[buf]), (n_acc >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
             tc_fence_after();
             float run_max = -INFINITY;
 #pragma unroll 1
-            for (int c0 = 0; c0 < upto; c0 += 32) {
+            for (int c0 = 0; c0 < lim; c0 += 32) {
                 uint32_t raw[32];
                 tmem_ld_x32(tmem + lane_base + buf * 256 + half * p.b_rows + c0, raw);
                 tmem_wait_ld();
@@ -325,6 +328,12 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                 float e[32];
                 const int64_t entry = ((int64_t)(p.tile0 + m) * 2 + rank) * 4 + q;
                 if (MODE == STATS) {
+                    if (p.logits != nullptr && v < p.cols) {
+                        float* dst = p.logits + (int64_t)t0 * p.ld_out + v;
+#pragma unroll
+                        for (int k = 0; k < 32; ++k)
+                            if (k < have) dst[(int64_t)k * p.ld_out] = __uint_as_float(raw[k]);
+                    }
                     float top[32];
 #pragma unroll
                     for (int k = 0; k < 32; ++k) {
@@ -342,31 +351,25 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                     float top[32];
 #pragma unroll
                     for (int k = 0; k < 32; ++k) {
-                        top[k] = -INFINITY;
+                        top[k] = -INFINITY; e[k] = 0.0f;
                         if (k < have) {
-                            const RowParam rp = bars->rowp[t0 + k];
-                            const bool own = bars->label[t0 + k] == p.col0 + v, out = own || v >= p.cols;
+                            const float ref = bars->ref[t0 + k];
+                            const bool out = v >= p.cols || bars->label[t0 + k] == p.col0 + v;
                             if (!out) top[k] = __uint_as_float(raw[k]);
-                            const float x = out ? -INFINITY : fmaf(__uint_as_float(raw[k]), LOG2E, -rp.r2);
+                            const float x = fmaf(top[k], LOG2E, -ref);
                             run_max = fmaxf(run_max, x);
-                            e[k] = ex2(x);
-                            dst[(int64_t)k * p.ld_out] = __float2bfloat16_rn(own ? rp.wl : e[k] * rp.w);
-                        } else {
-                            e[k] = 0.0f;
-                            // GRAD_W contracts over steps of 16 tokens
-                            if (c0 + k < upto) dst[(int64_t)k * p.ld_out] = __float2bfloat16_rn(0.0f);
+                            e[k] = out ? 0.0f : ex2(x);
+                            dst[(int64_t)k * p.ld_out] = __float2bfloat16_rn(e[k]);
                         }
                     }
-                    if (p.stat != nullptr) {
-                        const float sum = across_lanes<false>(e, lane), most = across_lanes<true>(top, lane) * LOG2E;
-                        if (lane < have) p.stat[entry * p.tpad + t0 + lane] = make_float2(most, sum);
-                    }
+                    const float sum = across_lanes<false>(e, lane), most = across_lanes<true>(top, lane) * LOG2E;
+                    if (lane < have) p.stat[entry * p.tpad + t0 + lane] = make_float2(most, sum);
                 }
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_leader_tmem(smem_u32(&bars->d_empty[buf]), rank);
-            if (MODE == PROBS && p.stat != nullptr && run_max > LIMIT) *p.redo = 1;
+            if (MODE == PROBS && run_max > LIMIT) *p.redo = 1;
         }
         for (int64_t item = pair; !SWAP && item < items; item += num_pairs, ++n_acc) {
             int split, m, n, kb0, kb1;
@@ -730,6 +733,43 @@ __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowArgs a)
     }
 }
 
+// Few tokens, gradient of the weights: the logits of the first product stay (at most 1 KiB per column of the vocabulary; they are read
+// from L2), and with the normaliser known this takes the place of a second reading of W: w (p - [v = y]) as bf16 for one piece of the
+// vocabulary, zero behind its last column and for the rows behind the last token up to a multiple of 16 (GRAD_W contracts over those).
+struct SoftmaxArgs {
+    const LossMeta* meta;
+    const float* logits;
+    int64_t ld, ld_out;
+    int32_t col0, cols, vecs;               // vecs: groups of eight columns of the piece, up to a whole tile
+    const int32_t* labels;
+    const RowParam* rowp;
+    __nv_bfloat16* out;
+};
+__global__ void loss_softmax_kernel(const SoftmaxArgs a)
+{
+    ahead_release();
+    ahead_wait();
+    const int count = a.meta->count;
+    const int64_t total = (int64_t)((count + 15) & ~15) * a.vecs;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
+        const int t = (int)(i / a.vecs), c = (int)(i - (int64_t)t * a.vecs) * 8;
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = 0.0f;
+        if (t < count) {
+            const RowParam rp = a.rowp[t];
+            const int lab = a.labels[t] - a.col0 - c;
+            const float4* src = reinterpret_cast<const float4*>(a.logits + (int64_t)t * a.ld + a.col0 + c);      // the rows have room up to a whole tile
+            const float4 u = src[0], v = src[1];
+            const float l[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (c + k < a.cols) x[k] = k == lab ? rp.wl : rp.w * ex2(fmaf(l[k], LOG2E, -rp.r2));
+        }
+        *reinterpret_cast<uint4*>(a.out + (int64_t)t * a.ld_out + c) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+    }
+}
+
 // Eight columns of a gradient row: joins the slices of the vocabulary. `sums`: the accumulator holds sum exp2(l2 - r2) W_v over the
 // other columns, `k` is the row's coef and `y` the label's row of W; otherwise it holds the finished gradient.
 __device__ __forceinline__ uint4 finish8(const float* __restrict__ acc, int64_t slice, int splits, bool sums, float2 k, const __nv_bfloat16* __restrict__ y)
@@ -888,6 +928,7 @@ LossPlan plan_loss(int64_t T, int32_t width, int32_t vocab, bool want_h, bool wa
     pl.stat_off = take((size_t)pl.entries * pl.tpad * (pl.few && !pl.exact ? 16 : 8));      // (few: a second pass has its own)
     pl.hidden_off = take((size_t)pl.tpad * width * 2);
     pl.piece_off = (want_h || want_w) ? take((size_t)pl.tpad * pl.piece * 2) : 0;
+    pl.logits_off = pl.few && want_w ? take((size_t)pl.tpad * tiles_v * 256 * 4) : 0;
     pl.acc_off = want_h ? take((size_t)cap * 256 * width * 4) : 0;
     pl.total = off + 256;
     return pl;
@@ -908,8 +949,10 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
     __nv_bfloat16* piece = reinterpret_cast<__nv_bfloat16*>(ws + pl.piece_off);
     float* acc = reinterpret_cast<float*>(ws + pl.acc_off);
     const bool want_h = a.grad_hidden != nullptr, want_w = a.grad_weight != nullptr;
+    float* logits = pl.few && want_w ? reinterpret_cast<float*>(ws + pl.logits_off) : nullptr;
     const int64_t mt = pl.tpad / 256, nt_h = (a.width + 255) / 256;
     const int32_t tiles_v = (a.vocab + 255) / 256;
+    const int64_t ld_logits = (int64_t)tiles_v * 256;
 
     { ProfileScope ps("loss_gather", st);
       // a block lists at most LIST of the 1024 tokens of a step: at least four blocks
@@ -948,7 +991,7 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
     base.meta = meta; base.tpad = pl.tpad; base.labels = labels; base.rowp = rowp; base.b_rows = b_rows; base.timeout_word = timeout_word;
     auto stats = [&](int32_t cols) {
         GemmParams p = base;
-        p.cols = cols; p.k = a.width; p.stat = stat; p.a_whole = p.b_whole = whole;
+        p.cols = cols; p.k = a.width; p.stat = stat; p.a_whole = p.b_whole = whole; p.logits = logits; p.ld_out = ld_logits;
         const int64_t tiles = (cols + 255) / 256;
         return few ? launch_gemm<STATS, true>("loss_stats", tm_w, tm_x, p, tiles, st) : launch_gemm<STATS, false>("loss_stats", tm_x, tm_w, p, mt * tiles, st);
     };
@@ -962,7 +1005,16 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
         return QLESS_OK;
     };
     const bool close = few && !pl.exact;
-    auto probs = [&](int32_t v0, int32_t cols, bool keep_sums, const int32_t* gate) {
+    auto probs = [&](int32_t v0, int32_t cols, bool keep_sums, const int32_t* gate) -> qless_status {
+        if (logits != nullptr) {
+            SoftmaxArgs f{};
+            f.meta = meta; f.logits = logits; f.ld = ld_logits; f.ld_out = pl.piece; f.col0 = v0; f.cols = cols; f.vecs = (cols + 255) / 256 * 32; f.labels = labels;
+            f.rowp = rowp; f.out = piece;
+            { ProfileScope ps("loss_softmax", st);
+              QLESS_CUDA_TRY(launch_ahead(loss_softmax_kernel, dim3(grid_of((a.T + 15) / 16 * 16 * f.vecs, 256)), dim3(256), 0, st, f)); }
+            count_launches(1);
+            return QLESS_OK;
+        }
         GemmParams p = base;
         p.gate = gate; p.cols = cols; p.col0 = v0; p.k = a.width; p.out = piece; p.ld_out = pl.piece; p.tile0 = v0 / 256;
         p.stat = keep_sums ? stat : nullptr; p.redo = &meta->redo; p.a_whole = p.b_whole = whole;

@@ -270,3 +270,14 @@ def test_a_second_pass_at_every_layout(T, keep):
     got = B.qless_lm_loss(*plain)
     check(dict(loss=got["loss"][live], grad_hidden=got["grad_hidden"][live], grad_weight=None),
           reference(plain[0][live], plain[1], plain[2][live], plain[3][live]), len(live), vocab)
+
+
+@pytest.mark.parametrize("T,wants", [(3, (True, True)), (40, (False, True)), (5, (True, False))])
+def test_few_tokens_over_a_vocabulary_of_several_pieces(T, wants):
+    # up to 256 tokens a piece holds 2^20 columns
+    width, vocab = 16, (1 << 20) + 1000
+    hidden, weight, labels, tw = _case(T, width, vocab, 47)
+    labels[0], labels[1], labels[2] = vocab - 1, (1 << 20) - 1, 1 << 20
+    got = B.qless_lm_loss(hidden, weight, labels, tw, want_hidden=wants[0], want_weight=wants[1])
+    B.qless_check()
+    check(got, reference(hidden, weight, labels, tw), T, vocab)
