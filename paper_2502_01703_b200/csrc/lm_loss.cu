@@ -100,29 +100,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
     return *reinterpret_cast<const uint32_t*>(&z);
 }
 
-// Four neighbouring lanes hold four 16-byte pieces each of a row of their own; afterwards lane i of the four holds piece i of each of the
-// four rows: a store instruction then covers 64 consecutive bytes of eight rows instead of 16 of thirty-two (GRAD_W of 23 tokens x
-// 3424 x 65225, whose time is its stores).
-__device__ __forceinline__ void transpose4(uint4 (&v)[4], int lane)
-{
-    auto swap = [](uint4 a, int m) {
-        a.x = __shfl_xor_sync(0xFFFFFFFFu, a.x, m); a.y = __shfl_xor_sync(0xFFFFFFFFu, a.y, m);
-        a.z = __shfl_xor_sync(0xFFFFFFFFu, a.z, m); a.w = __shfl_xor_sync(0xFFFFFFFFu, a.w, m);
-        return a;
-    };
-#pragma unroll
-    for (int m = 1; m <= 2; m <<= 1) {
-        const bool up = (lane & m) != 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (k & m) continue;
-            const uint4 got = swap(up ? v[k] : v[k + m], m);
-            if (up) v[k] = got;
-            else v[k + m] = got;
-        }
-    }
-}
-
 // Sum (or maximum) over the 32 lanes of each of 32 values: lane L ends with that of value L, after 31 shuffles.
 template <bool MAX>
 __device__ __forceinline__ float across_lanes(float (&v)[32], int lane)

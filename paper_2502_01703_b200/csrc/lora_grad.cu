@@ -6,8 +6,8 @@
 //   row e of the gradient matrix = [dA_e row-major | dB_e row-major].
 //
 // Both steps read x^ and dY once and do 2 r multiply-adds per element read: memory-bound work on the tensor cores. Measured, 128 examples of 65 536
-// tokens in all, 4096 -> 4096, rank 64, bf16 gradients: (1) 157 us, 5.1 TB/s of codes and dY; (2) 213 us, 3.8 TB/s and 134 MB of rows. In (2) stores,
-// expansion and products each cost a seventh (without one of them 186 to 190 us, without all three 138).
+// tokens in all, 4096 -> 4096, rank 64, bf16 gradients: (1) 157 us, 5.1 TB/s of codes and dY; (2) 201 us, 4.0 TB/s and 134 MB of rows. (2) waits for its
+// copies most of the time (converters 60 %), the products' issue takes 55 % of its clocks and a block of codes 1300 of the 5600 that a stage lives.
 // (1) lora_factors_kernel: M = 128 tokens, K = channels. The codes go TMA -> shared memory -> registers -> tensor memory as bf16
 //     (exact: a code has 8 significant bits and the step is a power of two), from where the MMA takes its A operand; dY goes TMA ->
 //     MMA as stored. fp32 sums over a slice of the channels; lora_split_kernel adds the slices.
@@ -40,7 +40,7 @@ constexpr int TILE = 256;                   // (2) channels per item
 // fp32 gradients: an accumulator in tensor memory takes at most SPAN channels or tokens (half as many tokens where three terms share it), then the
 // epilogue adds it to the sum so far in global memory (always the same thread; in L2). The tensor core cuts the sum's last bits at each of its steps
 // of 16 instead of rounding them, so a sum's error grows with its length, one way: 8 examples of 512 tokens, 4096 -> 4096, rank 64: 1.6e-6 of the norm
-// with sums taken whole, 5.4e-7 so (fp32 products elsewhere: 4.4e-7), for 125 -> 145 us with 32 examples of 16 381 tokens (spans of 256: 2.7e-7, and
+// with sums taken whole, 5.4e-7 so (fp32 products elsewhere: 4.4e-7), for 125 -> 140 us with 32 examples of 16 381 tokens (spans of 256: 2.7e-7, and
 // twice the additions). bf16 gradients are rounded to 8 bits and take their sums whole.
 constexpr int SPAN = 512;
 
@@ -109,6 +109,10 @@ __device__ __forceinline__ uint32_t load_step_bytes(const uint8_t* p, int n, boo
     uint32_t v = 0u;
     if (whole && n == 4) {
         asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v) : "l"(p));
+    } else if (whole && n == 2) {
+        asm volatile("ld.global.nc.u16 %0, [%1];" : "=r"(v) : "l"(p));
+    } else if (n == 1) {
+        asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(v) : "l"(p));
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -446,38 +450,87 @@ template <typename OutT> __device__ __forceinline__ OutT to_out(float v);
 template <> __device__ __forceinline__ float to_out<float>(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// One thread's 16 accumulator columns [c0, c0 + 16) of channel ch -> dA (column j of the row-major [rank, width]) or dB (row ch).
-template <typename OutT>
-__device__ __forceinline__ void store_columns(OutT* dst, bool is_x, int64_t ch, int64_t width, int c0, int rank, const uint32_t (&v)[16], bool zero,
-                                              bool add)
+// A warp's 16 accumulator columns [c0, c0 + 16) of the channels ch0 + lane -> dA (column of the row-major [rank, width]) or dB (rows of
+// `rank` numbers), or added to what the spans before have left there. Lanes exchange pieces so that an instruction writes whole sectors, 64
+// bytes of a row of dA or dB at a time where it can (bf16: 128 stores of 64 bytes for a tile of dA took 11.6 k clocks, longer than its products).
+__device__ __forceinline__ void store_columns(float* dst, bool is_x, int64_t ch0, int lane, int64_t width, int c0, int rank, const uint32_t (&v)[16], bool add)
 {
-    if (sizeof(OutT) == 4 && add) {                            // onto what the spans before have left there
-        float* sum = reinterpret_cast<float*>(dst);
-        if (is_x) {
+    if (is_x) {
+        const int64_t ch = ch0 + lane;
+        if (ch >= width) return;
+        if (add) {
 #pragma unroll
             for (int j = 0; j < 16; ++j)
-                if (c0 + j < rank) add_to(sum + (int64_t)(c0 + j) * width + ch, v[j]);
+                if (c0 + j < rank) add_to(dst + (int64_t)(c0 + j) * width + ch, v[j]);
         } else {
 #pragma unroll
-            for (int j = 0; j < 16; j += 4)
-                if (c0 + j < rank) add4_to(sum + ch * rank + c0 + j, v[j], v[j + 1], v[j + 2], v[j + 3]);
+            for (int j = 0; j < 16; ++j)
+                if (c0 + j < rank) dst[(int64_t)(c0 + j) * width + ch] = __uint_as_float(v[j]);
         }
-        return;
+    } else if (add) {
+        float* row = dst + (ch0 + lane) * rank + c0;           // 16-byte aligned: rank is a multiple of 8
+        if (ch0 + lane >= width) return;
+#pragma unroll
+        for (int j = 0; j < 16; j += 4)
+            if (c0 + j < rank) add4_to(row + j, v[j], v[j + 1], v[j + 2], v[j + 3]);
+    } else {
+        uint4 w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+        transpose4(w, lane);
+        const int c = c0 + (lane & 3) * 4;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t ch = ch0 + (lane & ~3) + k;
+            if (ch >= width || c >= rank) continue;
+            *reinterpret_cast<uint4*>(dst + ch * rank + c) = w[k];
+        }
+    }
+}
+__device__ __forceinline__ void store_columns(__nv_bfloat16* dst, bool is_x, int64_t ch0, int lane, int64_t width, int c0, int rank, const uint32_t (&v)[16], bool)
+{
+    uint32_t a[8];                                             // columns 2 i and 2 i + 1 of this lane's channel
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const __nv_bfloat162 z = __floats2bfloat162_rn(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+        a[i] = *reinterpret_cast<const uint32_t*>(&z);
     }
     if (is_x) {
+        // 8 x 8 transposes among eight lanes: afterwards lane L holds eight channels of columns L % 8 and 8 + L % 8
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (c0 + j < rank) dst[(int64_t)(c0 + j) * width + ch] = to_out<OutT>(zero ? 0.0f : __uint_as_float(v[j]));
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, a[i], 1);
+            a[i] = (lane & 1) ? __byte_perm(got, a[i], 0x7632) : __byte_perm(a[i], got, 0x5410);
+        }
+        uint32_t b[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool up = (lane & 2) != 0;
+            const uint32_t got = __shfl_xor_sync(0xFFFFFFFFu, up ? a[2 * i] : a[2 * i + 1], 2);
+            b[i][0] = up ? got : a[2 * i];
+            b[i][1] = up ? a[2 * i + 1] : got;
+        }
+        const int64_t ch = ch0 + (lane & ~7);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const bool up = (lane & 4) != 0;
+            const uint32_t g0 = __shfl_xor_sync(0xFFFFFFFFu, up ? b[2 * i][0] : b[2 * i + 1][0], 4), g1 = __shfl_xor_sync(0xFFFFFFFFu, up ? b[2 * i][1] : b[2 * i + 1][1], 4);
+            const uint4 o = up ? make_uint4(g0, g1, b[2 * i + 1][0], b[2 * i + 1][1]) : make_uint4(b[2 * i][0], b[2 * i][1], g0, g1);
+            const int c = c0 + 8 * i + (lane & 7);
+            if (ch < width && c < rank) *reinterpret_cast<uint4*>(dst + (int64_t)c * width + ch) = o;      // the width is a multiple of 16
+        }
     } else {
-        OutT* row = dst + ch * rank + c0;                      // 16-byte aligned: rank is a multiple of 8
+        const bool up = (lane & 1) != 0;                       // even lanes write columns c0 .. c0 + 7 of two rows, odd ones the next eight
+        uint32_t got[4];
 #pragma unroll
-        for (int j = 0; j < 16; j += 8) {
-            if (c0 + j >= rank) break;
-            __align__(16) OutT o[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) o[k] = to_out<OutT>(zero ? 0.0f : __uint_as_float(v[j + k]));
-#pragma unroll
-            for (int k = 0; k < (int)(8 * sizeof(OutT) / 16); ++k) reinterpret_cast<uint4*>(row + j)[k] = reinterpret_cast<const uint4*>(o)[k];
+        for (int k = 0; k < 4; ++k) got[k] = __shfl_xor_sync(0xFFFFFFFFu, up ? a[k] : a[4 + k], 1);
+        const uint4 o0 = up ? make_uint4(got[0], got[1], got[2], got[3]) : make_uint4(a[0], a[1], a[2], a[3]);
+        const uint4 o1 = up ? make_uint4(a[4], a[5], a[6], a[7]) : make_uint4(got[0], got[1], got[2], got[3]);
+        const int64_t ch = ch0 + (lane & ~1);
+        const int c = c0 + (up ? 8 : 0);
+        if (c < rank && ch < width) {                          // (the width is even)
+            *reinterpret_cast<uint4*>(dst + ch * rank + c) = o0;
+            *reinterpret_cast<uint4*>(dst + (ch + 1) * rank + c) = o1;
         }
     }
 }
@@ -516,14 +569,25 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
 
     const uint32_t items = (uint32_t)p.items, step_items = gridDim.x;
     constexpr int span = sizeof(OutT) == 4 ? (BOXES == 6 ? SPAN / 2 : SPAN) : 1 << 30;
-    auto chunk_of = [&](uint32_t item) {
-        const uint32_t k = min(item, items - 1) / (uint32_t)p.tiles;
-        return p.chunks != nullptr ? p.chunks[k] : p.few[k];
+    // The items of a block, one after another (chunk k, channel tile; no divisions on the way), with the next one's chunk already requested.
+    const uint32_t tiles = (uint32_t)p.tiles, last = (items - 1) / tiles, step_k = step_items / tiles, step_tile = step_items - step_k * tiles;
+    struct Walk { uint32_t item, k, tile, next_k, next_tile; LoraChunk c, ahead; bool is_x; int ch0; };
+    auto chunk_at = [&](uint32_t k) { return p.chunks != nullptr ? p.chunks[min(k, last)] : p.few[min(k, last)]; };
+    auto look = [&](Walk& w) {
+        w.is_x = (int)w.tile < p.tiles_x;
+        w.ch0 = (w.is_x ? (int)w.tile : (int)w.tile - p.tiles_x) * TILE;
+        w.next_k = w.k + step_k; w.next_tile = w.tile + step_tile;
+        if (w.next_tile >= tiles) { w.next_tile -= tiles; ++w.next_k; }
+        w.ahead = chunk_at(w.next_k);
     };
-    auto place_of = [&](uint32_t item, bool& is_x, int& ch0) {
-        const int tile = (int)(item % (uint32_t)p.tiles);
-        is_x = tile < p.tiles_x;
-        ch0 = (is_x ? tile : tile - p.tiles_x) * TILE;
+    auto first_item = [&](Walk& w) {
+        w.item = blockIdx.x; w.k = w.item / tiles; w.tile = w.item - w.k * tiles;
+        w.c = chunk_at(w.k);
+        look(w);
+    };
+    auto next_item = [&](Walk& w) {
+        w.item += step_items; w.k = w.next_k; w.tile = w.next_tile; w.c = w.ahead;
+        look(w);
     };
 
     // A wait of a whole warp: the same answer in every lane.
@@ -537,12 +601,10 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
             uint32_t it = 0;
             Ring ring;
             bool ok = true;
-            LoraChunk ahead = chunk_of(blockIdx.x);
-            for (uint32_t item = blockIdx.x; item < items && ok; item += step_items) {
-                const LoraChunk c = ahead;
-                ahead = chunk_of(item + step_items);
-                bool is_x; int ch0;
-                place_of(item, is_x, ch0);
+            Walk w;
+            for (first_item(w); w.item < items && ok; next_item(w)) {
+                const LoraChunk c = w.c;
+                const bool is_x = w.is_x; const int ch0 = w.ch0;
                 for (int t = 0; t < c.len; t += TOK, ++it, ring.next(nS)) {
                     if (!warp_wait(&bars->empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
                     const uint32_t full = smem_u32(&bars->full[ring.slot]);
@@ -572,12 +634,10 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
             Ring ring;
             uint32_t n = 0;
             bool ok = true;
-            LoraChunk ahead = chunk_of(blockIdx.x);
-            for (uint32_t item = blockIdx.x; item < items && ok; item += step_items) {
-                const LoraChunk c = ahead;
-                ahead = chunk_of(item + step_items);
-                bool is_x; int ch0;
-                place_of(item, is_x, ch0);
+            Walk w;
+            for (first_item(w); w.item < items && ok; next_item(w)) {
+                const LoraChunk c = w.c;
+                const bool is_x = w.is_x; const int ch0 = w.ch0;
                 const int subs = (is_x ? p.in : p.out) - ch0 > 128 ? 2 : 1;
                 for (int t0 = 0; (t0 < c.len || t0 == 0) && ok; t0 += span, ++n) {
                     const uint32_t buf = n & 1u;
@@ -619,44 +679,37 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
         const int tid = (threadIdx.x - 64) & 127, tok = tid & 63, box = tid >> 6;
         const uint32_t grp = (uint32_t)(warp - 2) >> 2;
         const int groups = (p.in + p.group - 1) / p.group, per = 128 / p.group;
-        struct Cursor { uint32_t item; LoraChunk c; bool is_x; int ch0, t; Ring ring; } cur;
-        // The next block of this group, at or behind the cursor's place.
-        auto seek = [&](Cursor& q) {
-            while (q.item < items) {
-                if (q.t >= q.c.len) {
-                    q.item += step_items;
-                    if (q.item >= items) return;
-                    q.c = chunk_of(q.item);
-                    place_of(q.item, q.is_x, q.ch0);
-                    q.t = 0;
-                    continue;
-                }
-                if (q.ring.slot == grp) return;
-                q.t += TOK; q.ring.next(nS);
+        // The group's blocks are every nS-th of all; `blk` is the block's place within the walk's item.
+        Walk w;
+        first_item(w);
+        int blk = (int)grp, blocks = (w.c.len + TOK - 1) / TOK;
+        auto settle = [&]() {
+            while (blk >= blocks && w.item < items) {
+                blk -= blocks;
+                next_item(w);
+                blocks = (w.c.len + TOK - 1) / TOK;
             }
         };
-        auto step_over = [&](Cursor& q) { q.t += TOK; q.ring.next(nS); };
-        auto load_steps = [&](const Cursor& q) -> uint32_t {
-            const int g0 = (q.ch0 + box * 128) / p.group;
-            return (q.item < items && q.is_x && q.t + tok < q.c.len)
-                       ? load_step_bytes(p.scales + (q.c.t0 + q.t + tok) * p.ld_scales + g0, min(per, groups - g0), p.steps_whole != 0) : 0u;
+        auto load_steps = [&]() -> uint32_t {
+            const int g0 = (w.ch0 + box * 128) / p.group, t = blk * TOK + tok;
+            return (w.item < items && w.is_x && t < w.c.len)
+                       ? load_step_bytes(p.scales + (w.c.t0 + t) * p.ld_scales + g0, min(per, groups - g0), p.steps_whole != 0) : 0u;
         };
-        cur.item = grp < nS ? blockIdx.x : items; cur.t = 0;
-        cur.c = chunk_of(cur.item);
-        place_of(cur.item, cur.is_x, cur.ch0);
-        seek(cur);
-        uint32_t step = load_steps(cur), read_parity = 0u;
-        while (cur.item < items) {
-            Cursor nxt = cur;
-            step_over(nxt);
-            seek(nxt);
-            const uint32_t step_next = load_steps(nxt);
-            const int live = min(TOK, cur.c.len - cur.t);        // token rows of this block that belong to the chunk
-            bool ok = mbar_wait(smem_u32(&bars->full[cur.ring.slot]), cur.ring.parity, abort_flag, p.timeout_word, TO_UNPACK);
+        if (grp >= nS) w.item = items;
+        settle();
+        uint32_t step = load_steps(), parity = 0u, read_parity = 0u;
+        while (w.item < items) {
+            const bool is_x = w.is_x;
+            const int live = min(TOK, w.c.len - blk * TOK);      // token rows of this block that belong to the chunk
+            blk += (int)nS;
+            settle();
+            const uint32_t step_next = load_steps();
+            bool ok = mbar_wait(smem_u32(&bars->full[grp]), parity, abort_flag, p.timeout_word, TO_UNPACK);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
-            uint8_t* big = smem + (size_t)cur.ring.slot * stage_bytes;
-            if (cur.is_x) {
+            parity ^= 1u;
+            uint8_t* big = smem + (size_t)grp * stage_bytes;
+            if (is_x) {
                 const uint4* src = reinterpret_cast<const uint4*>(big + box * 8192 + tok * 128);
                 uint4 raw[8];
 #pragma unroll
@@ -686,31 +739,28 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
                 }
             }
             if (live < TOK) {                                    // rows of the next example: zero in the factors, and in dY
-                const int from = cur.is_x ? 4 : 0, rows = TOK - live;
+                const int from = is_x ? 4 : 0, rows = TOK - live;
                 for (int i = tid; i < (4 - from + boxes) * rows * 8; i += 128) {
                     const int b = from + i / (rows * 8), rest = i % (rows * 8);
                     *reinterpret_cast<uint4*>(big + b * 8192 + (live + (rest >> 3)) * 128 + (rest & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
                 }
             }
-            if (cur.is_x || live < TOK) {
+            if (is_x || live < TOK) {
                 fence_proxy_async_smem();
                 __syncwarp();
             }
-            if (lane == 0) mbar_arrive(smem_u32(&bars->ready[cur.ring.slot]));
-            cur = nxt;
+            if (lane == 0) mbar_arrive(smem_u32(&bars->ready[grp]));
             step = step_next;
         }
     } else {
         const int row = (warp & 3) * 32 + lane;
         const int64_t width_all = (int64_t)p.rank * (p.in + p.out);
         uint32_t n = 0;
-        LoraChunk ahead = chunk_of(blockIdx.x);
         bool ok = true;
-        for (uint32_t item = blockIdx.x; item < items && ok; item += step_items) {
-            const LoraChunk c = ahead;
-            ahead = chunk_of(item + step_items);
-            bool is_x; int ch0;
-            place_of(item, is_x, ch0);
+        Walk w;
+        for (first_item(w); w.item < items && ok; next_item(w)) {
+            const LoraChunk c = w.c;
+            const bool is_x = w.is_x; const int ch0 = w.ch0;
             const int width = is_x ? p.in : p.out;
             for (int t0 = 0; t0 < c.len || t0 == 0; t0 += span, ++n) {
                 const uint32_t buf = n & 1u;
@@ -721,7 +771,7 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
                 const int64_t base = is_x ? 0 : (int64_t)p.rank * p.in;
                 for (int m = 0; m < 2; ++m) {
                     if (ch0 + m * 128 >= width) break;
-                    const int64_t ch = ch0 + m * 128 + row;
+                    const int64_t ch = ch0 + m * 128 + (warp & 3) * 32;
                     for (int c0 = 0; c0 < p.rank; c0 += 16) {
                         uint32_t v[16];
                         const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + buf * 256 + m * 128 + c0;
@@ -737,10 +787,12 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
                                 for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(low[j]));
                             }
                         }
-                        if (ch < width) {
-                            if (c.slot >= 0) store_columns<float>(p.part + (int64_t)c.slot * width_all + base, is_x, ch, width, c0, p.rank, v, c.len == 0, t0 > 0);
-                            else store_columns<OutT>(reinterpret_cast<OutT*>(p.grads) + (int64_t)c.example * p.ld_grads + base, is_x, ch, width, c0, p.rank, v, c.len == 0, t0 > 0);
+                        if (c.len == 0) {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) v[j] = 0u;
                         }
+                        if (c.slot >= 0) store_columns(p.part + (int64_t)c.slot * width_all + base, is_x, ch, lane, width, c0, p.rank, v, PARTS == 3 && t0 > 0);
+                        else store_columns(reinterpret_cast<OutT*>(p.grads) + (int64_t)c.example * p.ld_grads + base, is_x, ch, lane, width, c0, p.rank, v, PARTS == 3 && t0 > 0);
                     }
                 }
                 tc_fence_before();
@@ -866,7 +918,8 @@ qless_status launch_lora(const LoraArgs& a, const LoraPlan& pl, uint8_t* ws, uns
     if ((s = make_tmap_2d_sw128(&m.a, a.T > 0 ? a.lora_a : ws, 2, a.in, a.rank, (uint64_t)a.in * 2, 64, pl.nr)) != QLESS_OK) return s;
     if ((s = make_tmap_2d_sw128(&m.b, a.T > 0 ? a.lora_b : ws, 2, a.rank, a.out, (uint64_t)a.rank * 2, 64, 128)) != QLESS_OK) return s;
     if ((s = make_tmap_blocks_sw128(&m.fac, fac, 2, 2 * boxes, rows, 128, rows * 128, TOK, boxes)) != QLESS_OK) return s;
-    const bool steps_whole = a.group == 32 && reinterpret_cast<uintptr_t>(a.scales) % 4 == 0 && a.ld_scales % 4 == 0;
+    const int per = 128 / a.group;                            // step bytes of 128 channels: one load where they are one aligned word
+    const bool steps_whole = reinterpret_cast<uintptr_t>(a.scales) % per == 0 && a.ld_scales % per == 0;
     if (a.T > 0) {
         FactorParams f;
         f.T = a.T; f.ld_scales = a.ld_scales; f.scales = a.scales;
