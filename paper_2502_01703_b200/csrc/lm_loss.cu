@@ -749,28 +749,33 @@ __global__ void loss_softmax_kernel(const SoftmaxArgs a)
     }
 }
 
-// Eight columns of a gradient row: joins the slices of the vocabulary. `sums`: the accumulator holds sum exp2(l2 - r2) W_v over the
-// other columns, `k` is the row's coef and `y` the label's row of W; otherwise it holds the finished gradient.
-__device__ __forceinline__ uint4 finish8(const float* __restrict__ acc, int64_t slice, int splits, bool sums, float2 k, const __nv_bfloat16* __restrict__ y)
+// Eight columns of a gradient row, the slices of the vocabulary joined in order.
+struct Eight { float x[8]; };
+__device__ __forceinline__ Eight sum8(const float* __restrict__ acc, int64_t slice, int splits)
 {
-    float x[8];
+    Eight e;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = 0.0f;
+    for (int j = 0; j < 8; ++j) e.x[j] = 0.0f;
     for (int s = 0; s < splits; ++s) {
         const float4* src = reinterpret_cast<const float4*>(acc + s * slice);
         const float4 a = src[0], b = src[1];
-        x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w; x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
+        e.x[0] += a.x; e.x[1] += a.y; e.x[2] += a.z; e.x[3] += a.w; e.x[4] += b.x; e.x[5] += b.y; e.x[6] += b.z; e.x[7] += b.w;
     }
-    if (sums) {
-        const uint4 w = *reinterpret_cast<const uint4*>(y);
-        const uint32_t yw[4] = {w.x, w.y, w.z, w.w};
+    return e;
+}
+// From sum exp2(l2 - r2) W_v over the other columns to the gradient: `k` is the row's coef, `w` the label's row of W.
+__device__ __forceinline__ void apply8(Eight& e, float2 k, uint4 w)
+{
+    const uint32_t yw[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            x[2 * j] = k.x * (x[2 * j] * k.y - __uint_as_float(yw[j] << 16));
-            x[2 * j + 1] = k.x * (x[2 * j + 1] * k.y - __uint_as_float(yw[j] & 0xFFFF0000u));
-        }
+    for (int j = 0; j < 4; ++j) {
+        e.x[2 * j] = k.x * (e.x[2 * j] * k.y - __uint_as_float(yw[j] << 16));
+        e.x[2 * j + 1] = k.x * (e.x[2 * j + 1] * k.y - __uint_as_float(yw[j] & 0xFFFF0000u));
     }
-    return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+}
+__device__ __forceinline__ uint4 pack8(const Eight& e)
+{
+    return make_uint4(pack_bf16(e.x[0], e.x[1]), pack_bf16(e.x[2], e.x[3]), pack_bf16(e.x[4], e.x[5]), pack_bf16(e.x[6], e.x[7]));
 }
 
 struct FinishArgs {
@@ -803,9 +808,11 @@ __global__ void loss_finish_kernel(const FinishArgs a)
         const int c = (int)(i - t * vecs) * 8;
         const int r = a.place[t];
         uint4 o = make_uint4(0u, 0u, 0u, 0u);
-        if (r >= 0)
-            o = a.sums ? finish8(a.acc + (int64_t)r * a.width + c, slice, splits, true, a.coef[r], a.weight + (int64_t)a.labels[r] * a.ld_weight + c)
-                       : finish8(a.acc + (int64_t)r * a.width + c, slice, splits, false, make_float2(0.0f, 0.0f), nullptr);
+        if (r >= 0) {
+            Eight e = sum8(a.acc + (int64_t)r * a.width + c, slice, splits);
+            if (a.sums) apply8(e, a.coef[r], *reinterpret_cast<const uint4*>(a.weight + (int64_t)a.labels[r] * a.ld_weight + c));      // else finished
+            o = pack8(e);
+        }
         *reinterpret_cast<uint4*>(a.out + t * a.ld_out + c) = o;
     }
 }
@@ -822,6 +829,15 @@ __global__ void __launch_bounds__(512) loss_close_kernel(const FinishArgs a)
     const int64_t slice = (int64_t)(a.meta->count + 255) / 256 * 256 * a.width;
     for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
         const int r = a.place[t];
+        // the first eight columns' sums are on their way while the row's are taken
+        const int v0 = threadIdx.x;
+        Eight e0;
+        uint4 w0 = make_uint4(0u, 0u, 0u, 0u);
+        const __nv_bfloat16* y = r >= 0 ? a.weight + (int64_t)a.labels[r] * a.ld_weight : nullptr;
+        if (r >= 0 && v0 < vecs) {
+            e0 = sum8(a.acc + (int64_t)r * a.width + v0 * 8, slice, splits);
+            w0 = *reinterpret_cast<const uint4*>(y + v0 * 8);
+        }
         if (r >= 0) {
             const float2* stat = a.stat + (a.meta->redo != 0 ? (int64_t)a.entries * a.tpad : 0);
             float s = 0.0f;
@@ -841,9 +857,13 @@ __global__ void __launch_bounds__(512) loss_close_kernel(const FinishArgs a)
             }
             __syncthreads();
         }
-        for (int v = threadIdx.x; v < vecs; v += 512) {
+        for (int v = v0; v < vecs; v += 512) {
             uint4 o = make_uint4(0u, 0u, 0u, 0u);
-            if (r >= 0) o = finish8(a.acc + (int64_t)r * a.width + v * 8, slice, splits, true, coef, a.weight + (int64_t)a.labels[r] * a.ld_weight + v * 8);
+            if (r >= 0) {
+                Eight e = v == v0 ? e0 : sum8(a.acc + (int64_t)r * a.width + v * 8, slice, splits);
+                apply8(e, coef, v == v0 ? w0 : *reinterpret_cast<const uint4*>(y + v * 8));
+                o = pack8(e);
+            }
             *reinterpret_cast<uint4*>(a.out + t * a.ld_out + v * 8) = o;
         }
     }
