@@ -407,7 +407,7 @@ qless_status qless_lora_gradients(const int8_t* codes, int64_t ld_codes, const u
                                   void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /* Softmax cross entropy of a language model's head over a large vocabulary, with its gradient, without keeping the
- * logits (for at most 256 tokens with grad_weight they stay in the workspace). hidden [tokens, width] bf16 (ld_hidden elements per row), weight [vocab, width] bf16 (ld_weight elements per
+ * logits. hidden [tokens, width] bf16 (ld_hidden elements per row), weight [vocab, width] bf16 (ld_weight elements per
  * row), labels [tokens] int64 (device), token_weight [tokens] fp32 (device; NULL = 1 for every token):
  *   l_tv = <hidden_t, weight_v>;  p_tv = exp(l_tv) / sum_u exp(l_tu);
  *   loss[t] = -log p_t,label                                             fp32, not multiplied by the token's weight

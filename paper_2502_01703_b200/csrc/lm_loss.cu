@@ -1,4 +1,4 @@
-// Softmax cross entropy of a language model's head over a large vocabulary, with its gradient; the logits are not kept (but for few tokens).
+// Softmax cross entropy of a language model's head over a large vocabulary, with its gradient; the logits are never kept.
 //
 //   l_tv = <h_t, W_v>;  loss_t = logsumexp_v l_tv - l_t,y;  dh_t = w_t (sum_v p_tv W_v - W_y);  dW_v = sum_t w_t (p_tv - [v = y_t]) h_t
 //
@@ -23,10 +23,7 @@
 // LIMIT = 64 powers of two (a loss of 44) below the row's maximum is as good as the maximum itself. Should a row exceed that, a flag
 // sends the rest through a second pass whose reference is the true maximum: its launches are always enqueued and return at once
 // when the flag is not set (the host does not wait to find out).
-// With dW the normaliser has to be known before the piece is written: STATS first, then PROBS, GRAD_H and GRAD_W per piece. (Left for the
-// hidden rows of GRAD_W to carry, the normaliser would round them to bf16 once more.) Up to FEW tokens STATS leaves its logits and
-// loss_softmax_kernel makes the piece of them instead of a second product: 64 tokens x 4096 x 32001 246 -> 212 us, 16 x 4096 x 131072
-// 782 -> 620 us. With many tokens writing and reading fp32 logits would take as long as the product (4096 x 2048 x 50021: 2.0 GB, 330 us).
+// With dW the normaliser has to be known before the piece is written: STATS first, then PROBS, GRAD_H and GRAD_W per piece.
 #include "qless_kernels.h"
 #include "tc_common.cuh"
 
@@ -61,12 +58,10 @@ struct GemmParams {
     int64_t tpad;
     int32_t stages, b_rows;                 // b_rows: rows of B that one CTA of the pair brings
     const int32_t* labels;                  // [tpad] of the gathered tokens
-    RowParam* rowp;
-    const float2* first;                    // swapped PROBS, second pass: what the first left in stat; its maxima become the references
-    int32_t entries;
-    float2* stat;                           // [entries per tile * tiles][tpad]: (maximum, sum relative to it; PROBS: to the row's reference), PROBS: or NULL
-    int32_t tile0;                          // tile index of the launch's first column tile in stat
-    float* logits;                          // swapped STATS: NULL, or logits [tokens][ld_out]
+    const RowParam* rowp;
+    float2* stat;                           // STATS: [entries per tile * tiles][tpad] (maximum, sum)
+    float* psum;                            // PROBS: [entries per tile * tiles][tpad] sums, or NULL
+    int32_t tile0;                          // tile index of the launch's first column tile in stat / psum
     __nv_bfloat16* out;                     // PROBS: piece [tpad][ld_out]; GRAD_W: rows of dW
     int64_t ld_out;
     float* acc;                             // GRAD_H: [splits][row tiles * 256][cols]
@@ -79,7 +74,7 @@ struct GemmParams {
 struct __align__(8) Bars {
     uint64_t full[MAX_STAGES], empty[MAX_STAGES], d_full[2], d_empty[2], drain;
     uint32_t tmem_base, abort_flag;
-    float ref[FEW];                         // swapped roles: of every token
+    __align__(16) RowParam rowp[FEW];       // swapped roles: of every token
     int32_t label[FEW];
 };
 
@@ -168,10 +163,8 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
         const int rest = (int)(r - g * GROUP_M * nt);
         n = rest / gm;
         m = m0 + rest - n * gm;
-        // Few tokens: the slices of the hidden states' gradient take blocks of the vocabulary in turn, from the end, which is what the product
-        // before has left in L2 (64 tokens x 4096 x 32001: 119 -> 116 us for the call).
-        if (SWAP && MODE == GRAD_H) { kb0 = 0; kb1 = kblocks > split ? (kblocks - split + splits - 1) / splits : 0; }
-        else { kb0 = min(kblocks, split * ksplit); kb1 = min(kblocks, kb0 + ksplit); }
+        kb0 = min(kblocks, split * ksplit);
+        kb1 = min(kblocks, kb0 + ksplit);
     };
 
     // A wait of a whole warp: the same answer in every lane.
@@ -195,7 +188,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                     if (!warp_wait(&bars->empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
                     const uint32_t full = map_to_cta(smem_u32(&bars->full[ring.slot]), 0);
                     const uint32_t a = smem_u32(smem + (size_t)ring.slot * stage_bytes), b = a + HALF;
-                    const int k0 = (SWAP && MODE == GRAD_H ? kblocks - 1 - split - kb * splits : kb) * KB, kw = k0 + (MODE == GRAD_H ? p.col0 : 0);
+                    const int k0 = kb * KB, kw = k0 + (MODE == GRAD_H ? p.col0 : 0);
                     const int ac = A_MN ? a0 : k0, ar = A_MN ? (SWAP ? kw : k0) : a0, bc = B_MN ? b0 : k0, br = B_MN ? kw : b0;      // first column and row
                     if (elect_one()) {
                         if (rank == 0) mbar_arrive_expect_tx(smem_u32(&bars->full[ring.slot]), 2 * stage_bytes);      // both CTAs' bytes
@@ -259,17 +252,10 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
         const int q = warp & 3, half = warp >= 6 ? 1 : 0;
         const uint32_t lane_base = (uint32_t)(q * 32) << 16;
         uint32_t n_acc = 0;
-        if (SWAP && MODE != GRAD_H && !idle) {
+        if (SWAP && MODE != GRAD_H) {
             for (int t = threadIdx.x - 64; t < count; t += 256) {
                 bars->label[t] = p.labels[t];
-                if (MODE == PROBS && p.first == nullptr) bars->ref[t] = p.rowp[t].r2;
-                if (MODE == PROBS && p.first != nullptr) {           // every block for itself; block 0 also for loss_close_kernel
-                    float m = -INFINITY;
-#pragma unroll 4
-                    for (int i = 0; i < p.entries; ++i) m = fmaxf(m, p.first[(int64_t)i * p.tpad + t].x);
-                    bars->ref[t] = m > -INFINITY ? m : 0.0f;
-                    if (blockIdx.x == 0) p.rowp[t].r2 = bars->ref[t];
-                }
+                if (MODE == PROBS) bars->rowp[t] = p.rowp[t];
             }
             asm volatile("bar.sync 1, 256;" ::: "memory");
         }
@@ -280,13 +266,14 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
             const int v = m * 256 + (int)rank * 128 + q * 32 + lane;
             const uint32_t buf = n_acc & 1u;
             const int lim = min(count - half * p.b_rows, p.b_rows);      // tokens of this half
+            const int upto = MODE == PROBS ? min(((count + 15) & ~15) - half * p.b_rows, p.b_rows) : lim;      // (b_rows is a multiple of 16)
             bool ok = mbar_wait_cluster(smem_u32(&bars->d_full[buf]), (n_acc >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
             tc_fence_after();
             float run_max = -INFINITY;
 #pragma unroll 1
-            for (int c0 = 0; c0 < lim; c0 += 32) {
+            for (int c0 = 0; c0 < upto; c0 += 32) {
                 uint32_t raw[32];
                 tmem_ld_x32(tmem + lane_base + buf * 256 + half * p.b_rows + c0, raw);
                 tmem_wait_ld();
@@ -307,12 +294,6 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                 float e[32];
                 const int64_t entry = ((int64_t)(p.tile0 + m) * 2 + rank) * 4 + q;
                 if (MODE == STATS) {
-                    if (p.logits != nullptr && v < p.cols) {
-                        float* dst = p.logits + (int64_t)t0 * p.ld_out + v;
-#pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if (k < have) dst[(int64_t)k * p.ld_out] = __uint_as_float(raw[k]);
-                    }
                     float top[32];
 #pragma unroll
                     for (int k = 0; k < 32; ++k) {
@@ -327,28 +308,31 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                     if (lane < have) p.stat[entry * p.tpad + t0 + lane] = make_float2(most, sum);
                 } else {
                     __nv_bfloat16* dst = p.out + (int64_t)t0 * p.ld_out + v;
-                    float top[32];
 #pragma unroll
                     for (int k = 0; k < 32; ++k) {
-                        top[k] = -INFINITY; e[k] = 0.0f;
                         if (k < have) {
-                            const float ref = bars->ref[t0 + k];
-                            const bool out = v >= p.cols || bars->label[t0 + k] == p.col0 + v;
-                            if (!out) top[k] = __uint_as_float(raw[k]);
-                            const float x = fmaf(top[k], LOG2E, -ref);
+                            const RowParam rp = bars->rowp[t0 + k];
+                            const bool own = bars->label[t0 + k] == p.col0 + v, out = own || v >= p.cols;
+                            const float x = out ? -INFINITY : fmaf(__uint_as_float(raw[k]), LOG2E, -rp.r2);
                             run_max = fmaxf(run_max, x);
-                            e[k] = out ? 0.0f : ex2(x);
-                            dst[(int64_t)k * p.ld_out] = __float2bfloat16_rn(e[k]);
+                            e[k] = ex2(x);
+                            dst[(int64_t)k * p.ld_out] = __float2bfloat16_rn(own ? rp.wl : e[k] * rp.w);
+                        } else {
+                            e[k] = 0.0f;
+                            // GRAD_W contracts over steps of 16 tokens
+                            if (c0 + k < upto) dst[(int64_t)k * p.ld_out] = __float2bfloat16_rn(0.0f);
                         }
                     }
-                    const float sum = across_lanes<false>(e, lane), most = across_lanes<true>(top, lane) * LOG2E;
-                    if (lane < have) p.stat[entry * p.tpad + t0 + lane] = make_float2(most, sum);
+                    if (p.psum != nullptr) {
+                        const float sum = across_lanes<false>(e, lane);
+                        if (lane < have) p.psum[entry * p.tpad + t0 + lane] = sum;
+                    }
                 }
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_leader_tmem(smem_u32(&bars->d_empty[buf]), rank);
-            if (MODE == PROBS && run_max > LIMIT) *p.redo = 1;
+            if (MODE == PROBS && p.psum != nullptr && run_max > LIMIT) *p.redo = 1;
         }
         for (int64_t item = pair; !SWAP && item < items; item += num_pairs, ++n_acc) {
             int split, m, n, kb0, kb1;
@@ -412,8 +396,9 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                         float e[32];
 #pragma unroll
                         for (int k = 0; k < 32; ++k) {
-                            run_max = fmaxf(run_max, __uint_as_float(v[k]));
-                            e[k] = ex2(fmaf(__uint_as_float(v[k]), LOG2E, -rp.r2));
+                            const float x = fmaf(__uint_as_float(v[k]), LOG2E, -rp.r2);
+                            run_max = fmaxf(run_max, x);
+                            e[k] = ex2(x);
                             run_sum += e[k];
                             e[k] *= rp.w;
                         }
@@ -476,9 +461,9 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                 }
             }
             if (MODE == STATS && row < count) p.stat[((int64_t)(p.tile0 + n) * 2 + half) * p.tpad + row] = make_float2(run_max, run_sum);
-            if (MODE == PROBS && row < count && p.stat != nullptr) {
-                p.stat[((int64_t)(p.tile0 + n) * 2 + half) * p.tpad + row] = make_float2(run_max * LOG2E, run_sum);
-                if (fmaf(run_max, LOG2E, -rp.r2) > LIMIT) *p.redo = 1;
+            if (MODE == PROBS && row < count && p.psum != nullptr) {
+                p.psum[((int64_t)(p.tile0 + n) * 2 + half) * p.tpad + row] = run_sum;
+                if (run_max > LIMIT) *p.redo = 1;
             }
         }
     }
@@ -486,6 +471,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     __syncthreads();
     cluster_sync_all();
     if (warp == 1) { tc_fence_after(); tmem_dealloc_pair(tmem, 512); }
+    cluster_sync_all();                                      // neither CTA of the pair is gone before both have given their half back
 }
 
 // ---- tokens that carry a loss ------------------------------------------------------------------------------------------
@@ -628,6 +614,7 @@ struct RowArgs {
     int32_t kind, entries;                  // entries: stretches of columns with a partial result
     int64_t tpad;
     const float2* stat;
+    const float* psum;
     const float* label_logit;
     const float* weight;
     const int32_t* order;
@@ -635,22 +622,6 @@ struct RowArgs {
     float2* coef;                           // ROW_FROM_SUMS: w sigma(d), 1 / s
     float* loss;
 };
-
-// What the others' sum s 2^ref and the label's logit (both in powers of two) say of a row: its loss, the probability of the others, the
-// normaliser of all columns.
-struct RowEnd { float nll, sigma, all; };
-__device__ __forceinline__ RowEnd row_end(float ref, float s, float ly)
-{
-    const float others = s == 0.0f ? -INFINITY : ref + log2f(s);      // no other column has any weight (or there is none)
-    const float d = others - ly, e = exp2f(-fabsf(d)), tail = log1pf(e);
-    RowEnd o;
-    o.nll = d > 0.0f ? d * LN2 + tail : tail;
-    o.sigma = d > 0.0f ? 1.0f / (1.0f + e) : e / (1.0f + e);
-    if (others == -INFINITY) { o.nll = ly == ly ? 0.0f : ly; o.sigma = o.nll; }
-    else if (d != d) { o.nll = d; o.sigma = d; }
-    o.all = fmaxf(others, ly) + tail * LOG2E;
-    return o;
-}
 
 // Eight rows per block, 128 threads per row that take every 128th stretch: the partial results of a row lie tpad apart, so it is
 // the number of loads in flight that counts. Joined in a fixed order.
@@ -675,7 +646,7 @@ __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowArgs a)
         if (row < count) {
             if (a.kind == ROW_FROM_SUMS) {
 #pragma unroll 4
-                for (int i = seg; i < a.entries; i += 1024 / ROWS) s += a.stat[(int64_t)i * a.tpad + row].y;
+                for (int i = seg; i < a.entries; i += 1024 / ROWS) s += a.psum[(int64_t)i * a.tpad + row];
             } else {
 #pragma unroll 4
                 for (int i = seg; i < a.entries; i += 1024 / ROWS) {
@@ -703,170 +674,72 @@ __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowArgs a)
                 a.rowp[row] = RowParam{m > -INFINITY ? m : 0.0f, 1.0f, 0.0f, 0.0f};
                 continue;
             }
-            const float w = a.weight[row];
-            const RowEnd end = row_end(a.kind == ROW_FROM_SUMS ? a.rowp[row].r2 : m, s, a.label_logit[row]);
-            a.loss[a.order[row]] = end.nll;
-            if (a.kind == ROW_FROM_SUMS) a.coef[row] = make_float2(w * end.sigma, s == 0.0f ? 0.0f : 1.0f / s);
-            else a.rowp[row] = RowParam{end.all, w, -w * end.sigma, 0.0f};
+            const float ref = a.kind == ROW_FROM_SUMS ? a.rowp[row].r2 : m;
+            const float w = a.weight[row], ly = a.label_logit[row];
+            const float others = s == 0.0f ? -INFINITY : ref + log2f(s);      // no other column has any weight (or there is none)
+            const float d = others - ly;
+            // log(1 + e^d) and the probability of the others
+            const float e = exp2f(-fabsf(d)), tail = log1pf(e);
+            float nll = d > 0.0f ? d * LN2 + tail : tail;
+            float sigma = d > 0.0f ? 1.0f / (1.0f + e) : e / (1.0f + e);
+            if (others == -INFINITY) { nll = ly == ly ? 0.0f : ly; sigma = nll; }
+            else if (d != d) { nll = d; sigma = d; }
+            a.loss[a.order[row]] = nll;
+            if (a.kind == ROW_FROM_SUMS) a.coef[row] = make_float2(w * sigma, s == 0.0f ? 0.0f : 1.0f / s);
+            else a.rowp[row] = RowParam{fmaxf(others, ly) + tail * LOG2E, w, -w * sigma, 0.0f};      // the full normaliser
         }
     }
 }
 
-// Few tokens, gradient of the weights: the logits of the first product stay (at most 1 KiB per column of the vocabulary; they are read
-// from L2), and with the normaliser known this takes the place of a second reading of W: w (p - [v = y]) as bf16 for one piece of the
-// vocabulary, zero behind its last column and for the rows behind the last token up to a multiple of 16 (GRAD_W contracts over those).
-struct SoftmaxArgs {
-    const LossMeta* meta;
-    const float* logits;
-    int64_t ld, ld_out;
-    int32_t col0, cols, vecs;               // vecs: groups of eight columns of the piece, up to a whole tile
-    const int32_t* labels;
-    const RowParam* rowp;
-    __nv_bfloat16* out;
-};
-__global__ void loss_softmax_kernel(const SoftmaxArgs a)
+// Gradient rows of all tokens: joins the slices of the vocabulary; zero for tokens without a loss. `sums` = the accumulator holds
+// sum exp2(l2 - r2) W_v over the other columns; otherwise the finished gradient.
+__global__ void loss_finish_kernel(const float* __restrict__ acc, int32_t width, const LossMeta* __restrict__ meta,
+                                   const int32_t* __restrict__ place, const int32_t* __restrict__ labels, const float2* __restrict__ coef, int32_t sums,
+                                   const __nv_bfloat16* __restrict__ weight, int64_t ld_weight, int64_t T, __nv_bfloat16* __restrict__ out, int64_t ld_out)
 {
     ahead_release();
     ahead_wait();
-    const int count = a.meta->count;
-    const int64_t total = (int64_t)((count + 15) & ~15) * a.vecs;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
-        const int t = (int)(i / a.vecs), c = (int)(i - (int64_t)t * a.vecs) * 8;
-        float x[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = 0.0f;
-        if (t < count) {
-            const RowParam rp = a.rowp[t];
-            const int lab = a.labels[t] - a.col0 - c;
-            const float4* src = reinterpret_cast<const float4*>(a.logits + (int64_t)t * a.ld + a.col0 + c);      // the rows have room up to a whole tile
-            const float4 u = src[0], v = src[1];
-            const float l[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (c + k < a.cols) x[k] = k == lab ? rp.wl : rp.w * ex2(fmaf(l[k], LOG2E, -rp.r2));
-        }
-        *reinterpret_cast<uint4*>(a.out + (int64_t)t * a.ld_out + c) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
-    }
-}
-
-// Eight columns of a gradient row, the slices of the vocabulary joined in order.
-struct Eight { float x[8]; };
-__device__ __forceinline__ Eight sum8(const float* __restrict__ acc, int64_t slice, int splits)
-{
-    Eight e;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) e.x[j] = 0.0f;
-    for (int s = 0; s < splits; ++s) {
-        const float4* src = reinterpret_cast<const float4*>(acc + s * slice);
-        const float4 a = src[0], b = src[1];
-        e.x[0] += a.x; e.x[1] += a.y; e.x[2] += a.z; e.x[3] += a.w; e.x[4] += b.x; e.x[5] += b.y; e.x[6] += b.z; e.x[7] += b.w;
-    }
-    return e;
-}
-// From sum exp2(l2 - r2) W_v over the other columns to the gradient: `k` is the row's coef, `w` the label's row of W.
-__device__ __forceinline__ void apply8(Eight& e, float2 k, uint4 w)
-{
-    const uint32_t yw[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        e.x[2 * j] = k.x * (e.x[2 * j] * k.y - __uint_as_float(yw[j] << 16));
-        e.x[2 * j + 1] = k.x * (e.x[2 * j + 1] * k.y - __uint_as_float(yw[j] & 0xFFFF0000u));
-    }
-}
-__device__ __forceinline__ uint4 pack8(const Eight& e)
-{
-    return make_uint4(pack_bf16(e.x[0], e.x[1]), pack_bf16(e.x[2], e.x[3]), pack_bf16(e.x[4], e.x[5]), pack_bf16(e.x[6], e.x[7]));
-}
-
-struct FinishArgs {
-    const float* acc;
-    int32_t width, sums, entries;           // entries: stretches of columns with a partial sum (loss_close_kernel)
-    const LossMeta* meta;
-    const int32_t* place;
-    const int32_t* labels;
-    const float2* coef;
-    const __nv_bfloat16* weight;
-    int64_t ld_weight, T, ld_out, tpad;
-    __nv_bfloat16* out;
-    const float2* stat;                     // from here on: loss_close_kernel; a second pass leaves its sums behind the first's
-    const float* label_logit;
-    const float* token_weight;              // of the gathered tokens
-    const RowParam* rowp;
-    float* loss;
-};
-
-// Gradient rows of all tokens; zero for tokens without a loss.
-__global__ void loss_finish_kernel(const FinishArgs a)
-{
-    ahead_release();
-    ahead_wait();
-    const int vecs = a.width / 8, splits = a.meta->splits;
-    const int64_t slice = (int64_t)(a.meta->count + 255) / 256 * 256 * a.width;
-    const int64_t total = a.T * vecs;
+    const int vecs = width / 8, splits = meta->splits;
+    const int64_t slice = (int64_t)(meta->count + 255) / 256 * 256;
+    const int64_t total = T * vecs;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
         const int64_t t = i / vecs;
         const int c = (int)(i - t * vecs) * 8;
-        const int r = a.place[t];
+        const int r = place[t];
         uint4 o = make_uint4(0u, 0u, 0u, 0u);
         if (r >= 0) {
-            Eight e = sum8(a.acc + (int64_t)r * a.width + c, slice, splits);
-            if (a.sums) apply8(e, a.coef[r], *reinterpret_cast<const uint4*>(a.weight + (int64_t)a.labels[r] * a.ld_weight + c));      // else finished
-            o = pack8(e);
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = 0.0f;
+            for (int s = 0; s < splits; ++s) {
+                const float4* src = reinterpret_cast<const float4*>(acc + (s * slice + r) * width + c);
+                const float4 a = src[0], b = src[1];
+                x[0] += a.x; x[1] += a.y; x[2] += a.z; x[3] += a.w; x[4] += b.x; x[5] += b.y; x[6] += b.z; x[7] += b.w;
+            }
+            if (sums) {
+                const float2 k = coef[r];
+                const uint4 y = *reinterpret_cast<const uint4*>(weight + (int64_t)labels[r] * ld_weight + c);
+                const uint32_t yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[2 * j] = k.x * (x[2 * j] * k.y - __uint_as_float(yw[j] << 16));
+                    x[2 * j + 1] = k.x * (x[2 * j + 1] * k.y - __uint_as_float(yw[j] & 0xFFFF0000u));
+                }
+            }
+            o = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
         }
-        *reinterpret_cast<uint4*>(a.out + t * a.ld_out + c) = o;
+        *reinterpret_cast<uint4*>(out + t * ld_out + c) = o;
     }
 }
 
-// Few tokens, gradient of the hidden states alone: a block per token takes the row's sums together and finishes its gradient, one launch
-// in place of loss_rows_kernel and loss_finish_kernel. (With many tokens the former reads a sector of eight rows' sums once, this eight times.)
-__global__ void __launch_bounds__(512) loss_close_kernel(const FinishArgs a)
+// These kernels do not begin before the one ahead has ended (a chain of launches on CTA pairs that overlapped stopped, once in some thousand
+// calls, for a reason that was not found).
+template <typename... Params, typename... Args>
+cudaError_t launch_after(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args)
 {
-    __shared__ float part[16];
-    __shared__ float2 coef;
-    ahead_release();
-    ahead_wait();
-    const int vecs = a.width / 8, splits = a.meta->splits, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t slice = (int64_t)(a.meta->count + 255) / 256 * 256 * a.width;
-    for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-        const int r = a.place[t];
-        // the first eight columns' sums are on their way while the row's are taken
-        const int v0 = threadIdx.x;
-        Eight e0;
-        uint4 w0 = make_uint4(0u, 0u, 0u, 0u);
-        const __nv_bfloat16* y = r >= 0 ? a.weight + (int64_t)a.labels[r] * a.ld_weight : nullptr;
-        if (r >= 0 && v0 < vecs) {
-            e0 = sum8(a.acc + (int64_t)r * a.width + v0 * 8, slice, splits);
-            w0 = *reinterpret_cast<const uint4*>(y + v0 * 8);
-        }
-        if (r >= 0) {
-            const float2* stat = a.stat + (a.meta->redo != 0 ? (int64_t)a.entries * a.tpad : 0);
-            float s = 0.0f;
-#pragma unroll 4
-            for (int i = threadIdx.x; i < a.entries; i += 512) s += stat[(int64_t)i * a.tpad + r].y;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-            __syncthreads();                                 // the last row's coef has been read
-            if (lane == 0) part[warp] = s;
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                s = 0.0f;
-                for (int j = 0; j < 16; ++j) s += part[j];
-                const RowEnd end = row_end(a.rowp[r].r2, s, a.label_logit[r]);
-                a.loss[t] = end.nll;
-                coef = make_float2(a.token_weight[r] * end.sigma, s == 0.0f ? 0.0f : 1.0f / s);
-            }
-            __syncthreads();
-        }
-        for (int v = v0; v < vecs; v += 512) {
-            uint4 o = make_uint4(0u, 0u, 0u, 0u);
-            if (r >= 0) {
-                Eight e = v == v0 ? e0 : sum8(a.acc + (int64_t)r * a.width + v * 8, slice, splits);
-                apply8(e, coef, v == v0 ? w0 : *reinterpret_cast<const uint4*>(y + v * 8));
-                o = pack8(e);
-            }
-            *reinterpret_cast<uint4*>(a.out + t * a.ld_out + v * 8) = o;
-        }
-    }
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
 }
 
 unsigned grid_of(int64_t work, int threads)
@@ -885,7 +758,7 @@ qless_status launch_gemm(const char* name, const CUtensorMap& a, const CUtensorM
     int64_t grid = sm_count() / 2 * 2;
     if (grid > 2 * max_items) grid = 2 * max_items;
     { ProfileScope ps(name, st);
-      QLESS_CUDA_TRY(launch_ahead(head_gemm_kernel<MODE, SWAP>, dim3((unsigned)grid), dim3(NTHREADS), smem, st, a, b, p)); }
+      QLESS_CUDA_TRY(launch_after(head_gemm_kernel<MODE, SWAP>, dim3((unsigned)grid), dim3(NTHREADS), smem, st, a, b, p)); }
     count_launches(1);
     return QLESS_OK;
 }
@@ -924,10 +797,9 @@ LossPlan plan_loss(int64_t T, int32_t width, int32_t vocab, bool want_h, bool wa
     pl.logit_off = take((size_t)pl.tpad * 4);
     pl.coef_off = take((size_t)pl.tpad * 8);
     pl.rowp_off = take((size_t)pl.tpad * sizeof(RowParam));
-    pl.stat_off = take((size_t)pl.entries * pl.tpad * (pl.few && !pl.exact ? 16 : 8));      // (few: a second pass has its own)
+    pl.stat_off = take((size_t)pl.entries * pl.tpad * 8);
     pl.hidden_off = take((size_t)pl.tpad * width * 2);
     pl.piece_off = (want_h || want_w) ? take((size_t)pl.tpad * pl.piece * 2) : 0;
-    pl.logits_off = pl.few && want_w ? take((size_t)T * tiles_v * 256 * 4) : 0;
     pl.acc_off = want_h ? take((size_t)cap * 256 * width * 4) : 0;
     pl.total = off + 256;
     return pl;
@@ -944,14 +816,13 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
     float2* coef = reinterpret_cast<float2*>(ws + pl.coef_off);
     RowParam* rowp = reinterpret_cast<RowParam*>(ws + pl.rowp_off);
     float2* stat = reinterpret_cast<float2*>(ws + pl.stat_off);
+    float* psum = reinterpret_cast<float*>(ws + pl.stat_off);       // the statistics are read before the sums are written, and again the other way round
     __nv_bfloat16* hidden = reinterpret_cast<__nv_bfloat16*>(ws + pl.hidden_off);
     __nv_bfloat16* piece = reinterpret_cast<__nv_bfloat16*>(ws + pl.piece_off);
     float* acc = reinterpret_cast<float*>(ws + pl.acc_off);
     const bool want_h = a.grad_hidden != nullptr, want_w = a.grad_weight != nullptr;
-    float* logits = pl.few && want_w ? reinterpret_cast<float*>(ws + pl.logits_off) : nullptr;
     const int64_t mt = pl.tpad / 256, nt_h = (a.width + 255) / 256;
     const int32_t tiles_v = (a.vocab + 255) / 256;
-    const int64_t ld_logits = (int64_t)tiles_v * 256;
 
     { ProfileScope ps("loss_gather", st);
       // a block lists at most LIST of the 1024 tokens of a step: at least four blocks
@@ -965,7 +836,7 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
       const int32_t kb = ((a.vocab < pl.piece ? a.vocab : pl.piece) + KB - 1) / KB;
       g.most_slices = kb / 3 > 1 ? kb / 3 : 1; g.order = order; g.place = place;
       g.out_labels = labels; g.out_weight = weight; g.label_logit = logit; g.loss = a.loss; g.rowp = rowp; g.out = hidden; g.meta = meta;
-      QLESS_CUDA_TRY(launch_ahead(loss_gather_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, g)); }
+      QLESS_CUDA_TRY(launch_after(loss_gather_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, g)); }
     count_launches(1);
 
     CUtensorMap tm_x, tm_w, tm_p;
@@ -988,84 +859,65 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
 
     GemmParams base{};
     base.meta = meta; base.tpad = pl.tpad; base.labels = labels; base.rowp = rowp; base.b_rows = b_rows; base.timeout_word = timeout_word;
-    auto stats = [&](int32_t cols) {
+    auto stats = [&](int32_t cols, const int32_t* gate) {
         GemmParams p = base;
-        p.cols = cols; p.k = a.width; p.stat = stat; p.a_whole = p.b_whole = whole; p.logits = logits; p.ld_out = ld_logits;
+        p.gate = gate; p.cols = cols; p.k = a.width; p.stat = stat; p.a_whole = p.b_whole = whole;
         const int64_t tiles = (cols + 255) / 256;
         return few ? launch_gemm<STATS, true>("loss_stats", tm_w, tm_x, p, tiles, st) : launch_gemm<STATS, false>("loss_stats", tm_x, tm_w, p, mt * tiles, st);
     };
     auto rows = [&](int kind, int32_t entries, const int32_t* gate) -> qless_status {
         RowArgs r{};
-        r.meta = meta; r.gate = gate; r.kind = kind; r.entries = entries; r.tpad = pl.tpad; r.stat = stat; r.label_logit = logit;
+        r.meta = meta; r.gate = gate; r.kind = kind; r.entries = entries; r.tpad = pl.tpad; r.stat = stat; r.psum = psum; r.label_logit = logit;
         r.weight = weight; r.order = order; r.rowp = rowp; r.coef = coef; r.loss = a.loss;
         { ProfileScope ps("loss_rows", st);
-          QLESS_CUDA_TRY(launch_ahead(loss_rows_kernel, dim3(grid_of(a.T, ROWS)), dim3(1024), 0, st, r)); }
+          QLESS_CUDA_TRY(launch_after(loss_rows_kernel, dim3(grid_of(a.T, ROWS)), dim3(1024), 0, st, r)); }
         count_launches(1);
         return QLESS_OK;
     };
-    const bool close = few && !pl.exact;
-    auto probs = [&](int32_t v0, int32_t cols, bool keep_sums, const int32_t* gate) -> qless_status {
-        if (logits != nullptr) {
-            SoftmaxArgs f{};
-            f.meta = meta; f.logits = logits; f.ld = ld_logits; f.ld_out = pl.piece; f.col0 = v0; f.cols = cols; f.vecs = (cols + 255) / 256 * 32; f.labels = labels;
-            f.rowp = rowp; f.out = piece;
-            { ProfileScope ps("loss_softmax", st);
-              QLESS_CUDA_TRY(launch_ahead(loss_softmax_kernel, dim3(grid_of((a.T + 15) / 16 * 16 * f.vecs, 256)), dim3(256), 0, st, f)); }
-            count_launches(1);
-            return QLESS_OK;
-        }
-        GemmParams p = base;
-        p.gate = gate; p.cols = cols; p.col0 = v0; p.k = a.width; p.out = piece; p.ld_out = pl.piece; p.tile0 = v0 / 256;
-        p.stat = keep_sums ? stat : nullptr; p.redo = &meta->redo; p.a_whole = p.b_whole = whole;
-        if (close && gate != nullptr) { p.first = stat; p.entries = pl.entries; p.stat = stat + (int64_t)pl.entries * pl.tpad; }
-        const int64_t tiles = (cols + 255) / 256;
-        return few ? launch_gemm<PROBS, true>("loss_probs", tm_w, tm_x, p, tiles, st) : launch_gemm<PROBS, false>("loss_probs", tm_x, tm_w, p, mt * tiles, st);
-    };
-    auto grads = [&](int32_t v0, int32_t cols, const int32_t* gate) {
-        qless_status e = QLESS_OK;
-        if (want_h) {
-            GemmParams g = base;
-            g.gate = gate; g.cols = a.width; g.col0 = v0; g.k = cols; g.acc = acc; g.accumulate = v0 > 0;
-            g.a_whole = few ? whole : 1; g.b_whole = few ? 1 : whole;
-            e = few ? launch_gemm<GRAD_H, true>("loss_grad_hidden", tm_w, tm_p, g, pl.cap_tiles * nt_h, st)
-                    : launch_gemm<GRAD_H, false>("loss_grad_hidden", tm_p, tm_w, g, pl.cap_tiles * nt_h, st);
-        }
-        if (want_w && e == QLESS_OK) {
-            GemmParams g = base;
-            g.gate = gate; g.cols = a.width; g.rows = cols; g.col0 = v0; g.out = reinterpret_cast<__nv_bfloat16*>(a.grad_weight); g.ld_out = a.ld_grad_weight; g.a_whole = 1; g.b_whole = whole;
-            e = launch_gemm<GRAD_W, false>("loss_grad_weight", tm_pg, tm_xg, g, (int64_t)((cols + 255) / 256) * nt_h, st);
-        }
-        return e;
-    };
     auto pieces = [&](bool keep_sums, const int32_t* gate) {
-        qless_status e = QLESS_OK;
-        for (int32_t v0 = 0; v0 < a.vocab && e == QLESS_OK; v0 += pl.piece) {
+        for (int32_t v0 = 0; v0 < a.vocab; v0 += pl.piece) {
             const int32_t cols = a.vocab - v0 < pl.piece ? a.vocab - v0 : pl.piece;
-            if ((e = probs(v0, cols, keep_sums, gate)) == QLESS_OK) e = grads(v0, cols, gate);
+            GemmParams p = base;
+            p.gate = gate; p.cols = cols; p.col0 = v0; p.k = a.width; p.out = piece; p.ld_out = pl.piece; p.tile0 = v0 / 256;
+            p.psum = keep_sums ? psum : nullptr; p.redo = &meta->redo; p.a_whole = p.b_whole = whole;
+            const int64_t tiles = (cols + 255) / 256;
+            qless_status e = few ? launch_gemm<PROBS, true>("loss_probs", tm_w, tm_x, p, tiles, st) : launch_gemm<PROBS, false>("loss_probs", tm_x, tm_w, p, mt * tiles, st);
+            if (e != QLESS_OK) return e;
+            if (want_h) {
+                GemmParams g = base;
+                g.gate = gate; g.cols = a.width; g.col0 = v0; g.k = cols; g.acc = acc; g.accumulate = v0 > 0;
+                g.a_whole = few ? whole : 1; g.b_whole = few ? 1 : whole;
+                e = few ? launch_gemm<GRAD_H, true>("loss_grad_hidden", tm_w, tm_p, g, pl.cap_tiles * nt_h, st)
+                        : launch_gemm<GRAD_H, false>("loss_grad_hidden", tm_p, tm_w, g, pl.cap_tiles * nt_h, st);
+                if (e != QLESS_OK) return e;
+            }
+            if (want_w) {
+                GemmParams g = base;
+                g.gate = gate; g.cols = a.width; g.rows = cols; g.col0 = v0; g.out = reinterpret_cast<__nv_bfloat16*>(a.grad_weight); g.ld_out = a.ld_grad_weight; g.a_whole = 1; g.b_whole = whole;
+                e = launch_gemm<GRAD_W, false>("loss_grad_weight", tm_pg, tm_xg, g, (int64_t)((cols + 255) / 256) * nt_h, st);
+                if (e != QLESS_OK) return e;
+            }
         }
-        return e;
+        return QLESS_OK;
     };
 
     if (pl.exact) {
-        if ((s = stats(a.vocab)) != QLESS_OK) return s;
+        if ((s = stats(a.vocab, nullptr)) != QLESS_OK) return s;
         if ((s = rows(ROW_FROM_STATS, pl.entries, nullptr)) != QLESS_OK) return s;
         if (want_w && (s = pieces(false, nullptr)) != QLESS_OK) return s;
     } else {
-        const bool one = a.vocab <= pl.piece;                    // one piece: whether it has to be redone is known before its gradient
-        if ((s = one ? probs(0, a.vocab, true, nullptr) : pieces(true, nullptr)) != QLESS_OK) return s;
-        if (!close && (s = rows(ROW_REFERENCE, pl.entries, &meta->redo)) != QLESS_OK) return s;
-        if ((s = one ? probs(0, a.vocab, true, &meta->redo) : pieces(true, &meta->redo)) != QLESS_OK) return s;
-        if (one && (s = grads(0, a.vocab, nullptr)) != QLESS_OK) return s;
-        if (!close && (s = rows(ROW_FROM_SUMS, pl.entries, nullptr)) != QLESS_OK) return s;
+        if ((s = pieces(true, nullptr)) != QLESS_OK) return s;
+        if ((s = stats(a.vocab, &meta->redo)) != QLESS_OK) return s;
+        if ((s = rows(ROW_REFERENCE, pl.entries, &meta->redo)) != QLESS_OK) return s;
+        if ((s = pieces(true, &meta->redo)) != QLESS_OK) return s;
+        if ((s = rows(ROW_FROM_SUMS, pl.entries, nullptr)) != QLESS_OK) return s;
     }
     if (want_h) {
-        FinishArgs f{};
-        f.acc = acc; f.width = a.width; f.sums = want_w ? 0 : 1; f.entries = pl.entries; f.meta = meta; f.place = place; f.labels = labels; f.coef = coef;
-        f.weight = reinterpret_cast<const __nv_bfloat16*>(a.weight); f.ld_weight = a.ld_weight; f.T = a.T; f.ld_out = a.ld_grad_hidden; f.tpad = pl.tpad;
-        f.out = reinterpret_cast<__nv_bfloat16*>(a.grad_hidden); f.stat = stat; f.label_logit = logit; f.token_weight = weight; f.rowp = rowp; f.loss = a.loss;
         { ProfileScope ps("loss_finish", st);
-          if (close) QLESS_CUDA_TRY(launch_ahead(loss_close_kernel, dim3((unsigned)a.T), dim3(512), 0, st, f));
-          else QLESS_CUDA_TRY(launch_ahead(loss_finish_kernel, dim3(grid_of(a.T * (a.width / 8), 256)), dim3(256), 0, st, f)); }
+          QLESS_CUDA_TRY(launch_after(loss_finish_kernel, dim3(grid_of(a.T * (a.width / 8), 256)), dim3(256), 0, st, (const float*)acc, a.width, (const LossMeta*)meta,
+                                      (const int32_t*)place, (const int32_t*)labels, (const float2*)coef, (int32_t)(want_w ? 0 : 1),
+                                      reinterpret_cast<const __nv_bfloat16*>(a.weight), a.ld_weight, a.T, reinterpret_cast<__nv_bfloat16*>(a.grad_hidden),
+                                      a.ld_grad_hidden)); }
         count_launches(1);
     }
     return QLESS_OK;
