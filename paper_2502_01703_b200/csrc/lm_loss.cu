@@ -773,7 +773,8 @@ LossPlan plan_loss(int64_t T, int32_t width, int32_t vocab, bool want_h, bool wa
     const int64_t tiles_v = ((int64_t)vocab + 255) / 256;
     // The normaliser first (one more product): for the loss alone, and with the gradient of the weights. For the gradient of the hidden
     // states a reference that may have to be redone is never slower, the smallest problems included (28 tokens x 1720 x 1079: 38 us
-    // against 43 us with the product first, 33 x 512 x 4099: 36.7 against 36.0 us, 88 x 4040 x 2783: 57 against 73 us).
+    // against 43 us with the product first, 33 x 512 x 4099: 36.7 against 36.0 us, 88 x 4040 x 2783: 57 against 73 us; measured
+    // with launches that overlapped).
     pl.exact = !want_h || want_w;
     // Piece of the vocabulary whose probabilities are held at once: at most 512 MiB of bf16.
     int64_t piece_tiles = ((int64_t)512 << 20) / (pl.tpad * 256 * 2);
