@@ -4,6 +4,10 @@ Every function has the name of the C entry point it calls and does argument mars
 torch supplies device memory and the current CUDA stream, the arithmetic runs in the library's
 kernels. If ``libqless.so`` has not been built, or a call returns a non-OK status, an exception is
 raised; there is no other code path.
+
+``stream=`` runs a call on that stream instead of the current one. The caller orders the two (inputs
+written on the current stream, results read there); memory that the binding allocates for the call
+comes from that stream's pool, and the call's tensors are recorded as used on it.
 """
 import ctypes as C
 import os
@@ -179,10 +183,42 @@ def _projection(matrix):
     return C.byref(ProjectionCfg(int(matrix), (C.c_int32 * 3)(0, 0, 0)))
 
 
-def _workspace(nbytes, device, workspace):
+def _elsewhere(stream):
+    """True where a call is asked to run on another stream than the current one."""
+    return stream is not None and stream.cuda_stream != _stream()
+
+
+def _new(shape, dtype, device, stream):
+    """A new contiguous output of a call on `stream`. Where that is not the current stream, the memory comes from that stream's pool: a
+    block of the current stream's pool might still be in use there when the kernels begin. The current stream, on which the
+    caller is likely to read the result, is recorded as a user of it."""
+    if not _elsewhere(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+    here = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if t.is_cuda:
+        t.record_stream(here)
+    return t
+
+
+def _used(stream, *tensors):
+    """Records a call's tensors (None: absent) as used on `stream`, so that one that is dropped as soon as the call returns is not given
+    out again on the current stream while the kernels still run."""
+    if _elsewhere(stream):
+        for t in tensors:
+            if t is not None and t.is_cuda:
+                t.record_stream(stream)
+
+
+def _workspace(nbytes, device, workspace, stream):
     if workspace is not None:
         return workspace
-    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+    nbytes = max(int(nbytes), 256)
+    if not _elsewhere(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):        # goes back to that stream's pool when the call returns: reused behind the kernels only
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def qless_last_error():
@@ -208,13 +244,14 @@ def qless_project_quantize(grads, d, seed, bits, adam_m=None, adam_v=None, adam=
     out = out or {}
     codes = out.get("codes", None)
     if codes is None:
-        codes = torch.empty((n, d * bits // 8), dtype=torch.uint8, device=dev)
+        codes = _new((n, d * bits // 8), torch.uint8, dev, stream)
     scales = out.get("scales", None)
     if scales is None:
-        scales = torch.empty(n, dtype=torch.float32, device=dev)
-    sumsq = out.get("sumsq", torch.empty(n, dtype=torch.int32, device=dev) if want_sumsq else None)
-    proj = out.get("proj", torch.empty((n, d), dtype=torch.float32, device=dev) if want_proj else None)
-    ws = _workspace(qless_project_quantize_workspace(n, P, d, bits), dev, workspace)
+        scales = _new(n, torch.float32, dev, stream)
+    sumsq = out.get("sumsq", _new(n, torch.int32, dev, stream) if want_sumsq else None)
+    proj = out.get("proj", _new((n, d), torch.float32, dev, stream) if want_proj else None)
+    ws = _workspace(qless_project_quantize_workspace(n, P, d, bits), dev, workspace, stream)
+    _used(stream, grads, adam_m, adam_v, workspace, *out.values())
     if matrix is None:
         _check(lib().qless_project_quantize(_ptr(grads), _dtype_code(grads), n, grads.stride(0) if n > 0 else P,
                                             _ptr(adam_m), _ptr(adam_v), _adam(adam), P, d, seed, bits,
@@ -248,7 +285,8 @@ def qless_project_quantize_host(grads_host, d, seed, bits, adam_m=None, adam_v=N
     if sumsq is None:
         sumsq = torch.empty(n, dtype=torch.int32).pin_memory()
     code = _dtype_code(grads_host)
-    ws = _workspace(qless_project_quantize_host_workspace(n, P, d, bits, code), device, workspace)
+    ws = _workspace(qless_project_quantize_host_workspace(n, P, d, bits, code), device, workspace, stream)
+    _used(stream, adam_m, adam_v, workspace)
     if matrix is None:
         _check(lib().qless_project_quantize_host(_ptr(grads_host), code, n, grads_host.stride(0) if n > 0 else P,
                                                  _ptr(adam_m), _ptr(adam_v), _adam(adam), P, d, seed, bits,
@@ -286,9 +324,10 @@ def qless_profile_collect():
 def qless_quantize(x, bits, normalize=True, want_sumsq=True, stream=None):
     n, d = x.shape
     dev = x.device
-    codes = torch.empty((n, d * bits // 8), dtype=torch.uint8, device=dev)
-    scales = torch.empty(n, dtype=torch.float32, device=dev)
-    sumsq = torch.empty(n, dtype=torch.int32, device=dev) if want_sumsq else None
+    codes = _new((n, d * bits // 8), torch.uint8, dev, stream)
+    scales = _new(n, torch.float32, dev, stream)
+    sumsq = _new(n, torch.int32, dev, stream) if want_sumsq else None
+    _used(stream, x)
     _check(lib().qless_quantize(_ptr(x), n, d, 1 if normalize else 0, bits, _ptr(codes), _ptr(scales),
                                 _ptr(sumsq), _stream(stream)))
     return codes, scales, sumsq
@@ -298,9 +337,10 @@ def qless_quantize_absmean(x, bits, normalize=True, want_sumsq=True, stream=None
     """As qless_quantize, with the scale taken from the mean absolute value of the row."""
     n, d = x.shape
     dev = x.device
-    codes = torch.empty((n, d * bits // 8), dtype=torch.uint8, device=dev)
-    scales = torch.empty(n, dtype=torch.float32, device=dev)
-    sumsq = torch.empty(n, dtype=torch.int32, device=dev) if want_sumsq else None
+    codes = _new((n, d * bits // 8), torch.uint8, dev, stream)
+    scales = _new(n, torch.float32, dev, stream)
+    sumsq = _new(n, torch.int32, dev, stream) if want_sumsq else None
+    _used(stream, x)
     _check(lib().qless_quantize_absmean(_ptr(x), n, d, 1 if normalize else 0, bits, _ptr(codes), _ptr(scales),
                                         _ptr(sumsq), _stream(stream)))
     return codes, scales, sumsq
@@ -308,20 +348,21 @@ def qless_quantize_absmean(x, bits, normalize=True, want_sumsq=True, stream=None
 
 def qless_adam_gamma(grads, adam_m=None, adam_v=None, adam=None, stream=None):
     n, P = grads.shape
-    out = torch.empty((n, P), dtype=torch.bfloat16, device=grads.device)
+    out = _new((n, P), torch.bfloat16, grads.device, stream)
+    _used(stream, grads, adam_m, adam_v)
     _check(lib().qless_adam_gamma(_ptr(grads), _dtype_code(grads), n, grads.stride(0) if n > 0 else P,
                                   _ptr(adam_m), _ptr(adam_v), _adam(adam), P, _ptr(out), _stream(stream)))
     return out
 
 
 def qless_philox_entries(seed, r0, nr, j0, nj, device="cuda", stream=None):
-    out = torch.empty((nr, nj), dtype=torch.int8, device=device)
+    out = _new((nr, nj), torch.int8, device, stream)
     _check(lib().qless_philox_entries(seed, r0, nr, j0, nj, _ptr(out), _stream(stream)))
     return out
 
 
 def qless_gaussian_entries(seed, r0, nr, j0, nj, device="cuda", stream=None):
-    out = torch.empty((nr, nj), dtype=torch.float32, device=device)
+    out = _new((nr, nj), torch.float32, device, stream)
     _check(lib().qless_gaussian_entries(seed, r0, nr, j0, nj, _ptr(out), _stream(stream)))
     return out
 
@@ -342,9 +383,10 @@ def qless_score(train_codes, val_codes, train_scales, val_scales, lr_weights, ta
     eta = (C.c_float * Cn)(*[float(x) for x in lr_weights])
     off = (C.c_int32 * (T + 1))(*[int(x) for x in task_offsets])
     if scores is None:
-        scores = torch.empty(N, dtype=torch.float32, device=dev)
-    per_task = torch.empty((N, T), dtype=torch.float32, device=dev) if want_per_task else None
-    ws = _workspace(qless_score_workspace(N, V, Cn, T, d, bits), dev, workspace)
+        scores = _new(N, torch.float32, dev, stream)
+    per_task = _new((N, T), torch.float32, dev, stream) if want_per_task else None
+    ws = _workspace(qless_score_workspace(N, V, Cn, T, d, bits), dev, workspace, stream)
+    _used(stream, train_codes, val_codes, train_scales, val_scales, train_sumsq, val_sumsq, scores, workspace)
     _check(lib().qless_score(_ptr(train_codes), train_codes.stride(0) if Cn > 0 else 0,
                              _ptr(val_codes), val_codes.stride(0),
                              _ptr(train_scales), _ptr(val_scales), _ptr(train_sumsq), _ptr(val_sumsq),
@@ -360,7 +402,8 @@ def qless_score_16bit_workspace(N, V, Cn, T):
 def qless_inv_norms_16bit(rows, stream=None):
     """rows bf16 [C, n, d] -> 1 / ||row|| as f32 [C, n] (0 for a zero row)."""
     Cn, n, d = rows.shape
-    out = torch.empty((Cn, n), dtype=torch.float32, device=rows.device)
+    out = _new((Cn, n), torch.float32, rows.device, stream)
+    _used(stream, rows)
     _check(lib().qless_inv_norms_16bit(_ptr(rows), rows.stride(0) * 2, n, Cn, d, _ptr(out), _stream(stream)))
     return out
 
@@ -377,9 +420,10 @@ def qless_score_16bit(train_rows, val_rows, lr_weights, task_offsets, want_per_t
     eta = (C.c_float * Cn)(*[float(x) for x in lr_weights])
     off = (C.c_int32 * (T + 1))(*[int(x) for x in task_offsets])
     if scores is None:
-        scores = torch.empty(N, dtype=torch.float32, device=dev)
-    per_task = torch.empty((N, T), dtype=torch.float32, device=dev) if want_per_task else None
-    ws = _workspace(qless_score_16bit_workspace(N, V, Cn, T), dev, workspace)
+        scores = _new(N, torch.float32, dev, stream)
+    per_task = _new((N, T), torch.float32, dev, stream) if want_per_task else None
+    ws = _workspace(qless_score_16bit_workspace(N, V, Cn, T), dev, workspace, stream)
+    _used(stream, train_rows, val_rows, train_inv_norms, val_inv_norms, scores, workspace)
     _check(lib().qless_score_16bit(_ptr(train_rows), train_rows.stride(0) * 2 if Cn > 0 else 0, _ptr(val_rows),
                                    val_rows.stride(0) * 2, _ptr(train_inv_norms), _ptr(val_inv_norms), eta, off, N, V, Cn, T,
                                    d, _ptr(scores), _ptr(per_task),
@@ -397,8 +441,9 @@ def qless_score_dots(train_codes, val_codes, d, bits, t0=0, nt=None, workspace=N
         nt = train_codes.shape[0] - t0
     V = val_codes.shape[0]
     dev = train_codes.device
-    dots = torch.empty((nt, V), dtype=torch.int32, device=dev)
-    ws = _workspace(qless_score_dots_workspace(nt, V, d, bits), dev, workspace)
+    dots = _new((nt, V), torch.int32, dev, stream)
+    ws = _workspace(qless_score_dots_workspace(nt, V, d, bits), dev, workspace, stream)
+    _used(stream, train_codes, val_codes, workspace)
     _check(lib().qless_score_dots(_ptr(train_codes), _ptr(val_codes), t0, nt, V, d, bits, _ptr(dots),
                                   _ptr(ws), ws.numel(), _stream(stream)))
     return dots
@@ -413,8 +458,9 @@ def qless_select_topk(scores, frac, indices=None, workspace=None, stream=None):
     N = scores.numel()
     dev = scores.device
     if indices is None:
-        indices = torch.empty(max(N, 1), dtype=torch.int64, device=dev)
-    ws = _workspace(qless_select_topk_workspace(N), dev, workspace)
+        indices = _new(max(N, 1), torch.int64, dev, stream)
+    ws = _workspace(qless_select_topk_workspace(N), dev, workspace, stream)
+    _used(stream, scores, indices, workspace)
     k = C.c_int64(0)
     _check(lib().qless_select_topk(_ptr(scores), N, float(frac), _ptr(indices), C.byref(k), _ptr(ws),
                                    ws.numel(), _stream(stream)))
@@ -426,6 +472,7 @@ def qless_select_topk_static(scores, frac, indices, stream=None):
     array inside the library, so the caller passes only the input and a preallocated int64 `indices`
     tensor with room for k entries. Returns a view of the first k entries; nothing is allocated here
     either. Calls that overlap on the GPU share that array and must be serialised by the caller."""
+    _used(stream, scores, indices)
     k = C.c_int64(0)
     _check(lib().qless_select_topk_static(_ptr(scores), scores.numel(), float(frac), _ptr(indices), C.byref(k),
                                           _stream(stream)))
@@ -440,9 +487,11 @@ def _row_stride(t):
     return stride[0] if shape[0] > 1 else max(stride[0], shape[1])
 
 
-def _empty(rows, cols, dtype, device):
-    """A new contiguous [rows, cols] tensor (the strided form of torch.empty takes two thirds of its time)."""
-    return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
+def _empty(rows, cols, dtype, device, stream):
+    """A new contiguous [rows, cols] output (the strided form of torch.empty takes two thirds of its time)."""
+    if stream is None:
+        return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
+    return _new((rows, cols), dtype, device, stream)
 
 
 def _dtype_of(dtype):
@@ -459,13 +508,14 @@ def qless_activation_quantize(x, group=32, codes=None, scales=None, stream=None)
     T, width = x.shape
     groups = -(-width // max(int(group), 1))
     if codes is None:
-        codes = _empty(T, width, torch.int8, x.device)
+        codes = _empty(T, width, torch.int8, x.device, stream)
     elif codes.shape != (T, width) or codes.dtype != torch.int8:
         raise ValueError("codes must be int8 [tokens, width]")
     if scales is None:
-        scales = _empty(T, groups, torch.uint8, x.device)
+        scales = _empty(T, groups, torch.uint8, x.device, stream)
     elif scales.shape != (T, groups) or scales.dtype != torch.uint8:
         raise ValueError("scales must be uint8 [tokens, ceil(width / group)]")
+    _used(stream, x, codes, scales)
     _check(lib().qless_activation_quantize(x.data_ptr(), _dtype_code(x), T, width, _row_stride(x), group, codes.data_ptr(), _row_stride(codes),
                                            scales.data_ptr(), _row_stride(scales), _stream(stream)))
     return codes, scales
@@ -477,9 +527,10 @@ def qless_activation_dequantize(codes, scales, group=32, dtype=torch.bfloat16, o
     if codes.dtype != torch.int8 or scales.dtype != torch.uint8 or scales.shape != (T, -(-width // max(int(group), 1))):
         raise ValueError("codes must be int8 [tokens, width] and scales uint8 [tokens, ceil(width / group)]")
     if out is None:
-        out = _empty(T, width, dtype, codes.device)
+        out = _empty(T, width, dtype, codes.device, stream)
     elif out.shape != (T, width):
         raise ValueError("out must be [tokens, width]")
+    _used(stream, codes, scales, out)
     _check(lib().qless_activation_dequantize(_ptr(codes), _row_stride(codes), _ptr(scales), _row_stride(scales), T, width, group,
                                              _ptr(out), _dtype_code(out), _row_stride(out), _stream(stream)))
     return out
@@ -510,10 +561,11 @@ def qless_lora_gradients(codes, scales, grad_out, lora_a, lora_b, offsets, scali
     if not lora_a.is_contiguous() or not lora_b.is_contiguous():
         raise ValueError("lora_a and lora_b must be contiguous")
     if grads is None:
-        grads = _empty(n, rank * (wi + wo), dtype, codes.device)
+        grads = _empty(n, rank * (wi + wo), dtype, codes.device, stream)
     elif grads.shape != (n, rank * (wi + wo)):
         raise ValueError("grads must be [n, rank * (in + out)]")
-    ws = _workspace(qless_lora_gradients_workspace(T, n, wi, wo, rank, grads.dtype), codes.device, workspace)
+    ws = _workspace(qless_lora_gradients_workspace(T, n, wi, wo, rank, grads.dtype), codes.device, workspace, stream)
+    _used(stream, codes, scales, grad_out, lora_a, lora_b, grads, workspace)
     _check(lib().qless_lora_gradients(_ptr(codes), _row_stride(codes), _ptr(scales), _row_stride(scales), group, _ptr(grad_out),
                                       _row_stride(grad_out), _ptr(lora_a), _ptr(lora_b), _ptr(off), T, n, wi, wo, rank, scaling,
                                       _ptr(grads), _dtype_code(grads), _row_stride(grads), _ptr(ws), ws.numel(), _stream(stream)))
@@ -543,17 +595,18 @@ def qless_lm_loss(hidden, weight, labels, token_weight=None, want_hidden=True, w
     out = out or {}
     loss = out.get("loss")
     if loss is None:
-        loss = torch.empty(T, dtype=torch.float32, device=dev)
+        loss = _new(T, torch.float32, dev, stream)
     gh = out.get("grad_hidden")
     if gh is None and want_hidden:
-        gh = _empty(T, width, torch.bfloat16, dev)
+        gh = _empty(T, width, torch.bfloat16, dev, stream)
     gw = out.get("grad_weight")
     if gw is None and want_weight:
-        gw = _empty(vocab, width, torch.bfloat16, dev)
+        gw = _empty(vocab, width, torch.bfloat16, dev, stream)
     for t, shape in ((loss, (T,)), (gh, (T, width)), (gw, (vocab, width))):
         if t is not None and (t.shape != shape or t.dtype != (torch.float32 if t is loss else torch.bfloat16)):
             raise ValueError("an output has the wrong shape or type")
-    ws = _workspace(qless_lm_loss_workspace(T, width, vocab, gh is not None, gw is not None), dev, workspace)
+    ws = _workspace(qless_lm_loss_workspace(T, width, vocab, gh is not None, gw is not None), dev, workspace, stream)
+    _used(stream, hidden, weight, labels, token_weight, loss, gh, gw, workspace)
     _check(lib().qless_lm_loss(_ptr(hidden), _row_stride(hidden), _ptr(weight), _row_stride(weight), _ptr(labels), _ptr(token_weight),
                                T, width, vocab, _ptr(loss), _ptr(gh), _row_stride(gh) if gh is not None else 0,
                                _ptr(gw), _row_stride(gw) if gw is not None else 0, _ptr(ws), ws.numel(), _stream(stream)))
@@ -590,7 +643,7 @@ def qless_microbench(what, iters, device="cuda", stream=None, scratch=None):
     uint8 device tensor of at least 4 MiB whose contents the streaming benchmarks read (default: uninitialised)."""
     ms, ops = C.c_float(0), C.c_double(0)
     if scratch is None:
-        scratch = torch.empty(4 << 20, dtype=torch.uint8, device=device)
+        scratch = _new(4 << 20, torch.uint8, device, stream)
     _check(lib().qless_microbench(MICROBENCH[what], int(iters), C.byref(ms), C.byref(ops), _ptr(scratch), scratch.numel(),
                                   _stream(stream)))
     return ms.value, ops.value
