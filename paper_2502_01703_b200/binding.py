@@ -605,6 +605,8 @@ def qless_lm_loss(hidden, weight, labels, token_weight=None, want_hidden=True, w
     for t, shape in ((loss, (T,)), (gh, (T, width)), (gw, (vocab, width))):
         if t is not None and (t.shape != shape or t.dtype != (torch.float32 if t is loss else torch.bfloat16)):
             raise ValueError("an output has the wrong shape or type")
+    if not loss.is_contiguous():
+        raise ValueError("loss must be contiguous")
     ws = _workspace(qless_lm_loss_workspace(T, width, vocab, gh is not None, gw is not None), dev, workspace, stream)
     _used(stream, hidden, weight, labels, token_weight, loss, gh, gw, workspace)
     _check(lib().qless_lm_loss(_ptr(hidden), _row_stride(hidden), _ptr(weight), _row_stride(weight), _ptr(labels), _ptr(token_weight),
