@@ -487,6 +487,16 @@ def _row_stride(t):
     return stride[0] if shape[0] > 1 else max(stride[0], shape[1])
 
 
+def _on_gpu(stream, *tensors):
+    """Refuses tensors (None: absent) that the call's kernels cannot read: in host memory, or on another GPU than its stream."""
+    at = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and (at < 0 or t.get_device() != at):
+            raise ValueError("all tensors must be on one GPU")
+    if at != (torch.cuda.current_device() if stream is None else stream.device_index):
+        raise ValueError("the tensors must be on the GPU of the stream")
+
+
 def _empty(rows, cols, dtype, device, stream):
     """A new contiguous [rows, cols] output (the strided form of torch.empty takes two thirds of its time)."""
     if stream is None:
@@ -515,6 +525,7 @@ def qless_activation_quantize(x, group=32, codes=None, scales=None, stream=None)
         scales = _empty(T, groups, torch.uint8, x.device, stream)
     elif scales.shape != (T, groups) or scales.dtype != torch.uint8:
         raise ValueError("scales must be uint8 [tokens, ceil(width / group)]")
+    _on_gpu(stream, x, codes, scales)
     _used(stream, x, codes, scales)
     _check(lib().qless_activation_quantize(x.data_ptr(), _dtype_code(x), T, width, _row_stride(x), group, codes.data_ptr(), _row_stride(codes),
                                            scales.data_ptr(), _row_stride(scales), _stream(stream)))
@@ -530,6 +541,7 @@ def qless_activation_dequantize(codes, scales, group=32, dtype=torch.bfloat16, o
         out = _empty(T, width, dtype, codes.device, stream)
     elif out.shape != (T, width):
         raise ValueError("out must be [tokens, width]")
+    _on_gpu(stream, codes, scales, out)
     _used(stream, codes, scales, out)
     _check(lib().qless_activation_dequantize(_ptr(codes), _row_stride(codes), _ptr(scales), _row_stride(scales), T, width, group,
                                              _ptr(out), _dtype_code(out), _row_stride(out), _stream(stream)))
@@ -564,6 +576,7 @@ def qless_lora_gradients(codes, scales, grad_out, lora_a, lora_b, offsets, scali
         grads = _empty(n, rank * (wi + wo), dtype, codes.device, stream)
     elif grads.shape != (n, rank * (wi + wo)):
         raise ValueError("grads must be [n, rank * (in + out)]")
+    _on_gpu(stream, codes, scales, grad_out, lora_a, lora_b, grads, workspace)
     ws = _workspace(qless_lora_gradients_workspace(T, n, wi, wo, rank, grads.dtype), codes.device, workspace, stream)
     _used(stream, codes, scales, grad_out, lora_a, lora_b, grads, workspace)
     _check(lib().qless_lora_gradients(_ptr(codes), _row_stride(codes), _ptr(scales), _row_stride(scales), group, _ptr(grad_out),
@@ -607,6 +620,7 @@ def qless_lm_loss(hidden, weight, labels, token_weight=None, want_hidden=True, w
             raise ValueError("an output has the wrong shape or type")
     if not loss.is_contiguous():
         raise ValueError("loss must be contiguous")
+    _on_gpu(stream, hidden, weight, labels, token_weight, loss, gh, gw, workspace)
     ws = _workspace(qless_lm_loss_workspace(T, width, vocab, gh is not None, gw is not None), dev, workspace, stream)
     _used(stream, hidden, weight, labels, token_weight, loss, gh, gw, workspace)
     _check(lib().qless_lm_loss(_ptr(hidden), _row_stride(hidden), _ptr(weight), _row_stride(weight), _ptr(labels), _ptr(token_weight),

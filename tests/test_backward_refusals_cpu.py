@@ -13,3 +13,38 @@ def test_a_strided_loss_is_refused():
     # the kernels write it as consecutive numbers
     with pytest.raises(ValueError, match="contiguous"):
         B.qless_lm_loss(*_loss_inputs(), out=dict(loss=torch.zeros(8)[::2]))
+
+
+def test_tensors_in_host_memory_are_refused():
+    # the kernels would read them through their host addresses
+    bf = torch.bfloat16
+    with pytest.raises(ValueError, match="GPU"):
+        B.qless_lm_loss(*_loss_inputs())
+    with pytest.raises(ValueError, match="GPU"):
+        B.qless_activation_quantize(torch.zeros((4, 64)))
+    codes, scales = torch.zeros((4, 64), dtype=torch.int8), torch.zeros((4, 2), dtype=torch.uint8)
+    with pytest.raises(ValueError, match="GPU"):
+        B.qless_activation_dequantize(codes, scales)
+    with pytest.raises(ValueError, match="GPU"):
+        B.qless_lora_gradients(codes, scales, torch.zeros((4, 32), dtype=bf), torch.zeros((8, 64), dtype=bf), torch.zeros((32, 8), dtype=bf), [0, 4])
+
+
+class OnGpu:
+    """Stands in for a tensor on GPU `index` (-1: in host memory)."""
+    def __init__(self, index):
+        self.index = index
+
+    def get_device(self):
+        return self.index
+
+
+def test_one_tensor_elsewhere_is_enough(monkeypatch):
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    B._on_gpu(None, OnGpu(0), None, OnGpu(0))
+    for others in ((OnGpu(0), OnGpu(-1)), (OnGpu(0), None, OnGpu(1)), (OnGpu(-1), OnGpu(0)), (OnGpu(1), OnGpu(1))):
+        with pytest.raises(ValueError, match="GPU"):
+            B._on_gpu(None, *others)
+    stream = type("Stream", (), dict(device_index=1))()
+    B._on_gpu(stream, OnGpu(1), OnGpu(1))
+    with pytest.raises(ValueError, match="GPU"):
+        B._on_gpu(stream, OnGpu(0), OnGpu(0))
