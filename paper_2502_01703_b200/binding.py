@@ -484,7 +484,8 @@ def _row_stride(t):
     shape, stride = t.shape, t.stride()
     if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError("a 2-D tensor with contiguous rows is required")
-    return stride[0] if shape[0] > 1 else max(stride[0], shape[1])
+    # what a single row's stride says means nothing (torch calls such a tensor contiguous whatever it is): the next multiple of 16 will do
+    return stride[0] if shape[0] > 1 else -(-shape[1] // 16) * 16
 
 
 def _on_gpu(stream, *tensors):

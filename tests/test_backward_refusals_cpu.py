@@ -48,3 +48,13 @@ def test_one_tensor_elsewhere_is_enough(monkeypatch):
     B._on_gpu(stream, OnGpu(1), OnGpu(1))
     with pytest.raises(ValueError, match="GPU"):
         B._on_gpu(stream, OnGpu(0), OnGpu(0))
+
+
+@pytest.mark.parametrize("width,pad", [(72, 3), (64, 0), (8, 1), (4096, 5)])
+def test_a_single_row_is_taken_whatever_its_stride_says(width, pad):
+    # a row cut out of a wider buffer is contiguous to torch; its stride of width + 3 would be refused for rows that have neighbours
+    one = torch.zeros((2, width + pad), dtype=torch.bfloat16)[:1, :width]
+    assert one.is_contiguous()
+    assert B._row_stride(one) >= width and B._row_stride(one) % 16 == 0
+    two = torch.zeros((2, width + pad), dtype=torch.bfloat16)[:, :width]
+    assert B._row_stride(two) == width + pad
