@@ -157,11 +157,15 @@ def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
+# The raw handle of a device's current stream without building a Stream object for every call. Not part of torch's public interface:
+# a build of torch that lacks it takes the public way.
+_raw_current = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream=None):
     if stream is not None:
         return stream.cuda_stream
-    # the raw handle of torch.cuda.current_stream(), without building a Stream object for every call
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return _raw_current(torch.cuda.current_device()) if _raw_current is not None else torch.cuda.current_stream().cuda_stream
 
 
 def _dtype_code(t):

@@ -1,4 +1,5 @@
-"""Refusals of the binding's gradient-row calls that no status of the library stands behind: nothing is launched."""
+"""What the binding itself decides for the gradient-row calls, with nothing launched: refusals that no status of the library stands
+behind, the stride it passes, the stream it finds."""
 import pytest
 import torch
 
@@ -58,3 +59,12 @@ def test_a_single_row_is_taken_whatever_its_stride_says(width, pad):
     assert B._row_stride(one) >= width and B._row_stride(one) % 16 == 0
     two = torch.zeros((2, width + pad), dtype=torch.bfloat16)[:, :width]
     assert B._row_stride(two) == width + pad
+
+
+def test_the_current_stream_is_found_without_the_private_call(monkeypatch):
+    monkeypatch.setattr(B, "_raw_current", None)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: type("Stream", (), dict(cuda_stream=5))())
+    assert B._stream() == 5
+    monkeypatch.setattr(B, "_raw_current", lambda device: 7 + device)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    assert B._stream() == 7
