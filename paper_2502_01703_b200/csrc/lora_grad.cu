@@ -22,6 +22,7 @@
 // inputs give the same bits.
 #include <cstring>
 
+#include "lora_items.h"
 #include "qless_kernels.h"
 #include "tc_common.cuh"
 
@@ -192,14 +193,9 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
     ahead_wait();
     const uint32_t tmem = bars->tmem_base;                  // accumulators at columns 0 and 128, expanded codes of stage s at 256 + 64 s
 
-    // item -> (slice, token tile, kind): of two neighbouring items one reads codes and one dY, and a block takes them in turn, so that at
-    // any time half of the blocks read the one (bound by the work per block of codes) and half the other (bound by its bytes).
-    const int64_t per_slice = 2LL * p.token_tiles;
     auto item_of = [&](int64_t item, int& slice, bool& is_x, int64_t& tile, int& kb0, int& kb1) {
-        slice = (int)(item / per_slice);
-        const int64_t r = item - slice * per_slice;
-        is_x = ((r + item / gridDim.x) & 1) != 0;
-        tile = r >> 1;
+        const FactorItem f = factor_item(item, p.token_tiles, gridDim.x);
+        slice = f.slice; is_x = f.is_x; tile = f.tile;
         const int all = ((is_x ? p.in : p.out) + CH - 1) / CH, step = is_x ? p.kb_x : p.kb_y;
         kb0 = min(all, slice * step);
         kb1 = min(all, kb0 + step);
