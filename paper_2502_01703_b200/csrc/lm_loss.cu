@@ -129,7 +129,6 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     const uint32_t rank = cluster_ctarank();
     const int64_t pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
 
-    ahead_release();
     if (threadIdx.x == 0) {
         for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&bars->d_full[s]), 1); mbar_init(smem_u32(&bars->d_empty[s]), 16); }
@@ -144,7 +143,6 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;                   // accumulators at columns 0 and 256
-    ahead_wait();
     const bool idle = p.gate != nullptr && *p.gate == 0;     // the same for every thread of the grid
 
     const int count = p.meta->count;
@@ -510,8 +508,6 @@ __global__ void __launch_bounds__(1024) loss_gather_kernel(const GatherArgs a)
         a.label_logit[at] = l2;
         a.rowp[at] = RowParam{l2, 1.0f, 0.0f, 0.0f};
     };
-    ahead_release();
-    ahead_wait();
     int32_t base = 0, listed = 0;                                // tokens kept so far, and how many of them fell to this block since the last flush
     auto flush = [&]() {                                         // whole block
         __syncthreads();
@@ -628,8 +624,6 @@ struct RowArgs {
 constexpr int ROWS = 8;
 __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowArgs a)
 {
-    ahead_release();
-    ahead_wait();
     if (a.gate != nullptr && *a.gate == 0) return;
     __shared__ float2 part[32][ROWS];
     const int r = threadIdx.x & (ROWS - 1), seg = threadIdx.x / ROWS, warp = threadIdx.x >> 5;
@@ -697,8 +691,6 @@ __global__ void loss_finish_kernel(const float* __restrict__ acc, int32_t width,
                                    const int32_t* __restrict__ place, const int32_t* __restrict__ labels, const float2* __restrict__ coef, int32_t sums,
                                    const __nv_bfloat16* __restrict__ weight, int64_t ld_weight, int64_t T, __nv_bfloat16* __restrict__ out, int64_t ld_out)
 {
-    ahead_release();
-    ahead_wait();
     const int vecs = width / 8, splits = meta->splits;
     const int64_t slice = (int64_t)(meta->count + 255) / 256 * 256;
     const int64_t total = T * vecs;
@@ -732,10 +724,11 @@ __global__ void loss_finish_kernel(const float* __restrict__ acc, int32_t width,
     }
 }
 
-// These kernels do not begin before the one ahead has ended (a chain of launches on CTA pairs that overlapped stopped, once in some thousand
-// calls, for a reason that was not found).
+// Launched in order: none of these kernels begins before the one ahead has ended, and none lets the one behind it in early (a kernel of
+// another operator launched ahead begins when the last of these has ended). A chain of launches on CTA pairs that overlapped stopped, once in some
+// thousand calls, for a reason that was not found.
 template <typename... Params, typename... Args>
-cudaError_t launch_after(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args)
+cudaError_t launch_in_order(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, Args&&... args)
 {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = st;
@@ -758,7 +751,7 @@ qless_status launch_gemm(const char* name, const CUtensorMap& a, const CUtensorM
     int64_t grid = sm_count() / 2 * 2;
     if (grid > 2 * max_items) grid = 2 * max_items;
     { ProfileScope ps(name, st);
-      QLESS_CUDA_TRY(launch_after(head_gemm_kernel<MODE, SWAP>, dim3((unsigned)grid), dim3(NTHREADS), smem, st, a, b, p)); }
+      QLESS_CUDA_TRY(launch_in_order(head_gemm_kernel<MODE, SWAP>, dim3((unsigned)grid), dim3(NTHREADS), smem, st, a, b, p)); }
     count_launches(1);
     return QLESS_OK;
 }
@@ -837,7 +830,7 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
       const int32_t kb = ((a.vocab < pl.piece ? a.vocab : pl.piece) + KB - 1) / KB;
       g.most_slices = kb / 3 > 1 ? kb / 3 : 1; g.order = order; g.place = place;
       g.out_labels = labels; g.out_weight = weight; g.label_logit = logit; g.loss = a.loss; g.rowp = rowp; g.out = hidden; g.meta = meta;
-      QLESS_CUDA_TRY(launch_after(loss_gather_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, g)); }
+      QLESS_CUDA_TRY(launch_in_order(loss_gather_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, g)); }
     count_launches(1);
 
     CUtensorMap tm_x, tm_w, tm_p;
@@ -871,7 +864,7 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
         r.meta = meta; r.gate = gate; r.kind = kind; r.entries = entries; r.tpad = pl.tpad; r.stat = stat; r.psum = psum; r.label_logit = logit;
         r.weight = weight; r.order = order; r.rowp = rowp; r.coef = coef; r.loss = a.loss;
         { ProfileScope ps("loss_rows", st);
-          QLESS_CUDA_TRY(launch_after(loss_rows_kernel, dim3(grid_of(a.T, ROWS)), dim3(1024), 0, st, r)); }
+          QLESS_CUDA_TRY(launch_in_order(loss_rows_kernel, dim3(grid_of(a.T, ROWS)), dim3(1024), 0, st, r)); }
         count_launches(1);
         return QLESS_OK;
     };
@@ -915,7 +908,7 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
     }
     if (want_h) {
         { ProfileScope ps("loss_finish", st);
-          QLESS_CUDA_TRY(launch_after(loss_finish_kernel, dim3(grid_of(a.T * (a.width / 8), 256)), dim3(256), 0, st, (const float*)acc, a.width, (const LossMeta*)meta,
+          QLESS_CUDA_TRY(launch_in_order(loss_finish_kernel, dim3(grid_of(a.T * (a.width / 8), 256)), dim3(256), 0, st, (const float*)acc, a.width, (const LossMeta*)meta,
                                       (const int32_t*)place, (const int32_t*)labels, (const float2*)coef, (int32_t)(want_w ? 0 : 1),
                                       reinterpret_cast<const __nv_bfloat16*>(a.weight), a.ld_weight, a.T, reinterpret_cast<__nv_bfloat16*>(a.grad_hidden),
                                       a.ld_grad_hidden)); }
