@@ -198,6 +198,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                     __syncwarp();
                 }
             }
+            if (ok) ok = __all_sync(0xFFFFFFFFu, ring_drained(bars->empty, ring, nS, abort_flag, p.timeout_word, TO_PRODUCER));
             if (!ok) {       // leave no copy in flight: the leader waits (bounded) for the stages that are armed, the peer idles
                 if (rank == 0) {
                     for (uint32_t j = (it > nS ? it - nS : 0u); j < it; ++j)
@@ -467,6 +468,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     }
     tc_fence_before();
     __syncthreads();
+    if (warp == 1) pair_drained(&bars->drain);
     cluster_sync_all();
     if (warp == 1) { tc_fence_after(); tmem_dealloc_pair(tmem, 512); }
     cluster_sync_all();                                      // neither CTA of the pair is gone before both have given their half back

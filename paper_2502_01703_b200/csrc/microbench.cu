@@ -226,7 +226,7 @@ mma_tma_mix_kernel(const __grid_constant__ CUtensorMap tmap, int iters, int with
             }
             mma_commit_pair(smem_u32(&bars->empty[it % MX_STAGES]));      // arrives in both CTAs
         }
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&bars->done)) : "memory");
+        mma_commit_pair(smem_u32(&bars->done));
         mbar_wait(smem_u32(&bars->done), 0, &bars->abort_flag, timeout_word, TO_MMA);
     } else if (threadIdx.x == 32 && with_copies) {
         bool ok = true;
@@ -254,6 +254,9 @@ mma_tma_mix_kernel(const __grid_constant__ CUtensorMap tmap, int iters, int with
     }
     tc_fence_before();
     __syncthreads();
+    // (the peer may have been here from the start: a wait as long as the run)
+    if (threadIdx.x == 0) mbar_wait(smem_u32(&bars->done), 0, &bars->abort_flag, timeout_word, TO_MMA);
+    __syncwarp();
     cluster_sync_all();
     if (warp == 0) {
         tc_fence_after();
@@ -314,7 +317,7 @@ mma_stream_consume_kernel(const __grid_constant__ CUtensorMap tmap, int iters, u
             }
             mma_commit_pair(smem_u32(&bars->empty[s]));      // arrives in both CTAs
         }
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&bars->done)) : "memory");
+        mma_commit_pair(smem_u32(&bars->done));
         mbar_wait_quiet(smem_u32(&bars->done), 0u);
     } else if (threadIdx.x == 32) {
         // both CTAs: this CTA's three boxes of every stage; all of a stage's bytes complete on the leader's barrier
@@ -341,6 +344,7 @@ mma_stream_consume_kernel(const __grid_constant__ CUtensorMap tmap, int iters, u
     }
     tc_fence_before();
     __syncthreads();
+    if (warp == 0) pair_drained(&bars->done);
     cluster_sync_all();
     if (warp == 0) {
         tc_fence_after();

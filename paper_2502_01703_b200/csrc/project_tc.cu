@@ -96,6 +96,7 @@ project_tc_kernel(const __grid_constant__ CUtensorMap tmap_gamma, int64_t n, int
         // ------------------------------- TMA producer -------------------------------
         if (lane == 0) {
             uint32_t it = 0;     // global stage counter
+            struct Ring { uint32_t slot, parity; __device__ void next(uint32_t n) { if (++slot == n) { slot = 0; parity ^= 1u; } } };
             bool ok = true;
             for (int64_t item = pair; item < num_items && ok; item += num_pairs) {
                 const int64_t nt = item / ((int64_t)num_chunks * num_dt);
@@ -119,6 +120,7 @@ project_tc_kernel(const __grid_constant__ CUtensorMap tmap_gamma, int64_t n, int
                                          (int32_t)((kb64 + h) * n + nt * BN + rank * (BN / 2)));
                 }
             }
+            if (ok) ok = ring_drained(bars->b_empty, Ring{it % SB, (it / SB) & 1u}, SB, abort_flag, timeout_word, TO_PRODUCER);
             if (!ok) {
                 // Leave no copy in flight behind us. Stages 0 .. it-1 have been armed; all but the last SB of them were
                 // consumed before their slot was armed again. Every copy of the pair completes on the leader's barrier,
@@ -243,6 +245,9 @@ project_tc_kernel(const __grid_constant__ CUtensorMap tmap_gamma, int64_t n, int
                 if (lane == 0) mbar_arrive_leader_tmem(smem_u32(&bars->a_full[sa]), rank);
             }
         }
+        // the group's own stage free once more: the last commit of its barrier has arrived here
+        const uint32_t end = ita + ((ita & 1u) != grp ? 1u : 0u);
+        if (ok) mbar_wait_cluster(smem_u32(&bars->a_empty[grp]), ((end / SA) & 1u) ^ 1u, abort_flag, timeout_word, TO_GENERATOR);
     } else {
         // ------------------------------- accumulator drain -------------------------------
         const int q = warp & 3;
@@ -278,6 +283,7 @@ project_tc_kernel(const __grid_constant__ CUtensorMap tmap_gamma, int64_t n, int
 
     tc_fence_before();
     __syncthreads();
+    if (warp == 1) pair_drained(&bars->drain);
     cluster_sync_all();                 // neither CTA frees tensor memory or exits while its peer may still touch it
     if (warp == 1) {
         tc_fence_after();

@@ -247,8 +247,10 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmap_train, const __grid_con
                                 tma_load_3d_pair(smem_u32(st + A_SMEM + bh1), &tmap_val2, full, kb * KB, vt * p.vpad + p.n1 + (int)rank * (p.n2 / 2), i);
                         }
             }
+            const Ring end = st_ring;
             // an odd number of stages in all: the last pair's barrier still lacks its second arrival
             if (DIRECT && ok && (it & 1u) && rank == 0) mbar_arrive(smem_u32(&bars->full[st_ring.slot & ~1u]));
+            if (ok) ok = ring_drained(bars->empty, end, (uint32_t)p.nS, abort_flag, p.timeout_word, TO_PRODUCER);
             if (!ok) {
                 // Leave no copy in flight behind us. Packed loads 0 .. pq-1 have been issued into this CTA's own ring
                 // (barriers of its own: wait, bounded, for the phases of the last nP of them). Operand stages 0 .. it-1
@@ -588,6 +590,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmap_train, const __grid_con
 
     tc_fence_before();
     __syncthreads();
+    if (warp == 1) pair_drained(&bars->drain);
     cluster_sync_all();                 // neither CTA frees tensor memory or exits while its peer may still touch it
     if (warp == 1) {
         tc_fence_after();

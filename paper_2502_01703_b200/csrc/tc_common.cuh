@@ -121,6 +121,11 @@ __device__ __forceinline__ bool elect_one()
 }
 
 // ---- CTA pairs (cta_group::2) --------------------------------------------------------------------
+// A commit of the pair's leader (mma_commit_pair) arrives on a barrier in both CTAs' shared memory. Neither CTA may leave before the last of
+// these arrivals has landed in it, for its shared memory may be another block's by then, and the cluster barrier at the end orders the
+// pair's threads, not the arrivals of commits. So the role that waits for the slots of a ring waits, behind its last use of it, for all of them
+// to be free once more (ring_drained), and at the end both CTAs wait for the leader's last commit (pair_drained; the roles have ended, so this is
+// short; bounded: after a failed wait the leader's commits still come).
 __device__ __forceinline__ uint32_t cluster_ctarank()
 {
     uint32_t r;
@@ -184,6 +189,15 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity,
     atomicOr(timeout_word, code);
     return false;
 }
+template <typename Ring>
+__device__ __forceinline__ bool ring_drained(uint64_t* empty, Ring ring, uint32_t slots, volatile uint32_t* abort_flag, unsigned int* timeout_word,
+                                             uint32_t code)
+{
+    for (uint32_t j = 0; j < slots; ++j, ring.next(slots))
+        if (!mbar_wait_cluster(smem_u32(&empty[ring.slot]), ring.parity ^ 1u, abort_flag, timeout_word, code)) return false;
+    return true;
+}
+__device__ __forceinline__ void pair_drained(uint64_t* drain) { mbar_wait_quiet(smem_u32(drain), 0u); }
 // TMA tile load whose completion is signalled on a barrier that may belong to the peer CTA of the pair.
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t smem_dst, const CUtensorMap* tmap, uint32_t bar_cluster_addr,
                                                  int32_t c0, int32_t c1)
