@@ -416,8 +416,9 @@ qless_status qless_lora_gradients(const int8_t* codes, int64_t ld_codes, const u
  * (the gradients of sum_t w_t loss[t]). A token whose label lies outside [0, vocab), e.g. -100, carries no loss: its loss
  * and gradient row are 0, and whatever its hidden row and weight hold (infinities and NaN included) reaches nothing.
  * Logits are fp32 sums of exact products; the softmax statistics and all accumulators are fp32; the probabilities enter the
- * second product rounded to bf16 (with 1 - p of the label kept apart in fp32, so that tokens the model is sure of lose
- * nothing), and a gradient is rounded once more to bf16. The same inputs give the same bits.
+ * second product rounded to bf16, and a gradient is rounded once more to bf16. 1 - p of the label is formed apart from p, so that
+ * tokens the model is sure of lose no digits to a difference; in grad_hidden it acts as the fp32 number that it is, in grad_weight rounded to
+ * bf16 like the other probabilities. The same inputs give the same bits.
  * Requirements: tokens < 2^31 - 256; 1 <= vocab < 2^31 - 256; width a multiple of 8, 8 <= width <= 65536; hidden, weight,
  * grad_hidden, grad_weight 16-byte aligned, their row strides multiples of 8. */
 size_t qless_lm_loss_workspace(int64_t tokens, int32_t width, int32_t vocab, int32_t want_hidden, int32_t want_weight);
