@@ -680,8 +680,8 @@ __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowArgs a)
             const float e = exp2f(-fabsf(d)), tail = log1pf(e);
             float nll = d > 0.0f ? d * LN2 + tail : tail;
             float sigma = d > 0.0f ? 1.0f / (1.0f + e) : e / (1.0f + e);
-            if (others == -INFINITY) { nll = ly == ly ? 0.0f : ly; sigma = nll; }
-            else if (d != d) { nll = d; sigma = d; }
+            if (others == -INFINITY) { nll = ly - ly; sigma = nll; }               // 0; NaN where the label's logit is infinite or NaN
+            else if (d != d || ly == INFINITY) { nll = NAN; sigma = NAN; }         // (infinity - infinity)
             a.loss[a.order[row]] = nll;
             if (a.kind == ROW_FROM_SUMS) a.coef[row] = make_float2(w * sigma, s == 0.0f ? 0.0f : 1.0f / s);
             else a.rowp[row] = RowParam{fmaxf(others, ly) + tail * LOG2E, w, -w * sigma, 0.0f};      // the full normaliser
