@@ -101,7 +101,12 @@ __device__ __forceinline__ void expand4(uint32_t w, uint32_t step2, uint32_t& lo
     lo = codes_to_bf16x2(__byte_perm(w, 0x43434343u, 0x4140), step2);
     hi = codes_to_bf16x2(__byte_perm(w, 0x43434343u, 0x4342), step2);
 }
-__device__ __forceinline__ uint32_t step_bf16x2(uint32_t byte) { return (byte << 7) | (byte << 23); }      // 0xFF: infinity, and 0 * infinity = NaN
+// The step in both halves. 0xFF becomes NaN and not infinity, of which a code other than 0 would make an infinite value.
+__device__ __forceinline__ uint32_t step_bf16x2(uint32_t byte)
+{
+    const uint32_t one = (byte << 7) | (((byte + 1) >> 2) & 0x40u);
+    return one | (one << 16);
+}
 
 // Up to four consecutive step bytes, the first in the low byte. Volatile: requested here, a block before they are used, and not
 // where the compiler sees the use. `whole`: the groups of 128 channels start at a multiple of their number of bytes in memory.
