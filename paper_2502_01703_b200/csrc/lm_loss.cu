@@ -23,8 +23,8 @@
 // Gradient of the hidden states alone: two products instead of three. The reference r of a row is its label's logit, a dot product
 // taken when the row is gathered. Any reference gives the same softmax, and with the exponents of fp32 and bf16 one that lies up to
 // LIMIT = 64 powers of two (a loss of 44) below the row's maximum is as good as the maximum itself. Should a row exceed that, a flag
-// sends the rest through a second pass whose reference is the true maximum: its launches are always enqueued and return at once
-// when the flag is not set (the host does not wait to find out).
+// sends all rows through a second pass whose reference is the true maximum: its launches are always enqueued and return at once
+// when the flag is not set (the host does not wait to find out). A single such row, or one with an infinity, so costs the batch both products again.
 // With dW the normaliser has to be known before the piece is written: STATS first, then PROBS, GRAD_H and GRAD_W per piece.
 #include "qless_kernels.h"
 #include "tc_common.cuh"
@@ -119,6 +119,10 @@ template <int MODE, bool SWAP>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NTHREADS, 1)
 head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, const GemmParams p)
 {
+    // Nothing to do: leave before there are barriers and tensor memory to give back. Gate, count and slices are the same for every thread of the grid and
+    // for both CTAs of a pair, each reads them for itself: the launches before this one have ended, and the only writer among these kernels
+    // sets the gate of a second pass, which has begun only because it is set.
+    if (p.gate != nullptr && *p.gate == 0) return;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const int half_b = SWAP ? p.b_rows * 2 * KB : HALF;        // bytes of a stage's B operand in this CTA
@@ -145,7 +149,6 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     cluster_sync_all();
     tc_fence_after();
     const uint32_t tmem = bars->tmem_base;                   // accumulators at columns 0 and 256
-    const bool idle = p.gate != nullptr && *p.gate == 0;     // the same for every thread of the grid
 
     const int count = p.meta->count;
     const int mt = ((MODE == GRAD_W ? p.rows : SWAP ? (count > 0 ? p.cols : 0) : count) + 255) / 256, nt = SWAP ? 1 : (p.cols + 255) / 256;
@@ -153,7 +156,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     const int kblocks = ((MODE == GRAD_W ? count : p.k) + KB - 1) / KB;
     const int ksplit = (kblocks + splits - 1) / splits;
     const int64_t per_split = (int64_t)mt * nt;
-    const int64_t items = idle ? 0 : per_split * splits;
+    const int64_t items = per_split * splits;
     // item -> (split, column tile, row tile): GROUP_M row tiles at a time, row tiles fastest
     auto item_of = [&](int64_t item, int& split, int& m, int& n, int& kb0, int& kb1) {
         split = (int)(item / per_split);
@@ -774,10 +777,11 @@ LossPlan plan_loss(int64_t T, int32_t width, int32_t vocab, bool want_h, bool wa
     pl.tpad = (T + 255) / 256 * 256;
     const int64_t mt = pl.tpad / 256, pairs = sm_count() / 2, nt_h = (width + 255) / 256;
     const int64_t tiles_v = ((int64_t)vocab + 255) / 256;
-    // The normaliser first (one more product): for the loss alone, and with the gradient of the weights. For the gradient of the hidden
-    // states a reference that may have to be redone is never slower, the smallest problems included (28 tokens x 1720 x 1079: 38 us
-    // against 43 us with the product first, 33 x 512 x 4099: 36.7 against 36.0 us, 88 x 4040 x 2783: 57 against 73 us; measured
-    // with launches that overlapped).
+    // The normaliser first (one more product, six launches): for the loss alone, and with the gradient of the weights. For the gradient of the
+    // hidden states alone a reference that may have to be redone (nine launches, four of which leave at once): the product that it saves counts
+    // from a few MB of W on, the three launches cost 3 to 4 us where there is next to no product (against the normaliser first: 1 token x 512 x 1000
+    // 49.7 for 45.6 us, 33 x 512 x 4099 54.5 for 50.7, 28 x 1720 x 1079 53.4 for 54.8, 88 x 4040 x 2783 68 for 85, 64 x 4096 x 32001 137 for 176,
+    // 1024 x 2048 x 32001 237 for 317).
     pl.exact = !want_h || want_w;
     // Piece of the vocabulary whose probabilities are held at once: at most 512 MiB of bf16.
     int64_t piece_tiles = ((int64_t)512 << 20) / (pl.tpad * 256 * 2);
