@@ -18,8 +18,11 @@
 //   PROBS   h W^T        epilogue: exp(l - r) or w (p - [v = y]) as bf16 into one piece of the vocabulary    (gradients)
 //   GRAD_H  piece * W    epilogue: fp32, added to what the earlier pieces left
 //   GRAD_W  piece^T * h  epilogue: bf16 rows of dW
-// Up to FEW = 256 tokens the roles of rows and columns are swapped (256 rows of W, or hidden channels, by all tokens): with the tokens
-// as the 256 rows of a tile most of the tensor pipe's work would go to rows that do not exist, and took longer than W's bytes.
+// Up to FEW = 192 tokens the roles of rows and columns are swapped (256 rows of W, or hidden channels, by all tokens): with the tokens
+// as the 256 rows of a tile most of the tensor pipe's work would go to rows that do not exist, and takes longer than W's bytes. The swapped epilogue
+// exchanges a row's partial sums between lanes, which costs more the more tokens there are (hidden states' gradient, swapped against not:
+// 64 tokens x 4096 x 32001 138 for 157 us, 128 tokens 147 for 164, 192 tokens 161 for 165, 224 tokens 168 for 166, 256 tokens 177 for 171;
+// x 2048 x 50021: 96 tokens 127 for 134 us, 160 tokens 144 for 143, 192 tokens 151 for 146, 224 tokens 169 for 156).
 // Gradient of the hidden states alone: two products instead of three. The reference r of a row is its label's logit, a dot product
 // taken when the row is gathered. Any reference gives the same softmax, and with the exponents of fp32 and bf16 one that lies up to
 // LIMIT = 64 powers of two (a loss of 44) below the row's maximum is as good as the maximum itself. Should a row exceed that, a flag
@@ -39,7 +42,8 @@ constexpr int NTHREADS = 320;               // warp 0 TMA, warp 1 MMA, warps 2-9
 constexpr int MAX_STAGES = 5;
 constexpr int KB = 128;                     // K columns per stage: 64 KiB of operands per CTA
 constexpr int HALF = 32768;                 // bytes of the A operand of a stage (and of B, where it has 256 columns)
-constexpr int FEW = 256;                    // tokens up to which the roles are swapped
+constexpr int FEW = 192;                    // tokens up to which the roles are swapped
+constexpr int ROOM = 256;                   // token rows that the swapped roles' sums and tables have room for
 constexpr int GROUP_M = 16;                 // row tiles that share a pass over the column tiles (their operand stays in L2)
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LIMIT = 64.0f;
@@ -76,8 +80,8 @@ struct GemmParams {
 struct __align__(8) Bars {
     uint64_t full[MAX_STAGES], empty[MAX_STAGES], d_full[2], d_empty[2], drain;
     uint32_t tmem_base, abort_flag;
-    __align__(16) RowParam rowp[FEW];       // swapped roles: of every token
-    int32_t label[FEW];
+    __align__(16) RowParam rowp[ROOM];      // swapped roles: of every token
+    int32_t label[ROOM];
 };
 
 struct Ring {
@@ -284,7 +288,7 @@ head_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
                 const int t0 = half * p.b_rows + c0, have = lim - c0;
                 if (MODE == GRAD_H) {
                     if (v < p.cols) {
-                        float* dst = p.acc + ((int64_t)split * FEW + t0) * p.cols + v;
+                        float* dst = p.acc + ((int64_t)split * ROOM + t0) * p.cols + v;
 #pragma unroll
                         for (int k = 0; k < 32; ++k) {
                             if (k >= have) break;

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_2502_01703_b200 import binding as B
+from test_lm_loss_gpu import _case, check, reference
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -156,3 +157,12 @@ def test_the_calls_in_a_graph():
         B.qless_check()
         for have, want in zip(got, calls()):
             assert torch.equal(have, want)
+
+
+@pytest.mark.parametrize("wants", [(False, False), (True, False), (False, True), (True, True)])
+@pytest.mark.parametrize("T,width,vocab", [(161, 136, 2500), (192, 264, 1024), (193, 264, 1025), (255, 72, 4099)])
+def test_the_loss_around_the_change_of_orientation(T, width, vocab, wants):
+    case = _case(T, width, vocab, 61, 0.9, pad=8)
+    got = B.qless_lm_loss(*case, want_hidden=wants[0], want_weight=wants[1])
+    B.qless_check()
+    check(got, reference(*case), T, vocab)
