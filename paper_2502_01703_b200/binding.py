@@ -162,10 +162,13 @@ def _ptr(t):
 _raw_current = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream(stream=None):
+def _stream(stream=None, device=None):
+    """The stream's raw handle; None: that of the current stream (device: the current one, where the caller has asked already)."""
     if stream is not None:
         return stream.cuda_stream
-    return _raw_current(torch.cuda.current_device()) if _raw_current is not None else torch.cuda.current_stream().cuda_stream
+    if _raw_current is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_current(torch.cuda.current_device() if device is None else device)
 
 
 def _dtype_code(t):
@@ -493,13 +496,15 @@ def _row_stride(t):
 
 
 def _on_gpu(stream, *tensors):
-    """Refuses tensors (None: absent) that the call's kernels cannot read: in host memory, or on another GPU than its stream."""
+    """The GPU that a call runs on. Refuses tensors (None: absent) that its kernels cannot read: in host memory, or on another GPU than its
+    stream. Outputs that the binding has just made beside an input need no look."""
     at = tensors[0].get_device()
     for t in tensors:
         if t is not None and (at < 0 or t.get_device() != at):
             raise ValueError("all tensors must be on one GPU")
     if at != (torch.cuda.current_device() if stream is None else stream.device_index):
         raise ValueError("the tensors must be on the GPU of the stream")
+    return at
 
 
 def _empty(rows, cols, dtype, device, stream):
@@ -522,6 +527,7 @@ def qless_activation_quantize(x, group=32, codes=None, scales=None, stream=None)
     [tokens, ceil(width / group)]): the 8-bit checkpoint of a layer's input, one power-of-two step per group of channels."""
     T, width = x.shape
     groups = -(-width // max(int(group), 1))
+    at = _on_gpu(stream, x, codes, scales) if codes is not None or scales is not None else _on_gpu(stream, x)
     if codes is None:
         codes = _empty(T, width, torch.int8, x.device, stream)
     elif codes.shape != (T, width) or codes.dtype != torch.int8:
@@ -530,10 +536,10 @@ def qless_activation_quantize(x, group=32, codes=None, scales=None, stream=None)
         scales = _empty(T, groups, torch.uint8, x.device, stream)
     elif scales.shape != (T, groups) or scales.dtype != torch.uint8:
         raise ValueError("scales must be uint8 [tokens, ceil(width / group)]")
-    _on_gpu(stream, x, codes, scales)
-    _used(stream, x, codes, scales)
+    if stream is not None:
+        _used(stream, x, codes, scales)
     _check(lib().qless_activation_quantize(x.data_ptr(), _dtype_code(x), T, width, _row_stride(x), group, codes.data_ptr(), _row_stride(codes),
-                                           scales.data_ptr(), _row_stride(scales), _stream(stream)))
+                                           scales.data_ptr(), _row_stride(scales), _stream(stream, at)))
     return codes, scales
 
 
@@ -542,14 +548,15 @@ def qless_activation_dequantize(codes, scales, group=32, dtype=torch.bfloat16, o
     T, width = codes.shape
     if codes.dtype != torch.int8 or scales.dtype != torch.uint8 or scales.shape != (T, -(-width // max(int(group), 1))):
         raise ValueError("codes must be int8 [tokens, width] and scales uint8 [tokens, ceil(width / group)]")
+    at = _on_gpu(stream, codes, scales, out)
     if out is None:
         out = _empty(T, width, dtype, codes.device, stream)
     elif out.shape != (T, width):
         raise ValueError("out must be [tokens, width]")
-    _on_gpu(stream, codes, scales, out)
-    _used(stream, codes, scales, out)
+    if stream is not None:
+        _used(stream, codes, scales, out)
     _check(lib().qless_activation_dequantize(_ptr(codes), _row_stride(codes), _ptr(scales), _row_stride(scales), T, width, group,
-                                             _ptr(out), _dtype_code(out), _row_stride(out), _stream(stream)))
+                                             _ptr(out), _dtype_code(out), _row_stride(out), _stream(stream, at)))
     return out
 
 
@@ -581,12 +588,13 @@ def qless_lora_gradients(codes, scales, grad_out, lora_a, lora_b, offsets, scali
         grads = _empty(n, rank * (wi + wo), dtype, codes.device, stream)
     elif grads.shape != (n, rank * (wi + wo)):
         raise ValueError("grads must be [n, rank * (in + out)]")
-    _on_gpu(stream, codes, scales, grad_out, lora_a, lora_b, grads, workspace)
+    at = _on_gpu(stream, codes, scales, grad_out, lora_a, lora_b, grads, workspace)
     ws = _workspace(qless_lora_gradients_workspace(T, n, wi, wo, rank, grads.dtype), codes.device, workspace, stream)
-    _used(stream, codes, scales, grad_out, lora_a, lora_b, grads, workspace)
+    if stream is not None:
+        _used(stream, codes, scales, grad_out, lora_a, lora_b, grads, workspace)
     _check(lib().qless_lora_gradients(_ptr(codes), _row_stride(codes), _ptr(scales), _row_stride(scales), group, _ptr(grad_out),
                                       _row_stride(grad_out), _ptr(lora_a), _ptr(lora_b), _ptr(off), T, n, wi, wo, rank, scaling,
-                                      _ptr(grads), _dtype_code(grads), _row_stride(grads), _ptr(ws), ws.numel(), _stream(stream)))
+                                      _ptr(grads), _dtype_code(grads), _row_stride(grads), _ptr(ws), ws.numel(), _stream(stream, at)))
     return grads
 
 
@@ -625,12 +633,13 @@ def qless_lm_loss(hidden, weight, labels, token_weight=None, want_hidden=True, w
             raise ValueError("an output has the wrong shape or type")
     if not loss.is_contiguous():
         raise ValueError("loss must be contiguous")
-    _on_gpu(stream, hidden, weight, labels, token_weight, loss, gh, gw, workspace)
+    at = _on_gpu(stream, hidden, weight, labels, token_weight, loss, gh, gw, workspace)
     ws = _workspace(qless_lm_loss_workspace(T, width, vocab, gh is not None, gw is not None), dev, workspace, stream)
-    _used(stream, hidden, weight, labels, token_weight, loss, gh, gw, workspace)
+    if stream is not None:
+        _used(stream, hidden, weight, labels, token_weight, loss, gh, gw, workspace)
     _check(lib().qless_lm_loss(_ptr(hidden), _row_stride(hidden), _ptr(weight), _row_stride(weight), _ptr(labels), _ptr(token_weight),
                                T, width, vocab, _ptr(loss), _ptr(gh), _row_stride(gh) if gh is not None else 0,
-                               _ptr(gw), _row_stride(gw) if gw is not None else 0, _ptr(ws), ws.numel(), _stream(stream)))
+                               _ptr(gw), _row_stride(gw) if gw is not None else 0, _ptr(ws), ws.numel(), _stream(stream, at)))
     return dict(loss=loss, grad_hidden=gh, grad_weight=gw)
 
 

@@ -35,7 +35,7 @@ def world(monkeypatch):
         return made
 
     monkeypatch.setattr(B, "lib", lambda: FakeLibrary())
-    monkeypatch.setattr(B, "_stream", lambda stream=None: (log.current if stream is None else stream).cuda_stream)
+    monkeypatch.setattr(B, "_stream", lambda stream=None, device=None: (log.current if stream is None else stream).cuda_stream)
     monkeypatch.setattr(B, "_on_gpu", lambda *a: None, raising=False)
     monkeypatch.setattr(torch.cuda, "stream", use)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: log.current)
