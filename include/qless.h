@@ -62,13 +62,13 @@ typedef struct {
 const char* qless_last_error(void);
 
 /* Reads and clears the device-side timeout flag after synchronising `cuda_stream`. Kernels that
- * wait on asynchronous copies or tensor-core completion give up after a bounded number of polls,
+ * wait on asynchronous copies or tensor-core completion give up after about two seconds,
  * set the flag and exit; results of that call are then invalid. Returns QLESS_OK,
  * QLESS_ERR_TIMEOUT or QLESS_ERR_CUDA. */
 qless_status qless_check(void* cuda_stream);
 
 /* Self-test of that machinery (no counterpart in the paper). Enqueues a one-block kernel in which one thread waits,
- * with the library's own bounded-wait routine and a limit of `polls` polls (256 .. 65536), on a barrier that nothing
+ * with the library's own bounded-wait routine and a limit of `polls` polls (256 .. 65536; 0: the limit that the kernels use, about two seconds), on a barrier that nothing
  * ever signals, while a second thread waits on another such barrier with a limit 256 times larger. The first gives
  * up, records the producer code (0x1) in the device timeout word and raises the block-wide abort flag; the second
  * must leave on seeing that flag without recording a code of its own; the kernel then returns normally. The next

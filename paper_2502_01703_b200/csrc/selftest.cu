@@ -24,11 +24,13 @@ selftest_timeout_kernel(uint32_t polls, unsigned int* timeout_word)
         fence_barrier_init();
     }
     __syncthreads();
-    // thread 0 plays a producer whose slot is never released: it gives up after `polls` polls
+    // thread 0 plays a producer whose slot is never released: it gives up after `polls` polls (kWaitLimit: by the clock)
     if (threadIdx.x == 0) mbar_wait(smem_u32(&bar[0]), 0u, &abort_flag, timeout_word, TO_PRODUCER, polls);
-    // thread 32 plays a consumer with a far longer limit: it must leave as soon as it sees the CTA-wide abort flag,
-    // without recording a code of its own
-    if (threadIdx.x == 32) mbar_wait(smem_u32(&bar[1]), 0u, &abort_flag, timeout_word, TO_EPILOGUE, polls * 256u);
+    // thread 32 plays a consumer with a far longer limit (by the clock: one that begins a little later): it must leave as soon as it sees
+    // the CTA-wide abort flag, without recording a code of its own
+    if (threadIdx.x == 32 && polls > 65536u)
+        for (uint32_t t = 0; t < 2000u && !*(volatile uint32_t*)&abort_flag; ++t) __nanosleep(100000u);      // 0.2 s behind, well over a poll's length
+    if (threadIdx.x == 32) mbar_wait(smem_u32(&bar[1]), 0u, &abort_flag, timeout_word, TO_EPILOGUE, polls <= 65536u ? polls * 256u : polls);
     __syncthreads();
 }
 
@@ -41,10 +43,10 @@ using namespace qless;
 extern "C" qless_status qless_selftest_timeout(int32_t polls, void* cuda_stream)
 {
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-    QLESS_REQUIRE(polls >= 256 && polls <= (1 << 16), QLESS_ERR_INVALID_ARG, "polls must be in [256, 65536] (polls=%d)", polls);
+    QLESS_REQUIRE(polls == 0 || (polls >= 256 && polls <= (1 << 16)), QLESS_ERR_INVALID_ARG, "polls must be 0 or in [256, 65536] (polls=%d)", polls);
     unsigned int* flag = timeout_flag_ptr();
     QLESS_REQUIRE(flag != nullptr, QLESS_ERR_CUDA, "cannot resolve the device timeout flag");
-    selftest_timeout_kernel<<<1, 64, 0, st>>>((uint32_t)polls, flag);
+    selftest_timeout_kernel<<<1, 64, 0, st>>>(polls == 0 ? kWaitLimit : (uint32_t)polls, flag);
     count_launches(1);
     QLESS_CUDA_TRY(cudaGetLastError());
     return QLESS_OK;

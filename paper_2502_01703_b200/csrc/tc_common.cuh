@@ -12,11 +12,28 @@ namespace tc {
 // Codes stored in the device timeout word (which wait gave up).
 enum : uint32_t { TO_PRODUCER = 1u, TO_MMA = 2u, TO_GENERATOR = 4u, TO_EPILOGUE = 8u, TO_UNPACK = 16u };
 
-constexpr uint32_t kWaitLimit = 1u << 26;   // polls of a single wait before the kernel gives up
+// A wait gives up after about two seconds. A poll takes 0.1 to 4 us (the hardware may park the thread for a while; 2 us alone on an own
+// barrier, 4 us with cluster scope), so their number alone bounds little: 2^26 polls were two to four minutes. The clock counts from the
+// 256th poll on and only together with a least number of polls, so that a context that was switched out does not give up when it comes back.
+constexpr uint32_t kWaitMs = 2000, kWaitLeastPolls = 1u << 18, kWaitLimit = 1u << 26;
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 // ---- mbarrier ----------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t wall_ms()           // in units of 2^20 ns
+{
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return (uint32_t)(t >> 20);
+}
+// Looked at every 256th poll: is the wait to end without success (another role has given up, or the time is up)?
+__device__ __forceinline__ bool wait_over(uint32_t it, uint32_t& begin, volatile uint32_t* abort_flag)
+{
+    if (*abort_flag) return true;
+    if (it == 255u) begin = wall_ms();
+    if (it < kWaitLeastPolls || wall_ms() - begin < kWaitMs) return false;
+    return true;
+}
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
 {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -63,10 +80,12 @@ __device__ __forceinline__ bool mbar_try_wait_parked(uint32_t bar, uint32_t pari
 __device__ __forceinline__ bool mbar_wait_parked(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag,
                                                  unsigned int* timeout_word, uint32_t code, uint32_t hint_ns = 2000u)
 {
+    uint32_t begin = 0u;
     for (uint32_t it = 0; it < (1u << 22); ++it) {
         if (mbar_try_wait_parked(bar, parity, hint_ns)) return true;
-        if ((it & 15u) == 15u && *abort_flag) return false;
+        if ((it & 15u) == 15u && wait_over(it, begin, abort_flag)) break;
     }
+    if (*abort_flag) return false;
     *abort_flag = 1u;
     atomicOr(timeout_word, code);
     return false;
@@ -90,10 +109,12 @@ __device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity)
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag,
                                           unsigned int* timeout_word, uint32_t code, uint32_t limit = kWaitLimit)
 {
+    uint32_t begin = 0u;
     for (uint32_t it = 0; it < limit; ++it) {
         if (mbar_try_wait(bar, parity)) return true;
-        if ((it & 255u) == 255u && *abort_flag) return false;
+        if ((it & 255u) == 255u && wait_over(it, begin, abort_flag)) break;
     }
+    if (*abort_flag) return false;
     *abort_flag = 1u;
     atomicOr(timeout_word, code);
     return false;
@@ -180,11 +201,13 @@ __device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t par
 __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag,
                                                   unsigned int* timeout_word, uint32_t code, uint32_t backoff_ns = 0)
 {
+    uint32_t begin = 0u;
     for (uint32_t it = 0; it < kWaitLimit; ++it) {
         if (mbar_try_wait_cluster(bar, parity)) return true;
         if (backoff_ns) __nanosleep(backoff_ns);
-        if ((it & 255u) == 255u && *abort_flag) return false;
+        if ((it & 255u) == 255u && wait_over(it, begin, abort_flag)) break;
     }
+    if (*abort_flag) return false;
     *abort_flag = 1u;
     atomicOr(timeout_word, code);
     return false;
