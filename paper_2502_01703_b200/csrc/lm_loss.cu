@@ -792,6 +792,7 @@ LossPlan plan_loss(int64_t T, int32_t width, int32_t vocab, bool want_h, bool wa
     if (piece_tiles < 1) piece_tiles = 1;
     if (piece_tiles > tiles_v) piece_tiles = tiles_v;
     pl.piece = (int32_t)(piece_tiles * 256);
+    pl.pieces = (int32_t)((tiles_v + piece_tiles - 1) / piece_tiles);
     pl.few = T <= FEW;
     pl.entries = (int32_t)((pl.few ? 8 : 2) * tiles_v);         // partial statistics: one per warp of 32 rows of W, or per 128 columns
     // Slices where there is one row tile: as many as fill the pairs, in at most 64 MiB of sums.
@@ -887,7 +888,8 @@ qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, uns
         return QLESS_OK;
     };
     auto pieces = [&](bool keep_sums, const int32_t* gate) {
-        for (int32_t v0 = 0; v0 < a.vocab; v0 += pl.piece) {
+        for (int32_t k = 0; k < pl.pieces; ++k) {
+            const int32_t v0 = k * pl.piece;                     // (below the vocabulary; the next one's start may pass 2^31)
             const int32_t cols = a.vocab - v0 < pl.piece ? a.vocab - v0 : pl.piece;
             GemmParams p = base;
             p.gate = gate; p.cols = cols; p.col0 = v0; p.k = a.width; p.out = piece; p.ld_out = pl.piece; p.tile0 = v0 / 256;

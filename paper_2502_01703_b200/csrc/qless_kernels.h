@@ -119,7 +119,7 @@ struct LossPlan {
     int64_t tpad;
     bool exact;                             // the softmax normaliser is known before the probabilities are formed
     bool few;                               // roles of tokens and vocabulary swapped
-    int32_t piece, entries, cap_tiles;
+    int32_t piece, pieces, entries, cap_tiles;      // vocabulary columns of a piece, and how many pieces there are
     size_t meta_off, order_off, place_off, label_off, weight_off, logit_off, coef_off, rowp_off, stat_off, hidden_off, piece_off, acc_off, total;
 };
 LossPlan plan_loss(int64_t T, int32_t width, int32_t vocab, bool want_h, bool want_w);
