@@ -6,8 +6,9 @@
 //   row e of the gradient matrix = [dA_e row-major | dB_e row-major].
 //
 // Both steps read x^ and dY once and do 2 r multiply-adds per element read: memory-bound work on the tensor cores. Measured, 128 examples of 65 536
-// tokens in all, 4096 -> 4096, rank 64, bf16 gradients: (1) 157 us, 5.1 TB/s of codes and dY; (2) 201 us, 4.0 TB/s and 134 MB of rows. (2) waits for its
-// copies most of the time (converters 60 %), the products' issue takes 55 % of its clocks and a block of codes 1300 of the 5600 that a stage lives.
+// tokens in all, 4096 -> 4096, rank 64, bf16 gradients, in a short burst: (1) 157 us, 5.1 TB/s of codes and dY; (2) 207 us, 4.0 TB/s and 134 MB of rows
+// (both together 365 us; 428 us at the clocks that a minute of such work leaves). (2) waits for its copies most of the time (converters 60 %), the
+// products' issue takes 55 % of its clocks and a block of codes 1300 of the 5600 that a stage lives.
 // (1) lora_factors_kernel: M = 128 tokens, K = channels. The codes go TMA -> shared memory -> registers -> tensor memory as bf16
 //     (exact: a code has 8 significant bits and the step is a power of two), from where the MMA takes its A operand; dY goes TMA ->
 //     MMA as stored. fp32 sums over a slice of the channels; lora_split_kernel adds the slices.
