@@ -428,6 +428,92 @@ qless_status qless_lm_loss(const void* hidden, int64_t ld_hidden, const void* we
                            void* grad_hidden, int64_t ld_grad_hidden, void* grad_weight, int64_t ld_grad_weight,
                            void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* ------------------------------------------------------------------------------------------
+ * The way of a loss's gradient through a decoder layer: normalisation, attention, feed-forward block, forward and backward.
+ * What they give at a projection's output is the grad_out of qless_lora_gradients, so that gradient rows reach every adapted
+ * layer and not the last alone. Matrices are row-major with a row stride in elements (ld_...); outputs do not overlap
+ * inputs. All calls enqueue kernels on `cuda_stream` alone and read no host memory once they have returned; the same inputs
+ * give the same bits (no float atomics).
+ *
+ * Layer normalisation of the rows of x [tokens, width] (dtype: QLESS_F32 or QLESS_BF16, of x, out, grad_out and grad_x):
+ *   mean_t = sum_c x_tc / width (center = 0: 0);  rstd_t = 1 / sqrt(sum_c (x_tc - mean_t)^2 / width + eps)
+ *   out = (x - mean) rstd weight + bias
+ * weight [width], bias [width] or NULL, of param_dtype; mean, rstd [tokens] fp32 (outputs, either may be NULL). center = 0 is the normalisation
+ * by the root mean square. Statistics are fp32, from the values and not from their squares' sum; out is rounded once.
+ * qless_layer_norm_backward takes mean (center = 0: not read, may be NULL) and rstd as the forward call left them:
+ *   g = grad_out weight;  xh = (x - mean) rstd;  grad_x = rstd (g - [center] mean_c(g) - xh mean_c(g xh))
+ *   grad_weight = sum_t grad_out xh,  grad_bias = sum_t grad_out     [width] of param_dtype, NULL to skip
+ * Sums over tokens are fp32 in a fixed order. With tokens = 0 the parameters' gradients are zeros.
+ * Requirements: tokens < 2^31; 1 <= width <= 16384; eps >= 0. Rows need no alignment beyond their element type's; 16-byte aligned rows and
+ * parameters (width a multiple of 16 bytes) are read in vectors. Workspace: device, 256-byte aligned (backward; none is
+ * needed without grad_weight and grad_bias). */
+size_t qless_layer_norm_backward_workspace(int64_t tokens, int32_t width, int32_t want_params);
+
+qless_status qless_layer_norm(const void* x, qless_dtype dtype, int64_t tokens, int32_t width, int64_t ld_x, const void* weight, const void* bias,
+                              qless_dtype param_dtype, float eps, int32_t center, void* out, int64_t ld_out, float* mean, float* rstd,
+                              void* cuda_stream);
+
+qless_status qless_layer_norm_backward(const void* grad_out, int64_t ld_grad_out, const void* x, qless_dtype dtype, int64_t tokens, int32_t width,
+                                       int64_t ld_x, const void* weight, qless_dtype param_dtype, int32_t center, const float* mean,
+                                       const float* rstd, void* grad_x, int64_t ld_grad_x, void* grad_weight, void* grad_bias,
+                                       void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Causal attention over packed examples with grouped heads. q [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim] bf16: head h of
+ * token t lies at t * ld + h * head_dim (so slices of one matrix [tokens, (heads + 2 kv_heads) head_dim] serve); query head h reads key head
+ * h / (heads / kv_heads). offsets: HOST array [n + 1] as in qless_lora_gradients: a token attends to the tokens of its example up to itself.
+ *   s_ij = scale <q_i, k_j>,  p_ij = exp(s_ij) / sum_{j' <= i} exp(s_ij'),  out_i = sum_j p_ij v_j,  lse_i = log sum_j exp(s_ij)
+ * out [tokens, heads, head_dim] bf16 (ld_out), lse [tokens, heads] fp32 (contiguous; NULL: not wanted). Rows outside the examples are left as
+ * they were. Scores, exponentials, sums and out's accumulators are fp32; probabilities enter the second product rounded to bf16.
+ * An infinity or NaN in one example's rows reaches that example's rows only (within it, also rows before it that share its tile of 128 keys).
+ * qless_attention_backward: grad_out, out, lse as above (lse not NULL) ->
+ *   delta_i = <grad_out_i, out_i>;  ds_ij = p_ij (<grad_out_i, v_j> - delta_i);  grad_q_i = scale sum_j ds_ij k_j;
+ *   grad_k_j = scale sum_i ds_ij q_i,  grad_v_j = sum_i p_ij grad_out_i   (sums over i and the query heads of the group)
+ * with p and ds rounded to bf16 in these products, fp32 sums, and one rounding of each result to bf16.
+ * Requirements: tokens < 2^31; head_dim a multiple of 8, at most 128; heads a multiple of kv_heads, heads <= 4096; scale finite and positive; tensors
+ * 16-byte aligned, their row strides multiples of 8. Workspace: device, 256-byte aligned. */
+size_t qless_attention_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads);
+size_t qless_attention_backward_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads);
+
+qless_status qless_attention(const void* q, int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                             const int64_t* offsets /* host */, int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                             float scale, void* out, int64_t ld_out, float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+qless_status qless_attention_backward(const void* grad_out, int64_t ld_grad_out, const void* q, int64_t ld_q, const void* k, int64_t ld_k,
+                                      const void* v, int64_t ld_v, const void* out, int64_t ld_out, const float* lse,
+                                      const int64_t* offsets /* host */, int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads,
+                                      int32_t head_dim, float scale, void* grad_q, int64_t ld_grad_q, void* grad_k, int64_t ld_grad_k,
+                                      void* grad_v, int64_t ld_grad_v, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Gated feed-forward block. x [tokens, width], w_gate and w_up [inner, width], w_down [width, inner], all bf16:
+ *   gate = x w_gate^T;  up = x w_up^T;  hidden = act(gate) up;  out = hidden w_down^T
+ * act: QLESS_SILU g / (1 + e^-g), or QLESS_GELU g F(g) with the normal distribution F. out [tokens, width], hidden [tokens, inner] (the input of
+ * the down projection: always written), gate and up [tokens, inner] (both or neither NULL: kept for the backward pass), bf16.
+ * hidden is formed from the fp32 gate and up.
+ * qless_gated_ffn_backward, from gate and up as the forward call left them:
+ *   dh = grad_out w_down;  grad_gate = dh up act'(gate);  grad_up = dh act(gate);  grad_x = grad_gate w_gate + grad_up w_up
+ *   grad_w_gate = grad_gate^T x,  grad_w_up = grad_up^T x,  grad_w_down = grad_out^T hidden
+ * grad_gate and grad_up [tokens, inner] are always written (they are the gradients at the two projections' outputs); grad_x and each weight's
+ * gradient may be NULL. Products of bf16 operands with fp32 sums; hidden, grad_gate and grad_up are rounded to bf16 before the next product.
+ * x is read for grad_w_gate and grad_w_up alone (else it may be NULL). With tokens = 0 the weights' gradients are zeros.
+ * Requirements: tokens < 2^31 - 256; width and inner multiples of 8, at most 2^20; matrices 16-byte aligned, their row strides multiples of 8.
+ * Workspace: device, 256-byte aligned; want_weights: any weight's gradient. */
+typedef enum { QLESS_SILU = 0, QLESS_GELU = 1 } qless_activation;
+
+size_t qless_gated_ffn_workspace(int64_t tokens, int32_t width, int32_t inner);
+size_t qless_gated_ffn_backward_workspace(int64_t tokens, int32_t width, int32_t inner, int32_t want_weights);
+
+qless_status qless_gated_ffn(const void* x, int64_t ld_x, const void* w_gate, int64_t ld_w_gate, const void* w_up, int64_t ld_w_up,
+                             const void* w_down, int64_t ld_w_down, int64_t tokens, int32_t width, int32_t inner, qless_activation act,
+                             void* out, int64_t ld_out, void* hidden, int64_t ld_hidden, void* gate, int64_t ld_gate, void* up, int64_t ld_up,
+                             void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+qless_status qless_gated_ffn_backward(const void* grad_out, int64_t ld_grad_out, const void* x, int64_t ld_x, const void* gate, int64_t ld_gate,
+                                      const void* up, int64_t ld_up, const void* w_gate, int64_t ld_w_gate, const void* w_up, int64_t ld_w_up,
+                                      const void* w_down, int64_t ld_w_down, int64_t tokens, int32_t width, int32_t inner, qless_activation act,
+                                      void* grad_x, int64_t ld_grad_x, void* grad_gate, int64_t ld_grad_gate, void* grad_up, int64_t ld_grad_up,
+                                      void* grad_w_gate, int64_t ld_grad_w_gate, void* grad_w_up, int64_t ld_grad_w_up,
+                                      void* grad_w_down, int64_t ld_grad_w_down, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -32,7 +32,11 @@ EXPORTS = [
     "qless_project_quantize_ex", "qless_project_quantize_host_ex", "qless_gaussian_entries", "qless_selftest_timeout",
     "qless_activation_quantize", "qless_activation_dequantize", "qless_lora_gradients_workspace", "qless_lora_gradients",
     "qless_lm_loss_workspace", "qless_lm_loss",
+    "qless_layer_norm_backward_workspace", "qless_layer_norm", "qless_layer_norm_backward",
+    "qless_attention_workspace", "qless_attention_backward_workspace", "qless_attention", "qless_attention_backward",
+    "qless_gated_ffn_workspace", "qless_gated_ffn_backward_workspace", "qless_gated_ffn", "qless_gated_ffn_backward",
 ]
+SILU, GELU = 0, 1
 RADEMACHER, GAUSSIAN = 0, 1
 SELECT_STATIC_MAX_N = 1 << 22
 
@@ -144,6 +148,21 @@ def lib():
         L.qless_lm_loss_workspace.argtypes = [i64, i32, i32, i32, i32]
         L.qless_lm_loss.restype = C.c_int
         L.qless_lm_loss.argtypes = [vp, i64, vp, i64, vp, vp, i64, i32, i32, vp, vp, i64, vp, i64, vp, sz, vp]
+        fp = C.c_float
+        for name, result, args in (
+                ("qless_layer_norm_backward_workspace", sz, [i64, i32, i32]),
+                ("qless_layer_norm", C.c_int, [vp, C.c_int, i64, i32, i64, vp, vp, C.c_int, fp, i32, vp, i64, vp, vp, vp]),
+                ("qless_layer_norm_backward", C.c_int, [vp, i64, vp, C.c_int, i64, i32, i64, vp, C.c_int, i32, vp, vp, vp, i64, vp, vp, vp, sz, vp]),
+                ("qless_attention_workspace", sz, [i64, i64, i32, i32]),
+                ("qless_attention_backward_workspace", sz, [i64, i64, i32, i32]),
+                ("qless_attention", C.c_int, [vp, i64] * 3 + [vp, i64, i64, i32, i32, i32, fp, vp, i64, vp, vp, sz, vp]),
+                ("qless_attention_backward", C.c_int, [vp, i64] * 5 + [vp, vp, i64, i64, i32, i32, i32, fp] + [vp, i64] * 3 + [vp, sz, vp]),
+                ("qless_gated_ffn_workspace", sz, [i64, i32, i32]),
+                ("qless_gated_ffn_backward_workspace", sz, [i64, i32, i32, i32]),
+                ("qless_gated_ffn", C.c_int, [vp, i64] * 4 + [i64, i32, i32, C.c_int] + [vp, i64] * 4 + [vp, sz, vp]),
+                ("qless_gated_ffn_backward", C.c_int, [vp, i64] * 7 + [i64, i32, i32, C.c_int] + [vp, i64] * 6 + [vp, sz, vp])):
+            fn = getattr(L, name)
+            fn.restype, fn.argtypes = result, args
         _lib = L
     return _lib
 
@@ -641,6 +660,262 @@ def qless_lm_loss(hidden, weight, labels, token_weight=None, want_hidden=True, w
                                T, width, vocab, _ptr(loss), _ptr(gh), _row_stride(gh) if gh is not None else 0,
                                _ptr(gw), _row_stride(gw) if gw is not None else 0, _ptr(ws), ws.numel(), _stream(stream, at)))
     return dict(loss=loss, grad_hidden=gh, grad_weight=gw)
+
+
+def _param(p, width, name):
+    if p is not None and (p.shape != (width,) or not p.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous, [width]")
+    return p
+
+
+def qless_layer_norm(x, weight, bias=None, eps=1e-5, center=True, out=None, stream=None):
+    """Layer normalisation of the rows of x f32/bf16 [tokens, width] (row stride allowed); weight, bias [width] f32 or bf16; center=False: by
+    the root mean square. Returns dict(out [tokens, width] of x's type, mean f32 [tokens] | None without centring, rstd f32 [tokens])."""
+    T, width = x.shape
+    _param(weight, width, "weight")
+    _param(bias, width, "bias")
+    if bias is not None and bias.dtype != weight.dtype:
+        raise TypeError("weight and bias must have one type")
+    at = _on_gpu(stream, x, weight, bias, out)
+    if out is None:
+        out = _empty(T, width, x.dtype, x.device, stream)
+    elif out.shape != (T, width) or out.dtype != x.dtype:
+        raise ValueError("out must be [tokens, width] of x's type")
+    stats = _empty(2 if center else 1, T, torch.float32, x.device, stream)
+    mean, rstd = (stats[0], stats[1]) if center else (None, stats[0])
+    if stream is not None:
+        _used(stream, x, weight, bias, out)
+    _check(lib().qless_layer_norm(x.data_ptr(), _dtype_code(x), T, width, _row_stride(x), weight.data_ptr(), _ptr(bias), _dtype_code(weight), eps,
+                                  1 if center else 0, out.data_ptr(), _row_stride(out), _ptr(mean), rstd.data_ptr(), _stream(stream, at)))
+    return dict(out=out, mean=mean, rstd=rstd)
+
+
+def qless_layer_norm_backward_workspace(tokens, width, want_params=True):
+    return int(lib().qless_layer_norm_backward_workspace(tokens, width, 1 if want_params else 0))
+
+
+def qless_layer_norm_backward(grad_out, x, weight, mean, rstd, want_weight=False, want_bias=False, grad_x=None, workspace=None, stream=None):
+    """Gradients of qless_layer_norm from the mean (None: without centring) and rstd that it returned. Returns dict(grad_x [tokens, width] of
+    x's type, grad_weight | None, grad_bias | None: [width] of weight's type)."""
+    T, width = x.shape
+    _param(weight, width, "weight")
+    if grad_out.shape != (T, width) or grad_out.dtype != x.dtype:
+        raise ValueError("grad_out must be [tokens, width] of x's type")
+    for s in (mean, rstd):
+        if s is not None and (s.shape != (T,) or s.dtype != torch.float32 or not s.is_contiguous()):
+            raise ValueError("mean and rstd must be contiguous float32, [tokens]")
+    at = _on_gpu(stream, x, grad_out, weight, mean, rstd, grad_x, workspace)
+    if grad_x is None:
+        grad_x = _empty(T, width, x.dtype, x.device, stream)
+    elif grad_x.shape != (T, width) or grad_x.dtype != x.dtype:
+        raise ValueError("grad_x must be [tokens, width] of x's type")
+    gw = _new(width, weight.dtype, x.device, stream) if want_weight else None
+    gb = _new(width, weight.dtype, x.device, stream) if want_bias else None
+    ws = None
+    if want_weight or want_bias:
+        ws = _workspace(qless_layer_norm_backward_workspace(T, width), x.device, workspace, stream)
+    if stream is not None:
+        _used(stream, x, grad_out, weight, mean, rstd, grad_x, workspace)
+    _check(lib().qless_layer_norm_backward(grad_out.data_ptr(), _row_stride(grad_out), x.data_ptr(), _dtype_code(x), T, width, _row_stride(x),
+                                           weight.data_ptr(), _dtype_code(weight), 0 if mean is None else 1, _ptr(mean), rstd.data_ptr(),
+                                           grad_x.data_ptr(), _row_stride(grad_x), _ptr(gw), _ptr(gb), _ptr(ws), ws.numel() if ws is not None else 0,
+                                           _stream(stream, at)))
+    return dict(grad_x=grad_x, grad_weight=gw, grad_bias=gb)
+
+
+def _host_offsets(offsets):
+    off = offsets if torch.is_tensor(offsets) else torch.tensor(list(offsets), dtype=torch.int64)
+    if off.device.type != "cpu" or off.dtype != torch.int64 or not off.is_contiguous() or off.dim() != 1 or off.numel() < 1:
+        raise TypeError("offsets must be a contiguous int64 tensor in host memory, [n + 1]")
+    return off
+
+
+def _token_stride(t, name):
+    """Elements between tokens of a bf16 [tokens, heads, head_dim] tensor whose heads lie side by side."""
+    if t.dtype != torch.bfloat16 or t.dim() != 3:
+        raise TypeError(f"{name} must be bfloat16, [tokens, heads, head_dim]")
+    (T, h, d), (st, sh, sd) = t.shape, t.stride()
+    if (sd != 1 and d > 1) or (sh != d and h > 1):
+        raise ValueError(f"the heads of a token of {name} must lie side by side")
+    return st if T > 1 else h * d
+
+
+def _rows_like(shape, off, T, device, stream):
+    """A new bf16 output [tokens, heads, head_dim]; zeros where the examples leave tokens out, whose rows no kernel writes."""
+    t = _empty(T, shape[1] * shape[2], torch.bfloat16, device, stream)
+    _zero_outside(t, off, T, stream)
+    return t.view(shape)
+
+
+def _zero_outside(t, off, T, stream):
+    lo, hi = int(off[0]), int(off[-1])
+    if lo == 0 and hi == T:
+        return
+    if _elsewhere(stream):
+        with torch.cuda.stream(stream):
+            t.zero_()
+    else:
+        t.zero_()
+
+
+def qless_attention_workspace(tokens, n, heads, kv_heads):
+    return int(lib().qless_attention_workspace(tokens, n, heads, kv_heads))
+
+
+def qless_attention_backward_workspace(tokens, n, heads, kv_heads):
+    return int(lib().qless_attention_backward_workspace(tokens, n, heads, kv_heads))
+
+
+def _heads_of(q, k, v):
+    T, heads, d = q.shape
+    if k.shape != v.shape or k.dim() != 3 or k.shape[0] != T or k.shape[2] != d:
+        raise ValueError("shapes of q, k and v do not fit together")
+    return T, heads, k.shape[1], d
+
+
+def qless_attention(q, k, v, offsets, scale=None, out=None, workspace=None, stream=None):
+    """Causal attention over packed examples with grouped heads: q bf16 [tokens, heads, head_dim], k, v bf16 [tokens, kv_heads, head_dim] (a
+    stride between tokens is allowed); offsets: int64 CPU tensor (or sequence) [n + 1] of the examples' first tokens; scale: head_dim ** -0.5
+    by default. Returns dict(out bf16 [tokens, heads, head_dim], lse f32 [tokens, heads]). Rows outside the examples are left as they are
+    in a given `out` and are zeros in a new one."""
+    off = _host_offsets(offsets)
+    sq, sk, sv = _token_stride(q, "q"), _token_stride(k, "k"), _token_stride(v, "v")
+    T, heads, kv, d = _heads_of(q, k, v)
+    n = off.numel() - 1
+    at = _on_gpu(stream, q, k, v, out, workspace)
+    if out is None:
+        out = _rows_like(q.shape, off, T, q.device, stream)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    lse = _empty(T, heads, torch.float32, q.device, stream)
+    _zero_outside(lse, off, T, stream)
+    ws = _workspace(qless_attention_workspace(T, n, heads, kv), q.device, workspace, stream)
+    if stream is not None:
+        _used(stream, q, k, v, out, workspace)
+    _check(lib().qless_attention(q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv, off.data_ptr(), T, n, heads, kv, d,
+                                 d ** -0.5 if scale is None else scale, out.data_ptr(), _token_stride(out, "out"), lse.data_ptr(), ws.data_ptr(), ws.numel(),
+                                 _stream(stream, at)))
+    return dict(out=out, lse=lse)
+
+
+def qless_attention_backward(grad_out, q, k, v, out, lse, offsets, scale=None, grads=None, workspace=None, stream=None):
+    """Gradients of qless_attention from the out and lse that it returned. Returns dict(grad_q, grad_k, grad_v), bf16, of the shapes of q, k
+    and v. `grads` may pass preallocated tensors by those names (slices of one matrix, say); rows outside the examples are left as they are in
+    those and are zeros in new ones."""
+    off = _host_offsets(offsets)
+    T, heads, kv, d = _heads_of(q, k, v)
+    if grad_out.shape != q.shape or out.shape != q.shape:
+        raise ValueError("grad_out and out must have q's shape")
+    if lse.shape != (T, heads) or lse.dtype != torch.float32 or not lse.is_contiguous():
+        raise ValueError("lse must be contiguous float32, [tokens, heads]")
+    n = off.numel() - 1
+    grads = grads or {}
+    at = _on_gpu(stream, q, k, v, grad_out, out, lse, workspace, *grads.values())
+    got = {}
+    for name, like in (("grad_q", q), ("grad_k", k), ("grad_v", v)):
+        t = grads.get(name)
+        if t is None:
+            t = _rows_like(like.shape, off, T, q.device, stream)
+        elif t.shape != like.shape:
+            raise ValueError(f"{name} has the wrong shape")
+        got[name] = t
+    ws = _workspace(qless_attention_backward_workspace(T, n, heads, kv), q.device, workspace, stream)
+    if stream is not None:
+        _used(stream, q, k, v, grad_out, out, lse, workspace, *got.values())
+    args = []
+    for t, name in ((grad_out, "grad_out"), (q, "q"), (k, "k"), (v, "v"), (out, "out")):
+        args += [t.data_ptr(), _token_stride(t, name)]
+    args += [lse.data_ptr(), off.data_ptr(), T, n, heads, kv, d, d ** -0.5 if scale is None else scale]
+    for name, t in got.items():
+        args += [t.data_ptr(), _token_stride(t, name)]
+    _check(lib().qless_attention_backward(*args, ws.data_ptr(), ws.numel(), _stream(stream, at)))
+    return got
+
+
+def _activation_code(activation):
+    if activation not in ("silu", "gelu"):
+        raise ValueError("activation must be 'silu' or 'gelu'")
+    return SILU if activation == "silu" else GELU
+
+
+def _ffn_shapes(x, w_gate, w_up, w_down):
+    inner, width = w_gate.shape
+    if x.dim() != 2 or x.shape[1] != width or w_up.shape != (inner, width) or w_down.shape != (width, inner):
+        raise ValueError("shapes of the tokens, w_gate, w_up and w_down do not fit together")
+    return x.shape[0], width, inner
+
+
+def _bf16_args(*tensors):
+    """Pointer and row stride of each bf16 matrix (None: absent)."""
+    args = []
+    for t in tensors:
+        if t is None:
+            args += [None, 0]
+            continue
+        if t.dtype != torch.bfloat16:
+            raise TypeError("matrices must be bfloat16")
+        args += [t.data_ptr(), _row_stride(t)]
+    return args
+
+
+def _outputs(given, wanted, device, stream):
+    """name -> [rows, cols] bf16: the caller's tensor of that name or a new one (None where it is neither given nor wanted)."""
+    given = given or {}
+    got = {}
+    for name, (want, rows, cols) in wanted.items():
+        t = given.get(name)
+        if t is None:
+            t = _empty(rows, cols, torch.bfloat16, device, stream) if want else None
+        elif t.shape != (rows, cols) or t.dtype != torch.bfloat16:
+            raise ValueError(f"{name} has the wrong shape or type")
+        got[name] = t
+    return got
+
+
+def qless_gated_ffn_workspace(tokens, width, inner):
+    return int(lib().qless_gated_ffn_workspace(tokens, width, inner))
+
+
+def qless_gated_ffn_backward_workspace(tokens, width, inner, want_weight=False):
+    return int(lib().qless_gated_ffn_backward_workspace(tokens, width, inner, 1 if want_weight else 0))
+
+
+def qless_gated_ffn(x, w_gate, w_up, w_down, activation="silu", want_saved=False, out=None, workspace=None, stream=None):
+    """Gated feed-forward block out = (act(x w_gate^T) * (x w_up^T)) w_down^T: x bf16 [tokens, width], w_gate, w_up bf16 [inner, width], w_down
+    bf16 [width, inner]; activation 'silu' or 'gelu'. Returns dict(out [tokens, width], hidden [tokens, inner]: the down projection's
+    input, gate, up [tokens, inner] | None: kept for the backward pass where want_saved). `out` may pass preallocated tensors by those names."""
+    T, width, inner = _ffn_shapes(x, w_gate, w_up, w_down)
+    code = _activation_code(activation)
+    keep = want_saved or bool(out and (out.get("gate") is not None or out.get("up") is not None))
+    at = _on_gpu(stream, x, w_gate, w_up, w_down, workspace, *(out or {}).values())
+    got = _outputs(out, dict(out=(True, T, width), hidden=(True, T, inner), gate=(keep, T, inner), up=(keep, T, inner)), x.device, stream)
+    ws = _workspace(qless_gated_ffn_workspace(T, width, inner), x.device, workspace, stream)
+    if stream is not None:
+        _used(stream, x, w_gate, w_up, w_down, workspace, *got.values())
+    _check(lib().qless_gated_ffn(*_bf16_args(x, w_gate, w_up, w_down), T, width, inner, code, *_bf16_args(*got.values()), ws.data_ptr(), ws.numel(),
+                                 _stream(stream, at)))
+    return got
+
+
+def qless_gated_ffn_backward(grad_out, x, gate, up, w_gate, w_up, w_down, activation="silu", want_x=True, want_weight=False, grads=None,
+                             workspace=None, stream=None):
+    """Gradients of qless_gated_ffn from the gate and up that it kept. Returns dict(grad_x [tokens, width] | None, grad_gate, grad_up [tokens, inner]: at
+    the two projections' outputs, grad_w_gate, grad_w_up, grad_w_down | None: where want_weight). `grads` may pass preallocated
+    tensors by those names. x may be None where no weight's gradient is wanted."""
+    T, width, inner = _ffn_shapes(grad_out, w_gate, w_up, w_down)
+    code = _activation_code(activation)
+    if gate.shape != (T, inner) or up.shape != (T, inner) or (x is not None and x.shape != (T, width)):
+        raise ValueError("x must be [tokens, width], gate and up [tokens, inner]")
+    at = _on_gpu(stream, grad_out, x, gate, up, w_gate, w_up, w_down, workspace, *(grads or {}).values())
+    got = _outputs(grads, dict(grad_x=(want_x, T, width), grad_gate=(True, T, inner), grad_up=(True, T, inner), grad_w_gate=(want_weight, inner, width),
+                               grad_w_up=(want_weight, inner, width), grad_w_down=(want_weight, width, inner)), grad_out.device, stream)
+    weights = any(got[name] is not None for name in ("grad_w_gate", "grad_w_up", "grad_w_down"))
+    ws = _workspace(qless_gated_ffn_backward_workspace(T, width, inner, weights), grad_out.device, workspace, stream)
+    if stream is not None:
+        _used(stream, grad_out, x, gate, up, w_gate, w_up, w_down, workspace, *got.values())
+    _check(lib().qless_gated_ffn_backward(*_bf16_args(grad_out, x, gate, up, w_gate, w_up, w_down), T, width, inner, code, *_bf16_args(*got.values()),
+                                          ws.data_ptr(), ws.numel(), _stream(stream, at)))
+    return got
 
 
 def qless_set_projection_path(path):

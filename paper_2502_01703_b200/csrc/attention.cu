@@ -1,0 +1,445 @@
+// Causal attention over packed sequences with grouped heads: the forward kernel, and the tables of work.
+//
+//   s_ij = scale <q_i, k_j> for j <= i in the same sequence,  m_i = max_j s_ij,  o_i = sum_j e^(s_ij - m_i) v_j / sum_j e^(s_ij - m_i),
+//   lse_i = m_i + log sum_j e^(s_ij - m_i)
+//
+// One pass over the keys per tile of queries; scores never leave the SM. A block works on two tiles of 128 query rows that share the copies of
+// keys and values: while one tile's group of four warps takes exponentials, the tensor core works on the other's products.
+//   warp 0        TMA: queries of a tile once, keys and values through a ring of tiles
+//   warp 1        tcgen05: S = Q K^T (both from shared memory), O += P V (P from tensor memory, V as rows of tokens)
+//   warps 4-7     tile 0: a thread owns a row: maximum, exponentials in fp32, P rounded to bf16 over S in tensor memory
+//   warps 8-11    tile 1
+// Tensor memory: S (or P) and O of both tiles, 4 x 128 columns. Running maximum: O and the sum are rescaled only when the maximum has grown by
+// more than 2^8 since the reference was taken (e^(s - r) then stays below 2^8: neither fp32 sums nor bf16's relative rounding mind).
+// P is rounded to bf16 (2^-9 of each probability, independent of each other; the sum is that of the unrounded ones), O and the sums are fp32.
+// Bound: 128 x 128 exponentials take the special-function units 1024 clocks, the two products of the same tile (head_dim 128) 1024 of the tensor core.
+#include <algorithm>
+#include <string.h>
+
+#include "attention_common.cuh"
+
+namespace qless {
+
+namespace attn {
+
+namespace {
+
+constexpr int NTHREADS = 384, MAX_STAGES = 10;
+constexpr float SLACK = 8.0f;               // powers of two that the maximum may grow before O is rescaled
+
+struct ForwardParams {
+    TileTable table;
+    __nv_bfloat16* out; float* lse;
+    int64_t ld_out;
+    int32_t packs, pack, group, heads, head_dim, stages;      // packs: tiles' heads, heads / pack
+    int64_t items;
+    float scale_log2;
+    unsigned int* timeout_word;
+};
+
+struct __align__(8) Bars {
+    uint64_t q_full[2], q_empty[2], full[MAX_STAGES], empty[MAX_STAGES], s_full[2], p_ready[2], o_full[2], drain;
+    uint32_t tmem_base, abort_flag;
+};
+
+// DB: 64-column blocks of a head (head_dim up to 64 or 128).
+template <int DB>
+__global__ void __launch_bounds__(NTHREADS, 1)
+attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                 const __grid_constant__ ForwardParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    constexpr int OP = DB * 16384;                           // bytes of a 128-row operand
+    uint8_t* q_smem = smem;
+    uint8_t* ring_smem = smem + 2 * OP;
+    const uint32_t nS = (uint32_t)p.stages;
+    Bars* bars = reinterpret_cast<Bars*>(ring_smem + (size_t)nS * OP);
+    volatile uint32_t* abort_flag = &bars->abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int tok = TILE / p.pack;                           // tokens of a 128-row tile
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&bars->q_full[i]), 1); mbar_init(smem_u32(&bars->q_empty[i]), 1);
+            mbar_init(smem_u32(&bars->s_full[i]), 1); mbar_init(smem_u32(&bars->p_ready[i]), 4); mbar_init(smem_u32(&bars->o_full[i]), 1);
+        }
+        for (uint32_t i = 0; i < MAX_STAGES; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), 1); }
+        mbar_init(smem_u32(&bars->drain), 1);
+        bars->abort_flag = 0;
+        fence_barrier_init();
+        prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
+    }
+    if (warp == 1) { tmem_alloc(smem_u32(&bars->tmem_base), 512); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem_base;                   // S (P) of tile i at 128 i, O at 256 + 128 i
+    ahead_wait();
+    ahead_release();
+
+    auto warp_wait = [&](uint64_t* bar, uint32_t parity, uint32_t code) -> bool {
+        const bool w = mbar_wait(smem_u32(bar), parity, abort_flag, p.timeout_word, code);
+        return __all_sync(0xFFFFFFFFu, w);
+    };
+    // item -> tile, first head, key head; loops of the two row tiles over the keys (0: the second one does not exist)
+    struct Work { AttnTile t; int head0, kv, n[2]; };
+    auto work_of = [&](int64_t item) {
+        Work w;
+        const int i = (int)(item / p.packs), c = (int)(item - (int64_t)i * p.packs);
+        w.t = tile_at(p.table, i);
+        w.head0 = c * p.pack; w.kv = w.head0 / p.group;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int first = w.t.at + x * tok;
+            w.n[x] = first < w.t.len && (x == 0 || w.t.unused == 0) ? (min(first + tok, w.t.len) + TILE - 1) / TILE : 0;
+        }
+        return w;
+    };
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (warp == 0) {
+            Ring ring;
+            uint32_t it = 0, q_uses[2] = {0, 0};
+            bool ok = true;
+            auto load = [&](const CUtensorMap* map, int kv, int row) {
+                if (!warp_wait(&bars->empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; return; }
+                if (elect_one()) {
+                    const uint32_t full = smem_u32(&bars->full[ring.slot]), dst = smem_u32(ring_smem + (size_t)ring.slot * OP);
+                    mbar_arrive_expect_tx(full, OP);
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) tma_load_3d(dst + b * 16384, map, full, b * 64, kv, row);
+                }
+                __syncwarp();
+                ring.next(nS); ++it;
+            };
+            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+                const Work w = work_of(item);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (w.n[x] == 0 || !ok) continue;
+                    if (!warp_wait(&bars->q_empty[x], (q_uses[x] & 1u) ^ 1u, TO_PRODUCER)) { ok = false; break; }
+                    ++q_uses[x];
+                    if (elect_one()) {
+                        const uint32_t full = smem_u32(&bars->q_full[x]), dst = smem_u32(q_smem + x * OP);
+                        mbar_arrive_expect_tx(full, OP);
+#pragma unroll
+                        for (int b = 0; b < DB; ++b) tma_load_3d(dst + b * 16384, &tm_q, full, b * 64, w.head0, w.t.t0 + w.t.at + x * tok);
+                    }
+                    __syncwarp();
+                    if (x == 0) load(&tm_k, w.kv, w.t.t0);
+                }
+                if (ok) load(&tm_v, w.kv, w.t.t0);
+                const int n = max(w.n[0], w.n[1]);
+                for (int j = 1; j < n && ok; ++j) {
+                    load(&tm_k, w.kv, w.t.t0 + j * TILE);
+                    if (ok) load(&tm_v, w.kv, w.t.t0 + j * TILE);
+                }
+            }
+            // nothing of this block's copies is in flight when it leaves (the other roles wait for all of them unless one gave up)
+            if (!ok)
+                for (uint32_t j = it > nS ? it - nS : 0u; j < it; ++j)
+                    if (!mbar_wait_quiet(smem_u32(&bars->full[j % nS]), (j / nS) & 1u, 1u << 14)) break;
+        } else if (warp == 1) {
+            const uint32_t n_pv = (uint32_t)((p.head_dim + 15) / 16 * 16), steps = n_pv / 16;      // columns of a head that are there
+            const uint32_t idesc_s = make_idesc(1, 1, 1, 128, 128), idesc_o = make_idesc(1, 1, 1, 128, n_pv) | IDESC_B_MN;
+            Ring ring;
+            uint32_t q_uses[2] = {0, 0}, p_uses[2] = {0, 0};
+            bool ok = true;
+            auto scores = [&](int x, const uint8_t* k_op) {
+                if (elect_one()) {
+                    const uint64_t a = make_smem_desc_sw128(smem_u32(q_smem + x * OP)), b = make_smem_desc_sw128(smem_u32(k_op));
+                    for (uint32_t k = 0; k < steps; ++k) {
+                        const uint64_t off = (uint64_t)((k >> 2) * 1024 + (k & 3) * 2);
+                        mma_f16_ss(tmem + x * 128, a + off, b + off, idesc_s, k > 0);
+                    }
+                    mma_commit(smem_u32(&bars->s_full[x]));
+                }
+                __syncwarp();
+            };
+            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+                const Work w = work_of(item);
+                const int n = max(w.n[0], w.n[1]);
+                if (!warp_wait(&bars->full[ring.slot], ring.parity, TO_MMA)) { ok = false; break; }
+                tc_fence_after();
+                for (int x = 0; x < 2; ++x) {
+                    if (w.n[x] == 0) continue;
+                    if (!warp_wait(&bars->q_full[x], q_uses[x]++ & 1u, TO_MMA)) { ok = false; break; }
+                    tc_fence_after();
+                    scores(x, ring_smem + (size_t)ring.slot * OP);
+                    if (w.n[x] == 1 && elect_one()) mma_commit(smem_u32(&bars->q_empty[x]));
+                    __syncwarp();
+                }
+                if (!ok) break;
+                if (elect_one()) mma_commit(smem_u32(&bars->empty[ring.slot]));
+                __syncwarp();
+                ring.next(nS);
+                for (int j = 0; j < n && ok; ++j) {
+                    const Ring v = ring;
+                    ring.next(nS);
+                    const Ring k = ring;
+                    if (j + 1 < n) ring.next(nS);
+                    uint8_t* v_op = ring_smem + (size_t)v.slot * OP;
+                    if (!warp_wait(&bars->full[v.slot], v.parity, TO_MMA)) { ok = false; break; }
+                    if (w.t.len - j * TILE < TILE) zero_rows(v_op, DB, w.t.len - j * TILE, lane);
+                    if (j + 1 < n && !warp_wait(&bars->full[k.slot], k.parity, TO_MMA)) { ok = false; break; }
+                    for (int x = 0; x < 2; ++x) {
+                        if (j >= w.n[x]) continue;
+                        if (!warp_wait(&bars->p_ready[x], p_uses[x]++ & 1u, TO_MMA)) { ok = false; break; }
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint64_t b = make_smem_desc_mn_sw128(smem_u32(v_op), 16384);
+#pragma unroll
+                            for (int s = 0; s < 8; ++s) mma_f16_ts(tmem + 256 + x * 128, tmem + x * 128 + s * 8, b + (uint64_t)(s * 128), idesc_o, j > 0 || s > 0);
+                            if (j + 1 == w.n[x]) mma_commit(smem_u32(&bars->o_full[x]));
+                        }
+                        __syncwarp();
+                        if (j + 1 < w.n[x]) {
+                            scores(x, ring_smem + (size_t)k.slot * OP);
+                            if (j + 2 == w.n[x] && elect_one()) mma_commit(smem_u32(&bars->q_empty[x]));
+                            __syncwarp();
+                        }
+                    }
+                    if (!ok) break;
+                    if (elect_one()) {
+                        mma_commit(smem_u32(&bars->empty[v.slot]));
+                        if (j + 1 < n) mma_commit(smem_u32(&bars->empty[k.slot]));
+                    }
+                    __syncwarp();
+                }
+            }
+            if (elect_one()) mma_commit(smem_u32(&bars->drain));
+            __syncwarp();
+            mbar_wait_quiet(smem_u32(&bars->drain), 0u);
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        const int x = warp >= 8 ? 1 : 0, r = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_addr = tmem + lanes + x * 128, o_addr = tmem + lanes + 256 + x * 128;
+        const int my_tok = r / p.pack, my_head = r % p.pack;
+        uint32_t s_uses = 0, o_uses = 0;
+        bool ok = true;
+        for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            const Work w = work_of(item);
+            const int n = w.n[x];
+            if (n == 0) continue;
+            const int first = w.t.at + x * tok, at = first + my_tok;      // this row's token within its sequence
+            float ref = -INFINITY, sum = 0.0f;               // reference of the exponents (times scale, in powers of two)
+            for (int j = 0; j < n; ++j) {
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->s_full[x]), s_uses++ & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t s[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld_x32(s_addr + c * 32, s[c]);
+                tmem_wait_ld();
+                if (j * TILE + TILE - 1 > first) {           // keys behind the tile's first token: some row does not see all of them
+                    const int lim = at - j * TILE;           // its last key here
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) if (c * 32 + k > lim) s[c][k] = 0xFF800000u;
+                }
+                float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) top4[c] = fmaxf(top4[c], __uint_as_float(s[c][k]));
+                const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * p.scale_log2;
+                float by = 1.0f;
+                if (top > ref + SLACK || ref == -INFINITY) {
+                    if (top > -INFINITY) {
+                        by = ref == -INFINITY ? 0.0f : ex2(ref - top);
+                        ref = top;
+                    }
+                }
+                if (j > 0 && __any_sync(0xFFFFFFFFu, by != 1.0f)) {      // the products so far are complete: S was issued behind them
+#pragma unroll 1
+                    for (int c = 0; c < DB * 64; c += 32) {
+                        uint32_t o[32];
+                        tmem_ld_x32(o_addr + c, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(by == 0.0f ? 0.0f : __uint_as_float(o[k]) * by);
+                        tmem_st_x32(o_addr + c, o);
+                    }
+                    sum *= by;
+                }
+                const float off = ref > -INFINITY ? ref : 0.0f;
+                float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t e[16];
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const float a = ex2(fmaf(__uint_as_float(s[c][2 * k]), p.scale_log2, -off)), b = ex2(fmaf(__uint_as_float(s[c][2 * k + 1]), p.scale_log2, -off));
+                        part[(2 * k) & 3] += a; part[(2 * k + 1) & 3] += b;
+                        e[k] = pack_bf16(a, b);
+                    }
+                    tmem_st_x16(s_addr + c * 16, e);
+                }
+                sum += (part[0] + part[1]) + (part[2] + part[3]);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars->p_ready[x]));
+            }
+            if (!ok) break;
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->o_full[x]), o_uses++ & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
+            if (!ok) break;
+            tc_fence_after();
+            const float inv = 1.0f / sum;
+            if (p.lse != nullptr && at < w.t.len) p.lse[(int64_t)(w.t.t0 + at) * p.heads + w.head0 + my_head] = (ref + log2f(sum)) * LN2;
+            const int row0 = (warp & 3) * 32;
+            auto where = [&](int i) -> __nv_bfloat16* {
+                const int rr = row0 + i, a = first + rr / p.pack;
+                return a < w.t.len ? p.out + (int64_t)(w.t.t0 + a) * p.ld_out + (int64_t)(w.head0 + rr % p.pack) * p.head_dim : nullptr;
+            };
+#pragma unroll 1
+            for (int c = 0; c < p.head_dim; c += 32) {
+                uint32_t o[32];
+                float f[32];
+                tmem_ld_x32(o_addr + c, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int k = 0; k < 32; ++k) f[k] = __uint_as_float(o[k]) * inv;
+                store_rows32(f, c, p.head_dim, lane, where);
+            }
+            tc_fence_before();                               // (read before the next tile's products, which wait for its P)
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, 512); }
+}
+
+struct Chunk { AttnTile t[240]; };
+__global__ void table_kernel(const __grid_constant__ Chunk src, AttnTile* __restrict__ dst, int n)
+{
+    ahead_wait();
+    ahead_release();
+    if ((int)threadIdx.x < n) dst[threadIdx.x] = src.t[threadIdx.x];
+}
+
+// Tiles sorted by the length of their loops, longest first (a counting sort: loops are short numbers).
+std::vector<AttnTile> longest_first(const std::vector<AttnTile>& tiles, const std::vector<int32_t>& loops, int32_t most)
+{
+    std::vector<int32_t> place((size_t)most + 2, 0);
+    for (int32_t n : loops) ++place[(size_t)(most - n) + 1];
+    for (size_t i = 1; i < place.size(); ++i) place[i] += place[i - 1];
+    std::vector<AttnTile> out(tiles.size());
+    for (size_t i = 0; i < tiles.size(); ++i) out[(size_t)place[(size_t)(most - loops[i])]++] = tiles[i];
+    return out;
+}
+
+}  // namespace
+
+std::vector<AttnTile> query_tiles(const AttnArgs& a, int32_t tokens_per_tile)
+{
+    std::vector<AttnTile> tiles;
+    std::vector<int32_t> loops;
+    int32_t most = 1;
+    for (int64_t e = 0; e < a.n; ++e) {
+        const int64_t len = a.offsets[e + 1] - a.offsets[e];
+        for (int64_t at = 0; at < len; at += tokens_per_tile) {
+            tiles.push_back({(int32_t)a.offsets[e], (int32_t)len, (int32_t)at, 0});
+            const int32_t n = (int32_t)((std::min(at + tokens_per_tile, len) + TILE - 1) / TILE);
+            loops.push_back(n);
+            most = std::max(most, n);
+        }
+    }
+    return longest_first(tiles, loops, most);
+}
+
+std::vector<AttnTile> key_tiles(const AttnArgs& a)
+{
+    std::vector<AttnTile> tiles;
+    std::vector<int32_t> loops;
+    int32_t most = 1;
+    for (int64_t e = 0; e < a.n; ++e) {
+        const int64_t len = a.offsets[e + 1] - a.offsets[e];
+        for (int64_t at = 0; at < len; at += TILE) {
+            tiles.push_back({(int32_t)a.offsets[e], (int32_t)len, (int32_t)at, 0});
+            const int32_t n = (int32_t)((len - at + TILE - 1) / TILE);
+            loops.push_back(n);
+            most = std::max(most, n);
+        }
+    }
+    return longest_first(tiles, loops, most);
+}
+
+qless_status put_table(const std::vector<AttnTile>& tiles, TileTable* table, AttnTile* dev, cudaStream_t st)
+{
+    table->tiles = (int32_t)tiles.size();
+    table->list = nullptr;
+    if (tiles.size() <= (size_t)INLINE) {
+        memcpy(table->few, tiles.data(), tiles.size() * sizeof(AttnTile));
+        return QLESS_OK;
+    }
+    for (size_t i = 0; i < tiles.size(); i += 240) {         // as launch arguments: nothing of the host's is read once the call has returned
+        Chunk c;
+        const size_t n = std::min<size_t>(240, tiles.size() - i);
+        memcpy(c.t, tiles.data() + i, n * sizeof(AttnTile));
+        QLESS_CUDA_TRY(launch_ahead(table_kernel, dim3(1), dim3(256), 0, st, c, dev + i, (int)n));
+        count_launches(1);
+    }
+    table->list = dev;
+    return QLESS_OK;
+}
+
+qless_status head_map(CUtensorMap* out, const void* base, int64_t ld, int32_t heads, int32_t head_dim, int64_t tokens, uint32_t box_heads, uint32_t box_tokens)
+{
+    return make_tmap_heads_sw128(out, base, (uint64_t)head_dim, (uint64_t)heads, (uint64_t)tokens, (uint64_t)ld * 2, box_heads, box_tokens);
+}
+
+}  // namespace attn
+
+using namespace attn;
+
+int32_t attn_pack(int32_t heads, int32_t kv_heads)
+{
+    const int32_t group = heads / kv_heads;
+    int32_t pack = 1;
+    while (pack < 16 && group % (2 * pack) == 0) pack *= 2;
+    return pack;
+}
+
+template <int DB>
+static qless_status launch_forward(const AttnArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, ForwardParams& p, cudaStream_t st)
+{
+    const size_t op = (size_t)DB * 16384, budget = 227 * 1024 - 1024 - sizeof(Bars) - 2 * op;
+    p.stages = (int32_t)std::min<size_t>(MAX_STAGES, budget / op);
+    const size_t smem = 1024 + (2 + p.stages) * op + sizeof(Bars);
+    const int64_t grid = std::min<int64_t>(p.items, sm_count());
+    ProfileScope ps("attention", st);
+    QLESS_CUDA_TRY((allow_full_smem<attention_kernel<DB>>()));
+    QLESS_CUDA_TRY(launch_ahead(attention_kernel<DB>, dim3((unsigned)grid), dim3(NTHREADS), smem, st, q, k, v, p));
+    count_launches(1);
+    return QLESS_OK;
+}
+
+qless_status launch_attention(const AttnArgs& a, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st)
+{
+    const int32_t pack = attn_pack(a.heads, a.kv_heads), tok = TILE / pack, packs = a.heads / pack;
+    std::vector<AttnTile> tiles = query_tiles(a, 2 * tok);
+    // Too few pairs of tiles for the SMs: a tile to each block.
+    if ((int64_t)tiles.size() * packs < sm_count()) {
+        tiles = query_tiles(a, tok);
+        for (AttnTile& t : tiles) t.unused = 1;
+    }
+    if (tiles.empty()) return QLESS_OK;
+    ForwardParams p;
+    qless_status s = put_table(tiles, &p.table, reinterpret_cast<AttnTile*>(ws), st);
+    if (s != QLESS_OK) return s;
+    CUtensorMap q, k, v;
+    if ((s = head_map(&q, a.q, a.ld_q, a.heads, a.head_dim, a.tokens, pack, tok)) != QLESS_OK) return s;
+    if ((s = head_map(&k, a.k, a.ld_k, a.kv_heads, a.head_dim, a.tokens, 1, TILE)) != QLESS_OK) return s;
+    if ((s = head_map(&v, a.v, a.ld_v, a.kv_heads, a.head_dim, a.tokens, 1, TILE)) != QLESS_OK) return s;
+    p.out = reinterpret_cast<__nv_bfloat16*>(a.out); p.lse = a.lse; p.ld_out = a.ld_out;
+    p.packs = packs; p.pack = pack; p.group = a.heads / a.kv_heads; p.heads = a.heads; p.head_dim = a.head_dim;
+    p.items = (int64_t)tiles.size() * packs; p.scale_log2 = a.scale * LOG2E; p.timeout_word = timeout_word;
+    return a.head_dim <= 64 ? launch_forward<1>(a, q, k, v, p, st) : launch_forward<2>(a, q, k, v, p, st);
+}
+
+}  // namespace qless

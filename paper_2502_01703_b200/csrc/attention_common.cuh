@@ -1,0 +1,92 @@
+// What the attention kernels share: tiles of query rows, the table of work, small arithmetic.
+//
+// Query heads that read the same key head are packed into a tile's rows: with `pack` of them (the largest power of two that divides the group,
+// at most 16) a tile of 128 rows holds 128 / pack tokens, row r = token r / pack, head r % pack. One copy of a three-dimensional box
+// brings it, keys and values are read once for all of them, and short sequences fill their tiles better.
+#pragma once
+
+#include <vector>
+
+#include "qless_kernels.h"
+#include "tc_common.cuh"
+
+namespace qless {
+namespace attn {
+
+using namespace tc;
+
+constexpr int TILE = 128;                   // rows of a tile of queries, and of keys
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int INLINE = 160;                 // tiles that travel in the launch itself
+
+struct TileTable {
+    const AttnTile* list;                   // NULL: few
+    int32_t tiles;
+    AttnTile few[INLINE];
+};
+
+__device__ __forceinline__ AttnTile tile_at(const TileTable& t, int32_t i) { return t.list != nullptr ? t.list[i] : t.few[i]; }
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    const __nv_bfloat162 z = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&z);
+}
+__device__ __forceinline__ void unpack_bf16(const uint4& u, float (&v)[8])
+{
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { v[2 * k] = __uint_as_float(w[k] << 16); v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
+}
+
+struct Ring {
+    uint32_t slot = 0, parity = 0;
+    __device__ __forceinline__ void next(uint32_t n) { if (++slot == n) { slot = 0; parity ^= 1u; } }
+};
+
+// Rows [from, 128) of an operand of `blocks` 64-column blocks (128 rows of 128 bytes each) become zero: by a whole warp, between the copy's
+// arrival and the tensor core's reading. Rows behind a sequence's end are another sequence's (or nobody's): a zero factor alone would let
+// their infinities and NaN through.
+__device__ __forceinline__ void zero_rows(uint8_t* operand, int blocks, int from, int lane)
+{
+    for (int b = 0; b < blocks; ++b)
+        for (int i = from * 8 + lane; i < TILE * 8; i += 32) *reinterpret_cast<uint4*>(operand + b * 16384 + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async_smem();
+    __syncwarp();
+}
+
+// A row of D bf16 values, 32 of them (columns c0 ..) in each lane for a row of its own, goes to memory 64 bytes at a time: `where` gives a row's
+// address or NULL.
+template <typename Where>
+__device__ __forceinline__ void store_rows32(const float (&v)[32], int c0, int head_dim, int lane, Where where)
+{
+    uint4 w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        w[k] = make_uint4(pack_bf16(v[8 * k], v[8 * k + 1]), pack_bf16(v[8 * k + 2], v[8 * k + 3]), pack_bf16(v[8 * k + 4], v[8 * k + 5]),
+                          pack_bf16(v[8 * k + 6], v[8 * k + 7]));
+    transpose4(w, lane);
+    const int c = c0 + (lane & 3) * 8;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        __nv_bfloat16* dst = where((lane & ~3) + k);
+        if (dst != nullptr && c < head_dim) *reinterpret_cast<uint4*>(dst + c) = w[k];
+    }
+}
+
+// Work of one launch: query tiles of `rows` tokens, or key tiles of 128, of every sequence, those with the longest loops first.
+std::vector<AttnTile> query_tiles(const AttnArgs& a, int32_t tokens_per_tile);
+std::vector<AttnTile> key_tiles(const AttnArgs& a);
+// Fills the table, through device memory at `dev` where it does not fit into the launch.
+qless_status put_table(const std::vector<AttnTile>& tiles, TileTable* table, AttnTile* dev, cudaStream_t st);
+// [tokens][heads][head_dim] bf16, boxes of 64 columns x box_heads x box_tokens, zeros behind head_dim.
+qless_status head_map(CUtensorMap* out, const void* base, int64_t ld, int32_t heads, int32_t head_dim, int64_t tokens, uint32_t box_heads, uint32_t box_tokens);
+
+}  // namespace attn
+}  // namespace qless

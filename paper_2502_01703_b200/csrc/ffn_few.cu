@@ -1,0 +1,367 @@
+// Gated feed-forward block with few tokens: the weights' bytes are the floor, so the weights stream past the tokens.
+//
+// Every product is D^T = weights x tokens^T with 128 of the weights' output features as the rows of a tile and all tokens (up to 256) as its columns: the tensor
+// core's work goes to tokens that exist, and a block reads its part of the weights once. Tiles are cut along the contraction until they fill the
+// SMs (slices: fp32 partial sums, which stay in L2); few_finish_kernel adds a result's slices in order and applies what follows the product. No atomics.
+//   forward   [g; u] = [Wg; Wu] x^T, finish: h (g, u);   y = Wd h^T, finish: bf16
+//   backward  dh = Wd^T dy^T, finish: dg, du (h);   dx = Wg^T dg^T + Wu^T du^T, finish: bf16
+// Blocks are single CTAs: warp 0 TMA, warp 1 tcgen05, warps 2-5 epilogue; two accumulators in tensor memory.
+#include <algorithm>
+
+#include "ffn_common.cuh"
+
+namespace qless {
+namespace ffn {
+
+namespace {
+
+constexpr int NTHREADS = 192;
+constexpr int MAX_STAGES = 6;
+constexpr int KB = 128;                     // contraction per stage
+constexpr int A_BYTES = 32768;
+
+enum { GLU = 0, GLU_BACK = 1, OUT = 2 };
+
+struct FewParams {
+    int32_t tokens, feats, sets;            // sets: matrices that are multiplied side by side (Wg and Wu)
+    int32_t kblocks, kswitch;               // from block kswitch on: the second weights and the second tokens' operand
+    int32_t slices, per_slice, n_cols, stages;
+    float* part;                            // [slice][set][tokens][feats]
+    int64_t items;
+    unsigned int* timeout_word;
+};
+
+struct __align__(8) Bars {
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES], d_full[2], d_empty[2], drain;
+    uint32_t tmem_base, abort_flag;
+};
+
+struct Ring {
+    uint32_t slot = 0, parity = 0;
+    __device__ __forceinline__ void next(uint32_t n) { if (++slot == n) { slot = 0; parity ^= 1u; } }
+};
+
+// A_MN: the weights' rows in memory run along the features.
+template <bool A_MN>
+__global__ void __launch_bounds__(NTHREADS, 1)
+few_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_w2, const __grid_constant__ CUtensorMap tm_x,
+                const __grid_constant__ CUtensorMap tm_x2, const FewParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const int b_half = p.n_cols * 128, stage_bytes = A_BYTES + 2 * b_half;      // (n_cols a multiple of 16: blocks stay on 1024-byte boundaries)
+    const uint32_t nS = (uint32_t)p.stages;
+    Bars* bars = reinterpret_cast<Bars*>(smem + (size_t)nS * stage_bytes);
+    volatile uint32_t* abort_flag = &bars->abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&bars->d_full[s]), 1); mbar_init(smem_u32(&bars->d_empty[s]), 4); }
+        mbar_init(smem_u32(&bars->drain), 1);
+        bars->abort_flag = 0;
+        fence_barrier_init();
+        prefetch_tmap(&tm_w); prefetch_tmap(&tm_w2); prefetch_tmap(&tm_x); prefetch_tmap(&tm_x2);
+    }
+    if (warp == 1) { tmem_alloc(smem_u32(&bars->tmem_base), 512); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = bars->tmem_base;                   // accumulators at columns 0 and 256
+    ahead_wait();
+    ahead_release();
+
+    const int tiles = (p.feats + 127) / 128;
+    auto item_of = [&](int64_t item, int& set, int& tile, int& slice, int& kb0, int& kb1) {
+        const int64_t r = item / p.slices;
+        slice = (int)(item - r * p.slices);
+        set = (int)(r / tiles);
+        tile = (int)(r - (int64_t)set * tiles);
+        kb0 = min(p.kblocks, slice * p.per_slice);
+        kb1 = min(p.kblocks, kb0 + p.per_slice);
+    };
+    auto warp_wait = [&](uint64_t* bar, uint32_t parity, uint32_t code) -> bool {
+        const bool w = mbar_wait(smem_u32(bar), parity, abort_flag, p.timeout_word, code);
+        return __all_sync(0xFFFFFFFFu, w);
+    };
+
+    if (warp == 0) {
+        Ring ring;
+        uint32_t it = 0;
+        bool ok = true;
+        for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            int set, tile, slice, kb0, kb1;
+            item_of(item, set, tile, slice, kb0, kb1);
+            for (int kb = kb0; kb < kb1; ++kb, ++it, ring.next(nS)) {
+                if (!warp_wait(&bars->empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
+                const bool second = kb >= p.kswitch;
+                const CUtensorMap* mw = second || set ? &tm_w2 : &tm_w;
+                const CUtensorMap* mx = second ? &tm_x2 : &tm_x;
+                const int k0 = (second ? kb - p.kswitch : kb) * KB, f0 = tile * 128;
+                if (elect_one()) {
+                    const uint32_t full = smem_u32(&bars->full[ring.slot]), a = smem_u32(smem + (size_t)ring.slot * stage_bytes), b = a + A_BYTES;
+                    mbar_arrive_expect_tx(full, (uint32_t)stage_bytes);
+                    for (int j = 0; j < 2; ++j) tma_load_2d(a + j * 16384, mw, full, (A_MN ? f0 : k0) + 64 * j, A_MN ? k0 : f0);
+                    for (int j = 0; j < 2; ++j) tma_load_2d(b + j * b_half, mx, full, k0 + 64 * j, 0);
+                }
+                __syncwarp();
+            }
+        }
+        if (!ok)
+            for (uint32_t j = it > nS ? it - nS : 0u; j < it; ++j)
+                if (!mbar_wait_quiet(smem_u32(&bars->full[j % nS]), (j / nS) & 1u, 1u << 14)) break;
+    } else if (warp == 1) {
+        const uint32_t idesc = make_idesc(1, 1, 1, 128, (uint32_t)p.n_cols) | (A_MN ? IDESC_A_MN : 0u);
+        const uint64_t b_next = (uint64_t)(b_half / 16);      // the second 64 columns of the contraction
+        Ring ring;
+        uint32_t n_acc = 0;
+        bool ok = true;
+        for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++n_acc) {
+            int set, tile, slice, kb0, kb1;
+            item_of(item, set, tile, slice, kb0, kb1);
+            const uint32_t buf = n_acc & 1u, d = tmem + buf * 256;
+            if (!warp_wait(&bars->d_empty[buf], ((n_acc >> 1) & 1u) ^ 1u, TO_MMA)) { ok = false; break; }
+            tc_fence_after();
+            for (int kb = kb0; kb < kb1; ++kb, ring.next(nS)) {
+                if (!warp_wait(&bars->full[ring.slot], ring.parity, TO_MMA)) { ok = false; break; }
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint32_t a = smem_u32(smem + (size_t)ring.slot * stage_bytes);
+                    const uint64_t a0 = A_MN ? make_smem_desc_mn_sw128(a, 16384) : make_smem_desc_sw128(a), b0 = make_smem_desc_sw128(a + A_BYTES);
+#pragma unroll
+                    for (int k = 0; k < KB / 16; ++k)
+                        mma_f16_ss(d, a0 + (uint64_t)(A_MN ? k * 128 : (k >> 2) * 1024 + (k & 3) * 2), b0 + (k >> 2) * b_next + (uint64_t)((k & 3) * 2), idesc,
+                                   kb > kb0 || k > 0);
+                    mma_commit(smem_u32(&bars->empty[ring.slot]));
+                }
+                __syncwarp();
+            }
+            if (ok && elect_one()) mma_commit(smem_u32(&bars->d_full[buf]));
+            __syncwarp();
+        }
+        if (elect_one()) mma_commit(smem_u32(&bars->drain));
+        __syncwarp();
+        mbar_wait_quiet(smem_u32(&bars->drain), 0u);
+    } else {
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        uint32_t n_acc = 0;
+        for (int64_t item = blockIdx.x; item < p.items; item += gridDim.x, ++n_acc) {
+            int set, tile, slice, kb0, kb1;
+            item_of(item, set, tile, slice, kb0, kb1);
+            const uint32_t buf = n_acc & 1u;
+            const int f = tile * 128 + (warp & 3) * 32 + lane;
+            const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->d_full[buf]), (n_acc >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
+            if (!ok) break;
+            tc_fence_after();
+            float* dst = p.part + ((int64_t)slice * p.sets + set) * p.tokens * p.feats + f;
+#pragma unroll 1
+            for (int c0 = 0; c0 < p.tokens; c0 += 32) {
+                float v[32];
+                load_acc(tmem + lanes + buf * 256 + c0, v);
+                if (f < p.feats) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (c0 + k < p.tokens) dst[(int64_t)(c0 + k) * p.feats] = v[k];
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars->d_empty[buf]));
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, 512); }
+}
+
+struct FinishParams {
+    const float* part;
+    int32_t tokens, feats, slices, act;
+    const __nv_bfloat16* gate_in; const __nv_bfloat16* up_in;
+    __nv_bfloat16* out; __nv_bfloat16* out2; __nv_bfloat16* out3;      // GLU: h, g, u; GLU_BACK: dg, du, h; OUT: the result
+    int64_t ld_gate_in, ld_up_in, ld, ld2, ld3;
+};
+
+// Four features of a token to a thread.
+template <int MODE>
+__global__ void __launch_bounds__(256) few_finish_kernel(const FinishParams p)
+{
+    ahead_wait();
+    ahead_release();
+    const int quads = p.feats / 4;
+    const int64_t plane = (int64_t)p.tokens * p.feats, all = (int64_t)p.tokens * quads;
+    auto put = [](__nv_bfloat16* dst, const float (&v)[4]) { *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])); };
+    auto get = [](const __nv_bfloat16* src, float (&v)[4]) {
+        const uint2 u = *reinterpret_cast<const uint2*>(src);
+        v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xFFFF0000u); v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xFFFF0000u);
+    };
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t t = i / quads;
+        const int f = (int)(i - t * quads) * 4;
+        constexpr int SETS = MODE == GLU ? 2 : 1;
+        float v[2][4] = {};
+#pragma unroll 4
+        for (int s = 0; s < p.slices; ++s)
+#pragma unroll
+            for (int k = 0; k < SETS; ++k) {
+                const float4 y = *reinterpret_cast<const float4*>(p.part + ((int64_t)s * SETS + k) * plane + t * p.feats + f);
+                v[k][0] += y.x; v[k][1] += y.y; v[k][2] += y.z; v[k][3] += y.w;
+            }
+        if (MODE == OUT) {
+            put(p.out + t * p.ld + f, v[0]);
+        } else if (MODE == GLU) {
+            if (p.out2 != nullptr) { put(p.out2 + t * p.ld2 + f, v[0]); put(p.out3 + t * p.ld3 + f, v[1]); }
+            float h[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float a, da;
+                activation(p.act, v[0][k], a, da);
+                h[k] = a * v[1][k];
+            }
+            put(p.out + t * p.ld + f, h);
+        } else {
+            float g[4], u[4], h[4];
+            get(p.gate_in + t * p.ld_gate_in + f, g);
+            get(p.up_in + t * p.ld_up_in + f, u);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float a, da;
+                activation(p.act, g[k], a, da);
+                h[k] = a * u[k];
+                g[k] = v[0][k] * u[k] * da;
+                u[k] = v[0][k] * a;
+            }
+            put(p.out + t * p.ld + f, g);
+            put(p.out2 + t * p.ld2 + f, u);
+            if (p.out3 != nullptr) put(p.out3 + t * p.ld3 + f, h);
+        }
+    }
+}
+
+struct Slices { int32_t slices, per; };
+
+// Along the contraction: the fewest rounds of blocks, counted in stages; an item costs its stages, one for its start, and the writing and reading
+// of its partial sums (tokens x 128 x 8 bytes, in stages of 32 KiB of weights).
+Slices slices_of(int64_t tokens, int64_t feats, int64_t sets, int64_t kblocks)
+{
+    const int64_t sms = sm_count(), tiles = (feats + 127) / 128 * sets;
+    int64_t best = 1;
+    double best_cost = 0.0;
+    for (int64_t s = 1; s <= 32 && s <= (kblocks + 1) / 2; ++s) {
+        const int64_t per = (kblocks + s - 1) / s, rounds = (tiles * s + sms - 1) / sms;
+        const double cost = (double)rounds * ((double)per + 1.0 + (double)tokens / 32.0);
+        if (s == 1 || cost < best_cost) { best = s; best_cost = cost; }
+    }
+    const int64_t per = (kblocks + best - 1) / best;
+    return {(int32_t)((kblocks + per - 1) / per), (int32_t)per};
+}
+
+int64_t blocks_of(int64_t k) { return (k + KB - 1) / KB; }
+
+template <bool A_MN>
+qless_status product(const char* name, const CUtensorMap& w, const CUtensorMap& w2, const CUtensorMap& x, const CUtensorMap& x2, FewParams p, cudaStream_t st)
+{
+    const size_t stage = A_BYTES + (size_t)p.n_cols * 256, budget = 227 * 1024 - 1024 - sizeof(Bars);
+    p.stages = (int32_t)std::min<size_t>(MAX_STAGES, budget / stage);
+    p.items = (int64_t)p.sets * ((p.feats + 127) / 128) * p.slices;
+    const size_t smem = 1024 + p.stages * stage + sizeof(Bars);
+    ProfileScope ps(name, st);
+    QLESS_CUDA_TRY((allow_full_smem<few_gemm_kernel<A_MN>>()));
+    QLESS_CUDA_TRY(launch_ahead(few_gemm_kernel<A_MN>, dim3((unsigned)std::min<int64_t>(p.items, sm_count())), dim3(NTHREADS), smem, st, w, w2, x, x2, p));
+    count_launches(1);
+    return QLESS_OK;
+}
+
+template <int MODE>
+qless_status finish(const FinishParams& p, cudaStream_t st)
+{
+    const int64_t blocks = ((int64_t)p.tokens * (p.feats / 4) + 255) / 256;
+    ProfileScope ps("ffn_finish", st);
+    QLESS_CUDA_TRY(launch_ahead(few_finish_kernel<MODE>, dim3((unsigned)std::min<int64_t>(blocks, sm_count() * 8)), dim3(256), 0, st, p));
+    count_launches(1);
+    return QLESS_OK;
+}
+
+qless_status weight_map(CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int64_t ld)
+{
+    return make_tmap_2d_sw128(m, p, 2, (uint64_t)cols, (uint64_t)rows, (uint64_t)ld * 2, 64, 128);
+}
+qless_status token_map(CUtensorMap* m, const void* p, int64_t cols, int64_t tokens, int64_t ld, int32_t n_cols)
+{
+    return make_tmap_2d_sw128(m, p, 2, (uint64_t)cols, (uint64_t)tokens, (uint64_t)ld * 2, 64, (uint32_t)n_cols);
+}
+
+}  // namespace
+
+#define QLESS_STEP(expr)                         \
+    do {                                         \
+        const qless_status s__ = (expr);         \
+        if (s__ != QLESS_OK) return s__;         \
+    } while (0)
+
+size_t few_workspace(int64_t tokens, int32_t width, int32_t inner, bool backward)
+{
+    const size_t first = backward ? (size_t)slices_of(tokens, inner, 1, blocks_of(width)).slices : (size_t)2 * slices_of(tokens, inner, 2, blocks_of(width)).slices;
+    const size_t second = (size_t)slices_of(tokens, width, 1, (backward ? 2 : 1) * blocks_of(inner)).slices;
+    return align_up((size_t)tokens * 4 * std::max(first * inner, second * width), 256);
+}
+
+qless_status launch_few_forward(const FfnArgs& a, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st)
+{
+    const int32_t n_cols = (int32_t)((a.tokens + 15) / 16 * 16);
+    CUtensorMap x, wg, wu, wd, h;
+    QLESS_STEP(token_map(&x, a.x, a.width, a.tokens, a.ld_x, n_cols));
+    QLESS_STEP(token_map(&h, a.hidden, a.inner, a.tokens, a.ld_hidden, n_cols));
+    QLESS_STEP(weight_map(&wg, a.w_gate, a.width, a.inner, a.ld_wg));
+    QLESS_STEP(weight_map(&wu, a.w_up, a.width, a.inner, a.ld_wu));
+    QLESS_STEP(weight_map(&wd, a.w_down, a.inner, a.width, a.ld_wd));
+    FewParams p{};
+    p.tokens = (int32_t)a.tokens; p.n_cols = n_cols; p.part = reinterpret_cast<float*>(ws); p.timeout_word = timeout_word;
+    Slices s = slices_of(a.tokens, a.inner, 2, blocks_of(a.width));
+    p.feats = a.inner; p.sets = 2; p.kblocks = p.kswitch = (int32_t)blocks_of(a.width); p.slices = s.slices; p.per_slice = s.per;
+    QLESS_STEP(product<false>("ffn_glu", wg, wu, x, x, p, st));
+    FinishParams f{};
+    f.part = p.part; f.tokens = p.tokens; f.feats = a.inner; f.slices = s.slices; f.act = a.act;
+    f.out = reinterpret_cast<__nv_bfloat16*>(a.hidden); f.out2 = reinterpret_cast<__nv_bfloat16*>(a.gate); f.out3 = reinterpret_cast<__nv_bfloat16*>(a.up);
+    f.ld = a.ld_hidden; f.ld2 = a.ld_gate; f.ld3 = a.ld_up;
+    QLESS_STEP(finish<GLU>(f, st));
+    s = slices_of(a.tokens, a.width, 1, blocks_of(a.inner));
+    p.feats = a.width; p.sets = 1; p.kblocks = p.kswitch = (int32_t)blocks_of(a.inner); p.slices = s.slices; p.per_slice = s.per;
+    QLESS_STEP(product<false>("ffn_down", wd, wd, h, h, p, st));
+    f.feats = a.width; f.slices = s.slices; f.out = reinterpret_cast<__nv_bfloat16*>(a.out); f.ld = a.ld_out;
+    return finish<OUT>(f, st);
+}
+
+qless_status launch_few_backward(const FfnArgs& a, __nv_bfloat16* hidden, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st)
+{
+    const int32_t n_cols = (int32_t)((a.tokens + 15) / 16 * 16);
+    CUtensorMap dy, wg, wu, wd, dg, du;
+    QLESS_STEP(token_map(&dy, a.dy, a.width, a.tokens, a.ld_dy, n_cols));
+    QLESS_STEP(token_map(&dg, a.gate, a.inner, a.tokens, a.ld_gate, n_cols));
+    QLESS_STEP(token_map(&du, a.up, a.inner, a.tokens, a.ld_up, n_cols));
+    QLESS_STEP(weight_map(&wg, a.w_gate, a.width, a.inner, a.ld_wg));
+    QLESS_STEP(weight_map(&wu, a.w_up, a.width, a.inner, a.ld_wu));
+    QLESS_STEP(weight_map(&wd, a.w_down, a.inner, a.width, a.ld_wd));
+    FewParams p{};
+    p.tokens = (int32_t)a.tokens; p.n_cols = n_cols; p.sets = 1; p.part = reinterpret_cast<float*>(ws); p.timeout_word = timeout_word;
+    Slices s = slices_of(a.tokens, a.inner, 1, blocks_of(a.width));
+    p.feats = a.inner; p.kblocks = p.kswitch = (int32_t)blocks_of(a.width); p.slices = s.slices; p.per_slice = s.per;
+    QLESS_STEP(product<true>("ffn_glu_back", wd, wd, dy, dy, p, st));
+    FinishParams f{};
+    f.part = p.part; f.tokens = p.tokens; f.feats = a.inner; f.slices = s.slices; f.act = a.act;
+    f.gate_in = reinterpret_cast<const __nv_bfloat16*>(a.gate_in); f.up_in = reinterpret_cast<const __nv_bfloat16*>(a.up_in);
+    f.ld_gate_in = a.ld_gate_in; f.ld_up_in = a.ld_up_in;
+    f.out = reinterpret_cast<__nv_bfloat16*>(a.gate); f.out2 = reinterpret_cast<__nv_bfloat16*>(a.up); f.out3 = hidden;
+    f.ld = a.ld_gate; f.ld2 = a.ld_up; f.ld3 = a.inner;
+    QLESS_STEP(finish<GLU_BACK>(f, st));
+    if (a.out == nullptr) return QLESS_OK;
+    p.feats = a.width; p.kswitch = (int32_t)blocks_of(a.inner); p.kblocks = 2 * p.kswitch;
+    s = slices_of(a.tokens, a.width, 1, p.kblocks);
+    p.slices = s.slices; p.per_slice = s.per;
+    QLESS_STEP(product<true>("ffn_grad_x", wg, wu, dg, du, p, st));
+    f.feats = a.width; f.slices = s.slices; f.out = reinterpret_cast<__nv_bfloat16*>(a.out); f.ld = a.ld_out;
+    return finish<OUT>(f, st);
+}
+
+}  // namespace ffn
+}  // namespace qless

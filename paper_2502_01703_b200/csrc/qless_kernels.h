@@ -131,4 +131,52 @@ struct LossArgs {
 };
 qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st);
 
+// Layer normalisation (layer_norm.cu).
+struct NormPlan { int32_t share, block; int64_t blocks, workers; size_t total; };
+NormPlan plan_norm(int64_t tokens, int32_t width, bool sums);
+struct NormArgs {
+    const void* x; const void* dy; const void* weight; const void* bias;
+    void* out; float* mean; float* rstd; void* grad_weight; void* grad_bias;
+    int64_t tokens, ld_x, ld_dy, ld_out;
+    int32_t width, center;
+    qless_dtype dtype, param_dtype;
+    float eps;
+};
+qless_status launch_norm_forward(const NormArgs& a, cudaStream_t st);
+qless_status launch_norm_backward(const NormArgs& a, uint8_t* ws, cudaStream_t st);
+
+// Causal attention over packed sequences (attention.cu, attention_backward.cu).
+struct AttnTile { int32_t t0, len, at, unused; };       // a sequence's first token and length, and the tile's first token within it
+struct AttnArgs {
+    const void* q; const void* k; const void* v; const void* out_in; const void* dout;
+    int64_t ld_q, ld_k, ld_v, ld_out, ld_dout;
+    void* out; float* lse; const float* lse_in;
+    void* dq; void* dk; void* dv;
+    int64_t ld_dq, ld_dk, ld_dv;
+    const int64_t* offsets;                             // host
+    int64_t tokens, n;
+    int32_t heads, kv_heads, head_dim;
+    float scale;
+};
+int32_t attn_pack(int32_t heads, int32_t kv_heads);     // query heads that share a tile's rows
+size_t attention_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads, bool backward);
+qless_status launch_attention(const AttnArgs& a, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st);
+qless_status launch_attention_backward(const AttnArgs& a, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st);
+
+// Gated feed-forward block (ffn.cu; few tokens: ffn_few.cu).
+struct FfnArgs {
+    const void* x; const void* dy; const void* gate_in; const void* up_in;
+    const void* w_gate; const void* w_up; const void* w_down;
+    int64_t ld_x, ld_dy, ld_gate_in, ld_up_in, ld_wg, ld_wu, ld_wd;
+    void* out; void* hidden; void* gate; void* up;      // backward: dx, -, dgate, dup
+    int64_t ld_out, ld_hidden, ld_gate, ld_up;
+    void* dw_gate; void* dw_up; void* dw_down;
+    int64_t ld_dwg, ld_dwu, ld_dwd;
+    int64_t tokens;
+    int32_t width, inner, act;
+};
+size_t ffn_workspace(int64_t tokens, int32_t width, int32_t inner, bool backward, bool weights);
+qless_status launch_ffn_forward(const FfnArgs& a, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st);
+qless_status launch_ffn_backward(const FfnArgs& a, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st);
+
 }  // namespace qless

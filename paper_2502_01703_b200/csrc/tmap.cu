@@ -63,6 +63,25 @@ qless_status make_tmap_blocks_sw128(CUtensorMap* out, const void* base, int elem
     return QLESS_OK;
 }
 
+qless_status make_tmap_heads_sw128(CUtensorMap* out, const void* base, uint64_t head_dim, uint64_t heads, uint64_t tokens, uint64_t token_stride,
+                                   uint32_t box_heads, uint32_t box_tokens)
+{
+    PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
+    qless_status s = get_encoder(&encode);
+    if (s != QLESS_OK) return s;
+    QLESS_REQUIRE(box_heads >= 1 && box_tokens >= 1 && box_heads * box_tokens <= 256, QLESS_ERR_INVALID_ARG, "unsupported tensor map box");
+    QLESS_REQUIRE((reinterpret_cast<uintptr_t>(base) % 16) == 0 && token_stride % 16 == 0 && head_dim % 8 == 0, QLESS_ERR_INVALID_ARG,
+                  "tensor map base and strides must be multiples of 16 bytes");
+    const cuuint64_t dims[3] = {head_dim, heads, tokens};
+    const cuuint64_t strides[2] = {head_dim * 2, token_stride};
+    const cuuint32_t box[3] = {64, box_heads, box_tokens};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    QLESS_REQUIRE(r == CUDA_SUCCESS, QLESS_ERR_CUDA, "cuTensorMapEncodeTiled (heads) failed with CUresult %d", (int)r);
+    return QLESS_OK;
+}
+
 qless_status make_tmap_2d_sw128(CUtensorMap* out, const void* base, int elem_bytes, uint64_t inner, uint64_t outer,
                                 uint64_t row_stride_bytes, uint32_t box_inner, uint32_t box_outer)
 {
