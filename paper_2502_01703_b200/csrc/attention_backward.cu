@@ -12,7 +12,7 @@
 // dk/dv kernel: S^T = K Q^T and dp^T = V dO^T, so that P^T and dS^T are left operands of the products that follow and stay in tensor memory
 // (rounded to bf16 in the place of S^T and dp^T), and dv, dk: 4 x 128 columns. While the threads take exponentials of one tile the tensor core
 // works on dp and dk, while they form ds it works on dv and the next scores.
-// Eight warps do the arithmetic, each 32 rows by half of the columns; warp 0 brings tiles by TMA, warp 1 issues products, warps 2 and 3 bring
+// Sixteen warps do the arithmetic, each 32 rows by a quarter of the columns; warp 0 brings tiles by TMA, warp 1 issues products, warps 2 and 3 bring
 // lse and delta of the query rows (dk/dv kernel).
 // P and ds are rounded to bf16 (2^-9 of each, independent of each other); exponentials, differences and sums are fp32.
 // Bound: 128 x 128 scores cost three (dq) and four products of 512 clocks (head_dim 128) and 1024 clocks of the special-function units in each kernel.
@@ -26,10 +26,10 @@ using namespace attn;
 
 namespace {
 
-constexpr int NTHREADS = 384, MAX_STAGES = 10;
+constexpr int NTHREADS = 640, MAX_STAGES = 10;
 
-// Columns of step s (16 rows of the contraction) of a left operand in tensor memory that two groups of warps wrote, each over the first half of its own 64 columns.
-__device__ __forceinline__ constexpr uint32_t half_column(int s) { return (uint32_t)((s >> 2) * 64 + (s & 3) * 8); }
+// Columns of step s (16 rows of the contraction) of a left operand in tensor memory that four groups of warps wrote, each over the first half of its own 32 columns.
+__device__ __forceinline__ constexpr uint32_t quarter_column(int s) { return (uint32_t)((s >> 1) * 32 + (s & 1) * 8); }
 
 struct QueryParams {
     TileTable table;
@@ -46,7 +46,7 @@ struct QueryParams {
 struct __align__(8) QueryBars {
     uint64_t q_full, q_empty, full[MAX_STAGES], empty[MAX_STAGES], s_full[2], dp_full, ds_ready, dq_full, delta_ready, drain;
     uint32_t tmem_base, abort_flag;
-    float part[2][2][TILE];                 // halves of delta, of an item and the next
+    float part[2][4][TILE];                 // quarters of delta, of an item and the next
 };
 
 template <int DB>
@@ -69,8 +69,8 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         mbar_init(smem_u32(&bars->q_full), 1); mbar_init(smem_u32(&bars->q_empty), 1);
         for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&bars->s_full[i]), 1);
         for (uint32_t i = 0; i < MAX_STAGES; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), 1); }
-        mbar_init(smem_u32(&bars->dp_full), 1); mbar_init(smem_u32(&bars->ds_ready), 8); mbar_init(smem_u32(&bars->dq_full), 1);
-        mbar_init(smem_u32(&bars->delta_ready), 8);
+        mbar_init(smem_u32(&bars->dp_full), 1); mbar_init(smem_u32(&bars->ds_ready), 16); mbar_init(smem_u32(&bars->dq_full), 1);
+        mbar_init(smem_u32(&bars->delta_ready), 16);
         mbar_init(smem_u32(&bars->drain), 1);
         bars->abort_flag = 0;
         fence_barrier_init();
@@ -99,7 +99,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     };
 
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 0) {
             Ring ring;
             uint32_t it = 0, q_uses = 0;
@@ -190,7 +190,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         const uint64_t b = make_smem_desc_mn_sw128(smem_u32(ring_smem + (size_t)k.slot * OP), 16384);
                         const uint32_t a = tmem + ((s_uses + j) & 1u) * 128;
 #pragma unroll
-                        for (int s = 0; s < 8; ++s) mma_f16_ts(tmem + 384, a + half_column(s), b + (uint64_t)(s * 128), idesc_q, j > 0 || s > 0);
+                        for (int s = 0; s < 8; ++s) mma_f16_ts(tmem + 384, a + quarter_column(s), b + (uint64_t)(s * 128), idesc_q, j > 0 || s > 0);
                         mma_commit(smem_u32(&bars->empty[k.slot]));
                         if (j + 1 == w.n) mma_commit(smem_u32(&bars->dq_full));
                     }
@@ -205,8 +205,8 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             mbar_wait_quiet(smem_u32(&bars->drain), 0u);
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-        const int half = warp >= 8 ? 1 : 0, r = (warp & 3) * 32 + lane;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        const int part = (warp >> 2) - 1, r = (warp & 3) * 32 + lane;      // which quarter of the columns
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const int my_tok = r / p.pack, my_head = r % p.pack;
         uint32_t s_uses = 0, dp_uses = 0, dq_uses = 0;       // (dq_uses: items so far)
@@ -223,7 +223,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 const __nv_bfloat16* d = p.dout + token * p.ld_dout + (int64_t)head * p.head_dim;
                 float acc[2] = {0.0f, 0.0f};
 #pragma unroll 4
-                for (int c = half * 8; c < p.head_dim; c += 16) {
+                for (int c = part * 8; c < p.head_dim; c += 32) {
                     float a[8], b[8];
                     unpack_bf16(__ldg(reinterpret_cast<const uint4*>(o + c)), a);
                     unpack_bf16(__ldg(reinterpret_cast<const uint4*>(d + c)), b);
@@ -233,52 +233,42 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 delta = acc[0] + acc[1];
                 off = p.lse[token * p.heads + head] * LOG2E;
             }
-            // The two halves meet through an mbarrier, whose waits end (a block-wide barrier would wait for warps that gave up). An item's places are
+            // The quarters meet through an mbarrier, whose waits end (a block-wide barrier would wait for warps that gave up). An item's places are
             // written again two items later, when every warp has arrived for the item between.
-            bars->part[dq_uses & 1u][half][r] = delta;
+            bars->part[dq_uses & 1u][part][r] = delta;
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bars->delta_ready));
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->delta_ready), dq_uses & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
             if (!ok) break;
-            delta = bars->part[dq_uses & 1u][0][r] + bars->part[dq_uses & 1u][1][r];
-            if (there && half == 0) p.delta[token * p.heads + head] = delta;
+            const float (*quarters)[TILE] = bars->part[dq_uses & 1u];
+            delta = (quarters[0][r] + quarters[1][r]) + (quarters[2][r] + quarters[3][r]);
+            if (there && part == 0) p.delta[token * p.heads + head] = delta;
             for (int j = 0; j < w.n; ++j) {
-                const uint32_t buf = s_uses & 1u, s_addr = tmem + lanes + buf * 128 + half * 64;
+                const uint32_t buf = s_uses & 1u, s_addr = tmem + lanes + buf * 128 + part * 32;
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->s_full[buf]), (s_uses >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
                 if (!ok) break;
                 ++s_uses;
                 tc_fence_after();
-                uint32_t s[2][32];
-                tmem_ld_x32(s_addr, s[0]);
-                tmem_ld_x32(s_addr + 32, s[1]);
+                uint32_t s[32], dp[32], e[16];
+                tmem_ld_x32(s_addr, s);
                 tmem_wait_ld();
-                const int lim = at - j * TILE - half * 64;   // this row's last key among the 64
-                const bool masked = j * TILE + TILE - 1 > w.t.at;
+                const int lim = at - j * TILE - part * 32;   // this row's last key among the 32
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) s[c][k] = __float_as_uint(ex2(fmaf(__uint_as_float(s[c][k]), p.scale_log2, -off)));
+                for (int k = 0; k < 32; ++k) s[k] = __float_as_uint(ex2(fmaf(__uint_as_float(s[k]), p.scale_log2, -off)));
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->dp_full), dp_uses++ & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t e[2][16];
+                tmem_ld_x32(tmem + lanes + 256 + part * 32, dp);
+                tmem_wait_ld();
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t dp[32];
-                    tmem_ld_x32(tmem + lanes + 256 + half * 64 + c * 32, dp);
-                    tmem_wait_ld();
+                for (int k = 0; k < 32; ++k) dp[k] = __float_as_uint(__uint_as_float(s[k]) * (__uint_as_float(dp[k]) - delta));
+                if (j * TILE + TILE - 1 > w.t.at) {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) dp[k] = __float_as_uint(__uint_as_float(s[c][k]) * (__uint_as_float(dp[k]) - delta));
-                    if (masked) {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) if (c * 32 + k > lim) dp[k] = 0u;
-                    }
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) e[c][k] = pack_bf16(__uint_as_float(dp[2 * k]), __uint_as_float(dp[2 * k + 1]));
+                    for (int k = 0; k < 32; ++k) if (k > lim) dp[k] = 0u;
                 }
-                // over this half's own scores: columns 0 .. 31 and 64 .. 95 of S
-                tmem_st_x16(s_addr, e[0]);
-                tmem_st_x16(s_addr + 16, e[1]);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) e[k] = pack_bf16(__uint_as_float(dp[2 * k]), __uint_as_float(dp[2 * k + 1]));
+                tmem_st_x16(s_addr, e);                      // over this quarter's own scores
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -294,7 +284,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 return a < w.t.len ? p.dq + (int64_t)(w.t.t0 + a) * p.ld_dq + (int64_t)(w.head0 + rr % p.pack) * p.head_dim : nullptr;
             };
 #pragma unroll 1
-            for (int c = half * 32; c < p.head_dim; c += 64) {
+            for (int c = part * 32; c < p.head_dim; c += 128) {
                 uint32_t o[32];
                 float f[32];
                 tmem_ld_x32(tmem + lanes + 384 + c, o);
@@ -324,7 +314,7 @@ struct KeyParams {
 
 constexpr int KEY_STAGES = 2;
 struct __align__(16) KeyBars {
-    float2 stat[KEY_STAGES][TILE];          // of each query row: lse (times log2 e), delta
+    float lse[KEY_STAGES][TILE], delta[KEY_STAGES][TILE];      // of each query row: lse times log2 e, delta
     uint64_t kv_full, kv_empty, full[KEY_STAGES], empty[KEY_STAGES], stat_full[KEY_STAGES], stat_empty[KEY_STAGES], s_full, dp_full, p_ready, ds_ready, done, drain;
     uint32_t tmem_base, abort_flag;
 };
@@ -348,10 +338,10 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         mbar_init(smem_u32(&bars->kv_full), 1); mbar_init(smem_u32(&bars->kv_empty), 1);
         for (int i = 0; i < KEY_STAGES; ++i) {
             mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), 1);
-            mbar_init(smem_u32(&bars->stat_full[i]), 2); mbar_init(smem_u32(&bars->stat_empty[i]), 8);
+            mbar_init(smem_u32(&bars->stat_full[i]), 2); mbar_init(smem_u32(&bars->stat_empty[i]), 16);
         }
         mbar_init(smem_u32(&bars->s_full), 1); mbar_init(smem_u32(&bars->dp_full), 1); mbar_init(smem_u32(&bars->done), 1);
-        mbar_init(smem_u32(&bars->p_ready), 8); mbar_init(smem_u32(&bars->ds_ready), 8); mbar_init(smem_u32(&bars->drain), 1);
+        mbar_init(smem_u32(&bars->p_ready), 16); mbar_init(smem_u32(&bars->ds_ready), 16); mbar_init(smem_u32(&bars->drain), 1);
         bars->abort_flag = 0;
         fence_barrier_init();
         prefetch_tmap(&tm_q); prefetch_tmap(&tm_do); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
@@ -382,7 +372,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     };
 
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 0) {
             Ring ring;
             uint32_t it = 0, kv_uses = 0;
@@ -436,7 +426,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             auto gradient = [&](uint32_t d, uint32_t a, const uint8_t* b_op, bool more) {
                 const uint64_t b = make_smem_desc_mn_sw128(smem_u32(b_op), 16384);
 #pragma unroll
-                for (int s = 0; s < 8; ++s) mma_f16_ts(d, a + half_column(s), b + (uint64_t)(s * 128), idesc_g, more || s > 0);
+                for (int s = 0; s < 8; ++s) mma_f16_ts(d, a + quarter_column(s), b + (uint64_t)(s * 128), idesc_g, more || s > 0);
             };
             for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
                 const Work w = work_of(item);
@@ -506,19 +496,22 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 const Work w = work_of(item);
                 int head0 = w.kv * p.group, i = w.first, left = w.per;
                 for (int j = 0; j < w.n; ++j, ring.next(KEY_STAGES)) {
-                    float2 got[2];
+                    float lse[2], delta[2];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {            // rows behind the end: P = e^(0 - infinity) = 0, dS = 0
                         const int r = (warp - 2) * 64 + h * 32 + lane, at = i * tok + r / p.pack;
-                        got[h] = make_float2(INFINITY, 0.0f);
+                        lse[h] = INFINITY; delta[h] = 0.0f;
                         if (at < w.t.len) {
                             const int64_t row = (int64_t)(w.t.t0 + at) * p.heads + head0 + r % p.pack;
-                            got[h] = make_float2(p.lse[row] * LOG2E, p.delta[row]);
+                            lse[h] = p.lse[row] * LOG2E; delta[h] = p.delta[row];
                         }
                     }
                     if (!warp_wait(&bars->stat_empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) bars->stat[ring.slot][(warp - 2) * 64 + h * 32 + lane] = got[h];
+                    for (int h = 0; h < 2; ++h) {
+                        const int r = (warp - 2) * 64 + h * 32 + lane;
+                        bars->lse[ring.slot][r] = lse[h]; bars->delta[ring.slot][r] = delta[h];
+                    }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&bars->stat_full[ring.slot]));
                     ++i;
@@ -527,9 +520,9 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-        const int half = warp >= 8 ? 1 : 0, r = (warp & 3) * 32 + lane;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        const int part = (warp >> 2) - 1, r = (warp & 3) * 32 + lane;      // which quarter of the columns
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_addr = tmem + lanes + part * 32, dp_addr = s_addr + 128;
         uint32_t uses = 0, done_uses = 0;
         Ring ring;
         bool ok = true;
@@ -538,9 +531,9 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             const int key = w.t.at + r;
             int i = w.first, left = w.per;
             for (int j = 0; j < w.n; ++j, ++uses, ring.next(KEY_STAGES)) {
-                // column c of this half is query row half * 64 + c: token i * tok + (half * 64 + c) / pack; it sees this row's key from `from` on
+                // column c of this quarter is query row part * 32 + c: token i * tok + (part * 32 + c) / pack; it sees this row's key from `from` on
                 const bool masked = i * tok < w.t.at + TILE - 1;
-                const int from = (key - i * tok) * p.pack - half * 64;
+                const int from = (key - i * tok) * p.pack - part * 32;
                 ++i;
                 if (--left == 0) { left = w.per; i = w.first; }
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->stat_full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_EPILOGUE));
@@ -548,31 +541,26 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->s_full), uses & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
                 if (!ok) break;
                 tc_fence_after();
-                const float4* stat = reinterpret_cast<const float4*>(&bars->stat[ring.slot][half * 64]);      // two rows each
-                float pr[64];
+                uint32_t s[32], dp[32], e[16];
+                tmem_ld_x32(s_addr, s);
+                const float4* lse = reinterpret_cast<const float4*>(&bars->lse[ring.slot][part * 32]);
+                const float4* delta = reinterpret_cast<const float4*>(&bars->delta[ring.slot][part * 32]);
+                tmem_wait_ld();
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t s[32];
-                    tmem_ld_x32(tmem + lanes + half * 64 + c * 32, s);
-                    tmem_wait_ld();
+                for (int k = 0; k < 32; k += 4) {
+                    const float4 l = lse[k / 4];
+                    s[k] = __float_as_uint(ex2(fmaf(__uint_as_float(s[k]), p.scale_log2, -l.x)));
+                    s[k + 1] = __float_as_uint(ex2(fmaf(__uint_as_float(s[k + 1]), p.scale_log2, -l.y)));
+                    s[k + 2] = __float_as_uint(ex2(fmaf(__uint_as_float(s[k + 2]), p.scale_log2, -l.z)));
+                    s[k + 3] = __float_as_uint(ex2(fmaf(__uint_as_float(s[k + 3]), p.scale_log2, -l.w)));
+                }
+                if (masked) {
 #pragma unroll
-                    for (int k = 0; k < 32; k += 2) {
-                        const float4 st = stat[(c * 32 + k) / 2];
-                        pr[c * 32 + k] = ex2(fmaf(__uint_as_float(s[k]), p.scale_log2, -st.x));
-                        pr[c * 32 + k + 1] = ex2(fmaf(__uint_as_float(s[k + 1]), p.scale_log2, -st.z));
-                    }
-                    if (masked) {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) if (c * 32 + k < from) pr[c * 32 + k] = 0.0f;
-                    }
+                    for (int k = 0; k < 32; ++k) if (k < from) s[k] = 0u;
                 }
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t e[16];
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) e[k] = pack_bf16(pr[c * 32 + 2 * k], pr[c * 32 + 2 * k + 1]);
-                    tmem_st_x16(tmem + lanes + half * 64 + c * 16, e);
-                }
+                for (int k = 0; k < 16; ++k) e[k] = pack_bf16(__uint_as_float(s[2 * k]), __uint_as_float(s[2 * k + 1]));
+                tmem_st_x16(s_addr, e);                      // over this quarter's own scores
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -580,25 +568,23 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->dp_full), uses & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t e[2][16];
+                tmem_ld_x32(dp_addr, dp);
+                tmem_wait_ld();
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t dp[32];
-                    tmem_ld_x32(tmem + lanes + 128 + half * 64 + c * 32, dp);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int k = 0; k < 32; k += 2) {
-                        const float4 st = stat[(c * 32 + k) / 2];
-                        float a = pr[c * 32 + k] * (__uint_as_float(dp[k]) - st.y), b = pr[c * 32 + k + 1] * (__uint_as_float(dp[k + 1]) - st.w);
-                        if (masked) {
-                            if (c * 32 + k < from) a = 0.0f;
-                            if (c * 32 + k + 1 < from) b = 0.0f;
-                        }
-                        e[c][k / 2] = pack_bf16(a, b);
-                    }
+                for (int k = 0; k < 32; k += 4) {
+                    const float4 d = delta[k / 4];
+                    dp[k] = __float_as_uint(__uint_as_float(s[k]) * (__uint_as_float(dp[k]) - d.x));
+                    dp[k + 1] = __float_as_uint(__uint_as_float(s[k + 1]) * (__uint_as_float(dp[k + 1]) - d.y));
+                    dp[k + 2] = __float_as_uint(__uint_as_float(s[k + 2]) * (__uint_as_float(dp[k + 2]) - d.z));
+                    dp[k + 3] = __float_as_uint(__uint_as_float(s[k + 3]) * (__uint_as_float(dp[k + 3]) - d.w));
                 }
-                tmem_st_x16(tmem + lanes + 128 + half * 64, e[0]);
-                tmem_st_x16(tmem + lanes + 128 + half * 64 + 16, e[1]);
+                if (masked) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) if (k < from) dp[k] = 0u;
+                }
+#pragma unroll
+                for (int k = 0; k < 16; ++k) e[k] = pack_bf16(__uint_as_float(dp[2 * k]), __uint_as_float(dp[2 * k + 1]));
+                tmem_st_x16(dp_addr, e);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -608,19 +594,20 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->done), done_uses++ & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
             if (!ok) break;
             tc_fence_after();
-            // the first group of warps has dv, the second dk
-            __nv_bfloat16* base = half ? p.dk : p.dv;
-            const int64_t ld = half ? p.ld_dk : p.ld_dv;
-            const float by = half ? p.scale : 1.0f;
+            // two groups of warps have dv, two dk: every other 32 columns each
+            const bool is_k = part >= 2;
+            __nv_bfloat16* base = is_k ? p.dk : p.dv;
+            const int64_t ld = is_k ? p.ld_dk : p.ld_dv;
+            const float by = is_k ? p.scale : 1.0f;
             const int row0 = w.t.at + (warp & 3) * 32;
             auto where = [&](int k) -> __nv_bfloat16* {
                 return row0 + k < w.t.len ? base + (int64_t)(w.t.t0 + row0 + k) * ld + (int64_t)w.kv * p.head_dim : nullptr;
             };
 #pragma unroll 1
-            for (int c = 0; c < p.head_dim; c += 32) {
+            for (int c = (part & 1) * 32; c < p.head_dim; c += 64) {
                 uint32_t o[32];
                 float f[32];
-                tmem_ld_x32(tmem + lanes + 256 + half * 128 + c, o);
+                tmem_ld_x32(tmem + lanes + 256 + (is_k ? 128 : 0) + c, o);
                 tmem_wait_ld();
 #pragma unroll
                 for (int k = 0; k < 32; ++k) f[k] = __uint_as_float(o[k]) * by;

@@ -7,9 +7,11 @@
 // values stay in the registers of the threads that share it (32 values a thread, as 16-byte vectors where rows are aligned, else element by
 // element with neighbouring lanes on neighbouring elements), and the moments are taken from them in two steps, mean and then squares
 // of the differences, so that a mean far from zero costs no digits. 32, 128, 256 or 512 threads share a row: the fewest that hold it.
-// dw and db: blocks that walk over the rows keep their columns' sums in registers and leave one row of fp32 sums each, which a second
-// kernel adds in a fixed order (no atomics: the same inputs give the same bits).
+// dw and db: workers that walk over the rows keep their columns' sums in registers and leave one row of fp32 sums each, which a second
+// kernel adds in a fixed order (no atomics: the same inputs give the same bits). With the sums there is no room to hold rows ahead in
+// registers, and few warps an SM: aligned rows of up to 8192 values come through a ring in shared memory (norm_backward_ring_kernel).
 #include "qless_kernels.h"
+#include "tc_common.cuh"
 
 namespace qless {
 
@@ -242,6 +244,133 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormParams p
     }
 }
 
+// The same with the sums, rows brought ahead by bulk copies: every worker has a ring of `stages` places of a row of x and one of dy. A row is read
+// from its place twice (for the two means, then for dx); the place is filled again behind the barrier of the next row's means, when every
+// thread of the worker has left it.
+struct RingParams {
+    NormParams n;
+    int32_t stages, row_bytes;
+    unsigned int* timeout_word;
+};
+
+struct __align__(128) RingBars {
+    uint64_t full[8][8];                    // [worker of the block][place]
+    float room[8][2][8][2];                 // [worker][turn][warp][mean]
+    uint32_t abort_flag;
+};
+
+template <typename T, typename P>
+__global__ void __launch_bounds__(256, 2) norm_backward_ring_kernel(const RingParams q)
+{
+    using namespace tc;
+    constexpr int V = Elem<T>::VEC;
+    extern __shared__ __align__(128) uint8_t smem[];
+    RingBars* bars = reinterpret_cast<RingBars*>(smem);
+    auto& full = bars->full;
+    auto& room = bars->room;
+    const NormParams& p = q.n;
+    const int share = p.share, rank = threadIdx.x % share, mine = threadIdx.x / share, per = 256 / share;
+    const int lane = threadIdx.x & 31, warp_of = rank >> 5, warps = share >> 5;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < per; ++i) for (int s = 0; s < q.stages; ++s) mbar_init(smem_u32(&full[i][s]), 1);
+        bars->abort_flag = 0;
+        fence_barrier_init();
+    }
+    __syncthreads();
+    ahead_wait();
+    ahead_release();
+    const int64_t worker = (int64_t)blockIdx.x * per + mine, workers = (int64_t)gridDim.x * per;
+    uint8_t* ring = smem + sizeof(RingBars) + (size_t)mine * q.stages * 2 * q.row_bytes;
+    auto bring = [&](int64_t t, int place) {                 // one thread
+        const uint32_t bar = smem_u32(&full[mine][place]), dst = smem_u32(ring + (size_t)place * 2 * q.row_bytes);
+        mbar_arrive_expect_tx(bar, 2 * q.row_bytes);
+        bulk_load(dst, reinterpret_cast<const T*>(p.x) + t * p.ld_x, q.row_bytes, bar);
+        bulk_load(dst + q.row_bytes, reinterpret_cast<const T*>(p.dy) + t * p.ld_dy, q.row_bytes, bar);
+    };
+    if (rank == 0)
+        for (int s = 0; s < q.stages && worker + s * workers < p.tokens; ++s) bring(worker + s * workers, s);
+    const float inv = 1.0f / (float)p.width;
+    float sw[VALUES], sb[VALUES];
+#pragma unroll
+    for (int k = 0; k < VALUES; ++k) sw[k] = sb[k] = 0.0f;
+    int place = 0, turn = 0;
+    uint32_t parity = 0;
+    bool there = true;                                       // a copy that did not come within the wait's limit: nothing is waited for any more
+    for (int64_t t = worker; t < p.tokens; t += workers) {
+        const float mu = p.mean != nullptr ? p.mean[t] : 0.0f, r = p.rstd[t];
+        if (there) there = mbar_wait(smem_u32(&full[mine][place]), parity, &bars->abort_flag, q.timeout_word, TO_PRODUCER);
+        const uint8_t* xs = ring + (size_t)place * 2 * q.row_bytes;
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int n = 0; n < VALUES / V; ++n) {
+            const int c = (n * share + rank) * V;
+            if (c >= p.width) break;
+            float x[V], g[V], w[V];
+            Elem<T>::unpack(*reinterpret_cast<const uint4*>(xs + c * sizeof(T)), x);
+            Elem<T>::unpack(*reinterpret_cast<const uint4*>(xs + q.row_bytes + c * sizeof(T)), g);
+            load_params<P, V>(reinterpret_cast<const P*>(p.weight), c, w);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float xh = (x[e] - mu) * r;
+                sw[n * V + e] = fmaf(g[e], xh, sw[n * V + e]);
+                sb[n * V + e] += g[e];
+                g[e] *= w[e];
+                s[0] += g[e];
+                s[1] = fmaf(g[e], xh, s[1]);
+            }
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) { s[0] += __shfl_xor_sync(0xFFFFFFFFu, s[0], d); s[1] += __shfl_xor_sync(0xFFFFFFFFu, s[1], d); }
+        if (warps > 1) {
+            if (lane == 0) { room[mine][turn][warp_of][0] = s[0]; room[mine][turn][warp_of][1] = s[1]; }
+            asm volatile("bar.sync %0, %1;" ::"r"(mine + 1), "r"(share) : "memory");
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {                    // (in row_sum's order: dx is the same with and without the sums)
+                s[k] = lane < warps ? room[mine][turn][lane][k] : 0.0f;
+#pragma unroll
+                for (int d = 16; d > 0; d >>= 1) s[k] += __shfl_xor_sync(0xFFFFFFFFu, s[k], d);
+            }
+            turn ^= 1;
+        } else {
+            __syncwarp();
+        }
+        // every thread of the worker has left the row before: its place takes the row that is `stages` behind it
+        if (rank == 0 && t > worker) {
+            const int64_t next = t + (int64_t)(q.stages - 1) * workers;
+            if (next < p.tokens && there) bring(next, place == 0 ? q.stages - 1 : place - 1);
+        }
+        const float m = p.center ? s[0] * inv : 0.0f, along = s[1] * inv;
+        T* out = reinterpret_cast<T*>(p.out) + t * p.ld_out;
+#pragma unroll
+        for (int n = 0; n < VALUES / V; ++n) {
+            const int c = (n * share + rank) * V;
+            if (c >= p.width) break;
+            float x[V], g[V], w[V];
+            Elem<T>::unpack(*reinterpret_cast<const uint4*>(xs + c * sizeof(T)), x);
+            Elem<T>::unpack(*reinterpret_cast<const uint4*>(xs + q.row_bytes + c * sizeof(T)), g);
+            load_params<P, V>(reinterpret_cast<const P*>(p.weight), c, w);
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] = (__fmul_rn(g[e], w[e]) - m - __fmul_rn(x[e] - mu, r) * along) * r;
+            store_vec<T, V>(out + c, x);
+        }
+        if (++place == q.stages) { place = 0; parity ^= 1u; }
+    }
+    float* dst = p.part + worker * 2 * p.width;
+#pragma unroll
+    for (int n = 0; n < VALUES / V; ++n) {
+        const int c = (n * share + rank) * V;
+        if (c >= p.width) break;
+#pragma unroll
+        for (int e = 0; e < V; e += 4) {
+            *reinterpret_cast<float4*>(dst + c + e) = make_float4(sw[n * V + e], sw[n * V + e + 1], sw[n * V + e + 2], sw[n * V + e + 3]);
+            *reinterpret_cast<float4*>(dst + p.width + c + e) = make_float4(sb[n * V + e], sb[n * V + e + 1], sb[n * V + e + 2], sb[n * V + e + 3]);
+        }
+    }
+    // behind a wait that gave up: what is still on its way arrives before the block leaves
+    if (!there && rank == 0)
+        for (int s = 0; s < q.stages; ++s) mbar_wait_quiet(smem_u32(&full[mine][s]), 0u, 1u << 14);
+}
+
 // dw and db from the workers' sums: a block has 32 columns (of dw, then of db), its 32 warps every 32nd worker each, joined in order.
 template <typename P>
 __global__ void __launch_bounds__(1024) norm_join_kernel(const float* __restrict__ part, int64_t workers, int32_t width, P* dw, P* db)
@@ -271,19 +400,29 @@ bool vectors(const void* p, int64_t ld, int elem)
 
 }  // namespace
 
-NormPlan plan_norm(int64_t tokens, int32_t width, bool sums)
+NormPlan plan_norm(int64_t tokens, int32_t width, int32_t elem, bool sums)
 {
     NormPlan pl;
     pl.share = width <= 32 * VALUES ? 32 : width <= 128 * VALUES ? 128 : width <= 256 * VALUES ? 256 : 512;
-    pl.block = pl.share < ROOM_BLOCK ? ROOM_BLOCK : pl.share;
-    if (pl.share == 128) pl.block = 128;                     // a block's barriers are for one row
-    const int per = pl.block / pl.share;
-    const int64_t blocks = (tokens + per - 1) / per;
-    // Workers that keep sums: as many as are resident (a thread needs up to 128 registers).
-    const int64_t most = (int64_t)sm_count() * (pl.block == 128 ? 4 : pl.block == 256 ? 2 : 1);
-    pl.blocks = sums && blocks > most ? most : blocks;
-    pl.workers = pl.blocks * per;
-    pl.total = sums ? align_up((size_t)pl.workers * 2 * width * 4, 256) + 256 : 256;
+    pl.block = pl.share > ROOM_BLOCK ? pl.share : ROOM_BLOCK;
+    if (pl.share == 128 && !sums) pl.block = 128;            // (the barriers of the plain kernels are a block's)
+    const int64_t per = pl.block / pl.share, all = (tokens + per - 1) / per, sms = sm_count();
+    pl.blocks = all;
+    pl.workers = pl.ring_workers = all * per;
+    pl.ring_stages = 0;
+    pl.total = 256;
+    if (!sums) return pl;
+    // Two blocks an SM with some 96 KiB of rows on their way each.
+    const int64_t stages = (96 << 10) / (per * 2 * width * (int64_t)elem);
+    pl.ring_stages = (int32_t)(stages > 8 ? 8 : stages);
+    pl.ring_workers = (all < 2 * sms ? all : 2 * sms) * per;
+    // without the ring: as many blocks as are resident
+    if (pl.share == 128) { pl.block = 128; pl.blocks = tokens; }
+    const int64_t most = sms * (pl.block == 128 ? 3 : 1);
+    if (pl.blocks > most) pl.blocks = most;
+    pl.workers = pl.blocks * (pl.block / pl.share);
+    const int64_t rows = pl.workers > pl.ring_workers ? pl.workers : pl.ring_workers;
+    pl.total = align_up((size_t)rows * 2 * width * 4, 256) + 256;
     return pl;
 }
 
@@ -314,8 +453,8 @@ static cudaError_t backward_of(const NormPlan& pl, const NormParams& p, bool vec
 
 qless_status launch_norm_forward(const NormArgs& a, cudaStream_t st)
 {
-    const NormPlan pl = plan_norm(a.tokens, a.width, false);
     const int es = a.dtype == QLESS_F32 ? 4 : 2, vec = 16 / es;
+    const NormPlan pl = plan_norm(a.tokens, a.width, es, false);
     const bool whole = a.width % vec == 0 && vectors(a.x, a.ld_x, es) && vectors(a.out, a.ld_out, es) && vectors(a.weight, 0, 1) &&
                        (a.bias == nullptr || vectors(a.bias, 0, 1));
     NormParams p{};
@@ -333,17 +472,38 @@ qless_status launch_norm_forward(const NormArgs& a, cudaStream_t st)
     return QLESS_OK;
 }
 
-qless_status launch_norm_backward(const NormArgs& a, uint8_t* ws, cudaStream_t st)
+template <typename T, typename P>
+static cudaError_t ring_of(const NormPlan& pl, const RingParams& q, cudaStream_t st)
+{
+    const cudaError_t e = allow_full_smem<norm_backward_ring_kernel<T, P>>();
+    if (e != cudaSuccess) return e;
+    const size_t smem = sizeof(RingBars) + (size_t)(256 / pl.share) * pl.ring_stages * 2 * q.row_bytes;
+    return launch_ahead(norm_backward_ring_kernel<T, P>, dim3((unsigned)(pl.ring_workers / (256 / pl.share))), dim3(256), smem, st, q);
+}
+
+qless_status launch_norm_backward(const NormArgs& a, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st)
 {
     const bool sums = a.grad_weight != nullptr || a.grad_bias != nullptr;
-    const NormPlan pl = plan_norm(a.tokens, a.width, sums);
     const int es = a.dtype == QLESS_F32 ? 4 : 2, vec = 16 / es;
+    const NormPlan pl = plan_norm(a.tokens, a.width, es, sums);
     const bool whole = a.width % vec == 0 && vectors(a.x, a.ld_x, es) && vectors(a.dy, a.ld_dy, es) && vectors(a.out, a.ld_out, es) && vectors(a.weight, 0, 1);
     NormParams p{};
     p.x = a.x; p.dy = a.dy; p.weight = a.weight; p.out = a.out; p.mean = a.center ? a.mean : nullptr; p.rstd = a.rstd; p.part = reinterpret_cast<float*>(ws);
     p.tokens = a.tokens; p.ld_x = a.ld_x; p.ld_dy = a.ld_dy; p.ld_out = a.ld_out; p.width = a.width; p.share = pl.share; p.center = a.center;
+    const bool ring = sums && whole && pl.share <= 256 && pl.ring_stages >= 2;
+    const int64_t workers = ring ? pl.ring_workers : pl.workers;
     { ProfileScope ps("layer_norm_backward", st);
-      if (a.dtype == QLESS_F32) {
+      if (ring) {
+          RingParams q{};
+          q.n = p; q.stages = pl.ring_stages; q.row_bytes = a.width * es; q.timeout_word = timeout_word;
+          if (a.dtype == QLESS_F32) {
+              if (a.param_dtype == QLESS_F32) QLESS_CUDA_TRY((ring_of<float, float>(pl, q, st)));
+              else QLESS_CUDA_TRY((ring_of<float, __nv_bfloat16>(pl, q, st)));
+          } else {
+              if (a.param_dtype == QLESS_F32) QLESS_CUDA_TRY((ring_of<__nv_bfloat16, float>(pl, q, st)));
+              else QLESS_CUDA_TRY((ring_of<__nv_bfloat16, __nv_bfloat16>(pl, q, st)));
+          }
+      } else if (a.dtype == QLESS_F32) {
           if (a.param_dtype == QLESS_F32) QLESS_CUDA_TRY((backward_of<float, float>(pl, p, whole, sums, st)));
           else QLESS_CUDA_TRY((backward_of<float, __nv_bfloat16>(pl, p, whole, sums, st)));
       } else {
@@ -356,10 +516,10 @@ qless_status launch_norm_backward(const NormArgs& a, uint8_t* ws, cudaStream_t s
         const dim3 grid((unsigned)(2 * ((a.width + 31) / 32)));
         const float* part = p.part;
         if (a.param_dtype == QLESS_F32)
-            QLESS_CUDA_TRY(launch_ahead(norm_join_kernel<float>, grid, dim3(1024), 0, st, part, pl.workers, a.width, reinterpret_cast<float*>(a.grad_weight),
+            QLESS_CUDA_TRY(launch_ahead(norm_join_kernel<float>, grid, dim3(1024), 0, st, part, workers, a.width, reinterpret_cast<float*>(a.grad_weight),
                                         reinterpret_cast<float*>(a.grad_bias)));
         else
-            QLESS_CUDA_TRY(launch_ahead(norm_join_kernel<__nv_bfloat16>, grid, dim3(1024), 0, st, part, pl.workers, a.width,
+            QLESS_CUDA_TRY(launch_ahead(norm_join_kernel<__nv_bfloat16>, grid, dim3(1024), 0, st, part, workers, a.width,
                                         reinterpret_cast<__nv_bfloat16*>(a.grad_weight), reinterpret_cast<__nv_bfloat16*>(a.grad_bias)));
         count_launches(1);
     }

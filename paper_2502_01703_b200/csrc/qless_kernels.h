@@ -132,8 +132,8 @@ struct LossArgs {
 qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st);
 
 // Layer normalisation (layer_norm.cu).
-struct NormPlan { int32_t share, block; int64_t blocks, workers; size_t total; };
-NormPlan plan_norm(int64_t tokens, int32_t width, bool sums);
+struct NormPlan { int32_t share, block, ring_stages; int64_t blocks, workers, ring_workers; size_t total; };      // elem: bytes of a value
+NormPlan plan_norm(int64_t tokens, int32_t width, int32_t elem, bool sums);
 struct NormArgs {
     const void* x; const void* dy; const void* weight; const void* bias;
     void* out; float* mean; float* rstd; void* grad_weight; void* grad_bias;
@@ -143,7 +143,7 @@ struct NormArgs {
     float eps;
 };
 qless_status launch_norm_forward(const NormArgs& a, cudaStream_t st);
-qless_status launch_norm_backward(const NormArgs& a, uint8_t* ws, cudaStream_t st);
+qless_status launch_norm_backward(const NormArgs& a, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st);
 
 // Causal attention over packed sequences (attention.cu, attention_backward.cu).
 struct AttnTile { int32_t t0, len, at, unused; };       // a sequence's first token and length, and the tile's first token within it
