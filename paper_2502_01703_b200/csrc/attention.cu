@@ -4,11 +4,11 @@
 //   lse_i = m_i + log sum_j e^(s_ij - m_i)
 //
 // One pass over the keys per tile of queries; scores never leave the SM. A block works on two tiles of 128 query rows that share the copies of
-// keys and values: while one tile's group of four warps takes exponentials, the tensor core works on the other's products.
+// keys and values: while one tile's eight warps take exponentials, the tensor core works on the other's products.
 //   warp 0        TMA: queries of a tile once, keys and values through a ring of tiles
 //   warp 1        tcgen05: S = Q K^T (both from shared memory), O += P V (P from tensor memory, V as rows of tokens)
-//   warps 4-7     tile 0: a thread owns a row: maximum, exponentials in fp32, P rounded to bf16 over S in tensor memory
-//   warps 8-11    tile 1
+//   warps 4-11    tile 0: two threads share a row, half of the keys each: maximum, exponentials in fp32, P rounded to bf16 over S in tensor memory
+//   warps 12-19   tile 1
 // Tensor memory: S (or P) and O of both tiles, 4 x 128 columns. Running maximum: O and the sum are rescaled only when the maximum has grown by
 // more than 2^8 since the reference was taken (e^(s - r) then stays below 2^8: neither fp32 sums nor bf16's relative rounding mind).
 // P is rounded to bf16 (2^-9 of each probability, independent of each other; the sum is that of the unrounded ones), O and the sums are fp32.
@@ -24,21 +24,24 @@ namespace attn {
 
 namespace {
 
-constexpr int NTHREADS = 384, MAX_STAGES = 10;
+constexpr int NTHREADS = 640, MAX_STAGES = 10;
 constexpr float SLACK = 8.0f;               // powers of two that the maximum may grow before O is rescaled
+constexpr int SHARE = 3;                    // one in so many pairs of exponentials on the fp32 units
 
 struct ForwardParams {
     TileTable table;
     __nv_bfloat16* out; float* lse;
     int64_t ld_out;
-    int32_t packs, pack, group, heads, head_dim, stages;      // packs: tiles' heads, heads / pack
-    int64_t items;
+    uint32_t items, packs;                  // packs: heads / pack
+    int32_t pack, pack_shift, group, heads, head_dim, stages;
     float scale_log2;
     unsigned int* timeout_word;
 };
 
 struct __align__(8) Bars {
-    uint64_t q_full[2], q_empty[2], full[MAX_STAGES], empty[MAX_STAGES], s_full[2], p_ready[2], o_full[2], drain;
+    uint64_t q_full[2], q_empty[2], full[MAX_STAGES], empty[MAX_STAGES], s_full[2], p_ready[2][2], o_full[2], drain;      // P in two halves of the keys
+    uint64_t met[2][4];                     // the two warps of 32 rows have put down what the other needs
+    float swap[2][2][2][TILE];              // [turn][tile][half of the keys]: maxima, and sums at the end
     uint32_t tmem_base, abort_flag;
 };
 
@@ -56,13 +59,15 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     const uint32_t nS = (uint32_t)p.stages;
     Bars* bars = reinterpret_cast<Bars*>(ring_smem + (size_t)nS * OP);
     volatile uint32_t* abort_flag = &bars->abort_flag;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int tok = TILE / p.pack;                           // tokens of a 128-row tile
+    const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int tok = TILE >> p.pack_shift;                           // tokens of a 128-row tile
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&bars->q_full[i]), 1); mbar_init(smem_u32(&bars->q_empty[i]), 1);
-            mbar_init(smem_u32(&bars->s_full[i]), 1); mbar_init(smem_u32(&bars->p_ready[i]), 4); mbar_init(smem_u32(&bars->o_full[i]), 1);
+            mbar_init(smem_u32(&bars->s_full[i]), 1); mbar_init(smem_u32(&bars->p_ready[i][0]), 8); mbar_init(smem_u32(&bars->p_ready[i][1]), 4);
+            for (int k = 0; k < 4; ++k) mbar_init(smem_u32(&bars->met[i][k]), 2);
+            mbar_init(smem_u32(&bars->o_full[i]), 1);
         }
         for (uint32_t i = 0; i < MAX_STAGES; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), 1); }
         mbar_init(smem_u32(&bars->drain), 1);
@@ -84,11 +89,11 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     };
     // item -> tile, first head, key head; loops of the two row tiles over the keys (0: the second one does not exist)
     struct Work { AttnTile t; int head0, kv, n[2]; };
-    auto work_of = [&](int64_t item) {
+    auto work_of = [&](uint32_t item) {
         Work w;
-        const int i = (int)(item / p.packs), c = (int)(item - (int64_t)i * p.packs);
+        const uint32_t i = item / p.packs, c = item - i * p.packs;
         w.t = tile_at(p.table, i);
-        w.head0 = c * p.pack; w.kv = w.head0 / p.group;
+        w.head0 = (int)c * p.pack; w.kv = w.head0 / p.group;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const int first = w.t.at + x * tok;
@@ -98,7 +103,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     };
 
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 0) {
             Ring ring;
             uint32_t it = 0, q_uses[2] = {0, 0};
@@ -114,7 +119,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 __syncwarp();
                 ring.next(nS); ++it;
             };
-            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round) {
                 const Work w = work_of(item);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
@@ -150,19 +155,21 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             auto scores = [&](int x, const uint8_t* k_op) {
                 if (elect_one()) {
                     const uint64_t a = make_smem_desc_sw128(smem_u32(q_smem + x * OP)), b = make_smem_desc_sw128(smem_u32(k_op));
-                    for (uint32_t k = 0; k < steps; ++k) {
+#pragma unroll
+                    for (uint32_t k = 0; k < 4 * DB; ++k) {
                         const uint64_t off = (uint64_t)((k >> 2) * 1024 + (k & 3) * 2);
-                        mma_f16_ss(tmem + x * 128, a + off, b + off, idesc_s, k > 0);
+                        if (k < steps) mma_f16_ss(tmem + x * 128, a + off, b + off, idesc_s, k > 0);
                     }
                     mma_commit(smem_u32(&bars->s_full[x]));
                 }
                 __syncwarp();
             };
-            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round) {
                 const Work w = work_of(item);
                 const int n = max(w.n[0], w.n[1]);
                 if (!warp_wait(&bars->full[ring.slot], ring.parity, TO_MMA)) { ok = false; break; }
                 tc_fence_after();
+#pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     if (w.n[x] == 0) continue;
                     if (!warp_wait(&bars->q_full[x], q_uses[x]++ & 1u, TO_MMA)) { ok = false; break; }
@@ -184,17 +191,23 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                     if (!warp_wait(&bars->full[v.slot], v.parity, TO_MMA)) { ok = false; break; }
                     if (w.t.len - j * TILE < TILE) zero_rows(v_op, DB, w.t.len - j * TILE, lane);
                     if (j + 1 < n && !warp_wait(&bars->full[k.slot], k.parity, TO_MMA)) { ok = false; break; }
+#pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         if (j >= w.n[x]) continue;
-                        if (!warp_wait(&bars->p_ready[x], p_uses[x]++ & 1u, TO_MMA)) { ok = false; break; }
-                        tc_fence_after();
-                        if (elect_one()) {
-                            const uint64_t b = make_smem_desc_mn_sw128(smem_u32(v_op), 16384);
 #pragma unroll
-                            for (int s = 0; s < 8; ++s) mma_f16_ts(tmem + 256 + x * 128, tmem + x * 128 + s * 8, b + (uint64_t)(s * 128), idesc_o, j > 0 || s > 0);
-                            if (j + 1 == w.n[x]) mma_commit(smem_u32(&bars->o_full[x]));
+                        for (int half = 0; half < 2; ++half) {
+                            if (!warp_wait(&bars->p_ready[x][half], p_uses[x] & 1u, TO_MMA)) { ok = false; break; }
+                            tc_fence_after();
+                            if (elect_one()) {
+                                const uint64_t b = make_smem_desc_mn_sw128(smem_u32(v_op), 16384);
+#pragma unroll
+                                for (int s = half * 4; s < half * 4 + 4; ++s) mma_f16_ts(tmem + 256 + x * 128, tmem + x * 128 + half * 64 + (s & 3) * 8, b + (uint64_t)(s * 128), idesc_o, j > 0 || s > 0);
+                                if (half == 1 && j + 1 == w.n[x]) mma_commit(smem_u32(&bars->o_full[x]));
+                            }
+                            __syncwarp();
                         }
-                        __syncwarp();
+                        if (!ok) break;
+                        ++p_uses[x];
                         if (j + 1 < w.n[x]) {
                             scores(x, ring_smem + (size_t)k.slot * OP);
                             if (j + 2 == w.n[x] && elect_one()) mma_commit(smem_u32(&bars->q_empty[x]));
@@ -214,15 +227,28 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             mbar_wait_quiet(smem_u32(&bars->drain), 0u);
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-        const int x = warp >= 8 ? 1 : 0, r = (warp & 3) * 32 + lane;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_addr = tmem + lanes + x * 128, o_addr = tmem + lanes + 256 + x * 128;
-        const int my_tok = r / p.pack, my_head = r % p.pack;
-        uint32_t s_uses = 0, o_uses = 0;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        const int group = (warp >> 2) - 1, x = group >> 1, half = group & 1, q = warp & 3, r = q * 32 + lane;
+        const uint32_t lanes = (uint32_t)(q * 32) << 16, s_addr = tmem + lanes + x * 128 + half * 64, o_addr = tmem + lanes + 256 + x * 128 + half * (DB * 32);
+        const int my_tok = r >> p.pack_shift, my_head = r & (p.pack - 1);
+        const uint64_t scale2 = pair_of(p.scale_log2, p.scale_log2);
+        uint32_t s_uses = 0, o_uses = 0, met_uses = 0;
         bool ok = true;
-        for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+        // The two warps of 32 rows exchange a number for each row (through an mbarrier, whose waits end). A place is written again two exchanges later: by
+        // then the other warp has arrived for the one between, behind its reading of this one.
+        auto other = [&](float mine, float& its) -> bool {
+            const uint32_t turn = met_uses & 1u;
+            bars->swap[turn][x][half][r] = mine;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars->met[x][q]));
+            const bool met = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->met[x][q]), turn, abort_flag, p.timeout_word, TO_EPILOGUE));
+            ++met_uses;
+            its = bars->swap[turn][x][half ^ 1][r];
+            return met;
+        };
+        for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round) {
             const Work w = work_of(item);
-            const int n = w.n[x];
+            const int n = x ? w.n[1] : w.n[0];
             if (n == 0) continue;
             const int first = w.t.at + x * tok, at = first + my_tok;      // this row's token within its sequence
             float ref = -INFINITY, sum = 0.0f;               // reference of the exponents (times scale, in powers of two)
@@ -230,81 +256,109 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->s_full[x]), s_uses++ & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t s[4][32];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld_x32(s_addr + c * 32, s[c]);
+                uint32_t s[2][32];
+                float top2[2];
+                const bool masked = j * TILE + TILE - 1 > first;      // keys behind the tile's first token: some row does not see all of them
+                const int lim = at - j * TILE - half * 64;   // this row's last key among the 64
+                tmem_ld_x32(s_addr, s[0]);
                 tmem_wait_ld();
-                if (j * TILE + TILE - 1 > first) {           // keys behind the tile's first token: some row does not see all of them
-                    const int lim = at - j * TILE;           // its last key here
+                tmem_ld_x32(s_addr + 32, s[1]);              // on its way while the first half's maximum is taken
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                for (int c = 0; c < 2; ++c) {
+                    if (c == 1) tmem_wait_ld();
+                    if (masked) {
 #pragma unroll
                         for (int k = 0; k < 32; ++k) if (c * 32 + k > lim) s[c][k] = 0xFF800000u;
+                    }
+                    float t[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        t[h] = max3(__uint_as_float(s[c][h * 16]), __uint_as_float(s[c][h * 16 + 1]), __uint_as_float(s[c][h * 16 + 2]));
+#pragma unroll
+                        for (int k = 3; k + 1 < 16; k += 2) t[h] = max3(t[h], __uint_as_float(s[c][h * 16 + k]), __uint_as_float(s[c][h * 16 + k + 1]));
+                    }
+                    top2[c] = max3(max3(t[0], t[1], __uint_as_float(s[c][15])), __uint_as_float(s[c][31]), __uint_as_float(s[c][31]));
                 }
-                float top4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int k = 0; k < 32; ++k)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) top4[c] = fmaxf(top4[c], __uint_as_float(s[c][k]));
-                const float top = fmaxf(fmaxf(top4[0], top4[1]), fmaxf(top4[2], top4[3])) * p.scale_log2;
+                const float mine = max3(top2[0], top2[1], top2[1]);
+                float its;
+                ok = other(mine, its);
+                if (!ok) break;
+                const float top = max3(mine, its, its) * p.scale_log2;
                 float by = 1.0f;
-                if (top > ref + SLACK || ref == -INFINITY) {
-                    if (top > -INFINITY) {
+                if (!(top <= ref + SLACK)) {                 // (also where top is NaN: the whole row is from here on)
+                    if (top != -INFINITY) {
                         by = ref == -INFINITY ? 0.0f : ex2(ref - top);
                         ref = top;
                     }
                 }
                 if (j > 0 && __any_sync(0xFFFFFFFFu, by != 1.0f)) {      // the products so far are complete: S was issued behind them
 #pragma unroll 1
-                    for (int c = 0; c < DB * 64; c += 32) {
-                        uint32_t o[32];
-                        tmem_ld_x32(o_addr + c, o);
+                    for (int c = 0; c < DB * 32; c += 16) {
+                        uint32_t o[16];
+                        tmem_ld_x16(o_addr + c, o);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(by == 0.0f ? 0.0f : __uint_as_float(o[k]) * by);
-                        tmem_st_x32(o_addr + c, o);
+                        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(by == 0.0f ? 0.0f : __uint_as_float(o[k]) * by);
+                        tmem_st_x16(o_addr + c, o);
                     }
                     sum *= by;
+                    tmem_wait_st();
+                    tc_fence_before();
                 }
-                const float off = ref > -INFINITY ? ref : 0.0f;
-                float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (half == 1) {                             // the first products of P may begin when both halves of O are as they have to be
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&bars->p_ready[x][0]));
+                }
+                const float off = ref == -INFINITY ? 0.0f : ref;
+                const uint64_t off2 = pair_of(-off, -off);
+                uint64_t part[2] = {0, 0};
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    uint32_t e[16];
+                    uint32_t e[8];
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) {
-                        const float a = ex2(fmaf(__uint_as_float(s[c][2 * k]), p.scale_log2, -off)), b = ex2(fmaf(__uint_as_float(s[c][2 * k + 1]), p.scale_log2, -off));
-                        part[(2 * k) & 3] += a; part[(2 * k + 1) & 3] += b;
-                        e[k] = pack_bf16(a, b);
+                    for (int k = 0; k < 8; ++k) {
+                        const int i = c * 8 + k;
+                        const uint64_t x2 = fma2(pair_of(__uint_as_float(s[i >> 4][(2 * i) & 31]), __uint_as_float(s[i >> 4][(2 * i + 1) & 31])), scale2, off2);
+                        const uint64_t y2 = ex2_of<SHARE>(x2, i);
+                        part[k & 1] = add2(part[k & 1], y2);
+                        e[k] = pack_pair(y2);
                     }
-                    tmem_st_x16(s_addr + c * 16, e);
+                    tmem_st_x8(s_addr + c * 8, e);           // over this half's own scores
                 }
-                sum += (part[0] + part[1]) + (part[2] + part[3]);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bars->p_ready[x]));
+                if (lane == 0) mbar_arrive(smem_u32(&bars->p_ready[x][half]));
+                float pa, pb;
+                split_pair(add2(part[0], part[1]), pa, pb);
+                sum += pa + pb;
             }
             if (!ok) break;
+            float its;
+            ok = other(sum, its);
+            if (!ok) break;
+            sum = half ? its + sum : sum + its;
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->o_full[x]), o_uses++ & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
             if (!ok) break;
             tc_fence_after();
             const float inv = 1.0f / sum;
-            if (p.lse != nullptr && at < w.t.len) p.lse[(int64_t)(w.t.t0 + at) * p.heads + w.head0 + my_head] = (ref + log2f(sum)) * LN2;
-            const int row0 = (warp & 3) * 32;
-            auto where = [&](int i) -> __nv_bfloat16* {
-                const int rr = row0 + i, a = first + rr / p.pack;
-                return a < w.t.len ? p.out + (int64_t)(w.t.t0 + a) * p.ld_out + (int64_t)(w.head0 + rr % p.pack) * p.head_dim : nullptr;
-            };
-#pragma unroll 1
-            for (int c = 0; c < p.head_dim; c += 32) {
+            if (half == 0 && p.lse != nullptr && at < w.t.len) p.lse[(int64_t)(w.t.t0 + at) * p.heads + w.head0 + my_head] = (ref + log2f(sum)) * LN2;
+            __nv_bfloat16* dst[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int rr = q * 32 + (lane & ~3) + k, a = first + (rr >> p.pack_shift);
+                dst[k] = a < w.t.len ? p.out + (int64_t)(w.t.t0 + a) * p.ld_out + (int64_t)(w.head0 + (rr & (p.pack - 1))) * p.head_dim : nullptr;
+            }
+#pragma unroll
+            for (int c = 0; c < DB * 32; c += 32) {
+                if (half * (DB * 32) + c >= p.head_dim) break;
                 uint32_t o[32];
                 float f[32];
                 tmem_ld_x32(o_addr + c, o);
                 tmem_wait_ld();
 #pragma unroll
                 for (int k = 0; k < 32; ++k) f[k] = __uint_as_float(o[k]) * inv;
-                store_rows32(f, c, p.head_dim, lane, where);
+                store_rows32(f, half * (DB * 32) + c, p.head_dim, lane, dst);
             }
             tc_fence_before();                               // (read before the next tile's products, which wait for its P)
         }
@@ -397,6 +451,8 @@ qless_status head_map(CUtensorMap* out, const void* base, int64_t ld, int32_t he
 
 using namespace attn;
 
+static int32_t pack_shift(int32_t pack) { return pack <= 1 ? 0 : 1 + pack_shift(pack / 2); }
+
 int32_t attn_pack(int32_t heads, int32_t kv_heads)
 {
     const int32_t group = heads / kv_heads;
@@ -437,8 +493,9 @@ qless_status launch_attention(const AttnArgs& a, uint8_t* ws, unsigned int* time
     if ((s = head_map(&k, a.k, a.ld_k, a.kv_heads, a.head_dim, a.tokens, 1, TILE)) != QLESS_OK) return s;
     if ((s = head_map(&v, a.v, a.ld_v, a.kv_heads, a.head_dim, a.tokens, 1, TILE)) != QLESS_OK) return s;
     p.out = reinterpret_cast<__nv_bfloat16*>(a.out); p.lse = a.lse; p.ld_out = a.ld_out;
-    p.packs = packs; p.pack = pack; p.group = a.heads / a.kv_heads; p.heads = a.heads; p.head_dim = a.head_dim;
-    p.items = (int64_t)tiles.size() * packs; p.scale_log2 = a.scale * LOG2E; p.timeout_word = timeout_word;
+    p.packs = packs; p.pack = pack; p.pack_shift = pack_shift(pack); p.group = a.heads / a.kv_heads; p.heads = a.heads; p.head_dim = a.head_dim;
+    QLESS_REQUIRE((int64_t)tiles.size() * packs < MOST_ITEMS - 65536, QLESS_ERR_UNSUPPORTED, "too many tiles: %zu of %d heads", tiles.size(), packs);
+    p.items = (uint32_t)(tiles.size() * packs); p.scale_log2 = a.scale * LOG2E; p.timeout_word = timeout_word;
     return a.head_dim <= 64 ? launch_forward<1>(a, q, k, v, p, st) : launch_forward<2>(a, q, k, v, p, st);
 }
 

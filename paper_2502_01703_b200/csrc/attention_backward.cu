@@ -26,7 +26,8 @@ using namespace attn;
 
 namespace {
 
-constexpr int NTHREADS = 640, MAX_STAGES = 10;
+constexpr int NTHREADS = 640;
+constexpr int SHARE = 3;                    // one in so many pairs of exponentials on the fp32 units
 
 // Columns of step s (16 rows of the contraction) of a left operand in tensor memory that four groups of warps wrote, each over the first half of its own 32 columns.
 __device__ __forceinline__ constexpr uint32_t quarter_column(int s) { return (uint32_t)((s >> 1) * 32 + (s & 1) * 8); }
@@ -37,18 +38,25 @@ struct QueryParams {
     const float* lse; float* delta;
     __nv_bfloat16* dq;
     int64_t ld_out, ld_dout, ld_dq;
-    int32_t packs, pack, group, heads, head_dim, stages;
-    int64_t items;
+    uint32_t items, packs;
+    int32_t pack, pack_shift, group, heads, head_dim;
     float scale, scale_log2;
     unsigned int* timeout_word;
 };
 
-struct __align__(8) QueryBars {
-    uint64_t q_full, q_empty, full[MAX_STAGES], empty[MAX_STAGES], s_full[2], dp_full, ds_ready, dq_full, delta_ready, drain;
+// Stages: tiles of keys and of values have rings of their own, for a tile of values is done with long before the keys beside it.
+template <int DB> struct QueryStages { static constexpr int K = DB == 1 ? 4 : 2, V = DB == 1 ? 3 : 1; };
+
+template <int DB>
+struct __align__(16) QueryBars {
+    float lse[TILE], delta[TILE];           // of an item's rows: lse times log2 e, delta
+    uint64_t q_full[2], q_empty[2], k_full[QueryStages<DB>::K], k_empty[QueryStages<DB>::K], v_full[QueryStages<DB>::V], v_empty[QueryStages<DB>::V];
+    uint64_t s_full[2], dp_full, ds_ready, dq_full, stat_full, drain;
     uint32_t tmem_base, abort_flag;
-    float part[2][4][TILE];                 // quarters of delta, of an item and the next
 };
 
+// The roles walk over the same flat sequence of tiles, item after item: queries and dO of the next item are brought, its statistics taken and its first scores
+// formed while the last tiles of the one before are worked on.
 template <int DB>
 __global__ void __launch_bounds__(NTHREADS, 1)
 attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_k,
@@ -57,21 +65,21 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     constexpr int OP = DB * 16384;
-    uint8_t* q_smem = smem;                                  // queries, then the gradient of their outputs
-    uint8_t* ring_smem = smem + 2 * OP;
-    const uint32_t nS = (uint32_t)p.stages;
-    QueryBars* bars = reinterpret_cast<QueryBars*>(ring_smem + (size_t)nS * OP);
+    constexpr uint32_t KS = QueryStages<DB>::K, VS = QueryStages<DB>::V;
+    uint8_t* q_smem = smem;                                  // twice: queries, the gradient of their outputs
+    uint8_t* k_smem = smem + 4 * OP;
+    uint8_t* v_smem = k_smem + KS * OP;
+    QueryBars<DB>* bars = reinterpret_cast<QueryBars<DB>*>(v_smem + VS * OP);
     volatile uint32_t* abort_flag = &bars->abort_flag;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int tok = TILE / p.pack;
+    const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int tok = TILE >> p.pack_shift;
 
     if (threadIdx.x == 0) {
-        mbar_init(smem_u32(&bars->q_full), 1); mbar_init(smem_u32(&bars->q_empty), 1);
-        for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&bars->s_full[i]), 1);
-        for (uint32_t i = 0; i < MAX_STAGES; ++i) { mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars->q_full[i]), 1); mbar_init(smem_u32(&bars->q_empty[i]), 1); mbar_init(smem_u32(&bars->s_full[i]), 1); }
+        for (uint32_t i = 0; i < KS; ++i) { mbar_init(smem_u32(&bars->k_full[i]), 1); mbar_init(smem_u32(&bars->k_empty[i]), 1); }
+        for (uint32_t i = 0; i < VS; ++i) { mbar_init(smem_u32(&bars->v_full[i]), 1); mbar_init(smem_u32(&bars->v_empty[i]), 1); }
         mbar_init(smem_u32(&bars->dp_full), 1); mbar_init(smem_u32(&bars->ds_ready), 16); mbar_init(smem_u32(&bars->dq_full), 1);
-        mbar_init(smem_u32(&bars->delta_ready), 16);
-        mbar_init(smem_u32(&bars->drain), 1);
+        mbar_init(smem_u32(&bars->stat_full), 16); mbar_init(smem_u32(&bars->drain), 1);
         bars->abort_flag = 0;
         fence_barrier_init();
         prefetch_tmap(&tm_q); prefetch_tmap(&tm_do); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
@@ -89,11 +97,11 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         return __all_sync(0xFFFFFFFFu, w);
     };
     struct Work { AttnTile t; int head0, kv, n; };
-    auto work_of = [&](int64_t item) {
+    auto work_of = [&](uint32_t item) {
         Work w;
-        const int i = (int)(item / p.packs), c = (int)(item - (int64_t)i * p.packs);
+        const uint32_t i = item / p.packs, c = item - i * p.packs;
         w.t = tile_at(p.table, i);
-        w.head0 = c * p.pack; w.kv = w.head0 / p.group;
+        w.head0 = (int)c * p.pack; w.kv = w.head0 / p.group;
         w.n = (min(w.t.at + tok, w.t.len) + TILE - 1) / TILE;
         return w;
     };
@@ -101,25 +109,24 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 0) {
-            Ring ring;
-            uint32_t it = 0, q_uses = 0;
+            Ring k_ring, v_ring;
+            uint32_t items = 0, tiles = 0;
             bool ok = true;
-            auto load = [&](const CUtensorMap* map, int kv, int row) {
-                if (!warp_wait(&bars->empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; return; }
+            auto load = [&](const CUtensorMap* map, uint64_t* full_bar, uint8_t* dst_op, int kv, int row) {
                 if (elect_one()) {
-                    const uint32_t full = smem_u32(&bars->full[ring.slot]), dst = smem_u32(ring_smem + (size_t)ring.slot * OP);
+                    const uint32_t full = smem_u32(full_bar), dst = smem_u32(dst_op);
                     mbar_arrive_expect_tx(full, OP);
 #pragma unroll
                     for (int b = 0; b < DB; ++b) tma_load_3d(dst + b * 16384, map, full, b * 64, kv, row);
                 }
                 __syncwarp();
-                ring.next(nS); ++it;
             };
-            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round, ++items) {
                 const Work w = work_of(item);
-                if (!warp_wait(&bars->q_empty, (q_uses++ & 1u) ^ 1u, TO_PRODUCER)) { ok = false; break; }
+                const uint32_t b2 = items & 1u;
+                if (!warp_wait(&bars->q_empty[b2], ((items >> 1) & 1u) ^ 1u, TO_PRODUCER)) { ok = false; break; }
                 if (elect_one()) {
-                    const uint32_t full = smem_u32(&bars->q_full), dst = smem_u32(q_smem);
+                    const uint32_t full = smem_u32(&bars->q_full[b2]), dst = smem_u32(q_smem + b2 * 2 * OP);
                     mbar_arrive_expect_tx(full, 2 * OP);
 #pragma unroll
                     for (int b = 0; b < DB; ++b) {
@@ -128,77 +135,93 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     }
                 }
                 __syncwarp();
-                for (int j = 0; j < w.n && ok; ++j) {
-                    load(&tm_k, w.kv, w.t.t0 + j * TILE);
-                    if (ok) load(&tm_v, w.kv, w.t.t0 + j * TILE);
+                for (int j = 0; j < w.n; ++j, ++tiles) {
+                    if (!warp_wait(&bars->k_empty[k_ring.slot], k_ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
+                    load(&tm_k, &bars->k_full[k_ring.slot], k_smem + (size_t)k_ring.slot * OP, w.kv, w.t.t0 + j * TILE);
+                    k_ring.next(KS);
+                    if (!warp_wait(&bars->v_empty[v_ring.slot], v_ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
+                    load(&tm_v, &bars->v_full[v_ring.slot], v_smem + (size_t)v_ring.slot * OP, w.kv, w.t.t0 + j * TILE);
+                    v_ring.next(VS);
                 }
             }
-            if (!ok)
-                for (uint32_t j = it > nS ? it - nS : 0u; j < it; ++j)
-                    if (!mbar_wait_quiet(smem_u32(&bars->full[j % nS]), (j / nS) & 1u, 1u << 14)) break;
+            // behind a wait that gave up: what is still on its way arrives before the block leaves
+            if (!ok) {
+                for (uint32_t i = items > 1 ? items - 1 : 0u; i <= items; ++i) mbar_wait_quiet(smem_u32(&bars->q_full[i & 1u]), (i >> 1) & 1u, 1u << 14);
+                for (uint32_t i = tiles > KS ? tiles - KS : 0u; i <= tiles; ++i) mbar_wait_quiet(smem_u32(&bars->k_full[i % KS]), (i / KS) & 1u, 1u << 14);
+                for (uint32_t i = tiles > VS ? tiles - VS : 0u; i < tiles; ++i) mbar_wait_quiet(smem_u32(&bars->v_full[i % VS]), (i / VS) & 1u, 1u << 14);
+            }
         } else if (warp == 1) {
             const uint32_t n_d = (uint32_t)((p.head_dim + 15) / 16 * 16), steps = n_d / 16;
             const uint32_t idesc_s = make_idesc(1, 1, 1, 128, 128), idesc_q = make_idesc(1, 1, 1, 128, n_d) | IDESC_B_MN;
-            Ring ring;
-            uint32_t q_uses = 0, ds_uses = 0, s_uses = 0;
-            bool ok = true;
             auto product = [&](uint32_t d, const uint8_t* a_op, const uint8_t* b_op) {
                 const uint64_t a = make_smem_desc_sw128(smem_u32(a_op)), b = make_smem_desc_sw128(smem_u32(b_op));
-                for (uint32_t k = 0; k < steps; ++k) {
+#pragma unroll
+                for (uint32_t k = 0; k < 4 * DB; ++k) {
                     const uint64_t off = (uint64_t)((k >> 2) * 1024 + (k & 3) * 2);
-                    mma_f16_ss(d, a + off, b + off, idesc_s, k > 0);
+                    if (k < steps) mma_f16_ss(d, a + off, b + off, idesc_s, k > 0);
                 }
             };
-            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
-                const Work w = work_of(item);
-                if (!warp_wait(&bars->q_full, q_uses++ & 1u, TO_MMA)) { ok = false; break; }
-                Ring k = ring, v;                            // stages of keys and values of tile j
-                v = k; v.next(nS);
-                auto scores = [&](const Ring& at, int j) -> bool {      // keys behind the sequence's end become zeros: they meet ds = 0 in dq
-                    if (!warp_wait(&bars->full[at.slot], at.parity, TO_MMA)) return false;
-                    uint8_t* op = ring_smem + (size_t)at.slot * OP;
-                    if (w.t.len - j * TILE < TILE) zero_rows(op, DB, w.t.len - j * TILE, lane);
-                    tc_fence_after();
-                    if (elect_one()) {
-                        product(tmem + ((s_uses + j) & 1u) * 128, q_smem, op);
-                        mma_commit(smem_u32(&bars->s_full[(s_uses + j) & 1u]));
-                    }
-                    __syncwarp();
-                    return true;
-                };
-                auto dps = [&](const Ring& at, bool last) -> bool {
-                    if (!warp_wait(&bars->full[at.slot], at.parity, TO_MMA)) return false;
-                    tc_fence_after();
-                    if (elect_one()) {
-                        product(tmem + 256, q_smem + OP, ring_smem + (size_t)at.slot * OP);
-                        mma_commit(smem_u32(&bars->dp_full));
-                        mma_commit(smem_u32(&bars->empty[at.slot]));
-                        if (last) mma_commit(smem_u32(&bars->q_empty));
-                    }
-                    __syncwarp();
-                    return true;
-                };
-                ok = scores(k, 0) && dps(v, w.n == 1);
-                for (int j = 0; j < w.n && ok; ++j) {
-                    Ring k1 = v, v1;
-                    k1.next(nS); v1 = k1; v1.next(nS);
-                    if (j + 1 < w.n && !scores(k1, j + 1)) { ok = false; break; }
-                    if (!warp_wait(&bars->ds_ready, ds_uses++ & 1u, TO_MMA)) { ok = false; break; }
-                    if (j + 1 < w.n && !dps(v1, j + 2 == w.n)) { ok = false; break; }
-                    tc_fence_after();
-                    if (elect_one()) {
-                        const uint64_t b = make_smem_desc_mn_sw128(smem_u32(ring_smem + (size_t)k.slot * OP), 16384);
-                        const uint32_t a = tmem + ((s_uses + j) & 1u) * 128;
-#pragma unroll
-                        for (int s = 0; s < 8; ++s) mma_f16_ts(tmem + 384, a + quarter_column(s), b + (uint64_t)(s * 128), idesc_q, j > 0 || s > 0);
-                        mma_commit(smem_u32(&bars->empty[k.slot]));
-                        if (j + 1 == w.n) mma_commit(smem_u32(&bars->dq_full));
-                    }
-                    __syncwarp();
-                    k = k1; v = v1;
+            // A place in the sequence of tiles; the scores run one tile ahead of the rest.
+            struct Place { uint32_t round; Work w; int j; uint32_t items; };
+            Ring k_ring, k_use, v_ring;                      // keys for the scores, for dq; values
+            uint32_t s_tiles = 0, tiles = 0;
+            bool ok = true;
+            Place ahead;
+            ahead.round = 0; ahead.j = 0; ahead.items = 0;
+            bool more = item_of_round(0) < p.items;          // is there a tile at `ahead`?
+            if (more) ahead.w = work_of(item_of_round(0));
+            auto scores = [&]() -> bool {                    // of the tile at `ahead`: keys behind the sequence's end become zeros (they meet ds = 0 in dq)
+                const Place& a = ahead;
+                if (a.j == 0 && !warp_wait(&bars->q_full[a.items & 1u], (a.items >> 1) & 1u, TO_MMA)) return false;
+                if (!warp_wait(&bars->k_full[k_ring.slot], k_ring.parity, TO_MMA)) return false;
+                uint8_t* op = k_smem + (size_t)k_ring.slot * OP;
+                if (a.w.t.len - a.j * TILE < TILE) zero_rows(op, DB, a.w.t.len - a.j * TILE, lane);
+                tc_fence_after();
+                if (elect_one()) {
+                    product(tmem + (s_tiles & 1u) * 128, q_smem + (a.items & 1u) * 2 * OP, op);
+                    mma_commit(smem_u32(&bars->s_full[s_tiles & 1u]));
                 }
-                ring = k;                                    // (behind the last tile's)
-                s_uses += w.n;
+                __syncwarp();
+                k_ring.next(KS);
+                ++s_tiles;
+                return true;
+            };
+            auto dps = [&](const Place& a) -> bool {
+                if (!warp_wait(&bars->v_full[v_ring.slot], v_ring.parity, TO_MMA)) return false;
+                tc_fence_after();
+                if (elect_one()) {
+                    product(tmem + 256, q_smem + (a.items & 1u) * 2 * OP + OP, v_smem + (size_t)v_ring.slot * OP);
+                    mma_commit(smem_u32(&bars->dp_full));
+                    mma_commit(smem_u32(&bars->v_empty[v_ring.slot]));
+                    if (a.j + 1 == a.w.n) mma_commit(smem_u32(&bars->q_empty[a.items & 1u]));      // (its scores were issued before)
+                }
+                __syncwarp();
+                v_ring.next(VS);
+                return true;
+            };
+            if (more) ok = scores() && dps(ahead);
+            while (more && ok) {
+                const Place now = ahead;
+                if (++ahead.j == ahead.w.n) {
+                    ahead.j = 0; ++ahead.items; ++ahead.round;
+                    more = item_of_round(ahead.round) < p.items;
+                    if (more) ahead.w = work_of(item_of_round(ahead.round));
+                }
+                if (more && !scores()) { ok = false; break; }
+                if (!warp_wait(&bars->ds_ready, tiles & 1u, TO_MMA)) { ok = false; break; }
+                if (more && !dps(ahead)) { ok = false; break; }
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t b = make_smem_desc_mn_sw128(smem_u32(k_smem + (size_t)k_use.slot * OP), 16384);
+                    const uint32_t a = tmem + (tiles & 1u) * 128;
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) mma_f16_ts(tmem + 384, a + quarter_column(s), b + (uint64_t)(s * 128), idesc_q, now.j > 0 || s > 0);
+                    mma_commit(smem_u32(&bars->k_empty[k_use.slot]));
+                    if (now.j + 1 == now.w.n) mma_commit(smem_u32(&bars->dq_full));
+                }
+                __syncwarp();
+                k_use.next(KS);
+                ++tiles;
             }
             if (elect_one()) mma_commit(smem_u32(&bars->drain));
             __syncwarp();
@@ -208,81 +231,127 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
         const int part = (warp >> 2) - 1, r = (warp & 3) * 32 + lane;      // which quarter of the columns
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const int my_tok = r / p.pack, my_head = r % p.pack;
-        uint32_t s_uses = 0, dp_uses = 0, dq_uses = 0;       // (dq_uses: items so far)
+        const int my_tok = r >> p.pack_shift;
+        const uint64_t scale2 = pair_of(p.scale_log2, p.scale_log2);
+        uint32_t tiles = 0, items = 0;
         bool ok = true;
-        for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
-            const Work w = work_of(item);
-            const int at = w.t.at + my_tok;
-            const bool there = at < w.t.len;
-            const int64_t token = w.t.t0 + at;
-            const int head = w.head0 + my_head;
-            float delta = 0.0f, off = 0.0f;
-            if (there) {
-                const __nv_bfloat16* o = p.out + token * p.ld_out + (int64_t)head * p.head_dim;
-                const __nv_bfloat16* d = p.dout + token * p.ld_dout + (int64_t)head * p.head_dim;
-                float acc[2] = {0.0f, 0.0f};
-#pragma unroll 4
-                for (int c = part * 8; c < p.head_dim; c += 32) {
-                    float a[8], b[8];
-                    unpack_bf16(__ldg(reinterpret_cast<const uint4*>(o + c)), a);
-                    unpack_bf16(__ldg(reinterpret_cast<const uint4*>(d + c)), b);
+        // Statistics of an item's rows, eight to a warp: the lanes that share a row (8 or 16) read 16 bytes of out and of its gradient each, before the
+        // epilogue of the item in front; behind it they are added up and put down. One place will do: a warp comes here when the last tile's
+        // ds of every warp has arrived, so all have read what stood there.
+        constexpr int LANES = 8 * DB, ROWS = 32 / LANES, PARTS = 8 / ROWS;
+        const int sub = lane / LANES, c8 = (lane % LANES) * 8, stat_row = (warp - 4) * 8;
+        uint4 o8[PARTS], d8[PARTS];
+        float lse1 = 0.0f;
+        auto row_of = [&](const Work& w, int row, int64_t& token, int& head) -> bool {
+            const int a = w.t.at + (row >> p.pack_shift);
+            token = w.t.t0 + a; head = w.head0 + (row & (p.pack - 1));
+            return a < w.t.len;
+        };
+        auto fetch = [&](const Work& w) {
+            int64_t token;
+            int head;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) acc[k & 1] = fmaf(a[k], b[k], acc[k & 1]);
+            for (int i = 0; i < PARTS; ++i) {
+                o8[i] = d8[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (row_of(w, stat_row + i * ROWS + sub, token, head) && c8 < p.head_dim) {
+                    o8[i] = __ldg(reinterpret_cast<const uint4*>(p.out + token * p.ld_out + (int64_t)head * p.head_dim + c8));
+                    d8[i] = __ldg(reinterpret_cast<const uint4*>(p.dout + token * p.ld_dout + (int64_t)head * p.head_dim + c8));
                 }
-                delta = acc[0] + acc[1];
-                off = p.lse[token * p.heads + head] * LOG2E;
             }
-            // The quarters meet through an mbarrier, whose waits end (a block-wide barrier would wait for warps that gave up). An item's places are
-            // written again two items later, when every warp has arrived for the item between.
-            bars->part[dq_uses & 1u][part][r] = delta;
+            lse1 = lane < 8 && row_of(w, stat_row + lane, token, head) ? p.lse[token * p.heads + head] * LOG2E : 0.0f;
+        };
+        auto put_down = [&](const Work& w) {
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) {
+                float a[8], b[8], acc = 0.0f;
+                unpack_bf16(o8[i], a);
+                unpack_bf16(d8[i], b);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) acc = fmaf(a[k], b[k], acc);
+#pragma unroll
+                for (int s = LANES / 2; s > 0; s >>= 1) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, s);
+                if (lane % LANES == 0) bars->delta[stat_row + i * ROWS + sub] = acc;
+            }
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bars->delta_ready));
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->delta_ready), dq_uses & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
+            if (lane < 8) {
+                int64_t token;
+                int head;
+                bars->lse[stat_row + lane] = lse1;
+                if (row_of(w, stat_row + lane, token, head)) p.delta[token * p.heads + head] = bars->delta[stat_row + lane];
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars->stat_full));
+        };
+        Work w;
+        bool more = item_of_round(0) < p.items;
+        if (more) { w = work_of(item_of_round(0)); fetch(w); put_down(w); }
+        for (uint32_t round = 0; more && ok; ++round, ++items) {
+            const int at = w.t.at + my_tok;
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->stat_full), items & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
             if (!ok) break;
-            const float (*quarters)[TILE] = bars->part[dq_uses & 1u];
-            delta = (quarters[0][r] + quarters[1][r]) + (quarters[2][r] + quarters[3][r]);
-            if (there && part == 0) p.delta[token * p.heads + head] = delta;
-            for (int j = 0; j < w.n; ++j) {
-                const uint32_t buf = s_uses & 1u, s_addr = tmem + lanes + buf * 128 + part * 32;
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->s_full[buf]), (s_uses >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
+            const float off = -bars->lse[r], delta = -bars->delta[r];
+            const uint64_t off2 = pair_of(off, off), delta2 = pair_of(delta, delta);
+            for (int j = 0; j < w.n; ++j, ++tiles) {
+                const uint32_t buf = tiles & 1u, s_addr = tmem + lanes + buf * 128 + part * 32;
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->s_full[buf]), (tiles >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
                 if (!ok) break;
-                ++s_uses;
                 tc_fence_after();
-                uint32_t s[32], dp[32], e[16];
-                tmem_ld_x32(s_addr, s);
+                uint32_t s[2][16];
+                uint64_t pr[16];
+                tmem_ld_x16(s_addr, s[0]);
                 tmem_wait_ld();
+                tmem_ld_x16(s_addr + 16, s[1]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (h == 1) tmem_wait_ld();
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        pr[h * 8 + k] = ex2_of<SHARE>(fma2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), scale2, off2), h * 8 + k);
+                }
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->dp_full), tiles & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t dp_addr = tmem + lanes + 256 + part * 32;
+                tmem_ld_x16(dp_addr, s[0]);
+                tmem_wait_ld();
+                tmem_ld_x16(dp_addr + 16, s[1]);
+                const bool masked = j * TILE + TILE - 1 > w.t.at;
                 const int lim = at - j * TILE - part * 32;   // this row's last key among the 32
 #pragma unroll
-                for (int k = 0; k < 32; ++k) s[k] = __float_as_uint(ex2(fmaf(__uint_as_float(s[k]), p.scale_log2, -off)));
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->dp_full), dp_uses++ & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
-                if (!ok) break;
-                tc_fence_after();
-                tmem_ld_x32(tmem + lanes + 256 + part * 32, dp);
-                tmem_wait_ld();
+                for (int h = 0; h < 2; ++h) {
+                    if (h == 1) tmem_wait_ld();
+                    uint32_t e[8];
 #pragma unroll
-                for (int k = 0; k < 32; ++k) dp[k] = __float_as_uint(__uint_as_float(s[k]) * (__uint_as_float(dp[k]) - delta));
-                if (j * TILE + TILE - 1 > w.t.at) {
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) if (k > lim) dp[k] = 0u;
+                    for (int k = 0; k < 8; ++k) {
+                        uint64_t ds = mul2(pr[h * 8 + k], add2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), delta2));
+                        if (masked) {
+                            float a, b;
+                            split_pair(ds, a, b);
+                            ds = pair_of(h * 16 + 2 * k > lim ? 0.0f : a, h * 16 + 2 * k + 1 > lim ? 0.0f : b);
+                        }
+                        e[k] = pack_pair(ds);
+                    }
+                    tmem_st_x8(s_addr + h * 8, e);           // over this quarter's own scores
                 }
-#pragma unroll
-                for (int k = 0; k < 16; ++k) e[k] = pack_bf16(__uint_as_float(dp[2 * k]), __uint_as_float(dp[2 * k + 1]));
-                tmem_st_x16(s_addr, e);                      // over this quarter's own scores
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&bars->ds_ready));
             }
             if (!ok) break;
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->dq_full), dq_uses++ & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
+            const uint32_t item = item_of_round(round + 1);
+            more = item < p.items;
+            Work next = w;
+            if (more) { next = work_of(item); fetch(next); }
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->dq_full), items & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
             if (!ok) break;
             tc_fence_after();
-            const int row0 = (warp & 3) * 32;
-            auto where = [&](int i) -> __nv_bfloat16* {
-                const int rr = row0 + i, a = w.t.at + rr / p.pack;
-                return a < w.t.len ? p.dq + (int64_t)(w.t.t0 + a) * p.ld_dq + (int64_t)(w.head0 + rr % p.pack) * p.head_dim : nullptr;
-            };
+            __nv_bfloat16* dst[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int rr = (warp & 3) * 32 + (lane & ~3) + k, a = w.t.at + (rr >> p.pack_shift);
+                dst[k] = a < w.t.len ? p.dq + (int64_t)(w.t.t0 + a) * p.ld_dq + (int64_t)(w.head0 + (rr & (p.pack - 1))) * p.head_dim : nullptr;
+            }
 #pragma unroll 1
             for (int c = part * 32; c < p.head_dim; c += 128) {
                 uint32_t o[32];
@@ -291,9 +360,10 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 tmem_wait_ld();
 #pragma unroll
                 for (int k = 0; k < 32; ++k) f[k] = __uint_as_float(o[k]) * p.scale;
-                store_rows32(f, c, p.head_dim, lane, where);
+                store_rows32(f, c, p.head_dim, lane, dst);
             }
             tc_fence_before();
+            if (more) { put_down(next); w = next; }
         }
     }
     tc_fence_before();
@@ -306,15 +376,18 @@ struct KeyParams {
     const float* lse; const float* delta;
     __nv_bfloat16* dk; __nv_bfloat16* dv;
     int64_t ld_dk, ld_dv;
-    int32_t kv_heads, pack, group, heads, head_dim;
-    int64_t items;
+    uint32_t items, kv_heads;
+    int32_t pack, pack_shift, group, heads, head_dim;
     float scale, scale_log2;
     unsigned int* timeout_word;
 };
 
-constexpr int KEY_STAGES = 2;
+template <int DB> struct KeyStages { static constexpr int N = DB == 1 ? 4 : 2; };
+
+template <int DB>
 struct __align__(16) KeyBars {
-    float lse[KEY_STAGES][TILE], delta[KEY_STAGES][TILE];      // of each query row: lse times log2 e, delta
+    static constexpr int KEY_STAGES = KeyStages<DB>::N;
+    float lse[KEY_STAGES][TILE], delta[KEY_STAGES][TILE];      // of each query row, negated: lse times log2 e, delta
     uint64_t kv_full, kv_empty, full[KEY_STAGES], empty[KEY_STAGES], stat_full[KEY_STAGES], stat_empty[KEY_STAGES], s_full, dp_full, p_ready, ds_ready, done, drain;
     uint32_t tmem_base, abort_flag;
 };
@@ -329,10 +402,11 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     constexpr int OP = DB * 16384;
     uint8_t* kv_smem = smem;                                 // keys, values
     uint8_t* ring_smem = smem + 2 * OP;                      // queries and the gradient of their outputs, KEY_STAGES times
-    KeyBars* bars = reinterpret_cast<KeyBars*>(ring_smem + KEY_STAGES * 2 * OP);
+    constexpr int KEY_STAGES = KeyStages<DB>::N;
+    KeyBars<DB>* bars = reinterpret_cast<KeyBars<DB>*>(ring_smem + KEY_STAGES * 2 * OP);
     volatile uint32_t* abort_flag = &bars->abort_flag;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int tok = TILE / p.pack, passes = p.group / p.pack;
+    const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const int tok = TILE >> p.pack_shift, passes = p.group >> p.pack_shift;
 
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&bars->kv_full), 1); mbar_init(smem_u32(&bars->kv_empty), 1);
@@ -360,13 +434,13 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     };
     // loops: for every pass over `pack` heads of the group, the tiles of queries from the one that holds the first key's token on
     struct Work { AttnTile t; int kv, first, per, n; };
-    auto work_of = [&](int64_t item) {
+    auto work_of = [&](uint32_t item) {
         Work w;
-        const int i = (int)(item / p.kv_heads);
-        w.kv = (int)(item - (int64_t)i * p.kv_heads);
+        const uint32_t i = item / p.kv_heads;
+        w.kv = (int)(item - i * p.kv_heads);
         w.t = tile_at(p.table, i);
-        w.first = w.t.at / tok;
-        w.per = (w.t.len + tok - 1) / tok - w.first;
+        w.first = w.t.at >> (7 - p.pack_shift);
+        w.per = ((w.t.len + tok - 1) >> (7 - p.pack_shift)) - w.first;
         w.n = w.per * passes;
         return w;
     };
@@ -377,7 +451,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             Ring ring;
             uint32_t it = 0, kv_uses = 0;
             bool ok = true;
-            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round) {
                 const Work w = work_of(item);
                 if (!warp_wait(&bars->kv_empty, (kv_uses++ & 1u) ^ 1u, TO_PRODUCER)) { ok = false; break; }
                 if (elect_one()) {
@@ -418,9 +492,10 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             bool ok = true;
             auto product = [&](uint32_t d, const uint8_t* a_op, const uint8_t* b_op) {
                 const uint64_t a = make_smem_desc_sw128(smem_u32(a_op)), b = make_smem_desc_sw128(smem_u32(b_op));
-                for (uint32_t k = 0; k < steps; ++k) {
+#pragma unroll
+                for (uint32_t k = 0; k < 4 * DB; ++k) {
                     const uint64_t off = (uint64_t)((k >> 2) * 1024 + (k & 3) * 2);
-                    mma_f16_ss(d, a + off, b + off, idesc_s, k > 0);
+                    if (k < steps) mma_f16_ss(d, a + off, b + off, idesc_s, k > 0);
                 }
             };
             auto gradient = [&](uint32_t d, uint32_t a, const uint8_t* b_op, bool more) {
@@ -428,7 +503,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 #pragma unroll
                 for (int s = 0; s < 8; ++s) mma_f16_ts(d, a + quarter_column(s), b + (uint64_t)(s * 128), idesc_g, more || s > 0);
             };
-            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round) {
                 const Work w = work_of(item);
                 if (!warp_wait(&bars->kv_full, kv_uses++ & 1u, TO_MMA)) { ok = false; break; }
                 int i = w.first, left = w.per;
@@ -459,14 +534,15 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     const bool more = j + 1 < w.n;
                     const uint8_t* op = ring_smem + (size_t)ring.slot * 2 * OP;
                     const uint8_t* op1 = ring_smem + (size_t)next.slot * 2 * OP;
+                    if (more && !arrived(next)) { ok = false; break; }
                     if (!warp_wait(&bars->p_ready, p_uses++ & 1u, TO_MMA)) { ok = false; break; }
                     tc_fence_after();
-                    if (elect_one()) gradient(tmem + 256, tmem, op + OP, j > 0);
-                    __syncwarp();
-                    if (more && !arrived(next)) { ok = false; break; }
-                    if (more && elect_one()) {
-                        product(tmem, kv_smem, op1);
-                        mma_commit(smem_u32(&bars->s_full));
+                    if (elect_one()) {
+                        gradient(tmem + 256, tmem, op + OP, j > 0);
+                        if (more) {
+                            product(tmem, kv_smem, op1);
+                            mma_commit(smem_u32(&bars->s_full));
+                        }
                     }
                     __syncwarp();
                     if (!warp_wait(&bars->ds_ready, ds_uses++ & 1u, TO_MMA)) { ok = false; break; }
@@ -492,18 +568,18 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         } else {
             Ring ring;
             bool ok = true;
-            for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round) {
                 const Work w = work_of(item);
                 int head0 = w.kv * p.group, i = w.first, left = w.per;
                 for (int j = 0; j < w.n; ++j, ring.next(KEY_STAGES)) {
                     float lse[2], delta[2];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {            // rows behind the end: P = e^(0 - infinity) = 0, dS = 0
-                        const int r = (warp - 2) * 64 + h * 32 + lane, at = i * tok + r / p.pack;
-                        lse[h] = INFINITY; delta[h] = 0.0f;
+                        const int r = (warp - 2) * 64 + h * 32 + lane, at = i * tok + (r >> p.pack_shift);
+                        lse[h] = -INFINITY; delta[h] = 0.0f;
                         if (at < w.t.len) {
-                            const int64_t row = (int64_t)(w.t.t0 + at) * p.heads + head0 + r % p.pack;
-                            lse[h] = p.lse[row] * LOG2E; delta[h] = p.delta[row];
+                            const int64_t row = (int64_t)(w.t.t0 + at) * p.heads + head0 + (r & (p.pack - 1));
+                            lse[h] = -p.lse[row] * LOG2E; delta[h] = -p.delta[row];
                         }
                     }
                     if (!warp_wait(&bars->stat_empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
@@ -523,10 +599,11 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
         const int part = (warp >> 2) - 1, r = (warp & 3) * 32 + lane;      // which quarter of the columns
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_addr = tmem + lanes + part * 32, dp_addr = s_addr + 128;
+        const uint64_t scale2 = pair_of(p.scale_log2, p.scale_log2);
         uint32_t uses = 0, done_uses = 0;
         Ring ring;
         bool ok = true;
-        for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+        for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round) {
             const Work w = work_of(item);
             const int key = w.t.at + r;
             int i = w.first, left = w.per;
@@ -541,26 +618,34 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->s_full), uses & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t s[32], dp[32], e[16];
-                tmem_ld_x32(s_addr, s);
-                const float4* lse = reinterpret_cast<const float4*>(&bars->lse[ring.slot][part * 32]);
+                uint32_t s[2][16];
+                uint64_t pr[16];
+                tmem_ld_x16(s_addr, s[0]);
+                const float4* lse = reinterpret_cast<const float4*>(&bars->lse[ring.slot][part * 32]);      // negated, like delta
                 const float4* delta = reinterpret_cast<const float4*>(&bars->delta[ring.slot][part * 32]);
                 tmem_wait_ld();
+                tmem_ld_x16(s_addr + 16, s[1]);
 #pragma unroll
-                for (int k = 0; k < 32; k += 4) {
-                    const float4 l = lse[k / 4];
-                    s[k] = __float_as_uint(ex2(fmaf(__uint_as_float(s[k]), p.scale_log2, -l.x)));
-                    s[k + 1] = __float_as_uint(ex2(fmaf(__uint_as_float(s[k + 1]), p.scale_log2, -l.y)));
-                    s[k + 2] = __float_as_uint(ex2(fmaf(__uint_as_float(s[k + 2]), p.scale_log2, -l.z)));
-                    s[k + 3] = __float_as_uint(ex2(fmaf(__uint_as_float(s[k + 3]), p.scale_log2, -l.w)));
+                for (int h = 0; h < 2; ++h) {
+                    if (h == 1) tmem_wait_ld();
+                    uint32_t e[8];
+#pragma unroll
+                    for (int k = 0; k < 8; k += 2) {
+                        const float4 l = lse[(h * 8 + k) / 2];
+                        pr[h * 8 + k] = ex2_of<SHARE>(fma2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), scale2, pair_of(l.x, l.y)), h * 8 + k);
+                        pr[h * 8 + k + 1] = ex2_of<SHARE>(fma2(pair_of(__uint_as_float(s[h][2 * k + 2]), __uint_as_float(s[h][2 * k + 3])), scale2, pair_of(l.z, l.w)), h * 8 + k + 1);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if (masked) {
+                            float a, b;
+                            split_pair(pr[h * 8 + k], a, b);
+                            pr[h * 8 + k] = pair_of(h * 16 + 2 * k < from ? 0.0f : a, h * 16 + 2 * k + 1 < from ? 0.0f : b);
+                        }
+                        e[k] = pack_pair(pr[h * 8 + k]);
+                    }
+                    tmem_st_x8(s_addr + h * 8, e);           // over this quarter's own scores
                 }
-                if (masked) {
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) if (k < from) s[k] = 0u;
-                }
-#pragma unroll
-                for (int k = 0; k < 16; ++k) e[k] = pack_bf16(__uint_as_float(s[2 * k]), __uint_as_float(s[2 * k + 1]));
-                tmem_st_x16(s_addr, e);                      // over this quarter's own scores
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -568,23 +653,29 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->dp_full), uses & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
                 if (!ok) break;
                 tc_fence_after();
-                tmem_ld_x32(dp_addr, dp);
+                tmem_ld_x16(dp_addr, s[0]);
                 tmem_wait_ld();
+                tmem_ld_x16(dp_addr + 16, s[1]);
 #pragma unroll
-                for (int k = 0; k < 32; k += 4) {
-                    const float4 d = delta[k / 4];
-                    dp[k] = __float_as_uint(__uint_as_float(s[k]) * (__uint_as_float(dp[k]) - d.x));
-                    dp[k + 1] = __float_as_uint(__uint_as_float(s[k + 1]) * (__uint_as_float(dp[k + 1]) - d.y));
-                    dp[k + 2] = __float_as_uint(__uint_as_float(s[k + 2]) * (__uint_as_float(dp[k + 2]) - d.z));
-                    dp[k + 3] = __float_as_uint(__uint_as_float(s[k + 3]) * (__uint_as_float(dp[k + 3]) - d.w));
+                for (int h = 0; h < 2; ++h) {
+                    if (h == 1) tmem_wait_ld();
+                    uint32_t e[8];
+#pragma unroll
+                    for (int k = 0; k < 8; k += 2) {
+                        const float4 d = delta[(h * 8 + k) / 2];
+                        uint64_t a2 = mul2(pr[h * 8 + k], add2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), pair_of(d.x, d.y)));
+                        uint64_t b2 = mul2(pr[h * 8 + k + 1], add2(pair_of(__uint_as_float(s[h][2 * k + 2]), __uint_as_float(s[h][2 * k + 3])), pair_of(d.z, d.w)));
+                        if (masked) {
+                            float a, b;
+                            split_pair(a2, a, b);
+                            a2 = pair_of(h * 16 + 2 * k < from ? 0.0f : a, h * 16 + 2 * k + 1 < from ? 0.0f : b);
+                            split_pair(b2, a, b);
+                            b2 = pair_of(h * 16 + 2 * k + 2 < from ? 0.0f : a, h * 16 + 2 * k + 3 < from ? 0.0f : b);
+                        }
+                        e[k] = pack_pair(a2); e[k + 1] = pack_pair(b2);
+                    }
+                    tmem_st_x8(dp_addr + h * 8, e);
                 }
-                if (masked) {
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) if (k < from) dp[k] = 0u;
-                }
-#pragma unroll
-                for (int k = 0; k < 16; ++k) e[k] = pack_bf16(__uint_as_float(dp[2 * k]), __uint_as_float(dp[2 * k + 1]));
-                tmem_st_x16(dp_addr, e);
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -599,10 +690,10 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             __nv_bfloat16* base = is_k ? p.dk : p.dv;
             const int64_t ld = is_k ? p.ld_dk : p.ld_dv;
             const float by = is_k ? p.scale : 1.0f;
-            const int row0 = w.t.at + (warp & 3) * 32;
-            auto where = [&](int k) -> __nv_bfloat16* {
-                return row0 + k < w.t.len ? base + (int64_t)(w.t.t0 + row0 + k) * ld + (int64_t)w.kv * p.head_dim : nullptr;
-            };
+            const int row0 = w.t.at + (warp & 3) * 32 + (lane & ~3);
+            __nv_bfloat16* dst[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) dst[k] = row0 + k < w.t.len ? base + (int64_t)(w.t.t0 + row0 + k) * ld + (int64_t)w.kv * p.head_dim : nullptr;
 #pragma unroll 1
             for (int c = (part & 1) * 32; c < p.head_dim; c += 64) {
                 uint32_t o[32];
@@ -611,7 +702,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 tmem_wait_ld();
 #pragma unroll
                 for (int k = 0; k < 32; ++k) f[k] = __uint_as_float(o[k]) * by;
-                store_rows32(f, c, p.head_dim, lane, where);
+                store_rows32(f, c, p.head_dim, lane, dst);
             }
             tc_fence_before();
         }
@@ -622,11 +713,12 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 }
 
 template <int DB>
-qless_status launch_backward(const CUtensorMap& q, const CUtensorMap& d, const CUtensorMap& k, const CUtensorMap& v, QueryParams& qp, const KeyParams& kp, cudaStream_t st)
+qless_status launch_backward(const CUtensorMap& q, const CUtensorMap& d, const CUtensorMap& k, const CUtensorMap& v, const QueryParams& qp, const KeyParams& kp, cudaStream_t st)
 {
-    const size_t op = (size_t)DB * 16384, budget = 227 * 1024 - 1024 - sizeof(QueryBars) - 2 * op;
-    qp.stages = (int32_t)std::min<size_t>(MAX_STAGES, budget / op);
-    const size_t q_smem = 1024 + (2 + qp.stages) * op + sizeof(QueryBars), k_smem = 1024 + (2 + 2 * KEY_STAGES) * op + sizeof(KeyBars);
+    const size_t op = (size_t)DB * 16384;
+    const size_t q_smem = 1024 + (4 + QueryStages<DB>::K + QueryStages<DB>::V) * op + sizeof(QueryBars<DB>), k_smem = 1024 + (2 + 2 * KeyStages<DB>::N) * op + sizeof(KeyBars<DB>);
+    static_assert(1024 + (4 + QueryStages<DB>::K + QueryStages<DB>::V) * DB * 16384 + sizeof(QueryBars<DB>) <= 227 * 1024 &&
+                  1024 + (2 + 2 * KeyStages<DB>::N) * DB * 16384 + sizeof(KeyBars<DB>) <= 227 * 1024, "shared memory of an SM");
     { ProfileScope ps("attention_dq", st);
       QLESS_CUDA_TRY((allow_full_smem<attention_dq_kernel<DB>>()));
       QLESS_CUDA_TRY(launch_ahead(attention_dq_kernel<DB>, dim3((unsigned)std::min<int64_t>(qp.items, sm_count())), dim3(NTHREADS), q_smem, st, q, d, k, v, qp)); }
@@ -656,6 +748,10 @@ qless_status launch_attention_backward(const AttnArgs& a, uint8_t* ws, unsigned 
     const int32_t pack = attn_pack(a.heads, a.kv_heads), tok = TILE / pack, packs = a.heads / pack;
     const std::vector<AttnTile> queries = query_tiles(a, tok), keys = key_tiles(a);
     if (queries.empty()) return QLESS_OK;
+    // (fewer key tiles than query tiles, and no more key heads than packs)
+    QLESS_REQUIRE((int64_t)queries.size() * packs < MOST_ITEMS - 65536, QLESS_ERR_UNSUPPORTED, "too many tiles: %zu of %d heads", queries.size(), packs);
+    int32_t shift = 0;
+    while ((1 << shift) < pack) ++shift;
     const int64_t seqs = std::min(a.tokens, a.n);
     AttnTile* q_list = reinterpret_cast<AttnTile*>(ws);
     AttnTile* k_list = reinterpret_cast<AttnTile*>(ws + tiles_bytes(a.tokens, seqs, tok));
@@ -672,11 +768,11 @@ qless_status launch_attention_backward(const AttnArgs& a, uint8_t* ws, unsigned 
     if ((s = head_map(&v, a.v, a.ld_v, a.kv_heads, a.head_dim, a.tokens, 1, TILE)) != QLESS_OK) return s;
     qp.out = reinterpret_cast<const __nv_bfloat16*>(a.out_in); qp.dout = reinterpret_cast<const __nv_bfloat16*>(a.dout); qp.lse = a.lse_in; qp.delta = delta;
     qp.dq = reinterpret_cast<__nv_bfloat16*>(a.dq); qp.ld_out = a.ld_out; qp.ld_dout = a.ld_dout; qp.ld_dq = a.ld_dq;
-    qp.packs = packs; qp.pack = pack; qp.group = a.heads / a.kv_heads; qp.heads = a.heads; qp.head_dim = a.head_dim;
-    qp.items = (int64_t)queries.size() * packs; qp.scale = a.scale; qp.scale_log2 = a.scale * LOG2E; qp.timeout_word = timeout_word;
+    qp.packs = packs; qp.pack = pack; qp.pack_shift = shift; qp.group = a.heads / a.kv_heads; qp.heads = a.heads; qp.head_dim = a.head_dim;
+    qp.items = (uint32_t)(queries.size() * packs); qp.scale = a.scale; qp.scale_log2 = a.scale * LOG2E; qp.timeout_word = timeout_word;
     kp.lse = a.lse_in; kp.delta = delta; kp.dk = reinterpret_cast<__nv_bfloat16*>(a.dk); kp.dv = reinterpret_cast<__nv_bfloat16*>(a.dv);
-    kp.ld_dk = a.ld_dk; kp.ld_dv = a.ld_dv; kp.kv_heads = a.kv_heads; kp.pack = pack; kp.group = qp.group; kp.heads = a.heads; kp.head_dim = a.head_dim;
-    kp.items = (int64_t)keys.size() * a.kv_heads; kp.scale = a.scale; kp.scale_log2 = qp.scale_log2; kp.timeout_word = timeout_word;
+    kp.ld_dk = a.ld_dk; kp.ld_dv = a.ld_dv; kp.kv_heads = a.kv_heads; kp.pack = pack; kp.pack_shift = shift; kp.group = qp.group; kp.heads = a.heads; kp.head_dim = a.head_dim;
+    kp.items = (uint32_t)(keys.size() * a.kv_heads); kp.scale = a.scale; kp.scale_log2 = qp.scale_log2; kp.timeout_word = timeout_word;
     return a.head_dim <= 64 ? launch_backward<1>(q, d, k, v, qp, kp, st) : launch_backward<2>(q, d, k, v, qp, kp, st);
 }
 

@@ -25,7 +25,11 @@ struct TileTable {
     AttnTile few[INLINE];
 };
 
-__device__ __forceinline__ AttnTile tile_at(const TileTable& t, int32_t i) { return t.list != nullptr ? t.list[i] : t.few[i]; }
+__device__ __forceinline__ AttnTile tile_at(const TileTable& t, int32_t i)
+{
+    const AttnTile x = t.list != nullptr ? t.list[i] : t.few[i];
+    return {warp_uniform(x.t0), warp_uniform(x.len), warp_uniform(x.at), warp_uniform(x.unused)};
+}
 
 __device__ __forceinline__ float ex2(float x)
 {
@@ -33,6 +37,79 @@ __device__ __forceinline__ float ex2(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Two fp32 values in a register pair, for the instructions that work on both.
+__device__ __forceinline__ uint64_t pair_of(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void split_pair(uint64_t r, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// 2^x of a pair on the fp32 units, for a share of the exponentials: the special-function units alone take 1024 clocks for a tile's 16384. Cody and Waite's
+// reduction x = n + r, |r| <= 1/2, by adding and subtracting 1.5 2^23; 2^r by the minimax polynomial of degree 5 (Remez exchange for the relative error
+// on [-1/2, 1/2]: 7.5e-8; 2.1e-7 as evaluated in fp32); 2^n from the sum's low bits. Below -126.5 the result is 0; NaN stays NaN.
+__device__ __forceinline__ uint64_t ex2_pair(uint64_t x)
+{
+    float a, b;
+    split_pair(x, a, b);
+    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(a));        // -127: 2^n comes out as 0
+    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(b));
+    x = pair_of(a, b);
+    const uint64_t t = add2(x, pair_of(12583039.0f, 12583039.0f));      // 1.5 2^23 + 127: n + 127 in the low bits
+    const uint64_t r = fma2(add2(t, pair_of(-12583039.0f, -12583039.0f)), pair_of(-1.0f, -1.0f), x);
+    uint64_t y = fma2(r, pair_of(1.3276472454890609e-3f, 1.3276472454890609e-3f), pair_of(9.675540961325169e-3f, 9.675540961325169e-3f));
+    y = fma2(y, r, pair_of(5.550713092088699e-2f, 5.550713092088699e-2f));
+    y = fma2(y, r, pair_of(2.4022120237350464e-1f, 2.4022120237350464e-1f));
+    y = fma2(y, r, pair_of(6.931469440460205e-1f, 6.931469440460205e-1f));
+    y = fma2(y, r, pair_of(1.0000001192092896f, 1.0000001192092896f));
+    float ta, tb;
+    split_pair(t, ta, tb);
+    return mul2(y, pair_of(__uint_as_float(__float_as_uint(ta) << 23), __uint_as_float(__float_as_uint(tb) << 23)));
+}
+// 2^x of pair i of a row: every `SHARE`-th on the fp32 units.
+template <int SHARE>
+__device__ __forceinline__ uint64_t ex2_of(uint64_t x, int i)
+{
+    if (SHARE > 0 && i % (SHARE > 0 ? SHARE : 1) == 1) return ex2_pair(x);
+    float a, b;
+    split_pair(x, a, b);
+    return pair_of(ex2(a), ex2(b));
+}
+__device__ __forceinline__ uint32_t pack_pair(uint64_t x)
+{
+    float a, b;
+    split_pair(x, a, b);
+    const __nv_bfloat162 z = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&z);
+}
+__device__ __forceinline__ float max3(float a, float b, float c)      // NaN where one of them is
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+constexpr int64_t MOST_ITEMS = (int64_t)1 << 31;      // of a launch: counted in 32 bits
+// The block's item of round k: forwards and backwards in turn, so that the lists, which begin with the longest, come out even.
+__device__ __forceinline__ uint32_t item_of_round(uint32_t k) { return k * gridDim.x + ((k & 1u) ? gridDim.x - 1 - blockIdx.x : blockIdx.x); }
+
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
 {
     const __nv_bfloat162 z = __floats2bfloat162_rn(a, b);
@@ -61,10 +138,9 @@ __device__ __forceinline__ void zero_rows(uint8_t* operand, int blocks, int from
     __syncwarp();
 }
 
-// A row of D bf16 values, 32 of them (columns c0 ..) in each lane for a row of its own, goes to memory 64 bytes at a time: `where` gives a row's
-// address or NULL.
-template <typename Where>
-__device__ __forceinline__ void store_rows32(const float (&v)[32], int c0, int head_dim, int lane, Where where)
+// Rows of D bf16 values, 32 of them (columns c0 ..) in each lane for a row of its own, go to memory 64 bytes at a time: `dst` are the addresses of rows
+// (lane & ~3) + 0 .. 3 of the warp's 32, NULL for one that is not written.
+__device__ __forceinline__ void store_rows32(const float (&v)[32], int c0, int head_dim, int lane, __nv_bfloat16* const (&dst)[4])
 {
     uint4 w[4];
 #pragma unroll
@@ -74,10 +150,8 @@ __device__ __forceinline__ void store_rows32(const float (&v)[32], int c0, int h
     transpose4(w, lane);
     const int c = c0 + (lane & 3) * 8;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        __nv_bfloat16* dst = where((lane & ~3) + k);
-        if (dst != nullptr && c < head_dim) *reinterpret_cast<uint4*>(dst + c) = w[k];
-    }
+    for (int k = 0; k < 4; ++k)
+        if (dst[k] != nullptr && c < head_dim) *reinterpret_cast<uint4*>(dst[k] + c) = w[k];
 }
 
 // Work of one launch: query tiles of `rows` tokens, or key tiles of 128, of every sequence, those with the longest loops first.

@@ -53,7 +53,7 @@ few_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     const uint32_t nS = (uint32_t)p.stages;
     Bars* bars = reinterpret_cast<Bars*>(smem + (size_t)nS * stage_bytes);
     volatile uint32_t* abort_flag = &bars->abort_flag;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < MAX_STAGES; ++s) { mbar_init(smem_u32(&bars->full[s]), 1); mbar_init(smem_u32(&bars->empty[s]), 1); }

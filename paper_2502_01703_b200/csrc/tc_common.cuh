@@ -141,6 +141,10 @@ __device__ __forceinline__ bool elect_one()
     return p != 0;
 }
 
+// Lane 0's value in every lane: tells the compiler that it is one value for the warp, so that branches on it and what is computed from it (operands
+// of copies and tensor-core instructions above all) stay in uniform registers.
+__device__ __forceinline__ int warp_uniform(int x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
+
 // ---- CTA pairs (cta_group::2) --------------------------------------------------------------------
 // A commit of the pair's leader (mma_commit_pair) arrives on a barrier in both CTAs' shared memory. Neither CTA may leave before the last of
 // these arrivals has landed in it, for its shared memory may be another block's by then, and the cluster barrier at the end orders the
@@ -387,6 +391,12 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&v)[
         ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
         "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
         : "memory");
+}
+// 32 lanes x 8 consecutive 32-bit columns (whole warp).
+__device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint32_t (&v)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 // 32 lanes x 32 consecutive 32-bit columns (whole warp).
 __device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t (&v)[32])
