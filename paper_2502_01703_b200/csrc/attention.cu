@@ -26,7 +26,7 @@ namespace {
 
 constexpr int NTHREADS = 640, MAX_STAGES = 10;
 constexpr float SLACK = 8.0f;               // powers of two that the maximum may grow before O is rescaled
-constexpr int SHARE = 3;                    // one in so many pairs of exponentials on the fp32 units
+constexpr int SHARE = 5;                    // one in so many pairs of exponentials on the fp32 units
 
 struct ForwardParams {
     TileTable table;
@@ -89,11 +89,10 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     };
     // item -> tile, first head, key head; loops of the two row tiles over the keys (0: the second one does not exist)
     struct Work { AttnTile t; int head0, kv, n[2]; };
-    auto work_of = [&](uint32_t item) {
+    auto work_of = [&](const Walk& k) {
         Work w;
-        const uint32_t i = item / p.packs, c = item - i * p.packs;
-        w.t = tile_at(p.table, i);
-        w.head0 = (int)c * p.pack; w.kv = w.head0 / p.group;
+        w.t = k.tile;
+        w.head0 = (int)k.sub * p.pack; w.kv = w.head0 / p.group;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const int first = w.t.at + x * tok;
@@ -119,8 +118,8 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 __syncwarp();
                 ring.next(nS); ++it;
             };
-            for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round) {
-                const Work w = work_of(item);
+            for (Walk walk(p.table, p.items, p.packs); walk.more && ok; walk.next()) {
+                const Work w = work_of(walk);
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     if (w.n[x] == 0 || !ok) continue;
@@ -164,8 +163,8 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 }
                 __syncwarp();
             };
-            for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round) {
-                const Work w = work_of(item);
+            for (Walk walk(p.table, p.items, p.packs); walk.more && ok; walk.next()) {
+                const Work w = work_of(walk);
                 const int n = max(w.n[0], w.n[1]);
                 if (!warp_wait(&bars->full[ring.slot], ring.parity, TO_MMA)) { ok = false; break; }
                 tc_fence_after();
@@ -246,8 +245,8 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             its = bars->swap[turn][x][half ^ 1][r];
             return met;
         };
-        for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round) {
-            const Work w = work_of(item);
+        for (Walk walk(p.table, p.items, p.packs); walk.more && ok; walk.next()) {
+            const Work w = work_of(walk);
             const int n = x ? w.n[1] : w.n[0];
             if (n == 0) continue;
             const int first = w.t.at + x * tok, at = first + my_tok;      // this row's token within its sequence

@@ -27,7 +27,7 @@ using namespace attn;
 namespace {
 
 constexpr int NTHREADS = 640;
-constexpr int SHARE = 3;                    // one in so many pairs of exponentials on the fp32 units
+constexpr int SHARE = 5;                    // one in so many pairs of exponentials on the fp32 units
 
 // Columns of step s (16 rows of the contraction) of a left operand in tensor memory that four groups of warps wrote, each over the first half of its own 32 columns.
 __device__ __forceinline__ constexpr uint32_t quarter_column(int s) { return (uint32_t)((s >> 1) * 32 + (s & 1) * 8); }
@@ -35,7 +35,7 @@ __device__ __forceinline__ constexpr uint32_t quarter_column(int s) { return (ui
 struct QueryParams {
     TileTable table;
     const __nv_bfloat16* out; const __nv_bfloat16* dout;
-    const float* lse; float* delta;
+    const float* lse; float* delta;         // (delta is kept negated)
     __nv_bfloat16* dq;
     int64_t ld_out, ld_dout, ld_dq;
     uint32_t items, packs;
@@ -45,12 +45,12 @@ struct QueryParams {
 };
 
 // Stages: tiles of keys and of values have rings of their own, for a tile of values is done with long before the keys beside it.
-template <int DB> struct QueryStages { static constexpr int K = DB == 1 ? 4 : 2, V = DB == 1 ? 3 : 1; };
+template <int DB> struct QueryStages { static constexpr int K = DB == 1 ? 4 : 3, V = DB == 1 ? 3 : 1; };
 
 template <int DB>
 struct __align__(16) QueryBars {
-    float lse[TILE], delta[TILE];           // of an item's rows: lse times log2 e, delta
-    uint64_t q_full[2], q_empty[2], k_full[QueryStages<DB>::K], k_empty[QueryStages<DB>::K], v_full[QueryStages<DB>::V], v_empty[QueryStages<DB>::V];
+    float lse[TILE], delta[TILE];           // of an item's rows, negated: lse times log2 e, delta
+    uint64_t q_full[2], q_empty[2], do_full, do_empty, k_full[QueryStages<DB>::K], k_empty[QueryStages<DB>::K], v_full[QueryStages<DB>::V], v_empty[QueryStages<DB>::V];
     uint64_t s_full[2], dp_full, ds_ready, dq_full, stat_full, drain;
     uint32_t tmem_base, abort_flag;
 };
@@ -60,14 +60,15 @@ struct __align__(16) QueryBars {
 template <int DB>
 __global__ void __launch_bounds__(NTHREADS, 1)
 attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_do, const __grid_constant__ CUtensorMap tm_k,
-                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ QueryParams p)
+                    const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_o, const __grid_constant__ QueryParams p)
 {
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     constexpr int OP = DB * 16384;
     constexpr uint32_t KS = QueryStages<DB>::K, VS = QueryStages<DB>::V;
-    uint8_t* q_smem = smem;                                  // twice: queries, the gradient of their outputs
-    uint8_t* k_smem = smem + 4 * OP;
+    uint8_t* q_smem = smem;                                  // queries of two items, the gradient of one's outputs
+    uint8_t* do_smem = smem + 2 * OP;
+    uint8_t* k_smem = smem + 3 * OP;
     uint8_t* v_smem = k_smem + KS * OP;
     QueryBars<DB>* bars = reinterpret_cast<QueryBars<DB>*>(v_smem + VS * OP);
     volatile uint32_t* abort_flag = &bars->abort_flag;
@@ -80,6 +81,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         for (uint32_t i = 0; i < VS; ++i) { mbar_init(smem_u32(&bars->v_full[i]), 1); mbar_init(smem_u32(&bars->v_empty[i]), 1); }
         mbar_init(smem_u32(&bars->dp_full), 1); mbar_init(smem_u32(&bars->ds_ready), 16); mbar_init(smem_u32(&bars->dq_full), 1);
         mbar_init(smem_u32(&bars->stat_full), 16); mbar_init(smem_u32(&bars->drain), 1);
+        mbar_init(smem_u32(&bars->do_full), 1); mbar_init(smem_u32(&bars->do_empty), 1);
         bars->abort_flag = 0;
         fence_barrier_init();
         prefetch_tmap(&tm_q); prefetch_tmap(&tm_do); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
@@ -97,11 +99,10 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         return __all_sync(0xFFFFFFFFu, w);
     };
     struct Work { AttnTile t; int head0, kv, n; };
-    auto work_of = [&](uint32_t item) {
+    auto work_of = [&](const Walk& k) {
         Work w;
-        const uint32_t i = item / p.packs, c = item - i * p.packs;
-        w.t = tile_at(p.table, i);
-        w.head0 = (int)c * p.pack; w.kv = w.head0 / p.group;
+        w.t = k.tile;
+        w.head0 = (int)k.sub * p.pack; w.kv = w.head0 / p.group;
         w.n = (min(w.t.at + tok, w.t.len) + TILE - 1) / TILE;
         return w;
     };
@@ -121,24 +122,36 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 }
                 __syncwarp();
             };
-            for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round, ++items) {
-                const Work w = work_of(item);
+            for (Walk walk(p.table, p.items, p.packs); walk.more && ok; walk.next(), ++items) {
+                const Work w = work_of(walk);
                 const uint32_t b2 = items & 1u;
                 if (!warp_wait(&bars->q_empty[b2], ((items >> 1) & 1u) ^ 1u, TO_PRODUCER)) { ok = false; break; }
                 if (elect_one()) {
-                    const uint32_t full = smem_u32(&bars->q_full[b2]), dst = smem_u32(q_smem + b2 * 2 * OP);
-                    mbar_arrive_expect_tx(full, 2 * OP);
+                    const uint32_t full = smem_u32(&bars->q_full[b2]), dst = smem_u32(q_smem + b2 * OP);
+                    mbar_arrive_expect_tx(full, OP);
 #pragma unroll
-                    for (int b = 0; b < DB; ++b) {
-                        tma_load_3d(dst + b * 16384, &tm_q, full, b * 64, w.head0, w.t.t0 + w.t.at);
-                        tma_load_3d(dst + OP + b * 16384, &tm_do, full, b * 64, w.head0, w.t.t0 + w.t.at);
-                    }
+                    for (int b = 0; b < DB; ++b) tma_load_3d(dst + b * 16384, &tm_q, full, b * 64, w.head0, w.t.t0 + w.t.at);
                 }
                 __syncwarp();
                 for (int j = 0; j < w.n; ++j, ++tiles) {
                     if (!warp_wait(&bars->k_empty[k_ring.slot], k_ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
                     load(&tm_k, &bars->k_full[k_ring.slot], k_smem + (size_t)k_ring.slot * OP, w.kv, w.t.t0 + j * TILE);
                     k_ring.next(KS);
+                    if (j == 0) {
+                        if (!warp_wait(&bars->do_empty, (items & 1u) ^ 1u, TO_PRODUCER)) { ok = false; break; }
+                        load(&tm_do, &bars->do_full, do_smem, w.head0, w.t.t0 + w.t.at);
+                        // the statistics of the next item's rows come out of L2
+                        const uint32_t item = item_of_round(walk.round + 1);
+                        if (item < p.items) {
+                            const AttnTile t = uniform_tile(walk.after);
+                            const int head0 = (int)(item - item / p.packs * p.packs) * p.pack;
+                            if (elect_one()) {
+#pragma unroll
+                                for (int b = 0; b < DB; ++b) { tma_prefetch_3d(&tm_o, b * 64, head0, t.t0 + t.at); tma_prefetch_3d(&tm_do, b * 64, head0, t.t0 + t.at); }
+                            }
+                            __syncwarp();
+                        }
+                    }
                     if (!warp_wait(&bars->v_empty[v_ring.slot], v_ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
                     load(&tm_v, &bars->v_full[v_ring.slot], v_smem + (size_t)v_ring.slot * OP, w.kv, w.t.t0 + j * TILE);
                     v_ring.next(VS);
@@ -147,6 +160,8 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             // behind a wait that gave up: what is still on its way arrives before the block leaves
             if (!ok) {
                 for (uint32_t i = items > 1 ? items - 1 : 0u; i <= items; ++i) mbar_wait_quiet(smem_u32(&bars->q_full[i & 1u]), (i >> 1) & 1u, 1u << 14);
+                if (items > 0) mbar_wait_quiet(smem_u32(&bars->do_full), (items - 1) & 1u, 1u << 14);
+                mbar_wait_quiet(smem_u32(&bars->do_full), items & 1u, 1u << 14);
                 for (uint32_t i = tiles > KS ? tiles - KS : 0u; i <= tiles; ++i) mbar_wait_quiet(smem_u32(&bars->k_full[i % KS]), (i / KS) & 1u, 1u << 14);
                 for (uint32_t i = tiles > VS ? tiles - VS : 0u; i < tiles; ++i) mbar_wait_quiet(smem_u32(&bars->v_full[i % VS]), (i / VS) & 1u, 1u << 14);
             }
@@ -162,14 +177,14 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 }
             };
             // A place in the sequence of tiles; the scores run one tile ahead of the rest.
-            struct Place { uint32_t round; Work w; int j; uint32_t items; };
+            struct Place { Work w; int j; uint32_t items; };
             Ring k_ring, k_use, v_ring;                      // keys for the scores, for dq; values
             uint32_t s_tiles = 0, tiles = 0;
             bool ok = true;
+            Walk walk(p.table, p.items, p.packs);
             Place ahead;
-            ahead.round = 0; ahead.j = 0; ahead.items = 0;
-            bool more = item_of_round(0) < p.items;          // is there a tile at `ahead`?
-            if (more) ahead.w = work_of(item_of_round(0));
+            ahead.j = 0; ahead.items = 0;
+            if (walk.more) ahead.w = work_of(walk);
             auto scores = [&]() -> bool {                    // of the tile at `ahead`: keys behind the sequence's end become zeros (they meet ds = 0 in dq)
                 const Place& a = ahead;
                 if (a.j == 0 && !warp_wait(&bars->q_full[a.items & 1u], (a.items >> 1) & 1u, TO_MMA)) return false;
@@ -178,8 +193,9 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 if (a.w.t.len - a.j * TILE < TILE) zero_rows(op, DB, a.w.t.len - a.j * TILE, lane);
                 tc_fence_after();
                 if (elect_one()) {
-                    product(tmem + (s_tiles & 1u) * 128, q_smem + (a.items & 1u) * 2 * OP, op);
+                    product(tmem + (s_tiles & 1u) * 128, q_smem + (a.items & 1u) * OP, op);
                     mma_commit(smem_u32(&bars->s_full[s_tiles & 1u]));
+                    if (a.j + 1 == a.w.n) mma_commit(smem_u32(&bars->q_empty[a.items & 1u]));
                 }
                 __syncwarp();
                 k_ring.next(KS);
@@ -187,39 +203,47 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 return true;
             };
             auto dps = [&](const Place& a) -> bool {
+                if (a.j == 0 && !warp_wait(&bars->do_full, a.items & 1u, TO_MMA)) return false;
                 if (!warp_wait(&bars->v_full[v_ring.slot], v_ring.parity, TO_MMA)) return false;
                 tc_fence_after();
                 if (elect_one()) {
-                    product(tmem + 256, q_smem + (a.items & 1u) * 2 * OP + OP, v_smem + (size_t)v_ring.slot * OP);
+                    product(tmem + 256, do_smem, v_smem + (size_t)v_ring.slot * OP);
                     mma_commit(smem_u32(&bars->dp_full));
                     mma_commit(smem_u32(&bars->v_empty[v_ring.slot]));
-                    if (a.j + 1 == a.w.n) mma_commit(smem_u32(&bars->q_empty[a.items & 1u]));      // (its scores were issued before)
+                    if (a.j + 1 == a.w.n) mma_commit(smem_u32(&bars->do_empty));
                 }
                 __syncwarp();
                 v_ring.next(VS);
                 return true;
             };
-            if (more) ok = scores() && dps(ahead);
-            while (more && ok) {
+            if (walk.more) ok = scores() && dps(ahead);
+            while (walk.more && ok) {
                 const Place now = ahead;
                 if (++ahead.j == ahead.w.n) {
-                    ahead.j = 0; ++ahead.items; ++ahead.round;
-                    more = item_of_round(ahead.round) < p.items;
-                    if (more) ahead.w = work_of(item_of_round(ahead.round));
+                    ahead.j = 0; ++ahead.items;
+                    walk.next();
+                    if (walk.more) ahead.w = work_of(walk);
                 }
+                const bool more = walk.more;
                 if (more && !scores()) { ok = false; break; }
                 if (!warp_wait(&bars->ds_ready, tiles & 1u, TO_MMA)) { ok = false; break; }
-                if (more && !dps(ahead)) { ok = false; break; }
+                const bool last = now.j + 1 == now.w.n;
                 tc_fence_after();
-                if (elect_one()) {
-                    const uint64_t b = make_smem_desc_mn_sw128(smem_u32(k_smem + (size_t)k_use.slot * OP), 16384);
-                    const uint32_t a = tmem + (tiles & 1u) * 128;
+                auto sums = [&]() {
+                    if (elect_one()) {
+                        const uint64_t b = make_smem_desc_mn_sw128(smem_u32(k_smem + (size_t)k_use.slot * OP), 16384);
+                        const uint32_t a = tmem + (tiles & 1u) * 128;
 #pragma unroll
-                    for (int s = 0; s < 8; ++s) mma_f16_ts(tmem + 384, a + quarter_column(s), b + (uint64_t)(s * 128), idesc_q, now.j > 0 || s > 0);
-                    mma_commit(smem_u32(&bars->k_empty[k_use.slot]));
-                    if (now.j + 1 == now.w.n) mma_commit(smem_u32(&bars->dq_full));
-                }
-                __syncwarp();
+                        for (int s = 0; s < 8; ++s) mma_f16_ts(tmem + 384, a + quarter_column(s), b + (uint64_t)(s * 128), idesc_q, now.j > 0 || s > 0);
+                        mma_commit(smem_u32(&bars->k_empty[k_use.slot]));
+                        if (last) mma_commit(smem_u32(&bars->dq_full));
+                    }
+                    __syncwarp();
+                };
+                // dp of the next tile first, for the other warps wait for it; an item's last dq before the next item's gradient has to be there
+                if (last) sums();
+                if (more && !dps(ahead)) { ok = false; break; }
+                if (!last) sums();
                 k_use.next(KS);
                 ++tiles;
             }
@@ -235,9 +259,9 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const uint64_t scale2 = pair_of(p.scale_log2, p.scale_log2);
         uint32_t tiles = 0, items = 0;
         bool ok = true;
-        // Statistics of an item's rows, eight to a warp: the lanes that share a row (8 or 16) read 16 bytes of out and of its gradient each, before the
-        // epilogue of the item in front; behind it they are added up and put down. One place will do: a warp comes here when the last tile's
-        // ds of every warp has arrived, so all have read what stood there.
+        // Statistics of an item's rows, eight to a warp: the lanes that share a row (8 or 16) read 16 bytes of out and of its gradient each (from L2, where
+        // the producer has had them brought) before the epilogue of the item in front; behind it they are added up and put down. One place will do: a warp
+        // comes here when the last tile's ds of every warp has arrived, so all have read what stood there.
         constexpr int LANES = 8 * DB, ROWS = 32 / LANES, PARTS = 8 / ROWS;
         const int sub = lane / LANES, c8 = (lane % LANES) * 8, stat_row = (warp - 4) * 8;
         uint4 o8[PARTS], d8[PARTS];
@@ -250,6 +274,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         auto fetch = [&](const Work& w) {
             int64_t token;
             int head;
+            if (lane < 8 && row_of(w, stat_row + lane, token, head)) lse1 = p.lse[token * p.heads + head];
 #pragma unroll
             for (int i = 0; i < PARTS; ++i) {
                 o8[i] = d8[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -258,7 +283,6 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     d8[i] = __ldg(reinterpret_cast<const uint4*>(p.dout + token * p.ld_dout + (int64_t)head * p.head_dim + c8));
                 }
             }
-            lse1 = lane < 8 && row_of(w, stat_row + lane, token, head) ? p.lse[token * p.heads + head] * LOG2E : 0.0f;
         };
         auto put_down = [&](const Work& w) {
 #pragma unroll
@@ -270,26 +294,28 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 for (int k = 0; k < 8; ++k) acc = fmaf(a[k], b[k], acc);
 #pragma unroll
                 for (int s = LANES / 2; s > 0; s >>= 1) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, s);
-                if (lane % LANES == 0) bars->delta[stat_row + i * ROWS + sub] = acc;
+                if (lane % LANES == 0) bars->delta[stat_row + i * ROWS + sub] = -acc;
             }
             __syncwarp();
             if (lane < 8) {
                 int64_t token;
                 int head;
-                bars->lse[stat_row + lane] = lse1;
-                if (row_of(w, stat_row + lane, token, head)) p.delta[token * p.heads + head] = bars->delta[stat_row + lane];
+                const bool there = row_of(w, stat_row + lane, token, head);
+                bars->lse[stat_row + lane] = there ? -lse1 * LOG2E : 0.0f;
+                if (there) p.delta[token * p.heads + head] = bars->delta[stat_row + lane];
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bars->stat_full));
         };
+        Walk walk(p.table, p.items, p.packs);
         Work w;
-        bool more = item_of_round(0) < p.items;
-        if (more) { w = work_of(item_of_round(0)); fetch(w); put_down(w); }
-        for (uint32_t round = 0; more && ok; ++round, ++items) {
+        bool more = walk.more;
+        if (more) { w = work_of(walk); fetch(w); put_down(w); }
+        for (; more && ok; ++items) {
             const int at = w.t.at + my_tok;
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->stat_full), items & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
             if (!ok) break;
-            const float off = -bars->lse[r], delta = -bars->delta[r];
+            const float off = bars->lse[r], delta = bars->delta[r];
             const uint64_t off2 = pair_of(off, off), delta2 = pair_of(delta, delta);
             for (int j = 0; j < w.n; ++j, ++tiles) {
                 const uint32_t buf = tiles & 1u, s_addr = tmem + lanes + buf * 128 + part * 32;
@@ -339,10 +365,10 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 if (lane == 0) mbar_arrive(smem_u32(&bars->ds_ready));
             }
             if (!ok) break;
-            const uint32_t item = item_of_round(round + 1);
-            more = item < p.items;
+            walk.next();
+            more = walk.more;
             Work next = w;
-            if (more) { next = work_of(item); fetch(next); }
+            if (more) { next = work_of(walk); fetch(next); }
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->dq_full), items & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
             if (!ok) break;
             tc_fence_after();
@@ -434,11 +460,10 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     };
     // loops: for every pass over `pack` heads of the group, the tiles of queries from the one that holds the first key's token on
     struct Work { AttnTile t; int kv, first, per, n; };
-    auto work_of = [&](uint32_t item) {
+    auto work_of = [&](const Walk& k) {
         Work w;
-        const uint32_t i = item / p.kv_heads;
-        w.kv = (int)(item - i * p.kv_heads);
-        w.t = tile_at(p.table, i);
+        w.kv = (int)k.sub;
+        w.t = k.tile;
         w.first = w.t.at >> (7 - p.pack_shift);
         w.per = ((w.t.len + tok - 1) >> (7 - p.pack_shift)) - w.first;
         w.n = w.per * passes;
@@ -451,8 +476,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             Ring ring;
             uint32_t it = 0, kv_uses = 0;
             bool ok = true;
-            for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round) {
-                const Work w = work_of(item);
+            for (Walk walk(p.table, p.items, p.kv_heads); walk.more && ok; walk.next()) {
+                const Work w = work_of(walk);
                 if (!warp_wait(&bars->kv_empty, (kv_uses++ & 1u) ^ 1u, TO_PRODUCER)) { ok = false; break; }
                 if (elect_one()) {
                     const uint32_t full = smem_u32(&bars->kv_full), dst = smem_u32(kv_smem);
@@ -503,8 +528,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 #pragma unroll
                 for (int s = 0; s < 8; ++s) mma_f16_ts(d, a + quarter_column(s), b + (uint64_t)(s * 128), idesc_g, more || s > 0);
             };
-            for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round) {
-                const Work w = work_of(item);
+            for (Walk walk(p.table, p.items, p.kv_heads); walk.more && ok; walk.next()) {
+                const Work w = work_of(walk);
                 if (!warp_wait(&bars->kv_full, kv_uses++ & 1u, TO_MMA)) { ok = false; break; }
                 int i = w.first, left = w.per;
                 // The tile's queries have arrived; rows behind the sequence's end become zeros in both operands (they meet P = dS = 0).
@@ -568,8 +593,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         } else {
             Ring ring;
             bool ok = true;
-            for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round) {
-                const Work w = work_of(item);
+            for (Walk walk(p.table, p.items, p.kv_heads); walk.more && ok; walk.next()) {
+                const Work w = work_of(walk);
                 int head0 = w.kv * p.group, i = w.first, left = w.per;
                 for (int j = 0; j < w.n; ++j, ring.next(KEY_STAGES)) {
                     float lse[2], delta[2];
@@ -579,7 +604,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         lse[h] = -INFINITY; delta[h] = 0.0f;
                         if (at < w.t.len) {
                             const int64_t row = (int64_t)(w.t.t0 + at) * p.heads + head0 + (r & (p.pack - 1));
-                            lse[h] = -p.lse[row] * LOG2E; delta[h] = -p.delta[row];
+                            lse[h] = -p.lse[row] * LOG2E; delta[h] = p.delta[row];
                         }
                     }
                     if (!warp_wait(&bars->stat_empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
@@ -603,8 +628,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         uint32_t uses = 0, done_uses = 0;
         Ring ring;
         bool ok = true;
-        for (uint32_t round = 0, item; (item = item_of_round(round)) < p.items && ok; ++round) {
-            const Work w = work_of(item);
+        for (Walk walk(p.table, p.items, p.kv_heads); walk.more && ok; walk.next()) {
+            const Work w = work_of(walk);
             const int key = w.t.at + r;
             int i = w.first, left = w.per;
             for (int j = 0; j < w.n; ++j, ++uses, ring.next(KEY_STAGES)) {
@@ -713,15 +738,15 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 }
 
 template <int DB>
-qless_status launch_backward(const CUtensorMap& q, const CUtensorMap& d, const CUtensorMap& k, const CUtensorMap& v, const QueryParams& qp, const KeyParams& kp, cudaStream_t st)
+qless_status launch_backward(const CUtensorMap& q, const CUtensorMap& d, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& o, const QueryParams& qp, const KeyParams& kp, cudaStream_t st)
 {
     const size_t op = (size_t)DB * 16384;
-    const size_t q_smem = 1024 + (4 + QueryStages<DB>::K + QueryStages<DB>::V) * op + sizeof(QueryBars<DB>), k_smem = 1024 + (2 + 2 * KeyStages<DB>::N) * op + sizeof(KeyBars<DB>);
-    static_assert(1024 + (4 + QueryStages<DB>::K + QueryStages<DB>::V) * DB * 16384 + sizeof(QueryBars<DB>) <= 227 * 1024 &&
+    const size_t q_smem = 1024 + (3 + QueryStages<DB>::K + QueryStages<DB>::V) * op + sizeof(QueryBars<DB>), k_smem = 1024 + (2 + 2 * KeyStages<DB>::N) * op + sizeof(KeyBars<DB>);
+    static_assert(1024 + (3 + QueryStages<DB>::K + QueryStages<DB>::V) * DB * 16384 + sizeof(QueryBars<DB>) <= 227 * 1024 &&
                   1024 + (2 + 2 * KeyStages<DB>::N) * DB * 16384 + sizeof(KeyBars<DB>) <= 227 * 1024, "shared memory of an SM");
     { ProfileScope ps("attention_dq", st);
       QLESS_CUDA_TRY((allow_full_smem<attention_dq_kernel<DB>>()));
-      QLESS_CUDA_TRY(launch_ahead(attention_dq_kernel<DB>, dim3((unsigned)std::min<int64_t>(qp.items, sm_count())), dim3(NTHREADS), q_smem, st, q, d, k, v, qp)); }
+      QLESS_CUDA_TRY(launch_ahead(attention_dq_kernel<DB>, dim3((unsigned)std::min<int64_t>(qp.items, sm_count())), dim3(NTHREADS), q_smem, st, q, d, k, v, o, qp)); }
     count_launches(1);
     { ProfileScope ps("attention_dkv", st);
       QLESS_CUDA_TRY((allow_full_smem<attention_dkv_kernel<DB>>()));
@@ -761,9 +786,10 @@ qless_status launch_attention_backward(const AttnArgs& a, uint8_t* ws, unsigned 
     qless_status s;
     if ((s = put_table(queries, &qp.table, q_list, st)) != QLESS_OK) return s;
     if ((s = put_table(keys, &kp.table, k_list, st)) != QLESS_OK) return s;
-    CUtensorMap q, d, k, v;
+    CUtensorMap q, d, k, v, o;
     if ((s = head_map(&q, a.q, a.ld_q, a.heads, a.head_dim, a.tokens, pack, tok)) != QLESS_OK) return s;
     if ((s = head_map(&d, a.dout, a.ld_dout, a.heads, a.head_dim, a.tokens, pack, tok)) != QLESS_OK) return s;
+    if ((s = head_map(&o, a.out_in, a.ld_out, a.heads, a.head_dim, a.tokens, pack, tok)) != QLESS_OK) return s;
     if ((s = head_map(&k, a.k, a.ld_k, a.kv_heads, a.head_dim, a.tokens, 1, TILE)) != QLESS_OK) return s;
     if ((s = head_map(&v, a.v, a.ld_v, a.kv_heads, a.head_dim, a.tokens, 1, TILE)) != QLESS_OK) return s;
     qp.out = reinterpret_cast<const __nv_bfloat16*>(a.out_in); qp.dout = reinterpret_cast<const __nv_bfloat16*>(a.dout); qp.lse = a.lse_in; qp.delta = delta;
@@ -773,7 +799,7 @@ qless_status launch_attention_backward(const AttnArgs& a, uint8_t* ws, unsigned 
     kp.lse = a.lse_in; kp.delta = delta; kp.dk = reinterpret_cast<__nv_bfloat16*>(a.dk); kp.dv = reinterpret_cast<__nv_bfloat16*>(a.dv);
     kp.ld_dk = a.ld_dk; kp.ld_dv = a.ld_dv; kp.kv_heads = a.kv_heads; kp.pack = pack; kp.pack_shift = shift; kp.group = qp.group; kp.heads = a.heads; kp.head_dim = a.head_dim;
     kp.items = (uint32_t)(keys.size() * a.kv_heads); kp.scale = a.scale; kp.scale_log2 = qp.scale_log2; kp.timeout_word = timeout_word;
-    return a.head_dim <= 64 ? launch_backward<1>(q, d, k, v, qp, kp, st) : launch_backward<2>(q, d, k, v, qp, kp, st);
+    return a.head_dim <= 64 ? launch_backward<1>(q, d, k, v, o, qp, kp, st) : launch_backward<2>(q, d, k, v, o, qp, kp, st);
 }
 
 }  // namespace qless

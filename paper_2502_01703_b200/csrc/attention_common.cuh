@@ -25,11 +25,8 @@ struct TileTable {
     AttnTile few[INLINE];
 };
 
-__device__ __forceinline__ AttnTile tile_at(const TileTable& t, int32_t i)
-{
-    const AttnTile x = t.list != nullptr ? t.list[i] : t.few[i];
-    return {warp_uniform(x.t0), warp_uniform(x.len), warp_uniform(x.at), warp_uniform(x.unused)};
-}
+__device__ __forceinline__ AttnTile tile_of(const TileTable& t, uint32_t i) { return t.list != nullptr ? t.list[i] : t.few[i]; }
+__device__ __forceinline__ AttnTile uniform_tile(const AttnTile& x) { return {warp_uniform(x.t0), warp_uniform(x.len), warp_uniform(x.at), warp_uniform(x.unused)}; }
 
 __device__ __forceinline__ float ex2(float x)
 {
@@ -109,6 +106,33 @@ __device__ __forceinline__ float max3(float a, float b, float c)      // NaN whe
 constexpr int64_t MOST_ITEMS = (int64_t)1 << 31;      // of a launch: counted in 32 bits
 // The block's item of round k: forwards and backwards in turn, so that the lists, which begin with the longest, come out even.
 __device__ __forceinline__ uint32_t item_of_round(uint32_t k) { return k * gridDim.x + ((k & 1u) ? gridDim.x - 1 - blockIdx.x : blockIdx.x); }
+// A role's way over the block's items (item = tile * per_tile + sub). The table's entry of the item after is read while this one is worked on.
+struct Walk {
+    const TileTable& table;
+    uint32_t items, per_tile, round = 0, item, sub = 0;
+    AttnTile tile, after;
+    bool more;
+    __device__ __forceinline__ Walk(const TileTable& t, uint32_t n, uint32_t per) : table(t), items(n), per_tile(per)
+    {
+        item = item_of_round(0);
+        more = item < items;
+        tile = after = AttnTile{0, 0, 0, 0};
+        if (more) { after = tile_of(table, item / per_tile); arrive(); }
+    }
+    __device__ __forceinline__ void arrive()
+    {
+        sub = item - item / per_tile * per_tile;
+        tile = uniform_tile(after);
+        const uint32_t next = item_of_round(round + 1);
+        if (next < items) after = tile_of(table, next / per_tile);
+    }
+    __device__ __forceinline__ void next()
+    {
+        item = item_of_round(++round);
+        more = item < items;
+        if (more) arrive();
+    }
+};
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
 {
