@@ -135,6 +135,19 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                     if (x == 0) load(&tm_k, w.kv, w.t.t0);
                 }
                 if (ok) load(&tm_v, w.kv, w.t.t0);
+                const uint32_t item = item_of_round(walk.round + 1);
+                if (item < p.items) {                        // the next item's queries come out of L2
+                    const AttnTile t = uniform_tile(walk.after);
+                    const int head0 = (int)(item - item / p.packs * p.packs) * p.pack;
+                    if (elect_one()) {
+#pragma unroll
+                        for (int b = 0; b < DB; ++b) {
+                            tma_prefetch_3d(&tm_q, b * 64, head0, t.t0 + t.at);
+                            if (t.unused == 0 && t.at + tok < t.len) tma_prefetch_3d(&tm_q, b * 64, head0, t.t0 + t.at + tok);
+                        }
+                    }
+                    __syncwarp();
+                }
                 const int n = max(w.n[0], w.n[1]);
                 for (int j = 1; j < n && ok; ++j) {
                     load(&tm_k, w.kv, w.t.t0 + j * TILE);

@@ -17,6 +17,7 @@
 // P and ds are rounded to bf16 (2^-9 of each, independent of each other); exponentials, differences and sums are fp32.
 // Bound: 128 x 128 scores cost three (dq) and four products of 512 clocks (head_dim 128) and 1024 clocks of the special-function units in each kernel.
 #include <algorithm>
+#include <type_traits>
 
 #include "attention_common.cuh"
 
@@ -341,24 +342,27 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 tmem_ld_x16(dp_addr, s[0]);
                 tmem_wait_ld();
                 tmem_ld_x16(dp_addr + 16, s[1]);
-                const bool masked = j * TILE + TILE - 1 > w.t.at;
-                const int lim = at - j * TILE - part * 32;   // this row's last key among the 32
+                auto form = [&](auto diagonal) {
+                    const int lim = at - j * TILE - part * 32;      // this row's last key among the 32
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (h == 1) tmem_wait_ld();
-                    uint32_t e[8];
+                    for (int h = 0; h < 2; ++h) {
+                        if (h == 1) tmem_wait_ld();
+                        uint32_t e[8];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        uint64_t ds = mul2(pr[h * 8 + k], add2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), delta2));
-                        if (masked) {
-                            float a, b;
-                            split_pair(ds, a, b);
-                            ds = pair_of(h * 16 + 2 * k > lim ? 0.0f : a, h * 16 + 2 * k + 1 > lim ? 0.0f : b);
+                        for (int k = 0; k < 8; ++k) {
+                            uint64_t ds = mul2(pr[h * 8 + k], add2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), delta2));
+                            if constexpr (diagonal.value) {
+                                float a, b;
+                                split_pair(ds, a, b);
+                                ds = pair_of(h * 16 + 2 * k > lim ? 0.0f : a, h * 16 + 2 * k + 1 > lim ? 0.0f : b);
+                            }
+                            e[k] = pack_pair(ds);
                         }
-                        e[k] = pack_pair(ds);
+                        tmem_st_x8(s_addr + h * 8, e);       // over this quarter's own scores
                     }
-                    tmem_st_x8(s_addr + h * 8, e);           // over this quarter's own scores
-                }
+                };
+                if (j * TILE + TILE - 1 > w.t.at) form(std::true_type{});
+                else form(std::false_type{});
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -408,13 +412,15 @@ struct KeyParams {
     unsigned int* timeout_word;
 };
 
-template <int DB> struct KeyStages { static constexpr int N = DB == 1 ? 4 : 2; };
+// A tile's dO is done with before its queries are, and is needed later: rings of their own.
+template <int DB> struct KeyStages { static constexpr int Q = DB == 1 ? 4 : 3, D = DB == 1 ? 4 : 2; };
+constexpr int LSE_STAGES = 2;               // (delta is needed half a tile later than lse: one place)
 
 template <int DB>
 struct __align__(16) KeyBars {
-    static constexpr int KEY_STAGES = KeyStages<DB>::N;
-    float lse[KEY_STAGES][TILE], delta[KEY_STAGES][TILE];      // of each query row, negated: lse times log2 e, delta
-    uint64_t kv_full, kv_empty, full[KEY_STAGES], empty[KEY_STAGES], stat_full[KEY_STAGES], stat_empty[KEY_STAGES], s_full, dp_full, p_ready, ds_ready, done, drain;
+    float lse[LSE_STAGES][TILE], delta[TILE];      // of each query row, negated: lse times log2 e, delta
+    uint64_t kv_full, kv_empty, q_full[KeyStages<DB>::Q], q_empty[KeyStages<DB>::Q], do_full[KeyStages<DB>::D], do_empty[KeyStages<DB>::D];
+    uint64_t lse_full[LSE_STAGES], lse_empty[LSE_STAGES], delta_full, delta_empty, s_full, dp_full, p_ready, ds_ready, done, drain;
     uint32_t tmem_base, abort_flag;
 };
 
@@ -427,19 +433,20 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     constexpr int OP = DB * 16384;
     uint8_t* kv_smem = smem;                                 // keys, values
-    uint8_t* ring_smem = smem + 2 * OP;                      // queries and the gradient of their outputs, KEY_STAGES times
-    constexpr int KEY_STAGES = KeyStages<DB>::N;
-    KeyBars<DB>* bars = reinterpret_cast<KeyBars<DB>*>(ring_smem + KEY_STAGES * 2 * OP);
+    constexpr uint32_t QS = KeyStages<DB>::Q, DS = KeyStages<DB>::D;
+    uint8_t* q_smem = smem + 2 * OP;                         // queries
+    uint8_t* do_smem = q_smem + QS * OP;                     // the gradient of their outputs
+    KeyBars<DB>* bars = reinterpret_cast<KeyBars<DB>*>(do_smem + DS * OP);
     volatile uint32_t* abort_flag = &bars->abort_flag;
     const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const int tok = TILE >> p.pack_shift, passes = p.group >> p.pack_shift;
 
     if (threadIdx.x == 0) {
         mbar_init(smem_u32(&bars->kv_full), 1); mbar_init(smem_u32(&bars->kv_empty), 1);
-        for (int i = 0; i < KEY_STAGES; ++i) {
-            mbar_init(smem_u32(&bars->full[i]), 1); mbar_init(smem_u32(&bars->empty[i]), 1);
-            mbar_init(smem_u32(&bars->stat_full[i]), 2); mbar_init(smem_u32(&bars->stat_empty[i]), 16);
-        }
+        for (uint32_t i = 0; i < QS; ++i) { mbar_init(smem_u32(&bars->q_full[i]), 1); mbar_init(smem_u32(&bars->q_empty[i]), 1); }
+        for (uint32_t i = 0; i < DS; ++i) { mbar_init(smem_u32(&bars->do_full[i]), 1); mbar_init(smem_u32(&bars->do_empty[i]), 1); }
+        for (int i = 0; i < LSE_STAGES; ++i) { mbar_init(smem_u32(&bars->lse_full[i]), 2); mbar_init(smem_u32(&bars->lse_empty[i]), 16); }
+        mbar_init(smem_u32(&bars->delta_full), 2); mbar_init(smem_u32(&bars->delta_empty), 16);
         mbar_init(smem_u32(&bars->s_full), 1); mbar_init(smem_u32(&bars->dp_full), 1); mbar_init(smem_u32(&bars->done), 1);
         mbar_init(smem_u32(&bars->p_ready), 16); mbar_init(smem_u32(&bars->ds_ready), 16); mbar_init(smem_u32(&bars->drain), 1);
         bars->abort_flag = 0;
@@ -473,9 +480,18 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 0) {
-            Ring ring;
-            uint32_t it = 0, kv_uses = 0;
+            Ring q_ring, do_ring;
+            uint32_t tiles = 0, kv_uses = 0;
             bool ok = true;
+            auto load = [&](const CUtensorMap* map, uint64_t* full_bar, uint8_t* dst_op, int head, int row) {
+                if (elect_one()) {
+                    const uint32_t full = smem_u32(full_bar), dst = smem_u32(dst_op);
+                    mbar_arrive_expect_tx(full, OP);
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) tma_load_3d(dst + b * 16384, map, full, b * 64, head, row);
+                }
+                __syncwarp();
+            };
             for (Walk walk(p.table, p.items, p.kv_heads); walk.more && ok; walk.next()) {
                 const Work w = work_of(walk);
                 if (!warp_wait(&bars->kv_empty, (kv_uses++ & 1u) ^ 1u, TO_PRODUCER)) { ok = false; break; }
@@ -489,30 +505,35 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     }
                 }
                 __syncwarp();
-                int head0 = w.kv * p.group, i = w.first, left = w.per;
-                for (int j = 0; j < w.n; ++j, ++it, ring.next(KEY_STAGES)) {
-                    if (!warp_wait(&bars->empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
+                const uint32_t item = item_of_round(walk.round + 1);
+                if (item < p.items) {                        // the next item's keys and values come out of L2
+                    const AttnTile t = uniform_tile(walk.after);
+                    const int kv = (int)(item - item / p.kv_heads * p.kv_heads);
                     if (elect_one()) {
-                        const uint32_t full = smem_u32(&bars->full[ring.slot]), dst = smem_u32(ring_smem + (size_t)ring.slot * 2 * OP);
-                        mbar_arrive_expect_tx(full, 2 * OP);
 #pragma unroll
-                        for (int b = 0; b < DB; ++b) {
-                            tma_load_3d(dst + b * 16384, &tm_q, full, b * 64, head0, w.t.t0 + i * tok);
-                            tma_load_3d(dst + OP + b * 16384, &tm_do, full, b * 64, head0, w.t.t0 + i * tok);
-                        }
+                        for (int b = 0; b < DB; ++b) { tma_prefetch_3d(&tm_k, b * 64, kv, t.t0 + t.at); tma_prefetch_3d(&tm_v, b * 64, kv, t.t0 + t.at); }
                     }
                     __syncwarp();
+                }
+                int head0 = w.kv * p.group, i = w.first, left = w.per;
+                for (int j = 0; j < w.n; ++j, ++tiles, q_ring.next(QS), do_ring.next(DS)) {
+                    if (!warp_wait(&bars->q_empty[q_ring.slot], q_ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
+                    load(&tm_q, &bars->q_full[q_ring.slot], q_smem + (size_t)q_ring.slot * OP, head0, w.t.t0 + i * tok);
+                    if (!warp_wait(&bars->do_empty[do_ring.slot], do_ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
+                    load(&tm_do, &bars->do_full[do_ring.slot], do_smem + (size_t)do_ring.slot * OP, head0, w.t.t0 + i * tok);
                     ++i;
                     if (--left == 0) { left = w.per; i = w.first; head0 += p.pack; }
                 }
             }
-            if (!ok)
-                for (uint32_t j = it > KEY_STAGES ? it - KEY_STAGES : 0u; j < it; ++j)
-                    if (!mbar_wait_quiet(smem_u32(&bars->full[j % KEY_STAGES]), (j / KEY_STAGES) & 1u, 1u << 14)) break;
+            if (!ok) {
+                for (uint32_t i = kv_uses > 1 ? kv_uses - 2 : 0u; i < kv_uses; ++i) mbar_wait_quiet(smem_u32(&bars->kv_full), i & 1u, 1u << 14);
+                for (uint32_t i = tiles > QS ? tiles - QS : 0u; i <= tiles; ++i) mbar_wait_quiet(smem_u32(&bars->q_full[i % QS]), (i / QS) & 1u, 1u << 14);
+                for (uint32_t i = tiles > DS ? tiles - DS : 0u; i < tiles; ++i) mbar_wait_quiet(smem_u32(&bars->do_full[i % DS]), (i / DS) & 1u, 1u << 14);
+            }
         } else if (warp == 1) {
             const uint32_t n_d = (uint32_t)((p.head_dim + 15) / 16 * 16), steps = n_d / 16;
             const uint32_t idesc_s = make_idesc(1, 1, 1, 128, 128), idesc_g = make_idesc(1, 1, 1, 128, n_d) | IDESC_B_MN;
-            Ring ring;
+            Ring q_ring, do_ring;
             uint32_t kv_uses = 0, p_uses = 0, ds_uses = 0;
             bool ok = true;
             auto product = [&](uint32_t d, const uint8_t* a_op, const uint8_t* b_op) {
@@ -531,52 +552,56 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             for (Walk walk(p.table, p.items, p.kv_heads); walk.more && ok; walk.next()) {
                 const Work w = work_of(walk);
                 if (!warp_wait(&bars->kv_full, kv_uses++ & 1u, TO_MMA)) { ok = false; break; }
-                int i = w.first, left = w.per;
-                // The tile's queries have arrived; rows behind the sequence's end become zeros in both operands (they meet P = dS = 0).
-                auto arrived = [&](const Ring& at) -> bool {
-                    if (!warp_wait(&bars->full[at.slot], at.parity, TO_MMA)) return false;
-                    const int have = (w.t.len - i * tok) * p.pack;
-                    uint8_t* op = ring_smem + (size_t)at.slot * 2 * OP;
-                    if (have < TILE) zero_rows(op, 2 * DB, have, lane);
+                int i = w.first, left = w.per, have = TILE;   // have: query rows of the tile at `q_ring` that are there
+                // The tile's queries (its dO) have arrived; rows behind the sequence's end become zeros in both operands (they meet P = dS = 0).
+                auto q_arrived = [&](const Ring& at) -> bool {
+                    if (!warp_wait(&bars->q_full[at.slot], at.parity, TO_MMA)) return false;
+                    have = (w.t.len - i * tok) << p.pack_shift;
+                    if (have < TILE) zero_rows(q_smem + (size_t)at.slot * OP, DB, have, lane);
                     ++i;
                     if (--left == 0) { left = w.per; i = w.first; }
                     tc_fence_after();
                     return true;
                 };
-                if (!arrived(ring)) { ok = false; break; }
+                auto do_arrived = [&](const Ring& at) -> bool {      // (of the same tile, behind its queries)
+                    if (!warp_wait(&bars->do_full[at.slot], at.parity, TO_MMA)) return false;
+                    if (have < TILE) zero_rows(do_smem + (size_t)at.slot * OP, DB, have, lane);
+                    tc_fence_after();
+                    return true;
+                };
+                if (!q_arrived(q_ring) || !do_arrived(do_ring)) { ok = false; break; }
                 if (elect_one()) {
-                    const uint8_t* op = ring_smem + (size_t)ring.slot * 2 * OP;
-                    product(tmem, kv_smem, op);
+                    product(tmem, kv_smem, q_smem + (size_t)q_ring.slot * OP);
                     mma_commit(smem_u32(&bars->s_full));
-                    product(tmem + 128, kv_smem + OP, op + OP);
+                    product(tmem + 128, kv_smem + OP, do_smem + (size_t)do_ring.slot * OP);
                     mma_commit(smem_u32(&bars->dp_full));
                     if (w.n == 1) mma_commit(smem_u32(&bars->kv_empty));
                 }
                 __syncwarp();
                 for (int j = 0; j < w.n && ok; ++j) {
-                    Ring next = ring;
-                    next.next(KEY_STAGES);
+                    Ring q_next = q_ring, do_next = do_ring;
+                    q_next.next(QS); do_next.next(DS);
                     const bool more = j + 1 < w.n;
-                    const uint8_t* op = ring_smem + (size_t)ring.slot * 2 * OP;
-                    const uint8_t* op1 = ring_smem + (size_t)next.slot * 2 * OP;
-                    if (more && !arrived(next)) { ok = false; break; }
+                    if (more && !q_arrived(q_next)) { ok = false; break; }
                     if (!warp_wait(&bars->p_ready, p_uses++ & 1u, TO_MMA)) { ok = false; break; }
                     tc_fence_after();
                     if (elect_one()) {
-                        gradient(tmem + 256, tmem, op + OP, j > 0);
+                        gradient(tmem + 256, tmem, do_smem + (size_t)do_ring.slot * OP, j > 0);
+                        mma_commit(smem_u32(&bars->do_empty[do_ring.slot]));
                         if (more) {
-                            product(tmem, kv_smem, op1);
+                            product(tmem, kv_smem, q_smem + (size_t)q_next.slot * OP);
                             mma_commit(smem_u32(&bars->s_full));
                         }
                     }
                     __syncwarp();
+                    if (more && !do_arrived(do_next)) { ok = false; break; }
                     if (!warp_wait(&bars->ds_ready, ds_uses++ & 1u, TO_MMA)) { ok = false; break; }
                     tc_fence_after();
                     if (elect_one()) {
-                        gradient(tmem + 384, tmem + 128, op, j > 0);
-                        mma_commit(smem_u32(&bars->empty[ring.slot]));
+                        gradient(tmem + 384, tmem + 128, q_smem + (size_t)q_ring.slot * OP, j > 0);
+                        mma_commit(smem_u32(&bars->q_empty[q_ring.slot]));
                         if (more) {
-                            product(tmem + 128, kv_smem + OP, op1 + OP);
+                            product(tmem + 128, kv_smem + OP, do_smem + (size_t)do_next.slot * OP);
                             mma_commit(smem_u32(&bars->dp_full));
                             if (j + 2 == w.n) mma_commit(smem_u32(&bars->kv_empty));
                         } else {
@@ -584,7 +609,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         }
                     }
                     __syncwarp();
-                    ring = next;
+                    q_ring = q_next; do_ring = do_next;
                 }
             }
             if (elect_one()) mma_commit(smem_u32(&bars->drain));
@@ -592,11 +617,12 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             mbar_wait_quiet(smem_u32(&bars->drain), 0u);
         } else {
             Ring ring;
+            uint32_t tiles = 0;
             bool ok = true;
             for (Walk walk(p.table, p.items, p.kv_heads); walk.more && ok; walk.next()) {
                 const Work w = work_of(walk);
                 int head0 = w.kv * p.group, i = w.first, left = w.per;
-                for (int j = 0; j < w.n; ++j, ring.next(KEY_STAGES)) {
+                for (int j = 0; j < w.n; ++j, ++tiles, ring.next(LSE_STAGES)) {
                     float lse[2], delta[2];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {            // rows behind the end: P = e^(0 - infinity) = 0, dS = 0
@@ -607,14 +633,16 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                             lse[h] = -p.lse[row] * LOG2E; delta[h] = p.delta[row];
                         }
                     }
-                    if (!warp_wait(&bars->stat_empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
+                    if (!warp_wait(&bars->lse_empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int r = (warp - 2) * 64 + h * 32 + lane;
-                        bars->lse[ring.slot][r] = lse[h]; bars->delta[ring.slot][r] = delta[h];
-                    }
+                    for (int h = 0; h < 2; ++h) bars->lse[ring.slot][(warp - 2) * 64 + h * 32 + lane] = lse[h];
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&bars->stat_full[ring.slot]));
+                    if (lane == 0) mbar_arrive(smem_u32(&bars->lse_full[ring.slot]));
+                    if (!warp_wait(&bars->delta_empty, (tiles & 1u) ^ 1u, TO_PRODUCER)) { ok = false; break; }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) bars->delta[(warp - 2) * 64 + h * 32 + lane] = delta[h];
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&bars->delta_full));
                     ++i;
                     if (--left == 0) { left = w.per; i = w.first; head0 += p.pack; }
                 }
@@ -632,13 +660,13 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             const Work w = work_of(walk);
             const int key = w.t.at + r;
             int i = w.first, left = w.per;
-            for (int j = 0; j < w.n; ++j, ++uses, ring.next(KEY_STAGES)) {
+            for (int j = 0; j < w.n; ++j, ++uses, ring.next(LSE_STAGES)) {
                 // column c of this quarter is query row part * 32 + c: token i * tok + (part * 32 + c) / pack; it sees this row's key from `from` on
                 const bool masked = i * tok < w.t.at + TILE - 1;
                 const int from = (key - i * tok) * p.pack - part * 32;
                 ++i;
                 if (--left == 0) { left = w.per; i = w.first; }
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->stat_full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_EPILOGUE));
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->lse_full[ring.slot]), ring.parity, abort_flag, p.timeout_word, TO_EPILOGUE));
                 if (!ok) break;
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->s_full), uses & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
                 if (!ok) break;
@@ -647,64 +675,74 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 uint64_t pr[16];
                 tmem_ld_x16(s_addr, s[0]);
                 const float4* lse = reinterpret_cast<const float4*>(&bars->lse[ring.slot][part * 32]);      // negated, like delta
-                const float4* delta = reinterpret_cast<const float4*>(&bars->delta[ring.slot][part * 32]);
+                const float4* delta = reinterpret_cast<const float4*>(&bars->delta[part * 32]);
                 tmem_wait_ld();
                 tmem_ld_x16(s_addr + 16, s[1]);
+                auto form_p = [&](auto diagonal) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (h == 1) tmem_wait_ld();
-                    uint32_t e[8];
+                    for (int h = 0; h < 2; ++h) {
+                        if (h == 1) tmem_wait_ld();
+                        uint32_t e[8];
 #pragma unroll
-                    for (int k = 0; k < 8; k += 2) {
-                        const float4 l = lse[(h * 8 + k) / 2];
-                        pr[h * 8 + k] = ex2_of<SHARE>(fma2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), scale2, pair_of(l.x, l.y)), h * 8 + k);
-                        pr[h * 8 + k + 1] = ex2_of<SHARE>(fma2(pair_of(__uint_as_float(s[h][2 * k + 2]), __uint_as_float(s[h][2 * k + 3])), scale2, pair_of(l.z, l.w)), h * 8 + k + 1);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        if (masked) {
-                            float a, b;
-                            split_pair(pr[h * 8 + k], a, b);
-                            pr[h * 8 + k] = pair_of(h * 16 + 2 * k < from ? 0.0f : a, h * 16 + 2 * k + 1 < from ? 0.0f : b);
+                        for (int k = 0; k < 8; k += 2) {
+                            const float4 l = lse[(h * 8 + k) / 2];
+                            pr[h * 8 + k] = ex2_of<SHARE>(fma2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), scale2, pair_of(l.x, l.y)), h * 8 + k);
+                            pr[h * 8 + k + 1] = ex2_of<SHARE>(fma2(pair_of(__uint_as_float(s[h][2 * k + 2]), __uint_as_float(s[h][2 * k + 3])), scale2, pair_of(l.z, l.w)), h * 8 + k + 1);
                         }
-                        e[k] = pack_pair(pr[h * 8 + k]);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            if constexpr (diagonal.value) {
+                                float a, b;
+                                split_pair(pr[h * 8 + k], a, b);
+                                pr[h * 8 + k] = pair_of(h * 16 + 2 * k < from ? 0.0f : a, h * 16 + 2 * k + 1 < from ? 0.0f : b);
+                            }
+                            e[k] = pack_pair(pr[h * 8 + k]);
+                        }
+                        tmem_st_x8(s_addr + h * 8, e);           // over this quarter's own scores
                     }
-                    tmem_st_x8(s_addr + h * 8, e);           // over this quarter's own scores
-                }
+                };
+                if (masked) form_p(std::true_type{});
+                else form_p(std::false_type{});
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bars->p_ready));
+                if (lane == 0) { mbar_arrive(smem_u32(&bars->p_ready)); mbar_arrive(smem_u32(&bars->lse_empty[ring.slot])); }
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->delta_full), uses & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
+                if (!ok) break;
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->dp_full), uses & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
                 if (!ok) break;
                 tc_fence_after();
                 tmem_ld_x16(dp_addr, s[0]);
                 tmem_wait_ld();
                 tmem_ld_x16(dp_addr + 16, s[1]);
+                auto form_ds = [&](auto diagonal) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (h == 1) tmem_wait_ld();
-                    uint32_t e[8];
+                    for (int h = 0; h < 2; ++h) {
+                        if (h == 1) tmem_wait_ld();
+                        uint32_t e[8];
 #pragma unroll
-                    for (int k = 0; k < 8; k += 2) {
-                        const float4 d = delta[(h * 8 + k) / 2];
-                        uint64_t a2 = mul2(pr[h * 8 + k], add2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), pair_of(d.x, d.y)));
-                        uint64_t b2 = mul2(pr[h * 8 + k + 1], add2(pair_of(__uint_as_float(s[h][2 * k + 2]), __uint_as_float(s[h][2 * k + 3])), pair_of(d.z, d.w)));
-                        if (masked) {
-                            float a, b;
-                            split_pair(a2, a, b);
-                            a2 = pair_of(h * 16 + 2 * k < from ? 0.0f : a, h * 16 + 2 * k + 1 < from ? 0.0f : b);
-                            split_pair(b2, a, b);
-                            b2 = pair_of(h * 16 + 2 * k + 2 < from ? 0.0f : a, h * 16 + 2 * k + 3 < from ? 0.0f : b);
+                        for (int k = 0; k < 8; k += 2) {
+                            const float4 d = delta[(h * 8 + k) / 2];
+                            uint64_t a2 = mul2(pr[h * 8 + k], add2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), pair_of(d.x, d.y)));
+                            uint64_t b2 = mul2(pr[h * 8 + k + 1], add2(pair_of(__uint_as_float(s[h][2 * k + 2]), __uint_as_float(s[h][2 * k + 3])), pair_of(d.z, d.w)));
+                            if constexpr (diagonal.value) {
+                                float a, b;
+                                split_pair(a2, a, b);
+                                a2 = pair_of(h * 16 + 2 * k < from ? 0.0f : a, h * 16 + 2 * k + 1 < from ? 0.0f : b);
+                                split_pair(b2, a, b);
+                                b2 = pair_of(h * 16 + 2 * k + 2 < from ? 0.0f : a, h * 16 + 2 * k + 3 < from ? 0.0f : b);
+                            }
+                            e[k] = pack_pair(a2); e[k + 1] = pack_pair(b2);
                         }
-                        e[k] = pack_pair(a2); e[k + 1] = pack_pair(b2);
+                        tmem_st_x8(dp_addr + h * 8, e);
                     }
-                    tmem_st_x8(dp_addr + h * 8, e);
-                }
+                };
+                if (masked) form_ds(std::true_type{});
+                else form_ds(std::false_type{});
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) { mbar_arrive(smem_u32(&bars->ds_ready)); mbar_arrive(smem_u32(&bars->stat_empty[ring.slot])); }
+                if (lane == 0) { mbar_arrive(smem_u32(&bars->ds_ready)); mbar_arrive(smem_u32(&bars->delta_empty)); }
             }
             if (!ok) break;
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->done), done_uses++ & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
@@ -741,9 +779,9 @@ template <int DB>
 qless_status launch_backward(const CUtensorMap& q, const CUtensorMap& d, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& o, const QueryParams& qp, const KeyParams& kp, cudaStream_t st)
 {
     const size_t op = (size_t)DB * 16384;
-    const size_t q_smem = 1024 + (3 + QueryStages<DB>::K + QueryStages<DB>::V) * op + sizeof(QueryBars<DB>), k_smem = 1024 + (2 + 2 * KeyStages<DB>::N) * op + sizeof(KeyBars<DB>);
+    const size_t q_smem = 1024 + (3 + QueryStages<DB>::K + QueryStages<DB>::V) * op + sizeof(QueryBars<DB>), k_smem = 1024 + (2 + KeyStages<DB>::Q + KeyStages<DB>::D) * op + sizeof(KeyBars<DB>);
     static_assert(1024 + (3 + QueryStages<DB>::K + QueryStages<DB>::V) * DB * 16384 + sizeof(QueryBars<DB>) <= 227 * 1024 &&
-                  1024 + (2 + 2 * KeyStages<DB>::N) * DB * 16384 + sizeof(KeyBars<DB>) <= 227 * 1024, "shared memory of an SM");
+                  1024 + (2 + KeyStages<DB>::Q + KeyStages<DB>::D) * DB * 16384 + sizeof(KeyBars<DB>) <= 227 * 1024, "shared memory of an SM");
     { ProfileScope ps("attention_dq", st);
       QLESS_CUDA_TRY((allow_full_smem<attention_dq_kernel<DB>>()));
       QLESS_CUDA_TRY(launch_ahead(attention_dq_kernel<DB>, dim3((unsigned)std::min<int64_t>(qp.items, sm_count())), dim3(NTHREADS), q_smem, st, q, d, k, v, o, qp)); }
