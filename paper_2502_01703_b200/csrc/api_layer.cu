@@ -84,8 +84,7 @@ extern "C" {
 size_t qless_layer_norm_backward_workspace(int64_t tokens, int32_t width, int32_t want_params)
 {
     if (check_norm(QLESS_F32, QLESS_F32, tokens, width) != QLESS_OK || tokens == 0) return 256;
-    const size_t narrow = plan_norm(tokens, width, 2, want_params != 0).total, wide = plan_norm(tokens, width, 4, want_params != 0).total;      // whatever the type
-    return narrow > wide ? narrow : wide;
+    return norm_most_workspace(tokens, width, want_params != 0);
 }
 
 qless_status qless_layer_norm(const void* x, qless_dtype dtype, int64_t tokens, int32_t width, int64_t ld_x, const void* weight, const void* bias,
@@ -125,11 +124,11 @@ qless_status qless_layer_norm_backward(const void* grad_out, int64_t ld_grad_out
                   "row strides must cover a row (ld_x=%lld, ld_grad_out=%lld, ld_grad_x=%lld)", (long long)ld_x, (long long)ld_grad_out, (long long)ld_grad_x);
     QLESS_REQUIRE(aligned(x, es) && aligned(grad_out, es) && aligned(grad_x, es) && aligned(weight, ps) && aligned(mean, 4) && aligned(rstd, 4), QLESS_ERR_INVALID_ARG,
                   "tensors must be aligned to their element type");
-    if (params) QLESS_STEP(check_workspace(workspace, workspace_bytes, plan_norm(tokens, width, (int32_t)es, true).total));
     NormArgs a{};
     a.x = x; a.dy = grad_out; a.weight = weight; a.out = grad_x; a.mean = const_cast<float*>(mean); a.rstd = const_cast<float*>(rstd);
     a.grad_weight = grad_weight; a.grad_bias = grad_bias; a.tokens = tokens; a.ld_x = ld_x; a.ld_dy = ld_grad_out; a.ld_out = ld_grad_x;
     a.width = width; a.center = center != 0; a.dtype = dtype; a.param_dtype = param_dtype;
+    if (params) QLESS_STEP(check_workspace(workspace, workspace_bytes, norm_workspace(a)));
     unsigned int* flag = timeout_flag_ptr();
     QLESS_REQUIRE(flag != nullptr, QLESS_ERR_CUDA, "cannot resolve the device timeout flag");
     return launch_norm_backward(a, reinterpret_cast<uint8_t*>(workspace), flag, st);

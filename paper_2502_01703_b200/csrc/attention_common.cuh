@@ -7,6 +7,7 @@
 
 #include <vector>
 
+#include "pairs.cuh"
 #include "qless_kernels.h"
 #include "tc_common.cuh"
 
@@ -33,32 +34,6 @@ __device__ __forceinline__ float ex2(float x)
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
-}
-// Two fp32 values in a register pair, for the instructions that work on both.
-__device__ __forceinline__ uint64_t pair_of(float a, float b)
-{
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void split_pair(uint64_t r, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
 }
 // 2^x of a pair on the fp32 units, for a share of the exponentials: the special-function units alone take 1024 clocks for a tile's 16384. Cody and Waite's
 // reduction x = n + r, |r| <= 1/2, by adding and subtracting 1.5 2^23; 2^r by the minimax polynomial of degree 5 (Remez exchange for the relative error

@@ -132,8 +132,6 @@ struct LossArgs {
 qless_status launch_loss(const LossArgs& a, const LossPlan& pl, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st);
 
 // Layer normalisation (layer_norm.cu).
-struct NormPlan { int32_t share, block, ring_stages; int64_t blocks, workers, ring_workers; size_t total; };      // elem: bytes of a value
-NormPlan plan_norm(int64_t tokens, int32_t width, int32_t elem, bool sums);
 struct NormArgs {
     const void* x; const void* dy; const void* weight; const void* bias;
     void* out; float* mean; float* rstd; void* grad_weight; void* grad_bias;
@@ -142,6 +140,8 @@ struct NormArgs {
     qless_dtype dtype, param_dtype;
     float eps;
 };
+size_t norm_workspace(const NormArgs& a);
+size_t norm_most_workspace(int64_t tokens, int32_t width, bool sums);       // of any types and addresses
 qless_status launch_norm_forward(const NormArgs& a, cudaStream_t st);
 qless_status launch_norm_backward(const NormArgs& a, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st);
 
