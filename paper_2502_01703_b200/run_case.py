@@ -5,8 +5,9 @@
     python -m paper_2502_01703_b200.run_case score    --N 20000 --V 448 --C 4 --d 8192 --bits 8     (16: the bf16 baseline)
     python -m paper_2502_01703_b200.run_case select   --N 67108864 --frac 0.05
     python -m paper_2502_01703_b200.run_case extract  --n 32 --tokens 16384 --width 2048 --vocab 32000 --rank 16 --d 1024 --bits 4
+    python -m paper_2502_01703_b200.run_case layer    --n 32 --tokens 16384 --width 2048 --heads 16 --kv-heads 4 --inner 5632 --rank 16 --d 1024 --bits 4
 
-Prints the CUDA-event time per iteration of the library call (extract: of each call).
+Prints the CUDA-event time per iteration of the library call (extract, layer: of each call).
 """
 import argparse
 
@@ -57,13 +58,108 @@ def extract(n, tokens, width, vocab, rank, d, bits, seed=1, group=32, scaling=2.
                 checkpoint=(codes, scales), loss=loss, grads=grads, store=store, ms=ms)
 
 
+def layer(n, tokens, width, heads, kv_heads, inner, vocab, rank, d, bits, seed=1, group=32, scaling=2.0, device="cuda"):
+    """`extract` through a whole decoder layer (random weights, adapters merged into them): every one of its projections is adapted.
+
+        y = x + attention(q, k, v) Wo^T,  [q k v] = norm(x) Wqkv^T;   z = y + ffn(norm(y));   logits = norm(z) head^T
+
+    The loss's gradient goes back through the head, the normalisations, the feed-forward block and attention; at each projection it meets the
+    8-bit checkpoint of the projection's input, and the rows of all adapters side by side are projected and quantised. Returns the inputs, every
+    intermediate result and the milliseconds of each library call."""
+    g = torch.Generator(device=device)
+    g.manual_seed(seed)
+    def rand(*shape, scale=1.0):
+        return (torch.randn(shape, generator=g, device=device) * scale).to(torch.bfloat16)
+    head_dim = width // heads
+    cuts = torch.randint(0, tokens + 1, (n - 1,), generator=g, device=device).sort().values.cpu()
+    offsets = torch.cat([torch.zeros(1, dtype=torch.int64), cuts, torch.tensor([tokens])])
+    sizes = dict(qkv=(width, (heads + 2 * kv_heads) * head_dim), o=(width, width), gate=(width, inner), up=(width, inner), down=(inner, width))
+    w = {k: rand(o, i, scale=i ** -0.5) for k, (i, o) in sizes.items()}
+    a = {k: rand(rank, i, scale=i ** -0.5) for k, (i, o) in sizes.items()}
+    b = {k: rand(o, rank, scale=0.05) for k, (i, o) in sizes.items()}
+    norms = [(1.0 + 0.1 * torch.randn(width, generator=g, device=device)).to(torch.bfloat16) for _ in range(3)]
+    head = rand(vocab, width, scale=2.0 * width ** -0.5)
+    x = rand(tokens, width)
+    labels = torch.randint(0, vocab, (tokens,), generator=g, device=device)
+    token_weight = torch.zeros(tokens, device=device)
+    for e in range(n):
+        lo, hi = int(offsets[e]), int(offsets[e + 1])
+        answer = lo + (hi - lo) // 2
+        labels[lo:answer] = -100
+        token_weight[answer:hi] = 1.0 / max(hi - answer, 1)
+
+    ms = {}
+    def timed(name, fn):
+        start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record()
+        out = fn()
+        end.record()
+        end.synchronize()
+        ms[name] = ms.get(name, 0.0) + start.elapsed_time(end)
+        return out
+    def keep(t):
+        return timed("qless_activation_quantize", lambda: B.qless_activation_quantize(t, group=group))
+    def norm(t, i):
+        return timed("qless_layer_norm", lambda: B.qless_layer_norm(t, norms[i], center=False))
+    def norm_back(dy, t, i, kept):
+        return timed("qless_layer_norm_backward", lambda: B.qless_layer_norm_backward(dy, t, norms[i], None, kept["rstd"]))["grad_x"]
+    saved = {}
+    n1 = norm(x, 0)
+    saved["qkv"] = keep(n1["out"])
+    qkv = n1["out"] @ w["qkv"].T
+    q, k, v = qkv.split([heads * head_dim, kv_heads * head_dim, kv_heads * head_dim], dim=1)
+    q, k, v = q.unflatten(1, (heads, head_dim)), k.unflatten(1, (kv_heads, head_dim)), v.unflatten(1, (kv_heads, head_dim))
+    att = timed("qless_attention", lambda: B.qless_attention(q, k, v, offsets))
+    mixed = att["out"].flatten(1)
+    saved["o"] = keep(mixed)
+    y = x + mixed @ w["o"].T
+    n2 = norm(y, 1)
+    saved["gate"] = saved["up"] = keep(n2["out"])
+    ffn = timed("qless_gated_ffn", lambda: B.qless_gated_ffn(n2["out"], w["gate"], w["up"], w["down"], want_saved=True))
+    saved["down"] = keep(ffn["hidden"])
+    z = y + ffn["out"]
+    n3 = norm(z, 2)
+    loss = timed("qless_lm_loss", lambda: B.qless_lm_loss(n3["out"], head, labels, token_weight=token_weight))
+
+    at = {}                                                  # gradients at the projections' outputs
+    dz = norm_back(loss["grad_hidden"], z, 2, n3)
+    at["down"] = dz
+    back = timed("qless_gated_ffn_backward", lambda: B.qless_gated_ffn_backward(dz, None, ffn["gate"], ffn["up"], w["gate"], w["up"], w["down"]))
+    at["gate"], at["up"] = back["grad_gate"], back["grad_up"]
+    dy = dz + norm_back(back["grad_x"], y, 1, n2)
+    at["o"] = dy
+    dmixed = (dy @ w["o"]).unflatten(1, (heads, head_dim))
+    at["qkv"] = torch.empty_like(qkv)
+    dq, dk, dv = at["qkv"].split([heads * head_dim, kv_heads * head_dim, kv_heads * head_dim], dim=1)
+    timed("qless_attention_backward", lambda: B.qless_attention_backward(
+        dmixed, q, k, v, att["out"], att["lse"], offsets,
+        grads=dict(grad_q=dq.unflatten(1, (heads, head_dim)), grad_k=dk.unflatten(1, (kv_heads, head_dim)), grad_v=dv.unflatten(1, (kv_heads, head_dim)))))
+    dx = dy + norm_back(at["qkv"] @ w["qkv"], x, 0, n1)
+
+    grads = torch.empty((n, sum(rank * (i + o) for i, o in sizes.values())), dtype=torch.bfloat16, device=device)
+    column = 0
+    places = {}
+    for name, (i, o) in sizes.items():
+        places[name] = slice(column, column + rank * (i + o))
+        column += rank * (i + o)
+        timed("qless_lora_gradients", lambda: B.qless_lora_gradients(*saved[name], at[name], a[name], b[name], offsets, scaling=scaling, group=group,
+                                                                    grads=grads[:, places[name]]))
+    store = timed("qless_project_quantize", lambda: B.qless_project_quantize(grads, d, 7, bits))
+    B.qless_check()
+    return dict(offsets=offsets, x=x, w=w, a=a, b=b, norms=norms, head=head, labels=labels, token_weight=token_weight, scaling=scaling, group=group, heads=heads,
+                kv_heads=kv_heads, checkpoints=saved, loss=loss, at=at, grad_x=dx, grads=grads, places=places, store=store, ms=ms)
+
+
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("stage", choices=["project", "quantize", "score", "select", "extract"])
+    ap.add_argument("stage", choices=["project", "quantize", "score", "select", "extract", "layer"])
     ap.add_argument("--tokens", type=int, default=16384)
     ap.add_argument("--width", type=int, default=2048)
     ap.add_argument("--vocab", type=int, default=32000)
     ap.add_argument("--rank", type=int, default=16)
+    ap.add_argument("--heads", type=int, default=16)
+    ap.add_argument("--kv-heads", type=int, default=4)
+    ap.add_argument("--inner", type=int, default=5632)
     ap.add_argument("--n", type=int, default=256)
     ap.add_argument("--N", type=int, default=20000)
     ap.add_argument("--V", type=int, default=448)
@@ -77,11 +173,12 @@ def main():
     ap.add_argument("--matrix", choices=["rademacher", "gaussian"], default="rademacher", help="random matrix of the projection")
     a = ap.parse_args()
     dev = "cuda"
-    if a.stage == "extract":
+    if a.stage in ("extract", "layer"):
         for _ in range(a.iters):
-            got = extract(a.n, a.tokens, a.width, a.vocab, a.rank, a.d, a.bits)
+            got = extract(a.n, a.tokens, a.width, a.vocab, a.rank, a.d, a.bits) if a.stage == "extract" else layer(
+                a.n, a.tokens, a.width, a.heads, a.kv_heads, a.inner, a.vocab, a.rank, a.d, a.bits)
         kept = int((got["labels"] >= 0).sum())
-        print(f"extract: {a.n} examples, {a.tokens} tokens ({kept} with a loss), mean loss {got['loss']['loss'].sum().item() / max(kept, 1):.4f}, "
+        print(f"{a.stage}: {a.n} examples, {a.tokens} tokens ({kept} with a loss), mean loss {got['loss']['loss'].sum().item() / max(kept, 1):.4f}, "
               f"{got['grads'].shape[1]} gradient entries each; " + ", ".join(f"{k} {v:.3f} ms" for k, v in got["ms"].items()))
         return
     if a.stage == "project":
