@@ -533,6 +533,12 @@ def _empty(rows, cols, dtype, device, stream):
     return _new((rows, cols), dtype, device, stream)
 
 
+def _line(n, dtype, device, stream):
+    if stream is None:
+        return torch.empty_strided((n,), (1,), dtype=dtype, device=device)
+    return _new(n, dtype, device, stream)
+
+
 def _dtype_of(dtype):
     if dtype == torch.float32:
         return F32
@@ -681,8 +687,8 @@ def qless_layer_norm(x, weight, bias=None, eps=1e-5, center=True, out=None, stre
         out = _empty(T, width, x.dtype, x.device, stream)
     elif out.shape != (T, width) or out.dtype != x.dtype:
         raise ValueError("out must be [tokens, width] of x's type")
-    stats = _empty(2 if center else 1, T, torch.float32, x.device, stream)
-    mean, rstd = (stats[0], stats[1]) if center else (None, stats[0])
+    mean = _line(T, torch.float32, x.device, stream) if center else None
+    rstd = _line(T, torch.float32, x.device, stream)
     if stream is not None:
         _used(stream, x, weight, bias, out)
     _check(lib().qless_layer_norm(x.data_ptr(), _dtype_code(x), T, width, _row_stride(x), weight.data_ptr(), _ptr(bias), _dtype_code(weight), eps,
@@ -709,8 +715,8 @@ def qless_layer_norm_backward(grad_out, x, weight, mean, rstd, want_weight=False
         grad_x = _empty(T, width, x.dtype, x.device, stream)
     elif grad_x.shape != (T, width) or grad_x.dtype != x.dtype:
         raise ValueError("grad_x must be [tokens, width] of x's type")
-    gw = _new(width, weight.dtype, x.device, stream) if want_weight else None
-    gb = _new(width, weight.dtype, x.device, stream) if want_bias else None
+    gw = _line(width, weight.dtype, x.device, stream) if want_weight else None
+    gb = _line(width, weight.dtype, x.device, stream) if want_bias else None
     ws = None
     if want_weight or want_bias:
         ws = _workspace(qless_layer_norm_backward_workspace(T, width), x.device, workspace, stream)
@@ -732,30 +738,38 @@ def _host_offsets(offsets):
 
 def _token_stride(t, name):
     """Elements between tokens of a bf16 [tokens, heads, head_dim] tensor whose heads lie side by side."""
-    if t.dtype != torch.bfloat16 or t.dim() != 3:
+    shape, stride = t.shape, t.stride()
+    if t.dtype != torch.bfloat16 or len(shape) != 3:
         raise TypeError(f"{name} must be bfloat16, [tokens, heads, head_dim]")
-    (T, h, d), (st, sh, sd) = t.shape, t.stride()
-    if (sd != 1 and d > 1) or (sh != d and h > 1):
+    T, h, d = shape
+    if (stride[2] != 1 and d > 1) or (stride[1] != d and h > 1):
         raise ValueError(f"the heads of a token of {name} must lie side by side")
-    return st if T > 1 else h * d
+    return stride[0] if T > 1 else h * d
 
 
-def _rows_like(shape, off, T, device, stream):
-    """A new bf16 output [tokens, heads, head_dim]; zeros where the examples leave tokens out, whose rows no kernel writes."""
-    t = _empty(T, shape[1] * shape[2], torch.bfloat16, device, stream)
-    _zero_outside(t, off, T, stream)
-    return t.view(shape)
+def _covers(off, T):
+    """Do the examples cover all tokens? (Read at the addresses of the first and last offset: indexing a tensor takes microseconds.)"""
+    at = off.data_ptr()
+    return C.c_int64.from_address(at).value == 0 and C.c_int64.from_address(at + 8 * (off.numel() - 1)).value == T
 
 
-def _zero_outside(t, off, T, stream):
-    lo, hi = int(off[0]), int(off[-1])
-    if lo == 0 and hi == T:
-        return
+def _heads_like(t, whole, stream):
+    """A new bf16 output of t's shape; zeros where the examples leave tokens out, whose rows no kernel writes."""
+    T, h, d = t.shape
+    if stream is None:
+        out = torch.empty_strided((T, h, d), (h * d, d, 1), dtype=torch.bfloat16, device=t.device)
+    else:
+        out = _new((T, h, d), torch.bfloat16, t.device, stream)
+    return out if whole else _zeroed(out, stream)
+
+
+def _zeroed(t, stream):
     if _elsewhere(stream):
         with torch.cuda.stream(stream):
             t.zero_()
     else:
         t.zero_()
+    return t
 
 
 def qless_attention_workspace(tokens, n, heads, kv_heads):
@@ -783,17 +797,21 @@ def qless_attention(q, k, v, offsets, scale=None, out=None, workspace=None, stre
     T, heads, kv, d = _heads_of(q, k, v)
     n = off.numel() - 1
     at = _on_gpu(stream, q, k, v, out, workspace)
+    whole = _covers(off, T)
     if out is None:
-        out = _rows_like(q.shape, off, T, q.device, stream)
+        out, so = _heads_like(q, whole, stream), heads * d
     elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
+    else:
+        so = _token_stride(out, "out")
     lse = _empty(T, heads, torch.float32, q.device, stream)
-    _zero_outside(lse, off, T, stream)
+    if not whole:
+        _zeroed(lse, stream)
     ws = _workspace(qless_attention_workspace(T, n, heads, kv), q.device, workspace, stream)
     if stream is not None:
         _used(stream, q, k, v, out, workspace)
     _check(lib().qless_attention(q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv, off.data_ptr(), T, n, heads, kv, d,
-                                 d ** -0.5 if scale is None else scale, out.data_ptr(), _token_stride(out, "out"), lse.data_ptr(), ws.data_ptr(), ws.numel(),
+                                 d ** -0.5 if scale is None else scale, out.data_ptr(), so, lse.data_ptr(), ws.data_ptr(), ws.numel(),
                                  _stream(stream, at)))
     return dict(out=out, lse=lse)
 
@@ -811,11 +829,12 @@ def qless_attention_backward(grad_out, q, k, v, out, lse, offsets, scale=None, g
     n = off.numel() - 1
     grads = grads or {}
     at = _on_gpu(stream, q, k, v, grad_out, out, lse, workspace, *grads.values())
+    whole = _covers(off, T)
     got = {}
     for name, like in (("grad_q", q), ("grad_k", k), ("grad_v", v)):
         t = grads.get(name)
         if t is None:
-            t = _rows_like(like.shape, off, T, q.device, stream)
+            t = _heads_like(like, whole, stream)
         elif t.shape != like.shape:
             raise ValueError(f"{name} has the wrong shape")
         got[name] = t

@@ -1,8 +1,10 @@
 // Gated feed-forward block with few tokens: the weights' bytes are the floor, so the weights stream past the tokens.
 //
 // Every product is D^T = weights x tokens^T with 128 of the weights' output features as the rows of a tile and all tokens (up to 256) as its columns: the tensor
-// core's work goes to tokens that exist, and a block reads its part of the weights once. Tiles are cut along the contraction until they fill the
-// SMs (slices: fp32 partial sums, which stay in L2); few_finish_kernel adds a result's slices in order and applies what follows the product. No atomics.
+// core's work goes to tokens that exist, and a block reads its part of the weights once. The stages of all tiles (128 of the contraction each), one tile behind
+// the other, are dealt out evenly: block c has stages c R .. (c + 1) R - 1, so every SM streams the same bytes whatever the sizes. A tile that
+// several blocks share is left as that many fp32 partial sums (they stay in L2); few_finish_kernel adds a tile's in order and applies what follows the
+// product. No atomics. (61 tokens x 4096 x 11008: tiles cut into equal slices 63 us, dealt out XXX; the weights' bytes take 41.)
 //   forward   [g; u] = [Wg; Wu] x^T, finish: h (g, u);   y = Wd h^T, finish: bf16
 //   backward  dh = Wd^T dy^T, finish: dg, du (h);   dx = Wg^T dg^T + Wu^T du^T, finish: bf16
 // Blocks are single CTAs: warp 0 TMA, warp 1 tcgen05, warps 2-5 epilogue; two accumulators in tensor memory.
@@ -24,10 +26,10 @@ enum { GLU = 0, GLU_BACK = 1, OUT = 2 };
 
 struct FewParams {
     int32_t tokens, feats, sets;            // sets: matrices that are multiplied side by side (Wg and Wu)
-    int32_t kblocks, kswitch;               // from block kswitch on: the second weights and the second tokens' operand
-    int32_t slices, per_slice, n_cols, stages;
-    float* part;                            // [slice][set][tokens][feats]
-    int64_t items;
+    int32_t kblocks, kswitch;               // stages of a tile; from kswitch on: the second weights and the second tokens' operand
+    int32_t n_cols, ring;                   // columns of a tile (the tokens, rounded up), places of the ring
+    int32_t all, per;                       // stages of all tiles, stages of a block
+    float* part;                            // [block's place among those that share the tile][set][tokens][feats]
     unsigned int* timeout_word;
 };
 
@@ -50,7 +52,7 @@ few_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const int b_half = p.n_cols * 128, stage_bytes = A_BYTES + 2 * b_half;      // (n_cols a multiple of 16: blocks stay on 1024-byte boundaries)
-    const uint32_t nS = (uint32_t)p.stages;
+    const uint32_t nS = (uint32_t)p.ring;
     Bars* bars = reinterpret_cast<Bars*>(smem + (size_t)nS * stage_bytes);
     volatile uint32_t* abort_flag = &bars->abort_flag;
     const int warp = warp_uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -71,14 +73,18 @@ few_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     ahead_wait();
     ahead_release();
 
-    const int tiles = (p.feats + 127) / 128;
-    auto item_of = [&](int64_t item, int& set, int& tile, int& slice, int& kb0, int& kb1) {
-        const int64_t r = item / p.slices;
-        slice = (int)(item - r * p.slices);
-        set = (int)(r / tiles);
-        tile = (int)(r - (int64_t)set * tiles);
-        kb0 = min(p.kblocks, slice * p.per_slice);
-        kb1 = min(p.kblocks, kb0 + p.per_slice);
+    const int tiles = (p.feats + 127) / 128, end = min(p.all, ((int)blockIdx.x + 1) * p.per);
+    // The block's piece of a tile that begins at stage `at`: stages kb0 .. kb1 - 1 of the tile.
+    struct Piece { int set, tile, place, kb0, kb1; };
+    auto piece_of = [&](int at) {
+        Piece x;
+        const int i = at / p.kblocks, begin = i * p.kblocks;
+        x.set = i / tiles;
+        x.tile = i - x.set * tiles;
+        x.place = (int)blockIdx.x - begin / p.per;
+        x.kb0 = at - begin;
+        x.kb1 = min(p.kblocks, end - begin);
+        return x;
     };
     auto warp_wait = [&](uint64_t* bar, uint32_t parity, uint32_t code) -> bool {
         const bool w = mbar_wait(smem_u32(bar), parity, abort_flag, p.timeout_word, code);
@@ -89,15 +95,15 @@ few_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
         Ring ring;
         uint32_t it = 0;
         bool ok = true;
-        for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
-            int set, tile, slice, kb0, kb1;
-            item_of(item, set, tile, slice, kb0, kb1);
-            for (int kb = kb0; kb < kb1; ++kb, ++it, ring.next(nS)) {
+        for (int at = blockIdx.x * p.per; at < end && ok;) {
+            const Piece x = piece_of(at);
+            at += x.kb1 - x.kb0;
+            for (int kb = x.kb0; kb < x.kb1; ++kb, ++it, ring.next(nS)) {
                 if (!warp_wait(&bars->empty[ring.slot], ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
                 const bool second = kb >= p.kswitch;
-                const CUtensorMap* mw = second || set ? &tm_w2 : &tm_w;
+                const CUtensorMap* mw = second || x.set ? &tm_w2 : &tm_w;
                 const CUtensorMap* mx = second ? &tm_x2 : &tm_x;
-                const int k0 = (second ? kb - p.kswitch : kb) * KB, f0 = tile * 128;
+                const int k0 = (second ? kb - p.kswitch : kb) * KB, f0 = x.tile * 128;
                 if (elect_one()) {
                     const uint32_t full = smem_u32(&bars->full[ring.slot]), a = smem_u32(smem + (size_t)ring.slot * stage_bytes), b = a + A_BYTES;
                     mbar_arrive_expect_tx(full, (uint32_t)stage_bytes);
@@ -116,13 +122,13 @@ few_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
         Ring ring;
         uint32_t n_acc = 0;
         bool ok = true;
-        for (int64_t item = blockIdx.x; item < p.items && ok; item += gridDim.x, ++n_acc) {
-            int set, tile, slice, kb0, kb1;
-            item_of(item, set, tile, slice, kb0, kb1);
+        for (int at = blockIdx.x * p.per; at < end && ok; ++n_acc) {
+            const Piece x = piece_of(at);
+            at += x.kb1 - x.kb0;
             const uint32_t buf = n_acc & 1u, d = tmem + buf * 256;
             if (!warp_wait(&bars->d_empty[buf], ((n_acc >> 1) & 1u) ^ 1u, TO_MMA)) { ok = false; break; }
             tc_fence_after();
-            for (int kb = kb0; kb < kb1; ++kb, ring.next(nS)) {
+            for (int kb = x.kb0; kb < x.kb1; ++kb, ring.next(nS)) {
                 if (!warp_wait(&bars->full[ring.slot], ring.parity, TO_MMA)) { ok = false; break; }
                 tc_fence_after();
                 if (elect_one()) {
@@ -131,7 +137,7 @@ few_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
 #pragma unroll
                     for (int k = 0; k < KB / 16; ++k)
                         mma_f16_ss(d, a0 + (uint64_t)(A_MN ? k * 128 : (k >> 2) * 1024 + (k & 3) * 2), b0 + (k >> 2) * b_next + (uint64_t)((k & 3) * 2), idesc,
-                                   kb > kb0 || k > 0);
+                                   kb > x.kb0 || k > 0);
                     mma_commit(smem_u32(&bars->empty[ring.slot]));
                 }
                 __syncwarp();
@@ -145,15 +151,15 @@ few_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
     } else {
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         uint32_t n_acc = 0;
-        for (int64_t item = blockIdx.x; item < p.items; item += gridDim.x, ++n_acc) {
-            int set, tile, slice, kb0, kb1;
-            item_of(item, set, tile, slice, kb0, kb1);
+        for (int at = blockIdx.x * p.per; at < end; ++n_acc) {
+            const Piece x = piece_of(at);
+            at += x.kb1 - x.kb0;
             const uint32_t buf = n_acc & 1u;
-            const int f = tile * 128 + (warp & 3) * 32 + lane;
+            const int f = x.tile * 128 + (warp & 3) * 32 + lane;
             const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->d_full[buf]), (n_acc >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
             if (!ok) break;
             tc_fence_after();
-            float* dst = p.part + ((int64_t)slice * p.sets + set) * p.tokens * p.feats + f;
+            float* dst = p.part + ((int64_t)x.place * p.sets + x.set) * p.tokens * p.feats + f;
 #pragma unroll 1
             for (int c0 = 0; c0 < p.tokens; c0 += 32) {
                 float v[32];
@@ -176,7 +182,7 @@ few_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
 
 struct FinishParams {
     const float* part;
-    int32_t tokens, feats, slices, act;
+    int32_t tokens, feats, act, kblocks, per;
     const __nv_bfloat16* gate_in; const __nv_bfloat16* up_in;
     __nv_bfloat16* out; __nv_bfloat16* out2; __nv_bfloat16* out3;      // GLU: h, g, u; GLU_BACK: dg, du, h; OUT: the result
     int64_t ld_gate_in, ld_up_in, ld, ld2, ld3;
@@ -200,13 +206,16 @@ __global__ void __launch_bounds__(256) few_finish_kernel(const FinishParams p)
         const int f = (int)(i - t * quads) * 4;
         constexpr int SETS = MODE == GLU ? 2 : 1;
         float v[2][4] = {};
-#pragma unroll 4
-        for (int s = 0; s < p.slices; ++s)
 #pragma unroll
-            for (int k = 0; k < SETS; ++k) {
+        for (int k = 0; k < SETS; ++k) {
+            const int first = (k * ((p.feats + 127) / 128) + f / 128) * p.kblocks;      // the tile's first stage
+            const int places = (first + p.kblocks - 1) / p.per - first / p.per + 1;
+#pragma unroll 4
+            for (int s = 0; s < places; ++s) {
                 const float4 y = *reinterpret_cast<const float4*>(p.part + ((int64_t)s * SETS + k) * plane + t * p.feats + f);
                 v[k][0] += y.x; v[k][1] += y.y; v[k][2] += y.z; v[k][3] += y.w;
             }
+        }
         if (MODE == OUT) {
             put(p.out + t * p.ld + f, v[0]);
         } else if (MODE == GLU) {
@@ -238,22 +247,15 @@ __global__ void __launch_bounds__(256) few_finish_kernel(const FinishParams p)
     }
 }
 
-struct Slices { int32_t slices, per; };
-
-// Along the contraction: the fewest rounds of blocks, counted in stages; an item costs its stages, one for its start, and the writing and reading
-// of its partial sums (tokens x 128 x 8 bytes, in stages of 32 KiB of weights).
-Slices slices_of(int64_t tokens, int64_t feats, int64_t sets, int64_t kblocks)
+// Stages of a block: an even share of all, at least two.
+struct Share { int32_t all, per, blocks, places; };
+Share share_of(int64_t feats, int64_t sets, int64_t kblocks)
 {
-    const int64_t sms = sm_count(), tiles = (feats + 127) / 128 * sets;
-    int64_t best = 1;
-    double best_cost = 0.0;
-    for (int64_t s = 1; s <= 32 && s <= (kblocks + 1) / 2; ++s) {
-        const int64_t per = (kblocks + s - 1) / s, rounds = (tiles * s + sms - 1) / sms;
-        const double cost = (double)rounds * ((double)per + 1.0 + (double)tokens / 32.0);
-        if (s == 1 || cost < best_cost) { best = s; best_cost = cost; }
-    }
-    const int64_t per = (kblocks + best - 1) / best;
-    return {(int32_t)((kblocks + per - 1) / per), (int32_t)per};
+    const int64_t all = (feats + 127) / 128 * sets * kblocks, sms = sm_count();
+    int64_t per = (all + sms - 1) / sms;
+    if (per < 2) per = 2;
+    // a tile of kblocks stages lies in at most so many blocks
+    return {(int32_t)all, (int32_t)per, (int32_t)((all + per - 1) / per), (int32_t)((kblocks + per - 2) / per + 1)};
 }
 
 int64_t blocks_of(int64_t k) { return (k + KB - 1) / KB; }
@@ -262,12 +264,13 @@ template <bool A_MN>
 qless_status product(const char* name, const CUtensorMap& w, const CUtensorMap& w2, const CUtensorMap& x, const CUtensorMap& x2, FewParams p, cudaStream_t st)
 {
     const size_t stage = A_BYTES + (size_t)p.n_cols * 256, budget = 227 * 1024 - 1024 - sizeof(Bars);
-    p.stages = (int32_t)std::min<size_t>(MAX_STAGES, budget / stage);
-    p.items = (int64_t)p.sets * ((p.feats + 127) / 128) * p.slices;
-    const size_t smem = 1024 + p.stages * stage + sizeof(Bars);
+    p.ring = (int32_t)std::min<size_t>(MAX_STAGES, budget / stage);
+    const size_t smem = 1024 + p.ring * stage + sizeof(Bars);
+    const Share s = share_of(p.feats, p.sets, p.kblocks);
+    p.all = s.all; p.per = s.per;
     ProfileScope ps(name, st);
     QLESS_CUDA_TRY((allow_full_smem<few_gemm_kernel<A_MN>>()));
-    QLESS_CUDA_TRY(launch_ahead(few_gemm_kernel<A_MN>, dim3((unsigned)std::min<int64_t>(p.items, sm_count())), dim3(NTHREADS), smem, st, w, w2, x, x2, p));
+    QLESS_CUDA_TRY(launch_ahead(few_gemm_kernel<A_MN>, dim3((unsigned)s.blocks), dim3(NTHREADS), smem, st, w, w2, x, x2, p));
     count_launches(1);
     return QLESS_OK;
 }
@@ -301,8 +304,8 @@ qless_status token_map(CUtensorMap* m, const void* p, int64_t cols, int64_t toke
 
 size_t few_workspace(int64_t tokens, int32_t width, int32_t inner, bool backward)
 {
-    const size_t first = backward ? (size_t)slices_of(tokens, inner, 1, blocks_of(width)).slices : (size_t)2 * slices_of(tokens, inner, 2, blocks_of(width)).slices;
-    const size_t second = (size_t)slices_of(tokens, width, 1, (backward ? 2 : 1) * blocks_of(inner)).slices;
+    const size_t first = backward ? (size_t)share_of(inner, 1, blocks_of(width)).places : (size_t)2 * share_of(inner, 2, blocks_of(width)).places;
+    const size_t second = (size_t)share_of(width, 1, (backward ? 2 : 1) * blocks_of(inner)).places;
     return align_up((size_t)tokens * 4 * std::max(first * inner, second * width), 256);
 }
 
@@ -317,18 +320,16 @@ qless_status launch_few_forward(const FfnArgs& a, uint8_t* ws, unsigned int* tim
     QLESS_STEP(weight_map(&wd, a.w_down, a.inner, a.width, a.ld_wd));
     FewParams p{};
     p.tokens = (int32_t)a.tokens; p.n_cols = n_cols; p.part = reinterpret_cast<float*>(ws); p.timeout_word = timeout_word;
-    Slices s = slices_of(a.tokens, a.inner, 2, blocks_of(a.width));
-    p.feats = a.inner; p.sets = 2; p.kblocks = p.kswitch = (int32_t)blocks_of(a.width); p.slices = s.slices; p.per_slice = s.per;
+    p.feats = a.inner; p.sets = 2; p.kblocks = p.kswitch = (int32_t)blocks_of(a.width);
     QLESS_STEP(product<false>("ffn_glu", wg, wu, x, x, p, st));
     FinishParams f{};
-    f.part = p.part; f.tokens = p.tokens; f.feats = a.inner; f.slices = s.slices; f.act = a.act;
+    f.part = p.part; f.tokens = p.tokens; f.feats = a.inner; f.act = a.act; f.kblocks = p.kblocks; f.per = share_of(p.feats, p.sets, p.kblocks).per;
     f.out = reinterpret_cast<__nv_bfloat16*>(a.hidden); f.out2 = reinterpret_cast<__nv_bfloat16*>(a.gate); f.out3 = reinterpret_cast<__nv_bfloat16*>(a.up);
     f.ld = a.ld_hidden; f.ld2 = a.ld_gate; f.ld3 = a.ld_up;
     QLESS_STEP(finish<GLU>(f, st));
-    s = slices_of(a.tokens, a.width, 1, blocks_of(a.inner));
-    p.feats = a.width; p.sets = 1; p.kblocks = p.kswitch = (int32_t)blocks_of(a.inner); p.slices = s.slices; p.per_slice = s.per;
+    p.feats = a.width; p.sets = 1; p.kblocks = p.kswitch = (int32_t)blocks_of(a.inner);
     QLESS_STEP(product<false>("ffn_down", wd, wd, h, h, p, st));
-    f.feats = a.width; f.slices = s.slices; f.out = reinterpret_cast<__nv_bfloat16*>(a.out); f.ld = a.ld_out;
+    f.feats = a.width; f.kblocks = p.kblocks; f.per = share_of(p.feats, p.sets, p.kblocks).per; f.out = reinterpret_cast<__nv_bfloat16*>(a.out); f.ld = a.ld_out;
     return finish<OUT>(f, st);
 }
 
@@ -344,11 +345,10 @@ qless_status launch_few_backward(const FfnArgs& a, __nv_bfloat16* hidden, uint8_
     QLESS_STEP(weight_map(&wd, a.w_down, a.inner, a.width, a.ld_wd));
     FewParams p{};
     p.tokens = (int32_t)a.tokens; p.n_cols = n_cols; p.sets = 1; p.part = reinterpret_cast<float*>(ws); p.timeout_word = timeout_word;
-    Slices s = slices_of(a.tokens, a.inner, 1, blocks_of(a.width));
-    p.feats = a.inner; p.kblocks = p.kswitch = (int32_t)blocks_of(a.width); p.slices = s.slices; p.per_slice = s.per;
+    p.feats = a.inner; p.kblocks = p.kswitch = (int32_t)blocks_of(a.width);
     QLESS_STEP(product<true>("ffn_glu_back", wd, wd, dy, dy, p, st));
     FinishParams f{};
-    f.part = p.part; f.tokens = p.tokens; f.feats = a.inner; f.slices = s.slices; f.act = a.act;
+    f.part = p.part; f.tokens = p.tokens; f.feats = a.inner; f.act = a.act; f.kblocks = p.kblocks; f.per = share_of(p.feats, p.sets, p.kblocks).per;
     f.gate_in = reinterpret_cast<const __nv_bfloat16*>(a.gate_in); f.up_in = reinterpret_cast<const __nv_bfloat16*>(a.up_in);
     f.ld_gate_in = a.ld_gate_in; f.ld_up_in = a.ld_up_in;
     f.out = reinterpret_cast<__nv_bfloat16*>(a.gate); f.out2 = reinterpret_cast<__nv_bfloat16*>(a.up); f.out3 = hidden;
@@ -356,10 +356,8 @@ qless_status launch_few_backward(const FfnArgs& a, __nv_bfloat16* hidden, uint8_
     QLESS_STEP(finish<GLU_BACK>(f, st));
     if (a.out == nullptr) return QLESS_OK;
     p.feats = a.width; p.kswitch = (int32_t)blocks_of(a.inner); p.kblocks = 2 * p.kswitch;
-    s = slices_of(a.tokens, a.width, 1, p.kblocks);
-    p.slices = s.slices; p.per_slice = s.per;
     QLESS_STEP(product<true>("ffn_grad_x", wg, wu, dg, du, p, st));
-    f.feats = a.width; f.slices = s.slices; f.out = reinterpret_cast<__nv_bfloat16*>(a.out); f.ld = a.ld_out;
+    f.feats = a.width; f.kblocks = p.kblocks; f.per = share_of(p.feats, p.sets, p.kblocks).per; f.out = reinterpret_cast<__nv_bfloat16*>(a.out); f.ld = a.ld_out;
     return finish<OUT>(f, st);
 }
 
