@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2502_01703_b200 import binding as B
-from test_layer_gpu import act64, attention_exact, attention_inputs, close, gen
+from test_layer_gpu import act64, attention_exact, attention_inputs, check_ffn_backward, check_ffn_forward, close, gen
 
 pytestmark = pytest.mark.gpu
 
@@ -145,12 +145,15 @@ def test_beyond_32_bits():
     wg, wu, wd = [(torch.randn(s, generator=g, device="cuda") / 8).to(torch.bfloat16) for s in ((F, W), (F, W), (W, F))]
     x = torch.zeros((T, W), dtype=torch.bfloat16, device="cuda")
     x[-512:] = torch.randn((512, W), generator=g, device="cuda").to(torch.bfloat16)
+    dy = torch.zeros_like(x)
+    dy[-512:] = torch.randn((512, W), generator=g, device="cuda").to(torch.bfloat16)
     big = B.qless_gated_ffn(x, wg, wu, wd, want_saved=True)
-    here = B.qless_gated_ffn(x[-512:], wg, wu, wd, want_saved=True)
-    assert big["hidden"].numel() > 1 << 31 and all(torch.equal(big[n][-512:], here[n]) for n in here) and not big["out"][:-512].any()
-    back = B.qless_gated_ffn_backward(x, None, big["gate"], big["up"], wg, wu, wd)
-    here = B.qless_gated_ffn_backward(x[-512:], None, here["gate"], here["up"], wg, wu, wd)
-    assert all(torch.equal(back[n][-512:], here[n]) for n in ("grad_x", "grad_gate", "grad_up"))
+    last = {n: t[-512:] for n, t in big.items()}
+    assert big["hidden"].numel() > 1 << 31 and not big["out"][:-512].any()
+    check_ffn_forward(last, x[-512:], wg, wu, wd, "silu")
+    back = B.qless_gated_ffn_backward(dy, None, big["gate"], big["up"], wg, wu, wd)
+    check_ffn_backward({n: t[-512:] if t is not None else None for n, t in back.items()}, dy[-512:], None, last["gate"], last["up"], wg, wu, wd, "silu")
+    del dy, last
     del big, back, x
     x = torch.zeros((140_000, 16384), dtype=torch.bfloat16, device="cuda")
     x[-3:] = torch.randn((3, 16384), generator=g, device="cuda").to(torch.bfloat16)
