@@ -247,6 +247,15 @@ def _workspace(nbytes, device, workspace, stream):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
+def _workspace_if(nbytes, device, workspace, stream):
+    """(pointer, size, tensor) of a call's workspace: none where it needs none."""
+    if workspace is None:
+        if nbytes == 0:
+            return None, 0, None
+        workspace = _workspace(nbytes, device, None, stream)
+    return workspace.data_ptr(), workspace.numel(), workspace
+
+
 def qless_last_error():
     return lib().qless_last_error().decode()
 
@@ -717,14 +726,12 @@ def qless_layer_norm_backward(grad_out, x, weight, mean, rstd, want_weight=False
         raise ValueError("grad_x must be [tokens, width] of x's type")
     gw = _line(width, weight.dtype, x.device, stream) if want_weight else None
     gb = _line(width, weight.dtype, x.device, stream) if want_bias else None
-    ws = None
-    if want_weight or want_bias:
-        ws = _workspace(qless_layer_norm_backward_workspace(T, width), x.device, workspace, stream)
+    ws, ws_bytes, _hold = _workspace_if(lib().qless_layer_norm_backward_workspace(T, width, 1) if want_weight or want_bias else 0, x.device, workspace, stream)
     if stream is not None:
         _used(stream, x, grad_out, weight, mean, rstd, grad_x, workspace)
     _check(lib().qless_layer_norm_backward(grad_out.data_ptr(), _row_stride(grad_out), x.data_ptr(), _dtype_code(x), T, width, _row_stride(x),
                                            weight.data_ptr(), _dtype_code(weight), 0 if mean is None else 1, _ptr(mean), rstd.data_ptr(),
-                                           grad_x.data_ptr(), _row_stride(grad_x), _ptr(gw), _ptr(gb), _ptr(ws), ws.numel() if ws is not None else 0,
+                                           grad_x.data_ptr(), _row_stride(grad_x), _ptr(gw), _ptr(gb), ws, ws_bytes,
                                            _stream(stream, at)))
     return dict(grad_x=grad_x, grad_weight=gw, grad_bias=gb)
 
@@ -807,11 +814,11 @@ def qless_attention(q, k, v, offsets, scale=None, out=None, workspace=None, stre
     lse = _empty(T, heads, torch.float32, q.device, stream)
     if not whole:
         _zeroed(lse, stream)
-    ws = _workspace(qless_attention_workspace(T, n, heads, kv), q.device, workspace, stream)
+    ws, ws_bytes, _hold = _workspace_if(lib().qless_attention_workspace(T, n, heads, kv), q.device, workspace, stream)
     if stream is not None:
         _used(stream, q, k, v, out, workspace)
     _check(lib().qless_attention(q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv, off.data_ptr(), T, n, heads, kv, d,
-                                 d ** -0.5 if scale is None else scale, out.data_ptr(), so, lse.data_ptr(), ws.data_ptr(), ws.numel(),
+                                 d ** -0.5 if scale is None else scale, out.data_ptr(), so, lse.data_ptr(), ws, ws_bytes,
                                  _stream(stream, at)))
     return dict(out=out, lse=lse)
 
@@ -838,7 +845,7 @@ def qless_attention_backward(grad_out, q, k, v, out, lse, offsets, scale=None, g
         elif t.shape != like.shape:
             raise ValueError(f"{name} has the wrong shape")
         got[name] = t
-    ws = _workspace(qless_attention_backward_workspace(T, n, heads, kv), q.device, workspace, stream)
+    ws, ws_bytes, _hold = _workspace_if(lib().qless_attention_backward_workspace(T, n, heads, kv), q.device, workspace, stream)
     if stream is not None:
         _used(stream, q, k, v, grad_out, out, lse, workspace, *got.values())
     args = []
@@ -847,7 +854,7 @@ def qless_attention_backward(grad_out, q, k, v, out, lse, offsets, scale=None, g
     args += [lse.data_ptr(), off.data_ptr(), T, n, heads, kv, d, d ** -0.5 if scale is None else scale]
     for name, t in got.items():
         args += [t.data_ptr(), _token_stride(t, name)]
-    _check(lib().qless_attention_backward(*args, ws.data_ptr(), ws.numel(), _stream(stream, at)))
+    _check(lib().qless_attention_backward(*args, ws, ws_bytes, _stream(stream, at)))
     return got
 
 
@@ -864,6 +871,12 @@ def _ffn_shapes(x, w_gate, w_up, w_down):
     return x.shape[0], width, inner
 
 
+def _bf16(t):
+    if t.dtype != torch.bfloat16:
+        raise TypeError("matrices must be bfloat16")
+    return t.data_ptr()
+
+
 def _bf16_args(*tensors):
     """Pointer and row stride of each bf16 matrix (None: absent)."""
     args = []
@@ -871,9 +884,7 @@ def _bf16_args(*tensors):
         if t is None:
             args += [None, 0]
             continue
-        if t.dtype != torch.bfloat16:
-            raise TypeError("matrices must be bfloat16")
-        args += [t.data_ptr(), _row_stride(t)]
+        args += [_bf16(t), _row_stride(t)]
     return args
 
 
@@ -905,15 +916,25 @@ def qless_gated_ffn(x, w_gate, w_up, w_down, activation="silu", want_saved=False
     input, gate, up [tokens, inner] | None: kept for the backward pass where want_saved). `out` may pass preallocated tensors by those names."""
     T, width, inner = _ffn_shapes(x, w_gate, w_up, w_down)
     code = _activation_code(activation)
-    keep = want_saved or bool(out and (out.get("gate") is not None or out.get("up") is not None))
-    at = _on_gpu(stream, x, w_gate, w_up, w_down, workspace, *(out or {}).values())
-    got = _outputs(out, dict(out=(True, T, width), hidden=(True, T, inner), gate=(keep, T, inner), up=(keep, T, inner)), x.device, stream)
-    ws = _workspace(qless_gated_ffn_workspace(T, width, inner), x.device, workspace, stream)
+    gate = up = None
+    if out is None:
+        at = _on_gpu(stream, x, w_gate, w_up, w_down, workspace)
+        dev = x.device
+        y, hidden = _empty(T, width, torch.bfloat16, dev, stream), _empty(T, inner, torch.bfloat16, dev, stream)
+        if want_saved:
+            gate, up = _empty(T, inner, torch.bfloat16, dev, stream), _empty(T, inner, torch.bfloat16, dev, stream)
+    else:
+        at = _on_gpu(stream, x, w_gate, w_up, w_down, workspace, *out.values())
+        keep = want_saved or out.get("gate") is not None or out.get("up") is not None
+        got = _outputs(out, dict(out=(True, T, width), hidden=(True, T, inner), gate=(keep, T, inner), up=(keep, T, inner)), x.device, stream)
+        y, hidden, gate, up = got["out"], got["hidden"], got["gate"], got["up"]
+    ws, ws_bytes, _hold = _workspace_if(lib().qless_gated_ffn_workspace(T, width, inner), x.device, workspace, stream)
     if stream is not None:
-        _used(stream, x, w_gate, w_up, w_down, workspace, *got.values())
-    _check(lib().qless_gated_ffn(*_bf16_args(x, w_gate, w_up, w_down), T, width, inner, code, *_bf16_args(*got.values()), ws.data_ptr(), ws.numel(),
+        _used(stream, x, w_gate, w_up, w_down, workspace, y, hidden, gate, up)
+    _check(lib().qless_gated_ffn(_bf16(x), _row_stride(x), _bf16(w_gate), _row_stride(w_gate), _bf16(w_up), _row_stride(w_up), _bf16(w_down), _row_stride(w_down),
+                                 T, width, inner, code, _bf16(y), _row_stride(y), _bf16(hidden), _row_stride(hidden), *_bf16_args(gate, up), ws, ws_bytes,
                                  _stream(stream, at)))
-    return got
+    return dict(out=y, hidden=hidden, gate=gate, up=up)
 
 
 def qless_gated_ffn_backward(grad_out, x, gate, up, w_gate, w_up, w_down, activation="silu", want_x=True, want_weight=False, grads=None,
@@ -929,11 +950,11 @@ def qless_gated_ffn_backward(grad_out, x, gate, up, w_gate, w_up, w_down, activa
     got = _outputs(grads, dict(grad_x=(want_x, T, width), grad_gate=(True, T, inner), grad_up=(True, T, inner), grad_w_gate=(want_weight, inner, width),
                                grad_w_up=(want_weight, inner, width), grad_w_down=(want_weight, width, inner)), grad_out.device, stream)
     weights = any(got[name] is not None for name in ("grad_w_gate", "grad_w_up", "grad_w_down"))
-    ws = _workspace(qless_gated_ffn_backward_workspace(T, width, inner, weights), grad_out.device, workspace, stream)
+    ws, ws_bytes, _hold = _workspace_if(lib().qless_gated_ffn_backward_workspace(T, width, inner, 1 if weights else 0), grad_out.device, workspace, stream)
     if stream is not None:
         _used(stream, grad_out, x, gate, up, w_gate, w_up, w_down, workspace, *got.values())
     _check(lib().qless_gated_ffn_backward(*_bf16_args(grad_out, x, gate, up, w_gate, w_up, w_down), T, width, inner, code, *_bf16_args(*got.values()),
-                                          ws.data_ptr(), ws.numel(), _stream(stream, at)))
+                                          ws, ws_bytes, _stream(stream, at)))
     return got
 
 

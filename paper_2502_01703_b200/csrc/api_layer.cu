@@ -11,6 +11,7 @@ static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_
 
 static qless_status check_workspace(const void* workspace, size_t given, size_t needed)
 {
+    if (needed == 0) return QLESS_OK;
     QLESS_REQUIRE(workspace != nullptr && aligned(workspace, 256), QLESS_ERR_WORKSPACE, "workspace must be non-NULL and 256-byte aligned");
     QLESS_REQUIRE(given >= needed, QLESS_ERR_WORKSPACE, "workspace too small: %zu bytes given, %zu needed", given, needed);
     return QLESS_OK;
@@ -83,7 +84,7 @@ extern "C" {
 
 size_t qless_layer_norm_backward_workspace(int64_t tokens, int32_t width, int32_t want_params)
 {
-    if (check_norm(QLESS_F32, QLESS_F32, tokens, width) != QLESS_OK || tokens == 0) return 256;
+    if (check_norm(QLESS_F32, QLESS_F32, tokens, width) != QLESS_OK || tokens == 0 || want_params == 0) return 0;
     return norm_most_workspace(tokens, width, want_params != 0);
 }
 
@@ -138,13 +139,13 @@ qless_status qless_layer_norm_backward(const void* grad_out, int64_t ld_grad_out
 
 size_t qless_attention_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads)
 {
-    if (check_heads(tokens, n, heads, kv_heads, 8) != QLESS_OK) return 256;
+    if (check_heads(tokens, n, heads, kv_heads, 8) != QLESS_OK) return 0;
     return attention_workspace(tokens, n, heads, kv_heads, false);
 }
 
 size_t qless_attention_backward_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads)
 {
-    if (check_heads(tokens, n, heads, kv_heads, 8) != QLESS_OK) return 256;
+    if (check_heads(tokens, n, heads, kv_heads, 8) != QLESS_OK) return 0;
     return attention_workspace(tokens, n, heads, kv_heads, true);
 }
 
@@ -214,13 +215,13 @@ qless_status qless_attention_backward(const void* grad_out, int64_t ld_grad_out,
 
 size_t qless_gated_ffn_workspace(int64_t tokens, int32_t width, int32_t inner)
 {
-    if (check_ffn(tokens, width, inner, QLESS_SILU) != QLESS_OK) return 256;
+    if (check_ffn(tokens, width, inner, QLESS_SILU) != QLESS_OK) return 0;
     return ffn_workspace(tokens, width, inner, false, false);
 }
 
 size_t qless_gated_ffn_backward_workspace(int64_t tokens, int32_t width, int32_t inner, int32_t want_weights)
 {
-    if (check_ffn(tokens, width, inner, QLESS_SILU) != QLESS_OK) return 256;
+    if (check_ffn(tokens, width, inner, QLESS_SILU) != QLESS_OK) return 0;
     return ffn_workspace(tokens, width, inner, true, want_weights != 0);
 }
 

@@ -793,16 +793,20 @@ qless_status launch_backward(const CUtensorMap& q, const CUtensorMap& d, const C
     return QLESS_OK;
 }
 
-size_t tiles_bytes(int64_t tokens, int64_t n, int64_t rows) { return align_up((size_t)(tokens / rows + n + 1) * sizeof(AttnTile), 256); }
+// Room for a table of tiles: none where all travel in the launch. (A sequence has at most one tile that is not full; sequences without tokens have none.)
+size_t tiles_bytes(int64_t tokens, int64_t n, int64_t rows)
+{
+    const int64_t most = tokens / rows + std::min(tokens, n);
+    return most <= INLINE ? 0 : align_up((size_t)most * sizeof(AttnTile), 256);
+}
 
 }  // namespace
 
 size_t attention_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads, bool backward)
 {
-    // a sequence has at most one tile that is not full; sequences without tokens have none
-    const int64_t seqs = std::min(tokens, n), tok = TILE / attn_pack(heads, kv_heads);
-    size_t total = tiles_bytes(tokens, seqs, tok) + 256;
-    if (backward) total += tiles_bytes(tokens, seqs, TILE) + align_up((size_t)tokens * heads * 4, 256);
+    const int64_t tok = TILE / attn_pack(heads, kv_heads);
+    size_t total = tiles_bytes(tokens, n, tok);
+    if (backward) total += tiles_bytes(tokens, n, TILE) + align_up((size_t)tokens * heads * 4, 256);
     return total;
 }
 
@@ -815,10 +819,9 @@ qless_status launch_attention_backward(const AttnArgs& a, uint8_t* ws, unsigned 
     QLESS_REQUIRE((int64_t)queries.size() * packs < MOST_ITEMS - 65536, QLESS_ERR_UNSUPPORTED, "too many tiles: %zu of %d heads", queries.size(), packs);
     int32_t shift = 0;
     while ((1 << shift) < pack) ++shift;
-    const int64_t seqs = std::min(a.tokens, a.n);
     AttnTile* q_list = reinterpret_cast<AttnTile*>(ws);
-    AttnTile* k_list = reinterpret_cast<AttnTile*>(ws + tiles_bytes(a.tokens, seqs, tok));
-    float* delta = reinterpret_cast<float*>(ws + tiles_bytes(a.tokens, seqs, tok) + tiles_bytes(a.tokens, seqs, TILE));
+    AttnTile* k_list = reinterpret_cast<AttnTile*>(ws + tiles_bytes(a.tokens, a.n, tok));
+    float* delta = reinterpret_cast<float*>(ws + tiles_bytes(a.tokens, a.n, tok) + tiles_bytes(a.tokens, a.n, TILE));
     QueryParams qp;
     KeyParams kp;
     qless_status s;

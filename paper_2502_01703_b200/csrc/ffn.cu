@@ -289,8 +289,8 @@ qless_status map(CUtensorMap* m, const void* p, int64_t cols, int64_t rows, int6
 
 size_t ffn_workspace(int64_t tokens, int32_t width, int32_t inner, bool backward, bool weights)
 {
-    if (tokens == 0) return 256;
-    size_t total = 256;
+    size_t total = 0;
+    if (tokens == 0) return total;
     if (weights) total += align_up((size_t)tokens * inner * 2, 256);      // h
     if (few_tokens(tokens)) total += few_workspace(tokens, width, inner, backward);
     return total;

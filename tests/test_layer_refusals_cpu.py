@@ -43,12 +43,14 @@ def test_layer_norm_refusals(L):
 
 
 def test_attention_refusals(L):
-    def attn(q=FAKE, ldq=512, k=FAKE, ldk=128, v=FAKE, ldv=128, off=(0, 3, 4), tokens=4, n=2, heads=8, kv=2, d=64, scale=0.125, out=FAKE, ldo=512, lse=FAKE,
+    many = tuple(range(0, 4001, 10))                         # so many tiles that a table is needed
+
+    def attn(q=FAKE, ldq=512, k=FAKE, ldk=128, v=FAKE, ldv=128, off=many, tokens=4000, n=400, heads=8, kv=2, d=64, scale=0.125, out=FAKE, ldo=512, lse=FAKE,
              ws=FAKE, wsb=0):
         o = (C.c_int64 * len(off))(*off) if off is not None else None
         return L.qless_attention(q, ldq, k, ldk, v, ldv, o, tokens, n, heads, kv, d, scale, out, ldo, lse, ws, wsb, None)
 
-    def back(dout=FAKE, lddo=512, q=FAKE, ldq=512, k=FAKE, ldk=128, v=FAKE, ldv=128, out=FAKE, ldo=512, lse=FAKE, off=(0, 3, 4), tokens=4, n=2, heads=8, kv=2, d=64,
+    def back(dout=FAKE, lddo=512, q=FAKE, ldq=512, k=FAKE, ldk=128, v=FAKE, ldv=128, out=FAKE, ldo=512, lse=FAKE, off=many, tokens=4000, n=400, heads=8, kv=2, d=64,
              scale=0.125, dq=FAKE, lddq=512, dk=FAKE, lddk=128, dv=FAKE, lddv=128, ws=FAKE, wsb=0):
         o = (C.c_int64 * len(off))(*off) if off is not None else None
         return L.qless_attention_backward(dout, lddo, q, ldq, k, ldk, v, ldv, out, ldo, lse, o, tokens, n, heads, kv, d, scale, dq, lddq, dk, lddk, dv, lddv, ws, wsb, None)
@@ -62,24 +64,24 @@ def test_attention_refusals(L):
         assert call(tokens=1 << 31) == B.ERR_UNSUPPORTED
         for bad in (0.0, -1.0, float("nan"), float("inf")):
             assert call(scale=bad) == B.ERR_INVALID_ARG
-        assert call(off=(0, 3, 5)) == B.ERR_INVALID_ARG and call(off=(-1, 3, 4)) == B.ERR_INVALID_ARG and call(off=None) == B.ERR_INVALID_ARG
-        assert call(off=(0, 4, 3)) == B.ERR_INVALID_ARG and b"decrease" in L.qless_last_error()
+        assert call(off=(0, 3, 5), n=2, tokens=4) == B.ERR_INVALID_ARG and call(off=(-1, 3, 4), n=2) == B.ERR_INVALID_ARG and call(off=None) == B.ERR_INVALID_ARG
+        assert call(off=(0, 4, 3), n=2) == B.ERR_INVALID_ARG and b"decrease" in L.qless_last_error()
         assert call(q=None) == B.ERR_INVALID_ARG and call(k=ODD) == B.ERR_INVALID_ARG and call(v=None) == B.ERR_INVALID_ARG and call(out=ODD) == B.ERR_INVALID_ARG
         assert call(ldq=504) == B.ERR_INVALID_ARG and call(ldk=132) == B.ERR_INVALID_ARG
-        assert call(n=0, off=None, q=None) == B.QLESS_OK and call(tokens=0, off=(0, 0, 0), q=None, ws=None) == B.QLESS_OK
+        assert call(n=0, off=None, q=None) == B.QLESS_OK and call(tokens=0, n=2, off=(0, 0, 0), q=None, ws=None) == B.QLESS_OK
     assert attn(lse=C.c_void_p(4098)) == B.ERR_INVALID_ARG
     assert back(lse=None) == B.ERR_INVALID_ARG and back(dq=None) == B.ERR_INVALID_ARG and back(lddk=120) == B.ERR_INVALID_ARG and back(dout=ODD) == B.ERR_INVALID_ARG
 
 
 def test_gated_ffn_refusals(L):
-    def ffn(x=FAKE, ldx=64, wg=FAKE, ldg=64, wu=FAKE, ldu=64, wd=FAKE, ldd=128, tokens=4, width=64, inner=128, act=B.SILU, out=FAKE, ldo=64, h=FAKE, ldh=128, gate=None,
+    def ffn(x=FAKE, ldx=2048, wg=FAKE, ldg=2048, wu=FAKE, ldu=2048, wd=FAKE, ldd=8192, tokens=4, width=2048, inner=8192, act=B.SILU, out=FAKE, ldo=2048, h=FAKE, ldh=8192, gate=None,
             up=None, ws=FAKE, wsb=0):
-        return L.qless_gated_ffn(x, ldx, wg, ldg, wu, ldu, wd, ldd, tokens, width, inner, act, out, ldo, h, ldh, gate, 128, up, 128, ws, wsb, None)
+        return L.qless_gated_ffn(x, ldx, wg, ldg, wu, ldu, wd, ldd, tokens, width, inner, act, out, ldo, h, ldh, gate, 8192, up, 8192, ws, wsb, None)
 
-    def back(dy=FAKE, ldy=64, x=None, ldx=0, gate=FAKE, ldgt=128, up=FAKE, ldup=128, wg=FAKE, wu=FAKE, wd=FAKE, tokens=4, width=64, inner=128, act=B.GELU, dx=FAKE, lddx=64,
+    def back(dy=FAKE, ldy=2048, x=None, ldx=0, gate=FAKE, ldgt=8192, up=FAKE, ldup=8192, wg=FAKE, wu=FAKE, wd=FAKE, tokens=4, width=2048, inner=8192, act=B.GELU, dx=FAKE, lddx=2048,
              dg=FAKE, du=FAKE, dwg=None, dwu=None, dwd=None, ws=FAKE, wsb=0):
-        return L.qless_gated_ffn_backward(dy, ldy, x, ldx, gate, ldgt, up, ldup, wg, 64, wu, 64, wd, 128, tokens, width, inner, act, dx, lddx, dg, 128, du, 128, dwg, 64,
-                                          dwu, 64, dwd, 128, ws, wsb, None)
+        return L.qless_gated_ffn_backward(dy, ldy, x, ldx, gate, ldgt, up, ldup, wg, 2048, wu, 2048, wd, 8192, tokens, width, inner, act, dx, lddx, dg, 8192, du, 8192, dwg, 2048,
+                                          dwu, 2048, dwd, 8192, ws, wsb, None)
 
     for call in (ffn, back):
         assert call() == B.ERR_WORKSPACE and call(ws=ODD, wsb=1 << 30) == B.ERR_WORKSPACE and call(ws=None, wsb=1 << 30) == B.ERR_WORKSPACE
@@ -88,7 +90,7 @@ def test_gated_ffn_refusals(L):
         assert call(tokens=(1 << 31) - 256) == B.ERR_UNSUPPORTED
         assert call(wg=None) == B.ERR_INVALID_ARG and call(wu=ODD) == B.ERR_INVALID_ARG and call(wd=None) == B.ERR_INVALID_ARG
         assert call(tokens=0, wg=None, wd=None) == B.QLESS_OK
-    assert ffn(x=None) == B.ERR_INVALID_ARG and ffn(h=None) == B.ERR_INVALID_ARG and ffn(ldx=60) == B.ERR_INVALID_ARG and ffn(ldh=124) == B.ERR_INVALID_ARG
+    assert ffn(x=None) == B.ERR_INVALID_ARG and ffn(h=None) == B.ERR_INVALID_ARG and ffn(ldx=2040) == B.ERR_INVALID_ARG and ffn(ldh=8196) == B.ERR_INVALID_ARG
     assert ffn(gate=FAKE) == B.ERR_INVALID_ARG and b"together" in L.qless_last_error() and ffn(up=FAKE) == B.ERR_INVALID_ARG
     assert back(gate=None) == B.ERR_INVALID_ARG and back(dg=None) == B.ERR_INVALID_ARG and back(dx=ODD) == B.ERR_INVALID_ARG and back(dy=None) == B.ERR_INVALID_ARG
     assert back(dwu=FAKE) == B.ERR_INVALID_ARG and b"x is required" in L.qless_last_error()
@@ -127,11 +129,13 @@ def test_binding_refusals():
         B.qless_layer_norm_backward(bf(5, 64).float(), bf(5, 64), bf(64), None, torch.zeros(5))
 
 
-def test_workspaces_of_shapes_that_are_refused_and_of_large_ones():
-    assert B.qless_attention_workspace(-1, 1, 8, 2) == 256 and B.qless_gated_ffn_workspace(4, 60, 128) == 256
+def test_workspaces():
+    assert B.qless_attention_workspace(-1, 1, 8, 2) == 0 and B.qless_gated_ffn_workspace(4, 60, 128) == 0 and B.qless_layer_norm_backward_workspace(4, 20000) == 0
+    assert B.qless_layer_norm_backward_workspace(4, 64, False) == 0 and B.qless_layer_norm_backward_workspace(4, 64) >= 4 * 2 * 64 * 4
     # tables of tiles: 32 tokens to a tile of four heads, one more for every example; lse and delta's rows
     assert B.qless_attention_workspace(1 << 20, 100, 32, 8) >= ((1 << 15) + 100) * 16
     assert B.qless_attention_backward_workspace(1 << 20, 100, 32, 8) >= (1 << 20) * 32 * 4
-    assert B.qless_attention_workspace(10, 1 << 20, 32, 8) < 1 << 12            # examples without tokens need none
-    assert B.qless_gated_ffn_workspace(0, 4096, 11008) == 256 and B.qless_gated_ffn_workspace(64, 4096, 11008) >= 64 * 11008 * 4
+    assert B.qless_attention_workspace(10, 1 << 20, 32, 8) == 0                  # examples without tokens need none, few tiles travel in the launch
+    assert B.qless_gated_ffn_workspace(0, 4096, 11008) == 0 and B.qless_gated_ffn_workspace(64, 4096, 11008) >= 64 * 11008 * 4
+    assert B.qless_gated_ffn_workspace(5, 512, 1376) == 0
     assert B.qless_gated_ffn_backward_workspace(4096, 2048, 5632, True) >= 4096 * 5632 * 2
