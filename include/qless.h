@@ -465,9 +465,10 @@ qless_status qless_layer_norm_backward(const void* grad_out, int64_t ld_grad_out
  * they were. Scores, exponentials, sums and out's accumulators are fp32; probabilities enter the second product rounded to bf16.
  * An infinity or NaN in one example's rows reaches that example's rows only (within it, also rows before it that share its tile of 128 keys).
  * qless_attention_backward: grad_out, out, lse as above (lse not NULL) ->
- *   delta_i = <grad_out_i, out_i>;  ds_ij = p_ij (<grad_out_i, v_j> - delta_i);  grad_q_i = scale sum_j ds_ij k_j;
+ *   dp_ij = <grad_out_i, v_j>;  delta_i = sum_j p_ij dp_ij;  ds_ij = p_ij (dp_ij - delta_i);  grad_q_i = scale sum_j ds_ij k_j;
  *   grad_k_j = scale sum_i ds_ij q_i,  grad_v_j = sum_i p_ij grad_out_i   (sums over i and the query heads of the group)
- * with p and ds rounded to bf16 in these products, fp32 sums, and one rounding of each result to bf16.
+ * with p and ds rounded to bf16 in these products, fp32 sums, and one rounding of each result to bf16. <grad_out_i, out_i> is the first estimate of delta_i,
+ * whose error (out is rounded) is found and taken out of all results.
  * Requirements: tokens < 2^31; head_dim a multiple of 8, at most 128; heads a multiple of kv_heads, heads <= 4096; scale finite and positive; tensors
  * 16-byte aligned, their row strides multiples of 8. */
 size_t qless_attention_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads);

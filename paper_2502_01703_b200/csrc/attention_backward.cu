@@ -5,17 +5,22 @@
 //
 // Two kernels, each with its sums in tensor memory from the first product to the last: one owns a tile of query rows and walks over the keys
 // (dq, and delta for the other), one owns a tile of keys and walks over the query rows of every head of its group (dk, dv). Scores and dp are
-// computed in both: seven products of a tile instead of five, and in return no partial dq is added up in memory, nothing is
+// computed in both (seven products of a tile instead of five, and the eighth of kbar below), and in return no partial dq is added up in memory, nothing is
 // joined by atomics, and the same inputs give the same bits.
 //
-// dq kernel, tensor memory: S twice (of this tile of keys and the next), dp, dq: 4 x 128 columns; ds, rounded to bf16, replaces S.
-// dk/dv kernel: S^T = K Q^T and dp^T = V dO^T, so that P^T and dS^T are left operands of the products that follow and stay in tensor memory
-// (rounded to bf16 in the place of S^T and dp^T), and dv, dk: 4 x 128 columns. While the threads take exponentials of one tile the tensor core
-// works on dp and dk, while they form ds it works on dv and the next scores.
+// delta taken from the output as it was handed on, in bf16, would be off by up to 2^-8 of |do| |o|, and with rows that look at few keys (|o| near |v|, ds small)
+// that is more than all other roundings together: errors of 3e-3 to 4.4e-3 of the gradients' norm were seen where 2.4e-3 are due to bf16 operands and
+// results. But sum_j ds_ij = 0 when delta is exact, so the row sum of what is formed with the rough delta, rho_i = sum_j ds_ij (fp32, before rounding), is delta's
+// error: the dq kernel also sums kbar_i = sum_j p_ij k_j and returns scale (sum_j ds_ij k_j - rho_i kbar_i), and hands delta_i + rho_i to the other kernel.
+//
+// dq kernel, tensor memory: S, dp, dq, kbar: 4 x 128 columns; P and ds, rounded to bf16, replace S and dp. While the threads take exponentials of one tile
+// the tensor core works on dq and the next dp, while they form ds it works on kbar and the next scores.
+// dk/dv kernel, in the same order: S^T = K Q^T and dp^T = V dO^T, so that P^T and dS^T are left operands of the products that follow and stay in
+// tensor memory, and dv, dk.
 // Sixteen warps do the arithmetic, each 32 rows by a quarter of the columns; warp 0 brings tiles by TMA, warp 1 issues products, warps 2 and 3 bring
 // lse and delta of the query rows (dk/dv kernel).
 // P and ds are rounded to bf16 (2^-9 of each, independent of each other); exponentials, differences and sums are fp32.
-// Bound: 128 x 128 scores cost three (dq) and four products of 512 clocks (head_dim 128) and 1024 clocks of the special-function units in each kernel.
+// Bound: 128 x 128 scores cost four products of 512 clocks (head_dim 128) and 1024 clocks of the special-function units in each kernel.
 #include <algorithm>
 #include <type_traits>
 
@@ -50,9 +55,9 @@ template <int DB> struct QueryStages { static constexpr int K = DB == 1 ? 4 : 3,
 
 template <int DB>
 struct __align__(16) QueryBars {
-    float lse[TILE], delta[TILE];           // of an item's rows, negated: lse times log2 e, delta
+    float lse[TILE], delta[TILE];           // of an item's rows, negated: lse times log2 e, delta as taken from the output; at its end rho
     uint64_t q_full[2], q_empty[2], do_full, do_empty, k_full[QueryStages<DB>::K], k_empty[QueryStages<DB>::K], v_full[QueryStages<DB>::V], v_empty[QueryStages<DB>::V];
-    uint64_t s_full[2], dp_full, ds_ready, dq_full, stat_full, drain;
+    uint64_t s_full, dp_full, p_ready, ds_ready, dq_full, stat_full, rho_low, rho_sum, rho_read, drain;
     uint32_t tmem_base, abort_flag;
 };
 
@@ -77,9 +82,11 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const int tok = TILE >> p.pack_shift;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars->q_full[i]), 1); mbar_init(smem_u32(&bars->q_empty[i]), 1); mbar_init(smem_u32(&bars->s_full[i]), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&bars->q_full[i]), 1); mbar_init(smem_u32(&bars->q_empty[i]), 1); }
         for (uint32_t i = 0; i < KS; ++i) { mbar_init(smem_u32(&bars->k_full[i]), 1); mbar_init(smem_u32(&bars->k_empty[i]), 1); }
         for (uint32_t i = 0; i < VS; ++i) { mbar_init(smem_u32(&bars->v_full[i]), 1); mbar_init(smem_u32(&bars->v_empty[i]), 1); }
+        mbar_init(smem_u32(&bars->rho_low), 8); mbar_init(smem_u32(&bars->rho_sum), 8); mbar_init(smem_u32(&bars->rho_read), 16);
+        mbar_init(smem_u32(&bars->s_full), 1); mbar_init(smem_u32(&bars->p_ready), 16);
         mbar_init(smem_u32(&bars->dp_full), 1); mbar_init(smem_u32(&bars->ds_ready), 16); mbar_init(smem_u32(&bars->dq_full), 1);
         mbar_init(smem_u32(&bars->stat_full), 16); mbar_init(smem_u32(&bars->drain), 1);
         mbar_init(smem_u32(&bars->do_full), 1); mbar_init(smem_u32(&bars->do_empty), 1);
@@ -91,7 +98,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = bars->tmem_base;                   // S (ds) at 0 and 128, dp at 256, dq at 384
+    const uint32_t tmem = bars->tmem_base;                   // S (P) at 0, dp (ds) at 128, dq at 256, kbar at 384
     ahead_wait();
     ahead_release();
 
@@ -177,10 +184,10 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     if (k < steps) mma_f16_ss(d, a + off, b + off, idesc_s, k > 0);
                 }
             };
-            // A place in the sequence of tiles; the scores run one tile ahead of the rest.
+            // A place in the sequence of tiles; scores and dp run one tile ahead of the sums.
             struct Place { Work w; int j; uint32_t items; };
             Ring k_ring, k_use, v_ring;                      // keys for the scores, for dq; values
-            uint32_t s_tiles = 0, tiles = 0;
+            uint32_t tiles = 0;
             bool ok = true;
             Walk walk(p.table, p.items, p.packs);
             Place ahead;
@@ -194,13 +201,12 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 if (a.w.t.len - a.j * TILE < TILE) zero_rows(op, DB, a.w.t.len - a.j * TILE, lane);
                 tc_fence_after();
                 if (elect_one()) {
-                    product(tmem + (s_tiles & 1u) * 128, q_smem + (a.items & 1u) * OP, op);
-                    mma_commit(smem_u32(&bars->s_full[s_tiles & 1u]));
+                    product(tmem, q_smem + (a.items & 1u) * OP, op);
+                    mma_commit(smem_u32(&bars->s_full));
                     if (a.j + 1 == a.w.n) mma_commit(smem_u32(&bars->q_empty[a.items & 1u]));
                 }
                 __syncwarp();
                 k_ring.next(KS);
-                ++s_tiles;
                 return true;
             };
             auto dps = [&](const Place& a) -> bool {
@@ -208,7 +214,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 if (!warp_wait(&bars->v_full[v_ring.slot], v_ring.parity, TO_MMA)) return false;
                 tc_fence_after();
                 if (elect_one()) {
-                    product(tmem + 256, do_smem, v_smem + (size_t)v_ring.slot * OP);
+                    product(tmem + 128, do_smem, v_smem + (size_t)v_ring.slot * OP);
                     mma_commit(smem_u32(&bars->dp_full));
                     mma_commit(smem_u32(&bars->v_empty[v_ring.slot]));
                     if (a.j + 1 == a.w.n) mma_commit(smem_u32(&bars->do_empty));
@@ -225,26 +231,26 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                     walk.next();
                     if (walk.more) ahead.w = work_of(walk);
                 }
-                const bool more = walk.more;
+                const bool more = walk.more, last = now.j + 1 == now.w.n;
+                const uint64_t keys = make_smem_desc_mn_sw128(smem_u32(k_smem + (size_t)k_use.slot * OP), 16384);
+                auto sum_keys = [&](uint32_t d, uint32_t a) {
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) mma_f16_ts(d, a + quarter_column(s), keys + (uint64_t)(s * 128), idesc_q, now.j > 0 || s > 0);
+                };
+                if (!warp_wait(&bars->p_ready, tiles & 1u, TO_MMA)) { ok = false; break; }
+                tc_fence_after();
+                if (elect_one()) sum_keys(tmem + 384, tmem);
+                __syncwarp();
                 if (more && !scores()) { ok = false; break; }
                 if (!warp_wait(&bars->ds_ready, tiles & 1u, TO_MMA)) { ok = false; break; }
-                const bool last = now.j + 1 == now.w.n;
                 tc_fence_after();
-                auto sums = [&]() {
-                    if (elect_one()) {
-                        const uint64_t b = make_smem_desc_mn_sw128(smem_u32(k_smem + (size_t)k_use.slot * OP), 16384);
-                        const uint32_t a = tmem + (tiles & 1u) * 128;
-#pragma unroll
-                        for (int s = 0; s < 8; ++s) mma_f16_ts(tmem + 384, a + quarter_column(s), b + (uint64_t)(s * 128), idesc_q, now.j > 0 || s > 0);
-                        mma_commit(smem_u32(&bars->k_empty[k_use.slot]));
-                        if (last) mma_commit(smem_u32(&bars->dq_full));
-                    }
-                    __syncwarp();
-                };
-                // dp of the next tile first, for the other warps wait for it; an item's last dq before the next item's gradient has to be there
-                if (last) sums();
+                if (elect_one()) {
+                    sum_keys(tmem + 256, tmem + 128);
+                    mma_commit(smem_u32(&bars->k_empty[k_use.slot]));
+                    if (last) mma_commit(smem_u32(&bars->dq_full));
+                }
+                __syncwarp();
                 if (more && !dps(ahead)) { ok = false; break; }
-                if (!last) sums();
                 k_use.next(KS);
                 ++tiles;
             }
@@ -255,14 +261,13 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
         const int part = (warp >> 2) - 1, r = (warp & 3) * 32 + lane;      // which quarter of the columns
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const int my_tok = r >> p.pack_shift;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_addr = tmem + lanes + part * 32, dp_addr = s_addr + 128;
+        const int my_tok = r >> p.pack_shift, my_head = r & (p.pack - 1);
         const uint64_t scale2 = pair_of(p.scale_log2, p.scale_log2);
         uint32_t tiles = 0, items = 0;
         bool ok = true;
         // Statistics of an item's rows, eight to a warp: the lanes that share a row (8 or 16) read 16 bytes of out and of its gradient each (from L2, where
-        // the producer has had them brought) before the epilogue of the item in front; behind it they are added up and put down. One place will do: a warp
-        // comes here when the last tile's ds of every warp has arrived, so all have read what stood there.
+        // the producer has had them brought) before the epilogue of the item in front; behind it they are added up and put down.
         constexpr int LANES = 8 * DB, ROWS = 32 / LANES, PARTS = 8 / ROWS;
         const int sub = lane / LANES, c8 = (lane % LANES) * 8, stat_row = (warp - 4) * 8;
         uint4 o8[PARTS], d8[PARTS];
@@ -301,9 +306,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (lane < 8) {
                 int64_t token;
                 int head;
-                const bool there = row_of(w, stat_row + lane, token, head);
-                bars->lse[stat_row + lane] = there ? -lse1 * LOG2E : 0.0f;
-                if (there) p.delta[token * p.heads + head] = bars->delta[stat_row + lane];
+                bars->lse[stat_row + lane] = row_of(w, stat_row + lane, token, head) ? -lse1 * LOG2E : 0.0f;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&bars->stat_full));
@@ -318,9 +321,9 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (!ok) break;
             const float off = bars->lse[r], delta = bars->delta[r];
             const uint64_t off2 = pair_of(off, off), delta2 = pair_of(delta, delta);
+            uint64_t rho2[2] = {0, 0};
             for (int j = 0; j < w.n; ++j, ++tiles) {
-                const uint32_t buf = tiles & 1u, s_addr = tmem + lanes + buf * 128 + part * 32;
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->s_full[buf]), (tiles >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->s_full), tiles & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
                 if (!ok) break;
                 tc_fence_after();
                 uint32_t s[2][16];
@@ -328,22 +331,41 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 tmem_ld_x16(s_addr, s[0]);
                 tmem_wait_ld();
                 tmem_ld_x16(s_addr + 16, s[1]);
+                const bool masked = j * TILE + TILE - 1 > w.t.at;
+                const int lim = at - j * TILE - part * 32;   // this row's last key among the 32
+                auto hide = [&](uint64_t x, int k) {         // zeros behind it
+                    float a, b;
+                    split_pair(x, a, b);
+                    return pair_of(2 * k > lim ? 0.0f : a, 2 * k + 1 > lim ? 0.0f : b);
+                };
+                auto form_p = [&](auto diagonal) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (h == 1) tmem_wait_ld();
+                    for (int h = 0; h < 2; ++h) {
+                        if (h == 1) tmem_wait_ld();
+                        uint32_t e[8];
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        pr[h * 8 + k] = ex2_of<SHARE>(fma2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), scale2, off2), h * 8 + k);
-                }
+                        for (int k = 0; k < 8; ++k) {
+                            uint64_t& x = pr[h * 8 + k];
+                            x = ex2_of<SHARE>(fma2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), scale2, off2), h * 8 + k);
+                            if constexpr (diagonal.value) x = hide(x, h * 8 + k);
+                            e[k] = pack_pair(x);
+                        }
+                        tmem_st_x8(s_addr + h * 8, e);       // over this quarter's own scores
+                    }
+                };
+                if (masked) form_p(std::true_type{});
+                else form_p(std::false_type{});
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars->p_ready));
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->dp_full), tiles & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t dp_addr = tmem + lanes + 256 + part * 32;
                 tmem_ld_x16(dp_addr, s[0]);
                 tmem_wait_ld();
                 tmem_ld_x16(dp_addr + 16, s[1]);
-                auto form = [&](auto diagonal) {
-                    const int lim = at - j * TILE - part * 32;      // this row's last key among the 32
+                auto form_ds = [&](auto diagonal) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         if (h == 1) tmem_wait_ld();
@@ -351,18 +373,15 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
                             uint64_t ds = mul2(pr[h * 8 + k], add2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), delta2));
-                            if constexpr (diagonal.value) {
-                                float a, b;
-                                split_pair(ds, a, b);
-                                ds = pair_of(h * 16 + 2 * k > lim ? 0.0f : a, h * 16 + 2 * k + 1 > lim ? 0.0f : b);
-                            }
+                            if constexpr (diagonal.value) ds = hide(ds, h * 8 + k);      // (also where dp is not finite)
+                            rho2[k & 1] = add2(rho2[k & 1], ds);
                             e[k] = pack_pair(ds);
                         }
-                        tmem_st_x8(s_addr + h * 8, e);       // over this quarter's own scores
+                        tmem_st_x8(dp_addr + h * 8, e);
                     }
                 };
-                if (j * TILE + TILE - 1 > w.t.at) form(std::true_type{});
-                else form(std::false_type{});
+                if (masked) form_ds(std::true_type{});
+                else form_ds(std::false_type{});
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -373,8 +392,33 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             more = walk.more;
             Work next = w;
             if (more) { next = work_of(walk); fetch(next); }
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->dq_full), items & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
+            // rho of the row from its quarters, in the places of lse and delta, which everybody has read (the last tile's ds has arrived only when all had): the
+            // third and fourth leave theirs, the first and second add those and leave the two sums
+            float rho, low, high;
+            split_pair(add2(rho2[0], rho2[1]), low, high);
+            rho = low + high;
+            float* place = (part & 1) ? bars->delta : bars->lse;
+            auto meet = [&](uint64_t* bar) -> bool { return __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(bar), items & 1u, abort_flag, p.timeout_word, TO_EPILOGUE)); };
+            auto here = [&](uint64_t* bar) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(bar));
+            };
+            ok = meet(&bars->dq_full);
             if (!ok) break;
+            if (part >= 2) {
+                place[r] = rho;
+                here(&bars->rho_low);
+            } else {
+                ok = meet(&bars->rho_low);
+                if (!ok) break;
+                place[r] = rho + place[r];
+                here(&bars->rho_sum);
+            }
+            ok = meet(&bars->rho_sum);
+            if (!ok) break;
+            rho = bars->lse[r] + bars->delta[r];
+            here(&bars->rho_read);
+            if (part == 0 && at < w.t.len) p.delta[(int64_t)(w.t.t0 + at) * p.heads + w.head0 + my_head] = delta - rho;      // (negated)
             tc_fence_after();
             __nv_bfloat16* dst[4];
 #pragma unroll
@@ -382,17 +426,22 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 const int rr = (warp & 3) * 32 + (lane & ~3) + k, a = w.t.at + (rr >> p.pack_shift);
                 dst[k] = a < w.t.len ? p.dq + (int64_t)(w.t.t0 + a) * p.ld_dq + (int64_t)(w.head0 + (rr & (p.pack - 1))) * p.head_dim : nullptr;
             }
-#pragma unroll 1
-            for (int c = part * 32; c < p.head_dim; c += 128) {
+            if (part * 32 < p.head_dim) {
                 uint32_t o[32];
                 float f[32];
-                tmem_ld_x32(tmem + lanes + 384 + c, o);
+                tmem_ld_x32(tmem + lanes + 256 + part * 32, o);
                 tmem_wait_ld();
 #pragma unroll
-                for (int k = 0; k < 32; ++k) f[k] = __uint_as_float(o[k]) * p.scale;
-                store_rows32(f, c, p.head_dim, lane, dst);
+                for (int k = 0; k < 32; ++k) f[k] = __uint_as_float(o[k]);
+                tmem_ld_x32(tmem + lanes + 384 + part * 32, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int k = 0; k < 32; ++k) f[k] = fmaf(-rho, __uint_as_float(o[k]), f[k]) * p.scale;
+                store_rows32(f, part * 32, p.head_dim, lane, dst);
             }
             tc_fence_before();
+            ok = meet(&bars->rho_read);                      // the statistics' places are free
+            if (!ok) break;
             if (more) { put_down(next); w = next; }
         }
     }

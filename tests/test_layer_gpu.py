@@ -90,7 +90,8 @@ def test_layer_norm(T, W, dtype, pdtype):
 # ---- attention ---------------------------------------------------------------------------------------------------------
 
 def attention_exact(q, k, v, off, scale, dout=None, out=None):
-    """(out, room), lse and, with dout, the gradients with their rooms; delta from `out` as given."""
+    """Results and their rooms: out, lse and, with dout, the gradients. `out` as given to the backward pass counts for roundings only: ds is rounded as it is
+    with delta taken from it, and put right by rho = <dout, exact out - out> times the mean of the keys, whose probabilities are rounded."""
     T, H, D = q.shape
     K = k.shape[1]
     f = dict(dtype=torch.float64, device="cuda")
@@ -114,14 +115,15 @@ def attention_exact(q, k, v, off, scale, dout=None, out=None):
                 continue
             dO, O = dout[lo:hi, h].double(), out[lo:hi, h].double()
             dp = dO @ V.T
-            delta = (dO * O).sum(dim=1, keepdim=True)
-            ds = p * (dp - delta)
-            # dp and delta are fp32 sums of products
-            eds = p * SUMS * (dO.abs() @ V.abs().T + (dO * O).abs().sum(dim=1, keepdim=True)) + HALF * ds.abs()
+            ds = p * (dp - (dO * o).sum(dim=1, keepdim=True))
+            rho = (dO * (o - O)).sum(dim=1, keepdim=True)
+            rough = (ds + p * rho).abs()
+            # dp, delta and rho are fp32 sums of products
+            eds = p * SUMS * 2 * (dO.abs() @ V.abs().T + (dO * O).abs().sum(dim=1, keepdim=True))
             got["grad_q"][lo:hi, h] = scale * ds @ Kk
-            room["grad_q"][lo:hi, h] = scale * (eds + SUMS * ds.abs()) @ Kk.abs()
+            room["grad_q"][lo:hi, h] = scale * (eds + (HALF + SUMS) * (rough + p * rho.abs())) @ Kk.abs()
             got["grad_k"][lo:hi, c] += scale * ds.T @ Q
-            room["grad_k"][lo:hi, c] += scale * (eds + SUMS * ds.abs()).T @ Q.abs()
+            room["grad_k"][lo:hi, c] += scale * (eds + (HALF + SUMS) * ds.abs()).T @ Q.abs()
             got["grad_v"][lo:hi, c] += p.T @ dO
             room["grad_v"][lo:hi, c] += (HALF + SUMS) * p.T @ dO.abs()
     for n in ("grad_q", "grad_k", "grad_v"):
