@@ -33,7 +33,6 @@ using namespace attn;
 namespace {
 
 constexpr int NTHREADS = 640;
-constexpr int SHARE = 5;                    // one in so many pairs of exponentials on the fp32 units
 
 // Columns of step s (16 rows of the contraction) of a left operand in tensor memory that four groups of warps wrote, each over the first half of its own 32 columns.
 __device__ __forceinline__ constexpr uint32_t quarter_column(int s) { return (uint32_t)((s >> 1) * 32 + (s & 1) * 8); }
@@ -346,7 +345,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
                             uint64_t& x = pr[h * 8 + k];
-                            x = ex2_of<SHARE>(fma2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), scale2, off2), h * 8 + k);
+                            x = ex2_pair(fma2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), scale2, off2));
                             if constexpr (diagonal.value) x = hide(x, h * 8 + k);
                             e[k] = pack_pair(x);
                         }
@@ -735,8 +734,8 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 #pragma unroll
                         for (int k = 0; k < 8; k += 2) {
                             const float4 l = lse[(h * 8 + k) / 2];
-                            pr[h * 8 + k] = ex2_of<SHARE>(fma2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), scale2, pair_of(l.x, l.y)), h * 8 + k);
-                            pr[h * 8 + k + 1] = ex2_of<SHARE>(fma2(pair_of(__uint_as_float(s[h][2 * k + 2]), __uint_as_float(s[h][2 * k + 3])), scale2, pair_of(l.z, l.w)), h * 8 + k + 1);
+                            pr[h * 8 + k] = ex2_pair(fma2(pair_of(__uint_as_float(s[h][2 * k]), __uint_as_float(s[h][2 * k + 1])), scale2, pair_of(l.x, l.y)));
+                            pr[h * 8 + k + 1] = ex2_pair(fma2(pair_of(__uint_as_float(s[h][2 * k + 2]), __uint_as_float(s[h][2 * k + 3])), scale2, pair_of(l.z, l.w)));
                         }
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {

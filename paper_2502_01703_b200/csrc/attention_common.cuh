@@ -35,32 +35,8 @@ __device__ __forceinline__ float ex2(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// 2^x of a pair on the fp32 units, for a share of the exponentials: the special-function units alone take 1024 clocks for a tile's 16384. Cody and Waite's
-// reduction x = n + r, |r| <= 1/2, by adding and subtracting 1.5 2^23; 2^r by the minimax polynomial of degree 5 (Remez exchange for the relative error
-// on [-1/2, 1/2]: 7.5e-8; 2.1e-7 as evaluated in fp32); 2^n from the sum's low bits. Below -126.5 the result is 0; NaN stays NaN.
 __device__ __forceinline__ uint64_t ex2_pair(uint64_t x)
 {
-    float a, b;
-    split_pair(x, a, b);
-    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(a));        // -127: 2^n comes out as 0
-    asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(b));
-    x = pair_of(a, b);
-    const uint64_t t = add2(x, pair_of(12583039.0f, 12583039.0f));      // 1.5 2^23 + 127: n + 127 in the low bits
-    const uint64_t r = fma2(add2(t, pair_of(-12583039.0f, -12583039.0f)), pair_of(-1.0f, -1.0f), x);
-    uint64_t y = fma2(r, pair_of(1.3276472454890609e-3f, 1.3276472454890609e-3f), pair_of(9.675540961325169e-3f, 9.675540961325169e-3f));
-    y = fma2(y, r, pair_of(5.550713092088699e-2f, 5.550713092088699e-2f));
-    y = fma2(y, r, pair_of(2.4022120237350464e-1f, 2.4022120237350464e-1f));
-    y = fma2(y, r, pair_of(6.931469440460205e-1f, 6.931469440460205e-1f));
-    y = fma2(y, r, pair_of(1.0000001192092896f, 1.0000001192092896f));
-    float ta, tb;
-    split_pair(t, ta, tb);
-    return mul2(y, pair_of(__uint_as_float(__float_as_uint(ta) << 23), __uint_as_float(__float_as_uint(tb) << 23)));
-}
-// 2^x of pair i of a row: every `SHARE`-th on the fp32 units.
-template <int SHARE>
-__device__ __forceinline__ uint64_t ex2_of(uint64_t x, int i)
-{
-    if (SHARE > 0 && i % (SHARE > 0 ? SHARE : 1) == 1) return ex2_pair(x);
     float a, b;
     split_pair(x, a, b);
     return pair_of(ex2(a), ex2(b));
