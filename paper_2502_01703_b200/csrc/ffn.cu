@@ -177,6 +177,37 @@ ffn_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
             constexpr int SPAN = TILE_N / 2;                 // columns of the result to a group of warps
             const int c_lo = n * TILE_N + half * SPAN;
             const uint32_t taddr = tmem + lane_base + buf * 256 + half * SPAN;
+            // GLU_BACK: g and u of 32 columns as they lie in memory (64 bytes of a row at a time, from four lanes), brought a step ahead: the first before the
+            // accumulator is waited for, those of the pair's next tile into L2
+            uint4 raw[2][4];
+            auto fetch = [&](int c0) {
+                const bool there = c_lo + c0 + (lane & 3) * 8 < p.cols;
+                const __nv_bfloat16* g = p.gate_in + first * p.ld_gate_in + c_lo + c0 + (lane & 3) * 8;
+                const __nv_bfloat16* u = p.up_in + first * p.ld_up_in + c_lo + c0 + (lane & 3) * 8;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const bool in = there && first + k < p.rows;
+                    raw[0][k] = in ? __ldg(reinterpret_cast<const uint4*>(g + k * p.ld_gate_in)) : make_uint4(0u, 0u, 0u, 0u);
+                    raw[1][k] = in ? __ldg(reinterpret_cast<const uint4*>(u + k * p.ld_up_in)) : make_uint4(0u, 0u, 0u, 0u);
+                }
+            };
+            if (MODE == GLU_BACK) {
+                fetch(0);
+                if (item + num_pairs < items) {
+                    int set1, m1, n1;
+                    item_of(item + num_pairs, set1, m1, n1);
+                    const int64_t row1 = (int64_t)m1 * 256 + rank * 128 + q * 32 + lane;
+                    const int col1 = n1 * TILE_N + half * SPAN;
+                    if (row1 < p.rows) {
+#pragma unroll
+                        for (int c = 0; c < SPAN; c += 64) {
+                            if (col1 + c >= p.cols) break;
+                            prefetch_l2(p.gate_in + row1 * p.ld_gate_in + col1 + c);
+                            prefetch_l2(p.up_in + row1 * p.ld_up_in + col1 + c);
+                        }
+                    }
+                }
+            }
             bool ok = mbar_wait_cluster(smem_u32(&bars->d_full[buf]), (n_acc >> 1) & 1u, abort_flag, p.timeout_word, TO_EPILOGUE);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
@@ -192,38 +223,32 @@ ffn_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
                 for (int k = 0; k < 4; ++k)
                     if (in && first + k < p.rows) *reinterpret_cast<uint4*>(dst + k * ld) = w[k];
             };
-            // the same the other way round
-            auto get = [&](const __nv_bfloat16* in, int64_t ld, float (&v)[32], int c0) {
-                uint4 w[4];
-                const __nv_bfloat16* src = in + first * ld + c_lo + c0 + (lane & 3) * 8;
-                const bool there = c_lo + c0 + (lane & 3) * 8 < p.cols;
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    w[k] = there && first + k < p.rows ? __ldg(reinterpret_cast<const uint4*>(src + k * ld)) : make_uint4(0u, 0u, 0u, 0u);
-                transpose4(w, lane);
-                unpack_row32(w, v);
-            };
 #pragma unroll 1
             for (int c0 = 0; c0 < SPAN; c0 += 32) {
                 float v[32], u[32];
                 if (MODE == GLU_BACK) {
                     float g[32], h[32];
-                    get(p.gate_in, p.ld_gate_in, g, c0);
-                    get(p.up_in, p.ld_up_in, u, c0);
+                    transpose4(raw[0], lane);
+                    unpack_row32(raw[0], g);
+                    transpose4(raw[1], lane);
+                    unpack_row32(raw[1], u);
+                    if (c0 + 32 < SPAN) fetch(c0 + 32);
                     load_acc(taddr + c0, v);
                     if (c0 + 32 == SPAN) {
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive_leader_tmem(smem_u32(&bars->d_empty[buf]), rank);
                     }
+                    by_activation(p.act, [&](auto act) {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        float a, da;
-                        activation(p.act, g[k], a, da);
-                        h[k] = a * u[k];
-                        g[k] = v[k] * u[k] * da;
-                        u[k] = v[k] * a;
-                    }
+                        for (int k = 0; k < 32; ++k) {
+                            float a, da;
+                            activation<act.value>(g[k], a, da);
+                            h[k] = a * u[k];
+                            g[k] = v[k] * u[k] * da;
+                            u[k] = v[k] * a;
+                        }
+                    });
                     put(p.out, p.ld, g, c0);
                     put(p.out2, p.ld2, u, c0);
                     if (p.out3 != nullptr) put(p.out3, p.ld3, h, c0);
@@ -238,12 +263,14 @@ ffn_gemm_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant_
                 }
                 if (MODE == GLU) {
                     if (p.out2 != nullptr) { put(p.out2, p.ld2, v, c0); put(p.out3, p.ld3, u, c0); }
+                    by_activation(p.act, [&](auto act) {
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) {
-                        float a, da;
-                        activation(p.act, v[k], a, da);
-                        v[k] = a * u[k];
-                    }
+                        for (int k = 0; k < 32; ++k) {
+                            float a, da;
+                            activation<act.value>(v[k], a, da);
+                            v[k] = a * u[k];
+                        }
+                    });
                     put(p.out, p.ld, v, c0);
                 } else {
                     put(set ? p.out2 : p.out, set ? p.ld2 : p.ld, v, c0);

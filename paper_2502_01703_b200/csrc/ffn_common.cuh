@@ -1,6 +1,8 @@
 // What the kernels of the gated feed-forward block share.
 #pragma once
 
+#include <type_traits>
+
 #include "qless_kernels.h"
 #include "tc_common.cuh"
 
@@ -43,9 +45,10 @@ __device__ __forceinline__ void load_acc(uint32_t taddr, float (&v)[32])
 
 // a = act(g) and its derivative. SiLU: g s, s + g s (1 - s) with s = 1 / (1 + e^-g); GELU: g F(g), F(g) + g f(g) with the normal
 // distribution F and its density f.
-__device__ __forceinline__ void activation(int act, float g, float& a, float& da)
+template <int ACT>
+__device__ __forceinline__ void activation(float g, float& a, float& da)
 {
-    if (act == QLESS_SILU) {
+    if constexpr (ACT == QLESS_SILU) {
         const float s = __fdividef(1.0f, 1.0f + __expf(-g));      // (g far below 0: 1 / infinity = 0)
         a = g == -INFINITY ? 0.0f : g * s;
         da = isinf(g) ? s : fmaf(a, 1.0f - s, s);
@@ -54,6 +57,15 @@ __device__ __forceinline__ void activation(int act, float g, float& a, float& da
         a = g == -INFINITY ? 0.0f : g * F;
         da = isinf(g) ? F : fmaf(g, f, F);
     }
+}
+
+// What is done for many elements is written once for each activation: with the choice made for every element anew they would follow one another instead of
+// overlapping (dg and du of a 256 x 256 tile took 60 thousand clocks so, four times the product's).
+template <typename F>
+__device__ __forceinline__ void by_activation(int act, F f)
+{
+    if (act == QLESS_SILU) f(std::integral_constant<int, QLESS_SILU>{});
+    else f(std::integral_constant<int, QLESS_GELU>{});
 }
 
 // Few tokens (ffn_few.cu): the weights' rows or columns are the tile's rows, the tokens its columns.

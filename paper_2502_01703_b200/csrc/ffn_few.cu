@@ -219,26 +219,28 @@ few_gemm_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant_
                     }
                     continue;
                 }
+                by_activation(p.f.act, [&](auto act) {
 #pragma unroll
-                for (int k = 0; k < 32; ++k) {
-                    if (k >= have) break;
-                    const int64_t t = c0 + k;
-                    if constexpr (MODE == OUT) {
-                        p.f.out[t * p.f.ld + f] = __float2bfloat16_rn(v[k]);
-                    } else if constexpr (MODE == GLU) {
-                        if (p.f.out2 != nullptr) { p.f.out2[t * p.f.ld2 + f] = __float2bfloat16_rn(v[k]); p.f.out3[t * p.f.ld3 + f] = __float2bfloat16_rn(u[k]); }
-                        float a, da;
-                        activation(p.f.act, v[k], a, da);
-                        p.f.out[t * p.f.ld + f] = __float2bfloat16_rn(a * u[k]);
-                    } else {
-                        const float g = __bfloat162float(p.f.gate_in[t * p.f.ld_gate_in + f]), w = __bfloat162float(p.f.up_in[t * p.f.ld_up_in + f]);
-                        float a, da;
-                        activation(p.f.act, g, a, da);
-                        p.f.out[t * p.f.ld + f] = __float2bfloat16_rn(v[k] * w * da);
-                        p.f.out2[t * p.f.ld2 + f] = __float2bfloat16_rn(v[k] * a);
-                        if (p.f.out3 != nullptr) p.f.out3[t * p.f.ld3 + f] = __float2bfloat16_rn(a * w);
+                    for (int k = 0; k < 32; ++k) {
+                        if (k >= have) break;
+                        const int64_t t = c0 + k;
+                        if constexpr (MODE == OUT) {
+                            p.f.out[t * p.f.ld + f] = __float2bfloat16_rn(v[k]);
+                        } else if constexpr (MODE == GLU) {
+                            if (p.f.out2 != nullptr) { p.f.out2[t * p.f.ld2 + f] = __float2bfloat16_rn(v[k]); p.f.out3[t * p.f.ld3 + f] = __float2bfloat16_rn(u[k]); }
+                            float a, da;
+                            activation<act.value>(v[k], a, da);
+                            p.f.out[t * p.f.ld + f] = __float2bfloat16_rn(a * u[k]);
+                        } else {
+                            const float g = __bfloat162float(p.f.gate_in[t * p.f.ld_gate_in + f]), w = __bfloat162float(p.f.up_in[t * p.f.ld_up_in + f]);
+                            float a, da;
+                            activation<act.value>(g, a, da);
+                            p.f.out[t * p.f.ld + f] = __float2bfloat16_rn(v[k] * w * da);
+                            p.f.out2[t * p.f.ld2 + f] = __float2bfloat16_rn(v[k] * a);
+                            if (p.f.out3 != nullptr) p.f.out3[t * p.f.ld3 + f] = __float2bfloat16_rn(a * w);
+                        }
                     }
-                }
+                });
             }
             tc_fence_before();
             __syncwarp();
@@ -283,25 +285,29 @@ __global__ void __launch_bounds__(256) few_finish_kernel(const FinishParams p)
         } else if (MODE == GLU) {
             if (p.out2 != nullptr) { put(p.out2 + t * p.ld2 + f, v[0]); put(p.out3 + t * p.ld3 + f, v[1]); }
             float h[4];
+            by_activation(p.act, [&](auto act) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float a, da;
-                activation(p.act, v[0][k], a, da);
-                h[k] = a * v[1][k];
-            }
+                for (int k = 0; k < 4; ++k) {
+                    float a, da;
+                    activation<act.value>(v[0][k], a, da);
+                    h[k] = a * v[1][k];
+                }
+            });
             put(p.out + t * p.ld + f, h);
         } else {
             float g[4], u[4], h[4];
             get(p.gate_in + t * p.ld_gate_in + f, g);
             get(p.up_in + t * p.ld_up_in + f, u);
+            by_activation(p.act, [&](auto act) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float a, da;
-                activation(p.act, g[k], a, da);
-                h[k] = a * u[k];
-                g[k] = v[0][k] * u[k] * da;
-                u[k] = v[0][k] * a;
-            }
+                for (int k = 0; k < 4; ++k) {
+                    float a, da;
+                    activation<act.value>(g[k], a, da);
+                    h[k] = a * u[k];
+                    g[k] = v[0][k] * u[k] * da;
+                    u[k] = v[0][k] * a;
+                }
+            });
             put(p.out + t * p.ld + f, g);
             put(p.out2 + t * p.ld2 + f, u);
             if (p.out3 != nullptr) put(p.out3 + t * p.ld3 + f, h);
