@@ -828,34 +828,37 @@ def qless_attention_backward(grad_out, q, k, v, out, lse, offsets, scale=None, g
     and v. `grads` may pass preallocated tensors by those names (slices of one matrix, say); rows outside the examples are left as they are in
     those and are zeros in new ones."""
     off = _host_offsets(offsets)
+    sg, sq, sk, sv, so = _token_stride(grad_out, "grad_out"), _token_stride(q, "q"), _token_stride(k, "k"), _token_stride(v, "v"), _token_stride(out, "out")
     T, heads, kv, d = _heads_of(q, k, v)
     if grad_out.shape != q.shape or out.shape != q.shape:
         raise ValueError("grad_out and out must have q's shape")
     if lse.shape != (T, heads) or lse.dtype != torch.float32 or not lse.is_contiguous():
         raise ValueError("lse must be contiguous float32, [tokens, heads]")
     n = off.numel() - 1
-    grads = grads or {}
-    at = _on_gpu(stream, q, k, v, grad_out, out, lse, workspace, *grads.values())
     whole = _covers(off, T)
-    got = {}
-    for name, like in (("grad_q", q), ("grad_k", k), ("grad_v", v)):
-        t = grads.get(name)
-        if t is None:
-            t = _heads_like(like, whole, stream)
-        elif t.shape != like.shape:
-            raise ValueError(f"{name} has the wrong shape")
-        got[name] = t
+    if grads is None:
+        at = _on_gpu(stream, q, k, v, grad_out, out, lse, workspace)
+        gq, gk, gv = _heads_like(q, whole, stream), _heads_like(k, whole, stream), _heads_like(v, whole, stream)
+        tq, tk, tv = heads * d, kv * d, kv * d
+    else:
+        at = _on_gpu(stream, q, k, v, grad_out, out, lse, workspace, *grads.values())
+        got = []
+        for name, like in (("grad_q", q), ("grad_k", k), ("grad_v", v)):
+            t = grads.get(name)
+            if t is None:
+                t = _heads_like(like, whole, stream)
+            elif t.shape != like.shape:
+                raise ValueError(f"{name} has the wrong shape")
+            got.append(t)
+        gq, gk, gv = got
+        tq, tk, tv = _token_stride(gq, "grad_q"), _token_stride(gk, "grad_k"), _token_stride(gv, "grad_v")
     ws, ws_bytes, _hold = _workspace_if(lib().qless_attention_backward_workspace(T, n, heads, kv), q.device, workspace, stream)
     if stream is not None:
-        _used(stream, q, k, v, grad_out, out, lse, workspace, *got.values())
-    args = []
-    for t, name in ((grad_out, "grad_out"), (q, "q"), (k, "k"), (v, "v"), (out, "out")):
-        args += [t.data_ptr(), _token_stride(t, name)]
-    args += [lse.data_ptr(), off.data_ptr(), T, n, heads, kv, d, d ** -0.5 if scale is None else scale]
-    for name, t in got.items():
-        args += [t.data_ptr(), _token_stride(t, name)]
-    _check(lib().qless_attention_backward(*args, ws, ws_bytes, _stream(stream, at)))
-    return got
+        _used(stream, q, k, v, grad_out, out, lse, workspace, gq, gk, gv)
+    _check(lib().qless_attention_backward(grad_out.data_ptr(), sg, q.data_ptr(), sq, k.data_ptr(), sk, v.data_ptr(), sv, out.data_ptr(), so, lse.data_ptr(),
+                                          off.data_ptr(), T, n, heads, kv, d, d ** -0.5 if scale is None else scale, gq.data_ptr(), tq, gk.data_ptr(), tk,
+                                          gv.data_ptr(), tv, ws, ws_bytes, _stream(stream, at)))
+    return dict(grad_q=gq, grad_k=gk, grad_v=gv)
 
 
 def _activation_code(activation):
@@ -946,16 +949,29 @@ def qless_gated_ffn_backward(grad_out, x, gate, up, w_gate, w_up, w_down, activa
     code = _activation_code(activation)
     if gate.shape != (T, inner) or up.shape != (T, inner) or (x is not None and x.shape != (T, width)):
         raise ValueError("x must be [tokens, width], gate and up [tokens, inner]")
-    at = _on_gpu(stream, grad_out, x, gate, up, w_gate, w_up, w_down, workspace, *(grads or {}).values())
-    got = _outputs(grads, dict(grad_x=(want_x, T, width), grad_gate=(True, T, inner), grad_up=(True, T, inner), grad_w_gate=(want_weight, inner, width),
-                               grad_w_up=(want_weight, inner, width), grad_w_down=(want_weight, width, inner)), grad_out.device, stream)
-    weights = any(got[name] is not None for name in ("grad_w_gate", "grad_w_up", "grad_w_down"))
-    ws, ws_bytes, _hold = _workspace_if(lib().qless_gated_ffn_backward_workspace(T, width, inner, 1 if weights else 0), grad_out.device, workspace, stream)
+    dev = grad_out.device
+    if grads is None:
+        at = _on_gpu(stream, grad_out, x, gate, up, w_gate, w_up, w_down, workspace)
+        gx = _empty(T, width, torch.bfloat16, dev, stream) if want_x else None
+        gg, gu = _empty(T, inner, torch.bfloat16, dev, stream), _empty(T, inner, torch.bfloat16, dev, stream)
+        wg = wu = wd = None
+        if want_weight:
+            wg, wu = _empty(inner, width, torch.bfloat16, dev, stream), _empty(inner, width, torch.bfloat16, dev, stream)
+            wd = _empty(width, inner, torch.bfloat16, dev, stream)
+    else:
+        at = _on_gpu(stream, grad_out, x, gate, up, w_gate, w_up, w_down, workspace, *grads.values())
+        got = _outputs(grads, dict(grad_x=(want_x, T, width), grad_gate=(True, T, inner), grad_up=(True, T, inner), grad_w_gate=(want_weight, inner, width),
+                                   grad_w_up=(want_weight, inner, width), grad_w_down=(want_weight, width, inner)), dev, stream)
+        gx, gg, gu, wg, wu, wd = got.values()
+    weights = wg is not None or wu is not None or wd is not None
+    ws, ws_bytes, _hold = _workspace_if(lib().qless_gated_ffn_backward_workspace(T, width, inner, 1 if weights else 0), dev, workspace, stream)
     if stream is not None:
-        _used(stream, grad_out, x, gate, up, w_gate, w_up, w_down, workspace, *got.values())
-    _check(lib().qless_gated_ffn_backward(*_bf16_args(grad_out, x, gate, up, w_gate, w_up, w_down), T, width, inner, code, *_bf16_args(*got.values()),
+        _used(stream, grad_out, x, gate, up, w_gate, w_up, w_down, workspace, gx, gg, gu, wg, wu, wd)
+    _check(lib().qless_gated_ffn_backward(*_bf16_args(grad_out, x), _bf16(gate), _row_stride(gate), _bf16(up), _row_stride(up), _bf16(w_gate), _row_stride(w_gate),
+                                          _bf16(w_up), _row_stride(w_up), _bf16(w_down), _row_stride(w_down), T, width, inner, code, *_bf16_args(gx),
+                                          _bf16(gg), _row_stride(gg), _bf16(gu), _row_stride(gu), *(_bf16_args(wg, wu, wd) if weights else (None, 0) * 3),
                                           ws, ws_bytes, _stream(stream, at)))
-    return got
+    return dict(grad_x=gx, grad_gate=gg, grad_up=gu, grad_w_gate=wg, grad_w_up=wu, grad_w_down=wd)
 
 
 def qless_set_projection_path(path):
