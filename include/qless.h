@@ -432,8 +432,8 @@ qless_status qless_lm_loss(const void* hidden, int64_t ld_hidden, const void* we
  * The way of a loss's gradient through a decoder layer: normalisation, attention, feed-forward block, forward and backward.
  * What they give at a projection's output is the grad_out of qless_lora_gradients, so that gradient rows reach every adapted
  * layer and not the last alone. Matrices are row-major with a row stride in elements (ld_...); outputs do not overlap
- * inputs. Workspaces: device, 256-byte aligned; where the size function gives 0 none is needed, and NULL is taken. All calls enqueue kernels on `cuda_stream` alone and read no host memory once they have returned; the same inputs
- * give the same bits (no float atomics).
+ * inputs. Workspaces: device, 256-byte aligned; where the size function gives 0 none is needed, and NULL is taken. All calls enqueue kernels on
+ * `cuda_stream` alone and read no host memory once they have returned; the same inputs give the same bits (no float atomics).
  *
  * Layer normalisation of the rows of x [tokens, width] (dtype: QLESS_F32 or QLESS_BF16, of x, out, grad_out and grad_x):
  *   mean_t = sum_c x_tc / width (center = 0: 0);  rstd_t = 1 / sqrt(sum_c (x_tc - mean_t)^2 / width + eps)
@@ -469,8 +469,8 @@ qless_status qless_layer_norm_backward(const void* grad_out, int64_t ld_grad_out
  *   grad_k_j = scale sum_i ds_ij q_i,  grad_v_j = sum_i p_ij grad_out_i   (sums over i and the query heads of the group)
  * with p and ds rounded to bf16 in these products, fp32 sums, and one rounding of each result to bf16. <grad_out_i, out_i> is the first estimate of delta_i,
  * whose error (out is rounded) is found and taken out of all results.
- * Requirements: tokens < 2^31; head_dim a multiple of 8, at most 128; heads a multiple of kv_heads, heads <= 4096; scale finite and positive; tensors
- * 16-byte aligned, their row strides multiples of 8. */
+ * Requirements: tokens < 2^31, those of an example times heads / kv_heads at most 2^25; head_dim a multiple of 8, at most 128; heads a multiple of
+ * kv_heads, heads <= 4096; scale finite and positive; tensors 16-byte aligned, their row strides multiples of 8. */
 size_t qless_attention_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads);
 size_t qless_attention_backward_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads);
 
@@ -495,7 +495,7 @@ qless_status qless_attention_backward(const void* grad_out, int64_t ld_grad_out,
  * grad_gate and grad_up [tokens, inner] are always written (they are the gradients at the two projections' outputs); grad_x and each weight's
  * gradient may be NULL. Products of bf16 operands with fp32 sums; hidden, grad_gate and grad_up are rounded to bf16 before the next product.
  * x is read for grad_w_gate and grad_w_up alone (else it may be NULL). With tokens = 0 the weights' gradients are zeros.
- * Requirements: tokens < 2^31 - 256; width and inner multiples of 8, at most 2^20; matrices 16-byte aligned, their row strides multiples of 8.
+ * Requirements: tokens < 2^31 - 256 (at most 2^27 with any weight's gradient); width and inner multiples of 8, at most 2^20; matrices 16-byte aligned, their row strides multiples of 8.
  * want_weights: any weight's gradient. */
 typedef enum { QLESS_SILU = 0, QLESS_GELU = 1 } qless_activation;
 

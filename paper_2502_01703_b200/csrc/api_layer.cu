@@ -48,12 +48,19 @@ static qless_status check_heads(int64_t tokens, int64_t n, int32_t heads, int32_
     return QLESS_OK;
 }
 
-static qless_status check_offsets(const int64_t* offsets, int64_t tokens, int64_t n)
+// An item of the kernels walks over an example's rows (a tile of keys: over those of every head of the group), and others of its block wait that long for
+// the place it holds: at about 2 us for 128 rows, 2^25 rows take a quarter of the two seconds after which a wait gives up.
+constexpr int64_t MOST_ROWS = (int64_t)1 << 25;
+
+static qless_status check_offsets(const int64_t* offsets, int64_t tokens, int64_t n, int32_t group)
 {
     QLESS_REQUIRE(offsets != nullptr, QLESS_ERR_INVALID_ARG, "offsets are required");
     QLESS_REQUIRE(offsets[0] >= 0 && offsets[n] <= tokens, QLESS_ERR_INVALID_ARG, "offsets must lie in [0, tokens]");
     for (int64_t e = 0; e < n; ++e)
         QLESS_REQUIRE(offsets[e] <= offsets[e + 1], QLESS_ERR_INVALID_ARG, "offsets must not decrease (offsets[%lld] > offsets[%lld])", (long long)e, (long long)e + 1);
+    for (int64_t e = 0; e < n; ++e)
+        QLESS_REQUIRE(offsets[e + 1] - offsets[e] <= MOST_ROWS / group, QLESS_ERR_UNSUPPORTED,
+                      "an example's tokens times heads / kv_heads must be at most 2^25 (example %lld: %lld tokens)", (long long)e, (long long)(offsets[e + 1] - offsets[e]));
     return QLESS_OK;
 }
 
@@ -156,7 +163,7 @@ qless_status qless_attention(const void* q, int64_t ld_q, const void* k, int64_t
     QLESS_STEP(check_heads(tokens, n, heads, kv_heads, head_dim));
     QLESS_REQUIRE(std::isfinite(scale) && scale > 0.0f, QLESS_ERR_INVALID_ARG, "scale must be finite and positive");
     if (n == 0) return QLESS_OK;
-    QLESS_STEP(check_offsets(offsets, tokens, n));
+    QLESS_STEP(check_offsets(offsets, tokens, n, heads / kv_heads));
     if (tokens == 0) return QLESS_OK;
     QLESS_STEP(check_matrix("q", q, ld_q, (int64_t)heads * head_dim));
     QLESS_STEP(check_matrix("k", k, ld_k, (int64_t)kv_heads * head_dim));
@@ -185,7 +192,7 @@ qless_status qless_attention_backward(const void* grad_out, int64_t ld_grad_out,
     QLESS_STEP(check_heads(tokens, n, heads, kv_heads, head_dim));
     QLESS_REQUIRE(std::isfinite(scale) && scale > 0.0f, QLESS_ERR_INVALID_ARG, "scale must be finite and positive");
     if (n == 0) return QLESS_OK;
-    QLESS_STEP(check_offsets(offsets, tokens, n));
+    QLESS_STEP(check_offsets(offsets, tokens, n, heads / kv_heads));
     if (tokens == 0) return QLESS_OK;
     const int64_t wide = (int64_t)heads * head_dim, narrow = (int64_t)kv_heads * head_dim;
     QLESS_STEP(check_matrix("grad_out", grad_out, ld_grad_out, wide));
@@ -272,6 +279,8 @@ qless_status qless_gated_ffn_backward(const void* grad_out, int64_t ld_grad_out,
         return QLESS_OK;
     }
     const bool weights = grad_w_gate != nullptr || grad_w_up != nullptr || grad_w_down != nullptr;
+    // (a tile of a weight's gradient is one contraction over the tokens, and its epilogue waits for it: 2^20 stages, half a second)
+    QLESS_REQUIRE(!weights || tokens <= ((int64_t)1 << 27), QLESS_ERR_UNSUPPORTED, "tokens must be at most 2^27 where weights' gradients are wanted");
     QLESS_STEP(check_matrix("grad_out", grad_out, ld_grad_out, width));
     if (grad_w_gate != nullptr || grad_w_up != nullptr) QLESS_STEP(check_matrix("x", x, ld_x, width));
     QLESS_STEP(check_matrix("gate", gate, ld_gate, inner));

@@ -328,3 +328,36 @@ def test_in_captured_graphs_that_share_a_pool():
     torch.cuda.synchronize()
     assert same(fresh, outs[0])
     B.qless_check()
+
+
+def test_tables_of_work_in_captured_graphs_and_on_two_streams():
+    """So many examples that the tables of tiles lie in the workspace, put there by two launches each; two lists of examples take turns."""
+    H, K, D, n = 4, 1, 64, 300
+    lens = [[(7 * e + s) % 41 for e in range(n)] for s in (0, 13)]
+    off = [torch.tensor([sum(x[:e]) for e in range(n + 1)], dtype=torch.int64) for x in lens]
+    ins = [attention_inputs(int(o[-1]), H, K, D, 30 + i) for i, o in enumerate(off)]
+    want = [{k: t.clone() for k, t in run_attention(*x, o).items()} for x, o in zip(ins, off)]
+    torch.cuda.synchronize()
+    graphs, outs, pool = [], [], None
+    for x, o in zip(ins, off):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, pool=pool):
+            outs.append(run_attention(*x, o))
+        pool = pool or graph.pool()
+        graphs.append(graph)
+    for _ in range(3):
+        for graph, out, w in zip(graphs, outs, want):
+            graph.replay()
+            torch.cuda.synchronize()
+            assert same(w, out)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        for st, x, o in zip(streams, ins, off):
+            with torch.cuda.stream(st):
+                got.append(run_attention(*x, o))
+    torch.cuda.synchronize()
+    assert all(same(want[i % 2], g) for i, g in enumerate(got))
+    B.qless_check()

@@ -69,6 +69,10 @@ def test_attention_refusals(L):
         assert call(q=None) == B.ERR_INVALID_ARG and call(k=ODD) == B.ERR_INVALID_ARG and call(v=None) == B.ERR_INVALID_ARG and call(out=ODD) == B.ERR_INVALID_ARG
         assert call(ldq=504) == B.ERR_INVALID_ARG and call(ldk=132) == B.ERR_INVALID_ARG
         assert call(n=0, off=None, q=None) == B.QLESS_OK and call(tokens=0, n=2, off=(0, 0, 0), q=None, ws=None) == B.QLESS_OK
+    long = dict(heads=4096, kv=1, d=8, tokens=20000, n=2)     # 4096 heads share a key head: 2^13 tokens are the most
+    for call, wide in ((attn, dict(ldq=32768, ldo=32768)), (back, dict(ldq=32768, ldo=32768, lddo=32768, lddq=32768))):
+        assert call(**long, **wide, off=(3, 3, 8196)) == B.ERR_UNSUPPORTED and b"2^25" in L.qless_last_error()
+        assert call(**long, **wide, off=(3, 4, 8196)) == B.ERR_WORKSPACE
     assert attn(lse=C.c_void_p(4098)) == B.ERR_INVALID_ARG
     assert back(lse=None) == B.ERR_INVALID_ARG and back(dq=None) == B.ERR_INVALID_ARG and back(lddk=120) == B.ERR_INVALID_ARG and back(dout=ODD) == B.ERR_INVALID_ARG
 
@@ -95,6 +99,8 @@ def test_gated_ffn_refusals(L):
     assert back(gate=None) == B.ERR_INVALID_ARG and back(dg=None) == B.ERR_INVALID_ARG and back(dx=ODD) == B.ERR_INVALID_ARG and back(dy=None) == B.ERR_INVALID_ARG
     assert back(dwu=FAKE) == B.ERR_INVALID_ARG and b"x is required" in L.qless_last_error()
     assert back(dwd=ODD) == B.ERR_INVALID_ARG
+    assert back(dwd=FAKE, tokens=(1 << 27) + 1) == B.ERR_UNSUPPORTED and b"2^27" in L.qless_last_error()
+    assert back(dwd=FAKE, tokens=1 << 27) == B.ERR_WORKSPACE
 
 
 def test_binding_refusals():
