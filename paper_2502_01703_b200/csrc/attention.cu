@@ -495,7 +495,8 @@ qless_status launch_attention(const AttnArgs& a, uint8_t* ws, unsigned int* time
 {
     const int32_t pack = attn_pack(a.heads, a.kv_heads), tok = TILE / pack, packs = a.heads / pack;
     std::vector<AttnTile> tiles = query_tiles(a, 2 * tok);
-    // Too few pairs of tiles for the SMs: a tile to each block.
+    // Too few pairs of tiles for the SMs: a tile to each block (4000 tokens, 8/8 heads of 128: 64 us, in pairs 72; 16 examples of 8000 tokens in all, 16/4 heads,
+    // where there are enough: 59 us, in pairs 40).
     if ((int64_t)tiles.size() * packs < sm_count()) {
         tiles = query_tiles(a, tok);
         for (AttnTile& t : tiles) t.unused = 1;

@@ -68,7 +68,8 @@ __device__ __forceinline__ void by_activation(int act, F f)
     else f(std::integral_constant<int, QLESS_GELU>{});
 }
 
-// Few tokens (ffn_few.cu): the weights' rows or columns are the tile's rows, the tokens its columns.
+// Few tokens (ffn_few.cu): the weights' rows or columns are the tile's rows, the tokens its columns, as many as fit. 4096 x 11008, forward and
+// backward: 200 tokens 96 and 100 us, 256 tokens 105 and 110 us; on pairs of SMs (ffn.cu) 117 and 162, 118 and 162 us.
 constexpr int FEW = 256;
 inline bool few_tokens(int64_t tokens) { return tokens <= FEW; }
 size_t few_workspace(int64_t tokens, int32_t width, int32_t inner, bool backward);

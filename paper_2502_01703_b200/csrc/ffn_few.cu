@@ -315,14 +315,20 @@ __global__ void __launch_bounds__(256) few_finish_kernel(const FinishParams p)
     }
 }
 
-// Stages of a block: an even share of all, at least two; or whole tiles, where their rounds take no more than some 4 us longer than the even share (about what
-// the partial sums and the launch that joins them cost; a stage of 32 KiB of weights takes a block about 0.4 us).
+// Stages of a block: an even share of all, at least two; or whole tiles, where their rounds are at most 30 stages longer than the even share (a stage of 32 KiB of
+// weights takes a block about 0.3 us, the partial sums and the launch that joins them 8 us; 61 tokens x 4096 x 11008 forward: 60 us with whole tiles of gate and up, 63 with
+// shares; 30 x 4096 x 14336: 64 and 72; 200 x 1024 x 2816, the other way: 40 and 37; 250 x 2048 x 5632 with whole tiles of the down projection too: 73, with shares 60). GLU_BACK does so for few tokens alone: its
+// epilogue reads and writes five values where others write one, and a tile's 128 threads are slower at that than a kernel of its own (64 tokens x 2048 x 5632
+// backward: 42 us with whole tiles, 34 with shares; 200 x 1024 x 2816: 72 and 35; 16 x 4096 x 11008: 60 and 56; 5 x 4096 x 11008: 53 and 54).
+constexpr int64_t FEW_ENOUGH = 8;
+
 struct Share { int32_t all, per, blocks, places, direct; };
-Share share_of(int64_t feats, int64_t kblocks)
+template <int MODE>
+Share share_of(int64_t tokens, int64_t feats, int64_t kblocks)
 {
     const int64_t tiles = (feats + 127) / 128, all = tiles * kblocks, sms = sm_count();
     const int64_t rounds = (tiles + sms - 1) / sms, even = (all + sms - 1) / sms;
-    if (rounds * kblocks - even <= 10) {
+    if (rounds * kblocks - even <= 30 && (MODE != GLU_BACK || tokens <= FEW_ENOUGH)) {
         const int64_t per = rounds * kblocks;
         return {(int32_t)all, (int32_t)per, (int32_t)((all + per - 1) / per), 0, 1};
     }
@@ -351,7 +357,7 @@ qless_status product(const char* name, const CUtensorMap& w, const CUtensorMap& 
     FewParams p{};
     p.kswitch = (int32_t)blocks_of(k, KB<MODE>);
     f.kblocks = (twice ? 2 : 1) * p.kswitch;
-    const Share s = share_of(f.feats, f.kblocks);
+    const Share s = share_of<MODE>(f.tokens, f.feats, f.kblocks);
     f.per = s.per;
     p.f = f; p.n_cols = n_cols; p.all = s.all; p.direct = s.direct; p.timeout_word = timeout_word;
     const size_t stage = A_BYTES + (size_t)n_cols * 2 * KB<MODE>, budget = 227 * 1024 - 1024 - sizeof(Bars);
@@ -383,8 +389,8 @@ qless_status token_map(CUtensorMap* m, const void* p, int64_t cols, int64_t toke
 
 size_t few_workspace(int64_t tokens, int32_t width, int32_t inner, bool backward)
 {
-    const size_t first = backward ? (size_t)share_of(inner, blocks_of(width, KB<GLU_BACK>)).places : (size_t)2 * share_of(inner, blocks_of(width, KB<GLU>)).places;
-    const size_t second = (size_t)share_of(width, (backward ? 2 : 1) * blocks_of(inner, KB<OUT>)).places;
+    const size_t first = backward ? (size_t)share_of<GLU_BACK>(tokens, inner, blocks_of(width, KB<GLU_BACK>)).places : (size_t)2 * share_of<GLU>(tokens, inner, blocks_of(width, KB<GLU>)).places;
+    const size_t second = (size_t)share_of<OUT>(tokens, width, (backward ? 2 : 1) * blocks_of(inner, KB<OUT>)).places;
     return align_up((size_t)tokens * 4 * std::max(first * inner, second * width), 256);
 }
 

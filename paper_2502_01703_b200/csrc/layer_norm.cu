@@ -296,10 +296,10 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormParams p
     }
 }
 
-// The same with the sums, rows brought ahead by bulk copies: every worker has a ring of `stages` places of a row of x and one of dy. A worker takes
-// ROWS rows at a time (two where there are places and, with up to 24 columns a thread, registers enough: their weights are unpacked once and they share a
-// barrier: 65521 x 4112 bf16 in XXX us, one at a time 425). EIGHTS: columns of a thread, in eights. A row is read from its place
-// twice (for the two means, then for dx); the place is filled again behind the barrier of the next rows' means, when every thread of the worker has left it.
+// The same with the sums, rows brought ahead by bulk copies: every worker has a ring of `stages` places of a row of x and one of dy. EIGHTS: columns
+// of a thread, in eights. A row is read from its place twice (for the two means, then for dx); the place is filled again behind the barrier of the next
+// row's means, when every thread of the worker has left it. (Two rows at a time, which share a barrier and the weights' unpacking: the same times within 1 %,
+// 32768 rows of 1024 to 5632 columns, bf16 and fp32.)
 struct RingParams {
     NormParams n;
     int32_t stages, row_bytes;
@@ -308,11 +308,11 @@ struct RingParams {
 
 struct __align__(128) RingBars {
     uint64_t full[8][8];                    // [worker of the block][place]
-    float room[2][16][4];                   // [turn][warp][means of the rows], of a worker of several warps
+    float room[2][16][2];                   // [turn][warp][means of a row], of a worker of several warps
     uint32_t abort_flag;
 };
 
-template <typename T, typename P, int ROWS, int EIGHTS>
+template <typename T, typename P, int EIGHTS>
 __global__ void __launch_bounds__(512, 1) norm_backward_ring_kernel(const RingParams q)
 {
     using namespace tc;
@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(512, 1) norm_backward_ring_kernel(const RingPa
     const int lane = threadIdx.x & 31, warp_of = rank >> 5, warps = share >> 5;
     const int half = warps > 1 ? 1 << (31 - __clz(warps - 1)) : 0, at = lane & (2 * half - 1);      // (as in row_sum)
     uint64_t* full = bars->full[mine];
-    float (*room)[16][4] = bars->room;
+    float (*room)[16][2] = bars->room;
     if (threadIdx.x == 0) {
         for (int i = 0; i < per; ++i) for (int s = 0; s < q.stages; ++s) mbar_init(smem_u32(&bars->full[i][s]), 1);
         bars->abort_flag = 0;
@@ -347,112 +347,74 @@ __global__ void __launch_bounds__(512, 1) norm_backward_ring_kernel(const RingPa
     uint64_t sw[N * V / 2], sb[N * V / 2];
 #pragma unroll
     for (int k = 0; k < N * V / 2; ++k) sw[k] = sb[k] = 0;
-    int place[ROWS], turn = 0;
-    uint32_t parity[ROWS];
-    float mu[ROWS], r[ROWS], mu_next[ROWS], r_next[ROWS];
+    int place = 0, turn = 0;
+    uint32_t parity = 0;
+    float mu_next = 0.0f, r_next = 0.0f;
     bool there = true;                                       // a copy that did not come within the wait's limit: nothing is waited for any more
     auto stats = [&](int64_t t) {
-#pragma unroll
-        for (int u = 0; u < ROWS; ++u)
-            if (t + u * workers < p.tokens) {
-                mu_next[u] = p.mean != nullptr ? p.mean[t + u * workers] : 0.0f;
-                r_next[u] = p.rstd[t + u * workers];
-            }
-    };
-#pragma unroll
-    for (int u = 0; u < ROWS; ++u) { place[u] = u; parity[u] = 0; mu_next[u] = r_next[u] = 0.0f; }
-    stats(worker);
-    for (int64_t t = worker; t < p.tokens; t += ROWS * workers) {
-        const bool full_set = ROWS == 1 || t + workers < p.tokens;      // the last set may be short of its second row: it counts as one of zeros
-#pragma unroll
-        for (int u = 0; u < ROWS; ++u) { mu[u] = mu_next[u]; r[u] = r_next[u]; }
-        stats(t + ROWS * workers);
-        const uint8_t* xs[ROWS];
-#pragma unroll
-        for (int u = 0; u < ROWS; ++u) {
-            if (there && (u == 0 || full_set)) there = mbar_wait(smem_u32(&full[place[u]]), parity[u], &bars->abort_flag, q.timeout_word, TO_PRODUCER);
-            xs[u] = ring + (size_t)place[u] * 2 * q.row_bytes;
+        if (t < p.tokens) {
+            mu_next = p.mean != nullptr ? p.mean[t] : 0.0f;
+            r_next = p.rstd[t];
         }
-        auto values = [&](int u, int c, float* x, float* dy) {
-            if (ROWS > 1 && u > 0 && !full_set) {
-#pragma unroll
-                for (int e = 0; e < V; ++e) x[e] = dy[e] = 0.0f;
-                return;
-            }
-            Elem<T>::unpack(*reinterpret_cast<const uint4*>(xs[u] + c * sizeof(T)), x);
-            Elem<T>::unpack(*reinterpret_cast<const uint4*>(xs[u] + q.row_bytes + c * sizeof(T)), dy);
+    };
+    stats(worker);
+    for (int64_t t = worker; t < p.tokens; t += workers) {
+        const float mu = mu_next, r = r_next;
+        stats(t + workers);
+        if (there) there = mbar_wait(smem_u32(&full[place]), parity, &bars->abort_flag, q.timeout_word, TO_PRODUCER);
+        const uint8_t* xs = ring + (size_t)place * 2 * q.row_bytes;
+        auto values = [&](int c, float* x, float* dy) {
+            Elem<T>::unpack(*reinterpret_cast<const uint4*>(xs + c * sizeof(T)), x);
+            Elem<T>::unpack(*reinterpret_cast<const uint4*>(xs + q.row_bytes + c * sizeof(T)), dy);
         };
-        RowSums sums[ROWS];
+        RowSums sums;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int c = column<V>(n, 0, rank, share);
             if (c >= p.width) break;
-            float w[V];
+            float w[V], x[V], dy[V];
             load_params<P, V>(reinterpret_cast<const P*>(p.weight), n, p.width, rank, share, w);
-#pragma unroll
-            for (int u = 0; u < ROWS; ++u) {
-                float x[V], dy[V];
-                values(u, c, x, dy);
-                add_slot<V, true>(x, dy, w, mu[u], r[u], sums[u], sw + n * V / 2, sb + n * V / 2);
-            }
+            values(c, x, dy);
+            add_slot<V, true>(x, dy, w, mu, r, sums, sw + n * V / 2, sb + n * V / 2);
         }
-        float s[2 * ROWS];
+        float s[2];
+        close_sums(sums, s);
 #pragma unroll
-        for (int u = 0; u < ROWS; ++u) {
-            float one[2];
-            close_sums(sums[u], one);
-            s[2 * u] = one[0]; s[2 * u + 1] = one[1];
+        for (int d = 16; d > 0; d >>= 1) {
+            s[0] += __shfl_xor_sync(0xFFFFFFFFu, s[0], d);
+            s[1] += __shfl_xor_sync(0xFFFFFFFFu, s[1], d);
         }
-#pragma unroll
-        for (int d = 16; d > 0; d >>= 1)
-#pragma unroll
-            for (int k = 0; k < 2 * ROWS; ++k) s[k] += __shfl_xor_sync(0xFFFFFFFFu, s[k], d);
         if (warps > 1) {                                     // (in row_sum's order)
-            if (lane == 0) {
-#pragma unroll
-                for (int k = 0; k < 2 * ROWS; ++k) room[turn][warp_of][k] = s[k];
-            }
+            if (lane == 0) { room[turn][warp_of][0] = s[0]; room[turn][warp_of][1] = s[1]; }
             __syncthreads();                                 // (the block is this worker)
-#pragma unroll
-            for (int k = 0; k < 2 * ROWS; ++k) s[k] = at < warps ? room[turn][at][k] : 0.0f;
-            for (int d = half; d > 0; d >>= 1)
-#pragma unroll
-                for (int k = 0; k < 2 * ROWS; ++k) s[k] += __shfl_xor_sync(0xFFFFFFFFu, s[k], d);
+            s[0] = at < warps ? room[turn][at][0] : 0.0f;
+            s[1] = at < warps ? room[turn][at][1] : 0.0f;
+            for (int d = half; d > 0; d >>= 1) {
+                s[0] += __shfl_xor_sync(0xFFFFFFFFu, s[0], d);
+                s[1] += __shfl_xor_sync(0xFFFFFFFFu, s[1], d);
+            }
             turn ^= 1;
         } else {
             __syncwarp();
         }
-        // every thread of the worker has left the rows before: their places take the rows that are `stages` behind them
+        // every thread of the worker has left the row before: its place takes the row that is `stages` behind it
         if (rank == 0 && t > worker && there) {
-#pragma unroll
-            for (int u = 0; u < ROWS; ++u) {
-                const int64_t next = t + (int64_t)(q.stages - ROWS + u) * workers;
-                if (next < p.tokens) bring(next, place[u] >= ROWS ? place[u] - ROWS : place[u] + q.stages - ROWS);
-            }
+            const int64_t next = t + (int64_t)(q.stages - 1) * workers;
+            if (next < p.tokens) bring(next, place >= 1 ? place - 1 : q.stages - 1);
         }
-        float by_d[ROWS], shift[ROWS];
-#pragma unroll
-        for (int u = 0; u < ROWS; ++u) { by_d[u] = -r[u] * r[u] * (s[2 * u + 1] * inv * r[u]); shift[u] = p.center ? -s[2 * u] * inv * r[u] : 0.0f; }
+        const float by_d = -r * r * (s[1] * inv * r), shift = p.center ? -s[0] * inv * r : 0.0f;
         T* out = reinterpret_cast<T*>(p.out) + t * p.ld_out;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const int c = column<V>(n, 0, rank, share);
             if (c >= p.width) break;
-            float w[V];
+            float w[V], x[V], dy[V], dx[V];
             load_params<P, V>(reinterpret_cast<const P*>(p.weight), n, p.width, rank, share, w);
-#pragma unroll
-            for (int u = 0; u < ROWS; ++u) {
-                float x[V], dy[V], dx[V];
-                values(u, c, x, dy);
-                form_slot<V>(x, dy, w, mu[u], r[u], by_d[u], shift[u], dx);
-                if (u == 0 || full_set) store_slot<T, V>(out + u * workers * p.ld_out, n, p.width, rank, share, dx);
-            }
+            values(c, x, dy);
+            form_slot<V>(x, dy, w, mu, r, by_d, shift, dx);
+            store_slot<T, V>(out, n, p.width, rank, share, dx);
         }
-#pragma unroll
-        for (int u = 0; u < ROWS; ++u) {
-            place[u] += ROWS;
-            if (place[u] >= q.stages) { place[u] -= q.stages; parity[u] ^= 1u; }
-        }
+        if (++place == q.stages) { place = 0; parity ^= 1u; }
     }
     float* dst = p.part + worker * 2 * p.width;
 #pragma unroll
@@ -469,7 +431,7 @@ __global__ void __launch_bounds__(512, 1) norm_backward_ring_kernel(const RingPa
     }
     // behind a wait that gave up: what is still on its way arrives before the block leaves
     if (!there && rank == 0)
-        for (int s = 0; s < q.stages; ++s) mbar_wait_quiet(smem_u32(&full[s]), parity[0] ^ (s < place[0] ? 1u : 0u), 1u << 14);
+        for (int s = 0; s < q.stages; ++s) mbar_wait_quiet(smem_u32(&full[s]), parity ^ (s < place ? 1u : 0u), 1u << 14);
 }
 
 // dw and db from the workers' sums: a block has 32 columns (of dw, then of db), its 32 warps every 32nd worker each, joined in order.
@@ -546,27 +508,26 @@ cudaError_t backward_of(const NormPlan& pl, const NormParams& p, cudaStream_t st
     return launch_ahead(norm_backward_kernel<T, P, V, SUMS, 1024>, grid, block, 0, st, p);
 }
 
-template <typename T, typename P, int ROWS, int EIGHTS>
+template <typename T, typename P, int EIGHTS>
 cudaError_t ring_as(const NormPlan& pl, const RingParams& q, cudaStream_t st)
 {
-    const cudaError_t e = allow_full_smem<norm_backward_ring_kernel<T, P, ROWS, EIGHTS>>();
+    const cudaError_t e = allow_full_smem<norm_backward_ring_kernel<T, P, EIGHTS>>();
     if (e != cudaSuccess) return e;
     const size_t smem = sizeof(RingBars) + (size_t)(pl.block / pl.share) * pl.ring_stages * 2 * q.row_bytes;
-    return launch_ahead(norm_backward_ring_kernel<T, P, ROWS, EIGHTS>, dim3((unsigned)pl.blocks), dim3((unsigned)pl.block), smem, st, q);
+    return launch_ahead(norm_backward_ring_kernel<T, P, EIGHTS>, dim3((unsigned)pl.blocks), dim3((unsigned)pl.block), smem, st, q);
 }
 
 template <typename T, typename P>
 cudaError_t ring_of(const NormPlan& pl, const RingParams& q, cudaStream_t st)
 {
     const int eights = (q.n.width + 8 * pl.share - 1) / (8 * pl.share);
-    const bool two = pl.ring_stages >= 4;
-    if (eights == 1) return two ? ring_as<T, P, 2, 1>(pl, q, st) : ring_as<T, P, 1, 1>(pl, q, st);
+    if (eights == 1) return ring_as<T, P, 1>(pl, q, st);
     if constexpr (sizeof(T) == 4) {
-        return two ? ring_as<T, P, 2, 2>(pl, q, st) : ring_as<T, P, 1, 2>(pl, q, st);
+        return ring_as<T, P, 2>(pl, q, st);
     } else {
-        if (eights == 2) return two ? ring_as<T, P, 2, 2>(pl, q, st) : ring_as<T, P, 1, 2>(pl, q, st);
-        if (eights == 3) return two ? ring_as<T, P, 2, 3>(pl, q, st) : ring_as<T, P, 1, 3>(pl, q, st);
-        return ring_as<T, P, 1, 4>(pl, q, st);
+        if (eights == 2) return ring_as<T, P, 2>(pl, q, st);
+        if (eights == 3) return ring_as<T, P, 3>(pl, q, st);
+        return ring_as<T, P, 4>(pl, q, st);
     }
 }
 
