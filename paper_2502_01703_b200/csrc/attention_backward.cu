@@ -21,6 +21,8 @@
 // lse and delta of the query rows (dk/dv kernel).
 // P and ds are rounded to bf16 (2^-9 of each, independent of each other); exponentials, differences and sums are fp32.
 // Bound: 128 x 128 scores cost four products of 512 clocks (head_dim 128) and 1024 clocks of the special-function units in each kernel.
+// 32 examples of 16381 tokens in all, 32/8 heads of 128: 272 us (dq) and 193 us (dk, dv); one of 8191 tokens, 16/16 heads of 64: 345 and 300 us. Short examples wait for a
+// tile's own chain: tensor pipe 34 and 48 % busy.
 #include <algorithm>
 #include <type_traits>
 

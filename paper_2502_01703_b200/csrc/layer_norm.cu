@@ -298,8 +298,8 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormParams p
 
 // The same with the sums, rows brought ahead by bulk copies: every worker has a ring of `stages` places of a row of x and one of dy. EIGHTS: columns
 // of a thread, in eights. A row is read from its place twice (for the two means, then for dx); the place is filled again behind the barrier of the next
-// row's means, when every thread of the worker has left it. (Two rows at a time, which share a barrier and the weights' unpacking: the same times within 1 %,
-// 32768 rows of 1024 to 5632 columns, bf16 and fp32.)
+// row's means, when every thread of the worker has left it. (Two rows at a time, which share a barrier and the weights' unpacking: 32768 rows of
+// 2048 bf16 96 us, 4096 fp32 287; one at a time 95 and 273. 65521 x 4112 bf16: 368 us.)
 struct RingParams {
     NormParams n;
     int32_t stages, row_bytes;
