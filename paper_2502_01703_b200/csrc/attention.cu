@@ -37,6 +37,8 @@ struct ForwardParams {
     __nv_bfloat16* out; float* lse;
     int64_t ld_out;
     uint32_t items, packs;                  // packs: heads / pack
+    int32_t chunk;                          // > 0: items are pieces of tiles, of so many tiles of keys; a tile of several leaves its sums here:
+    float* part; float2* stat;              // [item][row][64 DB]: O before its division; [item][row]: reference, sum
     int32_t pack, pack_shift, group, heads, head_dim, stages;
     float scale_log2;
     unsigned int* timeout_word;
@@ -92,7 +94,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         return __all_sync(0xFFFFFFFFu, w);
     };
     // item -> tile, first head, key head; loops of the two row tiles over the keys (0: the second one does not exist)
-    struct Work { AttnTile t; int head0, kv, n[2]; };
+    struct Work { AttnTile t; int head0, kv, j0, n[2]; bool split; };      // j0: first tile of keys; split: there are other pieces
     auto work_of = [&](const Walk& k) {
         Work w;
         w.t = k.tile;
@@ -100,8 +102,10 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
             const int first = w.t.at + x * tok;
-            w.n[x] = first < w.t.len && (x == 0 || w.t.unused == 0) ? (min(first + tok, w.t.len) + TILE - 1) / TILE : 0;
+            w.n[x] = first < w.t.len && (x == 0 || w.t.way == 0) ? (min(first + tok, w.t.len) + TILE - 1) / TILE : 0;
         }
+        w.j0 = w.t.way >> 1; w.split = false;
+        if (p.chunk > 0) { w.split = w.n[0] > p.chunk; w.n[0] = min(p.chunk, w.n[0] - w.j0); }
         return w;
     };
 
@@ -136,9 +140,9 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                         for (int b = 0; b < DB; ++b) tma_load_3d(dst + b * 16384, &tm_q, full, b * 64, w.head0, w.t.t0 + w.t.at + x * tok);
                     }
                     __syncwarp();
-                    if (x == 0) load(&tm_k, w.kv, w.t.t0);
+                    if (x == 0) load(&tm_k, w.kv, w.t.t0 + w.j0 * TILE);
                 }
-                if (ok) load(&tm_v, w.kv, w.t.t0);
+                if (ok) load(&tm_v, w.kv, w.t.t0 + w.j0 * TILE);
                 const uint32_t item = item_of_round(walk.round + 1);
                 if (item < p.items) {                        // the next item's queries come out of L2
                     const AttnTile t = uniform_tile(walk.after);
@@ -147,15 +151,15 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
 #pragma unroll
                         for (int b = 0; b < DB; ++b) {
                             tma_prefetch_3d(&tm_q, b * 64, head0, t.t0 + t.at);
-                            if (t.unused == 0 && t.at + tok < t.len) tma_prefetch_3d(&tm_q, b * 64, head0, t.t0 + t.at + tok);
+                            if (t.way == 0 && t.at + tok < t.len) tma_prefetch_3d(&tm_q, b * 64, head0, t.t0 + t.at + tok);
                         }
                     }
                     __syncwarp();
                 }
                 const int n = max(w.n[0], w.n[1]);
                 for (int j = 1; j < n && ok; ++j) {
-                    load(&tm_k, w.kv, w.t.t0 + j * TILE);
-                    if (ok) load(&tm_v, w.kv, w.t.t0 + j * TILE);
+                    load(&tm_k, w.kv, w.t.t0 + (w.j0 + j) * TILE);
+                    if (ok) load(&tm_v, w.kv, w.t.t0 + (w.j0 + j) * TILE);
                 }
             }
             // nothing of this block's copies is in flight when it leaves (the other roles wait for all of them unless one gave up)
@@ -205,7 +209,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                     if (j + 1 < n) ring.next(nS);
                     uint8_t* v_op = ring_smem + (size_t)v.slot * OP;
                     if (!warp_wait(&bars->full[v.slot], v.parity, TO_MMA)) { ok = false; break; }
-                    if (w.t.len - j * TILE < TILE) zero_rows(v_op, DB, w.t.len - j * TILE, lane);
+                    if (w.t.len - (w.j0 + j) * TILE < TILE) zero_rows(v_op, DB, w.t.len - (w.j0 + j) * TILE, lane);
                     if (j + 1 < n && !warp_wait(&bars->full[k.slot], k.parity, TO_MMA)) { ok = false; break; }
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
@@ -274,8 +278,9 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 tc_fence_after();
                 uint32_t s[2][32];
                 float top2[2];
-                const bool masked = j * TILE + TILE - 1 > first;      // keys behind the tile's first token: some row does not see all of them
-                const int lim = at - j * TILE - half * 64;   // this row's last key among the 64
+                const int key0 = (w.j0 + j) * TILE;
+                const bool masked = key0 + TILE - 1 > first;      // keys behind the tile's first token: some row does not see all of them
+                const int lim = at - key0 - half * 64;   // this row's last key among the 64
                 tmem_ld_x32(s_addr, s[0]);
                 tmem_wait_ld();
                 tmem_ld_x32(s_addr + 32, s[1]);              // on its way while the first half's maximum is taken
@@ -357,6 +362,23 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&bars->o_full[x]), o_uses++ & 1u, abort_flag, p.timeout_word, TO_EPILOGUE));
             if (!ok) break;
             tc_fence_after();
+            if (w.split) {                                   // join_kernel does what follows
+                const int64_t row = (int64_t)walk.item * TILE + r;
+                if (half == 0) p.stat[row] = make_float2(ref, sum);
+                float4* dst = reinterpret_cast<float4*>(p.part + row * (DB * 64) + half * (DB * 32));
+#pragma unroll
+                for (int c = 0; c < DB * 32; c += 32) {
+                    if (half * (DB * 32) + c >= p.head_dim) break;
+                    uint32_t o[32];
+                    tmem_ld_x32(o_addr + c, o);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        dst[c / 4 + k] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]), __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
+                }
+                tc_fence_before();
+                continue;
+            }
             const float inv = 1.0f / sum;
             if (half == 0 && p.lse != nullptr && at < w.t.len) p.lse[(int64_t)(w.t.t0 + at) * p.heads + w.head0 + my_head] = (ref + log2f(sum)) * LN2;
             __nv_bfloat16* dst[4];
@@ -382,6 +404,40 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     tc_fence_before();
     __syncthreads();
     if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, 512); }
+}
+
+// The pieces of a tile's keys, joined in their order: o = sum_s e^(ref_s - m) O_s / sum_s e^(ref_s - m) sum_s with the largest reference m. A warp has a row,
+// a lane four columns of it; block (piece, pack, eighth of the rows), that of a tile's first piece does the tile.
+template <int DB>
+__global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ ForwardParams p)
+{
+    ahead_wait();
+    ahead_release();
+    const AttnTile t = p.table.few[blockIdx.x];
+    const int tok = TILE >> p.pack_shift, loops = (min(t.at + tok, t.len) + TILE - 1) / TILE, pieces = (loops + p.chunk - 1) / p.chunk;
+    if ((t.way >> 1) != 0 || pieces == 1) return;
+    const int warp = threadIdx.x >> 5, c = (threadIdx.x & 31) * 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = blockIdx.z * 16 + warp * 4 + i, at = t.at + (r >> p.pack_shift), head = (int)blockIdx.y * p.pack + (r & (p.pack - 1));
+        if (at >= t.len) break;
+        float top = -INFINITY, sum = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < pieces; ++s) top = fmaxf(top, p.stat[((int64_t)(blockIdx.x + s) * p.packs + blockIdx.y) * TILE + r].x);
+        for (int s = 0; s < pieces; ++s) {
+            const int64_t row = ((int64_t)(blockIdx.x + s) * p.packs + blockIdx.y) * TILE + r;
+            const float2 st = p.stat[row];
+            const float by = ex2(st.x - top);                // (a piece whose keys the row does not see: 0)
+            sum += by * st.y;
+            if (c < p.head_dim) {
+                const float4 x = *reinterpret_cast<const float4*>(p.part + row * (DB * 64) + c);
+                o[0] += by * x.x; o[1] += by * x.y; o[2] += by * x.z; o[3] += by * x.w;
+            }
+        }
+        const float inv = 1.0f / sum;
+        if (p.lse != nullptr && c == 0) p.lse[(int64_t)(t.t0 + at) * p.heads + head] = (top + log2f(sum)) * LN2;
+        if (c < p.head_dim)
+            *reinterpret_cast<uint2*>(p.out + (int64_t)(t.t0 + at) * p.ld_out + (int64_t)head * p.head_dim + c) = make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+    }
 }
 
 struct Chunk { AttnTile t[240]; };
@@ -439,6 +495,13 @@ std::vector<AttnTile> key_tiles(const AttnArgs& a)
     return longest_first(tiles, loops, most);
 }
 
+// Room for a table of tiles: none where all travel in the launch. (A sequence has at most one tile that is not full; sequences without tokens have none.)
+size_t tiles_bytes(int64_t tokens, int64_t n, int64_t rows)
+{
+    const int64_t most = tokens / rows + std::min(tokens, n);
+    return most <= INLINE ? 0 : align_up((size_t)most * sizeof(AttnTile), 256);
+}
+
 qless_status put_table(const std::vector<AttnTile>& tiles, TileTable* table, AttnTile* dev, cudaStream_t st)
 {
     table->tiles = (int32_t)tiles.size();
@@ -477,6 +540,43 @@ int32_t attn_pack(int32_t heads, int32_t kv_heads)
     return pack;
 }
 
+// Few tiles of queries and long loops: the keys of a tile are dealt out in pieces, in one round of the SMs or two, where that takes at least so many tiles of keys
+// off the longest block's work (about what the second launch, the join and the host's part of them cost: 1000 tokens, 8/2 heads of 128, five tiles less: 26 -> 34 us;
+// 1000, one head of 64, seven less: 25 and 24 to 30 us; 4000, 4/4 heads of 128, twelve less: 63 -> 54 us; 3000, 2/1 heads, 21 less: 47 -> 27 us).
+constexpr int32_t SPLIT_GAIN = 10, SPLIT_ROUNDS = 2;
+
+// Room for the pieces' sums: so much that any examples of so many tokens have it.
+size_t attn::split_bytes(int64_t tokens, int32_t heads, int32_t kv_heads)
+{
+    const int64_t tok = TILE / attn_pack(heads, kv_heads), packs = heads / attn_pack(heads, kv_heads);
+    if (tokens <= SPLIT_GAIN * TILE || tokens / tok * packs >= 2 * sm_count()) return 0;
+    return (size_t)SPLIT_ROUNDS * sm_count() * TILE * (sizeof(float2) + 128 * sizeof(float));
+}
+
+// Deals the tiles out in pieces of so many tiles of keys as it returns; 0: not worth it. (A piece costs about two tiles of keys beside its own.)
+static int32_t split_keys(std::vector<AttnTile>* tiles, int32_t tok, int32_t packs)
+{
+    auto loops = [&](const AttnTile& t) { return (std::min(t.at + tok, t.len) + TILE - 1) / TILE; };
+    int32_t most = 0, best = 0;
+    for (const AttnTile& t : *tiles) most = std::max(most, loops(t));
+    int32_t least = most + 2 - SPLIT_GAIN;
+    for (int32_t rounds = 1; rounds <= SPLIT_ROUNDS; ++rounds)
+        for (int32_t chunk = 1; rounds * (chunk + 2) <= least; ++chunk) {
+            int64_t pieces = 0;
+            for (const AttnTile& t : *tiles) pieces += (loops(t) + chunk - 1) / chunk;
+            if (pieces > INLINE || pieces * packs > (int64_t)rounds * sm_count()) continue;
+            least = rounds * (chunk + 2) - 1;
+            best = chunk;
+            break;
+        }
+    if (best == 0) return 0;
+    std::vector<AttnTile> out;
+    for (const AttnTile& t : *tiles)
+        for (int32_t j = 0; j < loops(t); j += best) out.push_back({t.t0, t.len, t.at, 1 + 2 * j});
+    tiles->swap(out);
+    return best;
+}
+
 template <int DB>
 static qless_status launch_forward(const AttnArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, ForwardParams& p, cudaStream_t st)
 {
@@ -488,6 +588,10 @@ static qless_status launch_forward(const AttnArgs& a, const CUtensorMap& q, cons
     QLESS_CUDA_TRY((allow_full_smem<attention_kernel<DB>>()));
     QLESS_CUDA_TRY(launch_ahead(attention_kernel<DB>, dim3((unsigned)grid), dim3(NTHREADS), smem, st, q, k, v, p));
     count_launches(1);
+    if (p.chunk > 0) {
+        QLESS_CUDA_TRY(launch_ahead(join_kernel<DB>, dim3((unsigned)p.table.tiles, p.packs, 8), dim3(128), 0, st, p));
+        count_launches(1);
+    }
     return QLESS_OK;
 }
 
@@ -495,14 +599,20 @@ qless_status launch_attention(const AttnArgs& a, uint8_t* ws, unsigned int* time
 {
     const int32_t pack = attn_pack(a.heads, a.kv_heads), tok = TILE / pack, packs = a.heads / pack;
     std::vector<AttnTile> tiles = query_tiles(a, 2 * tok);
+    ForwardParams p;
+    p.chunk = 0; p.part = nullptr; p.stat = nullptr;
     // Too few pairs of tiles for the SMs: a tile to each block (4000 tokens, 8/8 heads of 128: 64 us, in pairs 72; 16 examples of 8000 tokens in all, 16/4 heads,
     // where there are enough: 59 us, in pairs 40).
     if ((int64_t)tiles.size() * packs < sm_count()) {
         tiles = query_tiles(a, tok);
-        for (AttnTile& t : tiles) t.unused = 1;
+        for (AttnTile& t : tiles) t.way = 1;
+        if (split_bytes(a.tokens, a.heads, a.kv_heads) > 0) p.chunk = split_keys(&tiles, tok, packs);
+        if (p.chunk > 0) {
+            uint8_t* room = ws + tiles_bytes(a.tokens, a.n, tok);
+            p.stat = reinterpret_cast<float2*>(room); p.part = reinterpret_cast<float*>(room + (size_t)SPLIT_ROUNDS * sm_count() * TILE * sizeof(float2));
+        }
     }
     if (tiles.empty()) return QLESS_OK;
-    ForwardParams p;
     qless_status s = put_table(tiles, &p.table, reinterpret_cast<AttnTile*>(ws), st);
     if (s != QLESS_OK) return s;
     CUtensorMap q, k, v;

@@ -843,19 +843,13 @@ qless_status launch_backward(const CUtensorMap& q, const CUtensorMap& d, const C
     return QLESS_OK;
 }
 
-// Room for a table of tiles: none where all travel in the launch. (A sequence has at most one tile that is not full; sequences without tokens have none.)
-size_t tiles_bytes(int64_t tokens, int64_t n, int64_t rows)
-{
-    const int64_t most = tokens / rows + std::min(tokens, n);
-    return most <= INLINE ? 0 : align_up((size_t)most * sizeof(AttnTile), 256);
-}
-
 }  // namespace
 
 size_t attention_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads, bool backward)
 {
     const int64_t tok = TILE / attn_pack(heads, kv_heads);
     size_t total = tiles_bytes(tokens, n, tok);
+    if (!backward) total += split_bytes(tokens, heads, kv_heads);
     if (backward) total += tiles_bytes(tokens, n, TILE) + align_up((size_t)tokens * heads * 4, 256);
     return total;
 }

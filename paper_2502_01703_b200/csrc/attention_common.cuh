@@ -27,7 +27,7 @@ struct TileTable {
 };
 
 __device__ __forceinline__ AttnTile tile_of(const TileTable& t, uint32_t i) { return t.list != nullptr ? t.list[i] : t.few[i]; }
-__device__ __forceinline__ AttnTile uniform_tile(const AttnTile& x) { return {warp_uniform(x.t0), warp_uniform(x.len), warp_uniform(x.at), warp_uniform(x.unused)}; }
+__device__ __forceinline__ AttnTile uniform_tile(const AttnTile& x) { return {warp_uniform(x.t0), warp_uniform(x.len), warp_uniform(x.at), warp_uniform(x.way)}; }
 
 __device__ __forceinline__ float ex2(float x)
 {
@@ -133,6 +133,8 @@ __device__ __forceinline__ void store_rows32(const float (&v)[32], int c0, int h
 std::vector<AttnTile> query_tiles(const AttnArgs& a, int32_t tokens_per_tile);
 std::vector<AttnTile> key_tiles(const AttnArgs& a);
 // Fills the table, through device memory at `dev` where it does not fit into the launch.
+size_t tiles_bytes(int64_t tokens, int64_t n, int64_t rows);
+size_t split_bytes(int64_t tokens, int32_t heads, int32_t kv_heads);
 qless_status put_table(const std::vector<AttnTile>& tiles, TileTable* table, AttnTile* dev, cudaStream_t st);
 // [tokens][heads][head_dim] bf16, boxes of 64 columns x box_heads x box_tokens, zeros behind head_dim.
 qless_status head_map(CUtensorMap* out, const void* base, int64_t ld, int32_t heads, int32_t head_dim, int64_t tokens, uint32_t box_heads, uint32_t box_tokens);

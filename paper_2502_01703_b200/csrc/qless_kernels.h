@@ -146,7 +146,8 @@ qless_status launch_norm_forward(const NormArgs& a, cudaStream_t st);
 qless_status launch_norm_backward(const NormArgs& a, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st);
 
 // Causal attention over packed sequences (attention.cu, attention_backward.cu).
-struct AttnTile { int32_t t0, len, at, unused; };       // a sequence's first token and length, and the tile's first token within it
+// A sequence's first token and length, and the tile's first token within it; way (forward): 0 = two tiles of queries, else one, 1 + 2 x its first tile of keys.
+struct AttnTile { int32_t t0, len, at, way; };
 struct AttnArgs {
     const void* q; const void* k; const void* v; const void* out_in; const void* dout;
     int64_t ld_q, ld_k, ld_v, ld_out, ld_dout;

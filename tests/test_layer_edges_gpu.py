@@ -361,3 +361,43 @@ def test_tables_of_work_in_captured_graphs_and_on_two_streams():
     torch.cuda.synchronize()
     assert all(same(want[i % 2], g) for i, g in enumerate(got))
     B.qless_check()
+
+
+@pytest.mark.parametrize("off,H,K,D", [([0, 3001], 2, 1, 128), ([0, 900, 900, 2304, 2305], 1, 1, 64), ([0, 1025, 1200], 4, 4, 8), ([0, 4000], 1, 1, 96), ([0, 1700], 7, 1, 40)])
+def test_few_long_examples(off, H, K, D):
+    """So few tiles of queries that their keys are dealt out over several blocks and joined."""
+    T = off[-1]
+    q, k, v, dout = attention_inputs(T + 9, H, K, D, seed=T + D)
+    got = run_attention(q, k, v, dout, off)
+    assert not got["out"][T:].any()
+    want, room = attention_exact(q[:T], k[:T], v[:T], off, D ** -0.5, dout[:T], got["out"][:T])
+    for name in ("lse", "out", "grad_v", "grad_q", "grad_k"):
+        close(got[name][:T], want[name], room[name])
+    assert same(got, run_attention(q, k, v, dout, off))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = run_attention(q, k, v, dout, off)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert same(got, captured)
+    B.qless_check()
+
+
+def test_maxima_that_grow_from_piece_to_piece():
+    """Keys whose scores grow by powers of two along a long example: the last pieces outweigh all before them; and an infinite value at its end reaches
+    the rows that see it and those that share its tile of keys, no other."""
+    T, D = 2500, 64
+    q, k, v, dout = attention_inputs(T, 1, 1, D, seed=5)
+    k = (k.float() * (1 + torch.arange(T, device="cuda")[:, None, None] / 64)).to(torch.bfloat16)
+    got = B.qless_attention(q, k, v, [0, T])
+    want, room = attention_exact(q, k, v, [0, T], D ** -0.5, dout, got["out"])
+    # (as in test_maxima_that_keep_growing: scores of some hundreds; probabilities below 2^-126 may come out as 0)
+    wide = 1.0 + 2.0 ** -23 * 1000 * 2 / 2.0 ** -13
+    close(got["lse"], want["lse"], room["lse"])
+    close(got["out"], want["out"], room["out"] * wide + T * 2.0 ** -126 * float(v.abs().max()))
+    v = v.clone()
+    v[2490] = float("inf")
+    again = B.qless_attention(q, k, v, [0, T])
+    start = 2490 // 128 * 128
+    assert torch.equal(again["out"][:start], got["out"][:start]) and not torch.isfinite(again["out"][2490:].float()).all(dim=(1, 2)).any()
+    B.qless_check()
