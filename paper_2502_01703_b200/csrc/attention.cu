@@ -540,39 +540,44 @@ int32_t attn_pack(int32_t heads, int32_t kv_heads)
     return pack;
 }
 
-// Few tiles of queries and long loops: the keys of a tile are dealt out in pieces, in one round of the SMs or two, where that takes at least so many tiles of keys
-// off the longest block's work (about what the second launch, the join and the host's part of them cost: 1000 tokens, 8/2 heads of 128, five tiles less: 26 -> 34 us;
-// 1000, one head of 64, seven less: 25 and 24 to 30 us; 4000, 4/4 heads of 128, twelve less: 63 -> 54 us; 3000, 2/1 heads, 21 less: 47 -> 27 us).
-constexpr int32_t SPLIT_GAIN = 10, SPLIT_ROUNDS = 2;
-
-// Room for the pieces' sums: so much that any examples of so many tokens have it.
-size_t attn::split_bytes(int64_t tokens, int32_t heads, int32_t kv_heads)
+// Room for the pieces' sums, wherever some examples of so many tokens may want it: whether a tile is dealt out follows from the examples' lengths alone, and
+// so do the results' bits. (The backward pass leaves two sums of a row, and its longest loop is that over the query rows of a tile of keys.)
+size_t attn::split_bytes(int64_t tokens, int32_t heads, int32_t kv_heads, bool backward)
 {
-    const int64_t tok = TILE / attn_pack(heads, kv_heads), packs = heads / attn_pack(heads, kv_heads);
-    if (tokens <= SPLIT_GAIN * TILE || tokens / tok * packs >= 2 * sm_count()) return 0;
-    return (size_t)SPLIT_ROUNDS * sm_count() * TILE * (sizeof(float2) + 128 * sizeof(float));
+    const int32_t pack = attn_pack(heads, kv_heads);
+    const int64_t steps = backward ? (tokens / (TILE / pack) + 1) * (heads / kv_heads / pack) : tokens / TILE + 1;
+    if (steps <= (backward ? SPLIT_BACKWARD : SPLIT_FORWARD)) return 0;
+    return (size_t)SPLIT_ROUNDS * sm_count() * TILE * (sizeof(float2) + (backward ? 256 : 128) * sizeof(float));
 }
 
-// Deals the tiles out in pieces of so many tiles of keys as it returns; 0: not worth it. (A piece costs about two tiles of keys beside its own.)
-static int32_t split_keys(std::vector<AttnTile>* tiles, int32_t tok, int32_t packs)
+// Deals the tiles out in pieces of so many steps of their loops as it returns; 0: not worth it. per: items of a tile; gain: what has to come off.
+int32_t attn::split_tiles(std::vector<AttnTile>* tiles, int32_t per, int32_t gain, const std::function<int32_t(const AttnTile&)>& loops)
 {
-    auto loops = [&](const AttnTile& t) { return (std::min(t.at + tok, t.len) + TILE - 1) / TILE; };
+    if (tiles->size() > (size_t)INLINE || (int64_t)tiles->size() * per > SPLIT_ROUNDS * sm_count()) return 0;
+    std::vector<int32_t> n;
     int32_t most = 0, best = 0;
-    for (const AttnTile& t : *tiles) most = std::max(most, loops(t));
-    int32_t least = most + 2 - SPLIT_GAIN;
-    for (int32_t rounds = 1; rounds <= SPLIT_ROUNDS; ++rounds)
-        for (int32_t chunk = 1; rounds * (chunk + 2) <= least; ++chunk) {
-            int64_t pieces = 0;
-            for (const AttnTile& t : *tiles) pieces += (loops(t) + chunk - 1) / chunk;
-            if (pieces > INLINE || pieces * packs > (int64_t)rounds * sm_count()) continue;
-            least = rounds * (chunk + 2) - 1;
-            best = chunk;
-            break;
+    for (const AttnTile& t : *tiles) { n.push_back(loops(t)); most = std::max(most, n.back()); }
+    auto fits = [&](int32_t chunk, int32_t rounds) {
+        int64_t pieces = 0;
+        for (int32_t x : n) pieces += (x + chunk - 1) / chunk;
+        return pieces <= INLINE && pieces * per <= (int64_t)rounds * sm_count();
+    };
+    int32_t least = most + 2 - std::max(gain, most / 20 * 3);      // (a piece costs about two steps beside its own)
+    for (int32_t rounds = 1; rounds <= SPLIT_ROUNDS; ++rounds) {
+        int32_t lo = 1, hi = least / rounds - 2;             // the smallest that fits
+        if (hi < lo || !fits(hi, rounds)) continue;
+        while (lo < hi) {
+            const int32_t mid = lo + (hi - lo) / 2;
+            if (fits(mid, rounds)) hi = mid;
+            else lo = mid + 1;
         }
+        least = rounds * (lo + 2) - 1;
+        best = lo;
+    }
     if (best == 0) return 0;
     std::vector<AttnTile> out;
-    for (const AttnTile& t : *tiles)
-        for (int32_t j = 0; j < loops(t); j += best) out.push_back({t.t0, t.len, t.at, 1 + 2 * j});
+    for (size_t i = 0; i < n.size(); ++i)
+        for (int32_t j = 0; j < n[i]; j += best) { out.push_back((*tiles)[i]); out.back().way = j; }
     tiles->swap(out);
     return best;
 }
@@ -605,8 +610,8 @@ qless_status launch_attention(const AttnArgs& a, uint8_t* ws, unsigned int* time
     // where there are enough: 59 us, in pairs 40).
     if ((int64_t)tiles.size() * packs < sm_count()) {
         tiles = query_tiles(a, tok);
-        for (AttnTile& t : tiles) t.way = 1;
-        if (split_bytes(a.tokens, a.heads, a.kv_heads) > 0) p.chunk = split_keys(&tiles, tok, packs);
+        p.chunk = split_tiles(&tiles, packs, SPLIT_FORWARD, [&](const AttnTile& t) { return (std::min(t.at + tok, t.len) + TILE - 1) / TILE; });
+        for (AttnTile& t : tiles) t.way = 1 + 2 * t.way;
         if (p.chunk > 0) {
             uint8_t* room = ws + tiles_bytes(a.tokens, a.n, tok);
             p.stat = reinterpret_cast<float2*>(room); p.part = reinterpret_cast<float*>(room + (size_t)SPLIT_ROUNDS * sm_count() * TILE * sizeof(float2));

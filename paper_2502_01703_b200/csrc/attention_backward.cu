@@ -39,6 +39,17 @@ constexpr int NTHREADS = 640;
 // Columns of step s (16 rows of the contraction) of a left operand in tensor memory that four groups of warps wrote, each over the first half of its own 32 columns.
 __device__ __forceinline__ constexpr uint32_t quarter_column(int s) { return (uint32_t)((s >> 1) * 32 + (s & 1) * 8); }
 
+// 32 columns of this lane's row of sums, as they are.
+__device__ __forceinline__ void put_sums(uint32_t taddr, float* dst)
+{
+    uint32_t o[32];
+    tmem_ld_x32(taddr, o);
+    tmem_wait_ld();
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        reinterpret_cast<float4*>(dst)[k] = make_float4(__uint_as_float(o[4 * k]), __uint_as_float(o[4 * k + 1]), __uint_as_float(o[4 * k + 2]), __uint_as_float(o[4 * k + 3]));
+}
+
 struct QueryParams {
     TileTable table;
     const __nv_bfloat16* out; const __nv_bfloat16* dout;
@@ -46,6 +57,8 @@ struct QueryParams {
     __nv_bfloat16* dq;
     int64_t ld_out, ld_dout, ld_dq;
     uint32_t items, packs;
+    int32_t chunk;                          // > 0: items are pieces of tiles, of so many tiles of keys; a tile of several leaves its sums here:
+    float* part; float2* stat;              // [item][row][dq, kbar: 64 DB each]; [item][row]: rho, delta as taken from the output (negated)
     int32_t pack, pack_shift, group, heads, head_dim;
     float scale, scale_log2;
     unsigned int* timeout_word;
@@ -107,12 +120,14 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const bool w = mbar_wait(smem_u32(bar), parity, abort_flag, p.timeout_word, code);
         return __all_sync(0xFFFFFFFFu, w);
     };
-    struct Work { AttnTile t; int head0, kv, n; };
+    struct Work { AttnTile t; int head0, kv, n; };           // (tiles of keys from t.way on)
+    auto loops = [&](const AttnTile& t) { return (min(t.at + tok, t.len) + TILE - 1) / TILE; };
     auto work_of = [&](const Walk& k) {
         Work w;
         w.t = k.tile;
         w.head0 = (int)k.sub * p.pack; w.kv = w.head0 / p.group;
-        w.n = (min(w.t.at + tok, w.t.len) + TILE - 1) / TILE;
+        w.n = loops(w.t) - w.t.way;
+        if (p.chunk > 0) w.n = min(p.chunk, w.n);
         return w;
     };
 
@@ -144,7 +159,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 __syncwarp();
                 for (int j = 0; j < w.n; ++j, ++tiles) {
                     if (!warp_wait(&bars->k_empty[k_ring.slot], k_ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
-                    load(&tm_k, &bars->k_full[k_ring.slot], k_smem + (size_t)k_ring.slot * OP, w.kv, w.t.t0 + j * TILE);
+                    load(&tm_k, &bars->k_full[k_ring.slot], k_smem + (size_t)k_ring.slot * OP, w.kv, w.t.t0 + (w.t.way + j) * TILE);
                     k_ring.next(KS);
                     if (j == 0) {
                         if (!warp_wait(&bars->do_empty, (items & 1u) ^ 1u, TO_PRODUCER)) { ok = false; break; }
@@ -162,7 +177,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                         }
                     }
                     if (!warp_wait(&bars->v_empty[v_ring.slot], v_ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
-                    load(&tm_v, &bars->v_full[v_ring.slot], v_smem + (size_t)v_ring.slot * OP, w.kv, w.t.t0 + j * TILE);
+                    load(&tm_v, &bars->v_full[v_ring.slot], v_smem + (size_t)v_ring.slot * OP, w.kv, w.t.t0 + (w.t.way + j) * TILE);
                     v_ring.next(VS);
                 }
             }
@@ -199,7 +214,8 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 if (a.j == 0 && !warp_wait(&bars->q_full[a.items & 1u], (a.items >> 1) & 1u, TO_MMA)) return false;
                 if (!warp_wait(&bars->k_full[k_ring.slot], k_ring.parity, TO_MMA)) return false;
                 uint8_t* op = k_smem + (size_t)k_ring.slot * OP;
-                if (a.w.t.len - a.j * TILE < TILE) zero_rows(op, DB, a.w.t.len - a.j * TILE, lane);
+                const int have = a.w.t.len - (a.w.t.way + a.j) * TILE;
+                if (have < TILE) zero_rows(op, DB, have, lane);
                 tc_fence_after();
                 if (elect_one()) {
                     product(tmem, q_smem + (a.items & 1u) * OP, op);
@@ -332,8 +348,9 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 tmem_ld_x16(s_addr, s[0]);
                 tmem_wait_ld();
                 tmem_ld_x16(s_addr + 16, s[1]);
-                const bool masked = j * TILE + TILE - 1 > w.t.at;
-                const int lim = at - j * TILE - part * 32;   // this row's last key among the 32
+                const int key0 = (w.t.way + j) * TILE;
+                const bool masked = key0 + TILE - 1 > w.t.at;
+                const int lim = at - key0 - part * 32;   // this row's last key among the 32
                 auto hide = [&](uint64_t x, int k) {         // zeros behind it
                     float a, b;
                     split_pair(x, a, b);
@@ -419,7 +436,12 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (!ok) break;
             rho = bars->lse[r] + bars->delta[r];
             here(&bars->rho_read);
-            if (part == 0 && at < w.t.len) p.delta[(int64_t)(w.t.t0 + at) * p.heads + w.head0 + my_head] = delta - rho;      // (negated)
+            const bool split = p.chunk > 0 && loops(w.t) > p.chunk;      // there are other pieces of this tile
+            const int64_t sums_row = (int64_t)item_of_round(walk.round - 1) * TILE + r;
+            if (part == 0 && at < w.t.len) {
+                if (split) p.stat[sums_row] = make_float2(rho, delta);
+                else p.delta[(int64_t)(w.t.t0 + at) * p.heads + w.head0 + my_head] = delta - rho;      // (negated)
+            }
             tc_fence_after();
             __nv_bfloat16* dst[4];
 #pragma unroll
@@ -427,7 +449,12 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 const int rr = (warp & 3) * 32 + (lane & ~3) + k, a = w.t.at + (rr >> p.pack_shift);
                 dst[k] = a < w.t.len ? p.dq + (int64_t)(w.t.t0 + a) * p.ld_dq + (int64_t)(w.head0 + (rr & (p.pack - 1))) * p.head_dim : nullptr;
             }
-            if (part * 32 < p.head_dim) {
+            if (split) {                                     // query_join_kernel does what follows
+                if (part * 32 < p.head_dim) {
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) put_sums(tmem + lanes + 256 + h * 128 + part * 32, p.part + (sums_row * 2 + h) * (DB * 64) + part * 32);
+                }
+            } else if (part * 32 < p.head_dim) {
                 uint32_t o[32];
                 float f[32];
                 tmem_ld_x32(tmem + lanes + 256 + part * 32, o);
@@ -457,6 +484,8 @@ struct KeyParams {
     __nv_bfloat16* dk; __nv_bfloat16* dv;
     int64_t ld_dk, ld_dv;
     uint32_t items, kv_heads;
+    int32_t chunk;                          // > 0: items are pieces of tiles, of so many tiles of queries; a tile of several leaves its sums here:
+    float* part;                            // [item][row][dv, dk: 64 DB each]
     int32_t pack, pack_shift, group, heads, head_dim;
     float scale, scale_log2;
     unsigned int* timeout_word;
@@ -516,7 +545,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         return __all_sync(0xFFFFFFFFu, w);
     };
     // loops: for every pass over `pack` heads of the group, the tiles of queries from the one that holds the first key's token on
-    struct Work { AttnTile t; int kv, first, per, n; };
+    struct Work { AttnTile t; int kv, first, per, n, head0, i, left; };      // head0, i, left: where they begin (pieces: step t.way)
     auto work_of = [&](const Walk& k) {
         Work w;
         w.kv = (int)k.sub;
@@ -524,6 +553,12 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         w.first = w.t.at >> (7 - p.pack_shift);
         w.per = ((w.t.len + tok - 1) >> (7 - p.pack_shift)) - w.first;
         w.n = w.per * passes;
+        w.head0 = w.kv * p.group; w.i = w.first; w.left = w.per;
+        if (p.chunk > 0) {
+            const int j0 = w.t.way, pass = j0 / w.per, in = j0 - pass * w.per;
+            w.n = min(p.chunk, w.n - j0);
+            w.head0 += pass * p.pack; w.i += in; w.left -= in;
+        }
         return w;
     };
 
@@ -565,7 +600,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     }
                     __syncwarp();
                 }
-                int head0 = w.kv * p.group, i = w.first, left = w.per;
+                int head0 = w.head0, i = w.i, left = w.left;
                 for (int j = 0; j < w.n; ++j, ++tiles, q_ring.next(QS), do_ring.next(DS)) {
                     if (!warp_wait(&bars->q_empty[q_ring.slot], q_ring.parity ^ 1u, TO_PRODUCER)) { ok = false; break; }
                     load(&tm_q, &bars->q_full[q_ring.slot], q_smem + (size_t)q_ring.slot * OP, head0, w.t.t0 + i * tok);
@@ -602,7 +637,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             for (Walk walk(p.table, p.items, p.kv_heads); walk.more && ok; walk.next()) {
                 const Work w = work_of(walk);
                 if (!warp_wait(&bars->kv_full, kv_uses++ & 1u, TO_MMA)) { ok = false; break; }
-                int i = w.first, left = w.per, have = TILE;   // have: query rows of the tile at `q_ring` that are there
+                int i = w.i, left = w.left, have = TILE;   // have: query rows of the tile at `q_ring` that are there
                 // The tile's queries (its dO) have arrived; rows behind the sequence's end become zeros in both operands (they meet P = dS = 0).
                 auto q_arrived = [&](const Ring& at) -> bool {
                     if (!warp_wait(&bars->q_full[at.slot], at.parity, TO_MMA)) return false;
@@ -671,7 +706,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             bool ok = true;
             for (Walk walk(p.table, p.items, p.kv_heads); walk.more && ok; walk.next()) {
                 const Work w = work_of(walk);
-                int head0 = w.kv * p.group, i = w.first, left = w.per;
+                int head0 = w.head0, i = w.i, left = w.left;
                 for (int j = 0; j < w.n; ++j, ++tiles, ring.next(LSE_STAGES)) {
                     float lse[2], delta[2];
 #pragma unroll
@@ -709,7 +744,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         for (Walk walk(p.table, p.items, p.kv_heads); walk.more && ok; walk.next()) {
             const Work w = work_of(walk);
             const int key = w.t.at + r;
-            int i = w.first, left = w.per;
+            int i = w.i, left = w.left;
             for (int j = 0; j < w.n; ++j, ++uses, ring.next(LSE_STAGES)) {
                 // column c of this quarter is query row part * 32 + c: token i * tok + (part * 32 + c) / pack; it sees this row's key from `from` on
                 const bool masked = i * tok < w.t.at + TILE - 1;
@@ -800,6 +835,13 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             tc_fence_after();
             // two groups of warps have dv, two dk: every other 32 columns each
             const bool is_k = part >= 2;
+            if (p.chunk > 0 && w.per * passes > p.chunk) {   // (other pieces of this tile) key_join_kernel does what follows
+#pragma unroll 1
+                for (int c = (part & 1) * 32; c < p.head_dim; c += 64)
+                    put_sums(tmem + lanes + 256 + (is_k ? 128 : 0) + c, p.part + (((int64_t)walk.item * TILE + r) * 2 + (is_k ? 1 : 0)) * (DB * 64) + c);
+                tc_fence_before();
+                continue;
+            }
             __nv_bfloat16* base = is_k ? p.dk : p.dv;
             const int64_t ld = is_k ? p.ld_dk : p.ld_dv;
             const float by = is_k ? p.scale : 1.0f;
@@ -825,6 +867,68 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, 512); }
 }
 
+// The pieces of a tile, added up in their order. A warp has a row, a lane four columns of it; block (piece, head or pack of heads, eighth of the rows), that
+// of a tile's first piece does the tile.
+template <int DB>
+__global__ void __launch_bounds__(128) query_join_kernel(const __grid_constant__ QueryParams p)
+{
+    ahead_wait();
+    ahead_release();
+    const AttnTile t = p.table.few[blockIdx.x];
+    const int tok = TILE >> p.pack_shift, pieces = ((min(t.at + tok, t.len) + TILE - 1) / TILE + p.chunk - 1) / p.chunk;
+    if (t.way != 0 || pieces == 1) return;
+    const int c = (threadIdx.x & 31) * 4;
+    for (int i = 0; i < 4; ++i) {
+        const int r = blockIdx.z * 16 + (threadIdx.x >> 5) * 4 + i, at = t.at + (r >> p.pack_shift), head = (int)blockIdx.y * p.pack + (r & (p.pack - 1));
+        if (at >= t.len) break;
+        float rho = 0.0f, delta = 0.0f, dq[4] = {0.0f, 0.0f, 0.0f, 0.0f}, kbar[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < pieces; ++s) {
+            const int64_t row = ((int64_t)(blockIdx.x + s) * p.packs + blockIdx.y) * TILE + r;
+            const float2 st = p.stat[row];
+            rho += st.x; delta = st.y;
+            if (c < p.head_dim) {
+                const float4 a = *reinterpret_cast<const float4*>(p.part + row * 2 * (DB * 64) + c), b = *reinterpret_cast<const float4*>(p.part + (row * 2 + 1) * (DB * 64) + c);
+                dq[0] += a.x; dq[1] += a.y; dq[2] += a.z; dq[3] += a.w;
+                kbar[0] += b.x; kbar[1] += b.y; kbar[2] += b.z; kbar[3] += b.w;
+            }
+        }
+        if (c == 0) p.delta[(int64_t)(t.t0 + at) * p.heads + head] = delta - rho;
+        if (c < p.head_dim) {
+            float f[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f[k] = fmaf(-rho, kbar[k], dq[k]) * p.scale;
+            *reinterpret_cast<uint2*>(p.dq + (int64_t)(t.t0 + at) * p.ld_dq + (int64_t)head * p.head_dim + c) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
+        }
+    }
+}
+
+template <int DB>
+__global__ void __launch_bounds__(128) key_join_kernel(const __grid_constant__ KeyParams p)
+{
+    ahead_wait();
+    ahead_release();
+    const AttnTile t = p.table.few[blockIdx.x];
+    const int tok = TILE >> p.pack_shift, per = ((t.len + tok - 1) >> (7 - p.pack_shift)) - (t.at >> (7 - p.pack_shift));
+    const int pieces = (per * (p.group >> p.pack_shift) + p.chunk - 1) / p.chunk;
+    if (t.way != 0 || pieces == 1) return;
+    const int c = (threadIdx.x & 31) * 4;
+    if (c >= p.head_dim) return;
+    for (int i = 0; i < 4; ++i) {
+        const int r = blockIdx.z * 16 + (threadIdx.x >> 5) * 4 + i;
+        if (t.at + r >= t.len) break;
+        float dv[4] = {0.0f, 0.0f, 0.0f, 0.0f}, dk[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < pieces; ++s) {
+            const int64_t row = ((int64_t)(blockIdx.x + s) * p.kv_heads + blockIdx.y) * TILE + r;
+            const float4 a = *reinterpret_cast<const float4*>(p.part + row * 2 * (DB * 64) + c), b = *reinterpret_cast<const float4*>(p.part + (row * 2 + 1) * (DB * 64) + c);
+            dv[0] += a.x; dv[1] += a.y; dv[2] += a.z; dv[3] += a.w;
+            dk[0] += b.x; dk[1] += b.y; dk[2] += b.z; dk[3] += b.w;
+        }
+        const int64_t token = t.t0 + t.at + r, col = (int64_t)blockIdx.y * p.head_dim + c;
+        *reinterpret_cast<uint2*>(p.dv + token * p.ld_dv + col) = make_uint2(pack_bf16(dv[0], dv[1]), pack_bf16(dv[2], dv[3]));
+        *reinterpret_cast<uint2*>(p.dk + token * p.ld_dk + col) = make_uint2(pack_bf16(dk[0] * p.scale, dk[1] * p.scale), pack_bf16(dk[2] * p.scale, dk[3] * p.scale));
+    }
+}
+
 template <int DB>
 qless_status launch_backward(const CUtensorMap& q, const CUtensorMap& d, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& o, const QueryParams& qp, const KeyParams& kp, cudaStream_t st)
 {
@@ -834,11 +938,13 @@ qless_status launch_backward(const CUtensorMap& q, const CUtensorMap& d, const C
                   1024 + (2 + KeyStages<DB>::Q + KeyStages<DB>::D) * DB * 16384 + sizeof(KeyBars<DB>) <= 227 * 1024, "shared memory of an SM");
     { ProfileScope ps("attention_dq", st);
       QLESS_CUDA_TRY((allow_full_smem<attention_dq_kernel<DB>>()));
-      QLESS_CUDA_TRY(launch_ahead(attention_dq_kernel<DB>, dim3((unsigned)std::min<int64_t>(qp.items, sm_count())), dim3(NTHREADS), q_smem, st, q, d, k, v, o, qp)); }
+      QLESS_CUDA_TRY(launch_ahead(attention_dq_kernel<DB>, dim3((unsigned)std::min<int64_t>(qp.items, sm_count())), dim3(NTHREADS), q_smem, st, q, d, k, v, o, qp));
+      if (qp.chunk > 0) { QLESS_CUDA_TRY(launch_ahead(query_join_kernel<DB>, dim3((unsigned)qp.table.tiles, qp.packs, 8), dim3(128), 0, st, qp)); count_launches(1); } }
     count_launches(1);
     { ProfileScope ps("attention_dkv", st);
       QLESS_CUDA_TRY((allow_full_smem<attention_dkv_kernel<DB>>()));
-      QLESS_CUDA_TRY(launch_ahead(attention_dkv_kernel<DB>, dim3((unsigned)std::min<int64_t>(kp.items, sm_count())), dim3(NTHREADS), k_smem, st, q, d, k, v, kp)); }
+      QLESS_CUDA_TRY(launch_ahead(attention_dkv_kernel<DB>, dim3((unsigned)std::min<int64_t>(kp.items, sm_count())), dim3(NTHREADS), k_smem, st, q, d, k, v, kp));
+      if (kp.chunk > 0) { QLESS_CUDA_TRY(launch_ahead(key_join_kernel<DB>, dim3((unsigned)kp.table.tiles, kp.kv_heads, 8), dim3(128), 0, st, kp)); count_launches(1); } }
     count_launches(1);
     return QLESS_OK;
 }
@@ -849,7 +955,7 @@ size_t attention_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_
 {
     const int64_t tok = TILE / attn_pack(heads, kv_heads);
     size_t total = tiles_bytes(tokens, n, tok);
-    if (!backward) total += split_bytes(tokens, heads, kv_heads);
+    total += split_bytes(tokens, heads, kv_heads, backward);
     if (backward) total += tiles_bytes(tokens, n, TILE) + align_up((size_t)tokens * heads * 4, 256);
     return total;
 }
@@ -857,7 +963,7 @@ size_t attention_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_
 qless_status launch_attention_backward(const AttnArgs& a, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st)
 {
     const int32_t pack = attn_pack(a.heads, a.kv_heads), tok = TILE / pack, packs = a.heads / pack;
-    const std::vector<AttnTile> queries = query_tiles(a, tok), keys = key_tiles(a);
+    std::vector<AttnTile> queries = query_tiles(a, tok), keys = key_tiles(a);
     if (queries.empty()) return QLESS_OK;
     // (fewer key tiles than query tiles, and no more key heads than packs)
     QLESS_REQUIRE((int64_t)queries.size() * packs < MOST_ITEMS - 65536, QLESS_ERR_UNSUPPORTED, "too many tiles: %zu of %d heads", queries.size(), packs);
@@ -868,6 +974,12 @@ qless_status launch_attention_backward(const AttnArgs& a, uint8_t* ws, unsigned 
     float* delta = reinterpret_cast<float*>(ws + tiles_bytes(a.tokens, a.n, tok) + tiles_bytes(a.tokens, a.n, TILE));
     QueryParams qp;
     KeyParams kp;
+    const int32_t passes = a.heads / a.kv_heads / pack;
+    qp.chunk = split_tiles(&queries, packs, SPLIT_BACKWARD, [&](const AttnTile& t) { return (std::min(t.at + tok, t.len) + TILE - 1) / TILE; });
+    kp.chunk = split_tiles(&keys, a.kv_heads, SPLIT_BACKWARD, [&](const AttnTile& t) { return ((t.len + tok - 1) / tok - t.at / tok) * passes; });
+    // (one room for both: the keys' kernel begins when the queries' sums are joined)
+    uint8_t* room = reinterpret_cast<uint8_t*>(delta) + align_up((size_t)a.tokens * a.heads * 4, 256);
+    qp.stat = reinterpret_cast<float2*>(room); qp.part = kp.part = reinterpret_cast<float*>(room + (size_t)SPLIT_ROUNDS * sm_count() * TILE * sizeof(float2));
     qless_status s;
     if ((s = put_table(queries, &qp.table, q_list, st)) != QLESS_OK) return s;
     if ((s = put_table(keys, &kp.table, k_list, st)) != QLESS_OK) return s;

@@ -5,6 +5,7 @@
 // brings it, keys and values are read once for all of them, and short sequences fill their tiles better.
 #pragma once
 
+#include <functional>
 #include <vector>
 
 #include "pairs.cuh"
@@ -134,7 +135,14 @@ std::vector<AttnTile> query_tiles(const AttnArgs& a, int32_t tokens_per_tile);
 std::vector<AttnTile> key_tiles(const AttnArgs& a);
 // Fills the table, through device memory at `dev` where it does not fit into the launch.
 size_t tiles_bytes(int64_t tokens, int64_t n, int64_t rows);
-size_t split_bytes(int64_t tokens, int32_t heads, int32_t kv_heads);
+// Few tiles and long loops: a tile's loop is dealt out in pieces, in one round of the SMs or two, where that takes at least so many steps off the longest
+// block's work, and at least three in twenty (about what the launch of the join, the join and the host's part of them cost; backward there are two, with two sums
+// of a row each). Forward: 1000 tokens, 8/2 heads of 128, five steps less: 26 -> 34 us; 4000, 4/4 heads, twelve less: 63 -> 54 us; 3000, 2/1 heads, 21 less: 47 -> 27 us.
+// Backward: 4000 tokens, 4/4 heads, twelve less: 116 -> 122 us; 800, 8/2 heads, 22 less: 65 -> 50 us; 3000, 2/1 heads, 21 less: 123 -> 63 us; 3000, 32/1 heads:
+// 1276 -> 274 us (24 tiles of keys with up to 750 steps).
+constexpr int32_t SPLIT_FORWARD = 10, SPLIT_BACKWARD = 16, SPLIT_ROUNDS = 2;
+size_t split_bytes(int64_t tokens, int32_t heads, int32_t kv_heads, bool backward);
+int32_t split_tiles(std::vector<AttnTile>* tiles, int32_t per, int32_t gain, const std::function<int32_t(const AttnTile&)>& loops);
 qless_status put_table(const std::vector<AttnTile>& tiles, TileTable* table, AttnTile* dev, cudaStream_t st);
 // [tokens][heads][head_dim] bf16, boxes of 64 columns x box_heads x box_tokens, zeros behind head_dim.
 qless_status head_map(CUtensorMap* out, const void* base, int64_t ld, int32_t heads, int32_t head_dim, int64_t tokens, uint32_t box_heads, uint32_t box_tokens);

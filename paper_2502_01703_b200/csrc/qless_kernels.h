@@ -146,7 +146,7 @@ qless_status launch_norm_forward(const NormArgs& a, cudaStream_t st);
 qless_status launch_norm_backward(const NormArgs& a, uint8_t* ws, unsigned int* timeout_word, cudaStream_t st);
 
 // Causal attention over packed sequences (attention.cu, attention_backward.cu).
-// A sequence's first token and length, and the tile's first token within it; way (forward): 0 = two tiles of queries, else one, 1 + 2 x its first tile of keys.
+// A sequence's first token and length, and the tile's first token within it; way: the first step of its loop; forward: 0 = two tiles of queries, else one, 1 + 2 x its first tile of keys.
 struct AttnTile { int32_t t0, len, at, way; };
 struct AttnArgs {
     const void* q; const void* k; const void* v; const void* out_in; const void* dout;

@@ -401,3 +401,16 @@ def test_maxima_that_grow_from_piece_to_piece():
     start = 2490 // 128 * 128
     assert torch.equal(again["out"][:start], got["out"][:start]) and not torch.isfinite(again["out"][2490:].float()).all(dim=(1, 2)).any()
     B.qless_check()
+
+
+@pytest.mark.parametrize("T,H,K,D", [(700, 32, 1, 128), (413, 24, 1, 64), (1003, 7, 1, 40)])
+def test_many_heads_that_share_a_key_head(T, H, K, D):
+    """So many query rows to so few tiles of keys that these rows are dealt out, over the passes of the group's heads too; an example without tokens between."""
+    off = [0, 5, 5, T]
+    q, k, v, dout = attention_inputs(T, H, K, D, seed=T + H)
+    got = run_attention(q, k, v, dout, off)
+    want, room = attention_exact(q, k, v, off, D ** -0.5, dout, got["out"])
+    for name in ("lse", "out", "grad_v", "grad_q", "grad_k"):
+        close(got[name], want[name], room[name])
+    assert same(got, run_attention(q, k, v, dout, off))
+    B.qless_check()
