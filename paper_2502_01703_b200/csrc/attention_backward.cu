@@ -5,8 +5,8 @@
 //
 // Two kernels, each with its sums in tensor memory from the first product to the last: one owns a tile of query rows and walks over the keys
 // (dq, and delta for the other), one owns a tile of keys and walks over the query rows of every head of its group (dk, dv). Scores and dp are
-// computed in both (seven products of a tile instead of five, and the eighth of kbar below), and in return no partial dq is added up in memory, nothing is
-// joined by atomics, and the same inputs give the same bits.
+// computed in both (seven products of a tile instead of five, and the eighth of kbar below), and in return nothing is joined by atomics and the same inputs
+// give the same bits. Where tiles are few and loops long, pieces of a loop leave their sums in memory and a small kernel adds them in order (split_tiles).
 //
 // delta taken from the output as it was handed on, in bf16, would be off by up to 2^-8 of |do| |o|, and with rows that look at few keys (|o| near |v|, ds small)
 // that is more than all other roundings together: errors of 3e-3 to 4.4e-3 of the gradients' norm were seen where 2.4e-3 are due to bf16 operands and
@@ -21,7 +21,7 @@
 // lse and delta of the query rows (dk/dv kernel).
 // P and ds are rounded to bf16 (2^-9 of each, independent of each other); exponentials, differences and sums are fp32.
 // Bound: 128 x 128 scores cost four products of 512 clocks (head_dim 128) and 1024 clocks of the special-function units in each kernel.
-// 32 examples of 16381 tokens in all, 32/8 heads of 128: 272 us (dq) and 193 us (dk, dv); one of 8191 tokens, 16/16 heads of 64: 345 and 300 us. Short examples wait for a
+// 32 examples of 16381 tokens in all, 32/8 heads of 128: 275 us (dq) and 193 us (dk, dv); one of 8191 tokens, 16/16 heads of 64: 345 and 300 us. Short examples wait for a
 // tile's own chain: tensor pipe 34 and 48 % busy.
 #include <algorithm>
 #include <type_traits>
