@@ -198,7 +198,8 @@ __global__ void __launch_bounds__(BLOCK) norm_forward_kernel(const NormParams p)
 }
 
 // A row's backward pass in three steps, the same in both kernels, so that dx has the same bits with and without the sums. With d = x - mu, g = w dy:
-//   (1) sums of g and of g d (and, by column, of dy and r dy d)   (2) over the threads   (3) dx = d A + (g r - m r),  m = mean g,  A = -r^3 mean(g d)
+//   (1) sums of g and of g d (and, by column, of dy and r dy d)   (2) over the threads   (3) dx = (d r) A + (g r - m r),  m = mean g,  A = -r (mean(g d) r)
+// (d r is formed first and the factors of A in this order because r^2 and r^3 leave fp32's range where r and dx do not: a spread of 5e-20 or less, with eps = 0.)
 struct RowSums { uint64_t g = 0, gd = 0; };
 
 template <int S, bool SUMS>
@@ -223,13 +224,13 @@ __device__ __forceinline__ void close_sums(const RowSums& sums, float (&s)[2])
     s[1] = a + b;
 }
 template <int S>
-__device__ __forceinline__ void form_slot(const float* x, const float* dy, const float* w, float mu, float r, float by_d, float shift, float* dx)
+__device__ __forceinline__ void form_slot(const float* x, const float* dy, const float* w, float mu, float r, float by_xh, float shift, float* dx)
 {
-    const uint64_t mu2 = pair_of(-mu, -mu), r2 = pair_of(r, r), a2 = pair_of(by_d, by_d), s2 = pair_of(shift, shift);
+    const uint64_t mu2 = pair_of(-mu, -mu), r2 = pair_of(r, r), a2 = pair_of(by_xh, by_xh), s2 = pair_of(shift, shift);
 #pragma unroll
     for (int k = 0; k < S / 2; ++k) {
         const uint64_t g = mul2(pair_of(dy[2 * k], dy[2 * k + 1]), pair_of(w[2 * k], w[2 * k + 1])), d = add2(pair_of(x[2 * k], x[2 * k + 1]), mu2);
-        split_pair(fma2(d, a2, fma2(g, r2, s2)), dx[2 * k], dx[2 * k + 1]);
+        split_pair(fma2(mul2(d, r2), a2, fma2(g, r2, s2)), dx[2 * k], dx[2 * k + 1]);
     }
 }
 
@@ -269,14 +270,14 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormParams p
         float s[2];
         close_sums(sums, s);
         row_sum<2>(s, share, room, turn);
-        const float by_d = -r * r * (s[1] * inv * r), shift = p.center ? -s[0] * inv * r : 0.0f;
+        const float by_xh = -r * (s[1] * inv * r), shift = p.center ? -s[0] * inv * r : 0.0f;
         T* out = reinterpret_cast<T*>(p.out) + t * p.ld_out;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             if (column<V>(n, 0, rank, share) >= p.width) break;
             float w[S], dx[S];
             load_params<P, V>(reinterpret_cast<const P*>(p.weight), n, p.width, rank, share, w);
-            form_slot<S>(x + n * S, dy + n * S, w, mu, r, by_d, shift, dx);
+            form_slot<S>(x + n * S, dy + n * S, w, mu, r, by_xh, shift, dx);
             store_slot<T, V>(out, n, p.width, rank, share, dx);
         }
     }
@@ -402,7 +403,7 @@ __global__ void __launch_bounds__(512, 1) norm_backward_ring_kernel(const RingPa
             const int64_t next = t + (int64_t)(q.stages - 1) * workers;
             if (next < p.tokens) bring(next, place >= 1 ? place - 1 : q.stages - 1);
         }
-        const float by_d = -r * r * (s[1] * inv * r), shift = p.center ? -s[0] * inv * r : 0.0f;
+        const float by_xh = -r * (s[1] * inv * r), shift = p.center ? -s[0] * inv * r : 0.0f;
         T* out = reinterpret_cast<T*>(p.out) + t * p.ld_out;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
@@ -411,7 +412,7 @@ __global__ void __launch_bounds__(512, 1) norm_backward_ring_kernel(const RingPa
             float w[V], x[V], dy[V], dx[V];
             load_params<P, V>(reinterpret_cast<const P*>(p.weight), n, p.width, rank, share, w);
             values(c, x, dy);
-            form_slot<V>(x, dy, w, mu, r, by_d, shift, dx);
+            form_slot<V>(x, dy, w, mu, r, by_xh, shift, dx);
             store_slot<T, V>(out, n, p.width, rank, share, dx);
         }
         if (++place == q.stages) { place = 0; parity ^= 1u; }
