@@ -187,7 +187,6 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t nS = (uint32_t)p.stages;
 
-    ahead_release();
     if (threadIdx.x == 0) {
         init_barriers(bars);
         prefetch_tmap(&maps.codes1); prefetch_tmap(&maps.dy1); prefetch_tmap(&maps.a); prefetch_tmap(&maps.b);
@@ -196,6 +195,7 @@ lora_factors_kernel(const __grid_constant__ LoraMaps maps, const FactorParams p)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    ahead_release();                                        // (behind the allocation: a block of the next kernel may take what is left only)
     ahead_wait();
     const uint32_t tmem = bars->tmem_base;                  // accumulators at columns 0 and 128, expanded codes of stage s at 256 + 64 s
 
@@ -557,7 +557,6 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t nS = (uint32_t)p.stages;
 
-    ahead_release();
     if (threadIdx.x == 0) {
         init_barriers(bars);
         prefetch_tmap(&maps.codes2); prefetch_tmap(&maps.dy2); prefetch_tmap(&maps.fac);
@@ -566,6 +565,7 @@ lora_outer_kernel(const __grid_constant__ LoraMaps maps, const __grid_constant__
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    ahead_release();                                        // (behind the allocation: a block of the next kernel may take what is left only)
     ahead_wait();
     const uint32_t tmem = bars->tmem_base;                  // accumulator of item n, sub-tile m: column (n & 1) * 256 + m * 128
 

@@ -43,7 +43,9 @@ int sm_count();   // SM count of the current device (cached)
 #ifdef __CUDACC__
 // Launches that may begin while the kernel before them in the stream still runs (programmatic dependent launch): a kernel launched
 // by launch_ahead calls ahead_wait() before it touches global memory, which returns when the kernels before it have ended and
-// their writes can be seen, and ahead_release() once it no longer minds the next one's blocks moving in. What it saves is the
+// their writes can be seen, and ahead_release() once it no longer minds the next one's blocks moving in: with tensor memory, once it
+// has it and every thread of the block knows, for a block that came in early keeps what it takes until this kernel has ended, and one
+// that still waited for tensor memory beside it would never end. What it saves is the
 // launch latency and the set-up (barriers, tensor memory, tensor maps) between dependent kernels: 2 to 3 us each.
 __device__ __forceinline__ void ahead_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void ahead_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
