@@ -329,6 +329,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 if (half == 1) {                             // the first products of P may begin when both halves of O are as they have to be
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&bars->p_ready[x][0]));
+                    __syncwarp();                            // (what follows in tensor memory is a whole warp's)
                 }
                 const float off = ref == -INFINITY ? 0.0f : ref;
                 const uint64_t off2 = pair_of(-off, -off);
@@ -370,6 +371,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 for (int c = 0; c < DB * 32; c += 32) {
                     if (half * (DB * 32) + c >= p.head_dim) break;
                     uint32_t o[32];
+                    __syncwarp();
                     tmem_ld_x32(o_addr + c, o);
                     tmem_wait_ld();
 #pragma unroll
@@ -392,6 +394,7 @@ attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 if (half * (DB * 32) + c >= p.head_dim) break;
                 uint32_t o[32];
                 float f[32];
+                __syncwarp();
                 tmem_ld_x32(o_addr + c, o);
                 tmem_wait_ld();
 #pragma unroll

@@ -43,6 +43,7 @@ __device__ __forceinline__ constexpr uint32_t quarter_column(int s) { return (ui
 __device__ __forceinline__ void put_sums(uint32_t taddr, float* dst)
 {
     uint32_t o[32];
+    __syncwarp();                                            // (a whole warp's load: lanes may come from stores that some of them did not make)
     tmem_ld_x32(taddr, o);
     tmem_wait_ld();
 #pragma unroll
@@ -457,6 +458,7 @@ attention_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             } else if (part * 32 < p.head_dim) {
                 uint32_t o[32];
                 float f[32];
+                __syncwarp();
                 tmem_ld_x32(tmem + lanes + 256 + part * 32, o);
                 tmem_wait_ld();
 #pragma unroll
@@ -853,6 +855,7 @@ attention_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             for (int c = (part & 1) * 32; c < p.head_dim; c += 64) {
                 uint32_t o[32];
                 float f[32];
+                __syncwarp();
                 tmem_ld_x32(tmem + lanes + 256 + (is_k ? 128 : 0) + c, o);
                 tmem_wait_ld();
 #pragma unroll

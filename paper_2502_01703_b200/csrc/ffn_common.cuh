@@ -37,6 +37,7 @@ __device__ __forceinline__ void unpack_row32(const uint4 (&w)[4], float (&v)[32]
 __device__ __forceinline__ void load_acc(uint32_t taddr, float (&v)[32])
 {
     uint32_t raw[32];
+    __syncwarp();                                            // (the load is a whole warp's; lanes may come from stores that some of them did not make)
     tmem_ld_x32(taddr, raw);
     tmem_wait_ld();
 #pragma unroll

@@ -43,3 +43,46 @@ def test_no_kernel_lets_the_next_one_in_before_it_has_its_tensor_memory(name, ke
     alloc = re.search(r"\btmem_alloc\(", body).start()
     barrier = body.index("__syncthreads();", alloc)
     assert body.count("ahead_release();") == 1 and body.index("ahead_release();") > barrier
+
+
+# ---- accesses by whole warps ---------------------------------------------------------------------------------------------
+
+ACCESS = re.compile(r"\btmem_(?:ld|st)_x\d+\(")
+TOGETHER = re.compile(r"__syncwarp\(\);|__(?:all|any|shfl_xor|shfl)_sync\(|__syncthreads\(\);|\btmem_(?:ld|st)_x\d+\(")      # a warp's lanes are together behind these
+APART = re.compile(r"lane == 0|lane <|\bcontinue;|>= feats|at < w\.t\.len|store_rows32\(|\bput\(|\bdst\[|nullptr\)")      # and may part at these
+LAYER = ["attention.cu", "attention_backward.cu", "ffn.cu", "ffn_few.cu", "ffn_common.cuh"]
+
+
+def _blocks(text):
+    """(start, end) of every braced block."""
+    stack, got = [], []
+    for i, c in enumerate(text):
+        if c == "{":
+            stack.append(i)
+        elif c == "}":
+            got.append((stack.pop(), i))
+    return got
+
+
+@pytest.mark.parametrize("name", LAYER)
+def test_lanes_are_together_at_every_access_to_tensor_memory(name):
+    """tcgen05.ld and tcgen05.st are instructions of a whole warp (.sync.aligned). Between a statement at which lanes may part (a store by some of them, an arrival by
+    one) and the next such access stands one that brings them together: in a function, behind its beginning; in a loop, inside the loop, for its last statements
+    come before its first."""
+    text = _source(name)
+    blocks = _blocks(text)
+    looked_at = 0
+    for m in ACCESS.finditer(text):
+        looked_at += 1
+        before, line = text[:m.start()], text[m.start():m.start() + 60]
+        together = [t.start() for t in TOGETHER.finditer(before)]
+        apart = [t.start() for t in APART.finditer(before)]
+        assert together and (not apart or max(together) > max(apart)), line
+        for lo, hi in blocks:
+            if not lo < m.start() < hi:
+                continue
+            head = before[max(before.rfind(c, 0, lo) for c in ";}") + 1:lo]
+            loop = re.search(r"for \(int c0? = [^;]*;[^;]*;[^;]*\)\s*$", before[:lo])
+            if (loop and APART.search(text[lo:hi])) or re.search(r"__device__ __forceinline__ void", head):
+                assert any(t > lo for t in together), line
+    assert looked_at or name in ("ffn.cu", "ffn_few.cu")      # (all of theirs are load_acc's)
