@@ -1,4 +1,5 @@
-"""Normalisation's backward pass where rows' spread is so small that the cube of 1 / spread leaves fp32's range."""
+"""Normalisation's backward pass where its rows are very many or very small: rings of rows that are filled many times over, and rows whose spread is so small
+that the cube of 1 / spread leaves fp32's range."""
 import pytest
 import torch
 
@@ -38,3 +39,31 @@ def test_rows_whose_spread_is_tiny(W, dtype, center):
     close(back["grad_weight"], (DY * xh).sum(dim=0), 2.0 ** -19 * (DY * xh).abs().sum(dim=0) + step * (DY * xh).sum(dim=0).abs())
     alone = B.qless_layer_norm_backward(dy, x, w, got["mean"], got["rstd"])
     assert torch.equal(alone["grad_x"], back["grad_x"])
+
+
+@pytest.mark.parametrize("dtype,pdtype", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float32, torch.float32), (torch.float32, torch.bfloat16)])
+@pytest.mark.parametrize("T,W", [(40000, 64), (20001, 512), (20000, 1032), (3001, 4112), (2999, 8192), (5003, 16384), (70003, 8)])
+def test_more_rows_than_a_ring_holds(T, W, dtype, pdtype):
+    """Values and statistics are small whole numbers and halves, so that the parameters' gradients are exact in fp32 whatever the order of the sums: a row that is
+    left out, taken twice, or overwritten before it is read shows."""
+    g = gen(T + W)
+    draw = lambda lo, hi, *s: torch.randint(lo, hi + 1, s, generator=g, device="cuda")  # noqa: E731
+    x, dy = draw(-2, 2, T, W).to(dtype), draw(-3, 3, T, W).to(dtype)
+    w = (draw(1, 4, W) * 0.5).to(pdtype)
+    mean, rstd = draw(-1, 1, T).float(), torch.exp2(draw(-1, 1, T).float())
+    for center in (True, False):
+        back = B.qless_layer_norm_backward(dy, x, w, mean if center else None, rstd, want_weight=True, want_bias=True)
+        DY, R = dy.double(), rstd.double()[:, None]
+        xh = (x.double() - (mean.double()[:, None] if center else 0.0)) * R
+        # sums of halves: at most 70003 x 18 x 2 < 2^24 halves
+        assert torch.equal(back["grad_weight"], (DY * xh).sum(dim=0).float().to(pdtype))
+        assert torch.equal(back["grad_bias"], DY.sum(dim=0).float().to(pdtype))
+        gw = DY * w.double()
+        m, a = gw.mean(dim=1, keepdim=True) if center else 0.0, (gw * xh).mean(dim=1, keepdim=True)
+        dx = R * (gw - m - xh * a)
+        # fp32: g, xh and their sums are exact; the two means and the three products of a value are off by less than 2^-21 of what they add
+        room = R * 2.0 ** -21 * (gw.abs() + abs(m) + (xh * a).abs())
+        close(back["grad_x"], dx, room + (HALF if dtype == torch.bfloat16 else 0.0) * dx.abs())
+        alone = B.qless_layer_norm_backward(dy, x, w, mean if center else None, rstd)
+        assert torch.equal(alone["grad_x"], back["grad_x"])
+    B.qless_check()
