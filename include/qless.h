@@ -470,6 +470,8 @@ qless_status qless_layer_norm_backward(const void* grad_out, int64_t ld_grad_out
  *   grad_k_j = scale sum_i ds_ij q_i,  grad_v_j = sum_i p_ij grad_out_i   (sums over i and the query heads of the group)
  * with p and ds rounded to bf16 in these products, fp32 sums, and one rounding of each result to bf16. <grad_out_i, out_i> is the first estimate of delta_i,
  * whose error (out is rounded) is found and taken out of all results.
+ * The same list of lengths gives an example the same bits wherever it lies and whatever the others hold; beside examples of other lengths its sums may be cut
+ * elsewhere, and then added in another order.
  * Requirements: tokens < 2^31, those of an example times heads / kv_heads at most 2^25; head_dim a multiple of 8, at most 128; heads a multiple of
  * kv_heads, heads <= 4096; scale finite and positive; tensors 16-byte aligned, their row strides multiples of 8. */
 size_t qless_attention_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads);

@@ -543,8 +543,9 @@ int32_t attn_pack(int32_t heads, int32_t kv_heads)
     return pack;
 }
 
-// Room for the pieces' sums, wherever some examples of so many tokens may want it: whether a tile is dealt out follows from the examples' lengths alone, and
-// so do the results' bits. (The backward pass leaves two sums of a row, and its longest loop is that over the query rows of a tile of keys.)
+// Room for the pieces' sums, wherever some examples of so many tokens may want it: whether tiles are dealt out, and in how large pieces, follows from the whole list
+// of the call's lengths, the head counts and the number of SMs, and so does the order of the sums: the same list gives the same bits wherever the examples lie and whatever
+// the others hold; beside other lengths an example's sums may be cut elsewhere. (The backward pass leaves two sums of a row, and its longest loop is that over the query rows of a tile of keys.)
 size_t attn::split_bytes(int64_t tokens, int32_t heads, int32_t kv_heads, bool backward)
 {
     const int32_t pack = attn_pack(heads, kv_heads);
