@@ -505,8 +505,18 @@ cudaError_t backward_of(const NormPlan& pl, const NormParams& p, cudaStream_t st
 {
     const dim3 grid((unsigned)pl.blocks), block((unsigned)pl.block);
     if (pl.block <= 256) return launch_ahead(norm_backward_kernel<T, P, V, SUMS, 256>, grid, block, 0, st, p);
-    if (pl.block <= 512) return launch_ahead(norm_backward_kernel<T, P, V, SUMS, 512>, grid, block, 0, st, p);
-    return launch_ahead(norm_backward_kernel<T, P, V, SUMS, 1024>, grid, block, 0, st, p);
+    if constexpr (V < 8)                                     // (vectors of bf16: 16384 values are 512 threads')
+        if (pl.block > 512) return launch_ahead(norm_backward_kernel<T, P, V, SUMS, 1024>, grid, block, 0, st, p);
+    return launch_ahead(norm_backward_kernel<T, P, V, SUMS, 512>, grid, block, 0, st, p);
+}
+
+// With the sums and without a ring: rows that are not whole vectors, and fp32 rows beyond 32 KiB, which have more than 512 threads. (Whole bf16 rows always take the ring.)
+template <typename T, typename P>
+cudaError_t sums_of(const NormPlan& pl, const NormParams& p, bool whole, cudaStream_t st)
+{
+    if constexpr (sizeof(T) == 4)
+        if (whole) return launch_ahead(norm_backward_kernel<T, P, 4, true, 1024>, dim3((unsigned)pl.blocks), dim3((unsigned)pl.block), 0, st, p);
+    return backward_of<T, P, 1, true>(pl, p, st);
 }
 
 template <typename T, typename P, int EIGHTS>
@@ -601,7 +611,7 @@ qless_status launch_norm_backward(const NormArgs& a, uint8_t* ws, unsigned int* 
           QLESS_BY_TYPES(QLESS_CALL);
 #undef QLESS_CALL
       } else if (sums) {
-#define QLESS_CALL(T, P) whole ? backward_of<T, P, Elem<T>::VEC, true>(pl, p, st) : backward_of<T, P, 1, true>(pl, p, st)
+#define QLESS_CALL(T, P) sums_of<T, P>(pl, p, whole, st)
           QLESS_BY_TYPES(QLESS_CALL);
 #undef QLESS_CALL
       } else {
