@@ -440,7 +440,7 @@ qless_status qless_lm_loss(const void* hidden, int64_t ld_hidden, const void* we
  *   out = (x - mean) rstd weight + bias
  * weight [width], bias [width] or NULL, of param_dtype; mean, rstd [tokens] fp32 (outputs, either may be NULL). center = 0 is the normalisation
  * by the root mean square. Statistics are fp32, from the values and not from their squares' sum; out is rounded once.
- * (The squares are fp32 numbers: a row's spread may be up to 1.8e19, and where eps = 0, from 4e-20 on its statistics have all their digits.)
+ * (The squares are fp32 numbers: a row's spread may be up to 1.8e19; with eps = 0 rstd is good to 2^-18 for spreads from 4e-20 on.)
  * qless_layer_norm_backward takes mean (center = 0: not read, may be NULL) and rstd as the forward call left them:
  *   g = grad_out weight;  xh = (x - mean) rstd;  grad_x = rstd (g - [center] mean_c(g) - xh mean_c(g xh))
  *   grad_weight = sum_t grad_out xh,  grad_bias = sum_t grad_out     [width] of param_dtype, NULL to skip

@@ -11,11 +11,11 @@
 //   warps 12-19   tile 1
 // Tensor memory: S (or P) and O of both tiles, 4 x 128 columns. Running maximum: O and the sum are rescaled only when the maximum has grown by
 // more than 2^8 since the reference was taken (e^(s - r) then stays below 2^8: neither fp32 sums nor bf16's relative rounding mind).
-// P is rounded to bf16 (2^-9 of each probability, independent of each other; the sum is that of the unrounded ones), O and the sums are fp32.
+// P is rounded to bf16 (at most 2^-8 of each probability, independent of each other; the sum is that of the unrounded ones), O and the sums are fp32.
 // Bound: 128 x 128 exponentials take the special-function units 1024 clocks, the two products of the same tile (head_dim 128) 1024 of the tensor core; what is
 // measured for a pair of tiles is 3.5 to 3.8 thousand clocks, of which a tile's own chain (scores, maxima, exponentials, its products) takes nearly all: two
-// 128-column tiles with their sums fill tensor memory, so the next scores of a tile wait for its P to be read. 1.13 PFLOP/s for two documents of
-// 16383 tokens (32 heads of 128), where the SMs run at 1.75 GHz; short examples pay for the first loads and the epilogue of their items.
+// 128-column tiles with their sums fill tensor memory, so the next scores of a tile wait for its P to be read. Two examples of 16383 tokens in all (32/8 heads of
+// 128): 1.05 ms as a single call (1.11 PFLOP/s), 1.2 ms in a long row of them (0.97); short examples pay for the first loads and the epilogue of their items.
 // Some of the exponentials on the fp32 units instead (a polynomial; from one pair in two to one in eight): no difference beyond 1 %.
 // One thread to a row (four warps to a tile): 170 us instead of 141 for 32 examples of 16381 tokens in all, the same for long documents.
 #include <algorithm>

@@ -10,7 +10,8 @@
 //
 // delta taken from the output as it was handed on, in bf16, would be off by up to 2^-8 of |do| |o|, and with rows that look at few keys (|o| near |v|, ds small)
 // that is more than all other roundings together: errors of 3e-3 to 4.4e-3 of the gradients' norm were seen where 2.4e-3 are due to bf16 operands and
-// results. But sum_j ds_ij = 0 when delta is exact, so the row sum of what is formed with the rough delta, rho_i = sum_j ds_ij (fp32, before rounding), is delta's
+// results (examples of some hundred tokens and more; where a few entries of ds make up a gradient, their roundings do not average: up to 3.4e-3, and as much with an exact
+// delta). But sum_j ds_ij = 0 when delta is exact, so the row sum of what is formed with the rough delta, rho_i = sum_j ds_ij (fp32, before rounding), is delta's
 // error: the dq kernel also sums kbar_i = sum_j p_ij k_j and returns scale (sum_j ds_ij k_j - rho_i kbar_i), and hands delta_i + rho_i to the other kernel.
 //
 // dq kernel, tensor memory: S, dp, dq, kbar: 4 x 128 columns; P and ds, rounded to bf16, replace S and dp. While the threads take exponentials of one tile
@@ -19,10 +20,10 @@
 // tensor memory, and dv, dk.
 // Sixteen warps do the arithmetic, each 32 rows by a quarter of the columns; warp 0 brings tiles by TMA, warp 1 issues products, warps 2 and 3 bring
 // lse and delta of the query rows (dk/dv kernel).
-// P and ds are rounded to bf16 (2^-9 of each, independent of each other); exponentials, differences and sums are fp32.
+// P and ds are rounded to bf16 (at most 2^-8 of each, independent of each other); exponentials, differences and sums are fp32.
 // Bound: 128 x 128 scores cost four products of 512 clocks (head_dim 128) and 1024 clocks of the special-function units in each kernel.
-// 32 examples of 16381 tokens in all, 32/8 heads of 128: 275 us (dq) and 193 us (dk, dv); one of 8191 tokens, 16/16 heads of 64: 345 and 300 us. Short examples wait for a
-// tile's own chain: tensor pipe 34 and 48 % busy.
+// 32 examples of 16381 tokens in all, 32/8 heads of 128: 281 us (dq) and 196 us (dk, dv); one of 8191 tokens, 16/16 heads of 64: 361 and 314 us. Short examples wait for a
+// tile's own chain: tensor pipe 34 and 48 % busy. (S, dp and the two sums fill tensor memory, so neither S nor dp has a second place; without kbar there would be one.)
 #include <algorithm>
 #include <type_traits>
 

@@ -10,8 +10,8 @@
 //   OUT        h Wd^T, dg Wg + du Wu (one contraction over both halves), dy^T h, and dg^T x with du^T x (two sets of tiles in one launch)
 // Operands are read as they lie in memory, along the contraction or across it; what a tile's box has behind a matrix's edge arrives as zeros.
 // Roundings to bf16: g, u where they are kept, h, dg, du (operands of the next product), and the results; every sum is fp32.
-// Bound: the tensor pipe, at the clock that the power cap leaves (1.5 to 1.6 GHz). 4095 tokens x 4096 x 11008: dg and du 305 us (its epilogue reads and writes five matrices), dx
-// 515 us (1.43 PFLOP/s). Few tokens are left to ffn_few.cu, where the weights' bytes bound.
+// Bound: the tensor pipe, at the clock that the power cap leaves (1.5 to 1.6 GHz). 4095 tokens x 4096 x 11008: dg and du 306 us (its epilogue reads and writes five matrices), dx
+// 537 us (1.38 PFLOP/s). Few tokens are left to ffn_few.cu, where the weights' bytes bound.
 #include <algorithm>
 
 #include "ffn_common.cuh"

@@ -7,7 +7,8 @@
     python -m paper_2502_01703_b200.run_case extract  --n 32 --tokens 16384 --width 2048 --vocab 32000 --rank 16 --d 1024 --bits 4
     python -m paper_2502_01703_b200.run_case layer    --n 32 --tokens 16384 --width 2048 --heads 16 --kv-heads 4 --inner 5632 --rank 16 --d 1024 --bits 4
 
-Prints the CUDA-event time per iteration of the library call (extract, layer: of each call).
+Prints the CUDA-event time per iteration of the library call (extract, layer: of each call; the products of layer's attention projections, forward and backward, are
+torch's and not among the printed times).
 """
 import argparse
 
