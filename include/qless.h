@@ -473,7 +473,8 @@ qless_status qless_layer_norm_backward(const void* grad_out, int64_t ld_grad_out
  * The same list of lengths gives an example the same bits wherever it lies and whatever the others hold; beside examples of other lengths its sums may be cut
  * elsewhere, and then added in another order.
  * Requirements: tokens < 2^31, those of an example times heads / kv_heads at most 2^25; head_dim a multiple of 8, at most 128; heads a multiple of
- * kv_heads, heads <= 4096; scale finite and positive; tensors 16-byte aligned, their row strides multiples of 8. */
+ * kv_heads, heads <= 4096; scale finite and positive; tensors 16-byte aligned, their row strides multiples of 8. Terms are summed before they are divided by their
+ * sum: |v| times 2^8 times an example's tokens has to stay below 2^127. */
 size_t qless_attention_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads);
 size_t qless_attention_backward_workspace(int64_t tokens, int64_t n, int32_t heads, int32_t kv_heads);
 

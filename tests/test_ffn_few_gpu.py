@@ -43,3 +43,52 @@ def test_shared_tiles(W, F, T, act):
     check_ffn_backward(full, dy, x, got["gate"], got["up"], wg, wu, wd, act)
     assert all(torch.equal(full[n], back[n]) for n in ("grad_x", "grad_gate", "grad_up"))
     B.qless_check()
+
+
+def one_pass(s, **kw):
+    got = B.qless_gated_ffn(s["x"], s["wg"], s["wu"], s["wd"], want_saved=True, **kw)
+    back = B.qless_gated_ffn_backward(s["dy"], s["x"], got["gate"], got["up"], s["wg"], s["wu"], s["wd"], want_weight=True, **kw)
+    return [*got.values(), *back.values()]
+
+
+def inputs(seed, T, W, F):
+    g = gen(seed)
+    rand = lambda *s: (torch.randn(s, generator=g, device="cuda") / 4).to(torch.bfloat16)  # noqa: E731
+    return dict(x=rand(T, W), dy=rand(T, W), wg=rand(F, W), wu=rand(F, W), wd=rand(W, F))
+
+
+def same(a, b):
+    return all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("T,W,F", [(5, 264, 5000), (61, 3000, 5000), (130, 2600, 264), (200, 256, 1000)])
+def test_in_a_long_row_on_streams_and_in_graphs(T, W, F):
+    s = [inputs(T + i, T, W, F) for i in range(2)]
+    want = [[t.clone() for t in one_pass(x)] for x in s]
+    for _ in range(200):
+        last = one_pass(s[0])
+    assert same(last, want[0])
+    graphs, outs, pool = [], [], None
+    for x in s:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, pool=pool):
+            outs.append(one_pass(x))
+        pool = pool or graph.pool()
+        graphs.append(graph)
+    for _ in range(3):
+        for graph, out, w in zip(graphs, outs, want):        # one behind the other: they share workspaces
+            graph.replay()
+            torch.cuda.synchronize()
+            assert same(out, w)
+    for k, t in inputs(T + 1, T, W, F).items():
+        s[0][k].copy_(t)
+    graphs[0].replay()                                       # new contents at the captured addresses
+    torch.cuda.synchronize()
+    assert same(outs[0], want[1])
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    got = [one_pass(s[1], stream=st) for _ in range(5) for st in streams]
+    torch.cuda.synchronize()
+    assert all(same(x, want[1]) for x in got)
+    B.qless_check()
